@@ -304,6 +304,98 @@ esspt_status esspt_set_profile_events(esspt_ctx* ctx, void* before, void* after)
 esspt_status esspt_mf_worker_objective_noalloc(esspt_ctx* ctx, int32_t version, float lambda, double* h_sq,
                                                double* h_pen);
 
+/* ---- Softmax over a catalogue: cross entropy and distillation ------------- */
+
+/* Rows H [n, D] score every row of a catalogue W [V, D] (item rows read by GET,
+ * a vocabulary's embeddings):
+ *     s_tv = b h_t . w_v,   lse_t = log sum_v exp s_tv,   p_tv = exp(s_tv - lse_t).
+ * The losses below compare p_t with a target q_t of one or few items, and give
+ * the gradients of sum_t weight_t loss_t:
+ *     dh_t = b weight_t (sum_v p_tv w_v - sum_k q_tk w_id(t,k))
+ *     dw_v = b sum_t weight_t (p_tv - q_tv) h_t
+ * The n x V scores are never kept: they are formed piece by piece, as often as
+ * they are needed (for up to ESSPT_SOFTMAX_FEW_ROWS rows one row of V scores each
+ * stays in the workspace, less than W itself).
+ *
+ * Values are fp32, bf16 or fp16, H, W and both gradients alike.  Products are
+ * exact to fp32 rounding for fp32 rows; sums, statistics, losses and weights are
+ * fp32; of 16-bit rows the p_tv that meet a tensor core are rounded to 16 bits.
+ * Results do not depend on the order in which the GPU runs its blocks. */
+typedef enum { ESSPT_F32 = 0, ESSPT_BF16 = 1, ESSPT_F16 = 2 } esspt_dtype;
+
+#define ESSPT_SOFTMAX_FEW_ROWS 8
+
+typedef struct {
+  int64_t max_rows;  /* most rows of H per call, 1..2^24 */
+  int64_t n_items;   /* V: rows of W, 1..2^30 */
+  int32_t width;     /* D: values per row, 1..512 */
+  int32_t dtype;     /* esspt_dtype of H, W and the gradients */
+  int32_t max_top;   /* most entries per row of a teacher's list, >= 1; max_rows * max_top < 2^31 */
+  int32_t backward;  /* 1 = calls may ask for gradients */
+  void* stream;      /* cudaStream_t; NULL = legacy default stream */
+} esspt_softmax_config;
+
+typedef struct esspt_softmax esspt_softmax;
+
+/* Bytes of device workspace a handle needs.  0 on invalid config. */
+size_t esspt_softmax_workspace_bytes(const esspt_softmax_config* cfg);
+
+/* Create a handle over caller-allocated device workspace (256-byte aligned,
+ * `bytes` >= esspt_softmax_workspace_bytes(cfg), kept until
+ * esspt_softmax_destroy()).  Nothing in it outlives a call but the status word.
+ * ESSPT_EINVAL on a bad config, ESSPT_ENOSPC on a short workspace. */
+esspt_status esspt_softmax_create(const esspt_softmax_config* cfg, void* d_workspace, size_t bytes,
+                                  esspt_softmax** out);
+
+/* Release the host-side handle (not the workspace).  Synchronises the stream
+ * first.  NULL is accepted. */
+esspt_status esspt_softmax_destroy(esspt_softmax* sm);
+
+/* Softmax cross entropy: q_t is one at item d_targets[t], so
+ *     loss_t = lse_t - s_{t, target}.
+ *   d_h, d_w   device, rows h_stride and w_stride values apart (>= D; any
+ *              alignment of the type itself; 16-byte rows are the fast ones);
+ *   n          rows, 0..max_rows (0: only d_grad_w is written, with zeros);
+ *   d_targets  device int32[n]; a negative target marks an ignored row: its
+ *              loss, lse and dh are 0, it adds nothing to dw, and its h is not
+ *              used.  A target >= V does the same and is reported as ESSPT_EINVAL
+ *              by esspt_softmax_poll();
+ *   d_weight   device fp32[n], any sign, or NULL for 1;
+ *   inv_temperature  b, > 0 and finite;
+ *   d_loss, d_lse    device fp32[n], unweighted;
+ *   d_grad_h   device [n, D] rows of the handle's type, rows D apart, or NULL;
+ *   d_grad_w   device [V, D], likewise; both or neither.  They overwrite, and may
+ *              not overlap the inputs.
+ * Asynchronous on the handle's stream.  An infinity or NaN in W, in a row of H
+ * that is not ignored, in its weight, or a score that overflows fp32 gives NaN
+ * where the formula does. */
+esspt_status esspt_softmax_loss(esspt_softmax* sm, const void* d_h, int64_t h_stride, const void* d_w,
+                                int64_t w_stride, const int32_t* d_targets, int64_t n, const float* d_weight,
+                                float inv_temperature, float* d_loss, float* d_lse, void* d_grad_h, void* d_grad_w);
+
+/* Distillation from a teacher's top logits: row t of d_ids (device int32[n, top])
+ * lists items with the teacher's logits d_logits (device fp32[n, top]);
+ *     q_tk = softmax_k(b logit_tk) over the row's entries,
+ *     loss_t = sum_k q_tk log(q_tk / p_{t, id(t,k)}),
+ * the divergence from the teacher's list, renormalised, to the whole softmax.
+ * An id < 0 marks an absent entry (lists may be ragged, in any order), an id >= V
+ * one that is absent too and is reported by esspt_softmax_poll(); a logit of
+ * -infinity has q = 0.  A row left without an entry of positive q is ignored as
+ * above.  An item named twice in a row has the sum of both shares in q_tv, and two
+ * terms in the loss.  1 <= top <= max_top; the other arguments as above. */
+esspt_status esspt_softmax_distill(esspt_softmax* sm, const void* d_h, int64_t h_stride, const void* d_w,
+                                   int64_t w_stride, const int32_t* d_ids, const float* d_logits, int32_t top,
+                                   int64_t n, const float* d_weight, float inv_temperature, float* d_loss,
+                                   float* d_lse, void* d_grad_h, void* d_grad_w);
+
+/* Synchronise the stream and report, then clear, any error latched on the device
+ * (ESSPT_EINVAL: a target or id >= V). */
+esspt_status esspt_softmax_poll(esspt_softmax* sm);
+
+/* Text of the last error on this handle ("" if none), valid until the next call
+ * on it.  NULL gives the last esspt_softmax_create() error. */
+const char* esspt_softmax_last_error(const esspt_softmax* sm);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,179 @@
+// C-ABI of the softmax operators: handle, argument checks, workspace.
+#include <cmath>
+#include <new>
+#include <string>
+
+#include "softmax.h"
+
+using namespace esspt;
+
+struct esspt_softmax {
+  esspt_softmax_config cfg{};
+  cudaStream_t st = nullptr;
+  char* base = nullptr;
+  int sms = 0;
+  char err[256] = "";
+};
+
+namespace {
+
+thread_local char g_create_err[256] = "";
+
+esspt_status fail(esspt_softmax* sm, esspt_status code, const char* msg) {
+  snprintf(sm ? sm->err : g_create_err, 256, "%s", msg);
+  return code;
+}
+esspt_status cuda_fail(esspt_softmax* sm, cudaError_t e, const char* where) {
+  snprintf(sm ? sm->err : g_create_err, 256, "%s: %s", where, cudaGetErrorString(e));
+  return ESSPT_ECUDA;
+}
+
+#define SOFTMAX_CUDA(sm, call)                                   \
+  do {                                                           \
+    cudaError_t e_ = (call);                                     \
+    if (e_ != cudaSuccess) return cuda_fail((sm), e_, #call);    \
+  } while (0)
+
+const char* config_fault(const esspt_softmax_config* c) {
+  if (!c) return "null config";
+  if (c->max_rows < 1 || c->max_rows > (1 << 24)) return "max_rows must be in [1, 2^24]";
+  if (c->n_items < 1 || c->n_items > (1 << 30)) return "n_items must be in [1, 2^30]";
+  if (c->width < 1 || c->width > 512) return "width must be in [1, 512]";
+  if (c->dtype < ESSPT_F32 || c->dtype > ESSPT_F16) return "unknown dtype";
+  if (c->max_top < 1 || c->max_rows * c->max_top >= (int64_t)INT32_MAX)
+    return "max_top must be >= 1 and max_rows * max_top < 2^31";
+  return nullptr;
+}
+
+struct Carve {
+  size_t status, q, self, scores, part, stat, dh, dw, total;
+};
+
+constexpr int kMaxSms = 256;  // what the workspace is sized for
+
+Carve carve(const esspt_softmax_config& c) {
+  Carve k{};
+  size_t o = 0;
+  auto take = [&o](size_t bytes) {
+    const size_t at = o;
+    o += (bytes + 255) & ~size_t(255);
+    return at;
+  };
+  const size_t n = (size_t)c.max_rows, V = (size_t)c.n_items, D = (size_t)c.width;
+  k.status = take(256);
+  k.q = take(n * c.max_top * sizeof(float));
+  k.self = take(n * sizeof(float));
+  k.scores = take(V * kFewRows * sizeof(float));
+  k.part = take((size_t)few_blocks(kMaxSms) * kFewRows * sizeof(float2));
+  k.stat = take(2 * kFewRows * sizeof(float));
+  k.dh = take(c.backward ? (size_t)few_blocks(kMaxSms) * kFewRows * D * sizeof(float) : 0);
+  k.dw = take(c.backward && c.max_rows > kFewRows ? V * D * sizeof(float) : 0);
+  k.total = o;
+  return k;
+}
+
+esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void* w, int64_t w_stride,
+                 const int32_t* ids, const float* logits, int32_t top, int64_t n, const float* weight, float b,
+                 float* loss, float* lse, void* grad_h, void* grad_w) {
+  const esspt_softmax_config& c = sm->cfg;
+  const size_t size = c.dtype == ESSPT_F32 ? 4 : 2;
+  auto off = [](const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; };
+  if (n < 0 || n > c.max_rows) return fail(sm, ESSPT_EINVAL, "n must be in [0, max_rows]");
+  if (top < 1 || top > c.max_top) return fail(sm, ESSPT_EINVAL, "top must be in [1, max_top]");
+  if (!(b > 0.f) || !std::isfinite(b)) return fail(sm, ESSPT_EINVAL, "inv_temperature must be positive and finite");
+  if (!w || (n > 0 && (!h || !ids || !loss || !lse))) return fail(sm, ESSPT_EINVAL, "null pointer");
+  if (h_stride < c.width || w_stride < c.width) return fail(sm, ESSPT_EINVAL, "a row stride is below the width");
+  if (!grad_w != !grad_h && n > 0) return fail(sm, ESSPT_EINVAL, "both gradients or neither");
+  if (grad_w && !c.backward) return fail(sm, ESSPT_EINVAL, "the handle was made without backward");
+  if (off(h, size) || off(w, size) || off(grad_h, size) || off(grad_w, size) || off(ids, 4) || off(logits, 4) ||
+      off(weight, 4) || off(loss, 4) || off(lse, 4))
+    return fail(sm, ESSPT_EINVAL, "a pointer is not aligned to its type");
+  if (n == 0) {
+    if (grad_w) SOFTMAX_CUDA(sm, cudaMemsetAsync(grad_w, 0, (size_t)c.n_items * c.width * size, sm->st));
+    return ESSPT_OK;
+  }
+  const Carve k = carve(c);
+  SoftmaxArgs a{};
+  a.h = h, a.w = w, a.h_stride = h_stride, a.w_stride = w_stride, a.n = n;
+  a.V = (int32_t)c.n_items, a.D = c.width, a.dtype = c.dtype;
+  a.target = TargetArgs{ids, logits, top, n, a.V, b, reinterpret_cast<float*>(sm->base + k.q),
+                        reinterpret_cast<float*>(sm->base + k.self), reinterpret_cast<uint32_t*>(sm->base + k.status)};
+  a.weight = weight, a.b = b, a.loss = loss, a.lse = lse, a.grad_h = grad_h, a.grad_w = grad_w;
+  a.st = sm->st, a.sms = sm->sms;
+  if (logits) SOFTMAX_CUDA(sm, launch_targets(a.target, a.st));
+  FewScratch s{reinterpret_cast<float*>(sm->base + k.scores), reinterpret_cast<float2*>(sm->base + k.part),
+               reinterpret_cast<float*>(sm->base + k.stat), reinterpret_cast<float*>(sm->base + k.dh),
+               reinterpret_cast<float*>(sm->base + k.dw)};
+  SOFTMAX_CUDA(sm, launch_few_rows(a, s));
+  return ESSPT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t esspt_softmax_workspace_bytes(const esspt_softmax_config* cfg) {
+  return config_fault(cfg) ? 0 : carve(*cfg).total;
+}
+
+esspt_status esspt_softmax_create(const esspt_softmax_config* cfg, void* d_workspace, size_t bytes,
+                                  esspt_softmax** out) {
+  if (const char* why = config_fault(cfg)) return fail(nullptr, ESSPT_EINVAL, why);
+  if (!out || !d_workspace || reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0)
+    return fail(nullptr, ESSPT_EINVAL, "null or misaligned pointer");
+  if (bytes < carve(*cfg).total) return fail(nullptr, ESSPT_ENOSPC, "workspace too small");
+  int dev = 0, sms = 0;
+  SOFTMAX_CUDA(nullptr, cudaGetDevice(&dev));
+  SOFTMAX_CUDA(nullptr, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  SOFTMAX_CUDA(nullptr, cudaMemsetAsync(d_workspace, 0, 256, static_cast<cudaStream_t>(cfg->stream)));
+  esspt_softmax* sm = new (std::nothrow) esspt_softmax;
+  if (!sm) return fail(nullptr, ESSPT_ENOSPC, "out of host memory");
+  sm->cfg = *cfg;
+  sm->st = static_cast<cudaStream_t>(cfg->stream);
+  sm->base = static_cast<char*>(d_workspace);
+  sm->sms = sms < kMaxSms ? sms : kMaxSms;
+  *out = sm;
+  return ESSPT_OK;
+}
+
+esspt_status esspt_softmax_destroy(esspt_softmax* sm) {
+  if (!sm) return ESSPT_OK;
+  const cudaError_t e = cudaStreamSynchronize(sm->st);
+  delete sm;
+  return e == cudaSuccess ? ESSPT_OK : cuda_fail(nullptr, e, "esspt_softmax_destroy");
+}
+
+esspt_status esspt_softmax_loss(esspt_softmax* sm, const void* d_h, int64_t h_stride, const void* d_w,
+                                int64_t w_stride, const int32_t* d_targets, int64_t n, const float* d_weight,
+                                float inv_temperature, float* d_loss, float* d_lse, void* d_grad_h, void* d_grad_w) {
+  if (!sm) return ESSPT_EINVAL;
+  sm->err[0] = 0;
+  return run(sm, d_h, h_stride, d_w, w_stride, d_targets, nullptr, 1, n, d_weight, inv_temperature, d_loss, d_lse,
+             d_grad_h, d_grad_w);
+}
+
+esspt_status esspt_softmax_distill(esspt_softmax* sm, const void* d_h, int64_t h_stride, const void* d_w,
+                                   int64_t w_stride, const int32_t* d_ids, const float* d_logits, int32_t top,
+                                   int64_t n, const float* d_weight, float inv_temperature, float* d_loss,
+                                   float* d_lse, void* d_grad_h, void* d_grad_w) {
+  if (!sm) return ESSPT_EINVAL;
+  sm->err[0] = 0;
+  if (!d_logits && n > 0) return fail(sm, ESSPT_EINVAL, "null pointer");
+  return run(sm, d_h, h_stride, d_w, w_stride, d_ids, d_logits, top, n, d_weight, inv_temperature, d_loss, d_lse,
+             d_grad_h, d_grad_w);
+}
+
+esspt_status esspt_softmax_poll(esspt_softmax* sm) {
+  if (!sm) return ESSPT_EINVAL;
+  sm->err[0] = 0;
+  uint32_t bits = 0;
+  SOFTMAX_CUDA(sm, cudaMemcpyAsync(&bits, sm->base, sizeof(bits), cudaMemcpyDeviceToHost, sm->st));
+  SOFTMAX_CUDA(sm, cudaStreamSynchronize(sm->st));
+  if (!bits) return ESSPT_OK;
+  SOFTMAX_CUDA(sm, cudaMemsetAsync(sm->base, 0, sizeof(bits), sm->st));
+  return fail(sm, ESSPT_EINVAL, "a target or item id is outside the catalogue");
+}
+
+const char* esspt_softmax_last_error(const esspt_softmax* sm) { return sm ? sm->err : g_create_err; }
+
+}  // extern "C"

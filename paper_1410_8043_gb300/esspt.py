@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -29,6 +30,8 @@ EXPORTS = (
     "esspt_mf_stage_minibatch", "esspt_mf_stage_bytes", "esspt_set_profile_events",
     "esspt_mf_worker_objective_noalloc",
     "esspt_mf_sequential_work_bytes", "esspt_mf_sgd_clock_sequential",
+    "esspt_softmax_workspace_bytes", "esspt_softmax_create", "esspt_softmax_destroy", "esspt_softmax_loss",
+    "esspt_softmax_distill", "esspt_softmax_poll", "esspt_softmax_last_error",
 )
 
 
@@ -36,6 +39,9 @@ class EssptError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
         self.status = status
+
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class Config(ctypes.Structure):
@@ -51,6 +57,18 @@ class Config(ctypes.Structure):
         ("seed", ctypes.c_uint64),
         ("stream", ctypes.c_void_p),
         ("vap_v0", ctypes.c_double),
+    ]
+
+
+class SoftmaxConfig(ctypes.Structure):
+    _fields_ = [
+        ("max_rows", ctypes.c_int64),
+        ("n_items", ctypes.c_int64),
+        ("width", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("max_top", ctypes.c_int32),
+        ("backward", ctypes.c_int32),
+        ("stream", ctypes.c_void_p),
     ]
 
 
@@ -92,6 +110,13 @@ def lib() -> ctypes.CDLL:
         "esspt_mf_stage_minibatch": (ctypes.c_int, [P, I32, P, P, P, P, P, SZ, P]),
         "esspt_set_profile_events": (ctypes.c_int, [P, P, P]),
         "esspt_mf_worker_objective_noalloc": (ctypes.c_int, [P, I32, ctypes.c_float, P, P]),
+        "esspt_softmax_workspace_bytes": (SZ, [P]),
+        "esspt_softmax_create": (ctypes.c_int, [P, P, SZ, P]),
+        "esspt_softmax_destroy": (ctypes.c_int, [P]),
+        "esspt_softmax_loss": (ctypes.c_int, [P, P, I64, P, I64, P, I64, P, ctypes.c_float, P, P, P, P]),
+        "esspt_softmax_distill": (ctypes.c_int, [P, P, I64, P, I64, P, P, I32, I64, P, ctypes.c_float, P, P, P, P]),
+        "esspt_softmax_poll": (ctypes.c_int, [P]),
+        "esspt_softmax_last_error": (ctypes.c_char_p, [P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -345,3 +370,156 @@ class Table:
         t.mf_load(data.i, data.j, data.D, mb, wp, w.n_users, w.F)
         t.table_init(np.concatenate([data.L0, data.R0]))
         return t
+
+
+class SoftmaxResult(NamedTuple):
+    """loss and lse, fp32[n]; the gradients are None after a forward pass."""
+
+    loss: torch.Tensor
+    lse: torch.Tensor
+    grad_h: torch.Tensor | None
+    grad_w: torch.Tensor | None
+
+
+class SoftmaxHead:
+    """Softmax over a catalogue of `n_items` rows (one `esspt_softmax` handle).
+
+    `loss` is cross entropy against one item per row, `distill` the divergence
+    from a teacher's top logits; both give the gradients of the weighted sum of
+    the rows' losses.  The n x n_items scores are never kept.  The workspace is
+    allocated here once.  Work runs on `stream` (default: the current one at
+    construction); a call from another current stream is ordered after the work
+    queued there, and that stream's later work after the call.
+    """
+
+    def __init__(self, max_rows: int, n_items: int, width: int, dtype=torch.float32, max_top: int = 1,
+                 backward: bool = True, device=None, stream=None):
+        self._h = None
+        if not torch.cuda.is_available():
+            raise RuntimeError("esspt needs a CUDA device")
+        L = self._lib = lib()
+        if dtype not in DTYPES:
+            raise EssptError(EINVAL, f"dtype must be one of {', '.join(str(d) for d in DTYPES)}")
+        device = torch.device(device if device is not None else "cuda")
+        self.device = device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self.max_rows, self.n_items, self.width, self.dtype = max_rows, n_items, width, dtype
+        self.max_top, self.backward = max_top, backward
+        cfg = SoftmaxConfig(max_rows, n_items, width, DTYPES[dtype], max_top, int(backward),
+                            ctypes.c_void_p(self.stream.cuda_stream))
+        nbytes = L.esspt_softmax_workspace_bytes(ctypes.byref(cfg))
+        if nbytes == 0:
+            raise EssptError(EINVAL, "invalid softmax configuration")
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            st = L.esspt_softmax_create(ctypes.byref(cfg), self.workspace.data_ptr(), nbytes, ctypes.byref(h))
+        if st != OK:
+            raise EssptError(st, L.esspt_softmax_last_error(None).decode())
+        self._h = h
+
+    def _check(self, st: int) -> None:
+        if st != OK:
+            raise EssptError(st, self._lib.esspt_softmax_last_error(self._h).decode())
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            self._lib.esspt_softmax_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _rows(self, x, n, name) -> torch.Tensor:
+        """`x` as rows that the library reads in place; another layout is copied."""
+        if not isinstance(x, torch.Tensor) or x.dtype is not self.dtype or x.device != self.device:
+            raise EssptError(EINVAL, f"{name} must be a {self.dtype} tensor on {self.device}")
+        if x.dim() != 2 or x.shape[1] != self.width or (n is not None and x.shape[0] != n):
+            raise EssptError(EINVAL, f"{name} has shape {tuple(x.shape)}, not ({n if n is not None else 'n'}, {self.width})")
+        if (x.stride(1) != 1 and self.width > 1) or (x.shape[0] > 1 and x.stride(0) < self.width):
+            x = x.contiguous()
+        return x
+
+    def _list(self, x, shape, dtype, name) -> torch.Tensor:
+        if not isinstance(x, torch.Tensor) or x.device != self.device or tuple(x.shape) != tuple(shape):
+            raise EssptError(EINVAL, f"{name} must be a tensor of shape {tuple(shape)} on {self.device}")
+        if x.dtype is not dtype or not x.is_contiguous():
+            if x.dtype.is_floating_point != dtype.is_floating_point:
+                raise EssptError(EINVAL, f"{name} must hold {dtype} values")
+            if x.dtype is torch.int64:  # ids past 32 bits stay outside the catalogue
+                x = x.clamp(-1, 2**31 - 1)
+            x = x.to(dtype).contiguous()
+        return x
+
+    def _out(self, x, shape, name) -> torch.Tensor:
+        if x is None:
+            return torch.empty(shape, dtype=self.dtype, device=self.device)
+        if x.dtype is not self.dtype or x.device != self.device or tuple(x.shape) != shape or not x.is_contiguous():
+            raise EssptError(EINVAL, f"{name} must be a contiguous {self.dtype} tensor of shape {shape} on {self.device}")
+        return x
+
+    def _run(self, h, w, ids, logits, weight, inv_temperature, backward, grad_h, grad_w) -> SoftmaxResult:
+        if backward is None:
+            backward = self.backward
+        h = self._rows(h, None, "h")
+        w = self._rows(w, self.n_items, "w")
+        n = h.shape[0]
+        if n > self.max_rows:
+            raise EssptError(EINVAL, f"{n} rows, more than max_rows = {self.max_rows}")
+        if weight is not None:
+            weight = self._list(weight, (n,), torch.float32, "weight")
+        loss = torch.empty(n, dtype=torch.float32, device=self.device)
+        lse = torch.empty(n, dtype=torch.float32, device=self.device)
+        if backward:
+            grad_h = self._out(grad_h, (n, self.width), "grad_h")
+            grad_w = self._out(grad_w, (self.n_items, self.width), "grad_w")
+        else:
+            grad_h = grad_w = None
+        cur = torch.cuda.current_stream(self.device)
+        elsewhere = cur.cuda_stream != self.stream.cuda_stream
+        if elsewhere:
+            self.stream.wait_stream(cur)
+        tail = (n, _ptr(weight), inv_temperature, loss.data_ptr(), lse.data_ptr(), _ptr(grad_h), _ptr(grad_w))
+        head = (self._h, h.data_ptr(), h.stride(0) if n > 1 else self.width, w.data_ptr(),
+                w.stride(0) if self.n_items > 1 else self.width)
+        with torch.cuda.device(self.device):
+            if logits is None:
+                st = self._lib.esspt_softmax_loss(*head, ids.data_ptr(), *tail)
+            else:
+                st = self._lib.esspt_softmax_distill(*head, ids.data_ptr(), logits.data_ptr(), ids.shape[1], *tail)
+        if elsewhere:
+            cur.wait_stream(self.stream)
+        if st != OK:
+            self._check(st)
+        return SoftmaxResult(loss, lse, grad_h, grad_w)
+
+    def loss(self, h, w, targets, weight=None, inv_temperature: float = 1.0, backward: bool | None = None, grad_h=None,
+             grad_w=None) -> SoftmaxResult:
+        """esspt_softmax_loss: rows h (n, width) against w (n_items, width), targets
+        int32 (n,), a negative one marking an ignored row; weight fp32 (n,).  Rows of h
+        and w may be strided.  backward defaults to the handle's."""
+        targets = self._list(targets, (h.shape[0],), torch.int32, "targets")
+        return self._run(h, w, targets, None, weight, inv_temperature, backward, grad_h, grad_w)
+
+    def distill(self, h, w, ids, logits, weight=None, inv_temperature: float = 1.0, backward: bool | None = None,
+                grad_h=None, grad_w=None) -> SoftmaxResult:
+        """esspt_softmax_distill: ids int32 and teacher logits fp32, both (n, top); an
+        id < 0 is an absent entry."""
+        if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+            raise EssptError(EINVAL, "ids must be a tensor of shape (n, top)")
+        ids = self._list(ids, (h.shape[0], ids.shape[1]), torch.int32, "ids")
+        logits = self._list(logits, tuple(ids.shape), torch.float32, "logits")
+        return self._run(h, w, ids, logits, weight, inv_temperature, backward, grad_h, grad_w)
+
+    def poll(self) -> None:
+        """esspt_softmax_poll: synchronise and raise on a target or id outside the catalogue."""
+        self._check(self._lib.esspt_softmax_poll(self._h))
