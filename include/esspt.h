@@ -326,7 +326,7 @@ typedef enum { ESSPT_F32 = 0, ESSPT_BF16 = 1, ESSPT_F16 = 2 } esspt_dtype;
 #define ESSPT_SOFTMAX_FEW_ROWS 8
 
 typedef struct {
-  int64_t max_rows;  /* most rows of H per call, 1..2^24 */
+  int64_t max_rows;  /* most rows of H per call, 1..2^20 */
   int64_t n_items;   /* V: rows of W, 1..2^30 */
   int32_t width;     /* D: values per row, 1..512 */
   int32_t dtype;     /* esspt_dtype of H, W and the gradients */

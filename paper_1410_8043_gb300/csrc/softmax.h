@@ -12,6 +12,7 @@ namespace esspt {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kErrTarget = 1u;  // a target or id >= V (status word)
+constexpr uint32_t kErrStuck = 2u;   // a wait inside a kernel ran out (never expected)
 constexpr int kFewRows = ESSPT_SOFTMAX_FEW_ROWS;
 
 // The target of every row: one item (ids[t], q = 1: logits is null), or a list.
@@ -41,17 +42,52 @@ struct SoftmaxArgs {
   int sms;
 };
 
-// Up to kFewRows rows at once, by scores kept in the workspace.
+// Up to kFewRows rows, and small problems of up to kSmallRows, by scores kept in the
+// workspace, in groups of kFewRows rows.
+constexpr int kSmallRows = 128;
 struct FewScratch {
-  float* scores;   // [V][kFewRows]
-  float2* part;    // [few_blocks][kFewRows] maximum and sum of a block's items
-  float* stat;     // [kFewRows][2] maximum of a row and 1 / sum
-  float* dh;       // [few_blocks][kFewRows][D]
-  float* dw;       // [V][D] running gradient, or null where one group is all
+  float* scores;   // [groups][V][kFewRows]
+  float2* part;    // [few_blocks or groups][kFewRows] maximum and sum of a block's items
+  float* stat;     // [rows][2] maximum of a row and 1 / sum
+  float* dh;       // [few_blocks or groups][kFewRows][D]
 };
 int few_blocks(int sms);
 
+// Many rows: operands in 16 KB units of 128 rows by 64 16-bit values (tensor.cuh);
+// fp32 values in two halves of 11 bits (x = hi + lo, both fp16, all of H and all of W
+// scaled by a power of two each), so that three products of halves give fp32's.
+struct ManyWords {  // (device) what a call's kernels tell each other
+  uint32_t max_h, max_w, max_weight;  // largest finite magnitude, as fp32 bits
+  int32_t rows;                       // rows that are not ignored
+};
+struct ManyScratch {
+  ManyWords* words;
+  int32_t *act, *pos;      // [n] the kept rows in order; a row's place among them, or -1
+  char *units_h, *units_w;
+  float *row_max, *row_sum;  // [n] statistics of the kept rows, in order
+  float4* col;               // [(n up to 128) / 2] the kept rows as columns of dw: see MmaArgs
+  float* score;              // [n * top] scores of the targets
+  float2* stat;              // partial statistics, see many_slots
+  float* out;                // partial gradients, see many_slots
+  uint32_t *key[2], *val[2]; // [n * top] entries by item
+  int32_t* tile_first;       // [tiles of W + 1] first entry of a tile's items
+  float* run_sum[2];         // [n * top / kRun (^2) + 1][D] sums over whole runs of one item
+  void* sort_tmp;
+  size_t sort_bytes;
+};
+constexpr int kRun = 16;
+
+// Sizes of the above.
+struct ManySizes {
+  size_t units_h, units_w, stat, out, sort, run_sum[2];  // bytes
+};
+ManySizes many_sizes(int64_t rows, int64_t V, int32_t D, int32_t dtype, int64_t top, bool backward, int sms);
+cudaError_t launch_many_rows(const SoftmaxArgs& a, const ManyScratch& s);
+
 cudaError_t launch_targets(const TargetArgs& a, cudaStream_t st);
+// Whether a call of n rows goes by scores kept.
+bool few_rows(int64_t n, int64_t V, int32_t D, int32_t dtype);
+int few_groups(int64_t max_rows, int64_t V, int32_t D, int32_t dtype);  // most groups of such a call
 cudaError_t launch_few_rows(const SoftmaxArgs& a, const FewScratch& s);
 
 }  // namespace esspt

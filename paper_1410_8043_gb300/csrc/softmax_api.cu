@@ -7,10 +7,21 @@
 
 using namespace esspt;
 
+namespace {
+
+struct Carve {
+  size_t status, q, self, scores, part, stat, dh;
+  size_t words, act, pos, units_h, units_w, row_max, row_sum, score, col, slot_stat, out, key[2], val[2], tile_first, run_sum[2], sort;
+  size_t sort_bytes, total;
+};
+
+}  // namespace
+
 struct esspt_softmax {
   esspt_softmax_config cfg{};
   cudaStream_t st = nullptr;
   char* base = nullptr;
+  Carve k{};
   int sms = 0;
   char err[256] = "";
 };
@@ -36,7 +47,7 @@ esspt_status cuda_fail(esspt_softmax* sm, cudaError_t e, const char* where) {
 
 const char* config_fault(const esspt_softmax_config* c) {
   if (!c) return "null config";
-  if (c->max_rows < 1 || c->max_rows > (1 << 24)) return "max_rows must be in [1, 2^24]";
+  if (c->max_rows < 1 || c->max_rows > (1 << 20)) return "max_rows must be in [1, 2^20]";
   if (c->n_items < 1 || c->n_items > (1 << 30)) return "n_items must be in [1, 2^30]";
   if (c->width < 1 || c->width > 512) return "width must be in [1, 512]";
   if (c->dtype < ESSPT_F32 || c->dtype > ESSPT_F16) return "unknown dtype";
@@ -45,9 +56,6 @@ const char* config_fault(const esspt_softmax_config* c) {
   return nullptr;
 }
 
-struct Carve {
-  size_t status, q, self, scores, part, stat, dh, dw, total;
-};
 
 constexpr int kMaxSms = 256;  // what the workspace is sized for
 
@@ -63,11 +71,32 @@ Carve carve(const esspt_softmax_config& c) {
   k.status = take(256);
   k.q = take(n * c.max_top * sizeof(float));
   k.self = take(n * sizeof(float));
-  k.scores = take(V * kFewRows * sizeof(float));
-  k.part = take((size_t)few_blocks(kMaxSms) * kFewRows * sizeof(float2));
-  k.stat = take(2 * kFewRows * sizeof(float));
-  k.dh = take(c.backward ? (size_t)few_blocks(kMaxSms) * kFewRows * D * sizeof(float) : 0);
-  k.dw = take(c.backward && c.max_rows > kFewRows ? V * D * sizeof(float) : 0);
+  const size_t groups = (size_t)few_groups(c.max_rows, c.n_items, c.width, c.dtype);
+  const size_t few = groups > (size_t)few_blocks(kMaxSms) ? groups : (size_t)few_blocks(kMaxSms);
+  k.scores = take(groups * V * kFewRows * sizeof(float));
+  k.part = take(few * kFewRows * sizeof(float2));
+  k.stat = take(2 * groups * kFewRows * sizeof(float));
+  k.dh = take(c.backward ? few * kFewRows * D * sizeof(float) : 0);
+  if (c.max_rows > kFewRows) {
+    const ManySizes z = many_sizes(c.max_rows, c.n_items, c.width, c.dtype, c.max_top, c.backward != 0, kMaxSms);
+    const size_t back = c.backward ? 1 : 0, entries = back * n * c.max_top * sizeof(uint32_t);
+    k.words = take(sizeof(ManyWords));
+    k.act = take(n * sizeof(int32_t));
+    k.pos = take(n * sizeof(int32_t));
+    k.units_h = take(z.units_h);
+    k.units_w = take(z.units_w);
+    k.slot_stat = take(z.stat);
+    k.row_max = take(back * n * sizeof(float));
+    k.row_sum = take(back * n * sizeof(float));
+    k.score = take(entries);
+    k.col = take(back * (n + 128) * sizeof(float2));
+    k.out = take(z.out);
+    for (int i = 0; i < 2; ++i) k.key[i] = take(entries), k.val[i] = take(entries);
+    k.tile_first = take(back * ((V + 127) / 128 + 1) * sizeof(int32_t));
+    for (int i = 0; i < 2; ++i) k.run_sum[i] = take(z.run_sum[i]);
+    k.sort = take(z.sort);
+    k.sort_bytes = z.sort;
+  }
   k.total = o;
   return k;
 }
@@ -92,7 +121,7 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
     if (grad_w) SOFTMAX_CUDA(sm, cudaMemsetAsync(grad_w, 0, (size_t)c.n_items * c.width * size, sm->st));
     return ESSPT_OK;
   }
-  const Carve k = carve(c);
+  const Carve& k = sm->k;
   SoftmaxArgs a{};
   a.h = h, a.w = w, a.h_stride = h_stride, a.w_stride = w_stride, a.n = n;
   a.V = (int32_t)c.n_items, a.D = c.width, a.dtype = c.dtype;
@@ -101,10 +130,27 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   a.weight = weight, a.b = b, a.loss = loss, a.lse = lse, a.grad_h = grad_h, a.grad_w = grad_w;
   a.st = sm->st, a.sms = sm->sms;
   if (logits) SOFTMAX_CUDA(sm, launch_targets(a.target, a.st));
-  FewScratch s{reinterpret_cast<float*>(sm->base + k.scores), reinterpret_cast<float2*>(sm->base + k.part),
-               reinterpret_cast<float*>(sm->base + k.stat), reinterpret_cast<float*>(sm->base + k.dh),
-               reinterpret_cast<float*>(sm->base + k.dw)};
-  SOFTMAX_CUDA(sm, launch_few_rows(a, s));
+  auto at = [&](size_t offset) { return static_cast<void*>(sm->base + offset); };
+  if (few_rows(n, c.n_items, c.width, c.dtype)) {
+    const FewScratch s{static_cast<float*>(at(k.scores)), static_cast<float2*>(at(k.part)),
+                       static_cast<float*>(at(k.stat)), static_cast<float*>(at(k.dh))};
+    SOFTMAX_CUDA(sm, launch_few_rows(a, s));
+    return ESSPT_OK;
+  }
+  ManyScratch s{};
+  s.words = static_cast<ManyWords*>(at(k.words));
+  s.act = static_cast<int32_t*>(at(k.act)), s.pos = static_cast<int32_t*>(at(k.pos));
+  s.units_h = static_cast<char*>(at(k.units_h)), s.units_w = static_cast<char*>(at(k.units_w));
+  s.row_max = static_cast<float*>(at(k.row_max)), s.row_sum = static_cast<float*>(at(k.row_sum));
+  s.score = static_cast<float*>(at(k.score));
+  s.col = static_cast<float4*>(at(k.col)), s.stat = static_cast<float2*>(at(k.slot_stat));
+  s.out = static_cast<float*>(at(k.out));
+  for (int i = 0; i < 2; ++i)
+    s.key[i] = static_cast<uint32_t*>(at(k.key[i])), s.val[i] = static_cast<uint32_t*>(at(k.val[i]));
+  s.tile_first = static_cast<int32_t*>(at(k.tile_first));
+  for (int i = 0; i < 2; ++i) s.run_sum[i] = static_cast<float*>(at(k.run_sum[i]));
+  s.sort_tmp = at(k.sort), s.sort_bytes = k.sort_bytes;
+  SOFTMAX_CUDA(sm, launch_many_rows(a, s));
   return ESSPT_OK;
 }
 
@@ -131,6 +177,7 @@ esspt_status esspt_softmax_create(const esspt_softmax_config* cfg, void* d_works
   sm->cfg = *cfg;
   sm->st = static_cast<cudaStream_t>(cfg->stream);
   sm->base = static_cast<char*>(d_workspace);
+  sm->k = carve(*cfg);
   sm->sms = sms < kMaxSms ? sms : kMaxSms;
   *out = sm;
   return ESSPT_OK;
@@ -171,6 +218,7 @@ esspt_status esspt_softmax_poll(esspt_softmax* sm) {
   SOFTMAX_CUDA(sm, cudaStreamSynchronize(sm->st));
   if (!bits) return ESSPT_OK;
   SOFTMAX_CUDA(sm, cudaMemsetAsync(sm->base, 0, sizeof(bits), sm->st));
+  if (bits & kErrStuck) return fail(sm, ESSPT_ECUDA, "a wait inside a kernel ran out");
   return fail(sm, ESSPT_EINVAL, "a target or item id is outside the catalogue");
 }
 

@@ -1,5 +1,6 @@
-// Softmax operators for a few rows (single users, single tokens): one pass over
-// W gives the scores of up to kFewRows rows, a second one both gradients.
+// Softmax operators for a few rows (single users, single tokens) and for small
+// problems, where launches and latency count: the scores of groups of kFewRows rows
+// are kept, W is read once for them and once for dh.  All in fp32.
 #include <algorithm>
 
 #include "softmax.cuh"
@@ -61,10 +62,8 @@ __global__ void targets_kernel(TargetArgs a) {
 struct Few {
   SoftmaxArgs a;
   FewScratch s;
-  int64_t t0;  // first row of the group
-  int32_t rows;
-  int32_t blocks;
-  int first, last;  // of the call's groups
+  int32_t groups;  // of kFewRows rows
+  int32_t blocks;  // per group, of the kernel whose partial results are read
 };
 
 // Scores of all items: four lanes to an item (each a quarter of its slices of VEC
@@ -82,8 +81,8 @@ __global__ void __launch_bounds__(kThreads) few_scores_kernel(Few f) {
   const T* h = static_cast<const T*>(a.h);
   for (int i = threadIdx.x; i < slices * R * VEC; i += kThreads) {
     const int d = i / (R * VEC) * VEC + i % VEC, r = i / VEC % R;
-    const int64_t t = f.t0 + r;
-    hs[i] = r < f.rows && d < a.D && row_kept(a.target, t) ? to_float(h[t * a.h_stride + d]) : 0.f;
+    const int64_t t = (int64_t)blockIdx.y * R + r;
+    hs[i] = t < a.n && d < a.D && row_kept(a.target, t) ? to_float(h[t * a.h_stride + d]) : 0.f;
   }
   __syncthreads();
   const T* w = static_cast<const T*>(a.w);
@@ -138,7 +137,7 @@ __global__ void __launch_bounds__(kThreads) few_scores_kernel(Few f) {
       }
       const int64_t v = v0 + u * 8 + lane / 4;
       if (v < a.V) {
-        *reinterpret_cast<float2*>(f.s.scores + v * R + row0) = make_float2(s[0], s[1]);
+        *reinterpret_cast<float2*>(f.s.scores + ((int64_t)blockIdx.y * a.V + v) * R + row0) = make_float2(s[0], s[1]);
 #pragma unroll
         for (int r = 0; r < 2; ++r) merge_stat(m[r], l[r], s[r], 1.f);
       }
@@ -157,19 +156,19 @@ __global__ void __launch_bounds__(kThreads) few_scores_kernel(Few f) {
   if (threadIdx.x < R) {
     float2 t = warp_part[0][threadIdx.x];
     for (int i = 1; i < kThreads / 32; ++i) merge_stat(t.x, t.y, warp_part[i][threadIdx.x].x, warp_part[i][threadIdx.x].y);
-    f.s.part[blockIdx.x * R + threadIdx.x] = t;
+    f.s.part[(blockIdx.y * gridDim.x + blockIdx.x) * R + threadIdx.x] = t;
   }
 }
 
 // One warp per row: its maximum and sum over the blocks, its loss.
 __global__ void few_stat_kernel(Few f) {
   const SoftmaxArgs& a = f.a;
-  const int r = blockIdx.x, lane = threadIdx.x;
-  const int64_t t = f.t0 + r;
+  const int group = blockIdx.x / kFewRows, r = blockIdx.x % kFewRows, lane = threadIdx.x;
+  const int64_t t = blockIdx.x;
   const bool kept = row_kept(a.target, t);
   float m = -INFINITY, l = 0.f;
   for (int i = lane; i < f.blocks; i += 32) {
-    const float2 p = f.s.part[i * kFewRows + r];
+    const float2 p = f.s.part[(group * f.blocks + i) * kFewRows + r];
     merge_stat(m, l, p.x, p.y);
   }
 #pragma unroll
@@ -183,7 +182,7 @@ __global__ void few_stat_kernel(Few f) {
     const int32_t* ids = a.target.ids + t * a.target.top;
     for (int k = lane; k < a.target.top; k += 32) {
       const float q = a.target.logits ? a.target.q[t * a.target.top + k] : 1.f;
-      if (q != 0.f) loss2 += q * (lse2 - f.s.scores[(int64_t)ids[k] * kFewRows + r]);
+      if (q != 0.f) loss2 += q * (lse2 - f.s.scores[((int64_t)group * a.V + ids[k]) * kFewRows + r]);
     }
   }
   loss2 = warp_sum(loss2);
@@ -191,92 +190,118 @@ __global__ void few_stat_kernel(Few f) {
     if (!a.target.logits && a.target.ids[t] >= a.V) atomicOr(a.target.status, kErrTarget);
     a.loss[t] = kept ? loss2 * kLn2 + (a.target.logits ? a.target.self[t] : 0.f) : 0.f;
     a.lse[t] = kept ? lse2 * kLn2 : 0.f;
-    f.s.stat[2 * r] = m;
-    f.s.stat[2 * r + 1] = 1.f / l;
+    f.s.stat[2 * t] = m;
+    f.s.stat[2 * t + 1] = 1.f / l;
   }
 }
 
-// Both gradients, from the scores: a tile's coefficients g_vr = b weight_r (p_vr -
-// q_vr) go to shared memory, then each thread takes one slice of VEC columns of
-// every TY-th item: dw_v = sum_r g_vr h_r is written, dh_r += g_vr w_v summed in registers.
+// dw_v = sum_r g_vr h_r, with g_vr = b weight_r (p_vr - q_vr) taken from the scores of
+// a tile of items for all rows at once, and left in their place for dh.  Threads take
+// slices of VEC columns (tx of them at a time) of every ty-th item, four items deep.
 constexpr int kTile = 64;
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads, 2) few_grads_kernel(Few f, int tx) {
-  constexpr int R = kFewRows;
-  __shared__ __align__(16) float g[kTile][R];
-  __shared__ __align__(16) float red[kThreads * VEC];
-  __shared__ float bw[R], mx[R], inv[R];
-  __shared__ bool used[R];
+__global__ void __launch_bounds__(kThreads, 2) few_grad_w_kernel(Few f, int tx) {
+  constexpr int R = kFewRows, U = 4;
+  extern __shared__ __align__(16) float g[];  // [groups][kTile][R]
+  __shared__ float bw[kSmallRows], mx[kSmallRows], inv[kSmallRows];
+  __shared__ bool used[kSmallRows];
   const SoftmaxArgs& a = f.a;
-  const int ty_n = kThreads / tx, x = threadIdx.x % tx, y = threadIdx.x / tx;
-  const int col = (blockIdx.y * tx + x) * VEC;
-  const bool on = col < a.D;
-  if (threadIdx.x < R) {
-    const int r = threadIdx.x;
-    const int64_t t = f.t0 + r;
-    const bool kept = r < f.rows && row_kept(a.target, t);
-    used[r] = kept;
-    bw[r] = kept ? a.b * (a.weight ? a.weight[t] : 1.f) : 0.f;
-    mx[r] = f.s.stat[2 * r];
-    inv[r] = f.s.stat[2 * r + 1];
+  const int n = (int)a.n, ty_n = kThreads / tx, x = threadIdx.x % tx, y = threadIdx.x / tx, lane = threadIdx.x & 31;
+  for (int t = threadIdx.x; t < f.groups * R; t += kThreads) {
+    const bool kept = t < n && row_kept(a.target, t);
+    used[t] = kept;
+    bw[t] = kept ? a.b * (a.weight ? a.weight[t] : 1.f) : 0.f;
+    mx[t] = t < n ? f.s.stat[2 * t] : 0.f;
+    inv[t] = t < n ? f.s.stat[2 * t + 1] : 0.f;
   }
   __syncthreads();
-  float h[R][VEC], o[R][VEC];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) h[r][e] = o[r][e] = 0.f;
-    if (on && used[r]) load_vec<T, VEC>(static_cast<const T*>(a.h) + (f.t0 + r) * a.h_stride + col, h[r]);
-  }
-  const T* w = static_cast<const T*>(a.w);
   for (int64_t v0 = (int64_t)blockIdx.x * kTile; v0 < a.V; v0 += (int64_t)gridDim.x * kTile) {
     const int32_t items = (int32_t)min((int64_t)kTile, a.V - v0);
-    for (int i = threadIdx.x; i < items * R; i += kThreads) {
-      const int r = i % R;
-      g[i / R][r] = !used[r] ? 0.f : exp2f(f.s.scores[v0 * R + i] - mx[r]) * inv[r] * bw[r];
+    for (int i = threadIdx.x; i < f.groups * items * R; i += kThreads) {
+      const int group = i / (items * R), in = i - group * items * R, t = group * R + in % R;
+      const float s = f.s.scores[((int64_t)group * a.V + v0) * R + in];
+      g[group * kTile * R + in] = !used[t] ? 0.f : exp2f(s - mx[t]) * inv[t] * bw[t];
     }
     __syncthreads();
     // A warp per row takes its targets in this tile off, in the list's order where
     // two name one item.
-    for (int r = threadIdx.x / 32; r < f.rows; r += kThreads / 32) {
-      if (!used[r]) continue;
-      const int64_t t = f.t0 + r;
-      const int lane = threadIdx.x & 31;
+    for (int t = threadIdx.x / 32; t < n; t += kThreads / 32) {
+      if (!used[t]) continue;
       for (int k0 = 0; k0 < a.target.top; k0 += 32) {
         const int k = k0 + lane;
-        const int64_t at = k < a.target.top ? (int64_t)a.target.ids[t * a.target.top + k] - v0 : -1;
+        const int64_t e = (int64_t)t * a.target.top + k;
+        const int64_t at = k < a.target.top ? (int64_t)a.target.ids[e] - v0 : -1;
         const bool hit = at >= 0 && at < items;
-        const float q = !hit ? 0.f : a.target.logits ? a.target.q[t * a.target.top + k] : 1.f;
+        const float q = !hit ? 0.f : a.target.logits ? a.target.q[e] : 1.f;
         for (unsigned left = __ballot_sync(0xffffffffu, hit); left != 0u; left &= left - 1u) {
-          if (lane == __ffs(left) - 1) g[at][r] -= q * bw[r];
+          if (lane == __ffs(left) - 1) g[(t / R * kTile + at) * R + t % R] -= q * bw[t];
           __syncwarp();
         }
       }
     }
     __syncthreads();
-    if (on)
-      for (int i = y; i < items; i += ty_n) {
-        float x4[VEC], dw[VEC];
-        load_vec<T, VEC>(w + (v0 + i) * a.w_stride + col, x4);
-        const int64_t at = (v0 + i) * a.D + col;
+    for (int i = threadIdx.x; i < f.groups * items * R; i += kThreads) {
+      const int group = i / (items * R), in = i - group * items * R;
+      f.s.scores[((int64_t)group * a.V + v0) * R + in] = g[group * kTile * R + in];
+    }
+    for (int col = x * VEC; col < a.D; col += tx * VEC)
+      for (int i0 = y; i0 < items; i0 += ty_n * U) {
+        float dw[U][VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) dw[e] = f.first ? 0.f : f.s.dw[at + e];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const float c = g[i][r];
+          for (int e = 0; e < VEC; ++e) dw[u][e] = 0.f;
+        for (int t = 0; t < n; ++t) {
+          float h[VEC];
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            o[r][e] = fmaf(c, x4[e], o[r][e]);
-            dw[e] = fmaf(c, h[r][e], dw[e]);
+          for (int e = 0; e < VEC; ++e) h[e] = 0.f;
+          if (used[t]) load_vec<T, VEC>(static_cast<const T*>(a.h) + t * a.h_stride + col, h);
+          const float* c = g + (t / R * kTile + i0) * R + t % R;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const float cu = i0 + u * ty_n < items ? c[u * ty_n * R] : 0.f;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) dw[u][e] = fmaf(cu, h[e], dw[u][e]);
           }
         }
-        if (f.last)
-          store_vec<T, VEC>(static_cast<T*>(a.grad_w) + at, dw);
-        else
-          for (int e = 0; e < VEC; ++e) f.s.dw[at + e] = dw[e];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (i0 + u * ty_n < items)
+            store_vec<T, VEC>(static_cast<T*>(a.grad_w) + (v0 + i0 + u * ty_n) * a.D + col, dw[u]);
       }
     __syncthreads();
   }
+}
+
+// dh_r = sum_v g_vr w_v of a group of rows (blockIdx.z) by blocks, each over a part of
+// the items: threads as above, the rows' sums in registers.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kThreads, 2) few_grad_h_kernel(Few f, int tx) {
+  constexpr int R = kFewRows;
+  __shared__ __align__(16) float red[kThreads * VEC];
+  const SoftmaxArgs& a = f.a;
+  const int ty_n = kThreads / tx, x = threadIdx.x % tx, y = threadIdx.x / tx;
+  const int col = (blockIdx.y * tx + x) * VEC;
+  const bool on = col < a.D;
+  const float* g = f.s.scores + (int64_t)blockIdx.z * a.V * R;
+  const T* w = static_cast<const T*>(a.w) + col;
+  float o[R][VEC];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) o[r][e] = 0.f;
+  const int64_t end = a.V * (int64_t)(blockIdx.x + 1) / gridDim.x;
+  if (on)
+#pragma unroll 4
+    for (int64_t v = a.V * (int64_t)blockIdx.x / gridDim.x + y; v < end; v += ty_n) {
+      float k[VEC], c[R];
+      load_vec<T, VEC>(w + v * a.w_stride, k);
+      load_vec<float, R>(g + v * R, c);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[r][e] = fmaf(c[r], k[e], o[r][e]);
+    }
 #pragma unroll 1
   for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -291,21 +316,23 @@ __global__ void __launch_bounds__(kThreads, 2) few_grads_kernel(Few f, int tx) {
       for (int e = 0; e < VEC; ++e) {
         float sum = 0.f;
         for (int k = 0; k < ty_n; ++k) sum += red[(k * tx + x) * VEC + e];
-        f.s.dh[((int64_t)blockIdx.x * R + r) * a.D + col + e] = sum;
+        f.s.dh[((int64_t)(blockIdx.z * gridDim.x + blockIdx.x) * R + r) * a.D + col + e] = sum;
       }
     __syncthreads();
   }
 }
 
-// dh of the group: the blocks' sums in the order of the blocks.
+// dh: the blocks' sums in the order of the blocks.
 template <typename T>
-__global__ void few_finish_kernel(Few f, int blocks) {
-  const int r = blockIdx.y, d = blockIdx.x * blockDim.x + threadIdx.x;
+__global__ void few_finish_kernel(Few f) {
+  const int t = blockIdx.y, d = blockIdx.x * blockDim.x + threadIdx.x;
   if (d >= f.a.D) return;
+  const float* from = f.s.dh + ((int64_t)t / kFewRows * f.blocks * kFewRows + t % kFewRows) * f.a.D + d;
   float sum = 0.f;
 #pragma unroll 8
-  for (int i = 0; i < blocks; ++i) sum += f.s.dh[((int64_t)i * kFewRows + r) * f.a.D + d];
-  static_cast<T*>(f.a.grad_h)[(f.t0 + r) * f.a.D + d] = from_float<T>(sum);
+  for (int i = 0; i < f.blocks; ++i) sum += from[(int64_t)i * kFewRows * f.a.D];
+  const bool kept = row_kept(f.a.target, t);
+  static_cast<T*>(f.a.grad_h)[(int64_t)t * f.a.D + d] = from_float<T>(kept ? sum : 0.f);
 }
 
 // The widest vector of values that rows of W (and of the gradients, and H) can be read by.
@@ -319,16 +346,21 @@ int vector_of(const void* p, int64_t stride, int32_t D, int most) {
 template <typename T, int VEC>
 void scores(const Few& f) {
   const int32_t slices = (f.a.D + VEC - 1) / VEC;
-  few_scores_kernel<T, VEC><<<f.blocks, kThreads, sizeof(float) * slices * kFewRows * VEC, f.a.st>>>(f);
+  few_scores_kernel<T, VEC><<<dim3(f.blocks, f.groups), kThreads, sizeof(float) * slices * kFewRows * VEC, f.a.st>>>(f);
 }
 template <typename T, int VEC>
-int grads(const Few& f) {
+void grads(Few f) {
   const int32_t slices = (f.a.D + VEC - 1) / VEC;
   int tx = 1;
-  while (tx < slices && tx < kThreads) tx *= 2;
-  const int gx = (int)std::min<int64_t>(f.blocks, (f.a.V + kTile - 1) / kTile);
-  few_grads_kernel<T, VEC><<<dim3(gx, (slices + tx - 1) / tx), kThreads, 0, f.a.st>>>(f, tx);
-  return gx;
+  while (tx < slices && tx < 64) tx *= 2;
+  const int64_t tiles = ((int64_t)f.a.V + kTile - 1) / kTile;
+  const size_t smem = sizeof(float) * f.groups * kTile * kFewRows;
+  few_grad_w_kernel<T, VEC><<<(unsigned)std::min<int64_t>(tiles, 4 * f.a.sms), kThreads, smem, f.a.st>>>(f, tx);
+  // Blocks of a group: as many as fill the GPU, each with 16 items per thread at least.
+  const int64_t most = ((int64_t)f.a.V * tx + 16 * kThreads - 1) / (16 * kThreads);
+  f.blocks = (int)std::min<int64_t>(std::max(1, few_blocks(f.a.sms) / f.groups), most);
+  few_grad_h_kernel<T, VEC><<<dim3(f.blocks, (slices + tx - 1) / tx, f.groups), kThreads, 0, f.a.st>>>(f, tx);
+  few_finish_kernel<T><<<dim3((f.a.D + 127) / 128, (unsigned)f.a.n), 128, 0, f.a.st>>>(f);
 }
 
 template <typename T>
@@ -336,22 +368,29 @@ cudaError_t run(const SoftmaxArgs& a, const FewScratch& s) {
   constexpr int kWide = 16 / sizeof(T);
   const int vw = vector_of<T>(a.w, a.w_stride, a.D, kWide);
   const int vg = std::min(std::min(vw, 4), std::min(vector_of<T>(a.h, a.h_stride, a.D, 4), vector_of<T>(a.grad_w, a.D, a.D, 4)));
-  for (int64_t t0 = 0; t0 < a.n; t0 += kFewRows) {
-    Few f{a, s, t0, (int32_t)std::min<int64_t>(kFewRows, a.n - t0), few_blocks(a.sms), t0 == 0, t0 + kFewRows >= a.n};
-    if (vw == kWide) scores<T, kWide>(f);
-    else if (vw >= 4) scores<T, 4>(f);
-    else scores<T, 1>(f);
-    few_stat_kernel<<<f.rows, 32, 0, a.st>>>(f);
-    if (!a.grad_h) continue;
-    const int gx = vg == 4 ? grads<T, 4>(f) : grads<T, 1>(f);
-    few_finish_kernel<T><<<dim3((a.D + 127) / 128, f.rows), 128, 0, a.st>>>(f, gx);
-  }
+  Few f{a, s, (int32_t)((a.n + kFewRows - 1) / kFewRows), 0};
+  // A block takes 256 items at a time.
+  f.blocks = (int)std::min<int64_t>(std::max(1, few_blocks(a.sms) / f.groups), (a.V + kThreads - 1) / kThreads);
+  if (vw == kWide) scores<T, kWide>(f);
+  else if (vw >= 4) scores<T, 4>(f);
+  else scores<T, 1>(f);
+  few_stat_kernel<<<(unsigned)a.n, 32, 0, a.st>>>(f);
+  if (a.grad_h) vg == 4 ? grads<T, 4>(f) : grads<T, 1>(f);
   return cudaGetLastError();
 }
 
 }  // namespace
 
 int few_blocks(int sms) { return 2 * sms; }
+
+bool few_rows(int64_t n, int64_t V, int32_t D, int32_t dtype) {
+  return n <= kFewRows || (n <= kSmallRows && n * V * D <= 200'000'000);
+}
+int few_groups(int64_t max_rows, int64_t V, int32_t D, int32_t dtype) {
+  int64_t n = std::min<int64_t>(max_rows, kSmallRows);
+  while (!few_rows(n, V, D, dtype)) --n;
+  return (int)((n + kFewRows - 1) / kFewRows);
+}
 
 cudaError_t launch_targets(const TargetArgs& a, cudaStream_t st) {
   targets_kernel<<<(unsigned)((a.n + 7) / 8), 256, 0, st>>>(a);

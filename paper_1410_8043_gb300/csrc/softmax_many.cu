@@ -1,0 +1,551 @@
+// Softmax operators for many rows: operands laid out for the tensor cores, the
+// passes over tiles of scores, and what joins their partial results.
+//
+//   words      the kept rows in order, largest magnitudes
+//   units      H (kept rows) and W in 16 KB units, fp32 in two halves
+//   stats      maximum and sum of every row; losses
+//   rows       sum p w, then dh
+//   entries    targets sorted by item, sums over long runs of one item
+//   cols       sum weight p h, then dw
+#include <cub/device/device_radix_sort.cuh>
+
+#include <algorithm>
+
+#include "softmax_mma.cuh"
+
+namespace esspt {
+
+namespace {
+
+struct Many {
+  SoftmaxArgs a;
+  ManyScratch s;
+  MmaShape shape;
+  int blocks;  // of the pass whose slots are read
+  int ld;
+  int parts;
+};
+
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+  const uint32_t u = __float_as_uint(fabsf(x));
+  return u < 0x7f800000u ? u : 0u;
+}
+__device__ __forceinline__ void block_max(uint32_t x, uint32_t* to) {
+  x = __reduce_max_sync(0xffffffffu, x);
+  if ((threadIdx.x & 31) == 0 && x != 0u) atomicMax(to, x);
+}
+
+// Places of the kept rows.  A block counts the kept rows before its own 1024 first:
+// 16k rows take 8 such counts of 1k rows per block on average, a million 500.
+__global__ void __launch_bounds__(1024) compact_kernel(Many f) {
+  __shared__ int32_t sums[32];
+  const SoftmaxArgs& a = f.a;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t t0 = (int64_t)blockIdx.x * 1024, t = t0 + threadIdx.x;
+  int32_t before = 0;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < t0; i += 1024) before += row_kept(a.target, i);
+  before = __reduce_add_sync(0xffffffffu, before);
+  if (lane == 0) sums[warp] = before;
+  __syncthreads();
+  int32_t base = 0;
+  for (int i = 0; i < 32; ++i) base += sums[i];
+  __syncthreads();
+  const bool kept = t < a.n && row_kept(a.target, t);
+  const unsigned votes = __ballot_sync(0xffffffffu, kept);
+  if (lane == 0) sums[warp] = __popc(votes);
+  __syncthreads();
+  for (int i = 0; i < warp; ++i) base += sums[i];
+  base += __popc(votes & ((1u << lane) - 1u));
+  if (t < a.n) {
+    f.s.pos[t] = kept ? base : -1;
+    if (kept) f.s.act[base] = (int32_t)t;
+    if (!a.target.logits && a.target.ids[t] >= a.V) atomicOr(a.target.status, kErrTarget);
+    if (t == a.n - 1) f.s.words->rows = base + kept;
+  }
+  if (a.weight) block_max(kept ? finite_bits(a.weight[t]) : 0u, &f.s.words->max_weight);
+  else if (t == 0) f.s.words->max_weight = __float_as_uint(1.f);
+}
+
+// Largest finite magnitude of W, and of the kept rows of H (blockIdx.y = 1).
+template <int VEC>
+__global__ void __launch_bounds__(256) max_kernel(Many f) {
+  const SoftmaxArgs& a = f.a;
+  const bool is_h = blockIdx.y == 1;
+  const float* x = static_cast<const float*>(is_h ? a.h : a.w);
+  const int64_t rows = is_h ? f.s.words->rows : a.V, stride = is_h ? a.h_stride : a.w_stride;
+  const int32_t slices = a.D / VEC;
+  uint32_t top = 0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * slices; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / slices;
+    float v[VEC];
+    load_vec<float, VEC>(x + (is_h ? f.s.act[r] : r) * stride + (i - r * slices) * VEC, v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) top = max(top, finite_bits(v[e]));
+  }
+  block_max(top, is_h ? &f.s.words->max_h : &f.s.words->max_w);
+}
+
+// Rows to units: a thread makes 16 bytes (8 values) of a row.  The rows after the
+// last, up to the end of its tile, and the values after a row's last are zero.
+template <typename T, int PARTS, int VEC>
+__global__ void __launch_bounds__(256) units_kernel(Many f, bool is_h) {
+  const SoftmaxArgs& a = f.a;
+  const T* x = static_cast<const T*>(is_h ? a.h : a.w);
+  const int64_t rows = is_h ? f.s.words->rows : a.V, stride = is_h ? a.h_stride : a.w_stride;
+  char* units = is_h ? f.s.units_h : f.s.units_w;
+  const int32_t nk = f.shape.nk, pieces = nk * 8;
+  const int64_t total = (rows + 127) / 128 * 128 * pieces;
+  const int shift = PARTS == 2 ? half_shift_of(is_h ? f.s.words->max_h : f.s.words->max_w) : 0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / pieces;
+    const int32_t c = (int32_t)(i - r * pieces);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    if (r < rows) {
+      const T* from = x + (is_h ? f.s.act[r] : r) * stride + c * 8;
+#pragma unroll
+      for (int e = 0; e < 8; e += VEC)
+        if (c * 8 + e < a.D) {  // (VEC divides D)
+          float k[VEC];
+          load_vec<T, VEC>(from + e, k);
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) v[e + q] = k[q];
+        }
+    }
+    const int row = (int)(r & 127), piece = c & 7;
+    char* to = units + (((r >> 7) * PARTS * nk + (c >> 3)) * (int64_t)kUnitBytes) + row * 128 + ((piece ^ (row & 7)) << 4);
+    if constexpr (PARTS == 2) {
+      alignas(16) __half hi[8], lo[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float s = times_pow2(v[e], shift);
+        hi[e] = __float2half_rn(s);
+        lo[e] = __float2half_rn(s - __half2float(hi[e]));
+      }
+      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
+      *reinterpret_cast<uint4*>(to + nk * (int64_t)kUnitBytes) = *reinterpret_cast<const uint4*>(lo);
+    } else {
+      alignas(16) T out[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = from_float<T>(v[e]);
+      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(out);
+    }
+  }
+}
+
+// Column data of dw, two kept rows to a float4 (MmaArgs).
+__device__ __forceinline__ void set_col(const Many& f, int64_t pos, float m, float factor) {
+  float* c = reinterpret_cast<float*>(f.s.col + pos / 2) + (pos & 1);
+  c[0] = -m, c[2] = factor;
+}
+__device__ __forceinline__ float2 get_col(const Many& f, int64_t pos) {
+  const float* c = reinterpret_cast<const float*>(f.s.col + pos / 2) + (pos & 1);
+  return make_float2(-c[0], c[2]);
+}
+
+// A warp per row: its statistics from the partial ones, the scores of its targets
+// (8 lanes to an entry), its loss.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) loss_kernel(Many f) {
+  const SoftmaxArgs& a = f.a;
+  const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  const int lane = threadIdx.x & 31;
+  if (t >= a.n) return;
+  const int64_t pos = f.s.pos[t];
+  // Columns of dw past the last kept row: no term.
+  const int64_t rows = f.s.words->rows;
+  const int64_t padded = (rows + 127) / 128 * 128;
+  if (f.s.col && lane == 0 && t >= rows && t < padded) set_col(f, t, 1e30f, 0.f);
+  if (f.s.col && t == a.n - 1)
+    for (int64_t i = max(t + 1, rows) + lane; i < padded; i += 32) set_col(f, i, 1e30f, 0.f);
+  if (pos < 0) {
+    if (lane == 0) a.loss[t] = a.lse[t] = 0.f;
+    return;
+  }
+  const Ranges r(rows, a.V, f.shape.tiles, f.blocks);
+  const int64_t g = pos / (128 * f.shape.tiles);
+  const int tile = (int)(pos / 128 - g * f.shape.tiles), row = (int)(pos & 127);
+  const bool two = f.shape.tiles == 2 && (g * 2 + 1) * 128 < rows;  // half of the slot per tile, else all per row
+  const int64_t i0 = r.block_of(g * r.n_b), i1 = r.block_of((g + 1) * r.n_b - 1);
+  float m = -INFINITY, l = 0.f;
+  for (int64_t i = 4 * i0 + lane; i < 4 * i1 + 4; i += 32) {
+    const int part = (int)(i & 3);
+    if (two && part / 2 != tile) continue;
+    const float2 p = f.s.stat[((i / 4 + g) * 4 + part) * 128 + row];
+    merge_stat(m, l, p.x, p.y);
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, off), l2 = __shfl_xor_sync(0xffffffffu, l, off);
+    merge_stat(m, l, m2, l2);
+  }
+  const float lse2 = m + log2f(l), k2 = a.b * kLog2e;
+  const T* h = static_cast<const T*>(a.h) + t * a.h_stride;
+  const int32_t* ids = a.target.ids + t * a.target.top;
+  float loss2 = 0.f;
+  const int sub = lane & 7;
+  for (int k0 = 0; k0 < a.target.top; k0 += 32) {
+    // Entries by lane, so that no row's load waits for its id's.
+    const int count = min(32, a.target.top - k0);
+    const int64_t e = t * a.target.top + k0 + lane;
+    const int32_t lane_id = lane < count ? ids[k0 + lane] : -1;
+    const float lane_q = lane >= count ? 0.f : a.target.logits ? a.target.q[e] : 1.f;
+#pragma unroll 2
+    for (int i = 0; i < count; i += 4) {
+      const int32_t id = __shfl_sync(0xffffffffu, lane_id, (i + lane / 8) & 31);
+      const float q = __shfl_sync(0xffffffffu, lane_q, (i + lane / 8) & 31);
+      float s = 0.f;
+      if (q != 0.f) {
+        const T* w = static_cast<const T*>(a.w) + id * a.w_stride;
+#pragma unroll 2
+        for (int d = sub * VEC; d < a.D; d += 8 * VEC) {
+          float x[VEC], y[VEC];
+          load_vec<T, VEC>(h + d, x);
+          load_vec<T, VEC>(w + d, y);
+#pragma unroll
+          for (int c = 0; c < VEC; ++c) s = fmaf(x[c], y[c], s);
+        }
+      }
+#pragma unroll
+      for (int off = 4; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+      if (sub == 0 && q != 0.f) {
+        loss2 += q * (lse2 - s * k2);
+        if (f.s.col) f.s.score[t * a.target.top + k0 + i + lane / 8] = s * k2;
+      }
+    }
+  }
+  loss2 = warp_sum(loss2);
+  if (lane == 0) {
+    a.loss[t] = loss2 * kLn2 + (a.target.logits ? a.target.self[t] : 0.f);
+    a.lse[t] = lse2 * kLn2;
+    if (f.s.col) {
+      f.s.row_max[pos] = m;
+      f.s.row_sum[pos] = l;
+      const float weight = a.weight ? a.weight[t] : 1.f;
+      // fp16 probabilities: weight / 2^shift at most one, times 2^14
+      const float factor = a.dtype == ESSPT_BF16 ? weight
+                                                 : times_pow2(weight, (int)kHalfShift - weight_shift_of(f.s.words->max_weight));
+      set_col(f, pos, m, factor / l);
+    }
+  }
+}
+
+// Sum of a row of partial gradients over the slots of its group, columns d ...
+template <int VEC>
+__device__ __forceinline__ void add_slots(const Many& f, int64_t rows_a, int64_t rows_b, int64_t row, int d, float (&x)[VEC]) {
+  const Ranges r(rows_a, rows_b, f.shape.tiles, f.blocks);
+  const int64_t g = row / (128 * f.shape.tiles), in = row - g * 128 * f.shape.tiles;
+  const int64_t i0 = r.block_of(g * r.n_b), i1 = r.block_of((g + 1) * r.n_b - 1);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) x[e] = 0.f;
+  for (int64_t i = i0; i <= i1; ++i) {
+    float y[VEC];
+    load_vec<float, VEC>(f.s.out + ((i + g) * f.shape.tiles * 128 + in) * f.ld + d, y);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] += y[e];
+  }
+}
+
+// What rounding p to 16 bits took from the sum of a target's product.  Near a fit p - q
+// is small beside p, and that rounding would be most of it (p = 0.99, q = 1: 0.004 of
+// 0.01); other items' p are off by their own half-unit only.  (The score here and the
+// tensor core's differ in their last bits, so now and then p rounds the other way there.)
+template <typename T>
+__device__ __forceinline__ float rounded_off(float p) {
+  return sizeof(T) == 4 ? 0.f : p - to_float(from_float<T>(p));
+}
+
+// dh, a warp per row: b weight (sum p w / l - sum q w_id).
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
+  const SoftmaxArgs& a = f.a;
+  const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  if (t >= a.n) return;
+  const int64_t pos = f.s.pos[t];
+  T* to = static_cast<T*>(a.grad_h) + t * a.D;
+  const float bw = pos < 0 ? 0.f : a.b * (a.weight ? a.weight[t] : 1.f);
+  const float up = a.dtype == ESSPT_BF16 ? 0.f : kHalfShift;
+  const int shift = (f.parts == 2 ? half_shift_of(f.s.words->max_w) : 0) + (int)up;
+  const float inv = pos < 0 ? 0.f : 1.f / f.s.row_sum[pos], m = pos < 0 ? 0.f : f.s.row_max[pos];
+  const int lane = threadIdx.x & 31;
+  for (int d0 = 0; d0 < a.D; d0 += 32 * VEC) {
+    const int d = d0 + lane * VEC;
+    const bool on = d < a.D;
+    float x[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = 0.f;
+    if (pos >= 0) {
+      if (on) add_slots<VEC>(f, f.s.words->rows, a.V, pos, d, x);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[e] = ldexpf(x[e] * inv, -shift);
+      for (int k0 = 0; k0 < a.target.top; k0 += 32) {
+        const int count = min(32, a.target.top - k0);
+        const int64_t entry = t * a.target.top + k0 + lane;
+        const int32_t lane_id = lane < count ? a.target.ids[entry] : -1;
+        float c = lane >= count ? 0.f : a.target.logits ? -a.target.q[entry] : -1.f;
+        if (sizeof(T) == 2 && c != 0.f) c += ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - m + up)) * inv, -shift);
+        const unsigned share = __ballot_sync(0xffffffffu, c != 0.f);
+#pragma unroll 4
+        for (int i = 0; i < count; ++i) {
+          const float ci = __shfl_sync(0xffffffffu, c, i);
+          const int32_t id = __shfl_sync(0xffffffffu, lane_id, i);
+          if (!on || !(share >> i & 1u)) continue;
+          float y[VEC];
+          load_vec<T, VEC>(static_cast<const T*>(a.w) + id * a.w_stride + d, y);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x[e] = fmaf(ci, y[e], x[e]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[e] *= bw;
+    }
+    if (on) store_vec<T, VEC>(to + d, x);
+  }
+}
+
+// The targets as (item, entry) pairs; what has no share sorts behind the last item.
+__global__ void entries_kernel(Many f) {
+  const TargetArgs& a = f.a.target;
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= a.n * a.top) return;
+  const uint32_t id = (uint32_t)a.ids[i];
+  const bool share = id < (uint32_t)a.V && (!a.logits || a.q[i] != 0.f);
+  f.s.key[0][i] = share ? id : (uint32_t)a.V;
+  f.s.val[0][i] = (uint32_t)i;
+}
+
+// First entry of every tile of 128 items.
+__global__ void tile_first_kernel(Many f, const uint32_t* key) {
+  const int64_t tiles = ((int64_t)f.a.V + 127) / 128, i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i > tiles) return;
+  const uint32_t item = (uint32_t)min(i * 128, (int64_t)f.a.V);
+  int64_t lo = 0, hi = f.a.n * f.a.target.top;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (key[mid] < item) lo = mid + 1;
+    else hi = mid;
+  }
+  f.s.tile_first[i] = (int32_t)lo;
+}
+
+// The power of two by which the sums over columns are to be multiplied.
+__device__ __forceinline__ int cols_shift(const Many& f) {
+  return (f.parts == 2 ? -half_shift_of(f.s.words->max_h) : 0) +
+         (f.a.dtype == ESSPT_BF16 ? 0 : weight_shift_of(f.s.words->max_weight) - (int)kHalfShift);
+}
+
+// An entry's row of H, and weight q less what rounding took.
+template <typename T>
+__device__ __forceinline__ float entry_factor(const Many& f, int shift, uint32_t entry, int32_t& t) {
+  const SoftmaxArgs& a = f.a;
+  t = (int32_t)(entry / (uint32_t)a.target.top);
+  const float q = a.target.logits ? a.target.q[entry] : 1.f;
+  float g = a.weight ? q * a.weight[t] : q;
+  if (sizeof(T) == 2) {
+    const float2 c = get_col(f, f.s.pos[t]);
+    g -= ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - c.x) * c.y), shift);
+  }
+  return g;
+}
+// x += g h_t [d ...] over the first `count` lanes' entries, all lanes taking part.
+template <typename T, int VEC>
+__device__ __forceinline__ void add_rows(const SoftmaxArgs& a, int count, int32_t lane_t, float lane_g, int d, float (&x)[VEC]) {
+#pragma unroll 4
+  for (int i = 0; i < count; ++i) {
+    const float g = __shfl_sync(0xffffffffu, lane_g, i);
+    const int64_t t = __shfl_sync(0xffffffffu, lane_t, i);
+    if (d >= a.D) continue;
+    float y[VEC];
+    load_vec<T, VEC>(static_cast<const T*>(a.h) + t * a.h_stride + d, y);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = fmaf(g, y[e], x[e]);
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void add_sums(const float* sums, int32_t begin, int32_t end, int32_t D, int d, float (&x)[VEC]) {
+  if (d < D)
+#pragma unroll 4
+    for (int32_t i = begin; i < end; ++i) {
+      float y[VEC];
+      load_vec<float, VEC>(sums + (int64_t)i * D + d, y);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[e] += y[e];
+    }
+}
+
+// Sums over the runs of kRun entries (at multiples of kRun) that name one item, and of
+// kRun such runs (level 1), a warp each: no item of dw then adds more than 30 rows, 30
+// runs and what its entries make of runs of runs.
+template <typename T, int VEC, int LEVEL>
+__global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, const uint32_t* val) {
+  constexpr int kLong = LEVEL == 0 ? kRun : kRun * kRun;
+  const SoftmaxArgs& a = f.a;
+  const int64_t run = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, first = run * kLong;
+  const int lane = threadIdx.x & 31;
+  if (first + kLong > a.n * a.target.top) return;
+  if (key[first] != key[first + kLong - 1] || key[first] == (uint32_t)a.V) return;
+  int32_t t = 0;
+  float g = 0.f;
+  if (LEVEL == 0 && lane < kRun) g = entry_factor<T>(f, cols_shift(f), val[first + lane], t);
+  for (int d = lane * VEC; d - lane * VEC < a.D; d += 32 * VEC) {
+    float x[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = 0.f;
+    if (LEVEL == 0)
+      add_rows<T, VEC>(a, kRun, t, g, d, x);
+    else
+      add_sums<VEC>(f.s.run_sum[0], (int32_t)(run * kRun), (int32_t)(run * kRun + kRun), a.D, d, x);
+    if (d < a.D) store_vec<float, VEC>(f.s.run_sum[LEVEL] + run * a.D + d, x);
+  }
+}
+
+// dw, a warp per item: b (sum weight p h - sum weight q h).
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) grad_w_kernel(Many f, const uint32_t* key, const uint32_t* val) {
+  const SoftmaxArgs& a = f.a;
+  const int64_t v = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  const int lane = threadIdx.x & 31;
+  if (v >= a.V) return;
+  const int64_t rows = f.s.words->rows;
+  const int shift = cols_shift(f);
+  int32_t begin = f.s.tile_first[v / 128], end = f.s.tile_first[v / 128 + 1];
+  if (begin < end) {  // the item's own among the tile's
+    int32_t hi = end;
+    while (begin < hi) {
+      const int32_t mid = (begin + hi) / 2;
+      if (key[mid] < (uint32_t)v) begin = mid + 1;
+      else hi = mid;
+    }
+    for (hi = begin; hi < end;) {
+      const int32_t mid = (hi + end) / 2;
+      if (key[mid] <= (uint32_t)v) hi = mid + 1;
+      else end = mid;
+    }
+  }
+  // Whole runs [r0, r1), whole runs of runs [q0, q1), and single entries at both ends, one per lane.
+  int32_t r0 = (begin + kRun - 1) / kRun, r1 = end / kRun;
+  int32_t head = r0 * kRun - begin, tail = end - r1 * kRun;
+  if (r0 >= r1) r0 = r1 = 0, head = end - begin, tail = 0;
+  int32_t q0 = (r0 + kRun - 1) / kRun, q1 = r1 / kRun;
+  if (q0 >= q1) q0 = q1 = 0;
+  int32_t t = 0;
+  float g = 0.f;
+  if (lane < head + tail) g = entry_factor<T>(f, shift, val[lane < head ? begin + lane : end - tail + lane - head], t);
+  for (int d = lane * VEC; d - lane * VEC < a.D; d += 32 * VEC) {
+    float x[VEC], y[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = y[e] = 0.f;
+    if (rows > 0 && d < a.D) add_slots<VEC>(f, a.V, rows, v, d, x);
+    add_rows<T, VEC>(a, head + tail, t, g, d, y);
+    add_sums<VEC>(f.s.run_sum[0], r0, q0 < q1 ? q0 * kRun : r1, a.D, d, y);
+    add_sums<VEC>(f.s.run_sum[0], q0 < q1 ? q1 * kRun : r1, r1, a.D, d, y);
+    add_sums<VEC>(f.s.run_sum[1], q0, q1, a.D, d, y);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = a.b * (ldexpf(x[e], shift) - y[e]);
+    if (d < a.D) store_vec<T, VEC>(static_cast<T*>(a.grad_w) + v * a.D + d, x);
+  }
+}
+
+template <typename T>
+bool rows_by(int vec, const SoftmaxArgs& a, bool grads) {
+  auto ok = [&](const void* p, int64_t stride) { return stride % vec == 0 && reinterpret_cast<uintptr_t>(p) % (vec * sizeof(T)) == 0; };
+  return a.D % vec == 0 && ok(a.h, a.h_stride) && ok(a.w, a.w_stride) && (!grads || (ok(a.grad_h, a.D) && ok(a.grad_w, a.D)));
+}
+
+template <typename T, int PARTS, int VEC>
+void launch_units(const Many& f, bool is_h) {
+  const int64_t rows = is_h ? f.a.n : f.a.V, pieces = (rows + 127) / 128 * 128 * f.shape.nk * 8;
+  const int grid = (int)std::min<int64_t>((pieces + 255) / 256, 32ll * f.a.sms);
+  units_kernel<T, PARTS, VEC><<<grid, 256, 0, f.a.st>>>(f, is_h);
+}
+
+int bits_of(uint32_t most) {
+  int bits = 1;
+  while (bits < 32 && (most >> bits)) ++bits;
+  return bits;
+}
+
+template <typename T, int VEC>
+cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
+  constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  const bool grads = a.grad_h != nullptr;
+  const unsigned by_row = (unsigned)((a.n + 7) / 8);
+  Many f{a, s, mma_shape(Pass::kStats, a.D, kParts), a.sms, (a.D + 15) / 16 * 16, kParts};
+  if (!grads) f.s.col = nullptr;
+  cudaError_t e = cudaMemsetAsync(s.words, 0, sizeof(ManyWords), a.st);
+  if (e != cudaSuccess) return e;
+  compact_kernel<<<(unsigned)((a.n + 1023) / 1024), 1024, 0, a.st>>>(f);
+  if constexpr (kParts == 2) {
+    const int64_t work = std::max((int64_t)a.V, a.n) * a.D / VEC;
+    max_kernel<VEC><<<dim3((unsigned)std::min<int64_t>((work + 255) / 256, 8ll * a.sms), 2), 256, 0, a.st>>>(f);
+  }
+  launch_units<T, kParts, VEC>(f, true);
+  launch_units<T, kParts, VEC>(f, false);
+
+  MmaArgs m{};
+  m.A = s.units_h, m.B = s.units_w, m.s = f.shape, m.words = s.words, m.V = a.V, m.b = a.b;
+  m.row_max = s.row_max, m.col = s.col, m.stat = s.stat, m.out = s.out, m.ld = f.ld;
+  m.run = INT32_MAX, m.status = a.target.status;
+  if ((e = launch_mma(Pass::kStats, kBf16, kParts, m, a.sms, 1, a.st)) != cudaSuccess) return e;
+  loss_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
+  if (!grads) return cudaGetLastError();
+
+  // Tiles between additions in fp32.  4096 x 18k, K = 100, lists of 32: dh is 3.1e-6 off
+  // with 32 tiles, 1.6e-6 with 16, 8.5e-7 with 8 (7.5e-7 by fp32 products of whole
+  // matrices), 4.2e-7 with 4; the call takes 478, 484, 496 and 512 us.
+  const int out_chunks = (a.D + 255) / 256;
+  m.run = kParts == 2 ? 8 : 128;
+  m.s = f.shape = mma_shape(Pass::kRows, a.D, kParts);
+  if ((e = launch_mma(Pass::kRows, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
+  grad_h_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
+
+  const int64_t entries = a.n * a.target.top, tiles = ((int64_t)a.V + 127) / 128;
+  entries_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, a.st>>>(f);
+  cub::DoubleBuffer<uint32_t> key(s.key[0], s.key[1]), val(s.val[0], s.val[1]);
+  size_t bytes = s.sort_bytes;
+  if ((e = cub::DeviceRadixSort::SortPairs(s.sort_tmp, bytes, key, val, (int)entries, 0, bits_of((uint32_t)a.V), a.st)) !=
+      cudaSuccess)
+    return e;
+  tile_first_kernel<<<(unsigned)(tiles / 256 + 1), 256, 0, a.st>>>(f, key.Current());
+  if (entries >= kRun)
+    runs_kernel<T, VEC, 0><<<(unsigned)((entries / kRun + 7) / 8), 256, 0, a.st>>>(f, key.Current(), val.Current());
+  if (entries >= kRun * kRun)
+    runs_kernel<T, VEC, 1><<<(unsigned)((entries / kRun / kRun + 7) / 8), 256, 0, a.st>>>(f, key.Current(), val.Current());
+
+  m.A = s.units_w, m.B = s.units_h;
+  if ((e = launch_mma(Pass::kCols, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
+  grad_w_kernel<T, VEC><<<(unsigned)((a.V + 7) / 8), 256, 0, a.st>>>(f, key.Current(), val.Current());
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+ManySizes many_sizes(int64_t rows, int64_t V, int32_t D, int32_t dtype, int64_t top, bool backward, int sms) {
+  ManySizes z{};
+  const int parts = dtype == ESSPT_F32 ? 2 : 1;
+  const MmaShape stats = mma_shape(Pass::kStats, D, parts), grads = mma_shape(Pass::kRows, D, parts);
+  const int64_t tile_bytes = (int64_t)grads.nk * parts * kUnitBytes;
+  auto groups = [](int64_t n, int tiles) { return (n + 128 * tiles - 1) / (128 * tiles); };
+  z.units_h = (size_t)((rows + 127) / 128 * tile_bytes);
+  z.units_w = (size_t)((V + 127) / 128 * tile_bytes);
+  z.stat = (size_t)(groups(rows, stats.tiles) + sms) * 512 * sizeof(float2);
+  if (!backward) return z;
+  const int64_t slots = std::max(groups(rows, grads.tiles), groups(V, grads.tiles)) + sms;
+  z.out = (size_t)slots * grads.tiles * 128 * ((D + 15) / 16 * 16) * sizeof(float);
+  cub::DoubleBuffer<uint32_t> none(nullptr, nullptr);
+  cub::DeviceRadixSort::SortPairs(nullptr, z.sort, none, none, (int)(rows * top), 0, bits_of((uint32_t)V));
+  for (int i = 0, run = kRun; i < 2; ++i, run *= kRun) z.run_sum[i] = (size_t)(rows * top / run + 1) * D * sizeof(float);
+  return z;
+}
+
+cudaError_t launch_many_rows(const SoftmaxArgs& a, const ManyScratch& s) {
+  const bool grads = a.grad_h != nullptr;
+  if (a.dtype == ESSPT_BF16) return rows_by<__nv_bfloat16>(4, a, grads) ? run<__nv_bfloat16, 4>(a, s) : run<__nv_bfloat16, 1>(a, s);
+  if (a.dtype == ESSPT_F16) return rows_by<__half>(4, a, grads) ? run<__half, 4>(a, s) : run<__half, 1>(a, s);
+  return rows_by<float>(4, a, grads) ? run<float, 4>(a, s) : run<float, 1>(a, s);
+}
+
+}  // namespace esspt

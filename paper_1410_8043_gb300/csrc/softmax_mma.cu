@@ -1,0 +1,493 @@
+// The passes of the softmax operators over tiles of scores, on tensor cores.
+//
+// One block per SM holds one or two tiles (128 rows) of A and streams tiles of B.
+// One warp loads, one thread issues the matrix instructions, and two groups of eight
+// warps take the tiles of scores out of tensor memory by turns, half a row per thread.  For the
+// gradients the probabilities go back in place of their scores, in 16 bits, and are
+// the first operand of the second product, whose other operand is the tile of B that
+// gave the scores, read along its other dimension.  So the n x V scores and
+// probabilities exist only as tiles in tensor memory.
+//
+// fp32 (PARTS = 2): S = lo hi + hi lo + hi hi of the operands' halves, and the same
+// for p B.  Sums run over at most `run` tiles in the tensor core, whose additions
+// round worse than fp32's own, and are then added in fp32.
+#include "ptx.cuh"
+#include "softmax_mma.cuh"
+
+namespace esspt {
+
+namespace {
+
+struct Segment {  // consecutive tiles of B for one group
+  int64_t slot, group, first;
+  int32_t len;
+  bool add;  // an earlier segment of the block has the same slot
+};
+
+// The block's segments in order, the same for every warp.
+struct Walk {
+  Ranges r;
+  int64_t u, begin, end;
+  int run;
+  __device__ Walk(const Ranges& r_, int run_) : r(r_), run(run_) {
+    begin = u = blockIdx.x < r.blocks ? r.begin(blockIdx.x) : 0;
+    end = blockIdx.x < r.blocks ? r.begin(blockIdx.x + 1) : 0;
+  }
+  __device__ bool next(Segment& s) {
+    if (u >= end) return false;
+    s.group = u / r.n_b;
+    s.first = u - s.group * r.n_b;
+    s.slot = blockIdx.x + s.group;
+    s.len = (int32_t)min(min(r.n_b - s.first, end - u), (int64_t)run);
+    s.add = s.first != 0 && u != begin;
+    u += s.len;
+    return true;
+  }
+};
+
+struct Bars {  // shared addresses
+  uint32_t full, empty;             // [stages]
+  uint32_t a_full, a_empty;
+  uint32_t s_full, s_done;          // [4]: scores are there; scores read, or probabilities written
+  uint32_t o_full, o_empty;
+};
+constexpr int kBarBytes = 8 * (2 * kUnits + 2 + 8 + 2);
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  uint32_t r;
+  if (BF16)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// What the two halves of p leave of (lo, hi).
+__device__ __forceinline__ uint32_t pack16_rest(uint32_t p, float lo, float hi) {
+  const __half2 h = *reinterpret_cast<const __half2*>(&p);
+  const float2 f = __half22float2(h);
+  return pack16<false>(lo - f.x, hi - f.y);
+}
+
+template <Pass PASS, bool BF16, int PARTS>
+__global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ MmaArgs a) {
+  extern __shared__ __align__(1024) char smem[];
+  __shared__ uint32_t tmem_at;
+  __shared__ uint32_t dead_flag;
+  constexpr bool STATS = PASS == Pass::kStats;
+  constexpr int kBufs = STATS ? 4 : 2;  // score tiles in tensor memory
+  const MmaShape sh = a.s;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t rows_h = a.words->rows;
+  const int64_t rows_a = PASS == Pass::kCols ? a.V : rows_h, rows_b = PASS == Pass::kCols ? rows_h : a.V;
+  const Ranges ranges(rows_a, rows_b, sh.tiles, gridDim.x);
+  if (blockIdx.x >= ranges.blocks) return;
+
+  const uint32_t base = (smem_addr(smem) + 1023u) & ~1023u;
+  const uint32_t a_base = base, b_base = base + (sh.res ? sh.tiles * sh.nk * PARTS : 0) * kUnitBytes;
+  const uint32_t col_base = base + kUnits * kUnitBytes;  // [stages] of the columns' data
+  const uint32_t bar0 = col_base + kUnits * 1024;
+  Bars bar;
+  bar.full = bar0, bar.empty = bar.full + 8 * kUnits, bar.a_full = bar.empty + 8 * kUnits, bar.a_empty = bar.a_full + 8;
+  bar.s_full = bar.a_empty + 8, bar.s_done = bar.s_full + 32, bar.o_full = bar.s_done + 32, bar.o_empty = bar.o_full + 8;
+  volatile uint32_t* dead = &dead_flag;
+
+  if (threadIdx.x == 0) {
+    dead_flag = 0;
+    for (int i = 0; i < sh.stages; ++i) mbar_init(bar.full + 8 * i, 1), mbar_init(bar.empty + 8 * i, 1);
+    mbar_init(bar.a_full, 1), mbar_init(bar.a_empty, 1);
+    for (int i = 0; i < 4; ++i) mbar_init(bar.s_full + 8 * i, 1), mbar_init(bar.s_done + 8 * i, 8);
+    mbar_init(bar.o_full, 1), mbar_init(bar.o_empty, 16);
+    mbar_init_fence();
+  }
+  if (warp == 1) tmem_alloc(&tmem_at, 512);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = tmem_at;
+  const int out_unit = blockIdx.y * 4;  // first unit of the columns summed here
+  const int out_units = min(4, sh.nk - out_unit);
+  const int out_cols = min(256, sh.steps * 16 - (int)blockIdx.y * 256);
+  Walk walk(ranges, a.run);
+  Segment g;
+  // A group's last tile may lie outside: then the groups of warps share the first.
+  auto tiles_of = [&](const Segment& s) { return sh.tiles == 2 && (s.group * 2 + 1) * 128 < rows_a ? 2 : 1; };
+  const int64_t tile_bytes = (int64_t)sh.nk * PARTS * kUnitBytes;
+
+  if (warp == 0 && lane == 0) {
+    // ---- loads ----
+    uint32_t at = 0, a_phase = 1, segs = 0;  // stages so far
+    uint32_t tiles_b = 0;                    // tiles of B so far, which name their column data
+    bool ok = true;
+    auto unit = [&](const char* from, bool first_of_tile, int64_t tile) {
+      const uint32_t st = at % sh.stages;
+      ok = ok && mbar_wait(bar.empty + 8 * st, ((at / sh.stages) & 1) ^ 1, dead);
+      if (!ok) return;
+      const bool col = PASS == Pass::kCols && first_of_tile;
+      const uint32_t bytes = sh.stage_units * kUnitBytes;
+      mbar_expect(bar.full + 8 * st, bytes + (col ? 1024 : 0));
+      bulk_load(b_base + st * bytes, from, bytes, bar.full + 8 * st);
+      if (col) bulk_load(col_base + (tiles_b % sh.stages) * 1024, a.col + tile * 64, 1024, bar.full + 8 * st);
+      ++at;
+    };
+    auto scores_units = [&](int64_t tile, const char* from_a) {
+      const char* from = a.B + tile * tile_bytes;
+      if (sh.keep) {
+        unit(from, true, tile);
+      } else {
+        for (int kc = 0; kc < sh.nk && ok; ++kc) {
+          if (!sh.res)
+            for (int p = 0; p < PARTS && ok; ++p) unit(from_a + (p * sh.nk + kc) * (int64_t)kUnitBytes, false, 0);
+          for (int p = 0; p < PARTS && ok; ++p)
+            unit(from + (p * sh.nk + kc) * (int64_t)kUnitBytes, kc == 0 && p == 0, tile);
+        }
+      }
+      ++tiles_b;
+    };
+    auto sums_units = [&](int64_t tile) {
+      const char* from = a.B + tile * tile_bytes;
+      for (int kc = out_unit; kc < out_unit + out_units && ok; ++kc)
+        for (int p = 0; p < PARTS && ok; ++p) unit(from + (p * sh.nk + kc) * (int64_t)kUnitBytes, false, 0);
+    };
+    while (ok && walk.next(g)) {
+      const int nt = tiles_of(g);
+      const char* from_a = a.A + g.group * sh.tiles * tile_bytes;
+      if (sh.res) {
+        ok = mbar_wait(bar.a_empty, a_phase, dead);
+        if (!ok) break;
+        a_phase ^= 1;
+        ++segs;
+        mbar_expect(bar.a_full, (uint32_t)(nt * tile_bytes));
+        bulk_load(a_base, from_a, (uint32_t)(nt * tile_bytes), bar.a_full);
+      }
+      for (int32_t j = 0; j < g.len && ok; ++j) {
+        scores_units(g.first + j, from_a);
+        if (!STATS && !sh.keep && j > 0) sums_units(g.first + j - 1);
+      }
+      if (!STATS && !sh.keep && ok) sums_units(g.first + g.len - 1);
+    }
+    if (!ok) {  // copies in flight land before the block ends
+      for (uint32_t i = at > (uint32_t)sh.stages ? at - sh.stages : 0; i < at; ++i)
+        for (int k = 0; k < (1 << 16) && !mbar_try(bar.full + 8 * (i % sh.stages), (i / sh.stages) & 1); ++k) {
+        }
+      for (int k = 0; k < (1 << 16) && segs > 0 && !mbar_try(bar.a_full, (segs - 1) & 1); ++k) {
+      }
+    }
+  } else if (warp == 1 && lane == 0) {
+    // ---- matrix instructions ----
+    constexpr uint32_t idesc_s = mma_desc(BF16, 128, false);
+    const uint32_t idesc_o = mma_desc(BF16, out_cols, true);
+    uint32_t at = 0;          // stages taken for scores (and, without keep, for sums)
+    uint32_t at_sums = 0;     // keep: tiles taken for sums
+    uint32_t done_phase = STATS ? 0xfu : 0u;  // parity to wait for on s_done, a bit per buffer
+    uint32_t a_phase = 0, o_phase = 1;
+    bool ok = true;
+    auto stage_wait = [&](uint32_t& n) {  // shared address of the next stage
+      const uint32_t st = n % sh.stages;
+      ok = ok && mbar_wait(bar.full + 8 * st, (n / sh.stages) & 1, dead);
+      return b_base + st * sh.stage_units * kUnitBytes;
+    };
+    auto stage_free = [&](uint32_t n) { mma_commit(bar.empty + 8 * (n % sh.stages)); };
+    // Products of halves in the order of their size.
+    auto scores = [&](int32_t n, int nt) {
+      const int buf = n & (kBufs - 1), tile = nt == 2 ? n & 1 : 0;
+      const bool last = nt == 1 || tile == 1;  // of the tile of B
+      if (STATS) {
+        ok = ok && mbar_wait(bar.s_done + 8 * buf, (done_phase >> buf) & 1, dead);
+        done_phase ^= 1u << buf;
+        fence_after();
+      }
+      const uint32_t d = tmem + 128 * buf, a_at = a_base + tile * sh.nk * PARTS * kUnitBytes;
+      uint32_t add = 0;
+      auto products = [&](uint32_t ua, uint32_t ub, int kc) {
+        const int steps = min(4, sh.steps - 4 * kc);
+        for (int k = 0; k < steps; ++k, add = 1) mma_ss(d, desc_k(ua + 32 * k), desc_k(ub + 32 * k), idesc_s, add);
+      };
+      if (sh.keep) {
+        const uint32_t b_at = stage_wait(at);
+        if (!ok) return;
+        fence_after();
+#pragma unroll
+        for (int c = PARTS == 2 ? 0 : 2; c < 3; ++c) {  // (lo, hi), (hi, lo), (hi, hi)
+          const int pa = c == 0, pb = c == 1;
+          for (int kc = 0; kc < sh.nk; ++kc)
+            products(a_at + (pa * sh.nk + kc) * kUnitBytes, b_at + (pb * sh.nk + kc) * kUnitBytes, kc);
+        }
+        if (last && STATS) stage_free(at);
+        if (last) ++at;
+      } else {
+        for (int kc = 0; kc < sh.nk; ++kc) {
+          uint32_t ua[2], ub[2];
+          for (int p = 0; p < PARTS; ++p) ua[p] = a_at + (p * sh.nk + kc) * kUnitBytes;
+          const uint32_t first = at;
+          if (!sh.res)
+            for (int p = 0; p < PARTS; ++p, ++at) ua[p] = stage_wait(at);
+          for (int p = 0; p < PARTS; ++p, ++at) ub[p] = stage_wait(at);
+          if (!ok) return;
+          fence_after();
+          if (PARTS == 2) {
+            products(ua[1], ub[0], kc);
+            products(ua[0], ub[1], kc);
+          }
+          products(ua[0], ub[0], kc);
+          for (uint32_t i = first; i < at; ++i) stage_free(i);
+        }
+      }
+      mma_commit(bar.s_full + 8 * buf);
+    };
+    auto sums = [&](int32_t n, int nt, int32_t jobs) {
+      const int buf = n & 1, tile = nt == 2 ? n & 1 : 0;
+      ok = ok && mbar_wait(bar.s_done + 8 * buf, (done_phase >> buf) & 1, dead);
+      if (!ok) return;
+      done_phase ^= 1u << buf;
+      fence_after();
+      const uint32_t p_at = tmem + 128 * buf, d = tmem + 256 + 128 * tile;
+      const uint32_t first = n >= nt;  // the tile's first job of the segment overwrites
+      auto products = [&](int pp, uint32_t ub, uint32_t to, uint32_t idesc, uint32_t add) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          mma_ts(to, p_at + 32 * (k >> 1) + 8 * (k & 1) + 16 * pp, desc_mn(ub + 2048 * k), idesc, add | (k > 0));
+      };
+      if (sh.keep) {
+        const uint32_t st = at_sums % sh.stages, ub = b_base + st * sh.stage_units * kUnitBytes;
+        const uint32_t hi = ub + out_unit * kUnitBytes, lo = hi + sh.nk * kUnitBytes;
+        if (PARTS == 2) {
+          products(1, hi, d, idesc_o, first);
+          products(0, lo, d, idesc_o, 1);
+        }
+        products(0, hi, d, idesc_o, PARTS == 2 ? 1 : first);
+        if (nt == 1 || tile == 1) stage_free(at_sums++);
+      } else {
+        for (int kc = 0; kc < out_units; ++kc) {
+          const uint32_t to = d + 64 * kc, idesc = mma_desc(BF16, min(64, out_cols - 64 * kc), true);
+          for (int p = 0; p < PARTS; ++p) {
+            const uint32_t ub = stage_wait(at);
+            if (!ok) return;
+            fence_after();
+            if (PARTS == 2 && p == 0) products(1, ub, to, idesc, first);
+            products(0, ub, to, idesc, PARTS == 2 ? 1 : first);
+            stage_free(at++);
+          }
+        }
+      }
+      if (n == jobs - 1) mma_commit(bar.o_full);
+    };
+    while (ok && walk.next(g)) {
+      const int nt = tiles_of(g);
+      const int32_t jobs = nt * g.len;
+      if (sh.res) {
+        ok = mbar_wait(bar.a_full, a_phase, dead);
+        a_phase ^= 1;
+      }
+      for (int32_t n = 0; n < jobs && ok; ++n) {
+        scores(n, nt);
+        if (n == jobs - 1 && sh.res && ok) mma_commit(bar.a_empty);
+        if (STATS) continue;
+        if (n == 1 || jobs == 1) {
+          ok = ok && mbar_wait(bar.o_empty, o_phase, dead);
+          o_phase ^= 1;
+          fence_after();
+        }
+        if (n > 0 && ok) sums(n - 1, nt, jobs);
+      }
+      if (!STATS && ok) sums(jobs - 1, nt, jobs);
+    }
+    if (!ok) {  // what was issued ends before tensor memory is freed
+      mma_commit(bar.a_empty);
+      const long long begin = clock64();
+      while (clock64() - begin < 2'000'000) {
+      }
+    }
+  } else if (warp >= 4) {
+    // ---- exponentials ----
+    const int pair = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3;
+    const int row = quarter * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    const int shift_h = PARTS == 2 ? half_shift_of(a.words->max_h) : 0, shift_w = PARTS == 2 ? half_shift_of(a.words->max_w) : 0;
+    // (Kept off 0 and infinity: scores that far are 0 or overflow in any case, and
+    // masked ones stay -infinity.)
+    const float scale = fminf(fmaxf(ldexpf(a.b * kLog2e, -(shift_h + shift_w)), 1.1754944e-38f), 3.4028235e38f);
+    const u64 scale2 = pack2(scale, scale);
+    uint32_t phase = 0, o_phase = 0;  // parities of s_full, a bit per buffer
+    uint32_t tiles_b = 0;
+    bool ok = true;
+    while (ok && walk.next(g)) {
+      const int nt = tiles_of(g);
+      const int32_t jobs = nt * g.len;
+      float m = -INFINITY, l = 0.f, at = 0.f;  // kStats: maximum (without the scale), sum, and m scale
+      float offset = 0.f;
+      if (PASS == Pass::kRows) {
+        const int64_t r = (g.group * sh.tiles + (nt == 2 ? pair : 0)) * 128 + row;
+        offset = r < rows_a ? (BF16 ? 0.f : kHalfShift) - a.row_max[r] : -1e30f;
+      }
+      for (int32_t n = pair; n < jobs; n += 2) {
+        const int buf = n & (kBufs - 1);
+        const int32_t j = nt == 2 ? n >> 1 : n;
+        ok = mbar_wait(bar.s_full + 8 * buf, (phase >> buf) & 1, dead);
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
+        phase ^= 1u << buf;
+        fence_after();
+        const int64_t left = rows_b - (g.first + j) * 128 - 64 * half;  // of this half's columns
+        const uint32_t s_at = lanes + 128 * buf + 64 * half;
+        uint32_t r[2][32];
+        tmem_load32(r[0], s_at);
+        tmem_load32(r[1], s_at + 32);
+        tmem_loaded(r[0]);
+        tmem_loaded(r[1]);
+        if (STATS) {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar.s_done + 8 * buf);
+          if (left < 64) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (32 * c + i >= left) r[c][i] = 0xff800000u;
+          }
+          float top[4] = {m, m, m, m};
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; i += 2)
+              top[(i >> 1) & 3] = fmaxf(fmaxf(top[(i >> 1) & 3], __uint_as_float(r[c][i])), __uint_as_float(r[c][i + 1]));
+          const float m2 = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+          const float at2 = m2 == -INFINITY ? 0.f : m2 * scale;
+          const u64 minus = pack2(-at2, -at2);
+          u64 sum[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              float x, y;
+              unpack2(fma2(pack2(__uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1])), scale2, minus), x, y);
+              sum[(i >> 1) & 3] = add2(sum[(i >> 1) & 3], pack2(exp2_fast(x), exp2_fast(y)));
+            }
+          // (The same maximum again has to leave l as it is: a factor off by its rounding
+          // drifted by 7e-6 over 800 tiles.)
+          if (m2 != m) l = m == -INFINITY ? 0.f : l * exp2_fast(at - at2);
+          l += sum2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+          m = m2, at = at2;
+        } else {
+          const uint32_t col_at = col_base + ((tiles_b + j) % sh.stages) * 1024 + 512 * half;
+          const u64 offset2 = pack2(offset, offset);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t out[16 * PARTS];
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const u64 s2 = pack2(__uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1]));
+              float p[2];
+              if (PASS == Pass::kRows) {
+                unpack2(fma2(s2, scale2, offset2), p[0], p[1]);
+                p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
+                if (left < 64) {
+#pragma unroll
+                  for (int e = 0; e < 2; ++e)
+                    if (32 * c + i + e >= left) p[e] = 0.f;
+                }
+              } else {
+                u64 minus, factor;
+                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(minus), "=l"(factor) : "r"(col_at + 8 * (32 * c + i)));
+                unpack2(fma2(s2, scale2, minus), p[0], p[1]);
+                unpack2(mul2(pack2(exp2_fast(p[0]), exp2_fast(p[1])), factor), p[0], p[1]);
+              }
+              out[i / 2] = pack16<BF16>(p[0], p[1]);
+              if constexpr (PARTS == 2) out[16 + i / 2] = pack16_rest(out[i / 2], p[0], p[1]);
+            }
+            if constexpr (PARTS == 2)
+              tmem_store32(s_at + 32 * c, out);
+            else
+              tmem_store16(s_at + 32 * c, out);
+          }
+          tmem_wait_store();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar.s_done + 8 * buf);
+        }
+      }
+      tiles_b += g.len;
+      if (!ok) break;
+      if (STATS) {
+        a.stat[(g.slot * 4 + 2 * pair + half) * 128 + row] = make_float2(m == -INFINITY ? m : at, l);
+        continue;
+      }
+      ok = mbar_wait(bar.o_full, o_phase, dead);
+      if (!__all_sync(0xffffffffu, ok)) {
+        ok = false;
+        break;
+      }
+      o_phase ^= 1;
+      fence_after();
+      const int tile = nt == 2 ? pair : 0;
+      float* to = a.out + ((g.slot * sh.tiles + tile) * 128 + row) * (int64_t)a.ld + blockIdx.y * 256;
+      for (int c = nt == 2 ? half : 2 * pair + half; 16 * c < out_cols; c += nt == 2 ? 2 : 4) {
+        uint32_t v[16];
+        tmem_load16(v, lanes + 256 + 128 * tile + 16 * c);
+        float4* p = reinterpret_cast<float4*>(to + 16 * c);
+        float4 y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = g.add ? p[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+        tmem_loaded(v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          p[i] = make_float4(y[i].x + __uint_as_float(v[4 * i]), y[i].y + __uint_as_float(v[4 * i + 1]),
+                             y[i].z + __uint_as_float(v[4 * i + 2]), y[i].w + __uint_as_float(v[4 * i + 3]));
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar.o_empty);
+    }
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && dead_flag) atomicOr(a.status, kErrStuck);
+  if (warp == 1) tmem_free(tmem, 512);
+}
+
+template <Pass PASS, bool BF16, int PARTS>
+cudaError_t launch(const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st) {
+  constexpr int kSmem = 1024 + kUnits * (kUnitBytes + 1024) + kBarBytes;
+  auto kernel = mma_kernel<PASS, BF16, PARTS>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (e != cudaSuccess) return e;
+  kernel<<<dim3(blocks, out_chunks), kMmaThreads, kSmem, st>>>(a);
+  return cudaGetLastError();
+}
+
+template <Pass PASS>
+cudaError_t launch_type(bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st) {
+  if (parts == 2) return launch<PASS, false, 2>(a, blocks, out_chunks, st);
+  if (bf16) return launch<PASS, true, 1>(a, blocks, out_chunks, st);
+  return launch<PASS, false, 1>(a, blocks, out_chunks, st);
+}
+
+}  // namespace
+
+MmaShape mma_shape(Pass pass, int32_t D, int parts) {
+  MmaShape s{};
+  s.steps = (D + 15) / 16;
+  s.nk = (D + 63) / 64;
+  const int t = s.nk * parts;  // units of a tile
+  // Two tiles of A where they, two tiles of B and (for gradients) both sums fit: a
+  // tile of B is then loaded once for both.
+  s.tiles = 4 * t <= kUnits && (pass == Pass::kStats || D <= 128) ? 2 : 1;
+  s.res = 1, s.keep = 1;
+  if ((s.tiles + 2) * t > kUnits) s.keep = 0;
+  if (!s.keep && t + 4 > kUnits) s.res = 0;  // (one tile of A)
+  s.stage_units = s.keep ? t : 1;
+  s.stages = (kUnits - (s.res ? s.tiles * t : 0)) / s.stage_units;
+  return s;
+}
+
+cudaError_t launch_mma(Pass pass, bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st) {
+  if (pass == Pass::kStats) return launch_type<Pass::kStats>(bf16, parts, a, blocks, 1, st);
+  if (pass == Pass::kRows) return launch_type<Pass::kRows>(bf16, parts, a, blocks, out_chunks, st);
+  return launch_type<Pass::kCols>(bf16, parts, a, blocks, out_chunks, st);
+}
+
+}  // namespace esspt

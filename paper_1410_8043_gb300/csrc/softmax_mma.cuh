@@ -1,0 +1,75 @@
+// The tensor-core kernel of the softmax operators: scores of 128 x 128 tiles, and
+// what follows from them in one pass, on operands in units (tensor.cuh).
+#pragma once
+
+#include "softmax.cuh"
+#include "tensor.cuh"
+
+namespace esspt {
+
+// What a pass makes of the scores S = A B^T (b / ln 2 times, see MmaArgs::scale):
+//   kStats  per row of A the maximum and the sum of 2^(S - maximum)
+//   kRows   A = H, B = W: sum over B's rows of 2^(S - row_max) B
+//   kCols   A = W, B = H: sum over B's rows t of 2^(S - maximum_t) factor_t B
+enum class Pass { kStats, kRows, kCols };
+
+constexpr int kUnits = 13;             // units of shared memory
+constexpr float kHalfShift = 14.f;     // fp16 probabilities are kept 2^14 times as large
+constexpr int kMmaThreads = 640;       // a warp that loads, one that multiplies, two spare, two groups of eight
+
+// How a pass uses shared memory: A's units stay (res) or come with every tile of B,
+// for one or two tiles of A at once (tiles); a stage holds a whole tile of B, kept
+// from the scores to the sums (keep), or one unit, loaded again for the sums.
+struct MmaShape {
+  int nk, steps;       // units and 16-value steps of a row
+  int tiles, res, keep;
+  int stage_units, stages;
+};
+
+struct MmaArgs {
+  const char *A, *B;
+  MmaShape s;
+  const ManyWords* words;
+  int32_t V;
+  float b;
+  const float* row_max;  // kRows
+  const float4* col;     // kCols: two columns each, (-maximum, -maximum, factor, factor)
+  float2* stat;          // kStats out: [slot][4][128], by group and half of the columns
+  float* out;            // else: [slot][tiles][128][ld]
+  int ld;
+  int run;               // tiles of B between two additions to `out`
+  uint32_t* status;
+};
+
+// Work is the sequence of all (group of A's tiles, tile of B), cut into one even
+// range per block; block i's part of group g goes to slot i + g, and the slots of a
+// group are consecutive.
+struct Ranges {
+  int64_t groups, n_b, units, blocks;
+  __host__ __device__ Ranges(int64_t rows_a, int64_t rows_b, int tiles, int64_t grid) {
+    groups = (rows_a + 128 * tiles - 1) / (128 * tiles);
+    n_b = (rows_b + 127) / 128;
+    units = groups * n_b;
+    blocks = grid < units ? grid : units;
+  }
+  __host__ __device__ int64_t begin(int64_t i) const { return units * i / blocks; }
+  __host__ __device__ int64_t block_of(int64_t unit) const { return ((unit + 1) * blocks - 1) / units; }
+};
+
+// Scaling of fp32 operands: x 2^shift has its largest value in [2^14, 2^15).
+__device__ __forceinline__ int half_shift_of(uint32_t max_bits) {
+  return max_bits == 0u ? 0 : 14 - ((int)(max_bits >> 23) - 127);
+}
+__device__ __forceinline__ float times_pow2(float x, int e) {
+  const int e1 = e / 2;
+  return x * __int_as_float((e1 + 127) << 23) * __int_as_float((e - e1 + 127) << 23);
+}
+// Weights are divided by the power of two that is at least the largest, where p is kept in fp16.
+__device__ __forceinline__ int weight_shift_of(uint32_t max_bits) {
+  return max_bits == 0u ? 0 : (int)(max_bits >> 23) - 127 + 1;
+}
+
+cudaError_t launch_mma(Pass pass, bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st);
+MmaShape mma_shape(Pass pass, int32_t D, int parts);
+
+}  // namespace esspt
