@@ -45,6 +45,15 @@ struct Walk {
   }
 };
 
+// A place in the ring of stages: the parity flips with every turn.
+struct Ring {
+  int stage = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int stages) {
+    if (++stage == stages) stage = 0, phase ^= 1;
+  }
+};
+
 struct Bars {  // shared addresses
   uint32_t full, empty;             // [stages]
   uint32_t a_full, a_empty;
@@ -77,7 +86,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   constexpr bool STATS = PASS == Pass::kStats;
   constexpr int kBufs = STATS ? 4 : 2;  // score tiles in tensor memory
   const MmaShape sh = a.s;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int64_t rows_h = a.words->rows;
   const int64_t rows_a = PASS == Pass::kCols ? a.V : rows_h, rows_b = PASS == Pass::kCols ? rows_h : a.V;
   const Ranges ranges(rows_a, rows_b, sh.tiles, gridDim.x);
@@ -114,186 +123,191 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   auto tiles_of = [&](const Segment& s) { return sh.tiles == 2 && (s.group * 2 + 1) * 128 < rows_a ? 2 : 1; };
   const int64_t tile_bytes = (int64_t)sh.nk * PARTS * kUnitBytes;
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 0) {
     // ---- loads ----
-    uint32_t at = 0, a_phase = 1, segs = 0;  // stages so far
-    uint32_t tiles_b = 0;                    // tiles of B so far, which name their column data
-    bool ok = true;
-    auto unit = [&](const char* from, bool first_of_tile, int64_t tile) {
-      const uint32_t st = at % sh.stages;
-      ok = ok && mbar_wait(bar.empty + 8 * st, ((at / sh.stages) & 1) ^ 1, dead);
-      if (!ok) return;
-      const bool col = PASS == Pass::kCols && first_of_tile;
-      const uint32_t bytes = sh.stage_units * kUnitBytes;
-      mbar_expect(bar.full + 8 * st, bytes + (col ? 1024 : 0));
-      bulk_load(b_base + st * bytes, from, bytes, bar.full + 8 * st);
-      if (col) bulk_load(col_base + (tiles_b % sh.stages) * 1024, a.col + tile * 64, 1024, bar.full + 8 * st);
-      ++at;
-    };
-    auto scores_units = [&](int64_t tile, const char* from_a) {
-      const char* from = a.B + tile * tile_bytes;
-      if (sh.keep) {
-        unit(from, true, tile);
-      } else {
-        for (int kc = 0; kc < sh.nk && ok; ++kc) {
-          if (!sh.res)
-            for (int p = 0; p < PARTS && ok; ++p) unit(from_a + (p * sh.nk + kc) * (int64_t)kUnitBytes, false, 0);
-          for (int p = 0; p < PARTS && ok; ++p)
-            unit(from + (p * sh.nk + kc) * (int64_t)kUnitBytes, kc == 0 && p == 0, tile);
+    if (lane == 0) {
+      Ring ring;
+      int col = 0;  // stage of the column data
+      uint32_t a_phase = 1, loads = 0, segs = 0;
+      const uint32_t stage_bytes = sh.stage_units * kUnitBytes;
+      auto load = [&](const char* from, const float4* cols) {
+        mbar_wait(bar.empty + 8 * ring.stage, ring.phase ^ 1, dead);
+        const uint32_t full = bar.full + 8 * ring.stage;
+        mbar_expect(full, stage_bytes + (cols ? 1024 : 0));
+        bulk_load(b_base + ring.stage * stage_bytes, from, stage_bytes, full);
+        if (cols) bulk_load(col_base + col * 1024, cols, 1024, full);
+        ring.next(sh.stages);
+        ++loads;
+      };
+      auto scores_units = [&](int64_t tile, const char* from_a) {
+        const char* from = a.B + tile * tile_bytes;
+        const float4* cols = PASS == Pass::kCols ? a.col + tile * 64 : nullptr;
+        if (sh.keep) {
+          load(from, cols);
+        } else {
+          for (int kc = 0; kc < sh.nk; ++kc) {
+            if (!sh.res)
+              for (int p = 0; p < PARTS; ++p) load(from_a + (p * sh.nk + kc) * (int64_t)kUnitBytes, nullptr);
+            for (int p = 0; p < PARTS; ++p)
+              load(from + (p * sh.nk + kc) * (int64_t)kUnitBytes, kc == 0 && p == 0 ? cols : nullptr);
+          }
+        }
+        if (++col == sh.stages) col = 0;
+      };
+      auto sums_units = [&](int64_t tile) {
+        const char* from = a.B + tile * tile_bytes;
+        for (int kc = out_unit; kc < out_unit + out_units; ++kc)
+          for (int p = 0; p < PARTS; ++p) load(from + (p * sh.nk + kc) * (int64_t)kUnitBytes, nullptr);
+      };
+      while (walk.next(g)) {
+        const int nt = tiles_of(g);
+        const char* from_a = a.A + g.group * sh.tiles * tile_bytes;
+        if (sh.res) {
+          mbar_wait(bar.a_empty, a_phase, dead);
+          a_phase ^= 1;
+          ++segs;
+          mbar_expect(bar.a_full, (uint32_t)(nt * tile_bytes));
+          bulk_load(a_base, from_a, (uint32_t)(nt * tile_bytes), bar.a_full);
+        }
+        for (int32_t j = 0; j < g.len; ++j) {
+          scores_units(g.first + j, from_a);
+          if (!STATS && !sh.keep && j > 0) sums_units(g.first + j - 1);
+        }
+        if (!STATS && !sh.keep) sums_units(g.first + g.len - 1);
+      }
+      if (*dead) {  // copies in flight land before the block ends
+        for (uint32_t i = 0; i < (uint32_t)sh.stages && i < loads; ++i) {
+          const uint32_t n = loads - 1 - i;
+          for (int k = 0; k < (1 << 16) && !mbar_try(bar.full + 8 * (n % sh.stages), (n / sh.stages) & 1); ++k) {
+          }
+        }
+        for (int k = 0; k < (1 << 16) && segs > 0 && !mbar_try(bar.a_full, (segs - 1) & 1); ++k) {
         }
       }
-      ++tiles_b;
-    };
-    auto sums_units = [&](int64_t tile) {
-      const char* from = a.B + tile * tile_bytes;
-      for (int kc = out_unit; kc < out_unit + out_units && ok; ++kc)
-        for (int p = 0; p < PARTS && ok; ++p) unit(from + (p * sh.nk + kc) * (int64_t)kUnitBytes, false, 0);
-    };
-    while (ok && walk.next(g)) {
-      const int nt = tiles_of(g);
-      const char* from_a = a.A + g.group * sh.tiles * tile_bytes;
-      if (sh.res) {
-        ok = mbar_wait(bar.a_empty, a_phase, dead);
-        if (!ok) break;
-        a_phase ^= 1;
-        ++segs;
-        mbar_expect(bar.a_full, (uint32_t)(nt * tile_bytes));
-        bulk_load(a_base, from_a, (uint32_t)(nt * tile_bytes), bar.a_full);
-      }
-      for (int32_t j = 0; j < g.len && ok; ++j) {
-        scores_units(g.first + j, from_a);
-        if (!STATS && !sh.keep && j > 0) sums_units(g.first + j - 1);
-      }
-      if (!STATS && !sh.keep && ok) sums_units(g.first + g.len - 1);
     }
-    if (!ok) {  // copies in flight land before the block ends
-      for (uint32_t i = at > (uint32_t)sh.stages ? at - sh.stages : 0; i < at; ++i)
-        for (int k = 0; k < (1 << 16) && !mbar_try(bar.full + 8 * (i % sh.stages), (i / sh.stages) & 1); ++k) {
-        }
-      for (int k = 0; k < (1 << 16) && segs > 0 && !mbar_try(bar.a_full, (segs - 1) & 1); ++k) {
-      }
-    }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1) {
     // ---- matrix instructions ----
+    const uint32_t leader = elect_one();
     constexpr uint32_t idesc_s = mma_desc(BF16, 128, false);
     const uint32_t idesc_o = mma_desc(BF16, out_cols, true);
-    uint32_t at = 0;          // stages taken for scores (and, without keep, for sums)
-    uint32_t at_sums = 0;     // keep: tiles taken for sums
+    Ring ring;      // stages taken for scores (and, without keep, for sums)
+    Ring kept;      // keep: tiles taken for sums
     uint32_t done_phase = STATS ? 0xfu : 0u;  // parity to wait for on s_done, a bit per buffer
     uint32_t a_phase = 0, o_phase = 1;
-    bool ok = true;
-    auto stage_wait = [&](uint32_t& n) {  // shared address of the next stage
-      const uint32_t st = n % sh.stages;
-      ok = ok && mbar_wait(bar.full + 8 * st, (n / sh.stages) & 1, dead);
-      return b_base + st * sh.stage_units * kUnitBytes;
+    const uint32_t stage_bytes = sh.stage_units * kUnitBytes;
+    const int last_steps = sh.steps - 4 * (sh.nk - 1);  // of a row's last unit
+    auto stage_at = [&](const Ring& r) { return b_base + r.stage * stage_bytes; };
+    auto stage_wait = [&](const Ring& r) { warp_wait(bar.full + 8 * r.stage, r.phase, dead); };
+    auto done_wait = [&](int buf) {
+      warp_wait(bar.s_done + 8 * buf, (done_phase >> buf) & 1, dead);
+      done_phase ^= 1u << buf;
+      fence_after();
     };
-    auto stage_free = [&](uint32_t n) { mma_commit(bar.empty + 8 * (n % sh.stages)); };
-    // Products of halves in the order of their size.
     auto scores = [&](int32_t n, int nt) {
       const int buf = n & (kBufs - 1), tile = nt == 2 ? n & 1 : 0;
       const bool last = nt == 1 || tile == 1;  // of the tile of B
-      if (STATS) {
-        ok = ok && mbar_wait(bar.s_done + 8 * buf, (done_phase >> buf) & 1, dead);
-        done_phase ^= 1u << buf;
-        fence_after();
-      }
+      if (STATS) done_wait(buf);
       const uint32_t d = tmem + 128 * buf, a_at = a_base + tile * sh.nk * PARTS * kUnitBytes;
       uint32_t add = 0;
       auto products = [&](uint32_t ua, uint32_t ub, int kc) {
-        const int steps = min(4, sh.steps - 4 * kc);
-        for (int k = 0; k < steps; ++k, add = 1) mma_ss(d, desc_k(ua + 32 * k), desc_k(ub + 32 * k), idesc_s, add);
+        const uint32_t da = desc_k(ua), db = desc_k(ub);
+        const int steps = kc == sh.nk - 1 ? last_steps : 4;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k < steps) {
+            mma_ss(d, da + 2 * k, db + 2 * k, idesc_s, add, leader);
+            add = 1;
+          }
       };
       if (sh.keep) {
-        const uint32_t b_at = stage_wait(at);
-        if (!ok) return;
+        stage_wait(ring);
         fence_after();
+        const uint32_t b_at = stage_at(ring);
+        // Products of halves in the order of their size: (lo, hi), (hi, lo), (hi, hi).
 #pragma unroll
-        for (int c = PARTS == 2 ? 0 : 2; c < 3; ++c) {  // (lo, hi), (hi, lo), (hi, hi)
+        for (int c = PARTS == 2 ? 0 : 2; c < 3; ++c) {
           const int pa = c == 0, pb = c == 1;
           for (int kc = 0; kc < sh.nk; ++kc)
             products(a_at + (pa * sh.nk + kc) * kUnitBytes, b_at + (pb * sh.nk + kc) * kUnitBytes, kc);
         }
-        if (last && STATS) stage_free(at);
-        if (last) ++at;
+        if (last && STATS) mma_commit(bar.empty + 8 * ring.stage, leader);
+        if (last) ring.next(sh.stages);
       } else {
         for (int kc = 0; kc < sh.nk; ++kc) {
-          uint32_t ua[2], ub[2];
-          for (int p = 0; p < PARTS; ++p) ua[p] = a_at + (p * sh.nk + kc) * kUnitBytes;
-          const uint32_t first = at;
-          if (!sh.res)
-            for (int p = 0; p < PARTS; ++p, ++at) ua[p] = stage_wait(at);
-          for (int p = 0; p < PARTS; ++p, ++at) ub[p] = stage_wait(at);
-          if (!ok) return;
+          uint32_t ua[PARTS], ub[PARTS];
+          Ring r = ring;
+          for (int p = 0; p < PARTS; ++p) {
+            ua[p] = a_at + (p * sh.nk + kc) * kUnitBytes;
+            if (!sh.res) stage_wait(r), ua[p] = stage_at(r), r.next(sh.stages);
+          }
+          for (int p = 0; p < PARTS; ++p) stage_wait(r), ub[p] = stage_at(r), r.next(sh.stages);
           fence_after();
-          if (PARTS == 2) {
+          if constexpr (PARTS == 2) {
             products(ua[1], ub[0], kc);
             products(ua[0], ub[1], kc);
           }
           products(ua[0], ub[0], kc);
-          for (uint32_t i = first; i < at; ++i) stage_free(i);
+          for (int i = 0; i < (sh.res ? 1 : 2) * PARTS; ++i) mma_commit(bar.empty + 8 * ring.stage, leader), ring.next(sh.stages);
         }
       }
-      mma_commit(bar.s_full + 8 * buf);
+      mma_commit(bar.s_full + 8 * buf, leader);
     };
     auto sums = [&](int32_t n, int nt, int32_t jobs) {
       const int buf = n & 1, tile = nt == 2 ? n & 1 : 0;
-      ok = ok && mbar_wait(bar.s_done + 8 * buf, (done_phase >> buf) & 1, dead);
-      if (!ok) return;
-      done_phase ^= 1u << buf;
-      fence_after();
+      done_wait(buf);
       const uint32_t p_at = tmem + 128 * buf, d = tmem + 256 + 128 * tile;
-      const uint32_t first = n >= nt;  // the tile's first job of the segment overwrites
+      const uint32_t more = n >= nt;  // the tile's first job of the segment overwrites
       auto products = [&](int pp, uint32_t ub, uint32_t to, uint32_t idesc, uint32_t add) {
+        const uint32_t db = desc_mn(ub);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          mma_ts(to, p_at + 32 * (k >> 1) + 8 * (k & 1) + 16 * pp, desc_mn(ub + 2048 * k), idesc, add | (k > 0));
+          mma_ts(to, p_at + 32 * (k >> 1) + 8 * (k & 1) + 16 * pp, db + 128 * k, idesc, k > 0 ? 1u : add, leader);
       };
       if (sh.keep) {
-        const uint32_t st = at_sums % sh.stages, ub = b_base + st * sh.stage_units * kUnitBytes;
-        const uint32_t hi = ub + out_unit * kUnitBytes, lo = hi + sh.nk * kUnitBytes;
-        if (PARTS == 2) {
-          products(1, hi, d, idesc_o, first);
+        const uint32_t hi = stage_at(kept) + out_unit * kUnitBytes, lo = hi + sh.nk * kUnitBytes;
+        if constexpr (PARTS == 2) {
+          products(1, hi, d, idesc_o, more);
           products(0, lo, d, idesc_o, 1);
         }
-        products(0, hi, d, idesc_o, PARTS == 2 ? 1 : first);
-        if (nt == 1 || tile == 1) stage_free(at_sums++);
+        products(0, hi, d, idesc_o, PARTS == 2 ? 1 : more);
+        if (nt == 1 || tile == 1) mma_commit(bar.empty + 8 * kept.stage, leader), kept.next(sh.stages);
       } else {
         for (int kc = 0; kc < out_units; ++kc) {
           const uint32_t to = d + 64 * kc, idesc = mma_desc(BF16, min(64, out_cols - 64 * kc), true);
           for (int p = 0; p < PARTS; ++p) {
-            const uint32_t ub = stage_wait(at);
-            if (!ok) return;
+            stage_wait(ring);
             fence_after();
-            if (PARTS == 2 && p == 0) products(1, ub, to, idesc, first);
-            products(0, ub, to, idesc, PARTS == 2 ? 1 : first);
-            stage_free(at++);
+            const uint32_t ub = stage_at(ring);
+            if (PARTS == 2 && p == 0) products(1, ub, to, idesc, more);
+            products(0, ub, to, idesc, PARTS == 2 ? 1 : more);
+            mma_commit(bar.empty + 8 * ring.stage, leader);
+            ring.next(sh.stages);
           }
         }
       }
-      if (n == jobs - 1) mma_commit(bar.o_full);
+      if (n == jobs - 1) mma_commit(bar.o_full, leader);
     };
-    while (ok && walk.next(g)) {
+    while (walk.next(g)) {
       const int nt = tiles_of(g);
       const int32_t jobs = nt * g.len;
       if (sh.res) {
-        ok = mbar_wait(bar.a_full, a_phase, dead);
+        warp_wait(bar.a_full, a_phase, dead);
         a_phase ^= 1;
       }
-      for (int32_t n = 0; n < jobs && ok; ++n) {
+      for (int32_t n = 0; n < jobs; ++n) {
         scores(n, nt);
-        if (n == jobs - 1 && sh.res && ok) mma_commit(bar.a_empty);
+        if (n == jobs - 1 && sh.res) mma_commit(bar.a_empty, leader);
         if (STATS) continue;
         if (n == 1 || jobs == 1) {
-          ok = ok && mbar_wait(bar.o_empty, o_phase, dead);
+          warp_wait(bar.o_empty, o_phase, dead);
           o_phase ^= 1;
           fence_after();
         }
-        if (n > 0 && ok) sums(n - 1, nt, jobs);
+        if (n > 0) sums(n - 1, nt, jobs);
       }
-      if (!STATS && ok) sums(jobs - 1, nt, jobs);
+      if (!STATS) sums(jobs - 1, nt, jobs);
     }
-    if (!ok) {  // what was issued ends before tensor memory is freed
-      mma_commit(bar.a_empty);
+    if (*dead) {  // what was issued ends before tensor memory is freed
       const long long begin = clock64();
       while (clock64() - begin < 2'000'000) {
       }
@@ -309,9 +323,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const float scale = fminf(fmaxf(ldexpf(a.b * kLog2e, -(shift_h + shift_w)), 1.1754944e-38f), 3.4028235e38f);
     const u64 scale2 = pack2(scale, scale);
     uint32_t phase = 0, o_phase = 0;  // parities of s_full, a bit per buffer
-    uint32_t tiles_b = 0;
-    bool ok = true;
-    while (ok && walk.next(g)) {
+    int col0 = 0;  // stage of the segment's first column data
+    while (walk.next(g)) {
       const int nt = tiles_of(g);
       const int32_t jobs = nt * g.len;
       float m = -INFINITY, l = 0.f, at = 0.f;  // kStats: maximum (without the scale), sum, and m scale
@@ -320,14 +333,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         const int64_t r = (g.group * sh.tiles + (nt == 2 ? pair : 0)) * 128 + row;
         offset = r < rows_a ? (BF16 ? 0.f : kHalfShift) - a.row_max[r] : -1e30f;
       }
+      int col = nt == 2 ? col0 : col0 + pair;
       for (int32_t n = pair; n < jobs; n += 2) {
         const int buf = n & (kBufs - 1);
         const int32_t j = nt == 2 ? n >> 1 : n;
-        ok = mbar_wait(bar.s_full + 8 * buf, (phase >> buf) & 1, dead);
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
-        }
+        warp_wait(bar.s_full + 8 * buf, (phase >> buf) & 1, dead);
         phase ^= 1u << buf;
         fence_after();
         const int64_t left = rows_b - (g.first + j) * 128 - 64 * half;  // of this half's columns
@@ -372,7 +382,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
           l += sum2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
           m = m2, at = at2;
         } else {
-          const uint32_t col_at = col_base + ((tiles_b + j) % sh.stages) * 1024 + 512 * half;
+          if (col >= sh.stages) col -= sh.stages;
+          const uint32_t col_at = col_base + col * 1024 + 512 * half;
+          col += nt == 2 ? 1 : 2;
           const u64 offset2 = pack2(offset, offset);
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
@@ -409,17 +421,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
           if (lane == 0) mbar_arrive(bar.s_done + 8 * buf);
         }
       }
-      tiles_b += g.len;
-      if (!ok) break;
+      if (PASS == Pass::kCols) col0 = (col0 + g.len) % sh.stages;
       if (STATS) {
         a.stat[(g.slot * 4 + 2 * pair + half) * 128 + row] = make_float2(m == -INFINITY ? m : at, l);
         continue;
       }
-      ok = mbar_wait(bar.o_full, o_phase, dead);
-      if (!__all_sync(0xffffffffu, ok)) {
-        ok = false;
-        break;
-      }
+      warp_wait(bar.o_full, o_phase, dead);
       o_phase ^= 1;
       fence_after();
       const int tile = nt == 2 ? pair : 0;

@@ -36,18 +36,29 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 // Waits end: after kWaitCycles (some seconds), or once another thread of the block
-// gave up, false is returned and *dead is set; the caller leaves its loops.
+// gave up, *dead is set and the wait returns as if it had succeeded.  Every loop is
+// finite and every address is in bounds whatever the tiles hold, so the block then
+// runs to its end, on values that mean nothing, and reports that.
 constexpr long long kWaitCycles = 6'000'000'000ll;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
-  if (mbar_try(bar, parity)) return true;
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
+  if (mbar_try(bar, parity)) return;
   const long long begin = clock64();
-  for (uint32_t i = 1;; ++i) {
-    if (mbar_try(bar, parity)) return true;
+  for (uint32_t i = 1; !mbar_try(bar, parity); ++i)
     if ((i & 63u) == 0u && (*dead != 0u || clock64() - begin > kWaitCycles)) {
       *dead = 1u;
-      return false;
+      return;
     }
-  }
+}
+// By a whole warp, whose lanes go on together: one left behind could miss a phase.
+__device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
+  mbar_wait(bar, parity, dead);
+  __syncwarp();
+}
+// One lane of a converged warp.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+  return r;
 }
 
 // `bytes` (a multiple of 16) from global to shared memory; the barrier counts them.
@@ -99,38 +110,44 @@ __device__ __forceinline__ void tmem_loaded<16>(uint32_t (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) : : "memory");
 }
 
-// Shared-memory descriptors (address, byte offsets in units of 16; version 1;
-// 128-byte swizzle).  K-major: eight rows, 1024 bytes, repeat along the rows.
+// Shared-memory descriptors: address and byte offsets in units of 16; version 1;
+// 128-byte swizzle.  K-major: eight rows, 1024 bytes, repeat along the rows.
 // MN-major: eight steps of the inner dimension, 1024 bytes, repeat along it, and
-// whole units along the columns.
-constexpr uint64_t kDescBase = (1ull << 46) | (2ull << 61) | ((uint64_t)(1024 >> 4) << 32);
-__device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
-  return kDescBase | (1ull << 16) | (uint64_t)((addr & 0x3ffffu) >> 4);
-}
-__device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
-  return kDescBase | ((uint64_t)(kUnitBytes >> 4) << 16) | (uint64_t)((addr & 0x3ffffu) >> 4);
-}
+// whole units along the columns.  Only the low words differ, and steps add to them.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_k(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | ((kUnitBytes >> 4) << 16); }
 // Instruction descriptor: fp32 sums, both operands bf16 or both fp16, 128 rows.
 __host__ __device__ constexpr uint32_t mma_desc(bool bf16, uint32_t columns, bool b_mn) {
   return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_mn ? 1u : 0u) << 16) |
          ((columns >> 3) << 17) | (8u << 24);
 }
-// D (+)= A B^T over 16 steps: A from shared or from tensor memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+// D (+)= A B^T over 16 steps, A from shared or from tensor memory; issued by the lane
+// that has `leader`, so that the whole warp runs the loop around it and its operands
+// stay in uniform registers.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add, uint32_t leader) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(add)
+      "{\n .reg .pred p, q;\n .reg .b64 da, db;\n mov.b64 da, {%1, %6};\n mov.b64 db, {%2, %6};\n"
+      " setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(leader), "n"(kDescHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add, uint32_t leader) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(add)
+      "{\n .reg .pred p, q;\n .reg .b64 db;\n mov.b64 db, {%2, %6};\n"
+      " setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(leader), "n"(kDescHigh)
       : "memory");
 }
-// The barrier gets one arrival once the thread's matrix instructions so far are done.
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// The barrier gets one arrival once the leader's matrix instructions so far are done.
+__device__ __forceinline__ void mma_commit(uint32_t bar, uint32_t leader) {
+  asm volatile(
+      "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar),
+      "r"(leader)
+      : "memory");
 }
 
 }  // namespace esspt
