@@ -78,6 +78,45 @@ __device__ __forceinline__ uint32_t pack16_rest(uint32_t p, float lo, float hi) 
   return pack16<false>(lo - f.x, hi - f.y);
 }
 
+// STEPS products of 16 values over units that follow each other, written out: with
+// conditions or loops in between the issue of an instruction took 60 to 120 cycles
+// (here 17) where it runs for 64.
+template <int STEPS>
+__device__ __forceinline__ void steps_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add, uint32_t leader) {
+  constexpr uint32_t kUnit = kUnitBytes >> 4;
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k)
+    mma_ss(d, a + k / 4 * kUnit + k % 4 * 2, b + k / 4 * kUnit + k % 4 * 2, idesc, k > 0 ? 1u : add, leader);
+}
+// Scores of a tile of A and one of B: products of halves in the order of their size,
+// (lo, hi), (hi, lo), (hi, hi).
+template <int PARTS, int STEPS>
+__device__ __forceinline__ void scores_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t leader) {
+  if constexpr (PARTS == 2) {
+    constexpr uint32_t kHalf = (kUnitBytes >> 4) * ((STEPS + 3) / 4);
+    steps_mma<STEPS>(d, a + kHalf, b, idesc, 0, leader);
+    steps_mma<STEPS>(d, a, b + kHalf, idesc, 1, leader);
+  }
+  steps_mma<STEPS>(d, a, b, idesc, PARTS == 2, leader);
+}
+// The same for a pair of units of one tile each, of which `steps` are in use.
+__device__ __forceinline__ void unit_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps, uint32_t add,
+                                         uint32_t leader) {
+  switch (steps) {
+    case 1: return steps_mma<1>(d, a, b, idesc, add, leader);
+    case 2: return steps_mma<2>(d, a, b, idesc, add, leader);
+    case 3: return steps_mma<3>(d, a, b, idesc, add, leader);
+    default: return steps_mma<4>(d, a, b, idesc, add, leader);
+  }
+}
+// Sums: the 128 probabilities of every row (half `part`) times units of B.
+__device__ __forceinline__ void sums_mma(uint32_t d, uint32_t p, int part, uint32_t b, uint32_t idesc, uint32_t add,
+                                         uint32_t leader) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    mma_ts(d, p + 32 * (k >> 1) + 8 * (k & 1) + 16 * part, b + 128 * k, idesc, k > 0 ? 1u : add, leader);
+}
+
 template <Pass PASS, bool BF16, int PARTS>
 __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ MmaArgs a) {
   extern __shared__ __align__(1024) char smem[];
@@ -142,7 +181,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       auto scores_units = [&](int64_t tile, const char* from_a) {
         const char* from = a.B + tile * tile_bytes;
         const float4* cols = PASS == Pass::kCols ? a.col + tile * 64 : nullptr;
-        if (sh.keep) {
+        if (sh.stage_units > 1 || sh.nk * PARTS == 1) {
           load(from, cols);
         } else {
           for (int kc = 0; kc < sh.nk; ++kc) {
@@ -190,122 +229,173 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const uint32_t leader = elect_one();
     constexpr uint32_t idesc_s = mma_desc(BF16, 128, false);
     const uint32_t idesc_o = mma_desc(BF16, out_cols, true);
-    Ring ring;      // stages taken for scores (and, without keep, for sums)
-    Ring kept;      // keep: tiles taken for sums
+    Ring ring;      // stages taken for scores (and for sums, where B is loaded again)
+    Ring kept;      // stages taken for sums, where B is kept
     uint32_t done_phase = STATS ? 0xfu : 0u;  // parity to wait for on s_done, a bit per buffer
     uint32_t a_phase = 0, o_phase = 1;
     const uint32_t stage_bytes = sh.stage_units * kUnitBytes;
     const int last_steps = sh.steps - 4 * (sh.nk - 1);  // of a row's last unit
     auto stage_at = [&](const Ring& r) { return b_base + r.stage * stage_bytes; };
     auto stage_wait = [&](const Ring& r) { warp_wait(bar.full + 8 * r.stage, r.phase, dead); };
+    auto stage_free = [&](Ring& r) {
+      mma_commit(bar.empty + 8 * r.stage, leader);
+      r.next(sh.stages);
+    };
     auto done_wait = [&](int buf) {
       warp_wait(bar.s_done + 8 * buf, (done_phase >> buf) & 1, dead);
       done_phase ^= 1u << buf;
       fence_after();
     };
-    auto scores = [&](int32_t n, int nt) {
-      const int buf = n & (kBufs - 1), tile = nt == 2 ? n & 1 : 0;
-      const bool last = nt == 1 || tile == 1;  // of the tile of B
-      if (STATS) done_wait(buf);
-      const uint32_t d = tmem + 128 * buf, a_at = a_base + tile * sh.nk * PARTS * kUnitBytes;
-      uint32_t add = 0;
-      auto products = [&](uint32_t ua, uint32_t ub, int kc) {
-        const uint32_t da = desc_k(ua), db = desc_k(ub);
-        const int steps = kc == sh.nk - 1 ? last_steps : 4;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (k < steps) {
-            mma_ss(d, da + 2 * k, db + 2 * k, idesc_s, add, leader);
-            add = 1;
-          }
-      };
-      if (sh.keep) {
-        stage_wait(ring);
-        fence_after();
-        const uint32_t b_at = stage_at(ring);
-        // Products of halves in the order of their size: (lo, hi), (hi, lo), (hi, hi).
-#pragma unroll
-        for (int c = PARTS == 2 ? 0 : 2; c < 3; ++c) {
-          const int pa = c == 0, pb = c == 1;
-          for (int kc = 0; kc < sh.nk; ++kc)
-            products(a_at + (pa * sh.nk + kc) * kUnitBytes, b_at + (pb * sh.nk + kc) * kUnitBytes, kc);
-        }
-        if (last && STATS) mma_commit(bar.empty + 8 * ring.stage, leader);
-        if (last) ring.next(sh.stages);
-      } else {
-        for (int kc = 0; kc < sh.nk; ++kc) {
-          uint32_t ua[PARTS], ub[PARTS];
-          Ring r = ring;
-          for (int p = 0; p < PARTS; ++p) {
-            ua[p] = a_at + (p * sh.nk + kc) * kUnitBytes;
-            if (!sh.res) stage_wait(r), ua[p] = stage_at(r), r.next(sh.stages);
-          }
-          for (int p = 0; p < PARTS; ++p) stage_wait(r), ub[p] = stage_at(r), r.next(sh.stages);
-          fence_after();
-          if constexpr (PARTS == 2) {
-            products(ua[1], ub[0], kc);
-            products(ua[0], ub[1], kc);
-          }
-          products(ua[0], ub[0], kc);
-          for (int i = 0; i < (sh.res ? 1 : 2) * PARTS; ++i) mma_commit(bar.empty + 8 * ring.stage, leader), ring.next(sh.stages);
-        }
-      }
-      mma_commit(bar.s_full + 8 * buf, leader);
+    auto sums_begin = [&]() {  // the last segment's sums have been read
+      warp_wait(bar.o_empty, o_phase, dead);
+      o_phase ^= 1;
+      fence_after();
     };
-    auto sums = [&](int32_t n, int nt, int32_t jobs) {
-      const int buf = n & 1, tile = nt == 2 ? n & 1 : 0;
-      done_wait(buf);
-      const uint32_t p_at = tmem + 128 * buf, d = tmem + 256 + 128 * tile;
-      const uint32_t more = n >= nt;  // the tile's first job of the segment overwrites
-      auto products = [&](int pp, uint32_t ub, uint32_t to, uint32_t idesc, uint32_t add) {
-        const uint32_t db = desc_mn(ub);
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          mma_ts(to, p_at + 32 * (k >> 1) + 8 * (k & 1) + 16 * pp, db + 128 * k, idesc, k > 0 ? 1u : add, leader);
-      };
-      if (sh.keep) {
-        const uint32_t hi = stage_at(kept) + out_unit * kUnitBytes, lo = hi + sh.nk * kUnitBytes;
-        if constexpr (PARTS == 2) {
-          products(1, hi, d, idesc_o, more);
-          products(0, lo, d, idesc_o, 1);
-        }
-        products(0, hi, d, idesc_o, PARTS == 2 ? 1 : more);
-        if (nt == 1 || tile == 1) mma_commit(bar.empty + 8 * kept.stage, leader), kept.next(sh.stages);
-      } else {
-        for (int kc = 0; kc < out_units; ++kc) {
-          const uint32_t to = d + 64 * kc, idesc = mma_desc(BF16, min(64, out_cols - 64 * kc), true);
-          for (int p = 0; p < PARTS; ++p) {
-            stage_wait(ring);
-            fence_after();
-            const uint32_t ub = stage_at(ring);
-            if (PARTS == 2 && p == 0) products(1, ub, to, idesc, more);
-            products(0, ub, to, idesc, PARTS == 2 ? 1 : more);
-            mma_commit(bar.empty + 8 * ring.stage, leader);
-            ring.next(sh.stages);
-          }
-        }
-      }
-      if (n == jobs - 1) mma_commit(bar.o_full, leader);
-    };
+    const bool whole = sh.stage_units > 1 || sh.nk * PARTS == 1;  // a stage is a tile of B
     while (walk.next(g)) {
       const int nt = tiles_of(g);
-      const int32_t jobs = nt * g.len;
       if (sh.res) {
         warp_wait(bar.a_full, a_phase, dead);
         a_phase ^= 1;
       }
-      for (int32_t n = 0; n < jobs; ++n) {
-        scores(n, nt);
-        if (n == jobs - 1 && sh.res) mma_commit(bar.a_empty, leader);
-        if (STATS) continue;
-        if (n == 1 || jobs == 1) {
-          warp_wait(bar.o_empty, o_phase, dead);
-          o_phase ^= 1;
+      if (whole) {
+        // Order of issue: S(0) S(1) O(0) S(2) O(1) ..., so that the exponentials of one
+        // tile of scores run beside the products of the other.
+        const uint32_t a0 = desc_k(a_base), a1 = desc_k(a_base + sh.nk * PARTS * kUnitBytes);
+        auto scores = [&](uint32_t d, uint32_t a, uint32_t b) {
+          switch (sh.steps) {
+            case 1: return scores_mma<PARTS, 1>(d, a, b, idesc_s, leader);
+            case 2: return scores_mma<PARTS, 2>(d, a, b, idesc_s, leader);
+            case 3: return scores_mma<PARTS, 3>(d, a, b, idesc_s, leader);
+            case 4: return scores_mma<PARTS, 4>(d, a, b, idesc_s, leader);
+            case 5: return scores_mma<PARTS, PARTS == 1 ? 5 : 4>(d, a, b, idesc_s, leader);
+            case 6: return scores_mma<PARTS, PARTS == 1 ? 6 : 4>(d, a, b, idesc_s, leader);
+            case 7: return scores_mma<PARTS, PARTS == 1 ? 7 : 4>(d, a, b, idesc_s, leader);
+            default: return scores_mma<PARTS, PARTS == 1 ? 8 : 4>(d, a, b, idesc_s, leader);
+          }
+        };
+        auto sums = [&](int buf, int tile, uint32_t more, bool last) {
+          done_wait(buf);
+          const uint32_t p = tmem + 128 * buf, d = tmem + 256 + 128 * tile, b = desc_mn(stage_at(kept));
+          if constexpr (PARTS == 2) {
+            sums_mma(d, p, 1, b, idesc_o, more, leader);
+            sums_mma(d, p, 0, b + (sh.nk * kUnitBytes >> 4), idesc_o, 1, leader);
+          }
+          sums_mma(d, p, 0, b, idesc_o, PARTS == 2 ? 1 : more, leader);
+          if (last) stage_free(kept);
+        };
+        int n = 0;
+        for (int32_t j = 0; j < g.len; ++j) {
+          stage_wait(ring);
           fence_after();
+          const uint32_t b = desc_k(stage_at(ring));
+          if (nt == 2) {
+#pragma unroll
+            for (int tile = 0; tile < 2; ++tile) {
+              const int buf = STATS ? (j & 1) * 2 + tile : tile;
+              if (STATS) done_wait(buf);
+              scores(tmem + 128 * buf, tile ? a1 : a0, b);
+              mma_commit(bar.s_full + 8 * buf, leader);
+              if (STATS) continue;
+              if (j == 0 && tile == 1) sums_begin();
+              if (tile == 1) sums(0, 0, j > 0, false);
+              else if (j > 0) sums(1, 1, j > 1, true);
+            }
+            n = 1;
+          } else {
+            const int buf = j & (kBufs - 1);
+            if (STATS) done_wait(buf);
+            scores(tmem + 128 * buf, a0, b);
+            mma_commit(bar.s_full + 8 * buf, leader);
+            if (!STATS && (j == 1 || g.len == 1)) sums_begin();
+            if (!STATS && j > 0) sums(buf ^ 1, 0, j > 1, true);
+            n = j & 1;
+          }
+          if (STATS) stage_free(ring);
+          else ring.next(sh.stages);
         }
-        if (n > 0) sums(n - 1, nt, jobs);
+        if (sh.res) mma_commit(bar.a_empty, leader);
+        if (!STATS) sums(n, nt == 2 ? 1 : 0, g.len > 1, true);
+      } else if (STATS) {
+        // Units of B come one by one and go after their products with both tiles of A.
+        for (int32_t j = 0; j < g.len; ++j) {
+          const int buf = nt == 2 ? (j & 1) * 2 : j & 3;
+          for (int tile = 0; tile < nt; ++tile) done_wait(buf + tile);
+          for (int kc = 0; kc < sh.nk; ++kc) {
+            const int steps = kc == sh.nk - 1 ? last_steps : 4;
+            uint32_t ua[PARTS], ub[PARTS];
+            Ring r = ring;
+            if (!sh.res)
+              for (int p = 0; p < PARTS; ++p) stage_wait(r), ua[p] = desc_k(stage_at(r)), r.next(sh.stages);
+            for (int p = 0; p < PARTS; ++p) stage_wait(r), ub[p] = desc_k(stage_at(r)), r.next(sh.stages);
+            fence_after();
+            for (int tile = 0; tile < nt; ++tile) {
+              const uint32_t d = tmem + 128 * (buf + tile);
+              if (sh.res)
+                for (int p = 0; p < PARTS; ++p) ua[p] = desc_k(a_base + ((tile * PARTS + p) * sh.nk + kc) * kUnitBytes);
+              if constexpr (PARTS == 2) {
+                unit_mma(d, ua[1], ub[0], idesc_s, steps, kc > 0, leader);
+                unit_mma(d, ua[0], ub[1], idesc_s, steps, 1, leader);
+              }
+              unit_mma(d, ua[0], ub[0], idesc_s, steps, PARTS == 2 || kc > 0, leader);
+            }
+            for (int i = 0; i < (sh.res ? 1 : 2) * PARTS; ++i) stage_free(ring);
+          }
+          for (int tile = 0; tile < nt; ++tile) mma_commit(bar.s_full + 8 * (buf + tile), leader);
+        }
+        if (sh.res) mma_commit(bar.a_empty, leader);
+      } else {
+        // One tile of A; units of B stay until their part of the sums is done, or come twice.
+        auto scores = [&](int buf) {
+          const uint32_t d = tmem + 128 * buf;
+          for (int kc = 0; kc < sh.nk; ++kc) {
+            const int steps = kc == sh.nk - 1 ? last_steps : 4;
+            uint32_t ua[PARTS], ub[PARTS];
+            Ring r = ring;
+            for (int p = 0; p < PARTS; ++p) {
+              if (sh.res) ua[p] = desc_k(a_base + (p * sh.nk + kc) * kUnitBytes);
+              else stage_wait(r), ua[p] = desc_k(stage_at(r)), r.next(sh.stages);
+            }
+            for (int p = 0; p < PARTS; ++p) stage_wait(r), ub[p] = desc_k(stage_at(r)), r.next(sh.stages);
+            fence_after();
+            if constexpr (PARTS == 2) {
+              unit_mma(d, ua[1], ub[0], idesc_s, steps, kc > 0, leader);
+              unit_mma(d, ua[0], ub[1], idesc_s, steps, 1, leader);
+            }
+            unit_mma(d, ua[0], ub[0], idesc_s, steps, PARTS == 2 || kc > 0, leader);
+            if (sh.keep) ring = r;
+            else
+              for (int i = 0; i < (sh.res ? 1 : 2) * PARTS; ++i) stage_free(ring);
+          }
+          mma_commit(bar.s_full + 8 * buf, leader);
+        };
+        auto sums = [&](int buf, uint32_t more) {
+          done_wait(buf);
+          const uint32_t p_at = tmem + 128 * buf;
+          Ring& from = sh.keep ? kept : ring;
+          for (int kc = 0; kc < out_units; ++kc) {
+            const uint32_t d = tmem + 256 + 64 * kc, idesc = mma_desc(BF16, min(64, out_cols - 64 * kc), true);
+            for (int p = 0; p < PARTS; ++p) {
+              if (!sh.keep) {
+                stage_wait(from);
+                fence_after();
+              }
+              const uint32_t b = desc_mn(stage_at(from));
+              if (PARTS == 2 && p == 0) sums_mma(d, p_at, 1, b, idesc, more, leader);
+              sums_mma(d, p_at, 0, b, idesc, PARTS == 2 ? 1 : more, leader);
+              stage_free(from);
+            }
+          }
+        };
+        for (int32_t j = 0; j < g.len; ++j) {
+          scores(j & 1);
+          if (j == g.len - 1 && sh.res) mma_commit(bar.a_empty, leader);
+          if (j == 1 || g.len == 1) sums_begin();
+          if (j > 0) sums((j & 1) ^ 1, j > 1);
+        }
+        sums((g.len - 1) & 1, g.len > 1);
       }
-      if (!STATS) sums(jobs - 1, nt, jobs);
+      if (!STATS) mma_commit(bar.o_full, leader);
     }
     if (*dead) {  // what was issued ends before tensor memory is freed
       const long long begin = clock64();
@@ -475,18 +565,20 @@ cudaError_t launch_type(bool bf16, int parts, const MmaArgs& a, int blocks, int 
 
 }  // namespace
 
+// t units to a tile.  Up to two, a stage of the ring is a tile of B and two tiles of A
+// share it.  Above, stages are units: a tile of B is then never waited for as a whole
+// (K = 256, bf16: with two stages of 64 KB a tile waited 940 of 3150 cycles).  Two tiles
+// of A share those too where only their scores are wanted and three units are left.
 MmaShape mma_shape(Pass pass, int32_t D, int parts) {
   MmaShape s{};
   s.steps = (D + 15) / 16;
   s.nk = (D + 63) / 64;
-  const int t = s.nk * parts;  // units of a tile
-  // Two tiles of A where they, two tiles of B and (for gradients) both sums fit: a
-  // tile of B is then loaded once for both.
-  s.tiles = 4 * t <= kUnits && (pass == Pass::kStats || D <= 128) ? 2 : 1;
-  s.res = 1, s.keep = 1;
-  if ((s.tiles + 2) * t > kUnits) s.keep = 0;
-  if (!s.keep && t + 4 > kUnits) s.res = 0;  // (one tile of A)
-  s.stage_units = s.keep ? t : 1;
+  const int t = s.nk * parts;
+  const bool stats = pass == Pass::kStats;
+  s.tiles = t <= 2 || (stats && 2 * t + 3 <= kUnits) ? 2 : 1;
+  s.res = s.tiles * t + (parts == 2 ? 4 : 3) <= kUnits || s.tiles == 2;
+  s.keep = t <= 2 || (s.res && 3 * t <= kUnits);
+  s.stage_units = t <= 2 ? t : 1;
   s.stages = (kUnits - (s.res ? s.tiles * t : 0)) / s.stage_units;
   return s;
 }
