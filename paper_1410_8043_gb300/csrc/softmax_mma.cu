@@ -11,6 +11,8 @@
 // fp32 (PARTS = 2): S = lo hi + hi lo + hi hi of the operands' halves, and the same
 // for p B.  Sums run over at most `run` tiles in the tensor core, whose additions
 // round worse than fp32's own, and are then added in fp32.
+#include <type_traits>
+
 #include "ptx.cuh"
 #include "softmax_mma.cuh"
 
@@ -42,15 +44,6 @@ struct Walk {
     s.add = s.first != 0 && u != begin;
     u += s.len;
     return true;
-  }
-};
-
-// A place in the ring of stages: the parity flips with every turn.
-struct Ring {
-  int stage = 0;
-  uint32_t phase = 0;
-  __device__ __forceinline__ void next(int stages) {
-    if (++stage == stages) stage = 0, phase ^= 1;
   }
 };
 
@@ -99,16 +92,6 @@ __device__ __forceinline__ void scores_mma(uint32_t d, uint32_t a, uint32_t b, u
   }
   steps_mma<STEPS>(d, a, b, idesc, PARTS == 2, leader);
 }
-// The same for a pair of units of one tile each, of which `steps` are in use.
-__device__ __forceinline__ void unit_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps, uint32_t add,
-                                         uint32_t leader) {
-  switch (steps) {
-    case 1: return steps_mma<1>(d, a, b, idesc, add, leader);
-    case 2: return steps_mma<2>(d, a, b, idesc, add, leader);
-    case 3: return steps_mma<3>(d, a, b, idesc, add, leader);
-    default: return steps_mma<4>(d, a, b, idesc, add, leader);
-  }
-}
 // Sums: the 128 probabilities of every row (half `part`) times units of B.
 __device__ __forceinline__ void sums_mma(uint32_t d, uint32_t p, int part, uint32_t b, uint32_t idesc, uint32_t add,
                                          uint32_t leader) {
@@ -117,13 +100,206 @@ __device__ __forceinline__ void sums_mma(uint32_t d, uint32_t p, int part, uint3
     mma_ts(d, p + 32 * (k >> 1) + 8 * (k & 1) + 16 * part, b + 128 * k, idesc, k > 0 ? 1u : add, leader);
 }
 
+// A place in the ring of stages, with what is used of it.
+struct Ring {
+  uint32_t at, bar, phase;  // address, full barrier (the empty one lies kEmpty further), parity
+  uint32_t at0, bar0, bytes, end;
+  __device__ __forceinline__ Ring(uint32_t at_, uint32_t bar_, uint32_t bytes_, int stages)
+      : at(at_), bar(bar_), phase(0), at0(at_), bar0(bar_), bytes(bytes_), end(bar_ + 8 * stages) {}
+  __device__ __forceinline__ void next() {
+    at += bytes, bar += 8;
+    if (bar == end) at = at0, bar = bar0, phase ^= 1;
+  }
+};
+constexpr uint32_t kEmpty = 8 * kUnits;
+
+// The warp that issues the matrix instructions, for rows of NK units.  Everything that
+// can be is known at compile time: this one warp works through a chain of instructions
+// of a few cycles each, and with the loops and addresses left to run time it took longer
+// for them than the tensor cores for the products (K = 256, bf16, scores alone: 2500
+// cycles per tile, 1020 of them products).
+template <Pass PASS, bool BF16, int PARTS, int NK>
+struct Issue {
+  static constexpr bool STATS = PASS == Pass::kStats;
+  static constexpr MmaShape S = mma_shape(PASS, 64 * NK, PARTS);
+  static constexpr uint32_t kIdesc = mma_desc(BF16, 128, false);
+  static constexpr uint32_t kUnit = kUnitBytes >> 4, kTile = NK * PARTS * kUnit;  // in descriptors
+  const Bars& bar;
+  volatile uint32_t* dead;
+  const uint32_t leader, tmem, a_base;
+  const int last_steps;  // of a row's last unit
+  const int out_cols, out_units;
+  Ring ring, kept;       // stages for scores (and for sums, where B is loaded again); for sums of what was kept
+  uint32_t done_phase = STATS ? 0xfu : 0u;  // parity to wait for on s_done, a bit per buffer
+  uint32_t a_phase = 0, o_phase = 1;
+
+  __device__ __forceinline__ Issue(const Bars& bar_, volatile uint32_t* dead_, uint32_t tmem_, uint32_t a_base_, uint32_t b_base,
+                                   int steps, int out_cols_, int out_units_)
+      : bar(bar_), dead(dead_), leader(elect_one()), tmem(tmem_), a_base(desc_k(a_base_)), last_steps(steps - 4 * (NK - 1)),
+        out_cols(out_cols_), out_units(out_units_), ring(b_base, bar_.full, S.stage_units * kUnitBytes, S.stages), kept(ring) {}
+
+  __device__ __forceinline__ void take(const Ring& r) {  // wait for a stage's loads
+    warp_wait(r.bar, r.phase, dead);
+    fence_after();
+  }
+  __device__ __forceinline__ void free(Ring& r) {
+    mma_commit(r.bar + kEmpty, leader);
+    r.next();
+  }
+  __device__ __forceinline__ void done(uint32_t buf) {  // wait until its scores were read (or made probabilities)
+    warp_wait(bar.s_done + 8 * buf, (done_phase >> buf) & 1, dead);
+    done_phase ^= 1u << buf;
+    fence_after();
+  }
+  // Products of one unit of A and of B; STEPS of 16 values.
+  template <int STEPS>
+  __device__ __forceinline__ void steps(uint32_t d, uint32_t a, uint32_t b, uint32_t add) {
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) mma_ss(d, a + 2 * k, b + 2 * k, kIdesc, k > 0 ? 1u : add, leader);
+  }
+  // All products of a pair of units: of halves in the order of their size, (lo, hi),
+  // (hi, lo), (hi, hi); lo lies a_lo and b_lo further.
+  template <int STEPS>
+  __device__ __forceinline__ void pair(uint32_t d, uint32_t a, uint32_t b, uint32_t a_lo, uint32_t b_lo, uint32_t add) {
+    if constexpr (PARTS == 2) {
+      steps<STEPS>(d, a + a_lo, b, add);
+      steps<STEPS>(d, a, b + b_lo, 1);
+      steps<STEPS>(d, a, b, 1);
+    } else {
+      steps<STEPS>(d, a, b, add);
+    }
+  }
+  __device__ __forceinline__ void pair_last(uint32_t d, uint32_t a, uint32_t b, uint32_t a_lo, uint32_t b_lo, uint32_t add) {
+    switch (last_steps) {
+      case 1: return pair<1>(d, a, b, a_lo, b_lo, add);
+      case 2: return pair<2>(d, a, b, a_lo, b_lo, add);
+      case 3: return pair<3>(d, a, b, a_lo, b_lo, add);
+      default: return pair<4>(d, a, b, a_lo, b_lo, add);
+    }
+  }
+  // Scores of the next tile of B with NT tiles of A, to buffers at d, d + 128.
+  template <int NT>
+  __device__ __forceinline__ void scores(uint32_t d) {
+    if constexpr (S.stage_units == NK * PARTS) {  // a stage is the tile, as it lies in memory: parts, then units
+      take(ring);
+      const uint32_t b = desc_k(ring.at);
+#pragma unroll
+      for (int tile = 0; tile < NT; ++tile) {
+#pragma unroll
+        for (int kc = 0; kc < NK - 1; ++kc)
+          pair<4>(d + 128 * tile, a_base + tile * kTile + kc * kUnit, b + kc * kUnit, NK * kUnit, NK * kUnit, kc > 0);
+        pair_last(d + 128 * tile, a_base + tile * kTile + (NK - 1) * kUnit, b + (NK - 1) * kUnit, NK * kUnit, NK * kUnit, NK > 1);
+      }
+      if (STATS) free(ring);
+      else ring.next();
+    } else {
+#pragma unroll
+      for (int kc = 0; kc < NK; ++kc) {
+        Ring r = ring;
+        uint32_t ua[2] = {a_base + kc * kUnit, a_base + (NK + kc) * kUnit}, ub[2] = {0, 0};
+        if constexpr (!S.res) {
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) take(r), ua[p] = desc_k(r.at), r.next();
+        }
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) take(r), ub[p] = desc_k(r.at), r.next();
+#pragma unroll
+        for (int tile = 0; tile < NT; ++tile) {
+          if (kc < NK - 1)
+            pair<4>(d + 128 * tile, ua[0] + tile * kTile, ub[0], ua[1] - ua[0], ub[1] - ub[0], kc > 0);
+          else
+            pair_last(d + 128 * tile, ua[0] + tile * kTile, ub[0], ua[1] - ua[0], ub[1] - ub[0], kc > 0);
+        }
+        if constexpr (!STATS && S.keep) {
+          ring = r;
+        } else {
+#pragma unroll
+          for (int i = 0; i < (S.res ? 1 : 2) * PARTS; ++i) free(ring);
+        }
+      }
+    }
+  }
+  // Sums of the next tile of B from the probabilities in buffer `buf`.
+  __device__ __forceinline__ void sums(uint32_t buf, uint32_t more) {
+    done(buf);
+    const uint32_t p = tmem + 128 * buf, d = tmem + 128 * S.buffers;
+    if constexpr (S.stage_units == NK * PARTS) {
+      const uint32_t b = desc_mn(kept.at), idesc = mma_desc(BF16, out_cols, true);
+      if constexpr (PARTS == 2) {
+        sums_mma(d, p, 1, b, idesc, more, leader);
+        sums_mma(d, p, 0, b + NK * kUnit, idesc, 1, leader);
+      }
+      sums_mma(d, p, 0, b, idesc, PARTS == 2 ? 1 : more, leader);
+      free(kept);
+    } else {
+      Ring& from = S.keep ? kept : ring;
+      constexpr int kMost = NK < 4 ? NK : 4;
+#pragma unroll
+      for (int kc = 0; kc < kMost; ++kc) {
+        if (kc >= out_units) break;
+        const uint32_t idesc = mma_desc(BF16, min(64, out_cols - 64 * kc), true);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+          if (!S.keep) take(from);
+          const uint32_t b = desc_mn(from.at);
+          if (PARTS == 2 && part == 0) sums_mma(d + 64 * kc, p, 1, b, idesc, more, leader);
+          sums_mma(d + 64 * kc, p, 0, b, idesc, PARTS == 2 ? 1 : more, leader);
+          free(from);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void segment(int nt, int32_t len) {
+    if (S.res) {
+      warp_wait(bar.a_full, a_phase, dead);
+      a_phase ^= 1;
+    }
+    if constexpr (STATS) {
+      for (int32_t j = 0; j < len; ++j) {
+        if (S.tiles == 2 && nt == 2) {
+          const uint32_t buf = (j & 1) * 2;
+          done(buf), done(buf + 1);
+          scores<2>(tmem + 128 * buf);
+          mma_commit(bar.s_full + 8 * buf, leader), mma_commit(bar.s_full + 8 * buf + 8, leader);
+        } else {
+          const uint32_t buf = j & 3;
+          done(buf);
+          scores<1>(tmem + 128 * buf);
+          mma_commit(bar.s_full + 8 * buf, leader);
+        }
+      }
+      if (S.res) mma_commit(bar.a_empty, leader);
+    } else {
+      // Scores run ahead of the sums by all buffers but one, so that the exponentials
+      // of the next tiles need not wait for them.
+      constexpr uint32_t kAhead = S.buffers - 1;
+      uint32_t buf = 0, next = 0;  // of the next sums and scores
+      auto ahead = [&](bool last) {
+        scores<1>(tmem + 128 * next);
+        mma_commit(bar.s_full + 8 * next, leader);
+        if (last && S.res) mma_commit(bar.a_empty, leader);
+        if (++next == S.buffers) next = 0;
+      };
+      for (int32_t j = 0; j < (int32_t)kAhead && j < len; ++j) ahead(j == len - 1);
+      warp_wait(bar.o_empty, o_phase, dead);  // the last segment's sums have been read
+      o_phase ^= 1;
+      fence_after();
+      for (int32_t j = 0; j < len; ++j) {
+        if (j + (int32_t)kAhead < len) ahead(j + (int32_t)kAhead == len - 1);
+        sums(buf, j > 0);
+        if (++buf == S.buffers) buf = 0;
+      }
+      mma_commit(bar.o_full, leader);
+    }
+  }
+};
+
 template <Pass PASS, bool BF16, int PARTS>
 __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ MmaArgs a) {
   extern __shared__ __align__(1024) char smem[];
   __shared__ uint32_t tmem_at;
   __shared__ uint32_t dead_flag;
   constexpr bool STATS = PASS == Pass::kStats;
-  constexpr int kBufs = STATS ? 4 : 2;  // score tiles in tensor memory
   const MmaShape sh = a.s;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int64_t rows_h = a.words->rows;
@@ -136,7 +312,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   const uint32_t col_base = base + kUnits * kUnitBytes;  // [stages] of the columns' data
   const uint32_t bar0 = col_base + kUnits * 1024;
   Bars bar;
-  bar.full = bar0, bar.empty = bar.full + 8 * kUnits, bar.a_full = bar.empty + 8 * kUnits, bar.a_empty = bar.a_full + 8;
+  bar.full = bar0, bar.empty = bar.full + kEmpty, bar.a_full = bar.empty + 8 * kUnits, bar.a_empty = bar.a_full + 8;
   bar.s_full = bar.a_empty + 8, bar.s_done = bar.s_full + 32, bar.o_full = bar.s_done + 32, bar.o_empty = bar.o_full + 8;
   volatile uint32_t* dead = &dead_flag;
 
@@ -165,23 +341,23 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   if (warp == 0) {
     // ---- loads ----
     if (lane == 0) {
-      Ring ring;
+      Ring ring(b_base, bar.full, sh.stage_units * kUnitBytes, sh.stages);
       int col = 0;  // stage of the column data
       uint32_t a_phase = 1, loads = 0, segs = 0;
       const uint32_t stage_bytes = sh.stage_units * kUnitBytes;
       auto load = [&](const char* from, const float4* cols) {
-        mbar_wait(bar.empty + 8 * ring.stage, ring.phase ^ 1, dead);
-        const uint32_t full = bar.full + 8 * ring.stage;
-        mbar_expect(full, stage_bytes + (cols ? 1024 : 0));
-        bulk_load(b_base + ring.stage * stage_bytes, from, stage_bytes, full);
-        if (cols) bulk_load(col_base + col * 1024, cols, 1024, full);
-        ring.next(sh.stages);
+        mbar_wait(ring.bar + kEmpty, ring.phase ^ 1, dead);
+        if (*dead) return;
+        mbar_expect(ring.bar, stage_bytes + (cols ? 1024 : 0));
+        bulk_load(ring.at, from, stage_bytes, ring.bar);
+        if (cols) bulk_load(col_base + col * 1024, cols, 1024, ring.bar);
+        ring.next();
         ++loads;
       };
       auto scores_units = [&](int64_t tile, const char* from_a) {
         const char* from = a.B + tile * tile_bytes;
         const float4* cols = PASS == Pass::kCols ? a.col + tile * 64 : nullptr;
-        if (sh.stage_units > 1 || sh.nk * PARTS == 1) {
+        if (sh.stage_units == sh.nk * PARTS) {
           load(from, cols);
         } else {
           for (int kc = 0; kc < sh.nk; ++kc) {
@@ -204,6 +380,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         if (sh.res) {
           mbar_wait(bar.a_empty, a_phase, dead);
           a_phase ^= 1;
+          if (*dead) break;
           ++segs;
           mbar_expect(bar.a_full, (uint32_t)(nt * tile_bytes));
           bulk_load(a_base, from_a, (uint32_t)(nt * tile_bytes), bar.a_full);
@@ -226,176 +403,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     }
   } else if (warp == 1) {
     // ---- matrix instructions ----
-    const uint32_t leader = elect_one();
-    constexpr uint32_t idesc_s = mma_desc(BF16, 128, false);
-    const uint32_t idesc_o = mma_desc(BF16, out_cols, true);
-    Ring ring;      // stages taken for scores (and for sums, where B is loaded again)
-    Ring kept;      // stages taken for sums, where B is kept
-    uint32_t done_phase = STATS ? 0xfu : 0u;  // parity to wait for on s_done, a bit per buffer
-    uint32_t a_phase = 0, o_phase = 1;
-    const uint32_t stage_bytes = sh.stage_units * kUnitBytes;
-    const int last_steps = sh.steps - 4 * (sh.nk - 1);  // of a row's last unit
-    auto stage_at = [&](const Ring& r) { return b_base + r.stage * stage_bytes; };
-    auto stage_wait = [&](const Ring& r) { warp_wait(bar.full + 8 * r.stage, r.phase, dead); };
-    auto stage_free = [&](Ring& r) {
-      mma_commit(bar.empty + 8 * r.stage, leader);
-      r.next(sh.stages);
+    auto issue = [&](auto nk) {
+      Issue<PASS, BF16, PARTS, decltype(nk)::value> m(bar, dead, tmem, a_base, b_base, sh.steps, out_cols, out_units);
+      while (walk.next(g)) m.segment(tiles_of(g), g.len);
     };
-    auto done_wait = [&](int buf) {
-      warp_wait(bar.s_done + 8 * buf, (done_phase >> buf) & 1, dead);
-      done_phase ^= 1u << buf;
-      fence_after();
-    };
-    auto sums_begin = [&]() {  // the last segment's sums have been read
-      warp_wait(bar.o_empty, o_phase, dead);
-      o_phase ^= 1;
-      fence_after();
-    };
-    const bool whole = sh.stage_units > 1 || sh.nk * PARTS == 1;  // a stage is a tile of B
-    while (walk.next(g)) {
-      const int nt = tiles_of(g);
-      if (sh.res) {
-        warp_wait(bar.a_full, a_phase, dead);
-        a_phase ^= 1;
-      }
-      if (whole) {
-        // Order of issue: S(0) S(1) O(0) S(2) O(1) ..., so that the exponentials of one
-        // tile of scores run beside the products of the other.
-        const uint32_t a0 = desc_k(a_base), a1 = desc_k(a_base + sh.nk * PARTS * kUnitBytes);
-        auto scores = [&](uint32_t d, uint32_t a, uint32_t b) {
-          switch (sh.steps) {
-            case 1: return scores_mma<PARTS, 1>(d, a, b, idesc_s, leader);
-            case 2: return scores_mma<PARTS, 2>(d, a, b, idesc_s, leader);
-            case 3: return scores_mma<PARTS, 3>(d, a, b, idesc_s, leader);
-            case 4: return scores_mma<PARTS, 4>(d, a, b, idesc_s, leader);
-            case 5: return scores_mma<PARTS, PARTS == 1 ? 5 : 4>(d, a, b, idesc_s, leader);
-            case 6: return scores_mma<PARTS, PARTS == 1 ? 6 : 4>(d, a, b, idesc_s, leader);
-            case 7: return scores_mma<PARTS, PARTS == 1 ? 7 : 4>(d, a, b, idesc_s, leader);
-            default: return scores_mma<PARTS, PARTS == 1 ? 8 : 4>(d, a, b, idesc_s, leader);
-          }
-        };
-        auto sums = [&](int buf, int tile, uint32_t more, bool last) {
-          done_wait(buf);
-          const uint32_t p = tmem + 128 * buf, d = tmem + 256 + 128 * tile, b = desc_mn(stage_at(kept));
-          if constexpr (PARTS == 2) {
-            sums_mma(d, p, 1, b, idesc_o, more, leader);
-            sums_mma(d, p, 0, b + (sh.nk * kUnitBytes >> 4), idesc_o, 1, leader);
-          }
-          sums_mma(d, p, 0, b, idesc_o, PARTS == 2 ? 1 : more, leader);
-          if (last) stage_free(kept);
-        };
-        int n = 0;
-        for (int32_t j = 0; j < g.len; ++j) {
-          stage_wait(ring);
-          fence_after();
-          const uint32_t b = desc_k(stage_at(ring));
-          if (nt == 2) {
-#pragma unroll
-            for (int tile = 0; tile < 2; ++tile) {
-              const int buf = STATS ? (j & 1) * 2 + tile : tile;
-              if (STATS) done_wait(buf);
-              scores(tmem + 128 * buf, tile ? a1 : a0, b);
-              mma_commit(bar.s_full + 8 * buf, leader);
-              if (STATS) continue;
-              if (j == 0 && tile == 1) sums_begin();
-              if (tile == 1) sums(0, 0, j > 0, false);
-              else if (j > 0) sums(1, 1, j > 1, true);
-            }
-            n = 1;
-          } else {
-            const int buf = j & (kBufs - 1);
-            if (STATS) done_wait(buf);
-            scores(tmem + 128 * buf, a0, b);
-            mma_commit(bar.s_full + 8 * buf, leader);
-            if (!STATS && (j == 1 || g.len == 1)) sums_begin();
-            if (!STATS && j > 0) sums(buf ^ 1, 0, j > 1, true);
-            n = j & 1;
-          }
-          if (STATS) stage_free(ring);
-          else ring.next(sh.stages);
-        }
-        if (sh.res) mma_commit(bar.a_empty, leader);
-        if (!STATS) sums(n, nt == 2 ? 1 : 0, g.len > 1, true);
-      } else if (STATS) {
-        // Units of B come one by one and go after their products with both tiles of A.
-        for (int32_t j = 0; j < g.len; ++j) {
-          const int buf = nt == 2 ? (j & 1) * 2 : j & 3;
-          for (int tile = 0; tile < nt; ++tile) done_wait(buf + tile);
-          for (int kc = 0; kc < sh.nk; ++kc) {
-            const int steps = kc == sh.nk - 1 ? last_steps : 4;
-            uint32_t ua[PARTS], ub[PARTS];
-            Ring r = ring;
-            if (!sh.res)
-              for (int p = 0; p < PARTS; ++p) stage_wait(r), ua[p] = desc_k(stage_at(r)), r.next(sh.stages);
-            for (int p = 0; p < PARTS; ++p) stage_wait(r), ub[p] = desc_k(stage_at(r)), r.next(sh.stages);
-            fence_after();
-            for (int tile = 0; tile < nt; ++tile) {
-              const uint32_t d = tmem + 128 * (buf + tile);
-              if (sh.res)
-                for (int p = 0; p < PARTS; ++p) ua[p] = desc_k(a_base + ((tile * PARTS + p) * sh.nk + kc) * kUnitBytes);
-              if constexpr (PARTS == 2) {
-                unit_mma(d, ua[1], ub[0], idesc_s, steps, kc > 0, leader);
-                unit_mma(d, ua[0], ub[1], idesc_s, steps, 1, leader);
-              }
-              unit_mma(d, ua[0], ub[0], idesc_s, steps, PARTS == 2 || kc > 0, leader);
-            }
-            for (int i = 0; i < (sh.res ? 1 : 2) * PARTS; ++i) stage_free(ring);
-          }
-          for (int tile = 0; tile < nt; ++tile) mma_commit(bar.s_full + 8 * (buf + tile), leader);
-        }
-        if (sh.res) mma_commit(bar.a_empty, leader);
-      } else {
-        // One tile of A; units of B stay until their part of the sums is done, or come twice.
-        auto scores = [&](int buf) {
-          const uint32_t d = tmem + 128 * buf;
-          for (int kc = 0; kc < sh.nk; ++kc) {
-            const int steps = kc == sh.nk - 1 ? last_steps : 4;
-            uint32_t ua[PARTS], ub[PARTS];
-            Ring r = ring;
-            for (int p = 0; p < PARTS; ++p) {
-              if (sh.res) ua[p] = desc_k(a_base + (p * sh.nk + kc) * kUnitBytes);
-              else stage_wait(r), ua[p] = desc_k(stage_at(r)), r.next(sh.stages);
-            }
-            for (int p = 0; p < PARTS; ++p) stage_wait(r), ub[p] = desc_k(stage_at(r)), r.next(sh.stages);
-            fence_after();
-            if constexpr (PARTS == 2) {
-              unit_mma(d, ua[1], ub[0], idesc_s, steps, kc > 0, leader);
-              unit_mma(d, ua[0], ub[1], idesc_s, steps, 1, leader);
-            }
-            unit_mma(d, ua[0], ub[0], idesc_s, steps, PARTS == 2 || kc > 0, leader);
-            if (sh.keep) ring = r;
-            else
-              for (int i = 0; i < (sh.res ? 1 : 2) * PARTS; ++i) stage_free(ring);
-          }
-          mma_commit(bar.s_full + 8 * buf, leader);
-        };
-        auto sums = [&](int buf, uint32_t more) {
-          done_wait(buf);
-          const uint32_t p_at = tmem + 128 * buf;
-          Ring& from = sh.keep ? kept : ring;
-          for (int kc = 0; kc < out_units; ++kc) {
-            const uint32_t d = tmem + 256 + 64 * kc, idesc = mma_desc(BF16, min(64, out_cols - 64 * kc), true);
-            for (int p = 0; p < PARTS; ++p) {
-              if (!sh.keep) {
-                stage_wait(from);
-                fence_after();
-              }
-              const uint32_t b = desc_mn(stage_at(from));
-              if (PARTS == 2 && p == 0) sums_mma(d, p_at, 1, b, idesc, more, leader);
-              sums_mma(d, p_at, 0, b, idesc, PARTS == 2 ? 1 : more, leader);
-              stage_free(from);
-            }
-          }
-        };
-        for (int32_t j = 0; j < g.len; ++j) {
-          scores(j & 1);
-          if (j == g.len - 1 && sh.res) mma_commit(bar.a_empty, leader);
-          if (j == 1 || g.len == 1) sums_begin();
-          if (j > 0) sums((j & 1) ^ 1, j > 1);
-        }
-        sums((g.len - 1) & 1, g.len > 1);
-      }
-      if (!STATS) mma_commit(bar.o_full, leader);
+    using std::integral_constant;
+    switch (sh.nk) {
+      case 1: issue(integral_constant<int, 1>{}); break;
+      case 2: issue(integral_constant<int, 2>{}); break;
+      case 3: issue(integral_constant<int, 3>{}); break;
+      case 4: issue(integral_constant<int, 4>{}); break;
+      case 5: issue(integral_constant<int, 5>{}); break;
+      case 6: issue(integral_constant<int, 6>{}); break;
+      case 7: issue(integral_constant<int, 7>{}); break;
+      default: issue(integral_constant<int, 8>{});
     }
     if (*dead) {  // what was issued ends before tensor memory is freed
       const long long begin = clock64();
@@ -412,7 +433,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     // masked ones stay -infinity.)
     const float scale = fminf(fmaxf(ldexpf(a.b * kLog2e, -(shift_h + shift_w)), 1.1754944e-38f), 3.4028235e38f);
     const u64 scale2 = pack2(scale, scale);
-    uint32_t phase = 0, o_phase = 0;  // parities of s_full, a bit per buffer
+    uint32_t phase = 0, o_phase = 0;  // parities of s_full's next turn, a bit per buffer
     int col0 = 0;  // stage of the segment's first column data
     while (walk.next(g)) {
       const int nt = tiles_of(g);
@@ -420,18 +441,24 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       float m = -INFINITY, l = 0.f, at = 0.f;  // kStats: maximum (without the scale), sum, and m scale
       float offset = 0.f;
       if (PASS == Pass::kRows) {
-        const int64_t r = (g.group * sh.tiles + (nt == 2 ? pair : 0)) * 128 + row;
+        const int64_t r = g.group * 128 + row;
         offset = r < rows_a ? (BF16 ? 0.f : kHalfShift) - a.row_max[r] : -1e30f;
       }
-      int col = nt == 2 ? col0 : col0 + pair;
-      for (int32_t n = pair; n < jobs; n += 2) {
-        const int buf = n & (kBufs - 1);
+      // Jobs go to the pairs by turns, and to the buffers by turns: with three buffers
+      // both pairs come by each, so a pair counts the other's turns too.
+      int col = col0, buf = 0;
+      for (int32_t n = 0; n < jobs; ++n) {
+        const int at_buf = buf, at_col = col;
+        if (++buf == sh.buffers) buf = 0;
+        if (++col == sh.stages) col = 0;
+        const uint32_t parity = (phase >> at_buf) & 1;
+        phase ^= 1u << at_buf;
+        if ((n & 1) != pair) continue;
         const int32_t j = nt == 2 ? n >> 1 : n;
-        warp_wait(bar.s_full + 8 * buf, (phase >> buf) & 1, dead);
-        phase ^= 1u << buf;
+        warp_wait(bar.s_full + 8 * at_buf, parity, dead);
         fence_after();
         const int64_t left = rows_b - (g.first + j) * 128 - 64 * half;  // of this half's columns
-        const uint32_t s_at = lanes + 128 * buf + 64 * half;
+        const uint32_t s_at = lanes + 128 * at_buf + 64 * half;
         uint32_t r[2][32];
         tmem_load32(r[0], s_at);
         tmem_load32(r[1], s_at + 32);
@@ -440,7 +467,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         if (STATS) {
           fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar.s_done + 8 * buf);
+          if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);
           if (left < 64) {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
@@ -472,9 +499,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
           l += sum2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
           m = m2, at = at2;
         } else {
-          if (col >= sh.stages) col -= sh.stages;
-          const uint32_t col_at = col_base + col * 1024 + 512 * half;
-          col += nt == 2 ? 1 : 2;
+          const uint32_t col_at = col_base + at_col * 1024 + 512 * half;
           const u64 offset2 = pack2(offset, offset);
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
@@ -508,7 +533,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
           tmem_wait_store();
           fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar.s_done + 8 * buf);
+          if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);
         }
       }
       if (PASS == Pass::kCols) col0 = (col0 + g.len) % sh.stages;
@@ -519,11 +544,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       warp_wait(bar.o_full, o_phase, dead);
       o_phase ^= 1;
       fence_after();
-      const int tile = nt == 2 ? pair : 0;
-      float* to = a.out + ((g.slot * sh.tiles + tile) * 128 + row) * (int64_t)a.ld + blockIdx.y * 256;
-      for (int c = nt == 2 ? half : 2 * pair + half; 16 * c < out_cols; c += nt == 2 ? 2 : 4) {
+      float* to = a.out + (g.slot * 128 + row) * (int64_t)a.ld + blockIdx.y * 256;
+      for (int c = 2 * pair + half; 16 * c < out_cols; c += 4) {
         uint32_t v[16];
-        tmem_load16(v, lanes + 256 + 128 * tile + 16 * c);
+        tmem_load16(v, lanes + 128 * sh.buffers + 16 * c);
         float4* p = reinterpret_cast<float4*>(to + 16 * c);
         float4 y[4];
 #pragma unroll
@@ -564,24 +588,6 @@ cudaError_t launch_type(bool bf16, int parts, const MmaArgs& a, int blocks, int 
 }
 
 }  // namespace
-
-// t units to a tile.  Up to two, a stage of the ring is a tile of B and two tiles of A
-// share it.  Above, stages are units: a tile of B is then never waited for as a whole
-// (K = 256, bf16: with two stages of 64 KB a tile waited 940 of 3150 cycles).  Two tiles
-// of A share those too where only their scores are wanted and three units are left.
-MmaShape mma_shape(Pass pass, int32_t D, int parts) {
-  MmaShape s{};
-  s.steps = (D + 15) / 16;
-  s.nk = (D + 63) / 64;
-  const int t = s.nk * parts;
-  const bool stats = pass == Pass::kStats;
-  s.tiles = t <= 2 || (stats && 2 * t + 3 <= kUnits) ? 2 : 1;
-  s.res = s.tiles * t + (parts == 2 ? 4 : 3) <= kUnits || s.tiles == 2;
-  s.keep = t <= 2 || (s.res && 3 * t <= kUnits);
-  s.stage_units = t <= 2 ? t : 1;
-  s.stages = (kUnits - (s.res ? s.tiles * t : 0)) / s.stage_units;
-  return s;
-}
 
 cudaError_t launch_mma(Pass pass, bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st) {
   if (pass == Pass::kStats) return launch_type<Pass::kStats>(bf16, parts, a, blocks, 1, st);

@@ -17,14 +17,35 @@ constexpr int kUnits = 13;             // units of shared memory
 constexpr float kHalfShift = 14.f;     // fp16 probabilities are kept 2^14 times as large
 constexpr int kMmaThreads = 640;       // a warp that loads, one that multiplies, two spare, two groups of eight
 
-// How a pass uses shared memory: A's units stay (res) or come with every tile of B,
-// for one or two tiles of A at once (tiles); a stage holds a whole tile of B, kept
-// from the scores to the sums (keep), or one unit, loaded again for the sums.
+// How a pass uses shared and tensor memory: A's units stay (res) or come with every
+// tile of B, for one or two tiles of A at once (tiles); a stage of the ring holds
+// stage_units; B is kept from the scores to the sums (keep) or loaded again for them;
+// `buffers` tiles of scores are in tensor memory.
+//
+// Up to two units a row (t), a stage is a tile of B.  Above, stages are units: a tile
+// of B is then never waited for as a whole (K = 256, bf16: with two stages of 64 KB a
+// tile waited 940 of 3150 cycles).  Two tiles of A share B where only the scores are
+// wanted and three units are left for it; with sums, a third buffer of scores is worth
+// more than sharing.
 struct MmaShape {
   int nk, steps;       // units and 16-value steps of a row
   int tiles, res, keep;
-  int stage_units, stages;
+  int stage_units, stages, buffers;
 };
+__host__ __device__ constexpr MmaShape mma_shape(Pass pass, int32_t D, int parts) {
+  MmaShape s{};
+  s.steps = (D + 15) / 16;
+  s.nk = (D + 63) / 64;
+  const int t = s.nk * parts;
+  const bool stats = pass == Pass::kStats;
+  s.tiles = stats && 2 * t + 3 <= kUnits ? 2 : 1;
+  s.res = s.tiles == 2 || t + (parts == 2 ? 4 : 3) <= kUnits;
+  s.keep = s.res && 3 * t <= kUnits;
+  s.stage_units = t <= 2 ? t : 1;
+  s.stages = (kUnits - (s.res ? s.tiles * t : 0)) / s.stage_units;
+  s.buffers = stats ? 4 : t <= 2 ? 3 : 2;
+  return s;
+}
 
 struct MmaArgs {
   const char *A, *B;
@@ -35,7 +56,7 @@ struct MmaArgs {
   const float* row_max;  // kRows
   const float4* col;     // kCols: two columns each, (-maximum, -maximum, factor, factor)
   float2* stat;          // kStats out: [slot][4][128], by group and half of the columns
-  float* out;            // else: [slot][tiles][128][ld]
+  float* out;            // else: [slot][128][ld]
   int ld;
   int run;               // tiles of B between two additions to `out`
   uint32_t* status;
@@ -70,6 +91,5 @@ __device__ __forceinline__ int weight_shift_of(uint32_t max_bits) {
 }
 
 cudaError_t launch_mma(Pass pass, bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st);
-MmaShape mma_shape(Pass pass, int32_t D, int parts);
 
 }  // namespace esspt

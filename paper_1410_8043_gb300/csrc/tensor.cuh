@@ -36,9 +36,9 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 // Waits end: after kWaitCycles (some seconds), or once another thread of the block
-// gave up, *dead is set and the wait returns as if it had succeeded.  Every loop is
-// finite and every address is in bounds whatever the tiles hold, so the block then
-// runs to its end, on values that mean nothing, and reports that.
+// gave up, *dead is set and the wait returns as if it had succeeded.  Nothing more is
+// loaded then; every loop is finite and every address is in bounds whatever the tiles
+// hold, so the block runs to its end, on values that mean nothing, and reports that.
 constexpr long long kWaitCycles = 6'000'000'000ll;
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead) {
   if (mbar_try(bar, parity)) return;

@@ -142,6 +142,16 @@ def test_distill_shapes(T, V, D, top, dtype):
     _check(_run("distill", h, w, ids, z, weight, 0.5, backward=False), ref, dtype, D, 0.5)
 
 
+# Streams of many tiles per block: rings of stages and buffers go round several times.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,D", [(300, 150_001, 40), (2000, 60_000, 100), (9000, 3000, 60), (400, 90_000, 150), (300, 60_001, 250),
+                                   (300, 60_000, 300), (5000, 4000, 510)])
+def test_long_streams(T, V, D, dtype):
+    h, w, ids, z, weight = _inputs(T, V, D, dtype, 2, T + V + D)
+    ref = _reference(h, w, ids, z, weight, 1.0)
+    _check(_run("distill", h, w, ids, z, weight, 1.0), ref, dtype, D, 1.0)
+
+
 SIDES = [(8, 700, 32), (200, 700, 32)]  # a few rows, and more
 
 
