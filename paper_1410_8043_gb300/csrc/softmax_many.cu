@@ -67,21 +67,27 @@ __global__ void __launch_bounds__(1024) compact_kernel(Many f) {
   else if (t == 0) f.s.words->max_weight = __float_as_uint(1.f);
 }
 
-// Largest finite magnitude of W, and of the kept rows of H (blockIdx.y = 1).
+// Largest finite magnitude of W, and of the kept rows of H (blockIdx.y = 1): a warp
+// takes rows as they come, or a matrix without gaps as one long row in parts of 4096.
 template <int VEC>
 __global__ void __launch_bounds__(256) max_kernel(Many f) {
   const SoftmaxArgs& a = f.a;
   const bool is_h = blockIdx.y == 1;
   const float* x = static_cast<const float*>(is_h ? a.h : a.w);
-  const int64_t rows = is_h ? f.s.words->rows : a.V, stride = is_h ? a.h_stride : a.w_stride;
-  const int32_t slices = a.D / VEC;
+  const int64_t stride = is_h ? a.h_stride : a.w_stride, n = is_h ? f.s.words->rows : a.V;
+  const bool flat = !is_h && stride == a.D;
+  const int64_t rows = flat ? (n * a.D + 4095) / 4096 : n;
   uint32_t top = 0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * slices; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / slices;
-    float v[VEC];
-    load_vec<float, VEC>(x + (is_h ? f.s.act[r] : r) * stride + (i - r * slices) * VEC, v);
+  for (int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; r < rows; r += (int64_t)gridDim.x * 8) {
+    const float* row = x + (flat ? r * 4096 : (is_h ? f.s.act[r] : r) * stride);
+    const int len = flat ? (int)min((int64_t)4096, n * a.D - r * 4096) : a.D;
+#pragma unroll 8
+    for (int d = (threadIdx.x & 31) * VEC; d < len; d += 32 * VEC) {
+      float v[VEC];
+      load_vec<float, VEC>(row + d, v);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) top = max(top, finite_bits(v[e]));
+      for (int e = 0; e < VEC; ++e) top = max(top, finite_bits(v[e]));
+    }
   }
   block_max(top, is_h ? &f.s.words->max_h : &f.s.words->max_w);
 }
@@ -401,50 +407,82 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
   }
 }
 
-// dw, a warp per item: b (sum weight p h - sum weight q h).
+// dw: b (sum weight p h - sum weight q h), kItems items to a block.  Most items are
+// nobody's target: those rows go through all threads side by side, the others a warp each.
+constexpr int kItems = 64;
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) grad_w_kernel(Many f, const uint32_t* key, const uint32_t* val) {
+  __shared__ int32_t first[kItems + 1];
+  __shared__ int64_t slots[2];
   const SoftmaxArgs& a = f.a;
-  const int64_t v = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-  const int lane = threadIdx.x & 31;
-  if (v >= a.V) return;
-  const int64_t rows = f.s.words->rows;
-  const int shift = cols_shift(f);
-  int32_t begin = f.s.tile_first[v / 128], end = f.s.tile_first[v / 128 + 1];
-  if (begin < end) {  // the item's own among the tile's
-    int32_t hi = end;
-    while (begin < hi) {
-      const int32_t mid = (begin + hi) / 2;
-      if (key[mid] < (uint32_t)v) begin = mid + 1;
+  const int64_t v0 = (int64_t)blockIdx.x * kItems, rows = f.s.words->rows;
+  const int lane = threadIdx.x & 31, items = (int)min((int64_t)kItems, a.V - v0);
+  if (threadIdx.x <= items) {
+    int32_t lo = f.s.tile_first[v0 / 128], hi = f.s.tile_first[v0 / 128 + 1];
+    while (lo < hi) {
+      const int32_t mid = (lo + hi) / 2;
+      if (key[mid] < (uint32_t)(v0 + threadIdx.x)) lo = mid + 1;
       else hi = mid;
     }
-    for (hi = begin; hi < end;) {
-      const int32_t mid = (hi + end) / 2;
-      if (key[mid] <= (uint32_t)v) hi = mid + 1;
-      else end = mid;
+    first[threadIdx.x] = lo;
+  }
+  if (threadIdx.x == 0) {
+    slots[0] = 1, slots[1] = 0;
+    if (rows > 0) {
+      const Ranges r(a.V, rows, 1, f.blocks);
+      const int64_t g = v0 / 128;
+      slots[0] = r.block_of(g * r.n_b) + g, slots[1] = r.block_of((g + 1) * r.n_b - 1) + g;
     }
   }
-  // Whole runs [r0, r1), whole runs of runs [q0, q1), and single entries at both ends, one per lane.
-  int32_t r0 = (begin + kRun - 1) / kRun, r1 = end / kRun;
-  int32_t head = r0 * kRun - begin, tail = end - r1 * kRun;
-  if (r0 >= r1) r0 = r1 = 0, head = end - begin, tail = 0;
-  int32_t q0 = (r0 + kRun - 1) / kRun, q1 = r1 / kRun;
-  if (q0 >= q1) q0 = q1 = 0;
-  int32_t t = 0;
-  float g = 0.f;
-  if (lane < head + tail) g = entry_factor<T>(f, shift, val[lane < head ? begin + lane : end - tail + lane - head], t);
-  for (int d = lane * VEC; d - lane * VEC < a.D; d += 32 * VEC) {
-    float x[VEC], y[VEC];
+  __syncthreads();
+  const int shift = cols_shift(f);
+  auto sum = [&](int item, int d, float (&x)[VEC]) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = y[e] = 0.f;
-    if (rows > 0 && d < a.D) add_slots<VEC>(f, a.V, rows, v, d, x);
-    add_rows<T, VEC>(a, head + tail, t, g, d, y);
-    add_sums<VEC>(f.s.run_sum[0], r0, q0 < q1 ? q0 * kRun : r1, a.D, d, y);
-    add_sums<VEC>(f.s.run_sum[0], q0 < q1 ? q1 * kRun : r1, r1, a.D, d, y);
-    add_sums<VEC>(f.s.run_sum[1], q0, q1, a.D, d, y);
+    for (int e = 0; e < VEC; ++e) x[e] = 0.f;
+    for (int64_t s = slots[0]; s <= slots[1]; ++s) {
+      float y[VEC];
+      load_vec<float, VEC>(f.s.out + (s * 128 + v0 % 128 + item) * f.ld + d, y);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = a.b * (ldexpf(x[e], shift) - y[e]);
-    if (d < a.D) store_vec<T, VEC>(static_cast<T*>(a.grad_w) + v * a.D + d, x);
+      for (int e = 0; e < VEC; ++e) x[e] += y[e];
+    }
+  };
+  T* to = static_cast<T*>(a.grad_w) + v0 * a.D;
+  const int slices = a.D / VEC;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < items * slices; i += 256) {
+    const int item = i / slices, d = (i - item * slices) * VEC;
+    if (first[item] != first[item + 1]) continue;
+    float x[VEC];
+    sum(item, d, x);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = a.b * ldexpf(x[e], shift);
+    store_vec<T, VEC>(to + item * a.D + d, x);
+  }
+  for (int item = threadIdx.x / 32; item < items; item += 8) {
+    const int32_t begin = first[item], end = first[item + 1];
+    if (begin == end) continue;
+    // Whole runs [r0, r1), whole runs of runs [q0, q1), and single entries at both ends, one per lane.
+    int32_t r0 = (begin + kRun - 1) / kRun, r1 = end / kRun;
+    int32_t head = r0 * kRun - begin, tail = end - r1 * kRun;
+    if (r0 >= r1) r0 = r1 = 0, head = end - begin, tail = 0;
+    int32_t q0 = (r0 + kRun - 1) / kRun, q1 = r1 / kRun;
+    if (q0 >= q1) q0 = q1 = 0;
+    int32_t t = 0;
+    float g = 0.f;
+    if (lane < head + tail) g = entry_factor<T>(f, shift, val[lane < head ? begin + lane : end - tail + lane - head], t);
+    for (int d = lane * VEC; d - lane * VEC < a.D; d += 32 * VEC) {
+      float x[VEC], y[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[e] = y[e] = 0.f;
+      if (d < a.D) sum(item, d, x);
+      add_rows<T, VEC>(a, head + tail, t, g, d, y);
+      add_sums<VEC>(f.s.run_sum[0], r0, q0 < q1 ? q0 * kRun : r1, a.D, d, y);
+      add_sums<VEC>(f.s.run_sum[0], q0 < q1 ? q1 * kRun : r1, r1, a.D, d, y);
+      add_sums<VEC>(f.s.run_sum[1], q0, q1, a.D, d, y);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[e] = a.b * (ldexpf(x[e], shift) - y[e]);
+      if (d < a.D) store_vec<T, VEC>(to + item * a.D + d, x);
+    }
   }
 }
 
@@ -517,7 +555,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
 
   m.A = s.units_w, m.B = s.units_h;
   if ((e = launch_mma(Pass::kCols, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
-  grad_w_kernel<T, VEC><<<(unsigned)((a.V + 7) / 8), 256, 0, a.st>>>(f, key.Current(), val.Current());
+  grad_w_kernel<T, VEC><<<(unsigned)(((int64_t)a.V + kItems - 1) / kItems), 256, 0, a.st>>>(f, key.Current(), val.Current());
   return cudaGetLastError();
 }
 

@@ -20,13 +20,14 @@ namespace esspt {
 
 namespace {
 
-struct Segment {  // consecutive tiles of B for one group
+// Consecutive tiles of B for one group, all for one slot, cut into runs of a.run.
+struct Run {
   int64_t slot, group, first;
   int32_t len;
-  bool add;  // an earlier segment of the block has the same slot
+  bool begins, ends;  // the slot's first run, its last
 };
 
-// The block's segments in order, the same for every warp.
+// The block's runs in order, the same for every warp.
 struct Walk {
   Ranges r;
   int64_t u, begin, end;
@@ -35,13 +36,20 @@ struct Walk {
     begin = u = blockIdx.x < r.blocks ? r.begin(blockIdx.x) : 0;
     end = blockIdx.x < r.blocks ? r.begin(blockIdx.x + 1) : 0;
   }
-  __device__ bool next(Segment& s) {
+  __device__ bool next(Run& s) {
     if (u >= end) return false;
-    s.group = u / r.n_b;
-    s.first = u - s.group * r.n_b;
-    s.slot = blockIdx.x + s.group;
-    s.len = (int32_t)min(min(r.n_b - s.first, end - u), (int64_t)run);
-    s.add = s.first != 0 && u != begin;
+    if (u == begin || s.ends) {
+      s.group = u / r.n_b;
+      s.first = u - s.group * r.n_b;
+      s.slot = blockIdx.x + s.group;
+      s.begins = true;
+    } else {
+      s.first += s.len;
+      s.begins = false;
+    }
+    const int64_t left = min(r.n_b - s.first, end - u);
+    s.len = (int32_t)min(left, (int64_t)run);
+    s.ends = s.len == left;
     u += s.len;
     return true;
   }
@@ -71,27 +79,6 @@ __device__ __forceinline__ uint32_t pack16_rest(uint32_t p, float lo, float hi) 
   return pack16<false>(lo - f.x, hi - f.y);
 }
 
-// STEPS products of 16 values over units that follow each other, written out: with
-// conditions or loops in between the issue of an instruction took 60 to 120 cycles
-// (here 17) where it runs for 64.
-template <int STEPS>
-__device__ __forceinline__ void steps_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add, uint32_t leader) {
-  constexpr uint32_t kUnit = kUnitBytes >> 4;
-#pragma unroll
-  for (int k = 0; k < STEPS; ++k)
-    mma_ss(d, a + k / 4 * kUnit + k % 4 * 2, b + k / 4 * kUnit + k % 4 * 2, idesc, k > 0 ? 1u : add, leader);
-}
-// Scores of a tile of A and one of B: products of halves in the order of their size,
-// (lo, hi), (hi, lo), (hi, hi).
-template <int PARTS, int STEPS>
-__device__ __forceinline__ void scores_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t leader) {
-  if constexpr (PARTS == 2) {
-    constexpr uint32_t kHalf = (kUnitBytes >> 4) * ((STEPS + 3) / 4);
-    steps_mma<STEPS>(d, a + kHalf, b, idesc, 0, leader);
-    steps_mma<STEPS>(d, a, b + kHalf, idesc, 1, leader);
-  }
-  steps_mma<STEPS>(d, a, b, idesc, PARTS == 2, leader);
-}
 // Sums: the 128 probabilities of every row (half `part`) times units of B.
 __device__ __forceinline__ void sums_mma(uint32_t d, uint32_t p, int part, uint32_t b, uint32_t idesc, uint32_t add,
                                          uint32_t leader) {
@@ -249,8 +236,9 @@ struct Issue {
       }
     }
   }
-  __device__ __forceinline__ void segment(int nt, int32_t len) {
-    if (S.res) {
+  __device__ __forceinline__ void run(int nt, const Run& g) {
+    const int32_t len = g.len;
+    if (S.res && g.begins) {
       warp_wait(bar.a_full, a_phase, dead);
       a_phase ^= 1;
     }
@@ -277,11 +265,11 @@ struct Issue {
       auto ahead = [&](bool last) {
         scores<1>(tmem + 128 * next);
         mma_commit(bar.s_full + 8 * next, leader);
-        if (last && S.res) mma_commit(bar.a_empty, leader);
+        if (last && S.res && g.ends) mma_commit(bar.a_empty, leader);
         if (++next == S.buffers) next = 0;
       };
       for (int32_t j = 0; j < (int32_t)kAhead && j < len; ++j) ahead(j == len - 1);
-      warp_wait(bar.o_empty, o_phase, dead);  // the last segment's sums have been read
+      warp_wait(bar.o_empty, o_phase, dead);  // the last run's sums have been read
       o_phase ^= 1;
       fence_after();
       for (int32_t j = 0; j < len; ++j) {
@@ -333,9 +321,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   const int out_units = min(4, sh.nk - out_unit);
   const int out_cols = min(256, sh.steps * 16 - (int)blockIdx.y * 256);
   Walk walk(ranges, a.run);
-  Segment g;
+  Run g;
   // A group's last tile may lie outside: then the groups of warps share the first.
-  auto tiles_of = [&](const Segment& s) { return sh.tiles == 2 && (s.group * 2 + 1) * 128 < rows_a ? 2 : 1; };
+  auto tiles_of = [&](const Run& s) { return sh.tiles == 2 && (s.group * 2 + 1) * 128 < rows_a ? 2 : 1; };
   const int64_t tile_bytes = (int64_t)sh.nk * PARTS * kUnitBytes;
 
   if (warp == 0) {
@@ -377,7 +365,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       while (walk.next(g)) {
         const int nt = tiles_of(g);
         const char* from_a = a.A + g.group * sh.tiles * tile_bytes;
-        if (sh.res) {
+        if (sh.res && g.begins) {
           mbar_wait(bar.a_empty, a_phase, dead);
           a_phase ^= 1;
           if (*dead) break;
@@ -405,7 +393,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     // ---- matrix instructions ----
     auto issue = [&](auto nk) {
       Issue<PASS, BF16, PARTS, decltype(nk)::value> m(bar, dead, tmem, a_base, b_base, sh.steps, out_cols, out_units);
-      while (walk.next(g)) m.segment(tiles_of(g), g.len);
+      while (walk.next(g)) m.run(tiles_of(g), g);
     };
     using std::integral_constant;
     switch (sh.nk) {
@@ -434,7 +422,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const float scale = fminf(fmaxf(ldexpf(a.b * kLog2e, -(shift_h + shift_w)), 1.1754944e-38f), 3.4028235e38f);
     const u64 scale2 = pack2(scale, scale);
     uint32_t phase = 0, o_phase = 0;  // parities of s_full's next turn, a bit per buffer
-    int col0 = 0;  // stage of the segment's first column data
+    int col0 = 0;  // stage of the run's first column data
+    // fp32 rows of up to 128 values: a thread's sums over the runs so far (two times 16
+    // columns) are kept in registers, else where they go.
+    constexpr int kKept = PARTS == 2 && !STATS ? 2 : 0;
+    float kept[kKept > 0 ? kKept : 1][16];
     while (walk.next(g)) {
       const int nt = tiles_of(g);
       const int32_t jobs = nt * g.len;
@@ -459,12 +451,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         fence_after();
         const int64_t left = rows_b - (g.first + j) * 128 - 64 * half;  // of this half's columns
         const uint32_t s_at = lanes + 128 * at_buf + 64 * half;
-        uint32_t r[2][32];
+        // (fp32 rows: one half at a time, for the registers that hold sums.)
+        constexpr bool kBoth = STATS || PARTS == 1;
+        uint32_t r[kBoth ? 2 : 1][32];
         tmem_load32(r[0], s_at);
-        tmem_load32(r[1], s_at + 32);
+        if constexpr (kBoth) {
+          tmem_load32(r[1], s_at + 32);
+          tmem_loaded(r[1]);
+        }
         tmem_loaded(r[0]);
-        tmem_loaded(r[1]);
-        if (STATS) {
+        if constexpr (STATS) {
           fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);
@@ -504,9 +500,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             uint32_t out[16 * PARTS];
+            if (!kBoth && c == 1) {
+              tmem_load32(r[0], s_at + 32);
+              tmem_loaded(r[0]);
+            }
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              const u64 s2 = pack2(__uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1]));
+              const u64 s2 = pack2(__uint_as_float(r[kBoth ? c : 0][i]), __uint_as_float(r[kBoth ? c : 0][i + 1]));
               float p[2];
               if (PASS == Pass::kRows) {
                 unpack2(fma2(s2, scale2, offset2), p[0], p[1]);
@@ -545,13 +545,39 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       o_phase ^= 1;
       fence_after();
       float* to = a.out + (g.slot * 128 + row) * (int64_t)a.ld + blockIdx.y * 256;
+      const uint32_t o_at = lanes + 128 * sh.buffers;
+      if (kKept > 0 && out_cols <= 64 * kKept) {
+#pragma unroll
+        for (int k = 0; k < kKept; ++k) {
+          const int c = 4 * k + 2 * pair + half;
+          if (16 * c >= out_cols) break;
+          uint32_t v[16];
+          tmem_load16(v, o_at + 16 * c);
+          tmem_loaded(v);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) kept[k][i] = g.begins ? __uint_as_float(v[i]) : kept[k][i] + __uint_as_float(v[i]);
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar.o_empty);
+        if (!g.ends) continue;
+#pragma unroll
+        for (int k = 0; k < kKept; ++k) {
+          const int c = 4 * k + 2 * pair + half;
+          if (16 * c >= out_cols) break;
+          float4* p = reinterpret_cast<float4*>(to + 16 * c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = make_float4(kept[k][4 * i], kept[k][4 * i + 1], kept[k][4 * i + 2], kept[k][4 * i + 3]);
+        }
+        continue;
+      }
       for (int c = 2 * pair + half; 16 * c < out_cols; c += 4) {
         uint32_t v[16];
-        tmem_load16(v, lanes + 128 * sh.buffers + 16 * c);
+        tmem_load16(v, o_at + 16 * c);
         float4* p = reinterpret_cast<float4*>(to + 16 * c);
         float4 y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = g.add ? p[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < 4; ++i) y[i] = g.begins ? make_float4(0.f, 0.f, 0.f, 0.f) : p[i];
         tmem_loaded(v);
 #pragma unroll
         for (int i = 0; i < 4; ++i)

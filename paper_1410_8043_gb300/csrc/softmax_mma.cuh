@@ -58,7 +58,7 @@ struct MmaArgs {
   float2* stat;          // kStats out: [slot][4][128], by group and half of the columns
   float* out;            // else: [slot][128][ld]
   int ld;
-  int run;               // tiles of B between two additions to `out`
+  int run;               // tiles of B that the tensor core sums up before fp32 does
   uint32_t* status;
 };
 
