@@ -535,7 +535,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   // with 32 tiles, 1.6e-6 with 16, 8.5e-7 with 8 (7.5e-7 by fp32 products of whole
   // matrices), 4.2e-7 with 4; the call takes 478, 484, 496 and 512 us.
   const int out_chunks = (a.D + 255) / 256;
-  m.run = kParts == 2 ? 8 : 128;
+  m.run = kParts == 1 ? 128 : mma_shape(Pass::kRows, a.D, kParts).cross ? 16 : 8;
   m.s = f.shape = mma_shape(Pass::kRows, a.D, kParts);
   if ((e = launch_mma(Pass::kRows, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
   grad_h_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);

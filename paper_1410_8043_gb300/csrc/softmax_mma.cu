@@ -210,13 +210,14 @@ struct Issue {
   __device__ __forceinline__ void sums(uint32_t buf, uint32_t more) {
     done(buf);
     const uint32_t p = tmem + 128 * buf, d = tmem + 128 * S.buffers;
-    if constexpr (S.stage_units == NK * PARTS) {
-      const uint32_t b = desc_mn(kept.at), idesc = mma_desc(BF16, out_cols, true);
-      if constexpr (PARTS == 2) {
-        sums_mma(d, p, 1, b, idesc, more, leader);
-        sums_mma(d, p, 0, b + NK * kUnit, idesc, 1, leader);
-      }
-      sums_mma(d, p, 0, b, idesc, PARTS == 2 ? 1 : more, leader);
+    if constexpr (PARTS == 2 && NK == 1) {
+      // hi (hi | lo): the two units are the halves of 128 columns, the sums too.
+      const uint32_t b = desc_mn(kept.at);
+      sums_mma(d, p, 0, b, mma_desc(BF16, 128, true), more, leader);
+      sums_mma(d + 64, p, 1, b, mma_desc(BF16, out_cols, true), 1, leader);
+      free(kept);
+    } else if constexpr (S.stage_units == NK * PARTS) {
+      sums_mma(d, p, 0, desc_mn(kept.at), mma_desc(BF16, out_cols, true), more, leader);
       free(kept);
     } else {
       Ring& from = S.keep ? kept : ring;
@@ -229,8 +230,9 @@ struct Issue {
         for (int part = 0; part < PARTS; ++part) {
           if (!S.keep) take(from);
           const uint32_t b = desc_mn(from.at);
-          if (PARTS == 2 && part == 0) sums_mma(d + 64 * kc, p, 1, b, idesc, more, leader);
-          sums_mma(d + 64 * kc, p, 0, b, idesc, PARTS == 2 ? 1 : more, leader);
+          const uint32_t cross = d + 64 * kc + (S.cross ? 64 * NK : 0);
+          if (PARTS == 2 && part == 0) sums_mma(cross, p, 1, b, idesc, more, leader);
+          sums_mma(part == 0 ? d + 64 * kc : cross, p, 0, b, idesc, part == 1 || (PARTS == 2 && !S.cross) ? 1 : more, leader);
           free(from);
         }
       }
@@ -546,16 +548,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       fence_after();
       float* to = a.out + (g.slot * 128 + row) * (int64_t)a.ld + blockIdx.y * 256;
       const uint32_t o_at = lanes + 128 * sh.buffers;
-      if (kKept > 0 && out_cols <= 64 * kKept) {
+      if (kKept > 0 && sh.cross) {
 #pragma unroll
         for (int k = 0; k < kKept; ++k) {
           const int c = 4 * k + 2 * pair + half;
           if (16 * c >= out_cols) break;
-          uint32_t v[16];
+          uint32_t v[16], x[16];
           tmem_load16(v, o_at + 16 * c);
+          tmem_load16(x, o_at + 64 * sh.nk + 16 * c);
           tmem_loaded(v);
+          tmem_loaded(x);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) kept[k][i] = g.begins ? __uint_as_float(v[i]) : kept[k][i] + __uint_as_float(v[i]);
+          for (int i = 0; i < 16; ++i)
+            kept[k][i] = (g.begins ? 0.f : kept[k][i]) + (__uint_as_float(v[i]) + __uint_as_float(x[i]));
         }
         fence_before();
         __syncwarp();

@@ -31,6 +31,7 @@ struct MmaShape {
   int nk, steps;       // units and 16-value steps of a row
   int tiles, res, keep;
   int stage_units, stages, buffers;
+  int cross;           // sums of products of halves hi lo and lo hi have columns of their own
 };
 __host__ __device__ constexpr MmaShape mma_shape(Pass pass, int32_t D, int parts) {
   MmaShape s{};
@@ -44,6 +45,7 @@ __host__ __device__ constexpr MmaShape mma_shape(Pass pass, int32_t D, int parts
   s.stage_units = t <= 2 ? t : 1;
   s.stages = (kUnits - (s.res ? s.tiles * t : 0)) / s.stage_units;
   s.buffers = stats ? 4 : t <= 2 ? 3 : 2;
+  s.cross = !stats && parts == 2 && s.nk <= 2;
   return s;
 }
 
