@@ -180,16 +180,22 @@ struct Issue {
       if (STATS) free(ring);
       else ring.next();
     } else {
+      auto unit = [&](Ring& r) {
+        take(r);
+        const uint32_t at = desc_k(r.at);
+        r.next();
+        return at;
+      };
 #pragma unroll
       for (int kc = 0; kc < NK; ++kc) {
         Ring r = ring;
         uint32_t ua[2] = {a_base + kc * kUnit, a_base + (NK + kc) * kUnit}, ub[2] = {0, 0};
         if constexpr (!S.res) {
 #pragma unroll
-          for (int p = 0; p < PARTS; ++p) take(r), ua[p] = desc_k(r.at), r.next();
+          for (int p = 0; p < PARTS; ++p) ua[p] = unit(r);
         }
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) take(r), ub[p] = desc_k(r.at), r.next();
+        for (int p = 0; p < PARTS; ++p) ub[p] = unit(r);
 #pragma unroll
         for (int tile = 0; tile < NT; ++tile) {
           if (kc < NK - 1)
@@ -300,6 +306,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   const uint32_t base = (smem_addr(smem) + 1023u) & ~1023u;
   const uint32_t a_base = base, b_base = base + (sh.res ? sh.tiles * sh.nk * PARTS : 0) * kUnitBytes;
   const uint32_t col_base = base + kUnits * kUnitBytes;  // [stages] of the columns' data
+  const char* col_data = smem + (col_base - smem_addr(smem));
   const uint32_t bar0 = col_base + kUnits * 1024;
   Bars bar;
   bar.full = bar0, bar.empty = bar.full + kEmpty, bar.a_full = bar.empty + 8 * kUnits, bar.a_empty = bar.a_full + 8;
@@ -456,56 +463,48 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         // (fp32 rows: one half at a time, for the registers that hold sums.)
         constexpr bool kBoth = STATS || PARTS == 1;
         uint32_t r[kBoth ? 2 : 1][32];
-        tmem_load32(r[0], s_at);
-        if constexpr (kBoth) {
-          tmem_load32(r[1], s_at + 32);
-          tmem_loaded(r[1]);
-        }
-        tmem_loaded(r[0]);
+        if constexpr (kBoth) tmem_load(r[0], s_at, r[1], s_at + 32);
+        else tmem_load(r[0], s_at);
         if constexpr (STATS) {
           fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);
-          if (left < 64) {
+        }
+        if constexpr (STATS) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+          for (int c = 0; c < 2; ++c) {
+            if (left < 64) {
 #pragma unroll
               for (int i = 0; i < 32; ++i)
                 if (32 * c + i >= left) r[c][i] = 0xff800000u;
-          }
-          float top[4] = {m, m, m, m};
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
+            }
+            float top[4] = {m, m, m, m};
 #pragma unroll
             for (int i = 0; i < 32; i += 2)
               top[(i >> 1) & 3] = fmaxf(fmaxf(top[(i >> 1) & 3], __uint_as_float(r[c][i])), __uint_as_float(r[c][i + 1]));
-          const float m2 = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-          const float at2 = m2 == -INFINITY ? 0.f : m2 * scale;
-          const u64 minus = pack2(-at2, -at2);
-          u64 sum[4] = {0ull, 0ull, 0ull, 0ull};
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
+            const float m2 = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            const float at2 = m2 == -INFINITY ? 0.f : m2 * scale;
+            const u64 minus = pack2(-at2, -at2);
+            u64 sum[2] = {0ull, 0ull};
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
               float x, y;
               unpack2(fma2(pack2(__uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1])), scale2, minus), x, y);
-              sum[(i >> 1) & 3] = add2(sum[(i >> 1) & 3], pack2(exp2_fast(x), exp2_fast(y)));
+              sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(exp2_fast(x), exp2_fast(y)));
             }
-          // (The same maximum again has to leave l as it is: a factor off by its rounding
-          // drifted by 7e-6 over 800 tiles.)
-          if (m2 != m) l = m == -INFINITY ? 0.f : l * exp2_fast(at - at2);
-          l += sum2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
-          m = m2, at = at2;
+            // (The same maximum again has to leave l as it is: a factor off by its rounding
+            // drifted by 7e-6 over 800 tiles.)
+            const float keep = m2 == m ? 1.f : m == -INFINITY ? 0.f : exp2_fast(at - at2);
+            l = fmaf(l, keep, sum2(add2(sum[0], sum[1])));
+            m = m2, at = at2;
+          }
         } else {
-          const uint32_t col_at = col_base + at_col * 1024 + 512 * half;
+          const ulonglong2* cols = reinterpret_cast<const ulonglong2*>(col_data + at_col * 1024 + 512 * half);
           const u64 offset2 = pack2(offset, offset);
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             uint32_t out[16 * PARTS];
-            if (!kBoth && c == 1) {
-              tmem_load32(r[0], s_at + 32);
-              tmem_loaded(r[0]);
-            }
+            if (!kBoth && c == 1) tmem_load(r[0], s_at + 32);
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
               const u64 s2 = pack2(__uint_as_float(r[kBoth ? c : 0][i]), __uint_as_float(r[kBoth ? c : 0][i + 1]));
@@ -519,10 +518,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
                     if (32 * c + i + e >= left) p[e] = 0.f;
                 }
               } else {
-                u64 minus, factor;
-                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(minus), "=l"(factor) : "r"(col_at + 8 * (32 * c + i)));
-                unpack2(fma2(s2, scale2, minus), p[0], p[1]);
-                unpack2(mul2(pack2(exp2_fast(p[0]), exp2_fast(p[1])), factor), p[0], p[1]);
+                const ulonglong2 q = cols[16 * c + i / 2];
+                unpack2(fma2(s2, scale2, q.x), p[0], p[1]);
+                unpack2(mul2(pack2(exp2_fast(p[0]), exp2_fast(p[1])), q.y), p[0], p[1]);
               }
               out[i / 2] = pack16<BF16>(p[0], p[1]);
               if constexpr (PARTS == 2) out[16 + i / 2] = pack16_rest(out[i / 2], p[0], p[1]);
@@ -554,10 +552,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
           const int c = 4 * k + 2 * pair + half;
           if (16 * c >= out_cols) break;
           uint32_t v[16], x[16];
-          tmem_load16(v, o_at + 16 * c);
-          tmem_load16(x, o_at + 64 * sh.nk + 16 * c);
-          tmem_loaded(v);
-          tmem_loaded(x);
+          tmem_load(v, o_at + 16 * c, x, o_at + 64 * sh.nk + 16 * c);
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             kept[k][i] = (g.begins ? 0.f : kept[k][i]) + (__uint_as_float(v[i]) + __uint_as_float(x[i]));
@@ -578,12 +573,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       }
       for (int c = 2 * pair + half; 16 * c < out_cols; c += 4) {
         uint32_t v[16];
-        tmem_load16(v, o_at + 16 * c);
+        tmem_load(v, o_at + 16 * c);
         float4* p = reinterpret_cast<float4*>(to + 16 * c);
         float4 y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = g.begins ? make_float4(0.f, 0.f, 0.f, 0.f) : p[i];
-        tmem_loaded(v);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           p[i] = make_float4(y[i].x + __uint_as_float(v[4 * i]), y[i].y + __uint_as_float(v[4 * i + 1]),
