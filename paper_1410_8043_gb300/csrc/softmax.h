@@ -74,6 +74,8 @@ struct ManyScratch {
   float* run_sum[2];         // [n * top / kRun (^2) + 1][D] sums over whole runs of one item
   void* sort_tmp;
   size_t sort_bytes;
+  cudaStream_t side;         // the targets are sorted beside the scores
+  cudaEvent_t fork, join;
 };
 constexpr int kRun = 16;
 

@@ -22,6 +22,8 @@ struct esspt_softmax {
   cudaStream_t st = nullptr;
   char* base = nullptr;
   Carve k{};
+  cudaStream_t side = nullptr;
+  cudaEvent_t fork = nullptr, join = nullptr;
   int sms = 0;
   char err[256] = "";
 };
@@ -37,6 +39,13 @@ esspt_status fail(esspt_softmax* sm, esspt_status code, const char* msg) {
 esspt_status cuda_fail(esspt_softmax* sm, cudaError_t e, const char* where) {
   snprintf(sm ? sm->err : g_create_err, 256, "%s: %s", where, cudaGetErrorString(e));
   return ESSPT_ECUDA;
+}
+
+void release(esspt_softmax* sm) {
+  if (sm->fork) cudaEventDestroy(sm->fork);
+  if (sm->join) cudaEventDestroy(sm->join);
+  if (sm->side) cudaStreamDestroy(sm->side);
+  delete sm;
 }
 
 #define SOFTMAX_CUDA(sm, call)                                   \
@@ -150,6 +159,7 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   s.tile_first = static_cast<int32_t*>(at(k.tile_first));
   for (int i = 0; i < 2; ++i) s.run_sum[i] = static_cast<float*>(at(k.run_sum[i]));
   s.sort_tmp = at(k.sort), s.sort_bytes = k.sort_bytes;
+  s.side = sm->side, s.fork = sm->fork, s.join = sm->join;
   SOFTMAX_CUDA(sm, launch_many_rows(a, s));
   return ESSPT_OK;
 }
@@ -179,14 +189,23 @@ esspt_status esspt_softmax_create(const esspt_softmax_config* cfg, void* d_works
   sm->base = static_cast<char*>(d_workspace);
   sm->k = carve(*cfg);
   sm->sms = sms < kMaxSms ? sms : kMaxSms;
+  if (cfg->backward && cfg->max_rows > kFewRows) {
+    cudaError_t e = cudaStreamCreateWithFlags(&sm->side, cudaStreamNonBlocking);
+    if (e == cudaSuccess) e = cudaEventCreateWithFlags(&sm->fork, cudaEventDisableTiming);
+    if (e == cudaSuccess) e = cudaEventCreateWithFlags(&sm->join, cudaEventDisableTiming);
+    if (e != cudaSuccess) {
+      release(sm);
+      return cuda_fail(nullptr, e, "esspt_softmax_create");
+    }
+  }
   *out = sm;
   return ESSPT_OK;
 }
 
 esspt_status esspt_softmax_destroy(esspt_softmax* sm) {
   if (!sm) return ESSPT_OK;
-  const cudaError_t e = cudaStreamSynchronize(sm->st);
-  delete sm;
+  const cudaError_t e = cudaStreamSynchronize(sm->st);  // (the side stream's work ended before it)
+  release(sm);
   return e == cudaSuccess ? ESSPT_OK : cuda_fail(nullptr, e, "esspt_softmax_destroy");
 }
 

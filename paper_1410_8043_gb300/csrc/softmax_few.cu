@@ -70,9 +70,9 @@ struct Few {
 // values), eight items to a warp side by side, U deep; rows of H from shared memory, where
 // the four lanes read one 64-byte line for all items.  The lanes' sums meet by
 // halving: each lane ends with two rows' totals, so no exponential is taken twice.
-template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) few_scores_kernel(Few f) {
-  constexpr int U = 4, R = kFewRows;
+template <typename T, int VEC, int U>
+__global__ void __launch_bounds__(kThreads, 2) few_scores_kernel(Few f) {
+  constexpr int R = kFewRows, kDeep = U == 1 ? 8 : 8 / VEC > 0 ? 8 / VEC : 1;  // slices under way
   extern __shared__ __align__(16) float hs[];  // [slices][R][VEC]
   __shared__ float2 warp_part[kThreads / 32][R];
   const SoftmaxArgs& a = f.a;
@@ -99,6 +99,7 @@ __global__ void __launch_bounds__(kThreads) few_scores_kernel(Few f) {
     const T* row[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) row[u] = w + min(v0 + u * 8 + lane / 4, (int64_t)a.V - 1) * a.w_stride;
+#pragma unroll(kDeep)
     for (int i = ql; i < slices; i += 4) {
       float x[U][VEC];
 #pragma unroll
@@ -198,8 +199,7 @@ __global__ void few_stat_kernel(Few f) {
 // dw_v = sum_r g_vr h_r, with g_vr = b weight_r (p_vr - q_vr) taken from the scores of
 // a tile of items for all rows at once, and left in their place for dh.  Threads take
 // slices of VEC columns (tx of them at a time) of every ty-th item, four items deep.
-constexpr int kTile = 64;
-template <typename T, int VEC>
+template <typename T, int VEC, int kTile>
 __global__ void __launch_bounds__(kThreads, 2) few_grad_w_kernel(Few f, int tx) {
   constexpr int R = kFewRows, U = 4;
   extern __shared__ __align__(16) float g[];  // [groups][kTile][R]
@@ -251,6 +251,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_grad_w_kernel(Few f, int tx) 
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int e = 0; e < VEC; ++e) dw[u][e] = 0.f;
+#pragma unroll 4
         for (int t = 0; t < n; ++t) {
           float h[VEC];
 #pragma unroll
@@ -343,21 +344,31 @@ int vector_of(const void* p, int64_t stride, int32_t D, int most) {
   return 1;
 }
 
+// Warps take 8 items at a time where that gives the GPU few warps, else 32.
 template <typename T, int VEC>
-void scores(const Few& f) {
+void scores(Few& f) {
   const int32_t slices = (f.a.D + VEC - 1) / VEC;
-  few_scores_kernel<T, VEC><<<dim3(f.blocks, f.groups), kThreads, sizeof(float) * slices * kFewRows * VEC, f.a.st>>>(f);
+  const size_t smem = sizeof(float) * slices * kFewRows * VEC;
+  const int64_t most = std::max(1, few_blocks(f.a.sms) / f.groups);
+  const bool small = (int64_t)f.a.V < most * kThreads;
+  f.blocks = (int)std::min<int64_t>(most, ((int64_t)f.a.V + (small ? 64 : 256) - 1) / (small ? 64 : 256));
+  if (small) few_scores_kernel<T, VEC, 1><<<dim3(f.blocks, f.groups), kThreads, smem, f.a.st>>>(f);
+  else few_scores_kernel<T, VEC, 4><<<dim3(f.blocks, f.groups), kThreads, smem, f.a.st>>>(f);
 }
 template <typename T, int VEC>
 void grads(Few f) {
   const int32_t slices = (f.a.D + VEC - 1) / VEC;
   int tx = 1;
   while (tx < slices && tx < 64) tx *= 2;
+  const bool small = (int64_t)f.a.V < 64 * f.a.sms;  // tiles of 8 items, else of 64
+  const int kTile = small ? 8 : 64;
   const int64_t tiles = ((int64_t)f.a.V + kTile - 1) / kTile;
   const size_t smem = sizeof(float) * f.groups * kTile * kFewRows;
-  few_grad_w_kernel<T, VEC><<<(unsigned)std::min<int64_t>(tiles, 4 * f.a.sms), kThreads, smem, f.a.st>>>(f, tx);
-  // Blocks of a group: as many as fill the GPU, each with 16 items per thread at least.
-  const int64_t most = ((int64_t)f.a.V * tx + 16 * kThreads - 1) / (16 * kThreads);
+  const unsigned grid = (unsigned)std::min<int64_t>(tiles, 4 * f.a.sms);
+  if (small) few_grad_w_kernel<T, VEC, 8><<<grid, kThreads, smem, f.a.st>>>(f, tx);
+  else few_grad_w_kernel<T, VEC, 64><<<grid, kThreads, smem, f.a.st>>>(f, tx);
+  // Blocks of a group: as many as fill the GPU, each with 4 items per thread at least.
+  const int64_t most = ((int64_t)f.a.V * tx + 4 * kThreads - 1) / (4 * kThreads);
   f.blocks = (int)std::min<int64_t>(std::max(1, few_blocks(f.a.sms) / f.groups), most);
   few_grad_h_kernel<T, VEC><<<dim3(f.blocks, (slices + tx - 1) / tx, f.groups), kThreads, 0, f.a.st>>>(f, tx);
   few_finish_kernel<T><<<dim3((f.a.D + 127) / 128, (unsigned)f.a.n), 128, 0, f.a.st>>>(f);
@@ -369,8 +380,6 @@ cudaError_t run(const SoftmaxArgs& a, const FewScratch& s) {
   const int vw = vector_of<T>(a.w, a.w_stride, a.D, kWide);
   const int vg = std::min(std::min(vw, 4), std::min(vector_of<T>(a.h, a.h_stride, a.D, 4), vector_of<T>(a.grad_w, a.D, a.D, 4)));
   Few f{a, s, (int32_t)((a.n + kFewRows - 1) / kFewRows), 0};
-  // A block takes 256 items at a time.
-  f.blocks = (int)std::min<int64_t>(std::max(1, few_blocks(a.sms) / f.groups), (a.V + kThreads - 1) / kThreads);
   if (vw == kWide) scores<T, kWide>(f);
   else if (vw >= 4) scores<T, 4>(f);
   else scores<T, 1>(f);

@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
   if (key[first] != key[first + kLong - 1] || key[first] == (uint32_t)a.V) return;
   int32_t t = 0;
   float g = 0.f;
-  if (LEVEL == 0 && lane < kRun) g = entry_factor<T>(f, cols_shift(f), val[first + lane], t);
+  if (LEVEL == 0 && lane < kRun) g = entry_factor<T>(f, sizeof(T) == 2 ? cols_shift(f) : 0, val[first + lane], t);
   for (int d = lane * VEC; d - lane * VEC < a.D; d += 32 * VEC) {
     float x[VEC];
 #pragma unroll
@@ -515,6 +515,27 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   if (!grads) f.s.col = nullptr;
   cudaError_t e = cudaMemsetAsync(s.words, 0, sizeof(ManyWords), a.st);
   if (e != cudaSuccess) return e;
+  // The targets by item, on the handle's second stream beside what follows.
+  const int64_t entries = a.n * a.target.top, tiles = ((int64_t)a.V + 127) / 128;
+  cub::DoubleBuffer<uint32_t> key(s.key[0], s.key[1]), val(s.val[0], s.val[1]);
+  auto launch_runs = [&]() {
+    const cudaStream_t st = sizeof(T) == 2 ? a.st : s.side;
+    if (entries >= kRun)
+      runs_kernel<T, VEC, 0><<<(unsigned)((entries / kRun + 7) / 8), 256, 0, st>>>(f, key.Current(), val.Current());
+    if (entries >= kRun * kRun)
+      runs_kernel<T, VEC, 1><<<(unsigned)((entries / kRun / kRun + 7) / 8), 256, 0, st>>>(f, key.Current(), val.Current());
+  };
+  if (grads) {
+    if ((e = cudaEventRecord(s.fork, a.st)) != cudaSuccess || (e = cudaStreamWaitEvent(s.side, s.fork, 0)) != cudaSuccess) return e;
+    entries_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, s.side>>>(f);
+    size_t bytes = s.sort_bytes;
+    if ((e = cub::DeviceRadixSort::SortPairs(s.sort_tmp, bytes, key, val, (int)entries, 0, bits_of((uint32_t)a.V), s.side)) !=
+        cudaSuccess)
+      return e;
+    tile_first_kernel<<<(unsigned)(tiles / 256 + 1), 256, 0, s.side>>>(f, key.Current());
+    if (sizeof(T) == 4) launch_runs();
+    if ((e = cudaEventRecord(s.join, s.side)) != cudaSuccess) return e;
+  }
   compact_kernel<<<(unsigned)((a.n + 1023) / 1024), 1024, 0, a.st>>>(f);
   if constexpr (kParts == 2) {
     const int64_t work = std::max((int64_t)a.V, a.n) * a.D / VEC;
@@ -540,19 +561,8 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   if ((e = launch_mma(Pass::kRows, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
   grad_h_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
 
-  const int64_t entries = a.n * a.target.top, tiles = ((int64_t)a.V + 127) / 128;
-  entries_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, a.st>>>(f);
-  cub::DoubleBuffer<uint32_t> key(s.key[0], s.key[1]), val(s.val[0], s.val[1]);
-  size_t bytes = s.sort_bytes;
-  if ((e = cub::DeviceRadixSort::SortPairs(s.sort_tmp, bytes, key, val, (int)entries, 0, bits_of((uint32_t)a.V), a.st)) !=
-      cudaSuccess)
-    return e;
-  tile_first_kernel<<<(unsigned)(tiles / 256 + 1), 256, 0, a.st>>>(f, key.Current());
-  if (entries >= kRun)
-    runs_kernel<T, VEC, 0><<<(unsigned)((entries / kRun + 7) / 8), 256, 0, a.st>>>(f, key.Current(), val.Current());
-  if (entries >= kRun * kRun)
-    runs_kernel<T, VEC, 1><<<(unsigned)((entries / kRun / kRun + 7) / 8), 256, 0, a.st>>>(f, key.Current(), val.Current());
-
+  if ((e = cudaStreamWaitEvent(a.st, s.join, 0)) != cudaSuccess) return e;
+  if (sizeof(T) == 2) launch_runs();  // (want the statistics: entry_factor)
   m.A = s.units_w, m.B = s.units_h;
   if ((e = launch_mma(Pass::kCols, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
   grad_w_kernel<T, VEC><<<(unsigned)(((int64_t)a.V + kItems - 1) / kItems), 256, 0, a.st>>>(f, key.Current(), val.Current());
