@@ -71,16 +71,16 @@ struct Few {
 // the four lanes read one 64-byte line for all items.  The lanes' sums meet by
 // halving: each lane ends with two rows' totals, so no exponential is taken twice.
 template <typename T, int VEC, int U>
-__global__ void __launch_bounds__(kThreads, 2) few_scores_kernel(Few f) {
-  constexpr int R = kFewRows, kDeep = U == 1 ? 8 : 8 / VEC > 0 ? 8 / VEC : 1;  // slices under way
-  extern __shared__ __align__(16) float hs[];  // [slices][R][VEC]
+__global__ void __launch_bounds__(kThreads, U == 1 ? 2 : 4) few_scores_kernel(Few f) {
+  constexpr int R = kFewRows, kDeep = U == 1 ? 8 : VEC == 8 ? 1 : 2;  // slices under way
+  extern __shared__ __align__(16) float hs[];  // [R][slices][VEC]
   __shared__ float2 warp_part[kThreads / 32][R];
   const SoftmaxArgs& a = f.a;
   const int lane = threadIdx.x & 31, ql = lane & 3;
   const int32_t slices = (a.D + VEC - 1) / VEC;
   const T* h = static_cast<const T*>(a.h);
   for (int i = threadIdx.x; i < slices * R * VEC; i += kThreads) {
-    const int d = i / (R * VEC) * VEC + i % VEC, r = i / VEC % R;
+    const int r = i / (slices * VEC), d = i - r * slices * VEC;
     const int64_t t = (int64_t)blockIdx.y * R + r;
     hs[i] = t < a.n && d < a.D && row_kept(a.target, t) ? to_float(h[t * a.h_stride + d]) : 0.f;
   }
@@ -104,18 +104,18 @@ __global__ void __launch_bounds__(kThreads, 2) few_scores_kernel(Few f) {
       float x[U][VEC];
 #pragma unroll
       for (int u = 0; u < U; ++u) load_vec<T, VEC>(row[u] + i * VEC, x[u]);
-      const float* hv = hs + i * R * VEC;
+      const float* hv = hs + i * VEC;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         float y[VEC];
         if constexpr (VEC >= 4) {
 #pragma unroll
           for (int e = 0; e < VEC; e += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(hv + r * VEC + e);
+            const float4 q = *reinterpret_cast<const float4*>(hv + r * slices * VEC + e);
             y[e] = q.x, y[e + 1] = q.y, y[e + 2] = q.z, y[e + 3] = q.w;
           }
         } else {
-          y[0] = hv[r];
+          y[0] = hv[r * slices];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -344,16 +344,16 @@ int vector_of(const void* p, int64_t stride, int32_t D, int most) {
   return 1;
 }
 
-// Warps take 8 items at a time where that gives the GPU few warps, else 32.
+// Warps take 8 items at a time where that gives the GPU few warps, else 16.
 template <typename T, int VEC>
 void scores(Few& f) {
   const int32_t slices = (f.a.D + VEC - 1) / VEC;
   const size_t smem = sizeof(float) * slices * kFewRows * VEC;
   const int64_t most = std::max(1, few_blocks(f.a.sms) / f.groups);
-  const bool small = (int64_t)f.a.V < most * kThreads;
-  f.blocks = (int)std::min<int64_t>(most, ((int64_t)f.a.V + (small ? 64 : 256) - 1) / (small ? 64 : 256));
+  const bool small = (int64_t)f.a.V < most * 128;
+  f.blocks = (int)std::min<int64_t>(most, ((int64_t)f.a.V + (small ? 64 : 128) - 1) / (small ? 64 : 128));
   if (small) few_scores_kernel<T, VEC, 1><<<dim3(f.blocks, f.groups), kThreads, smem, f.a.st>>>(f);
-  else few_scores_kernel<T, VEC, 4><<<dim3(f.blocks, f.groups), kThreads, smem, f.a.st>>>(f);
+  else few_scores_kernel<T, VEC, 2><<<dim3(f.blocks, f.groups), kThreads, smem, f.a.st>>>(f);
 }
 template <typename T, int VEC>
 void grads(Few f) {
@@ -390,7 +390,7 @@ cudaError_t run(const SoftmaxArgs& a, const FewScratch& s) {
 
 }  // namespace
 
-int few_blocks(int sms) { return 2 * sms; }
+int few_blocks(int sms) { return 4 * sms; }
 
 bool few_rows(int64_t n, int64_t V, int32_t D, int32_t dtype) {
   return n <= kFewRows || (n <= kSmallRows && n * V * D <= 200'000'000);
