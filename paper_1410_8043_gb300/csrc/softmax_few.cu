@@ -200,9 +200,9 @@ __global__ void few_stat_kernel(Few f) {
 // a tile of items for all rows at once, and left in their place for dh.  Threads take
 // slices of VEC columns (tx of them at a time) of every ty-th item, four items deep.
 template <typename T, int VEC, int kTile>
-__global__ void __launch_bounds__(kThreads, 2) few_grad_w_kernel(Few f, int tx) {
+__global__ void __launch_bounds__(kThreads, 3) few_grad_w_kernel(Few f, int tx) {
   constexpr int R = kFewRows, U = 4;
-  extern __shared__ __align__(16) float g[];  // [groups][kTile][R]
+  extern __shared__ __align__(32) float g[];  // [groups][kTile][R]
   __shared__ float bw[kSmallRows], mx[kSmallRows], inv[kSmallRows];
   __shared__ bool used[kSmallRows];
   const SoftmaxArgs& a = f.a;
@@ -244,25 +244,33 @@ __global__ void __launch_bounds__(kThreads, 2) few_grad_w_kernel(Few f, int tx) 
       const int group = i / (items * R), in = i - group * items * R;
       f.s.scores[((int64_t)group * a.V + v0) * R + in] = g[group * kTile * R + in];
     }
-    for (int col = x * VEC; col < a.D; col += tx * VEC)
+    for (int col = x * VEC; col < a.D; col += tx * VEC) {
+      float h[R][VEC];
+      auto load_rows = [&](int group) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) h[r][e] = 0.f;
+          if (used[group * R + r]) load_vec<T, VEC>(static_cast<const T*>(a.h) + (group * R + r) * a.h_stride + col, h[r]);
+        }
+      };
+      if (f.groups == 1) load_rows(0);
       for (int i0 = y; i0 < items; i0 += ty_n * U) {
         float dw[U][VEC];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int e = 0; e < VEC; ++e) dw[u][e] = 0.f;
-#pragma unroll 4
-        for (int t = 0; t < n; ++t) {
-          float h[VEC];
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) h[e] = 0.f;
-          if (used[t]) load_vec<T, VEC>(static_cast<const T*>(a.h) + t * a.h_stride + col, h);
-          const float* c = g + (t / R * kTile + i0) * R + t % R;
+        for (int group = 0; group < f.groups; ++group) {
+          if (f.groups > 1) load_rows(group);
 #pragma unroll
           for (int u = 0; u < U; ++u) {
-            const float cu = i0 + u * ty_n < items ? c[u * ty_n * R] : 0.f;
+            float c[R];
+            load_vec<float, R>(g + (group * kTile + min(i0 + u * ty_n, items - 1)) * R, c);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) dw[u][e] = fmaf(cu, h[e], dw[u][e]);
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) dw[u][e] = fmaf(c[r], h[r][e], dw[u][e]);
           }
         }
 #pragma unroll
@@ -270,15 +278,18 @@ __global__ void __launch_bounds__(kThreads, 2) few_grad_w_kernel(Few f, int tx) 
           if (i0 + u * ty_n < items)
             store_vec<T, VEC>(static_cast<T*>(a.grad_w) + (v0 + i0 + u * ty_n) * a.D + col, dw[u]);
       }
+    }
     __syncthreads();
   }
 }
 
 // dh_r = sum_v g_vr w_v of a group of rows (blockIdx.z) by blocks, each over a part of
-// the items: threads as above, the rows' sums in registers.
+// the items: threads as above, coefficients by tiles through shared memory, the rows'
+// sums in registers.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads, 2) few_grad_h_kernel(Few f, int tx) {
-  constexpr int R = kFewRows;
+__global__ void __launch_bounds__(kThreads, 3) few_grad_h_kernel(Few f, int tx) {
+  constexpr int R = kFewRows, U = 8, kTile = 256;
+  __shared__ __align__(32) float c[kTile * R];
   __shared__ __align__(16) float red[kThreads * VEC];
   const SoftmaxArgs& a = f.a;
   const int ty_n = kThreads / tx, x = threadIdx.x % tx, y = threadIdx.x / tx;
@@ -292,17 +303,29 @@ __global__ void __launch_bounds__(kThreads, 2) few_grad_h_kernel(Few f, int tx) 
 #pragma unroll
     for (int e = 0; e < VEC; ++e) o[r][e] = 0.f;
   const int64_t end = a.V * (int64_t)(blockIdx.x + 1) / gridDim.x;
-  if (on)
-#pragma unroll 4
-    for (int64_t v = a.V * (int64_t)blockIdx.x / gridDim.x + y; v < end; v += ty_n) {
-      float k[VEC], c[R];
-      load_vec<T, VEC>(w + v * a.w_stride, k);
-      load_vec<float, R>(g + v * R, c);
+  for (int64_t v0 = a.V * (int64_t)blockIdx.x / gridDim.x; v0 < end; v0 += kTile) {
+    const int items = (int)min((int64_t)kTile, end - v0);
+    __syncthreads();
+    for (int i = threadIdx.x; i < items * R; i += kThreads) c[i] = g[v0 * R + i];
+    __syncthreads();
+    if (on)
+      for (int i = y; i < items; i += U * ty_n) {
+        float k[U][VEC];
 #pragma unroll
-      for (int r = 0; r < R; ++r)
+        for (int u = 0; u < U; ++u) load_vec<T, VEC>(w + (v0 + min(i + u * ty_n, items - 1)) * a.w_stride, k[u]);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) o[r][e] = fmaf(c[r], k[e], o[r][e]);
-    }
+        for (int u = 0; u < U; ++u) {
+          if (i + u * ty_n >= items) break;
+          float cu[R];
+          load_vec<float, R>(c + (i + u * ty_n) * R, cu);
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) o[r][e] = fmaf(cu[r], k[u][e], o[r][e]);
+        }
+      }
+  }
+  __syncthreads();
 #pragma unroll 1
   for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -323,15 +346,20 @@ __global__ void __launch_bounds__(kThreads, 2) few_grad_h_kernel(Few f, int tx) 
   }
 }
 
-// dh: the blocks' sums in the order of the blocks.
+// dh: the blocks' sums, eight parts of them side by side and then in order.
 template <typename T>
 __global__ void few_finish_kernel(Few f) {
-  const int t = blockIdx.y, d = blockIdx.x * blockDim.x + threadIdx.x;
-  if (d >= f.a.D) return;
+  __shared__ float part[8][32];
+  const int t = blockIdx.y, d = blockIdx.x * 32 + threadIdx.x;
   const float* from = f.s.dh + ((int64_t)t / kFewRows * f.blocks * kFewRows + t % kFewRows) * f.a.D + d;
   float sum = 0.f;
+  if (d < f.a.D)
 #pragma unroll 8
-  for (int i = 0; i < f.blocks; ++i) sum += from[(int64_t)i * kFewRows * f.a.D];
+    for (int i = threadIdx.y; i < f.blocks; i += 8) sum += from[(int64_t)i * kFewRows * f.a.D];
+  part[threadIdx.y][threadIdx.x] = sum;
+  __syncthreads();
+  if (threadIdx.y > 0 || d >= f.a.D) return;
+  for (int i = 1; i < 8; ++i) sum += part[i][threadIdx.x];
   const bool kept = row_kept(f.a.target, t);
   static_cast<T*>(f.a.grad_h)[(int64_t)t * f.a.D + d] = from_float<T>(kept ? sum : 0.f);
 }
@@ -360,18 +388,19 @@ void grads(Few f) {
   const int32_t slices = (f.a.D + VEC - 1) / VEC;
   int tx = 1;
   while (tx < slices && tx < 64) tx *= 2;
-  const bool small = (int64_t)f.a.V < 64 * f.a.sms;  // tiles of 8 items, else of 64
-  const int kTile = small ? 8 : 64;
+  // Tiles of 8 items where there are few, of 256 where a few rows meet many, else of 64.
+  const int kTile = (int64_t)f.a.V < 64 * f.a.sms ? 8 : f.groups == 1 && (int64_t)f.a.V >= 1024 * f.a.sms ? 256 : 64;
   const int64_t tiles = ((int64_t)f.a.V + kTile - 1) / kTile;
   const size_t smem = sizeof(float) * f.groups * kTile * kFewRows;
-  const unsigned grid = (unsigned)std::min<int64_t>(tiles, 4 * f.a.sms);
-  if (small) few_grad_w_kernel<T, VEC, 8><<<grid, kThreads, smem, f.a.st>>>(f, tx);
+  const unsigned grid = (unsigned)std::min<int64_t>(tiles, 3 * f.a.sms);  // (what is resident at once)
+  if (kTile == 8) few_grad_w_kernel<T, VEC, 8><<<grid, kThreads, smem, f.a.st>>>(f, tx);
+  else if (kTile == 256) few_grad_w_kernel<T, VEC, 256><<<grid, kThreads, smem, f.a.st>>>(f, tx);
   else few_grad_w_kernel<T, VEC, 64><<<grid, kThreads, smem, f.a.st>>>(f, tx);
   // Blocks of a group: as many as fill the GPU, each with 4 items per thread at least.
   const int64_t most = ((int64_t)f.a.V * tx + 4 * kThreads - 1) / (4 * kThreads);
-  f.blocks = (int)std::min<int64_t>(std::max(1, few_blocks(f.a.sms) / f.groups), most);
+  f.blocks = (int)std::min<int64_t>(std::max(1, 3 * f.a.sms / f.groups), most);
   few_grad_h_kernel<T, VEC><<<dim3(f.blocks, (slices + tx - 1) / tx, f.groups), kThreads, 0, f.a.st>>>(f, tx);
-  few_finish_kernel<T><<<dim3((f.a.D + 127) / 128, (unsigned)f.a.n), 128, 0, f.a.st>>>(f);
+  few_finish_kernel<T><<<dim3((f.a.D + 31) / 32, (unsigned)f.a.n), dim3(32, 8), 0, f.a.st>>>(f);
 }
 
 template <typename T>
