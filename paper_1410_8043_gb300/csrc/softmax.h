@@ -59,13 +59,14 @@ int few_blocks(int sms);
 struct ManyWords {  // (device) what a call's kernels tell each other
   uint32_t max_h, max_w, max_weight;  // largest finite magnitude, as fp32 bits
   int32_t rows;                       // rows that are not ignored
+  uint32_t negative;                  // whether one of their weights is
 };
 struct ManyScratch {
   ManyWords* words;
   int32_t *act, *pos;      // [n] the kept rows in order; a row's place among them, or -1
   char *units_h, *units_w;
   float *row_max, *row_sum;  // [n] statistics of the kept rows, in order
-  float4* col;               // [(n up to 128) / 2] the kept rows as columns of dw: see MmaArgs
+  float* col;                // [2 (n up to 128)] the kept rows as columns of dw: see MmaArgs
   float* score;              // [n * top] scores of the targets
   float2* stat;              // partial statistics, see many_slots
   float* out;                // partial gradients, see many_slots

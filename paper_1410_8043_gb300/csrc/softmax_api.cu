@@ -152,7 +152,7 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   s.units_h = static_cast<char*>(at(k.units_h)), s.units_w = static_cast<char*>(at(k.units_w));
   s.row_max = static_cast<float*>(at(k.row_max)), s.row_sum = static_cast<float*>(at(k.row_sum));
   s.score = static_cast<float*>(at(k.score));
-  s.col = static_cast<float4*>(at(k.col)), s.stat = static_cast<float2*>(at(k.slot_stat));
+  s.col = static_cast<float*>(at(k.col)), s.stat = static_cast<float2*>(at(k.slot_stat));
   s.out = static_cast<float*>(at(k.out));
   for (int i = 0; i < 2; ++i)
     s.key[i] = static_cast<uint32_t*>(at(k.key[i])), s.val[i] = static_cast<uint32_t*>(at(k.val[i]));

@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(1024) compact_kernel(Many f) {
     if (!a.target.logits && a.target.ids[t] >= a.V) atomicOr(a.target.status, kErrTarget);
     if (t == a.n - 1) f.s.words->rows = base + kept;
   }
+  if (a.weight && __any_sync(0xffffffffu, kept && a.weight[t] < 0.f) && lane == 0) f.s.words->negative = 1u;
   if (a.weight) block_max(kept ? finite_bits(a.weight[t]) : 0u, &f.s.words->max_weight);
   else if (t == 0) f.s.words->max_weight = __float_as_uint(1.f);
 }
@@ -141,20 +142,26 @@ __global__ void __launch_bounds__(256) units_kernel(Many f, bool is_h) {
   }
 }
 
-// Column data of dw, two kept rows to a float4 (MmaArgs).
+// Column data of dw (MmaArgs); what the kernel makes of a score by it.
+template <int PARTS>
 __device__ __forceinline__ void set_col(const Many& f, int64_t pos, float m, float factor) {
-  float* c = reinterpret_cast<float*>(f.s.col + pos / 2) + (pos & 1);
-  c[0] = -m, c[2] = factor;
+  if (PARTS == 2) {
+    float* c = f.s.col + pos / 2 * 4 + (pos & 1);
+    c[0] = -m, c[2] = factor;
+  } else {
+    f.s.col[pos] = __uint_as_float((__float_as_uint(log2f(fabsf(factor)) - m) & ~1u) | (factor < 0.f ? 1u : 0u));
+  }
 }
-__device__ __forceinline__ float2 get_col(const Many& f, int64_t pos) {
-  const float* c = reinterpret_cast<const float*>(f.s.col + pos / 2) + (pos & 1);
-  return make_float2(-c[0], c[2]);
+__device__ __forceinline__ float col_probability(const Many& f, int64_t pos, float score) {  // (16-bit rows)
+  const float c = f.s.col[pos], p = exp2_fast(score + c);
+  return __float_as_uint(c) & 1u && f.s.words->negative ? -p : p;
 }
 
 // A warp per row: its statistics from the partial ones, the scores of its targets
 // (8 lanes to an entry), its loss.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) loss_kernel(Many f) {
+  constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
   const SoftmaxArgs& a = f.a;
   const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
   const int lane = threadIdx.x & 31;
@@ -163,9 +170,9 @@ __global__ void __launch_bounds__(256) loss_kernel(Many f) {
   // Columns of dw past the last kept row: no term.
   const int64_t rows = f.s.words->rows;
   const int64_t padded = (rows + 127) / 128 * 128;
-  if (f.s.col && lane == 0 && t >= rows && t < padded) set_col(f, t, 1e30f, 0.f);
+  if (f.s.col && lane == 0 && t >= rows && t < padded) set_col<kParts>(f, t, 1e30f, 0.f);
   if (f.s.col && t == a.n - 1)
-    for (int64_t i = max(t + 1, rows) + lane; i < padded; i += 32) set_col(f, i, 1e30f, 0.f);
+    for (int64_t i = max(t + 1, rows) + lane; i < padded; i += 32) set_col<kParts>(f, i, 1e30f, 0.f);
   if (pos < 0) {
     if (lane == 0) a.loss[t] = a.lse[t] = 0.f;
     return;
@@ -233,7 +240,7 @@ __global__ void __launch_bounds__(256) loss_kernel(Many f) {
       // fp16 probabilities: weight / 2^shift at most one, times 2^14
       const float factor = a.dtype == ESSPT_BF16 ? weight
                                                  : times_pow2(weight, (int)kHalfShift - weight_shift_of(f.s.words->max_weight));
-      set_col(f, pos, m, factor / l);
+      set_col<kParts>(f, pos, m, factor / l);
     }
   }
 }
@@ -350,8 +357,7 @@ __device__ __forceinline__ float entry_factor(const Many& f, int shift, uint32_t
   const float q = a.target.logits ? a.target.q[entry] : 1.f;
   float g = a.weight ? q * a.weight[t] : q;
   if (sizeof(T) == 2) {
-    const float2 c = get_col(f, f.s.pos[t]);
-    g -= ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - c.x) * c.y), shift);
+    g -= ldexpf(rounded_off<T>(col_probability(f, f.s.pos[t], f.s.score[entry])), shift);
   }
   return g;
 }

@@ -290,12 +290,23 @@ struct Issue {
   }
 };
 
+// Scores of columns from `left` on become -infinity.  Only a tile at the end of B has
+// any: a branch of its own (as selects these were most of the instructions).
+__device__ __forceinline__ void mask_scores(uint32_t (&r)[32], int left) {
+  if (left >= 32) return;
+  asm volatile("");
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i >= left) r[i] = 0xff800000u;
+}
+
 template <Pass PASS, bool BF16, int PARTS>
 __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ MmaArgs a) {
   extern __shared__ __align__(1024) char smem[];
   __shared__ uint32_t tmem_at;
   __shared__ uint32_t dead_flag;
   constexpr bool STATS = PASS == Pass::kStats;
+  constexpr int kColBytes = PARTS == 2 ? 1024 : 512;  // of a tile's columns
   const MmaShape sh = a.s;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int64_t rows_h = a.words->rows;
@@ -342,18 +353,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       int col = 0;  // stage of the column data
       uint32_t a_phase = 1, loads = 0, segs = 0;
       const uint32_t stage_bytes = sh.stage_units * kUnitBytes;
-      auto load = [&](const char* from, const float4* cols) {
+      auto load = [&](const char* from, const char* cols) {
         mbar_wait(ring.bar + kEmpty, ring.phase ^ 1, dead);
         if (*dead) return;
-        mbar_expect(ring.bar, stage_bytes + (cols ? 1024 : 0));
+        mbar_expect(ring.bar, stage_bytes + (cols ? kColBytes : 0));
         bulk_load(ring.at, from, stage_bytes, ring.bar);
-        if (cols) bulk_load(col_base + col * 1024, cols, 1024, ring.bar);
+        if (cols) bulk_load(col_base + col * 1024, cols, kColBytes, ring.bar);
         ring.next();
         ++loads;
       };
       auto scores_units = [&](int64_t tile, const char* from_a) {
         const char* from = a.B + tile * tile_bytes;
-        const float4* cols = PASS == Pass::kCols ? a.col + tile * 64 : nullptr;
+        const char* cols = PASS == Pass::kCols ? reinterpret_cast<const char*>(a.col) + tile * kColBytes : nullptr;
         if (sh.stage_units == sh.nk * PARTS) {
           load(from, cols);
         } else {
@@ -430,6 +441,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     // masked ones stay -infinity.)
     const float scale = fminf(fmaxf(ldexpf(a.b * kLog2e, -(shift_h + shift_w)), 1.1754944e-38f), 3.4028235e38f);
     const u64 scale2 = pack2(scale, scale);
+    const bool negative = PASS == Pass::kCols && a.words->negative != 0u;
     uint32_t phase = 0, o_phase = 0;  // parities of s_full's next turn, a bit per buffer
     int col0 = 0;  // stage of the run's first column data
     // fp32 rows of up to 128 values: a thread's sums over the runs so far (two times 16
@@ -458,7 +470,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         const int32_t j = nt == 2 ? n >> 1 : n;
         warp_wait(bar.s_full + 8 * at_buf, parity, dead);
         fence_after();
-        const int64_t left = rows_b - (g.first + j) * 128 - 64 * half;  // of this half's columns
+        const int left = (int)min((int64_t)64, rows_b - (g.first + j) * 128 - 64 * half);  // of this half's columns
         const uint32_t s_at = lanes + 128 * at_buf + 64 * half;
         // (fp32 rows: one half at a time, for the registers that hold sums.)
         constexpr bool kBoth = STATS || PARTS == 1;
@@ -473,11 +485,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         if constexpr (STATS) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            if (left < 64) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (32 * c + i >= left) r[c][i] = 0xff800000u;
-            }
+            mask_scores(r[c], left - 32 * c);
             float top[4] = {m, m, m, m};
 #pragma unroll
             for (int i = 0; i < 32; i += 2)
@@ -499,12 +507,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
             m = m2, at = at2;
           }
         } else {
-          const ulonglong2* cols = reinterpret_cast<const ulonglong2*>(col_data + at_col * 1024 + 512 * half);
+          const ulonglong2* cols = reinterpret_cast<const ulonglong2*>(col_data + at_col * 1024 + kColBytes / 2 * half);
           const u64 offset2 = pack2(offset, offset);
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             uint32_t out[16 * PARTS];
             if (!kBoth && c == 1) tmem_load(r[0], s_at + 32);
+            if (PASS == Pass::kRows) mask_scores(r[kBoth ? c : 0], left - 32 * c);
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
               const u64 s2 = pack2(__uint_as_float(r[kBoth ? c : 0][i]), __uint_as_float(r[kBoth ? c : 0][i + 1]));
@@ -512,15 +521,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
               if (PASS == Pass::kRows) {
                 unpack2(fma2(s2, scale2, offset2), p[0], p[1]);
                 p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
-                if (left < 64) {
-#pragma unroll
-                  for (int e = 0; e < 2; ++e)
-                    if (32 * c + i + e >= left) p[e] = 0.f;
-                }
-              } else {
+              } else if (PARTS == 2) {
                 const ulonglong2 q = cols[16 * c + i / 2];
                 unpack2(fma2(s2, scale2, q.x), p[0], p[1]);
                 unpack2(mul2(pack2(exp2_fast(p[0]), exp2_fast(p[1])), q.y), p[0], p[1]);
+              } else {
+                const ulonglong2 q = cols[8 * c + i / 4];
+                const u64 k = i & 2 ? q.y : q.x;
+                unpack2(fma2(s2, scale2, k), p[0], p[1]);
+                p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
+                if (negative) {  // a factor's sign is the lowest bit of its logarithm
+                  p[0] = __uint_as_float(__float_as_uint(p[0]) ^ ((uint32_t)k << 31));
+                  p[1] = __uint_as_float(__float_as_uint(p[1]) ^ ((uint32_t)(k >> 32) << 31));
+                }
               }
               out[i / 2] = pack16<BF16>(p[0], p[1]);
               if constexpr (PARTS == 2) out[16 + i / 2] = pack16_rest(out[i / 2], p[0], p[1]);

@@ -56,7 +56,9 @@ struct MmaArgs {
   int32_t V;
   float b;
   const float* row_max;  // kRows
-  const float4* col;     // kCols: two columns each, (-maximum, -maximum, factor, factor)
+  // kCols, fp32 rows: two columns to a float4, (-maximum, -maximum, factor, factor); of
+  // 16-bit rows a float to a column, log2 |factor| - maximum with the sign as its lowest bit.
+  const float* col;
   float2* stat;          // kStats out: [slot][4][128], by group and half of the columns
   float* out;            // else: [slot][128][ld]
   int ld;
