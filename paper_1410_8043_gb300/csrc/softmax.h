@@ -60,6 +60,7 @@ struct ManyWords {  // (device) what a call's kernels tell each other
   uint32_t max_h, max_w, max_weight;  // largest finite magnitude, as fp32 bits
   int32_t rows;                       // rows that are not ignored
   uint32_t negative;                  // whether one of their weights is
+  uint32_t redo;                      // a row's reference was too low: the exact passes run
 };
 struct ManyScratch {
   ManyWords* words;

@@ -17,6 +17,10 @@ namespace esspt {
 
 namespace {
 
+// Probabilities by a sampled reference r are 2^(s - r + 4): up to 2^12 times too large
+// for their row, a sum of fp16 still holds them.
+constexpr float kSampledShift = 4.f;
+
 struct Many {
   SoftmaxArgs a;
   ManyScratch s;
@@ -24,6 +28,9 @@ struct Many {
   int blocks;  // of the pass whose slots are read
   int ld;
   int parts;
+  int32_t sample;  // rows of W that the rows' references are taken over, 0: all (exact maxima)
+  float up;        // probabilities of the rows pass are taken 2^up times as large
+  int if_redo;     // only where words->redo is set
 };
 
 __device__ __forceinline__ uint32_t finite_bits(float x) {
@@ -157,33 +164,16 @@ __device__ __forceinline__ float col_probability(const Many& f, int64_t pos, flo
   return __float_as_uint(c) & 1u && f.s.words->negative ? -p : p;
 }
 
-// A warp per row: its statistics from the partial ones, the scores of its targets
-// (8 lanes to an entry), its loss.
-template <typename T, int VEC>
-__global__ void __launch_bounds__(256) loss_kernel(Many f) {
-  constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
-  const SoftmaxArgs& a = f.a;
-  const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-  const int lane = threadIdx.x & 31;
-  if (t >= a.n) return;
-  const int64_t pos = f.s.pos[t];
-  // Columns of dw past the last kept row: no term.
+// A warp's row: the maximum and sum of its partial statistics over W's first `items` rows.
+__device__ __forceinline__ void merge_slots(const Many& f, int64_t pos, int64_t items, float& m, float& l) {
   const int64_t rows = f.s.words->rows;
-  const int64_t padded = (rows + 127) / 128 * 128;
-  if (f.s.col && lane == 0 && t >= rows && t < padded) set_col<kParts>(f, t, 1e30f, 0.f);
-  if (f.s.col && t == a.n - 1)
-    for (int64_t i = max(t + 1, rows) + lane; i < padded; i += 32) set_col<kParts>(f, i, 1e30f, 0.f);
-  if (pos < 0) {
-    if (lane == 0) a.loss[t] = a.lse[t] = 0.f;
-    return;
-  }
-  const Ranges r(rows, a.V, f.shape.tiles, f.blocks);
+  const Ranges r(rows, items, f.shape.tiles, f.blocks);
   const int64_t g = pos / (128 * f.shape.tiles);
   const int tile = (int)(pos / 128 - g * f.shape.tiles), row = (int)(pos & 127);
   const bool two = f.shape.tiles == 2 && (g * 2 + 1) * 128 < rows;  // half of the slot per tile, else all per row
   const int64_t i0 = r.block_of(g * r.n_b), i1 = r.block_of((g + 1) * r.n_b - 1);
-  float m = -INFINITY, l = 0.f;
-  for (int64_t i = 4 * i0 + lane; i < 4 * i1 + 4; i += 32) {
+  m = -INFINITY, l = 0.f;
+  for (int64_t i = 4 * i0 + (threadIdx.x & 31); i < 4 * i1 + 4; i += 32) {
     const int part = (int)(i & 3);
     if (two && part / 2 != tile) continue;
     const float2 p = f.s.stat[((i / 4 + g) * 4 + part) * 128 + row];
@@ -194,11 +184,16 @@ __global__ void __launch_bounds__(256) loss_kernel(Many f) {
     const float m2 = __shfl_xor_sync(0xffffffffu, m, off), l2 = __shfl_xor_sync(0xffffffffu, l, off);
     merge_stat(m, l, m2, l2);
   }
-  const float lse2 = m + log2f(l), k2 = a.b * kLog2e;
+}
+
+// The scores of a row's targets, 8 lanes to an entry: use(entry of the row, q, score)
+// by one of them, and by that one always.
+template <typename T, int VEC, typename F>
+__device__ __forceinline__ void target_scores(const SoftmaxArgs& a, int64_t t, F use) {
+  const int lane = threadIdx.x & 31, sub = lane & 7;
+  const float k2 = a.b * kLog2e;
   const T* h = static_cast<const T*>(a.h) + t * a.h_stride;
   const int32_t* ids = a.target.ids + t * a.target.top;
-  float loss2 = 0.f;
-  const int sub = lane & 7;
   for (int k0 = 0; k0 < a.target.top; k0 += 32) {
     // Entries by lane, so that no row's load waits for its id's.
     const int count = min(32, a.target.top - k0);
@@ -223,26 +218,81 @@ __global__ void __launch_bounds__(256) loss_kernel(Many f) {
       }
 #pragma unroll
       for (int off = 4; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-      if (sub == 0 && q != 0.f) {
-        loss2 += q * (lse2 - s * k2);
-        if (f.s.col) f.s.score[t * a.target.top + k0 + i + lane / 8] = s * k2;
-      }
+      if (sub == 0 && q != 0.f) use(k0 + i + lane / 8, q, s * k2);
     }
   }
+}
+
+// Columns of dw past the last kept row: no term.
+template <int PARTS>
+__device__ __forceinline__ void pad_cols(const Many& f, int64_t t) {
+  const int lane = threadIdx.x & 31;
+  const int64_t rows = f.s.words->rows, padded = (rows + 127) / 128 * 128;
+  if (lane == 0 && t >= rows && t < padded) set_col<PARTS>(f, t, 1e30f, 0.f);
+  if (t == f.a.n - 1)
+    for (int64_t i = max(t + 1, rows) + lane; i < padded; i += 32) set_col<PARTS>(f, i, 1e30f, 0.f);
+}
+
+// What one lane writes of a row with maximum (or reference) m and sum l over it.
+template <int PARTS>
+__device__ __forceinline__ void finish_row(const Many& f, int64_t t, int64_t pos, float m, float l, float loss2) {
+  const SoftmaxArgs& a = f.a;
+  a.loss[t] = loss2 * kLn2 + (a.target.logits ? a.target.self[t] : 0.f);
+  a.lse[t] = (m + log2f(l)) * kLn2;
+  if (!f.s.col) return;
+  f.s.row_max[pos] = m;
+  f.s.row_sum[pos] = l;
+  const float weight = a.weight ? a.weight[t] : 1.f;
+  // fp16 probabilities: weight / 2^shift at most one, times 2^14
+  const float factor =
+      a.dtype == ESSPT_BF16 ? weight : times_pow2(weight, (int)kHalfShift - weight_shift_of(f.s.words->max_weight));
+  set_col<PARTS>(f, pos, m, factor / l);
+}
+
+// A warp per row: its statistics, the scores of its targets, its loss.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) loss_kernel(Many f) {
+  constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
+  const SoftmaxArgs& a = f.a;
+  const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  const int lane = threadIdx.x & 31;
+  if (t >= a.n || (f.if_redo && f.s.words->redo == 0u)) return;
+  const int64_t pos = f.s.pos[t];
+  if (f.s.col) pad_cols<kParts>(f, t);
+  if (pos < 0) {
+    if (lane == 0) a.loss[t] = a.lse[t] = 0.f;
+    return;
+  }
+  float m, l, loss2 = 0.f;
+  merge_slots(f, pos, a.V, m, l);
+  const float lse2 = m + log2f(l);
+  target_scores<T, VEC>(a, t, [&](int k, float q, float s) {
+    loss2 += q * (lse2 - s);
+    if (f.s.col) f.s.score[t * a.target.top + k] = s;
+  });
   loss2 = warp_sum(loss2);
-  if (lane == 0) {
-    a.loss[t] = loss2 * kLn2 + (a.target.logits ? a.target.self[t] : 0.f);
-    a.lse[t] = lse2 * kLn2;
-    if (f.s.col) {
-      f.s.row_max[pos] = m;
-      f.s.row_sum[pos] = l;
-      const float weight = a.weight ? a.weight[t] : 1.f;
-      // fp16 probabilities: weight / 2^shift at most one, times 2^14
-      const float factor = a.dtype == ESSPT_BF16 ? weight
-                                                 : times_pow2(weight, (int)kHalfShift - weight_shift_of(f.s.words->max_weight));
-      set_col<kParts>(f, pos, m, factor / l);
-    }
-  }
+  if (lane == 0) finish_row<kParts>(f, t, pos, m, l, loss2);
+}
+
+// A warp per row: a reference for its probabilities without all of its scores, the
+// largest of those of its targets and of W's first rows.  Probabilities may then be
+// larger than one; where one leaves the range of their type, which shows in the sums, the
+// exact passes run (grad_h_kernel).
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) reference_kernel(Many f) {
+  const SoftmaxArgs& a = f.a;
+  const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  if (t >= a.n) return;
+  const int64_t pos = f.s.pos[t];
+  if (pos < 0) return;
+  float m, l;
+  merge_slots(f, pos, f.sample, m, l);
+  target_scores<T, VEC>(a, t, [&](int k, float q, float s) {
+    m = fmaxf(m, s);
+    f.s.score[t * a.target.top + k] = s;
+  });
+  m = warp_max(m);
+  if ((threadIdx.x & 31) == 0) f.s.row_max[pos] = m == -INFINITY ? 0.f : m;
 }
 
 // Sum of a row of partial gradients over the slots of its group, columns d ...
@@ -270,18 +320,47 @@ __device__ __forceinline__ float rounded_off(float p) {
   return sizeof(T) == 4 ? 0.f : p - to_float(from_float<T>(p));
 }
 
-// dh, a warp per row: b weight (sum p w / l - sum q w_id).
-template <typename T, int VEC>
+// dh, a warp per row: b weight (sum p w / l - sum q w_id).  After a pass by references
+// (SAMPLED) the row's sum and loss come first, and a sum that is no number asks for the
+// exact passes.
+template <typename T, int VEC, bool SAMPLED>
 __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
+  constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
   const SoftmaxArgs& a = f.a;
   const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-  if (t >= a.n) return;
+  if (t >= a.n || (f.if_redo && f.s.words->redo == 0u)) return;
   const int64_t pos = f.s.pos[t];
+  if (SAMPLED) {
+    pad_cols<kParts>(f, t);
+    if (pos < 0 && (threadIdx.x & 31) == 0) a.loss[t] = a.lse[t] = 0.f;
+  }
+  float row_sum = 1.f;
+  if (SAMPLED && pos >= 0) {
+    const int lane = threadIdx.x & 31;
+    const Ranges r(f.s.words->rows, a.V, 1, f.blocks);
+    const int64_t g = pos / 128, i0 = r.block_of(g * r.n_b), i1 = r.block_of((g + 1) * r.n_b - 1);
+    const float* sums = reinterpret_cast<const float*>(f.s.stat);
+    float l = 0.f, loss2 = 0.f;
+    for (int64_t i = 4 * i0 + lane; i < 4 * i1 + 4; i += 32) l += sums[((i / 4 + g) * 4 + (i & 3)) * 128 + (pos & 127)];
+    row_sum = l = warp_sum(l) * exp2f(-f.up);
+    const float lse2 = f.s.row_max[pos] + log2f(l);
+    for (int64_t k = t * a.target.top + lane; k < (t + 1) * a.target.top; k += 32) {
+      const float q = a.target.logits ? a.target.q[k] : 1.f;
+      if (q != 0.f) loss2 += q * (lse2 - f.s.score[k]);
+    }
+    loss2 = warp_sum(loss2);
+    if (lane == 0) {
+      finish_row<kParts>(f, t, pos, f.s.row_max[pos], l, loss2);
+      if (!(l < 3e38f)) f.s.words->redo = 1u;
+    }
+  } else if (pos >= 0) {
+    row_sum = f.s.row_sum[pos];
+  }
   T* to = static_cast<T*>(a.grad_h) + t * a.D;
   const float bw = pos < 0 ? 0.f : a.b * (a.weight ? a.weight[t] : 1.f);
-  const float up = a.dtype == ESSPT_BF16 ? 0.f : kHalfShift;
+  const float up = f.up;
   const int shift = (f.parts == 2 ? half_shift_of(f.s.words->max_w) : 0) + (int)up;
-  const float inv = pos < 0 ? 0.f : 1.f / f.s.row_sum[pos], m = pos < 0 ? 0.f : f.s.row_max[pos];
+  const float inv = 1.f / row_sum, m = pos < 0 ? 0.f : f.s.row_max[pos];
   const int lane = threadIdx.x & 31;
   for (int d0 = 0; d0 < a.D; d0 += 32 * VEC) {
     const int d = d0 + lane * VEC;
@@ -291,6 +370,12 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
     for (int e = 0; e < VEC; ++e) x[e] = 0.f;
     if (pos >= 0) {
       if (on) add_slots<VEC>(f, f.s.words->rows, a.V, pos, d, x);
+      if (SAMPLED) {
+        bool fine = true;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) fine &= fabsf(x[e]) < 3e38f;
+        if (!fine) f.s.words->redo = 1u;
+      }
 #pragma unroll
       for (int e = 0; e < VEC; ++e) x[e] = ldexpf(x[e] * inv, -shift);
       for (int k0 = 0; k0 < a.target.top; k0 += 32) {
@@ -517,7 +602,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   const bool grads = a.grad_h != nullptr;
   const unsigned by_row = (unsigned)((a.n + 7) / 8);
-  Many f{a, s, mma_shape(Pass::kStats, a.D, kParts), a.sms, (a.D + 15) / 16 * 16, kParts};
+  Many f{a, s, mma_shape(Pass::kStats, a.D, kParts), a.sms, (a.D + 15) / 16 * 16, kParts, 0, 0.f, 0};
   if (!grads) f.s.col = nullptr;
   cudaError_t e = cudaMemsetAsync(s.words, 0, sizeof(ManyWords), a.st);
   if (e != cudaSuccess) return e;
@@ -551,21 +636,53 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   launch_units<T, kParts, VEC>(f, false);
 
   MmaArgs m{};
-  m.A = s.units_h, m.B = s.units_w, m.s = f.shape, m.words = s.words, m.V = a.V, m.b = a.b;
+  m.A = s.units_h, m.B = s.units_w, m.words = s.words, m.V = a.V, m.b = a.b;
   m.row_max = s.row_max, m.col = s.col, m.stat = s.stat, m.out = s.out, m.ld = f.ld;
-  m.run = INT32_MAX, m.status = a.target.status;
-  if ((e = launch_mma(Pass::kStats, kBf16, kParts, m, a.sms, 1, a.st)) != cudaSuccess) return e;
-  loss_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
-  if (!grads) return cudaGetLastError();
-
-  // Tiles between additions in fp32.  4096 x 18k, K = 100, lists of 32: dh is 3.1e-6 off
-  // with 32 tiles, 1.6e-6 with 16, 8.5e-7 with 8 (7.5e-7 by fp32 products of whole
-  // matrices), 4.2e-7 with 4; the call takes 478, 484, 496 and 512 us.
-  const int out_chunks = (a.D + 255) / 256;
-  m.run = kParts == 1 ? 128 : mma_shape(Pass::kRows, a.D, kParts).cross ? 16 : 8;
-  m.s = f.shape = mma_shape(Pass::kRows, a.D, kParts);
-  if ((e = launch_mma(Pass::kRows, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
-  grad_h_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
+  m.status = a.target.status;
+  // Tiles between additions in fp32.  4096 x 18k, K = 100, lists of 32: dh is 1.0e-6 off
+  // with 32 tiles, 5.8e-7 with 16, 3.4e-7 with 8 (7.5e-7 by fp32 products of whole
+  // matrices); the call takes as long with any of the three, to 1%.  Where the small
+  // products of halves have no sums of their own, half as many tiles.
+  const MmaShape stats_shape = mma_shape(Pass::kStats, a.D, kParts), rows_shape = mma_shape(Pass::kRows, a.D, kParts);
+  const int out_chunks = (a.D + 255) / 256, run_tiles = kParts == 1 ? 128 : rows_shape.cross ? 16 : 8;
+  // Maxima and sums over W's first `items` rows, and what is made of them.
+  auto stats = [&](int32_t items, int if_redo) {
+    f.shape = m.s = stats_shape, f.if_redo = m.if_redo = if_redo, m.V = items, m.run = INT32_MAX;
+    const cudaError_t err = launch_mma(Pass::kStats, kBf16, kParts, m, a.sms, 1, a.st);
+    m.V = a.V;
+    return err;
+  };
+  auto rows = [&](bool sampled, int if_redo) {
+    f.shape = m.s = rows_shape, f.if_redo = m.if_redo = if_redo, m.run = run_tiles;
+    f.up = m.up = kBf16 ? 0.f : sampled ? kSampledShift : kHalfShift;
+    m.sums = sampled ? reinterpret_cast<float*>(s.stat) : nullptr;
+    return launch_mma(Pass::kRows, kBf16, kParts, m, a.sms, out_chunks, a.st);
+  };
+  auto exact = [&](int if_redo) {
+    cudaError_t err = stats(a.V, if_redo);
+    if (err != cudaSuccess) return err;
+    loss_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
+    if (!grads) return cudaGetLastError();
+    if ((err = rows(false, if_redo)) != cudaSuccess) return err;
+    grad_h_kernel<T, VEC, false><<<by_row, 256, 0, a.st>>>(f);
+    return cudaGetLastError();
+  };
+  // A pass over all scores for the rows' maxima alone is a third of the work.  Where it
+  // is more than that of the launches that stand by (about 10 us), references from a
+  // sixteenth of W do, and the exact passes run only if one of them was too low.
+  const int64_t n_w = ((int64_t)a.V + 127) / 128;
+  if (grads && n_w >= 32 && (a.n + 127) / 128 * n_w >= 24ll * a.sms) {
+    f.sample = (int32_t)(128 * (n_w / 16));
+    if ((e = stats(f.sample, 0)) != cudaSuccess) return e;
+    reference_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
+    if ((e = rows(true, 0)) != cudaSuccess) return e;
+    grad_h_kernel<T, VEC, true><<<by_row, 256, 0, a.st>>>(f);
+    if ((e = exact(1)) != cudaSuccess) return e;
+  } else if ((e = exact(0)) != cudaSuccess) {
+    return e;
+  }
+  if (!grads) return cudaSuccess;
+  m.if_redo = f.if_redo = 0;
 
   if ((e = cudaStreamWaitEvent(a.st, s.join, 0)) != cudaSuccess) return e;
   if (sizeof(T) == 2) launch_runs();  // (want the statistics: entry_factor)

@@ -290,6 +290,12 @@ struct Issue {
   }
 };
 
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
+
 // Scores of columns from `left` on become -infinity.  Only a tile at the end of B has
 // any: a branch of its own (as selects these were most of the instructions).
 __device__ __forceinline__ void mask_scores(uint32_t (&r)[32], int left) {
@@ -312,7 +318,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   const int64_t rows_h = a.words->rows;
   const int64_t rows_a = PASS == Pass::kCols ? a.V : rows_h, rows_b = PASS == Pass::kCols ? rows_h : a.V;
   const Ranges ranges(rows_a, rows_b, sh.tiles, gridDim.x);
-  if (blockIdx.x >= ranges.blocks) return;
+  if (blockIdx.x >= ranges.blocks || (a.if_redo && a.words->redo == 0u)) return;
 
   const uint32_t base = (smem_addr(smem) + 1023u) & ~1023u;
   const uint32_t a_base = base, b_base = base + (sh.res ? sh.tiles * sh.nk * PARTS : 0) * kUnitBytes;
@@ -448,14 +454,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     // columns) are kept in registers, else where they go.
     constexpr int kKept = PARTS == 2 && !STATS ? 2 : 0;
     float kept[kKept > 0 ? kKept : 1][16];
+    float m = 0.f, l = 0.f, at = 0.f;  // kStats: maximum (without the scale), sum, and m scale; kRows: sum
     while (walk.next(g)) {
       const int nt = tiles_of(g);
       const int32_t jobs = nt * g.len;
-      float m = -INFINITY, l = 0.f, at = 0.f;  // kStats: maximum (without the scale), sum, and m scale
+      if (g.begins) m = -INFINITY, l = 0.f, at = 0.f;
       float offset = 0.f;
       if (PASS == Pass::kRows) {
         const int64_t r = g.group * 128 + row;
-        offset = r < rows_a ? (BF16 ? 0.f : kHalfShift) - a.row_max[r] : -1e30f;
+        offset = r < rows_a ? a.up - a.row_max[r] : -1e30f;
       }
       // Jobs go to the pairs by turns, and to the buffers by turns: with three buffers
       // both pairs come by each, so a pair counts the other's turns too.
@@ -489,8 +496,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
             float top[4] = {m, m, m, m};
 #pragma unroll
             for (int i = 0; i < 32; i += 2)
-              top[(i >> 1) & 3] = fmaxf(fmaxf(top[(i >> 1) & 3], __uint_as_float(r[c][i])), __uint_as_float(r[c][i + 1]));
-            const float m2 = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+              top[(i >> 1) & 3] = max3(top[(i >> 1) & 3], __uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1]));
+            const float m2 = fmaxf(max3(top[0], top[1], top[2]), top[3]);
             const float at2 = m2 == -INFINITY ? 0.f : m2 * scale;
             const u64 minus = pack2(-at2, -at2);
             u64 sum[2] = {0ull, 0ull};
@@ -509,6 +516,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         } else {
           const ulonglong2* cols = reinterpret_cast<const ulonglong2*>(col_data + at_col * 1024 + kColBytes / 2 * half);
           const u64 offset2 = pack2(offset, offset);
+          u64 sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             uint32_t out[16 * PARTS];
@@ -521,6 +529,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
               if (PASS == Pass::kRows) {
                 unpack2(fma2(s2, scale2, offset2), p[0], p[1]);
                 p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
+                sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(p[0], p[1]));
               } else if (PARTS == 2) {
                 const ulonglong2 q = cols[16 * c + i / 2];
                 unpack2(fma2(s2, scale2, q.x), p[0], p[1]);
@@ -547,8 +556,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
           fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);
+          if (PASS == Pass::kRows) l += sum2(add2(sum[0], sum[1]));
         }
       }
+      if (PASS == Pass::kRows && a.sums && g.ends && blockIdx.y == 0) a.sums[(g.slot * 4 + 2 * pair + half) * 128 + row] = l;
       if (PASS == Pass::kCols) col0 = (col0 + g.len) % sh.stages;
       if (STATS) {
         a.stat[(g.slot * 4 + 2 * pair + half) * 128 + row] = make_float2(m == -INFINITY ? m : at, l);

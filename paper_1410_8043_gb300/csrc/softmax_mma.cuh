@@ -9,7 +9,7 @@ namespace esspt {
 
 // What a pass makes of the scores S = A B^T (b / ln 2 times, see MmaArgs::scale):
 //   kStats  per row of A the maximum and the sum of 2^(S - maximum)
-//   kRows   A = H, B = W: sum over B's rows of 2^(S - row_max) B
+//   kRows   A = H, B = W: sum over B's rows of 2^(S - row_max) B, and of 2^(S - row_max)
 //   kCols   A = W, B = H: sum over B's rows t of 2^(S - maximum_t) factor_t B
 enum class Pass { kStats, kRows, kCols };
 
@@ -60,6 +60,9 @@ struct MmaArgs {
   // 16-bit rows a float to a column, log2 |factor| - maximum with the sign as its lowest bit.
   const float* col;
   float2* stat;          // kStats out: [slot][4][128], by group and half of the columns
+  float* sums;           // kRows out: sums of the probabilities, likewise, or null
+  float up;              // kRows: probabilities are taken 2^up times as large
+  int if_redo;           // only where words->redo is set
   float* out;            // else: [slot][128][ld]
   int ld;
   int run;               // tiles of B that the tensor core sums up before fp32 does
