@@ -421,12 +421,18 @@ cudaError_t run(const SoftmaxArgs& a, const FewScratch& s) {
 
 int few_blocks(int sms) { return 4 * sms; }
 
-bool few_rows(int64_t n, int64_t V, int32_t D, int32_t dtype) {
-  return n <= kFewRows || (n <= kSmallRows && n * V * D <= 200'000'000);
+// By what both ways take, in us, fitted to 12 to 128 rows on 1000 to 800k items of 16 to
+// 256 values (fp32 and bf16, with gradients and without).  With gradients, here and by
+// tensor cores: 20k items, K = 64, 128 rows 105 and 116; 200k, K = 64, 24 rows 177 and
+// 239, 48 rows 306 and 241.  Forward: 200k, K = 64, 24 rows 44 and 66, 48 rows 73 and 67.
+bool few_rows(int64_t n, int64_t V, int32_t D, bool grads) {
+  if (n <= kFewRows || n > kSmallRows) return n <= kFewRows;
+  const double items = (double)V, few = grads ? 45 + n * items * (1.6e-5 + 2.1e-7 * D) : 28 + n * items * (1e-6 + 7e-8 * D);
+  return few <= (grads ? 95 + items * (2.5e-4 + 5e-6 * D) : 44 + items * (5e-5 + 1e-6 * D));
 }
-int few_groups(int64_t max_rows, int64_t V, int32_t D, int32_t dtype) {
+int few_groups(int64_t max_rows, int64_t V, int32_t D, bool backward) {
   int64_t n = std::min<int64_t>(max_rows, kSmallRows);
-  while (!few_rows(n, V, D, dtype)) --n;
+  while (!few_rows(n, V, D, false) && !(backward && few_rows(n, V, D, true))) --n;
   return (int)((n + kFewRows - 1) / kFewRows);
 }
 

@@ -303,6 +303,7 @@ __device__ __forceinline__ void add_slots(const Many& f, int64_t rows_a, int64_t
   const int64_t i0 = r.block_of(g * r.n_b), i1 = r.block_of((g + 1) * r.n_b - 1);
 #pragma unroll
   for (int e = 0; e < VEC; ++e) x[e] = 0.f;
+#pragma unroll 8
   for (int64_t i = i0; i <= i1; ++i) {
     float y[VEC];
     load_vec<float, VEC>(f.s.out + ((i + g) * f.shape.tiles * 128 + in) * f.ld + d, y);
@@ -320,7 +321,7 @@ __device__ __forceinline__ float rounded_off(float p) {
   return sizeof(T) == 4 ? 0.f : p - to_float(from_float<T>(p));
 }
 
-// dh, a warp per row: b weight (sum p w / l - sum q w_id).  After a pass by references
+// dh, a warp per row and 32 VEC columns: b weight (sum p w / l - sum q w_id).  After a pass by references
 // (SAMPLED) the row's sum and loss come first, and a sum that is no number asks for the
 // exact passes.
 template <typename T, int VEC, bool SAMPLED>
@@ -330,7 +331,7 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
   const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
   if (t >= a.n || (f.if_redo && f.s.words->redo == 0u)) return;
   const int64_t pos = f.s.pos[t];
-  if (SAMPLED) {
+  if (SAMPLED && blockIdx.y == 0) {
     pad_cols<kParts>(f, t);
     if (pos < 0 && (threadIdx.x & 31) == 0) a.loss[t] = a.lse[t] = 0.f;
   }
@@ -349,7 +350,7 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
       if (q != 0.f) loss2 += q * (lse2 - f.s.score[k]);
     }
     loss2 = warp_sum(loss2);
-    if (lane == 0) {
+    if (lane == 0 && blockIdx.y == 0) {
       finish_row<kParts>(f, t, pos, f.s.row_max[pos], l, loss2);
       if (!(l < 3e38f)) f.s.words->redo = 1u;
     }
@@ -361,46 +362,43 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
   const float up = f.up;
   const int shift = (f.parts == 2 ? half_shift_of(f.s.words->max_w) : 0) + (int)up;
   const float inv = 1.f / row_sum, m = pos < 0 ? 0.f : f.s.row_max[pos];
-  const int lane = threadIdx.x & 31;
-  for (int d0 = 0; d0 < a.D; d0 += 32 * VEC) {
-    const int d = d0 + lane * VEC;
-    const bool on = d < a.D;
-    float x[VEC];
+  const int lane = threadIdx.x & 31, d = blockIdx.y * 32 * VEC + lane * VEC;
+  const bool on = d < a.D;
+  float x[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = 0.f;
-    if (pos >= 0) {
-      if (on) add_slots<VEC>(f, f.s.words->rows, a.V, pos, d, x);
-      if (SAMPLED) {
-        bool fine = true;
+  for (int e = 0; e < VEC; ++e) x[e] = 0.f;
+  if (pos >= 0) {
+    if (on) add_slots<VEC>(f, f.s.words->rows, a.V, pos, d, x);
+    if (SAMPLED) {
+      bool fine = true;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) fine &= fabsf(x[e]) < 3e38f;
-        if (!fine) f.s.words->redo = 1u;
-      }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) x[e] = ldexpf(x[e] * inv, -shift);
-      for (int k0 = 0; k0 < a.target.top; k0 += 32) {
-        const int count = min(32, a.target.top - k0);
-        const int64_t entry = t * a.target.top + k0 + lane;
-        const int32_t lane_id = lane < count ? a.target.ids[entry] : -1;
-        float c = lane >= count ? 0.f : a.target.logits ? -a.target.q[entry] : -1.f;
-        if (sizeof(T) == 2 && c != 0.f) c += ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - m + up)) * inv, -shift);
-        const unsigned share = __ballot_sync(0xffffffffu, c != 0.f);
-#pragma unroll 4
-        for (int i = 0; i < count; ++i) {
-          const float ci = __shfl_sync(0xffffffffu, c, i);
-          const int32_t id = __shfl_sync(0xffffffffu, lane_id, i);
-          if (!on || !(share >> i & 1u)) continue;
-          float y[VEC];
-          load_vec<T, VEC>(static_cast<const T*>(a.w) + id * a.w_stride + d, y);
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) x[e] = fmaf(ci, y[e], x[e]);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) x[e] *= bw;
+      for (int e = 0; e < VEC; ++e) fine &= fabsf(x[e]) < 3e38f;
+      if (!fine) f.s.words->redo = 1u;
     }
-    if (on) store_vec<T, VEC>(to + d, x);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = ldexpf(x[e] * inv, -shift);
+    for (int k0 = 0; k0 < a.target.top; k0 += 32) {
+      const int count = min(32, a.target.top - k0);
+      const int64_t entry = t * a.target.top + k0 + lane;
+      const int32_t lane_id = lane < count ? a.target.ids[entry] : -1;
+      float c = lane >= count ? 0.f : a.target.logits ? -a.target.q[entry] : -1.f;
+      if (sizeof(T) == 2 && c != 0.f) c += ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - m + up)) * inv, -shift);
+      const unsigned share = __ballot_sync(0xffffffffu, c != 0.f);
+#pragma unroll 4
+      for (int i = 0; i < count; ++i) {
+        const float ci = __shfl_sync(0xffffffffu, c, i);
+        const int32_t id = __shfl_sync(0xffffffffu, lane_id, i);
+        if (!on || !(share >> i & 1u)) continue;
+        float y[VEC];
+        load_vec<T, VEC>(static_cast<const T*>(a.w) + id * a.w_stride + d, y);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[e] = fmaf(ci, y[e], x[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] *= bw;
   }
+  if (on) store_vec<T, VEC>(to + d, x);
 }
 
 // The targets as (item, entry) pairs; what has no share sorts behind the last item.
@@ -486,16 +484,15 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
   int32_t t = 0;
   float g = 0.f;
   if (LEVEL == 0 && lane < kRun) g = entry_factor<T>(f, sizeof(T) == 2 ? cols_shift(f) : 0, val[first + lane], t);
-  for (int d = lane * VEC; d - lane * VEC < a.D; d += 32 * VEC) {
-    float x[VEC];
+  const int d = blockIdx.y * 32 * VEC + lane * VEC;
+  float x[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = 0.f;
-    if (LEVEL == 0)
-      add_rows<T, VEC>(a, kRun, t, g, d, x);
-    else
-      add_sums<VEC>(f.s.run_sum[0], (int32_t)(run * kRun), (int32_t)(run * kRun + kRun), a.D, d, x);
-    if (d < a.D) store_vec<float, VEC>(f.s.run_sum[LEVEL] + run * a.D + d, x);
-  }
+  for (int e = 0; e < VEC; ++e) x[e] = 0.f;
+  if (LEVEL == 0)
+    add_rows<T, VEC>(a, kRun, t, g, d, x);
+  else
+    add_sums<VEC>(f.s.run_sum[0], (int32_t)(run * kRun), (int32_t)(run * kRun + kRun), a.D, d, x);
+  if (d < a.D) store_vec<float, VEC>(f.s.run_sum[LEVEL] + run * a.D + d, x);
 }
 
 // dw: b (sum weight p h - sum weight q h), kItems items to a block.  Most items are
@@ -549,7 +546,10 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, const uint32_t* key
     for (int e = 0; e < VEC; ++e) x[e] = a.b * ldexpf(x[e], shift);
     store_vec<T, VEC>(to + item * a.D + d, x);
   }
-  for (int item = threadIdx.x / 32; item < items; item += 8) {
+  // (By item and 32 VEC columns.)
+  const int chunks = (a.D + 32 * VEC - 1) / (32 * VEC);
+  for (int part = threadIdx.x / 32; part < items * chunks; part += 8) {
+    const int item = part / chunks, d = (part - item * chunks) * 32 * VEC + lane * VEC;
     const int32_t begin = first[item], end = first[item + 1];
     if (begin == end) continue;
     // Whole runs [r0, r1), whole runs of runs [q0, q1), and single entries at both ends, one per lane.
@@ -561,19 +561,17 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, const uint32_t* key
     int32_t t = 0;
     float g = 0.f;
     if (lane < head + tail) g = entry_factor<T>(f, shift, val[lane < head ? begin + lane : end - tail + lane - head], t);
-    for (int d = lane * VEC; d - lane * VEC < a.D; d += 32 * VEC) {
-      float x[VEC], y[VEC];
+    float x[VEC], y[VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[e] = y[e] = 0.f;
-      if (d < a.D) sum(item, d, x);
-      add_rows<T, VEC>(a, head + tail, t, g, d, y);
-      add_sums<VEC>(f.s.run_sum[0], r0, q0 < q1 ? q0 * kRun : r1, a.D, d, y);
-      add_sums<VEC>(f.s.run_sum[0], q0 < q1 ? q1 * kRun : r1, r1, a.D, d, y);
-      add_sums<VEC>(f.s.run_sum[1], q0, q1, a.D, d, y);
+    for (int e = 0; e < VEC; ++e) x[e] = y[e] = 0.f;
+    if (d < a.D) sum(item, d, x);
+    add_rows<T, VEC>(a, head + tail, t, g, d, y);
+    add_sums<VEC>(f.s.run_sum[0], r0, q0 < q1 ? q0 * kRun : r1, a.D, d, y);
+    add_sums<VEC>(f.s.run_sum[0], q0 < q1 ? q1 * kRun : r1, r1, a.D, d, y);
+    add_sums<VEC>(f.s.run_sum[1], q0, q1, a.D, d, y);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[e] = a.b * (ldexpf(x[e], shift) - y[e]);
-      if (d < a.D) store_vec<T, VEC>(to + item * a.D + d, x);
-    }
+    for (int e = 0; e < VEC; ++e) x[e] = a.b * (ldexpf(x[e], shift) - y[e]);
+    if (d < a.D) store_vec<T, VEC>(to + item * a.D + d, x);
   }
 }
 
@@ -601,7 +599,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   const bool grads = a.grad_h != nullptr;
-  const unsigned by_row = (unsigned)((a.n + 7) / 8);
+  const unsigned by_row = (unsigned)((a.n + 7) / 8), col_chunks = (unsigned)((a.D + 32 * VEC - 1) / (32 * VEC));
   Many f{a, s, mma_shape(Pass::kStats, a.D, kParts), a.sms, (a.D + 15) / 16 * 16, kParts, 0, 0.f, 0};
   if (!grads) f.s.col = nullptr;
   cudaError_t e = cudaMemsetAsync(s.words, 0, sizeof(ManyWords), a.st);
@@ -612,9 +610,9 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   auto launch_runs = [&]() {
     const cudaStream_t st = sizeof(T) == 2 ? a.st : s.side;
     if (entries >= kRun)
-      runs_kernel<T, VEC, 0><<<(unsigned)((entries / kRun + 7) / 8), 256, 0, st>>>(f, key.Current(), val.Current());
+      runs_kernel<T, VEC, 0><<<dim3((unsigned)((entries / kRun + 7) / 8), col_chunks), 256, 0, st>>>(f, key.Current(), val.Current());
     if (entries >= kRun * kRun)
-      runs_kernel<T, VEC, 1><<<(unsigned)((entries / kRun / kRun + 7) / 8), 256, 0, st>>>(f, key.Current(), val.Current());
+      runs_kernel<T, VEC, 1><<<dim3((unsigned)((entries / kRun / kRun + 7) / 8), col_chunks), 256, 0, st>>>(f, key.Current(), val.Current());
   };
   if (grads) {
     if ((e = cudaEventRecord(s.fork, a.st)) != cudaSuccess || (e = cudaStreamWaitEvent(s.side, s.fork, 0)) != cudaSuccess) return e;
@@ -664,7 +662,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
     loss_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
     if (!grads) return cudaGetLastError();
     if ((err = rows(false, if_redo)) != cudaSuccess) return err;
-    grad_h_kernel<T, VEC, false><<<by_row, 256, 0, a.st>>>(f);
+    grad_h_kernel<T, VEC, false><<<dim3(by_row, col_chunks), 256, 0, a.st>>>(f);
     return cudaGetLastError();
   };
   // A pass over all scores for the rows' maxima alone is a third of the work.  Where it
@@ -676,7 +674,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
     if ((e = stats(f.sample, 0)) != cudaSuccess) return e;
     reference_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
     if ((e = rows(true, 0)) != cudaSuccess) return e;
-    grad_h_kernel<T, VEC, true><<<by_row, 256, 0, a.st>>>(f);
+    grad_h_kernel<T, VEC, true><<<dim3(by_row, col_chunks), 256, 0, a.st>>>(f);
     if ((e = exact(1)) != cudaSuccess) return e;
   } else if ((e = exact(0)) != cudaSuccess) {
     return e;
