@@ -76,15 +76,19 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
 __device__ __forceinline__ uint32_t pack16_rest(uint32_t p, float lo, float hi) {
   const __half2 h = *reinterpret_cast<const __half2*>(&p);
   const float2 f = __half22float2(h);
-  return pack16<false>(lo - f.x, hi - f.y);
+  float x, y;
+  unpack2(fma2(pack2(f.x, f.y), pack2(-1.f, -1.f), pack2(lo, hi)), x, y);
+  return pack16<false>(x, y);
 }
 
-// Sums: the 128 probabilities of every row (half `part`) times units of B.
+// Sums: the 128 probabilities of every row (half `part`) times units of B.  They lie in
+// the place of their scores, 16 words for 32 values, of halves 8 and 8 for 16 values.
+template <int PARTS>
 __device__ __forceinline__ void sums_mma(uint32_t d, uint32_t p, int part, uint32_t b, uint32_t idesc, uint32_t add,
                                          uint32_t leader) {
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    mma_ts(d, p + 32 * (k >> 1) + 8 * (k & 1) + 16 * part, b + 128 * k, idesc, k > 0 ? 1u : add, leader);
+    mma_ts(d, p + (PARTS == 2 ? 16 * k + 8 * part : 32 * (k >> 1) + 8 * (k & 1)), b + 128 * k, idesc, k > 0 ? 1u : add, leader);
 }
 
 // A place in the ring of stages, with what is used of it.
@@ -219,11 +223,11 @@ struct Issue {
     if constexpr (PARTS == 2 && NK == 1) {
       // hi (hi | lo): the two units are the halves of 128 columns, the sums too.
       const uint32_t b = desc_mn(kept.at);
-      sums_mma(d, p, 0, b, mma_desc(BF16, 128, true), more, leader);
-      sums_mma(d + 64, p, 1, b, mma_desc(BF16, out_cols, true), 1, leader);
+      sums_mma<PARTS>(d, p, 0, b, mma_desc(BF16, 128, true), more, leader);
+      sums_mma<PARTS>(d + 64, p, 1, b, mma_desc(BF16, out_cols, true), 1, leader);
       free(kept);
     } else if constexpr (S.stage_units == NK * PARTS) {
-      sums_mma(d, p, 0, desc_mn(kept.at), mma_desc(BF16, out_cols, true), more, leader);
+      sums_mma<PARTS>(d, p, 0, desc_mn(kept.at), mma_desc(BF16, out_cols, true), more, leader);
       free(kept);
     } else {
       Ring& from = S.keep ? kept : ring;
@@ -237,8 +241,8 @@ struct Issue {
           if (!S.keep) take(from);
           const uint32_t b = desc_mn(from.at);
           const uint32_t cross = d + 64 * kc + (S.cross ? 64 * NK : 0);
-          if (PARTS == 2 && part == 0) sums_mma(cross, p, 1, b, idesc, more, leader);
-          sums_mma(part == 0 ? d + 64 * kc : cross, p, 0, b, idesc, part == 1 || (PARTS == 2 && !S.cross) ? 1 : more, leader);
+          if (PARTS == 2 && part == 0) sums_mma<PARTS>(cross, p, 1, b, idesc, more, leader);
+          sums_mma<PARTS>(part == 0 ? d + 64 * kc : cross, p, 0, b, idesc, part == 1 || (PARTS == 2 && !S.cross) ? 1 : more, leader);
           free(from);
         }
       }
@@ -450,10 +454,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const bool negative = PASS == Pass::kCols && a.words->negative != 0u;
     uint32_t phase = 0, o_phase = 0;  // parities of s_full's next turn, a bit per buffer
     int col0 = 0;  // stage of the run's first column data
-    // fp32 rows of up to 128 values: a thread's sums over the runs so far (two times 16
-    // columns) are kept in registers, else where they go.
-    constexpr int kKept = PARTS == 2 && !STATS ? 2 : 0;
-    float kept[kKept > 0 ? kKept : 1][16];
     float m = 0.f, l = 0.f, at = 0.f;  // kStats: maximum (without the scale), sum, and m scale; kRows: sum
     while (walk.next(g)) {
       const int nt = tiles_of(g);
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         fence_after();
         const int left = (int)min((int64_t)64, rows_b - (g.first + j) * 128 - 64 * half);  // of this half's columns
         const uint32_t s_at = lanes + 128 * at_buf + 64 * half;
-        // (fp32 rows: one half at a time, for the registers that hold sums.)
+        // (fp32 rows: 32 columns at a time, for the registers.)
         constexpr bool kBoth = STATS || PARTS == 1;
         uint32_t r[kBoth ? 2 : 1][32];
         if constexpr (kBoth) tmem_load(r[0], s_at, r[1], s_at + 32);
@@ -519,38 +519,40 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
           u64 sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            uint32_t out[16 * PARTS];
             if (!kBoth && c == 1) tmem_load(r[0], s_at + 32);
             if (PASS == Pass::kRows) mask_scores(r[kBoth ? c : 0], left - 32 * c);
+            // 16 words at a time: 32 values, or the halves of 16.
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const u64 s2 = pack2(__uint_as_float(r[kBoth ? c : 0][i]), __uint_as_float(r[kBoth ? c : 0][i + 1]));
-              float p[2];
-              if (PASS == Pass::kRows) {
-                unpack2(fma2(s2, scale2, offset2), p[0], p[1]);
-                p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
-                sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(p[0], p[1]));
-              } else if (PARTS == 2) {
-                const ulonglong2 q = cols[16 * c + i / 2];
-                unpack2(fma2(s2, scale2, q.x), p[0], p[1]);
-                unpack2(mul2(pack2(exp2_fast(p[0]), exp2_fast(p[1])), q.y), p[0], p[1]);
-              } else {
-                const ulonglong2 q = cols[8 * c + i / 4];
-                const u64 k = i & 2 ? q.y : q.x;
-                unpack2(fma2(s2, scale2, k), p[0], p[1]);
-                p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
-                if (negative) {  // a factor's sign is the lowest bit of its logarithm
-                  p[0] = __uint_as_float(__float_as_uint(p[0]) ^ ((uint32_t)k << 31));
-                  p[1] = __uint_as_float(__float_as_uint(p[1]) ^ ((uint32_t)(k >> 32) << 31));
+            for (int i0 = 0; i0 < 32; i0 += 32 / PARTS) {
+              uint32_t out[16];
+#pragma unroll
+              for (int i = i0; i < i0 + 32 / PARTS; i += 2) {
+                const u64 s2 = pack2(__uint_as_float(r[kBoth ? c : 0][i]), __uint_as_float(r[kBoth ? c : 0][i + 1]));
+                float p[2];
+                if (PASS == Pass::kRows) {
+                  unpack2(fma2(s2, scale2, offset2), p[0], p[1]);
+                  p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
+                  sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(p[0], p[1]));
+                } else if (PARTS == 2) {
+                  const ulonglong2 q = cols[16 * c + i / 2];
+                  unpack2(fma2(s2, scale2, q.x), p[0], p[1]);
+                  unpack2(mul2(pack2(exp2_fast(p[0]), exp2_fast(p[1])), q.y), p[0], p[1]);
+                } else {
+                  const ulonglong2 q = cols[8 * c + i / 4];
+                  const u64 k = i & 2 ? q.y : q.x;
+                  unpack2(fma2(s2, scale2, k), p[0], p[1]);
+                  p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
+                  if (negative) {  // a factor's sign is the lowest bit of its logarithm
+                    p[0] = __uint_as_float(__float_as_uint(p[0]) ^ ((uint32_t)k << 31));
+                    p[1] = __uint_as_float(__float_as_uint(p[1]) ^ ((uint32_t)(k >> 32) << 31));
+                  }
                 }
+                const int o = (i - i0) / 2;
+                out[o] = pack16<BF16>(p[0], p[1]);
+                if constexpr (PARTS == 2) out[8 + o] = pack16_rest(out[o], p[0], p[1]);
               }
-              out[i / 2] = pack16<BF16>(p[0], p[1]);
-              if constexpr (PARTS == 2) out[16 + i / 2] = pack16_rest(out[i / 2], p[0], p[1]);
+              tmem_store16(s_at + 32 * c + i0, out);
             }
-            if constexpr (PARTS == 2)
-              tmem_store32(s_at + 32 * c, out);
-            else
-              tmem_store16(s_at + 32 * c, out);
           }
           tmem_wait_store();
           fence_before();
@@ -570,38 +572,21 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       fence_after();
       float* to = a.out + (g.slot * 128 + row) * (int64_t)a.ld + blockIdx.y * 256;
       const uint32_t o_at = lanes + 128 * sh.buffers;
-      if (kKept > 0 && sh.cross) {
-#pragma unroll
-        for (int k = 0; k < kKept; ++k) {
-          const int c = 4 * k + 2 * pair + half;
-          if (16 * c >= out_cols) break;
-          uint32_t v[16], x[16];
-          tmem_load(v, o_at + 16 * c, x, o_at + 64 * sh.nk + 16 * c);
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            kept[k][i] = (g.begins ? 0.f : kept[k][i]) + (__uint_as_float(v[i]) + __uint_as_float(x[i]));
-        }
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar.o_empty);
-        if (!g.ends) continue;
-#pragma unroll
-        for (int k = 0; k < kKept; ++k) {
-          const int c = 4 * k + 2 * pair + half;
-          if (16 * c >= out_cols) break;
-          float4* p = reinterpret_cast<float4*>(to + 16 * c);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = make_float4(kept[k][4 * i], kept[k][4 * i + 1], kept[k][4 * i + 2], kept[k][4 * i + 3]);
-        }
-        continue;
-      }
       for (int c = 2 * pair + half; 16 * c < out_cols; c += 4) {
-        uint32_t v[16];
-        tmem_load(v, o_at + 16 * c);
+        // (What is added to is on its way while tensor memory is read.)
         float4* p = reinterpret_cast<float4*>(to + 16 * c);
         float4 y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = g.begins ? make_float4(0.f, 0.f, 0.f, 0.f) : p[i];
+        uint32_t v[16];
+        if (PARTS == 2 && sh.cross) {
+          uint32_t x[16];
+          tmem_load(v, o_at + 16 * c, x, o_at + 64 * sh.nk + 16 * c);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(x[i]));
+        } else {
+          tmem_load(v, o_at + 16 * c);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           p[i] = make_float4(y[i].x + __uint_as_float(v[4 * i]), y[i].y + __uint_as_float(v[4 * i + 1]),
