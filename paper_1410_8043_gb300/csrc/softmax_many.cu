@@ -432,22 +432,24 @@ __device__ __forceinline__ int cols_shift(const Many& f) {
          (f.a.dtype == ESSPT_BF16 ? 0 : weight_shift_of(f.s.words->max_weight) - (int)kHalfShift);
 }
 
-// An entry's row of H, and weight q less what rounding took.
+// Of every entry in order of the items its row of H, and weight q less what rounding took.
 template <typename T>
-__device__ __forceinline__ float entry_factor(const Many& f, int shift, uint32_t entry, int32_t& t) {
+__global__ void factors_kernel(Many f, const uint32_t* key, const uint32_t* val, int32_t* row, float* factor) {
   const SoftmaxArgs& a = f.a;
-  t = (int32_t)(entry / (uint32_t)a.target.top);
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= a.n * a.target.top || key[i] == (uint32_t)a.V) return;
+  const uint32_t entry = val[i];
+  const int32_t t = (int32_t)(entry / (uint32_t)a.target.top);
   const float q = a.target.logits ? a.target.q[entry] : 1.f;
   float g = a.weight ? q * a.weight[t] : q;
-  if (sizeof(T) == 2) {
-    g -= ldexpf(rounded_off<T>(col_probability(f, f.s.pos[t], f.s.score[entry])), shift);
-  }
-  return g;
+  if (sizeof(T) == 2) g -= ldexpf(rounded_off<T>(col_probability(f, f.s.pos[t], f.s.score[entry])), cols_shift(f));
+  row[i] = t;
+  factor[i] = g;
 }
 // x += g h_t [d ...] over the first `count` lanes' entries, all lanes taking part.
 template <typename T, int VEC>
 __device__ __forceinline__ void add_rows(const SoftmaxArgs& a, int count, int32_t lane_t, float lane_g, int d, float (&x)[VEC]) {
-#pragma unroll 4
+#pragma unroll 8
   for (int i = 0; i < count; ++i) {
     const float g = __shfl_sync(0xffffffffu, lane_g, i);
     const int64_t t = __shfl_sync(0xffffffffu, lane_t, i);
@@ -474,7 +476,7 @@ __device__ __forceinline__ void add_sums(const float* sums, int32_t begin, int32
 // kRun such runs (level 1), a warp each: no item of dw then adds more than 30 rows, 30
 // runs and what its entries make of runs of runs.
 template <typename T, int VEC, int LEVEL>
-__global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, const uint32_t* val) {
+__global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, const int32_t* row, const float* factor) {
   constexpr int kLong = LEVEL == 0 ? kRun : kRun * kRun;
   const SoftmaxArgs& a = f.a;
   const int64_t run = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, first = run * kLong;
@@ -483,7 +485,7 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
   if (key[first] != key[first + kLong - 1] || key[first] == (uint32_t)a.V) return;
   int32_t t = 0;
   float g = 0.f;
-  if (LEVEL == 0 && lane < kRun) g = entry_factor<T>(f, sizeof(T) == 2 ? cols_shift(f) : 0, val[first + lane], t);
+  if (LEVEL == 0 && lane < kRun) t = row[first + lane], g = factor[first + lane];
   const int d = blockIdx.y * 32 * VEC + lane * VEC;
   float x[VEC];
 #pragma unroll
@@ -499,7 +501,7 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
 // nobody's target: those rows go through all threads side by side, the others a warp each.
 constexpr int kItems = 64;
 template <typename T, int VEC>
-__global__ void __launch_bounds__(256) grad_w_kernel(Many f, const uint32_t* key, const uint32_t* val) {
+__global__ void __launch_bounds__(256) grad_w_kernel(Many f, const uint32_t* key, const int32_t* row, const float* factor) {
   __shared__ int32_t first[kItems + 1];
   __shared__ int64_t slots[2];
   const SoftmaxArgs& a = f.a;
@@ -560,7 +562,10 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, const uint32_t* key
     if (q0 >= q1) q0 = q1 = 0;
     int32_t t = 0;
     float g = 0.f;
-    if (lane < head + tail) g = entry_factor<T>(f, shift, val[lane < head ? begin + lane : end - tail + lane - head], t);
+    if (lane < head + tail) {
+      const int32_t i = lane < head ? begin + lane : end - tail + lane - head;
+      t = row[i], g = factor[i];
+    }
     float x[VEC], y[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) x[e] = y[e] = 0.f;
@@ -607,12 +612,18 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   // The targets by item, on the handle's second stream beside what follows.
   const int64_t entries = a.n * a.target.top, tiles = ((int64_t)a.V + 127) / 128;
   cub::DoubleBuffer<uint32_t> key(s.key[0], s.key[1]), val(s.val[0], s.val[1]);
-  auto launch_runs = [&]() {
-    const cudaStream_t st = sizeof(T) == 2 ? a.st : s.side;
+  // (The sort leaves one of its buffers of each pair free.)
+  int32_t* entry_row = nullptr;
+  float* entry_factor = nullptr;
+  auto launch_runs = [&](cudaStream_t st) {
+    entry_row = reinterpret_cast<int32_t*>(val.Alternate()), entry_factor = reinterpret_cast<float*>(key.Alternate());
+    factors_kernel<T><<<(unsigned)((entries + 255) / 256), 256, 0, st>>>(f, key.Current(), val.Current(), entry_row, entry_factor);
     if (entries >= kRun)
-      runs_kernel<T, VEC, 0><<<dim3((unsigned)((entries / kRun + 7) / 8), col_chunks), 256, 0, st>>>(f, key.Current(), val.Current());
+      runs_kernel<T, VEC, 0>
+          <<<dim3((unsigned)((entries / kRun + 7) / 8), col_chunks), 256, 0, st>>>(f, key.Current(), entry_row, entry_factor);
     if (entries >= kRun * kRun)
-      runs_kernel<T, VEC, 1><<<dim3((unsigned)((entries / kRun / kRun + 7) / 8), col_chunks), 256, 0, st>>>(f, key.Current(), val.Current());
+      runs_kernel<T, VEC, 1>
+          <<<dim3((unsigned)((entries / kRun / kRun + 7) / 8), col_chunks), 256, 0, st>>>(f, key.Current(), entry_row, entry_factor);
   };
   if (grads) {
     if ((e = cudaEventRecord(s.fork, a.st)) != cudaSuccess || (e = cudaStreamWaitEvent(s.side, s.fork, 0)) != cudaSuccess) return e;
@@ -622,7 +633,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
         cudaSuccess)
       return e;
     tile_first_kernel<<<(unsigned)(tiles / 256 + 1), 256, 0, s.side>>>(f, key.Current());
-    if (sizeof(T) == 4) launch_runs();
+    if (sizeof(T) == 4) launch_runs(s.side);
     if ((e = cudaEventRecord(s.join, s.side)) != cudaSuccess) return e;
   }
   compact_kernel<<<(unsigned)((a.n + 1023) / 1024), 1024, 0, a.st>>>(f);
@@ -683,10 +694,10 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   m.if_redo = f.if_redo = 0;
 
   if ((e = cudaStreamWaitEvent(a.st, s.join, 0)) != cudaSuccess) return e;
-  if (sizeof(T) == 2) launch_runs();  // (want the statistics: entry_factor)
+  if (sizeof(T) == 2) launch_runs(a.st);  // (wants the rows' sums)
   m.A = s.units_w, m.B = s.units_h;
   if ((e = launch_mma(Pass::kCols, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
-  grad_w_kernel<T, VEC><<<(unsigned)(((int64_t)a.V + kItems - 1) / kItems), 256, 0, a.st>>>(f, key.Current(), val.Current());
+  grad_w_kernel<T, VEC><<<(unsigned)(((int64_t)a.V + kItems - 1) / kItems), 256, 0, a.st>>>(f, key.Current(), entry_row, entry_factor);
   return cudaGetLastError();
 }
 

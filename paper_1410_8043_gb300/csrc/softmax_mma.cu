@@ -114,7 +114,7 @@ struct Issue {
   static constexpr bool STATS = PASS == Pass::kStats;
   static constexpr MmaShape S = mma_shape(PASS, 64 * NK, PARTS);
   static constexpr uint32_t kIdesc = mma_desc(BF16, 128, false);
-  static constexpr uint32_t kUnit = kUnitBytes >> 4, kTile = NK * PARTS * kUnit;  // in descriptors
+  static constexpr uint32_t kUnit = kUnitBytes >> 4;  // in descriptors
   const Bars& bar;
   volatile uint32_t* dead;
   const uint32_t leader, tmem, a_base;
@@ -178,11 +178,26 @@ struct Issue {
       for (int tile = 0; tile < NT; ++tile) {
 #pragma unroll
         for (int kc = 0; kc < NK - 1; ++kc)
-          pair<4>(d + 128 * tile, a_base + tile * kTile + kc * kUnit, b + kc * kUnit, NK * kUnit, NK * kUnit, kc > 0);
-        pair_last(d + 128 * tile, a_base + tile * kTile + (NK - 1) * kUnit, b + (NK - 1) * kUnit, NK * kUnit, NK * kUnit, NK > 1);
+          pair<4>(d + 128 * tile, a_base + tile * NK * PARTS * kUnit + kc * kUnit, b + kc * kUnit, NK * kUnit, NK * kUnit, kc > 0);
+        pair_last(d + 128 * tile, a_base + tile * NK * PARTS * kUnit + (NK - 1) * kUnit, b + (NK - 1) * kUnit, NK * kUnit, NK * kUnit, NK > 1);
       }
       if (STATS) free(ring);
       else ring.next();
+    } else if constexpr (S.stage_units == 2) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        take(ring);
+        const uint32_t b = desc_k(ring.at);
+        if constexpr (PARTS == 2) {
+          if (k == 0) pair<4>(d, a_base, b, NK * kUnit, kUnit, 0);
+          else pair_last(d, a_base + kUnit, b, NK * kUnit, kUnit, 1);
+        } else {
+          pair<4>(d, a_base + 2 * k * kUnit, b, 0, 0, k > 0);
+          if (k == 0) pair<4>(d, a_base + kUnit, b + kUnit, 0, 0, 1);
+          else pair_last(d, a_base + 3 * kUnit, b + kUnit, 0, 0, 1);
+        }
+        ring.next();
+      }
     } else {
       auto unit = [&](Ring& r) {
         take(r);
@@ -203,9 +218,9 @@ struct Issue {
 #pragma unroll
         for (int tile = 0; tile < NT; ++tile) {
           if (kc < NK - 1)
-            pair<4>(d + 128 * tile, ua[0] + tile * kTile, ub[0], ua[1] - ua[0], ub[1] - ub[0], kc > 0);
+            pair<4>(d + 128 * tile, ua[0] + tile * NK * PARTS * kUnit, ub[0], ua[1] - ua[0], ub[1] - ub[0], kc > 0);
           else
-            pair_last(d + 128 * tile, ua[0] + tile * kTile, ub[0], ua[1] - ua[0], ub[1] - ub[0], kc > 0);
+            pair_last(d + 128 * tile, ua[0] + tile * NK * PARTS * kUnit, ub[0], ua[1] - ua[0], ub[1] - ub[0], kc > 0);
         }
         if constexpr (!STATS && S.keep) {
           ring = r;
@@ -220,12 +235,23 @@ struct Issue {
   __device__ __forceinline__ void sums(uint32_t buf, uint32_t more) {
     done(buf);
     const uint32_t p = tmem + 128 * buf, d = tmem + 128 * S.buffers;
-    if constexpr (PARTS == 2 && NK == 1) {
-      // hi (hi | lo): the two units are the halves of 128 columns, the sums too.
-      const uint32_t b = desc_mn(kept.at);
-      sums_mma<PARTS>(d, p, 0, b, mma_desc(BF16, 128, true), more, leader);
-      sums_mma<PARTS>(d + 64, p, 1, b, mma_desc(BF16, out_cols, true), 1, leader);
-      free(kept);
+    if constexpr (S.cross) {
+      // hi (hi | lo) and lo hi: a stage is the two halves of a unit, 128 columns, and so are
+      // the sums of the products of halves hi hi, and of hi lo and lo hi.
+#pragma unroll
+      for (int kc = 0; kc < NK; ++kc) {
+        const uint32_t b = desc_mn(kept.at), to = d + 128 * kc;
+        sums_mma<PARTS>(to, p, 0, b, mma_desc(BF16, 128, true), more, leader);
+        sums_mma<PARTS>(to + 64, p, 1, b, mma_desc(BF16, min(64, out_cols - 64 * kc), true), 1, leader);
+        free(kept);
+      }
+    } else if constexpr (S.stage_units == 2 && NK == 4) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (k == 1 && out_cols <= 128) break;
+        sums_mma<PARTS>(d + 128 * k, p, 0, desc_mn(kept.at), mma_desc(BF16, min(128, out_cols - 128 * k), true), more, leader);
+        free(kept);
+      }
     } else if constexpr (S.stage_units == NK * PARTS) {
       sums_mma<PARTS>(d, p, 0, desc_mn(kept.at), mma_desc(BF16, out_cols, true), more, leader);
       free(kept);
@@ -240,9 +266,8 @@ struct Issue {
         for (int part = 0; part < PARTS; ++part) {
           if (!S.keep) take(from);
           const uint32_t b = desc_mn(from.at);
-          const uint32_t cross = d + 64 * kc + (S.cross ? 64 * NK : 0);
-          if (PARTS == 2 && part == 0) sums_mma<PARTS>(cross, p, 1, b, idesc, more, leader);
-          sums_mma<PARTS>(part == 0 ? d + 64 * kc : cross, p, 0, b, idesc, part == 1 || (PARTS == 2 && !S.cross) ? 1 : more, leader);
+          if (PARTS == 2 && part == 0) sums_mma<PARTS>(d + 64 * kc, p, 1, b, idesc, more, leader);
+          sums_mma<PARTS>(d + 64 * kc, p, 0, b, idesc, PARTS == 2 ? 1 : more, leader);
           free(from);
         }
       }
@@ -363,11 +388,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       int col = 0;  // stage of the column data
       uint32_t a_phase = 1, loads = 0, segs = 0;
       const uint32_t stage_bytes = sh.stage_units * kUnitBytes;
-      auto load = [&](const char* from, const char* cols) {
+      // A stage of what lies at `from`, or its second unit `apart` further on.
+      auto load = [&](const char* from, const char* cols, uint32_t apart = 0) {
         mbar_wait(ring.bar + kEmpty, ring.phase ^ 1, dead);
         if (*dead) return;
         mbar_expect(ring.bar, stage_bytes + (cols ? kColBytes : 0));
-        bulk_load(ring.at, from, stage_bytes, ring.bar);
+        bulk_load(ring.at, from, apart ? kUnitBytes : stage_bytes, ring.bar);
+        if (apart) bulk_load(ring.at + kUnitBytes, from + apart, kUnitBytes, ring.bar);
         if (cols) bulk_load(col_base + col * 1024, cols, kColBytes, ring.bar);
         ring.next();
         ++loads;
@@ -377,6 +404,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         const char* cols = PASS == Pass::kCols ? reinterpret_cast<const char*>(a.col) + tile * kColBytes : nullptr;
         if (sh.stage_units == sh.nk * PARTS) {
           load(from, cols);
+        } else if (sh.stage_units == 2) {  // two units of a row's, or the halves of one
+          for (int k = 0; k < 2; ++k)
+            load(from + k * (PARTS == 2 ? 1 : 2) * kUnitBytes, k == 0 ? cols : nullptr, PARTS == 2 ? sh.nk * kUnitBytes : 0);
         } else {
           for (int kc = 0; kc < sh.nk; ++kc) {
             if (!sh.res)
@@ -581,7 +611,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         uint32_t v[16];
         if (PARTS == 2 && sh.cross) {
           uint32_t x[16];
-          tmem_load(v, o_at + 16 * c, x, o_at + 64 * sh.nk + 16 * c);
+          const uint32_t at16 = o_at + 128 * (c >> 2) + 16 * (c & 3);
+          tmem_load(v, at16, x, at16 + 64);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(x[i]));
         } else {

@@ -24,7 +24,7 @@ constexpr int kMmaThreads = 640;       // a warp that loads, one that multiplies
 //
 // Up to two units a row (t), a stage is a tile of B.  Above, stages are units: a tile
 // of B is then never waited for as a whole (K = 256, bf16: with two stages of 64 KB a
-// tile waited 940 of 3150 cycles).  Two tiles of A share B where only the scores are
+// tile waited 940 of 3150 cycles), or pairs of units where two tiles of four fit.  Two tiles of A share B where only the scores are
 // wanted and three units are left for it; with sums, a third buffer of scores is worth
 // more than sharing.
 struct MmaShape {
@@ -42,7 +42,7 @@ __host__ __device__ constexpr MmaShape mma_shape(Pass pass, int32_t D, int parts
   s.tiles = stats && 2 * t + 3 <= kUnits ? 2 : 1;
   s.res = s.tiles == 2 || t + (parts == 2 ? 4 : 3) <= kUnits;
   s.keep = s.res && 3 * t <= kUnits;
-  s.stage_units = t <= 2 ? t : 1;
+  s.stage_units = t <= 2 ? t : t == 4 && !stats ? 2 : 1;
   s.stages = (kUnits - (s.res ? s.tiles * t : 0)) / s.stage_units;
   s.buffers = stats ? 4 : t <= 2 ? 3 : 2;
   s.cross = !stats && parts == 2 && s.nk <= 2;
