@@ -218,6 +218,24 @@ def test_scores_far_above_the_first_items(rows, dtype):
     _check(_run("loss", h, w, ids, z, weight, 1.0), ref, dtype, D, 1.0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("T", [8, 60, 900])
+def test_near_a_fit(T, dtype):
+    """Targets with p of about 0.99: the gradients are the small differences p - q.  The
+    other items' p keep the type's relative precision, so do the results; p of the target
+    rounded to the type would be off by up to 2^-9 of one, a fifth of 1 - p and more."""
+    V, D = 2000, 64
+    h, w, ids, z, weight = _inputs(T, V, D, dtype, 1, 19, pad=0.0)
+    weight = weight.abs() + 0.5
+    h = (w[ids[:, 0].long()].float() * 0.9).to(h.dtype)
+    ref = _reference(h, w, ids, torch.zeros_like(z), weight, 1.0)
+    assert 1e-4 < float(ref["loss"].median()) < 5e-2
+    r = _run("loss", h, w, ids, z, weight, 1.0)
+    for name in ("grad_h", "grad_w"):
+        err = (getattr(r, name).double() - ref[name]).norm() / ref[name].norm()
+        assert float(err) <= 2 * HALF_UNIT[dtype], (name, float(err))
+
+
 @pytest.mark.parametrize("T,V,D", SIDES)
 @pytest.mark.parametrize("size", [1e-12, 1e-3, 30.0, 3000.0])
 def test_magnitudes(T, V, D, size):
