@@ -69,8 +69,8 @@ struct ManyScratch {
   float *row_max, *row_sum;  // [n] statistics of the kept rows, in order
   float* col;                // [2 (n up to 128)] the kept rows as columns of dw: see MmaArgs
   float* score;              // [n * top] scores of the targets
-  float2* stat;              // partial statistics, see many_slots
-  float* out;                // partial gradients, see many_slots
+  float2* stat;              // partial statistics and
+  float* out;                // partial gradients by slot (Ranges, softmax_mma.cuh)
   uint32_t *key[2], *val[2]; // [n * top] entries by item
   int32_t* tile_first;       // [tiles of W + 1] first entry of a tile's items
   float* run_sum[2];         // [n * top / kRun (^2) + 1][D] sums over whole runs of one item
@@ -89,7 +89,7 @@ ManySizes many_sizes(int64_t rows, int64_t V, int32_t D, int32_t dtype, int64_t 
 cudaError_t launch_many_rows(const SoftmaxArgs& a, const ManyScratch& s);
 
 cudaError_t launch_targets(const TargetArgs& a, cudaStream_t st);
-// Whether a call of n rows goes by scores kept.
+// Whether a call of n rows goes by scores kept (launch_few_rows).
 bool few_rows(int64_t n, int64_t V, int32_t D, bool grads);
 int few_groups(int64_t max_rows, int64_t V, int32_t D, bool backward);  // most groups of such a call
 cudaError_t launch_few_rows(const SoftmaxArgs& a, const FewScratch& s);

@@ -1,6 +1,11 @@
 // Softmax operators for a few rows (single users, single tokens) and for small
 // problems, where launches and latency count: the scores of groups of kFewRows rows
 // are kept, W is read once for them and once for dh.  All in fp32.
+//
+// 1M items, K = 64, fp32, eight rows, GB300: scores 58 us (256 MB, 4.4 TB/s: loads in
+// flight), dw 100 (320 MB), dh 102 (288 MB, 2.8 TB/s), against 38 us for 256 MB.  A
+// single row's scores without gradients: a call of 54 us in fp32 and 34 in bf16, where
+// the kernel for eight rows takes 64 and 55.
 #include <algorithm>
 
 #include "softmax.cuh"
@@ -64,16 +69,20 @@ struct Few {
   FewScratch s;
   int32_t groups;  // of kFewRows rows
   int32_t blocks;  // per group, of the kernel whose partial results are read
+  int store;       // whether scores are kept: gradients and long lists want them
 };
 
 // Scores of all items: four lanes to an item (each a quarter of its slices of VEC
 // values), eight items to a warp side by side, U deep; rows of H from shared memory, where
 // the four lanes read one 64-byte line for all items.  The lanes' sums meet by
 // halving: each lane ends with two rows' totals, so no exponential is taken twice.
-template <typename T, int VEC, int U>
-__global__ void __launch_bounds__(kThreads, U == 1 ? 2 : 4) few_scores_kernel(Few f) {
-  constexpr int R = kFewRows, kDeep = U == 1 ? 8 : VEC == 8 ? 1 : 2;  // slices under way
-  extern __shared__ __align__(16) float hs[];  // [R][slices][VEC]
+// A single row (R = 1) has its four lanes' sums in all of them, and each lane keeps
+// every fourth item.
+template <typename T, int VEC, int U, int R, bool SINGLE>
+__global__ void __launch_bounds__(kThreads, U == 1 || SINGLE ? 2 : 4) few_scores_kernel(Few f) {
+  constexpr int kDeep = U == 1 ? 8 : VEC == 8 ? 1 : 2;  // slices under way
+  constexpr int kMine = R == 1 ? 1 : 2;                 // rows of a lane's statistics
+  extern __shared__ __align__(16) float hs[];           // [R][slices][VEC]
   __shared__ float2 warp_part[kThreads / 32][R];
   const SoftmaxArgs& a = f.a;
   const int lane = threadIdx.x & 31, ql = lane & 3;
@@ -81,14 +90,16 @@ __global__ void __launch_bounds__(kThreads, U == 1 ? 2 : 4) few_scores_kernel(Fe
   const T* h = static_cast<const T*>(a.h);
   for (int i = threadIdx.x; i < slices * R * VEC; i += kThreads) {
     const int r = i / (slices * VEC), d = i - r * slices * VEC;
-    const int64_t t = (int64_t)blockIdx.y * R + r;
+    const int64_t t = (int64_t)blockIdx.y * kFewRows + r;
     hs[i] = t < a.n && d < a.D && row_kept(a.target, t) ? to_float(h[t * a.h_stride + d]) : 0.f;
   }
   __syncthreads();
   const T* w = static_cast<const T*>(a.w);
   const float k2 = a.b * kLog2e;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-  const int row0 = (lane & 2) * 2 + (lane & 1) * 2;  // this lane's rows after halving: row0, row0 + 1
+  float m[kMine], l[kMine];
+#pragma unroll
+  for (int r = 0; r < kMine; ++r) m[r] = -INFINITY, l[r] = 0.f;
+  const int row0 = R == 1 ? 0 : (lane & 2) * 2 + (lane & 1) * 2;  // this lane's rows after halving: row0, row0 + 1
   const int64_t step = (int64_t)gridDim.x * (kThreads / 32) * 8 * U;
   for (int64_t v0 = ((int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32) * 8 * U; v0 < a.V; v0 += step) {
     float acc[U][R];
@@ -103,19 +114,22 @@ __global__ void __launch_bounds__(kThreads, U == 1 ? 2 : 4) few_scores_kernel(Fe
     for (int i = ql; i < slices; i += 4) {
       float x[U][VEC];
 #pragma unroll
-      for (int u = 0; u < U; ++u) load_vec<T, VEC>(row[u] + i * VEC, x[u]);
+      for (int u = 0; u < U; ++u) {
+        if constexpr (SINGLE) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x[u][e] = i * VEC + e < a.D ? to_float(row[u][i * VEC + e]) : 0.f;
+        } else {
+          load_vec<T, VEC>(row[u] + i * VEC, x[u]);
+        }
+      }
       const float* hv = hs + i * VEC;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         float y[VEC];
-        if constexpr (VEC >= 4) {
 #pragma unroll
-          for (int e = 0; e < VEC; e += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(hv + r * slices * VEC + e);
-            y[e] = q.x, y[e + 1] = q.y, y[e + 2] = q.z, y[e + 3] = q.w;
-          }
-        } else {
-          y[0] = hv[r * slices];
+        for (int e = 0; e < VEC; e += 4) {
+          const float4 q = *reinterpret_cast<const float4*>(hv + r * slices * VEC + e);
+          y[e] = q.x, y[e + 1] = q.y, y[e + 2] = q.z, y[e + 3] = q.w;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -125,43 +139,54 @@ __global__ void __launch_bounds__(kThreads, U == 1 ? 2 : 4) few_scores_kernel(Fe
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float half[4], s[2];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float give = (lane & 2) ? acc[u][r] : acc[u][r + 4], keep = (lane & 2) ? acc[u][r + 4] : acc[u][r];
-        half[r] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
-      }
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float give = (lane & 1) ? half[r] : half[r + 2], keep = (lane & 1) ? half[r + 2] : half[r];
-        s[r] = (keep + __shfl_xor_sync(0xffffffffu, give, 1)) * k2;
-      }
       const int64_t v = v0 + u * 8 + lane / 4;
-      if (v < a.V) {
-        *reinterpret_cast<float2*>(f.s.scores + ((int64_t)blockIdx.y * a.V + v) * R + row0) = make_float2(s[0], s[1]);
+      float* kept = f.s.scores + ((int64_t)blockIdx.y * a.V + v) * kFewRows;
+      if constexpr (R == 1) {
+        float s = acc[u][0] + __shfl_xor_sync(0xffffffffu, acc[u][0], 2);
+        s = (s + __shfl_xor_sync(0xffffffffu, s, 1)) * k2;
+        if (v < a.V && ql == u % 4) {
+          if (f.store) kept[0] = s;
+          merge_stat(m[0], l[0], s, 1.f);
+        }
+      } else {
+        float half[4], s[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) merge_stat(m[r], l[r], s[r], 1.f);
+        for (int r = 0; r < 4; ++r) {
+          const float give = (lane & 2) ? acc[u][r] : acc[u][r + 4], keep = (lane & 2) ? acc[u][r + 4] : acc[u][r];
+          half[r] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float give = (lane & 1) ? half[r] : half[r + 2], keep = (lane & 1) ? half[r + 2] : half[r];
+          s[r] = (keep + __shfl_xor_sync(0xffffffffu, give, 1)) * k2;
+        }
+        if (v < a.V) {
+          if (f.store) *reinterpret_cast<float2*>(kept + row0) = make_float2(s[0], s[1]);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) merge_stat(m[r], l[r], s[r], 1.f);
+        }
       }
     }
   }
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int r = 0; r < kMine; ++r) {
 #pragma unroll
-    for (int off = 4; off < 32; off <<= 1) {
+    for (int off = R == 1 ? 1 : 4; off < 32; off <<= 1) {
       const float m2 = __shfl_xor_sync(0xffffffffu, m[r], off), l2 = __shfl_xor_sync(0xffffffffu, l[r], off);
       merge_stat(m[r], l[r], m2, l2);
     }
-    if (lane < 4) warp_part[threadIdx.x / 32][row0 + r] = make_float2(m[r], l[r]);
+    if (lane < (R == 1 ? 1 : 4)) warp_part[threadIdx.x / 32][row0 + r] = make_float2(m[r], l[r]);
   }
   __syncthreads();
   if (threadIdx.x < R) {
     float2 t = warp_part[0][threadIdx.x];
     for (int i = 1; i < kThreads / 32; ++i) merge_stat(t.x, t.y, warp_part[i][threadIdx.x].x, warp_part[i][threadIdx.x].y);
-    f.s.part[(blockIdx.y * gridDim.x + blockIdx.x) * R + threadIdx.x] = t;
+    f.s.part[(blockIdx.y * gridDim.x + blockIdx.x) * kFewRows + threadIdx.x] = t;
   }
 }
 
 // One warp per row: its maximum and sum over the blocks, its loss.
+template <typename T>
 __global__ void few_stat_kernel(Few f) {
   const SoftmaxArgs& a = f.a;
   const int group = blockIdx.x / kFewRows, r = blockIdx.x % kFewRows, lane = threadIdx.x;
@@ -179,11 +204,21 @@ __global__ void few_stat_kernel(Few f) {
   }
   const float lse2 = m + log2f(l);
   float loss2 = 0.f;  // sum q (lse - s), in units of log 2
-  if (kept) {
-    const int32_t* ids = a.target.ids + t * a.target.top;
+  const int32_t* ids = a.target.ids + t * a.target.top;
+  if (kept && f.store) {
     for (int k = lane; k < a.target.top; k += 32) {
       const float q = a.target.logits ? a.target.q[t * a.target.top + k] : 1.f;
       if (q != 0.f) loss2 += q * (lse2 - f.s.scores[((int64_t)group * a.V + ids[k]) * kFewRows + r]);
+    }
+  } else if (kept) {
+    for (int k = 0; k < a.target.top; ++k) {
+      const float q = a.target.logits ? a.target.q[t * a.target.top + k] : 1.f;
+      if (q == 0.f) continue;
+      const T *h = static_cast<const T*>(a.h) + t * a.h_stride, *w = static_cast<const T*>(a.w) + ids[k] * a.w_stride;
+      float s = 0.f;
+      for (int d = lane; d < a.D; d += 32) s = fmaf(to_float(w[d]), to_float(h[d]), s);
+      s = warp_sum(s);
+      if (lane == 0) loss2 += q * (lse2 - s * (a.b * kLog2e));
     }
   }
   loss2 = warp_sum(loss2);
@@ -196,12 +231,39 @@ __global__ void few_stat_kernel(Few f) {
   }
 }
 
+// Four columns of a row per thread: side by side, or (SPREAD, rows that no vector of
+// four can be read from) one of each of four groups of tx, so that a warp's loads join.
+constexpr int kCols = 4;
+template <bool SPREAD>
+__device__ __forceinline__ int first_col(int chunk, int x, int tx) {
+  return SPREAD ? chunk * kCols * tx + x : (chunk * tx + x) * kCols;
+}
+template <typename T, bool SPREAD>
+__device__ __forceinline__ void load_cols(const T* row, int col, int tx, int D, float (&x)[kCols]) {
+  if constexpr (SPREAD) {
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) x[e] = col + e * tx < D ? to_float(row[col + e * tx]) : 0.f;
+  } else {
+    load_vec<T, kCols>(row + col, x);
+  }
+}
+template <typename T, bool SPREAD>
+__device__ __forceinline__ void store_cols(T* row, int col, int tx, int D, const float (&x)[kCols]) {
+  if constexpr (SPREAD) {
+#pragma unroll
+    for (int e = 0; e < kCols; ++e)
+      if (col + e * tx < D) row[col + e * tx] = from_float<T>(x[e]);
+  } else {
+    store_vec<T, kCols>(row + col, x);
+  }
+}
+
 // dw_v = sum_r g_vr h_r, with g_vr = b weight_r (p_vr - q_vr) taken from the scores of
 // a tile of items for all rows at once, and left in their place for dh.  Threads take
-// slices of VEC columns (tx of them at a time) of every ty-th item, four items deep.
-template <typename T, int VEC, int kTile>
-__global__ void __launch_bounds__(kThreads, 3) few_grad_w_kernel(Few f, int tx) {
-  constexpr int R = kFewRows, U = 4;
+// four columns (tx threads to a row) of every ty-th item, four items deep.
+template <typename T, bool SPREAD, int kTile>
+__global__ void __launch_bounds__(kThreads, SPREAD ? 2 : 3) few_grad_w_kernel(Few f, int tx) {
+  constexpr int R = kFewRows, U = 4, VEC = kCols;
   extern __shared__ __align__(32) float g[];  // [groups][kTile][R]
   __shared__ float bw[kSmallRows], mx[kSmallRows], inv[kSmallRows];
   __shared__ bool used[kSmallRows];
@@ -244,14 +306,17 @@ __global__ void __launch_bounds__(kThreads, 3) few_grad_w_kernel(Few f, int tx) 
       const int group = i / (items * R), in = i - group * items * R;
       f.s.scores[((int64_t)group * a.V + v0) * R + in] = g[group * kTile * R + in];
     }
-    for (int col = x * VEC; col < a.D; col += tx * VEC) {
+    for (int chunk = 0; chunk * tx * VEC < a.D; ++chunk) {
+      const int col = first_col<SPREAD>(chunk, x, tx);
+      if (col >= a.D) break;
       float h[R][VEC];
       auto load_rows = [&](int group) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
           for (int e = 0; e < VEC; ++e) h[r][e] = 0.f;
-          if (used[group * R + r]) load_vec<T, VEC>(static_cast<const T*>(a.h) + (group * R + r) * a.h_stride + col, h[r]);
+          if (used[group * R + r])
+            load_cols<T, SPREAD>(static_cast<const T*>(a.h) + (group * R + r) * a.h_stride, col, tx, a.D, h[r]);
         }
       };
       if (f.groups == 1) load_rows(0);
@@ -276,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 3) few_grad_w_kernel(Few f, int tx) 
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (i0 + u * ty_n < items)
-            store_vec<T, VEC>(static_cast<T*>(a.grad_w) + (v0 + i0 + u * ty_n) * a.D + col, dw[u]);
+            store_cols<T, SPREAD>(static_cast<T*>(a.grad_w) + (v0 + i0 + u * ty_n) * a.D, col, tx, a.D, dw[u]);
       }
     }
     __syncthreads();
@@ -286,17 +351,17 @@ __global__ void __launch_bounds__(kThreads, 3) few_grad_w_kernel(Few f, int tx) 
 // dh_r = sum_v g_vr w_v of a group of rows (blockIdx.z) by blocks, each over a part of
 // the items: threads as above, coefficients by tiles through shared memory, the rows'
 // sums in registers.
-template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads, 3) few_grad_h_kernel(Few f, int tx) {
-  constexpr int R = kFewRows, U = 8, kTile = 256;
+template <typename T, bool SPREAD>
+__global__ void __launch_bounds__(kThreads, SPREAD ? 2 : 3) few_grad_h_kernel(Few f, int tx) {
+  constexpr int R = kFewRows, VEC = kCols, U = SPREAD ? 4 : 8, kTile = 256;
   __shared__ __align__(32) float c[kTile * R];
   __shared__ __align__(16) float red[kThreads * VEC];
   const SoftmaxArgs& a = f.a;
   const int ty_n = kThreads / tx, x = threadIdx.x % tx, y = threadIdx.x / tx;
-  const int col = (blockIdx.y * tx + x) * VEC;
+  const int col = first_col<SPREAD>(blockIdx.y, x, tx);
   const bool on = col < a.D;
   const float* g = f.s.scores + (int64_t)blockIdx.z * a.V * R;
-  const T* w = static_cast<const T*>(a.w) + col;
+  const T* w = static_cast<const T*>(a.w);
   float o[R][VEC];
 #pragma unroll
   for (int r = 0; r < R; ++r)
@@ -312,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 3) few_grad_h_kernel(Few f, int tx) 
       for (int i = y; i < items; i += U * ty_n) {
         float k[U][VEC];
 #pragma unroll
-        for (int u = 0; u < U; ++u) load_vec<T, VEC>(w + (v0 + min(i + u * ty_n, items - 1)) * a.w_stride, k[u]);
+        for (int u = 0; u < U; ++u) load_cols<T, SPREAD>(w + (v0 + min(i + u * ty_n, items - 1)) * a.w_stride, col, tx, a.D, k[u]);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           if (i + u * ty_n >= items) break;
@@ -338,9 +403,11 @@ __global__ void __launch_bounds__(kThreads, 3) few_grad_h_kernel(Few f, int tx) 
     __syncthreads();
     if (y == 0 && on)
       for (int e = 0; e < VEC; ++e) {
+        const int d = col + e * (SPREAD ? tx : 1);
+        if (d >= a.D) break;
         float sum = 0.f;
         for (int k = 0; k < ty_n; ++k) sum += red[(k * tx + x) * VEC + e];
-        f.s.dh[((int64_t)(blockIdx.z * gridDim.x + blockIdx.x) * R + r) * a.D + col + e] = sum;
+        f.s.dh[((int64_t)(blockIdx.z * gridDim.x + blockIdx.x) * R + r) * a.D + d] = sum;
       }
     __syncthreads();
   }
@@ -372,34 +439,39 @@ int vector_of(const void* p, int64_t stride, int32_t D, int most) {
   return 1;
 }
 
-// Warps take 8 items at a time where that gives the GPU few warps, else 16.
-template <typename T, int VEC>
+// Warps take 8 items at a time where that gives the GPU few warps, else 16 (of a single
+// row 32).
+template <typename T, int VEC, bool SINGLE>
 void scores(Few& f) {
   const int32_t slices = (f.a.D + VEC - 1) / VEC;
-  const size_t smem = sizeof(float) * slices * kFewRows * VEC;
+  const bool one = f.a.n == 1;
+  const size_t smem = sizeof(float) * slices * (one ? 1 : kFewRows) * VEC;
   const int64_t most = std::max(1, few_blocks(f.a.sms) / f.groups);
-  const bool small = (int64_t)f.a.V < most * 128;
-  f.blocks = (int)std::min<int64_t>(most, ((int64_t)f.a.V + (small ? 64 : 128) - 1) / (small ? 64 : 128));
-  if (small) few_scores_kernel<T, VEC, 1><<<dim3(f.blocks, f.groups), kThreads, smem, f.a.st>>>(f);
-  else few_scores_kernel<T, VEC, 2><<<dim3(f.blocks, f.groups), kThreads, smem, f.a.st>>>(f);
+  const int many = one ? 256 : 128, take = (int64_t)f.a.V < most * many ? 64 : many;  // items of a block at a time
+  f.blocks = (int)std::min<int64_t>(most, ((int64_t)f.a.V + take - 1) / take);
+  const dim3 grid(f.blocks, f.groups);
+  if (one && take == 64) few_scores_kernel<T, VEC, 1, 1, SINGLE><<<grid, kThreads, smem, f.a.st>>>(f);
+  else if (one) few_scores_kernel<T, VEC, 4, 1, SINGLE><<<grid, kThreads, smem, f.a.st>>>(f);
+  else if (take == 64) few_scores_kernel<T, VEC, 1, kFewRows, SINGLE><<<grid, kThreads, smem, f.a.st>>>(f);
+  else few_scores_kernel<T, VEC, 2, kFewRows, SINGLE><<<grid, kThreads, smem, f.a.st>>>(f);
 }
-template <typename T, int VEC>
+template <typename T, bool SPREAD>
 void grads(Few f) {
-  const int32_t slices = (f.a.D + VEC - 1) / VEC;
+  const int32_t slices = (f.a.D + kCols - 1) / kCols;
   int tx = 1;
   while (tx < slices && tx < 64) tx *= 2;
   // Tiles of 8 items where there are few, of 256 where a few rows meet many, else of 64.
   const int kTile = (int64_t)f.a.V < 64 * f.a.sms ? 8 : f.groups == 1 && (int64_t)f.a.V >= 1024 * f.a.sms ? 256 : 64;
   const int64_t tiles = ((int64_t)f.a.V + kTile - 1) / kTile;
   const size_t smem = sizeof(float) * f.groups * kTile * kFewRows;
-  const unsigned grid = (unsigned)std::min<int64_t>(tiles, 3 * f.a.sms);  // (what is resident at once)
-  if (kTile == 8) few_grad_w_kernel<T, VEC, 8><<<grid, kThreads, smem, f.a.st>>>(f, tx);
-  else if (kTile == 256) few_grad_w_kernel<T, VEC, 256><<<grid, kThreads, smem, f.a.st>>>(f, tx);
-  else few_grad_w_kernel<T, VEC, 64><<<grid, kThreads, smem, f.a.st>>>(f, tx);
+  const unsigned grid = (unsigned)std::min<int64_t>(tiles, (SPREAD ? 2 : 3) * f.a.sms);  // (what is resident at once)
+  if (kTile == 8) few_grad_w_kernel<T, SPREAD, 8><<<grid, kThreads, smem, f.a.st>>>(f, tx);
+  else if (kTile == 256) few_grad_w_kernel<T, SPREAD, 256><<<grid, kThreads, smem, f.a.st>>>(f, tx);
+  else few_grad_w_kernel<T, SPREAD, 64><<<grid, kThreads, smem, f.a.st>>>(f, tx);
   // Blocks of a group: as many as fill the GPU, each with 4 items per thread at least.
   const int64_t most = ((int64_t)f.a.V * tx + 4 * kThreads - 1) / (4 * kThreads);
-  f.blocks = (int)std::min<int64_t>(std::max(1, 3 * f.a.sms / f.groups), most);
-  few_grad_h_kernel<T, VEC><<<dim3(f.blocks, (slices + tx - 1) / tx, f.groups), kThreads, 0, f.a.st>>>(f, tx);
+  f.blocks = (int)std::min<int64_t>(std::max(1, (SPREAD ? 2 : 3) * f.a.sms / f.groups), most);
+  few_grad_h_kernel<T, SPREAD><<<dim3(f.blocks, (slices + tx - 1) / tx, f.groups), kThreads, 0, f.a.st>>>(f, tx);
   few_finish_kernel<T><<<dim3((f.a.D + 31) / 32, (unsigned)f.a.n), dim3(32, 8), 0, f.a.st>>>(f);
 }
 
@@ -408,12 +480,12 @@ cudaError_t run(const SoftmaxArgs& a, const FewScratch& s) {
   constexpr int kWide = 16 / sizeof(T);
   const int vw = vector_of<T>(a.w, a.w_stride, a.D, kWide);
   const int vg = std::min(std::min(vw, 4), std::min(vector_of<T>(a.h, a.h_stride, a.D, 4), vector_of<T>(a.grad_w, a.D, a.D, 4)));
-  Few f{a, s, (int32_t)((a.n + kFewRows - 1) / kFewRows), 0};
-  if (vw == kWide) scores<T, kWide>(f);
-  else if (vw >= 4) scores<T, 4>(f);
-  else scores<T, 1>(f);
-  few_stat_kernel<<<(unsigned)a.n, 32, 0, a.st>>>(f);
-  if (a.grad_h) vg == 4 ? grads<T, 4>(f) : grads<T, 1>(f);
+  Few f{a, s, (int32_t)((a.n + kFewRows - 1) / kFewRows), 0, a.grad_h || a.target.top > 4};
+  if (vw == kWide) scores<T, kWide, false>(f);
+  else if (vw >= 4) scores<T, 4, false>(f);
+  else scores<T, kWide, true>(f);
+  few_stat_kernel<T><<<(unsigned)a.n, 32, 0, a.st>>>(f);
+  if (a.grad_h) vg == 4 ? grads<T, false>(f) : grads<T, true>(f);
   return cudaGetLastError();
 }
 

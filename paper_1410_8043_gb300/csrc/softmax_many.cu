@@ -1,12 +1,17 @@
 // Softmax operators for many rows: operands laid out for the tensor cores, the
 // passes over tiles of scores, and what joins their partial results.
 //
-//   words      the kept rows in order, largest magnitudes
-//   units      H (kept rows) and W in 16 KB units, fp32 in two halves
-//   stats      maximum and sum of every row; losses
-//   rows       sum p w, then dh
-//   entries    targets sorted by item, sums over long runs of one item
+//   compact    the kept rows in order (ignored ones cost nothing from here on)
+//   max, units H (kept rows) and W in 16 KB units, fp32 in two halves
+//   stats      maximum and sum of every row, then its loss; or, with gradients of large
+//              problems, references for the rows from their targets and a part of W
+//   rows       sum p w (and sum p), then dh and the loss
+//   entries    targets sorted by item on a second stream, sums over long runs of one item
 //   cols       sum weight p h, then dw
+//
+// The kernels here are bound by bytes or by latency: 2048 x 1M, K = 64, fp32, GB300:
+// max 43 us (256 MB, 6.0 TB/s), units 72 (512 MB, 7.1 TB/s), dw 154 (512 MB, 3.3 TB/s,
+// with its scattered targets) of the call's 2550.
 #include <cub/device/device_radix_sort.cuh>
 
 #include <algorithm>
@@ -42,8 +47,8 @@ __device__ __forceinline__ void block_max(uint32_t x, uint32_t* to) {
   if ((threadIdx.x & 31) == 0 && x != 0u) atomicMax(to, x);
 }
 
-// Places of the kept rows.  A block counts the kept rows before its own 1024 first:
-// 16k rows take 8 such counts of 1k rows per block on average, a million 500.
+// Places of the kept rows.  A block counts the kept rows before its own 1024 first, so
+// one launch does: 4 us at 8k rows, of which a block reads 4k on average.
 __global__ void __launch_bounds__(1024) compact_kernel(Many f) {
   __shared__ int32_t sums[32];
   const SoftmaxArgs& a = f.a;
@@ -498,15 +503,17 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
 }
 
 // dw: b (sum weight p h - sum weight q h), kItems items to a block.  Most items are
-// nobody's target: those rows go through all threads side by side, the others a warp each.
-constexpr int kItems = 64;
+// nobody's target: those rows go through all threads side by side, the others a warp
+// each (2048 x 1M, K = 64: a warp for every item took 470 us, this 154).
+constexpr int kItems = 64;  // at most; 16 where 64 would leave SMs idle
 template <typename T, int VEC>
-__global__ void __launch_bounds__(256) grad_w_kernel(Many f, const uint32_t* key, const int32_t* row, const float* factor) {
+__global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, const uint32_t* key, const int32_t* row,
+                                                     const float* factor) {
   __shared__ int32_t first[kItems + 1];
   __shared__ int64_t slots[2];
   const SoftmaxArgs& a = f.a;
-  const int64_t v0 = (int64_t)blockIdx.x * kItems, rows = f.s.words->rows;
-  const int lane = threadIdx.x & 31, items = (int)min((int64_t)kItems, a.V - v0);
+  const int64_t v0 = (int64_t)blockIdx.x * per_block, rows = f.s.words->rows;
+  const int lane = threadIdx.x & 31, items = (int)min((int64_t)per_block, a.V - v0);
   if (threadIdx.x <= items) {
     int32_t lo = f.s.tile_first[v0 / 128], hi = f.s.tile_first[v0 / 128 + 1];
     while (lo < hi) {
@@ -697,7 +704,9 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   if (sizeof(T) == 2) launch_runs(a.st);  // (wants the rows' sums)
   m.A = s.units_w, m.B = s.units_h;
   if ((e = launch_mma(Pass::kCols, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
-  grad_w_kernel<T, VEC><<<(unsigned)(((int64_t)a.V + kItems - 1) / kItems), 256, 0, a.st>>>(f, key.Current(), entry_row, entry_factor);
+  const int per_block = (int64_t)a.V < (int64_t)kItems * 8 * a.sms ? 16 : kItems;
+  grad_w_kernel<T, VEC><<<(unsigned)(((int64_t)a.V + per_block - 1) / per_block), 256, 0, a.st>>>(f, per_block, key.Current(),
+                                                                                           entry_row, entry_factor);
   return cudaGetLastError();
 }
 

@@ -1,16 +1,22 @@
 // The passes of the softmax operators over tiles of scores, on tensor cores.
 //
-// One block per SM holds one or two tiles (128 rows) of A and streams tiles of B.
-// One warp loads, one thread issues the matrix instructions, and two groups of eight
-// warps take the tiles of scores out of tensor memory by turns, half a row per thread.  For the
-// gradients the probabilities go back in place of their scores, in 16 bits, and are
-// the first operand of the second product, whose other operand is the tile of B that
-// gave the scores, read along its other dimension.  So the n x V scores and
-// probabilities exist only as tiles in tensor memory.
+// One block per SM holds one or two tiles (128 rows) of A and streams tiles of B.  One
+// warp loads, one issues the matrix instructions, and two groups of eight warps take
+// the tiles of scores out of tensor memory by turns, half a row of a tile per thread.
+// For the gradients the probabilities go back in place of their scores, in 16 bits, and
+// are the first operand of the second product, whose other operand is the tile of B
+// that gave the scores, read along its other dimension.  So the n x V scores and
+// probabilities exist only as tiles in tensor memory, and B is loaded once for both.
 //
-// fp32 (PARTS = 2): S = lo hi + hi lo + hi hi of the operands' halves, and the same
-// for p B.  Sums run over at most `run` tiles in the tensor core, whose additions
-// round worse than fp32's own, and are then added in fp32.
+// fp32 (PARTS = 2): S = lo hi + hi lo + hi hi of the operands' halves, and the same for
+// p B.  The tensor core's additions round towards zero, so a long sum loses in
+// proportion to its length; sums run over at most `run` tiles and are then added in fp32.
+//
+// Rows and cols pass, 2048 x 120k, GB300 (tensor pipe active / instruction issue /
+// exponentials, of their peaks): bf16, K = 64: 64 and 75 us (45/60/45%, 37/50/38%):
+// issue, tensor cores and exponentials share the limit; K = 256: 190 and 199 us
+// (59/23/15%, 55/22/14%) and fp32, K = 100: 247 and 222 us (60/24/11%, 68/28/13%): the
+// products, and their waits for loads (a tile of B is 64 KB at both).
 #include <type_traits>
 
 #include "ptx.cuh"

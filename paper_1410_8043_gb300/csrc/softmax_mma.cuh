@@ -7,7 +7,7 @@
 
 namespace esspt {
 
-// What a pass makes of the scores S = A B^T (b / ln 2 times, see MmaArgs::scale):
+// What a pass makes of the scores S = A B^T b / ln 2:
 //   kStats  per row of A the maximum and the sum of 2^(S - maximum)
 //   kRows   A = H, B = W: sum over B's rows of 2^(S - row_max) B, and of 2^(S - row_max)
 //   kCols   A = W, B = H: sum over B's rows t of 2^(S - maximum_t) factor_t B
@@ -24,9 +24,11 @@ constexpr int kMmaThreads = 640;       // a warp that loads, one that multiplies
 //
 // Up to two units a row (t), a stage is a tile of B.  Above, stages are units: a tile
 // of B is then never waited for as a whole (K = 256, bf16: with two stages of 64 KB a
-// tile waited 940 of 3150 cycles), or pairs of units where two tiles of four fit.  Two tiles of A share B where only the scores are
-// wanted and three units are left for it; with sums, a third buffer of scores is worth
-// more than sharing.
+// tile waited 940 of 3150 cycles); or pairs of units, half as many waits, where two
+// tiles of four fit (4096 x 18k, K = 100, fp32: 251 and 238 us for the call).  Two tiles
+// of A share B where only the scores are wanted and three units are left for it; with
+// sums, a third buffer of scores is worth more than sharing (4001 x 200k, K = 64, bf16:
+// 295 and 222 us for the rows pass).
 struct MmaShape {
   int nk, steps;       // units and 16-value steps of a row
   int tiles, res, keep;
@@ -63,14 +65,14 @@ struct MmaArgs {
   float* sums;           // kRows out: sums of the probabilities, likewise, or null
   float up;              // kRows: probabilities are taken 2^up times as large
   int if_redo;           // only where words->redo is set
-  float* out;            // else: [slot][128][ld]
+  float* out;            // kRows, kCols: [slot][128][ld]
   int ld;
   int run;               // tiles of B that the tensor core sums up before fp32 does
   uint32_t* status;
 };
 
-// Work is the sequence of all (group of A's tiles, tile of B), cut into one even
-// range per block; block i's part of group g goes to slot i + g, and the slots of a
+// Work is the sequence of all (group of A's tiles, tile of B), cut into one even range
+// per block, so that no SM waits whatever the two sizes are; block i's part of group g goes to slot i + g, and the slots of a
 // group are consecutive.
 struct Ranges {
   int64_t groups, n_b, units, blocks;
