@@ -3,11 +3,12 @@
 // are kept, W is read once for them and once for dh.  All in fp32.
 //
 // 1M items, K = 64, fp32, eight rows, GB300: scores 58 us (256 MB, 4.4 TB/s: loads in
-// flight), dw 100 (320 MB), dh 102 (288 MB, 2.8 TB/s), against 38 us for 256 MB.  A
+// flight), dw 100 (320 MB), dh 86 (288 MB, 3.3 TB/s), against 38 us for 256 MB.  A
 // single row's scores without gradients: a call of 54 us in fp32 and 34 in bf16, where
 // the kernel for eight rows takes 64 and 55.
 #include <algorithm>
 
+#include "ptx.cuh"
 #include "softmax.cuh"
 
 namespace esspt {
@@ -354,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, SPREAD ? 2 : 3) few_grad_w_kernel(Fe
 template <typename T, bool SPREAD>
 __global__ void __launch_bounds__(kThreads, SPREAD ? 2 : 3) few_grad_h_kernel(Few f, int tx) {
   constexpr int R = kFewRows, VEC = kCols, U = SPREAD ? 4 : 8, kTile = 256;
-  __shared__ __align__(32) float c[kTile * R];
+  __shared__ __align__(32) float tiles[2][kTile * R];
   __shared__ __align__(16) float red[kThreads * VEC];
   const SoftmaxArgs& a = f.a;
   const int ty_n = kThreads / tx, x = threadIdx.x % tx, y = threadIdx.x / tx;
@@ -368,11 +369,19 @@ __global__ void __launch_bounds__(kThreads, SPREAD ? 2 : 3) few_grad_h_kernel(Fe
 #pragma unroll
     for (int e = 0; e < VEC; ++e) o[r][e] = 0.f;
   const int64_t end = a.V * (int64_t)(blockIdx.x + 1) / gridDim.x;
-  for (int64_t v0 = a.V * (int64_t)blockIdx.x / gridDim.x; v0 < end; v0 += kTile) {
+  auto fetch = [&](float* to, int64_t v) {  // coefficients of a tile, while the one before is at work
+    const int quads = (int)min((int64_t)kTile, end - v) * (R / 4);
+    for (int i = threadIdx.x; i < quads; i += kThreads) cp_async16_if(to + 4 * i, g + v * R + 4 * i, true);
+    cp_async_commit();
+  };
+  int64_t v0 = a.V * (int64_t)blockIdx.x / gridDim.x;
+  fetch(tiles[0], v0);
+  for (int turn = 0; v0 < end; v0 += kTile, turn ^= 1) {
     const int items = (int)min((int64_t)kTile, end - v0);
+    const float* c = tiles[turn];
+    cp_async_wait_all();
     __syncthreads();
-    for (int i = threadIdx.x; i < items * R; i += kThreads) c[i] = g[v0 * R + i];
-    __syncthreads();
+    if (v0 + kTile < end) fetch(tiles[turn ^ 1], v0 + kTile);
     if (on)
       for (int i = y; i < items; i += U * ty_n) {
         float k[U][VEC];
