@@ -313,9 +313,9 @@ esspt_status esspt_mf_worker_objective_noalloc(esspt_ctx* ctx, int32_t version, 
  * the gradients of sum_t weight_t loss_t:
  *     dh_t = b weight_t (sum_v p_tv w_v - sum_k q_tk w_id(t,k))
  *     dw_v = b sum_t weight_t (p_tv - q_tv) h_t
- * The n x V scores are never kept: they are formed piece by piece, as often as
- * they are needed (for up to ESSPT_SOFTMAX_FEW_ROWS rows one row of V scores each
- * stays in the workspace, less than W itself).
+ * The n x V scores are not kept: they are formed piece by piece, as often as they
+ * are needed.  (Calls of up to ESSPT_SOFTMAX_FEW_ROWS rows, and of up to 128 where
+ * that is faster, keep theirs in the workspace, whose size counts them.)
  *
  * Values are fp32, bf16 or fp16, H, W and both gradients alike.  Products are
  * exact to fp32 rounding for fp32 rows; sums, statistics, losses and weights are
@@ -342,7 +342,8 @@ size_t esspt_softmax_workspace_bytes(const esspt_softmax_config* cfg);
 
 /* Create a handle over caller-allocated device workspace (256-byte aligned,
  * `bytes` >= esspt_softmax_workspace_bytes(cfg), kept until
- * esspt_softmax_destroy()).  Nothing in it outlives a call but the status word.
+ * esspt_softmax_destroy(), and not written by others: counters in it are zero
+ * between calls).  Only the status word carries anything from one call to the next.
  * ESSPT_EINVAL on a bad config, ESSPT_ENOSPC on a short workspace. */
 esspt_status esspt_softmax_create(const esspt_softmax_config* cfg, void* d_workspace, size_t bytes,
                                   esspt_softmax** out);
@@ -389,7 +390,8 @@ esspt_status esspt_softmax_distill(esspt_softmax* sm, const void* d_h, int64_t h
                                    float* d_lse, void* d_grad_h, void* d_grad_w);
 
 /* Synchronise the stream and report, then clear, any error latched on the device
- * (ESSPT_EINVAL: a target or id >= V). */
+ * (ESSPT_EINVAL: a target or id >= V; ESSPT_ECUDA: a wait inside a kernel ran out,
+ * which is not expected, and the results since the last poll are void). */
 esspt_status esspt_softmax_poll(esspt_softmax* sm);
 
 /* Text of the last error on this handle ("" if none), valid until the next call

@@ -50,6 +50,7 @@ struct FewScratch {
   float2* part;    // [few_blocks or groups][kFewRows] maximum and sum of a block's items
   float* stat;     // [rows][2] maximum of a row and 1 / sum
   float* dh;       // [few_blocks or groups][kFewRows][D]
+  uint32_t* done;  // [groups] blocks of a group that have ended; 0 between calls
 };
 int few_blocks(int sms);
 

@@ -67,6 +67,8 @@ const char* config_fault(const esspt_softmax_config* c) {
 
 
 constexpr int kMaxSms = 256;  // what the workspace is sized for
+constexpr int kStatusBytes = 256, kDoneAt = 64;  // the status word, and FewScratch::done behind it
+static_assert(kDoneAt + kSmallRows / kFewRows * sizeof(uint32_t) <= kStatusBytes, "counters outgrow their place");
 
 Carve carve(const esspt_softmax_config& c) {
   Carve k{};
@@ -77,7 +79,7 @@ Carve carve(const esspt_softmax_config& c) {
     return at;
   };
   const size_t n = (size_t)c.max_rows, V = (size_t)c.n_items, D = (size_t)c.width;
-  k.status = take(256);
+  k.status = take(kStatusBytes);
   k.q = take(n * c.max_top * sizeof(float));
   k.self = take(n * sizeof(float));
   const size_t groups = (size_t)few_groups(c.max_rows, c.n_items, c.width, c.backward != 0);
@@ -142,7 +144,8 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   auto at = [&](size_t offset) { return static_cast<void*>(sm->base + offset); };
   if (few_rows(n, c.n_items, c.width, grad_w != nullptr)) {
     const FewScratch s{static_cast<float*>(at(k.scores)), static_cast<float2*>(at(k.part)),
-                       static_cast<float*>(at(k.stat)), static_cast<float*>(at(k.dh))};
+                       static_cast<float*>(at(k.stat)), static_cast<float*>(at(k.dh)),
+                       static_cast<uint32_t*>(at(k.status + kDoneAt))};
     SOFTMAX_CUDA(sm, launch_few_rows(a, s));
     return ESSPT_OK;
   }
@@ -181,7 +184,7 @@ esspt_status esspt_softmax_create(const esspt_softmax_config* cfg, void* d_works
   int dev = 0, sms = 0;
   SOFTMAX_CUDA(nullptr, cudaGetDevice(&dev));
   SOFTMAX_CUDA(nullptr, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  SOFTMAX_CUDA(nullptr, cudaMemsetAsync(d_workspace, 0, 256, static_cast<cudaStream_t>(cfg->stream)));
+  SOFTMAX_CUDA(nullptr, cudaMemsetAsync(d_workspace, 0, kStatusBytes, static_cast<cudaStream_t>(cfg->stream)));
   esspt_softmax* sm = new (std::nothrow) esspt_softmax;
   if (!sm) return fail(nullptr, ESSPT_ENOSPC, "out of host memory");
   sm->cfg = *cfg;
@@ -204,7 +207,8 @@ esspt_status esspt_softmax_create(const esspt_softmax_config* cfg, void* d_works
 
 esspt_status esspt_softmax_destroy(esspt_softmax* sm) {
   if (!sm) return ESSPT_OK;
-  const cudaError_t e = cudaStreamSynchronize(sm->st);  // (the side stream's work ended before it)
+  cudaError_t e = cudaStreamSynchronize(sm->st);
+  if (e == cudaSuccess && sm->side) e = cudaStreamSynchronize(sm->side);  // (after a call that failed half-way)
   release(sm);
   return e == cudaSuccess ? ESSPT_OK : cuda_fail(nullptr, e, "esspt_softmax_destroy");
 }

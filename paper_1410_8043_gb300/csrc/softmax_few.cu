@@ -73,6 +73,54 @@ struct Few {
   int store;       // whether scores are kept: gradients and long lists want them
 };
 
+// One warp per row: its maximum and sum over the blocks, its loss.  Other blocks wrote
+// what it reads (past L1).
+template <typename T>
+__device__ void few_loss(const Few& f, int group, int r) {
+  const SoftmaxArgs& a = f.a;
+  const int lane = threadIdx.x & 31;
+  const int64_t t = (int64_t)group * kFewRows + r;
+  if (t >= a.n) return;
+  const bool kept = row_kept(a.target, t);
+  float m = -INFINITY, l = 0.f;
+  for (int i = lane; i < gridDim.x; i += 32) {
+    const float2 p = __ldcg(f.s.part + (group * gridDim.x + i) * kFewRows + r);
+    merge_stat(m, l, p.x, p.y);
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, off), l2 = __shfl_xor_sync(0xffffffffu, l, off);
+    merge_stat(m, l, m2, l2);
+  }
+  const float lse2 = m + log2f(l);
+  float loss2 = 0.f;  // sum q (lse - s), in units of log 2
+  const int32_t* ids = a.target.ids + t * a.target.top;
+  if (kept && f.store) {
+    for (int k = lane; k < a.target.top; k += 32) {
+      const float q = a.target.logits ? a.target.q[t * a.target.top + k] : 1.f;
+      if (q != 0.f) loss2 += q * (lse2 - __ldcg(f.s.scores + ((int64_t)group * a.V + ids[k]) * kFewRows + r));
+    }
+  } else if (kept) {
+    for (int k = 0; k < a.target.top; ++k) {
+      const float q = a.target.logits ? a.target.q[t * a.target.top + k] : 1.f;
+      if (q == 0.f) continue;
+      const T *h = static_cast<const T*>(a.h) + t * a.h_stride, *w = static_cast<const T*>(a.w) + ids[k] * a.w_stride;
+      float s = 0.f;
+      for (int d = lane; d < a.D; d += 32) s = fmaf(to_float(w[d]), to_float(h[d]), s);
+      s = warp_sum(s);
+      if (lane == 0) loss2 += q * (lse2 - s * (a.b * kLog2e));
+    }
+  }
+  loss2 = warp_sum(loss2);
+  if (lane == 0) {
+    if (!a.target.logits && a.target.ids[t] >= a.V) atomicOr(a.target.status, kErrTarget);
+    a.loss[t] = kept ? loss2 * kLn2 + (a.target.logits ? a.target.self[t] : 0.f) : 0.f;
+    a.lse[t] = kept ? lse2 * kLn2 : 0.f;
+    f.s.stat[2 * t] = m;
+    f.s.stat[2 * t + 1] = 1.f / l;
+  }
+}
+
 // Scores of all items: four lanes to an item (each a quarter of its slices of VEC
 // values), eight items to a warp side by side, U deep; rows of H from shared memory, where
 // the four lanes read one 64-byte line for all items.  The lanes' sums meet by
@@ -184,52 +232,18 @@ __global__ void __launch_bounds__(kThreads, U == 1 || SINGLE ? 2 : 4) few_scores
     for (int i = 1; i < kThreads / 32; ++i) merge_stat(t.x, t.y, warp_part[i][threadIdx.x].x, warp_part[i][threadIdx.x].y);
     f.s.part[(blockIdx.y * gridDim.x + blockIdx.x) * kFewRows + threadIdx.x] = t;
   }
-}
-
-// One warp per row: its maximum and sum over the blocks, its loss.
-template <typename T>
-__global__ void few_stat_kernel(Few f) {
-  const SoftmaxArgs& a = f.a;
-  const int group = blockIdx.x / kFewRows, r = blockIdx.x % kFewRows, lane = threadIdx.x;
-  const int64_t t = blockIdx.x;
-  const bool kept = row_kept(a.target, t);
-  float m = -INFINITY, l = 0.f;
-  for (int i = lane; i < f.blocks; i += 32) {
-    const float2 p = f.s.part[(group * f.blocks + i) * kFewRows + r];
-    merge_stat(m, l, p.x, p.y);
+  // The block of a group that ends last goes on with its rows' losses: a launch less.
+  __shared__ bool last;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last = atomicAdd(f.s.done + blockIdx.y, 1u) == gridDim.x - 1;
+    __threadfence();
   }
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, m, off), l2 = __shfl_xor_sync(0xffffffffu, l, off);
-    merge_stat(m, l, m2, l2);
-  }
-  const float lse2 = m + log2f(l);
-  float loss2 = 0.f;  // sum q (lse - s), in units of log 2
-  const int32_t* ids = a.target.ids + t * a.target.top;
-  if (kept && f.store) {
-    for (int k = lane; k < a.target.top; k += 32) {
-      const float q = a.target.logits ? a.target.q[t * a.target.top + k] : 1.f;
-      if (q != 0.f) loss2 += q * (lse2 - f.s.scores[((int64_t)group * a.V + ids[k]) * kFewRows + r]);
-    }
-  } else if (kept) {
-    for (int k = 0; k < a.target.top; ++k) {
-      const float q = a.target.logits ? a.target.q[t * a.target.top + k] : 1.f;
-      if (q == 0.f) continue;
-      const T *h = static_cast<const T*>(a.h) + t * a.h_stride, *w = static_cast<const T*>(a.w) + ids[k] * a.w_stride;
-      float s = 0.f;
-      for (int d = lane; d < a.D; d += 32) s = fmaf(to_float(w[d]), to_float(h[d]), s);
-      s = warp_sum(s);
-      if (lane == 0) loss2 += q * (lse2 - s * (a.b * kLog2e));
-    }
-  }
-  loss2 = warp_sum(loss2);
-  if (lane == 0) {
-    if (!a.target.logits && a.target.ids[t] >= a.V) atomicOr(a.target.status, kErrTarget);
-    a.loss[t] = kept ? loss2 * kLn2 + (a.target.logits ? a.target.self[t] : 0.f) : 0.f;
-    a.lse[t] = kept ? lse2 * kLn2 : 0.f;
-    f.s.stat[2 * t] = m;
-    f.s.stat[2 * t + 1] = 1.f / l;
-  }
+  __syncthreads();
+  if (!last) return;
+  for (int r = threadIdx.x / 32; r < R; r += kThreads / 32) few_loss<T>(f, blockIdx.y, r);
+  if (threadIdx.x == 0) f.s.done[blockIdx.y] = 0u;
 }
 
 // Four columns of a row per thread: side by side, or (SPREAD, rows that no vector of
@@ -493,7 +507,6 @@ cudaError_t run(const SoftmaxArgs& a, const FewScratch& s) {
   if (vw == kWide) scores<T, kWide, false>(f);
   else if (vw >= 4) scores<T, 4, false>(f);
   else scores<T, kWide, true>(f);
-  few_stat_kernel<T><<<(unsigned)a.n, 32, 0, a.st>>>(f);
   if (a.grad_h) vg == 4 ? grads<T, false>(f) : grads<T, true>(f);
   return cudaGetLastError();
 }

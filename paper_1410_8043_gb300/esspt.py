@@ -467,6 +467,11 @@ class SoftmaxHead:
             raise EssptError(EINVAL, f"{name} must be a contiguous {self.dtype} tensor of shape {shape} on {self.device}")
         return x
 
+    def _call(self, head, ids, logits, tail) -> int:
+        if logits is None:
+            return self._lib.esspt_softmax_loss(*head, ids.data_ptr(), *tail)
+        return self._lib.esspt_softmax_distill(*head, ids.data_ptr(), logits.data_ptr(), ids.shape[1], *tail)
+
     def _run(self, h, w, ids, logits, weight, inv_temperature, backward, grad_h, grad_w) -> SoftmaxResult:
         if backward is None:
             backward = self.backward
@@ -491,11 +496,11 @@ class SoftmaxHead:
         tail = (n, _ptr(weight), inv_temperature, loss.data_ptr(), lse.data_ptr(), _ptr(grad_h), _ptr(grad_w))
         head = (self._h, h.data_ptr(), h.stride(0) if n > 1 else self.width, w.data_ptr(),
                 w.stride(0) if self.n_items > 1 else self.width)
-        with torch.cuda.device(self.device):
-            if logits is None:
-                st = self._lib.esspt_softmax_loss(*head, ids.data_ptr(), *tail)
-            else:
-                st = self._lib.esspt_softmax_distill(*head, ids.data_ptr(), logits.data_ptr(), ids.shape[1], *tail)
+        if torch.cuda.current_device() == self.device.index:
+            st = self._call(head, ids, logits, tail)
+        else:
+            with torch.cuda.device(self.device):
+                st = self._call(head, ids, logits, tail)
         if elsewhere:
             cur.wait_stream(self.stream)
         if st != OK:
