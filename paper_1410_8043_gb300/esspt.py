@@ -389,7 +389,8 @@ class SoftmaxHead:
     the rows' losses.  The n x n_items scores are never kept.  The workspace is
     allocated here once.  Work runs on `stream` (default: the current one at
     construction); a call from another current stream is ordered after the work
-    queued there, and that stream's later work after the call.
+    queued there, and that stream's later work after the call.  Calls may be captured
+    in a CUDA graph, where `stream` is the captured one.
     """
 
     def __init__(self, max_rows: int, n_items: int, width: int, dtype=torch.float32, max_top: int = 1,

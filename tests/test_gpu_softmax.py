@@ -376,6 +376,34 @@ def test_another_stream(T):
     head.poll()
 
 
+@pytest.mark.parametrize("T,V", [(6, 5000), (100, 700), (200, 5000)])
+def test_captured_in_a_graph(T, V):
+    """Calls of a handle on the captured stream, replayed on other values: what a call gives."""
+    D = 48
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        head = _esspt().SoftmaxHead(T, V, D, max_top=3)
+        h, w, ids, z, weight = _inputs(T, V, D, "f32", 3, 71)
+
+        def both():
+            return [*head.loss(h, w, ids[:, 0], weight=weight), *head.distill(h, w, ids, z, weight=weight)]
+
+        both()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = both()
+        for seed in (72, 73):
+            for x, y in zip((h, w, ids, z, weight), _inputs(T, V, D, "f32", 3, seed)):
+                x.copy_(y)
+            graph.replay()
+            got = [x.clone() for x in out]
+            assert all(torch.equal(x, y) for x, y in zip(got, both()))
+        head.poll()
+    torch.cuda.current_stream().wait_stream(stream)
+
+
 @pytest.mark.parametrize("T", [6, 200])
 def test_ids_outside_the_catalogue(T):
     """They count as absent, and poll reports them once."""
