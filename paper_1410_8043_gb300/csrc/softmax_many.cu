@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, cons
     }
     first[threadIdx.x] = lo;
   }
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 255) {  // (divisions, beside the searches)
     slots[0] = 1, slots[1] = 0;
     if (rows > 0) {
       const Ranges r(a.V, rows, 1, f.blocks);
@@ -545,15 +545,33 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, cons
   };
   T* to = static_cast<T*>(a.grad_w) + v0 * a.D;
   const int slices = a.D / VEC;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < items * slices; i += 256) {
-    const int item = i / slices, d = (i - item * slices) * VEC;
-    if (first[item] != first[item + 1]) continue;
-    float x[VEC];
-    sum(item, d, x);
+  constexpr int U = 4;  // loads of a thread under way
+  for (int i0 = threadIdx.x; i0 < items * slices; i0 += U * 256) {
+    float x[U][VEC] = {};
+    int from[U];  // where in its slots; < 0: none, or an item with targets
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = a.b * ldexpf(x[e], shift);
-    store_vec<T, VEC>(to + item * a.D + d, x);
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * 256, item = i / slices;
+      from[u] = i < items * slices && first[item] == first[item + 1] ? item * f.ld + (i - item * slices) * VEC : -1;
+    }
+    for (int64_t s = slots[0]; s <= slots[1]; ++s) {
+      const float* part = f.s.out + (s * 128 + v0 % 128) * f.ld;
+      float y[U][VEC] = {};
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (from[u] >= 0) load_vec<float, VEC>(part + from[u], y[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][e] += y[u][e];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (from[u] < 0) continue;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[u][e] = a.b * ldexpf(x[u][e], shift);
+      store_vec<T, VEC>(to + (i0 + u * 256) * VEC, x[u]);
+    }
   }
   // (By item and 32 VEC columns.)
   const int chunks = (a.D + 32 * VEC - 1) / (32 * VEC);
