@@ -10,7 +10,7 @@
 //   cols       sum weight p h, then dw
 //
 // The kernels here are bound by bytes or by latency: 2048 x 1M, K = 64, fp32, GB300:
-// max 43 us (256 MB, 6.0 TB/s), units 72 (512 MB, 7.1 TB/s), dw 154 (512 MB, 3.3 TB/s,
+// max 43 us (256 MB, 6.0 TB/s), units 72 (512 MB, 7.1 TB/s), dw 118 (512 MB, 4.3 TB/s,
 // with its scattered targets) of the call's 2550.
 #include <cub/device/device_radix_sort.cuh>
 
@@ -504,8 +504,10 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
 
 // dw: b (sum weight p h - sum weight q h), kItems items to a block.  Most items are
 // nobody's target: those rows go through all threads side by side, the others a warp
-// each (2048 x 1M, K = 64: a warp for every item took 470 us, this 154).
-constexpr int kItems = 64;  // at most; 16 where 64 would leave SMs idle
+// each (2048 x 1M, K = 64: a warp for every item took 470 us, this 118).
+// Items of a block: 16 where 64 would leave SMs idle, 64 up to 32 blocks of them per SM,
+// else 128 (that case: 118 us, by 64 129).
+constexpr int kItems = 128;
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, const uint32_t* key, const int32_t* row,
                                                      const float* factor) {
@@ -722,7 +724,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   if (sizeof(T) == 2) launch_runs(a.st);  // (wants the rows' sums)
   m.A = s.units_w, m.B = s.units_h;
   if ((e = launch_mma(Pass::kCols, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
-  const int per_block = (int64_t)a.V < (int64_t)kItems * 8 * a.sms ? 16 : kItems;
+  const int per_block = (int64_t)a.V < 64ll * 8 * a.sms ? 16 : (int64_t)a.V < 64ll * 32 * a.sms ? 64 : kItems;
   grad_w_kernel<T, VEC><<<(unsigned)(((int64_t)a.V + per_block - 1) / per_block), 256, 0, a.st>>>(f, per_block, key.Current(),
                                                                                            entry_row, entry_factor);
   return cudaGetLastError();
