@@ -543,14 +543,17 @@ cudaError_t run(const SoftmaxArgs& a, const FewScratch& s) {
 
 int few_blocks(int sms) { return 4 * sms; }
 
-// By what both ways take, in us, fitted to 12 to 128 rows on 1000 to 800k items of 16 to
-// 256 values (fp32 and bf16, with gradients and without).  With gradients, here and by
-// tensor cores: 20k items, K = 64, 128 rows 105 and 116; 200k, K = 64, 24 rows 177 and
-// 239, 48 rows 306 and 241.  Forward: 200k, K = 64, 24 rows 44 and 66, 48 rows 73 and 67.
+// By what both ways take, in us, fitted to 12 to 128 rows on 1000 to 800k items of 4 to
+// 500 values (fp32 and bf16, with gradients and without), and 2^24 scores kept at most.
+// With gradients, here and by tensor cores: 20k items, K = 64, 128 rows 90 and 108; 200k,
+// K = 64, 24 rows 164 and 213, 48 rows 286 and 215; 9k, K = 256, 128 rows 132 and 120.
+// Forward: 200k, K = 64, 24 rows 41 and 68, 48 rows 71 and 68; 9k, K = 256, 128 rows 37 and 44.
 bool few_rows(int64_t n, int64_t V, int32_t D, bool grads) {
   if (n <= kFewRows || n > kSmallRows) return n <= kFewRows;
-  const double items = (double)V, few = grads ? 45 + n * items * (1.6e-5 + 2.1e-7 * D) : 28 + n * items * (1e-6 + 7e-8 * D);
-  return few <= (grads ? 95 + items * (2.5e-4 + 5e-6 * D) : 44 + items * (5e-5 + 1e-6 * D));
+  if (n * V > (1 << 24)) return false;
+  const double items = (double)V, scores = n * items;
+  const double few = grads ? 34 + items * (1.8e-4 + 3.5e-7 * D) + scores * (6.8e-6 + 2.4e-7 * D) : 10 + scores * (1e-6 + 8e-8 * D);
+  return few <= (grads ? 88 + items * (2e-4 + 6.3e-6 * D) : 36 + items * (5e-5 + 1e-6 * D));
 }
 int few_groups(int64_t max_rows, int64_t V, int32_t D, bool backward) {
   int64_t n = std::min<int64_t>(max_rows, kSmallRows);

@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
   if (d < a.D) store_vec<float, VEC>(f.s.run_sum[LEVEL] + run * a.D + d, x);
 }
 
-// dw: b (sum weight p h - sum weight q h), kItems items to a block.  Most items are
+// dw: b (sum weight p h - sum weight q h), some items to a block.  Most items are
 // nobody's target: those rows go through all threads side by side, the others a warp
 // each (2048 x 1M, K = 64: a warp for every item took 470 us, this 118).
 // Items of a block: 16 where 64 would leave SMs idle, 64 up to 32 blocks of them per SM,

@@ -154,6 +154,24 @@ def test_long_streams(T, V, D, dtype):
     _check(_run("distill", h, w, ids, z, weight, 1.0), ref, dtype, D, 1.0)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,V,D,top", [(1, 200_003, 24, 1), (1, 200_003, 61, 3), (1, 90_001, 500, 9), (5, 200_003, 24, 9),
+                                       (5, 160_001, 61, 3), (2, 300_000, 130, 40)])
+def test_few_rows_over_many_items(T, V, D, top, dtype):
+    """Lists short and long, scores kept and not, widths read by vectors and by single values."""
+    h, w, ids, z, weight = _inputs(T, V, D, dtype, top, T + V + D, pad=0.0 if T == 1 else 0.2)
+    ref = _reference(h, w, ids, z, weight, 1.0)
+    _check(_run("distill", h, w, ids, z, weight, 1.0), ref, dtype, D, 1.0)
+    _check(_run("distill", h, w, ids, z, weight, 1.0, backward=False), ref, dtype, D, 1.0)
+    ids[:, 0], h = V - 1, h.nan_to_num(0.0)
+    ref = _reference(h, w, ids[:, :1], torch.zeros_like(z[:, :1]), weight, 1.0)
+    _check(_run("loss", h, w, ids, z, weight, 1.0, backward=False), ref, dtype, D, 1.0)
+    w[V // 2, D - 1] = math.nan
+    assert bool(_run("loss", h, w, ids, z, weight, 1.0, backward=False).loss.isnan().all())
+    r = _run("loss", h, w, ids.fill_(-1), z, weight, 1.0, backward=False)
+    assert bool((r.loss == 0).all()) and bool((r.lse == 0).all())
+
+
 SIDES = [(8, 700, 32), (200, 700, 32)]  # a few rows, and more
 
 
