@@ -278,7 +278,7 @@ __device__ __forceinline__ void store_cols(T* row, int col, int tx, int D, const
 // four columns (tx threads to a row) of every ty-th item, four items deep.
 template <typename T, bool SPREAD, int kTile>
 __global__ void __launch_bounds__(kThreads, SPREAD ? 2 : 3) few_grad_w_kernel(Few f, int tx) {
-  constexpr int R = kFewRows, U = 4, VEC = kCols;
+  constexpr int R = kFewRows, U = SPREAD ? 2 : 4, VEC = kCols;
   extern __shared__ __align__(32) float g[];  // [groups][kTile][R]
   __shared__ __align__(16) float red[kTile == 8 ? kThreads * VEC : 1];
   __shared__ float bw[kSmallRows], mx[kSmallRows], inv[kSmallRows];
