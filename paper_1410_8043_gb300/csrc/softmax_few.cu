@@ -3,8 +3,8 @@
 // are kept, W is read once for them and once for dh.  All in fp32.
 //
 // 1M items, K = 64, fp32, eight rows, GB300: scores 58 us (256 MB, 4.4 TB/s: loads in
-// flight), dw 100 (320 MB), dh 86 (288 MB, 3.3 TB/s), against 38 us for 256 MB.  A
-// single row's scores without gradients: a call of 54 us in fp32 and 34 in bf16, where
+// flight), dw 100 (320 MB), dh 82 (288 MB, 3.5 TB/s), against 38 us for 256 MB.  A
+// single row's scores without gradients: a call of 50 us in fp32 and 34 in bf16, where
 // the kernel for eight rows takes 64 and 55.
 #include <algorithm>
 
