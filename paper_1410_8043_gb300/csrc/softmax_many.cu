@@ -3,8 +3,8 @@
 //
 //   compact    the kept rows in order (ignored ones cost nothing from here on)
 //   max, units H (kept rows) and W in 16 KB units, fp32 in two halves
-//   stats      maximum and sum of every row, then its loss; or, with gradients of large
-//              problems, references for the rows from their targets and a part of W
+//   stats      maximum and sum of every row, then its loss; or, with gradients, references
+//              for the rows: their maxima, of large problems of bf16 rows over a part of W
 //   rows       sum p w (and sum p), then dh and the loss
 //   entries    targets sorted by item on a second stream, sums over long runs of one item
 //   cols       sum weight p h, then dw
@@ -21,10 +21,6 @@
 namespace esspt {
 
 namespace {
-
-// Probabilities by a sampled reference r are 2^(s - r + 4): up to 2^12 times too large
-// for their row, a sum of fp16 still holds them.
-constexpr float kSampledShift = 4.f;
 
 struct Many {
   SoftmaxArgs a;
@@ -279,10 +275,13 @@ __global__ void __launch_bounds__(256) loss_kernel(Many f) {
   if (lane == 0) finish_row<kParts>(f, t, pos, m, l, loss2);
 }
 
-// A warp per row: a reference for its probabilities without all of its scores, the
-// largest of those of its targets and of W's first rows.  Probabilities may then be
-// larger than one; where one leaves the range of their type, which shows in the sums, the
-// exact passes run (grad_h_kernel).
+// A warp per row: the reference of its probabilities, the largest of the scores of its
+// targets and of W's first f.sample rows.  fp16 probabilities (the halves of fp32 rows
+// too) are kept 2^14 times as large, in steps of 2^-24, so that a tail of a million items
+// of 2^-30 of the largest is still there; that leaves no room above one, and the sample
+// is all of W.  bf16 has fp32's range: there a sample does, probabilities may be larger
+// than one, and where they leave that range, which shows in the sums, the exact passes
+// run (grad_h_kernel).
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) reference_kernel(Many f) {
   const SoftmaxArgs& a = f.a;
@@ -327,21 +326,22 @@ __device__ __forceinline__ float rounded_off(float p) {
 }
 
 // dh, a warp per row and 32 VEC columns: b weight (sum p w / l - sum q w_id).  After a pass by references
-// (SAMPLED) the row's sum and loss come first, and a sum that is no number asks for the
-// exact passes.
-template <typename T, int VEC, bool SAMPLED>
+// (BY_REF) the row's sum and loss come first, and of bf16 rows a sum that is no number
+// asks for the exact passes.
+template <typename T, int VEC, bool BY_REF>
 __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
   constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
+  constexpr bool kMayRedo = BY_REF && std::is_same<T, __nv_bfloat16>::value;
   const SoftmaxArgs& a = f.a;
   const int64_t t = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
   if (t >= a.n || (f.if_redo && f.s.words->redo == 0u)) return;
   const int64_t pos = f.s.pos[t];
-  if (SAMPLED && blockIdx.y == 0) {
+  if (BY_REF && blockIdx.y == 0) {
     pad_cols<kParts>(f, t);
     if (pos < 0 && (threadIdx.x & 31) == 0) a.loss[t] = a.lse[t] = 0.f;
   }
   float row_sum = 1.f;
-  if (SAMPLED && pos >= 0) {
+  if (BY_REF && pos >= 0) {
     const int lane = threadIdx.x & 31;
     const Ranges r(f.s.words->rows, a.V, 1, f.blocks);
     const int64_t g = pos / 128, i0 = r.block_of(g * r.n_b), i1 = r.block_of((g + 1) * r.n_b - 1);
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
     loss2 = warp_sum(loss2);
     if (lane == 0 && blockIdx.y == 0) {
       finish_row<kParts>(f, t, pos, f.s.row_max[pos], l, loss2);
-      if (!(l < 3e38f)) f.s.words->redo = 1u;
+      if (kMayRedo && !(l < 3e38f)) f.s.words->redo = 1u;
     }
   } else if (pos >= 0) {
     row_sum = f.s.row_sum[pos];
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
   for (int e = 0; e < VEC; ++e) x[e] = 0.f;
   if (pos >= 0) {
     if (on) add_slots<VEC>(f, f.s.words->rows, a.V, pos, d, x);
-    if (SAMPLED) {
+    if (kMayRedo) {
       bool fine = true;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) fine &= fabsf(x[e]) < 3e38f;
@@ -681,21 +681,21 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   // products of halves have no sums of their own, half as many tiles.
   const MmaShape stats_shape = mma_shape(Pass::kStats, a.D, kParts), rows_shape = mma_shape(Pass::kRows, a.D, kParts);
   const int out_chunks = (a.D + 255) / 256, run_tiles = kParts == 1 ? 128 : rows_shape.cross ? 16 : 8;
-  // Maxima and sums over W's first `items` rows, and what is made of them.
-  auto stats = [&](int32_t items, int if_redo) {
+  // Maxima (and sums) over W's first `items` rows, and what is made of them.
+  auto stats = [&](Pass pass, int32_t items, int if_redo) {
     f.shape = m.s = stats_shape, f.if_redo = m.if_redo = if_redo, m.V = items, m.run = INT32_MAX;
-    const cudaError_t err = launch_mma(Pass::kStats, kBf16, kParts, m, a.sms, 1, a.st);
+    const cudaError_t err = launch_mma(pass, kBf16, kParts, m, a.sms, 1, a.st);
     m.V = a.V;
     return err;
   };
-  auto rows = [&](bool sampled, int if_redo) {
+  auto rows = [&](bool by_ref, int if_redo) {
     f.shape = m.s = rows_shape, f.if_redo = m.if_redo = if_redo, m.run = run_tiles;
-    f.up = m.up = kBf16 ? 0.f : sampled ? kSampledShift : kHalfShift;
-    m.sums = sampled ? reinterpret_cast<float*>(s.stat) : nullptr;
+    f.up = m.up = kBf16 ? 0.f : kHalfShift;
+    m.sums = by_ref ? reinterpret_cast<float*>(s.stat) : nullptr;
     return launch_mma(Pass::kRows, kBf16, kParts, m, a.sms, out_chunks, a.st);
   };
   auto exact = [&](int if_redo) {
-    cudaError_t err = stats(a.V, if_redo);
+    cudaError_t err = stats(Pass::kStats, a.V, if_redo);
     if (err != cudaSuccess) return err;
     loss_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
     if (!grads) return cudaGetLastError();
@@ -703,17 +703,18 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
     grad_h_kernel<T, VEC, false><<<dim3(by_row, col_chunks), 256, 0, a.st>>>(f);
     return cudaGetLastError();
   };
-  // A pass over all scores for the rows' maxima alone is a third of the work.  Where it
-  // is more than that of the launches that stand by (about 10 us), references from a
-  // sixteenth of W do, and the exact passes run only if one of them was too low.
+  // A pass over all scores of bf16 rows for their maxima alone is a fifth of the work.
+  // Where it is more than that of the launches that stand by (about 10 us), references
+  // from a sixteenth of W do, and the exact passes run only if one of them was too low.
   const int64_t n_w = ((int64_t)a.V + 127) / 128;
-  if (grads && n_w >= 32 && (a.n + 127) / 128 * n_w >= 24ll * a.sms) {
-    f.sample = (int32_t)(128 * (n_w / 16));
-    if ((e = stats(f.sample, 0)) != cudaSuccess) return e;
+  const bool sampled = kBf16 && n_w >= 32 && (a.n + 127) / 128 * n_w >= 24ll * a.sms;
+  if (grads && (sampled || !kBf16)) {
+    f.sample = sampled ? (int32_t)(128 * (n_w / 16)) : a.V;
+    if ((e = stats(Pass::kMax, f.sample, 0)) != cudaSuccess) return e;
     reference_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
     if ((e = rows(true, 0)) != cudaSuccess) return e;
     grad_h_kernel<T, VEC, true><<<dim3(by_row, col_chunks), 256, 0, a.st>>>(f);
-    if ((e = exact(1)) != cudaSuccess) return e;
+    if (sampled && (e = exact(1)) != cudaSuccess) return e;
   } else if ((e = exact(0)) != cudaSuccess) {
     return e;
   }

@@ -117,7 +117,7 @@ constexpr uint32_t kEmpty = 8 * kUnits;
 // cycles per tile, 1020 of them products).
 template <Pass PASS, bool BF16, int PARTS, int NK>
 struct Issue {
-  static constexpr bool STATS = PASS == Pass::kStats;
+  static constexpr bool STATS = only_scores(PASS);
   static constexpr MmaShape S = mma_shape(PASS, 64 * NK, PARTS);
   static constexpr uint32_t kIdesc = mma_desc(BF16, 128, false);
   static constexpr uint32_t kUnit = kUnitBytes >> 4;  // in descriptors
@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   extern __shared__ __align__(1024) char smem[];
   __shared__ uint32_t tmem_at;
   __shared__ uint32_t dead_flag;
-  constexpr bool STATS = PASS == Pass::kStats;
+  constexpr bool STATS = only_scores(PASS);
   constexpr int kColBytes = PARTS == 2 ? 1024 : 512;  // of a tile's columns
   const MmaShape sh = a.s;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const bool negative = PASS == Pass::kCols && a.words->negative != 0u;
     uint32_t phase = 0, o_phase = 0;  // parities of s_full's next turn, a bit per buffer
     int col0 = 0;  // stage of the run's first column data
-    float m = 0.f, l = 0.f, at = 0.f;  // kStats: maximum (without the scale), sum, and m scale; kRows: sum
+    float m = 0.f, l = 0.f, at = 0.f;  // kStats, kMax: maximum (without the scale), sum, and m scale; kRows: sum
     while (walk.next(g)) {
       const int nt = tiles_of(g);
       const int32_t jobs = nt * g.len;
@@ -534,6 +534,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
             for (int i = 0; i < 32; i += 2)
               top[(i >> 1) & 3] = max3(top[(i >> 1) & 3], __uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1]));
             const float m2 = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+            if constexpr (PASS == Pass::kMax) {
+              m = m2, at = m2 * scale;
+              continue;
+            }
             const float at2 = m2 == -INFINITY ? 0.f : m2 * scale;
             const u64 minus = pack2(-at2, -at2);
             u64 sum[2] = {0ull, 0ull};
@@ -662,6 +666,7 @@ cudaError_t launch_type(bool bf16, int parts, const MmaArgs& a, int blocks, int 
 
 cudaError_t launch_mma(Pass pass, bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st) {
   if (pass == Pass::kStats) return launch_type<Pass::kStats>(bf16, parts, a, blocks, 1, st);
+  if (pass == Pass::kMax) return launch_type<Pass::kMax>(bf16, parts, a, blocks, 1, st);
   if (pass == Pass::kRows) return launch_type<Pass::kRows>(bf16, parts, a, blocks, out_chunks, st);
   return launch_type<Pass::kCols>(bf16, parts, a, blocks, out_chunks, st);
 }

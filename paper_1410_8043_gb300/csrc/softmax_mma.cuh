@@ -9,9 +9,11 @@ namespace esspt {
 
 // What a pass makes of the scores S = A B^T b / ln 2:
 //   kStats  per row of A the maximum and the sum of 2^(S - maximum)
+//   kMax    per row of A the maximum
 //   kRows   A = H, B = W: sum over B's rows of 2^(S - row_max) B, and of 2^(S - row_max)
 //   kCols   A = W, B = H: sum over B's rows t of 2^(S - maximum_t) factor_t B
-enum class Pass { kStats, kRows, kCols };
+enum class Pass { kStats, kMax, kRows, kCols };
+__host__ __device__ constexpr bool only_scores(Pass pass) { return pass == Pass::kStats || pass == Pass::kMax; }
 
 constexpr int kUnits = 13;             // units of shared memory
 constexpr float kHalfShift = 14.f;     // fp16 probabilities are kept 2^14 times as large
@@ -40,7 +42,7 @@ __host__ __device__ constexpr MmaShape mma_shape(Pass pass, int32_t D, int parts
   s.steps = (D + 15) / 16;
   s.nk = (D + 63) / 64;
   const int t = s.nk * parts;
-  const bool stats = pass == Pass::kStats;
+  const bool stats = only_scores(pass);
   s.tiles = stats && 2 * t + 3 <= kUnits ? 2 : 1;
   s.res = s.tiles == 2 || t + (parts == 2 ? 4 : 3) <= kUnits;
   s.keep = s.res && 3 * t <= kUnits;
@@ -61,7 +63,7 @@ struct MmaArgs {
   // kCols, fp32 rows: two columns to a float4, (-maximum, -maximum, factor, factor); of
   // 16-bit rows a float to a column, log2 |factor| - maximum with the sign as its lowest bit.
   const float* col;
-  float2* stat;          // kStats out: [slot][4][128], by group and half of the columns
+  float2* stat;          // kStats, kMax out: [slot][4][128], by group and half of the columns
   float* sums;           // kRows out: sums of the probabilities, likewise, or null
   float up;              // kRows: probabilities are taken 2^up times as large
   int if_redo;           // only where words->redo is set
