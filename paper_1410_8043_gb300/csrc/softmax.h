@@ -59,6 +59,7 @@ int few_blocks(int sms);
 // scaled by a power of two each), so that three products of halves give fp32's.
 struct ManyWords {  // (device) what a call's kernels tell each other
   uint32_t max_h, max_w, max_weight;  // largest finite magnitude, as fp32 bits
+  uint32_t min_weight;                // smallest but zero, as its distance below infinity
   int32_t rows;                       // rows that are not ignored
   uint32_t negative;                  // whether one of their weights is
   uint32_t redo;                      // a row's reference was too low: the exact passes run
@@ -68,7 +69,8 @@ struct ManyScratch {
   int32_t *act, *pos;      // [n] the kept rows in order; a row's place among them, or -1
   char *units_h, *units_w;
   float *row_max, *row_sum;  // [n] statistics of the kept rows, in order
-  float* col;                // [2 (n up to 128)] the kept rows as columns of dw: see MmaArgs
+  float *col, *col_top;      // [2 (n up to 128)], [n up to 128] the kept rows as columns of dw: see MmaArgs
+  uint32_t* item_top;        // [V] an item's largest log2 of weight p over the rows (top_key); fp32 and fp16
   float* score;              // [n * top] scores of the targets
   float2* stat;              // partial statistics and
   float* out;                // partial gradients by slot (Ranges, softmax_mma.cuh)

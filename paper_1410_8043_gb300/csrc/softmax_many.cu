@@ -7,7 +7,8 @@
 //              for the rows: their maxima, of large problems of bf16 rows over a part of W
 //   rows       sum p w (and sum p), then dh and the loss
 //   entries    targets sorted by item on a second stream, sums over long runs of one item
-//   cols       sum weight p h, then dw
+//   cols       fp32 rows (and fp16 rows of weights far apart): the largest weight p of every
+//              item; sum weight p h, then dw
 //
 // The kernels here are bound by bytes or by latency: 2048 x 1M, K = 64, fp32, GB300:
 // max 43 us (256 MB, 6.0 TB/s), units 72 (512 MB, 7.1 TB/s), dw 118 (512 MB, 4.3 TB/s,
@@ -72,8 +73,14 @@ __global__ void __launch_bounds__(1024) compact_kernel(Many f) {
     if (t == a.n - 1) f.s.words->rows = base + kept;
   }
   if (a.weight && __any_sync(0xffffffffu, kept && a.weight[t] < 0.f) && lane == 0) f.s.words->negative = 1u;
-  if (a.weight) block_max(kept ? finite_bits(a.weight[t]) : 0u, &f.s.words->max_weight);
-  else if (t == 0) f.s.words->max_weight = __float_as_uint(1.f);
+  if (a.weight) {
+    const uint32_t bits = kept ? finite_bits(a.weight[t]) : 0u;
+    block_max(bits, &f.s.words->max_weight);
+    block_max(bits ? 0x7f800000u - bits : 0u, &f.s.words->min_weight);
+  } else if (t == 0) {
+    f.s.words->max_weight = __float_as_uint(1.f);
+    f.s.words->min_weight = 0x7f800000u - __float_as_uint(1.f);
+  }
 }
 
 // Largest finite magnitude of W, and of the kept rows of H (blockIdx.y = 1): a warp
@@ -115,6 +122,7 @@ __global__ void __launch_bounds__(256) units_kernel(Many f, bool is_h) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / pieces;
     const int32_t c = (int32_t)(i - r * pieces);
+    if (!is_h && c == 0 && r < rows && f.s.col) f.s.item_top[r] = 0u;
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 0.f;
@@ -156,12 +164,13 @@ __device__ __forceinline__ void set_col(const Many& f, int64_t pos, float m, flo
   if (PARTS == 2) {
     float* c = f.s.col + pos / 2 * 4 + (pos & 1);
     c[0] = -m, c[2] = factor;
+    f.s.col_top[pos] = log2f(fabsf(factor)) - m;
   } else {
     f.s.col[pos] = __uint_as_float((__float_as_uint(log2f(fabsf(factor)) - m) & ~1u) | (factor < 0.f ? 1u : 0u));
   }
 }
-__device__ __forceinline__ float col_probability(const Many& f, int64_t pos, float score) {  // (16-bit rows)
-  const float c = f.s.col[pos], p = exp2_fast(score + c);
+__device__ __forceinline__ float col_probability(const Many& f, int64_t pos, float score, float up) {  // (16-bit rows)
+  const float c = f.s.col[pos], p = exp2_fast(score + (c + up));
   return __float_as_uint(c) & 1u && f.s.words->negative ? -p : p;
 }
 
@@ -244,10 +253,7 @@ __device__ __forceinline__ void finish_row(const Many& f, int64_t t, int64_t pos
   f.s.row_max[pos] = m;
   f.s.row_sum[pos] = l;
   const float weight = a.weight ? a.weight[t] : 1.f;
-  // fp16 probabilities: weight / 2^shift at most one, times 2^14
-  const float factor =
-      a.dtype == ESSPT_BF16 ? weight : times_pow2(weight, (int)kHalfShift - weight_shift_of(f.s.words->max_weight));
-  set_col<PARTS>(f, pos, m, factor / l);
+  set_col<PARTS>(f, pos, m, weight / l);
 }
 
 // A warp per row: its statistics, the scores of its targets, its loss.
@@ -431,10 +437,12 @@ __global__ void tile_first_kernel(Many f, const uint32_t* key) {
   f.s.tile_first[i] = (int32_t)lo;
 }
 
-// The power of two by which the sums over columns are to be multiplied.
-__device__ __forceinline__ int cols_shift(const Many& f) {
-  return (f.parts == 2 ? -half_shift_of(f.s.words->max_h) : 0) +
-         (f.a.dtype == ESSPT_BF16 ? 0 : weight_shift_of(f.s.words->max_weight) - (int)kHalfShift);
+// The power of two by which an item's sum over columns is to be multiplied.
+template <typename T>
+__device__ __forceinline__ int item_shift(const Many& f, int64_t item) {
+  const ManyWords& w = *f.s.words;
+  return -(int)item_up<std::is_same<T, __nv_bfloat16>::value, sizeof(T) == 4 ? 2 : 1>(w, f.s.item_top, item) -
+         (sizeof(T) == 4 ? half_shift_of(w.max_h) : 0);
 }
 
 // Of every entry in order of the items its row of H, and weight q less what rounding took.
@@ -447,7 +455,10 @@ __global__ void factors_kernel(Many f, const uint32_t* key, const uint32_t* val,
   const int32_t t = (int32_t)(entry / (uint32_t)a.target.top);
   const float q = a.target.logits ? a.target.q[entry] : 1.f;
   float g = a.weight ? q * a.weight[t] : q;
-  if (sizeof(T) == 2) g -= ldexpf(rounded_off<T>(col_probability(f, f.s.pos[t], f.s.score[entry])), cols_shift(f));
+  if (sizeof(T) == 2) {
+    const int shift = item_shift<T>(f, key[i]);
+    g -= ldexpf(rounded_off<T>(col_probability(f, f.s.pos[t], f.s.score[entry], (float)-shift)), shift);
+  }
   row[i] = t;
   factor[i] = g;
 }
@@ -512,6 +523,7 @@ template <typename T, int VEC>
 __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, const uint32_t* key, const int32_t* row,
                                                      const float* factor) {
   __shared__ int32_t first[kItems + 1];
+  __shared__ int shifts[kItems];
   __shared__ int64_t slots[2];
   const SoftmaxArgs& a = f.a;
   const int64_t v0 = (int64_t)blockIdx.x * per_block, rows = f.s.words->rows;
@@ -524,6 +536,7 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, cons
       else hi = mid;
     }
     first[threadIdx.x] = lo;
+    if (threadIdx.x < items) shifts[threadIdx.x] = item_shift<T>(f, v0 + threadIdx.x);
   }
   if (threadIdx.x == 255) {  // (divisions, beside the searches)
     slots[0] = 1, slots[1] = 0;
@@ -534,7 +547,6 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, cons
     }
   }
   __syncthreads();
-  const int shift = cols_shift(f);
   auto sum = [&](int item, int d, float (&x)[VEC]) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) x[e] = 0.f;
@@ -550,11 +562,12 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, cons
   constexpr int U = 4;  // loads of a thread under way
   for (int i0 = threadIdx.x; i0 < items * slices; i0 += U * 256) {
     float x[U][VEC] = {};
-    int from[U];  // where in its slots; < 0: none, or an item with targets
+    int from[U], shift[U];  // where in its slots; < 0: none, or an item with targets
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * 256, item = i / slices;
       from[u] = i < items * slices && first[item] == first[item + 1] ? item * f.ld + (i - item * slices) * VEC : -1;
+      shift[u] = from[u] >= 0 ? shifts[item] : 0;
     }
     for (int64_t s = slots[0]; s <= slots[1]; ++s) {
       const float* part = f.s.out + (s * 128 + v0 % 128) * f.ld;
@@ -571,7 +584,7 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, cons
     for (int u = 0; u < U; ++u) {
       if (from[u] < 0) continue;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[u][e] = a.b * ldexpf(x[u][e], shift);
+      for (int e = 0; e < VEC; ++e) x[u][e] = a.b * ldexpf(x[u][e], shift[u]);
       store_vec<T, VEC>(to + (i0 + u * 256) * VEC, x[u]);
     }
   }
@@ -602,7 +615,7 @@ __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, cons
     add_sums<VEC>(f.s.run_sum[0], q0 < q1 ? q1 * kRun : r1, r1, a.D, d, y);
     add_sums<VEC>(f.s.run_sum[1], q0, q1, a.D, d, y);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = a.b * (ldexpf(x[e], shift) - y[e]);
+    for (int e = 0; e < VEC; ++e) x[e] = a.b * (ldexpf(x[e], shifts[item]) - y[e]);
     if (d < a.D) store_vec<T, VEC>(to + item * a.D + d, x);
   }
 }
@@ -722,8 +735,13 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   m.if_redo = f.if_redo = 0;
 
   if ((e = cudaStreamWaitEvent(a.st, s.join, 0)) != cudaSuccess) return e;
-  if (sizeof(T) == 2) launch_runs(a.st);  // (wants the rows' sums)
-  m.A = s.units_w, m.B = s.units_h;
+  m.A = s.units_w, m.B = s.units_h, m.item_top = s.item_top;
+  if (!kBf16) {
+    m.s = stats_shape, m.run = INT32_MAX, m.if_apart = kParts == 1, m.col = kParts == 2 ? s.col_top : s.col;
+    if ((e = launch_mma(Pass::kMaxCols, false, kParts, m, a.sms, 1, a.st)) != cudaSuccess) return e;
+    m.s = rows_shape, m.run = run_tiles, m.col = s.col;
+  }
+  if (sizeof(T) == 2) launch_runs(a.st);  // (wants the rows' sums and the items' references)
   if ((e = launch_mma(Pass::kCols, kBf16, kParts, m, a.sms, out_chunks, a.st)) != cudaSuccess) return e;
   const int per_block = (int64_t)a.V < 64ll * 8 * a.sms ? 16 : (int64_t)a.V < 64ll * 32 * a.sms ? 64 : kItems;
   grad_w_kernel<T, VEC><<<(unsigned)(((int64_t)a.V + per_block - 1) / per_block), 256, 0, a.st>>>(f, per_block, key.Current(),

@@ -347,18 +347,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   __shared__ uint32_t tmem_at;
   __shared__ uint32_t dead_flag;
   constexpr bool STATS = only_scores(PASS);
-  constexpr int kColBytes = PARTS == 2 ? 1024 : 512;  // of a tile's columns
+  constexpr int kColBytes = PARTS == 2 && PASS == Pass::kCols ? 1024 : 512;  // of a tile's columns
   const MmaShape sh = a.s;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int64_t rows_h = a.words->rows;
-  const int64_t rows_a = PASS == Pass::kCols ? a.V : rows_h, rows_b = PASS == Pass::kCols ? rows_h : a.V;
+  const int64_t rows_a = items_first(PASS) ? a.V : rows_h, rows_b = items_first(PASS) ? rows_h : a.V;
   const Ranges ranges(rows_a, rows_b, sh.tiles, gridDim.x);
   if (blockIdx.x >= ranges.blocks || (a.if_redo && a.words->redo == 0u)) return;
+  if (PASS == Pass::kMaxCols && a.if_apart && !weights_apart(*a.words)) return;
 
   const uint32_t base = (smem_addr(smem) + 1023u) & ~1023u;
   const uint32_t a_base = base, b_base = base + (sh.res ? sh.tiles * sh.nk * PARTS : 0) * kUnitBytes;
-  const uint32_t col_base = base + kUnits * kUnitBytes;  // [stages] of the columns' data
+  const uint32_t col_base = base + kUnits * kUnitBytes;  // [col_slots] of the columns' data
   const char* col_data = smem + (col_base - smem_addr(smem));
+  const int col_slots = sh.stages + (PASS == Pass::kMaxCols ? kTopSlots : 0);
   const uint32_t bar0 = col_base + kUnits * 1024;
   Bars bar;
   bar.full = bar0, bar.empty = bar.full + kEmpty, bar.a_full = bar.empty + 8 * kUnits, bar.a_empty = bar.a_full + 8;
@@ -391,7 +393,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     // ---- loads ----
     if (lane == 0) {
       Ring ring(b_base, bar.full, sh.stage_units * kUnitBytes, sh.stages);
-      int col = 0;  // stage of the column data
+      int col = 0;  // slot of the column data
       uint32_t a_phase = 1, loads = 0, segs = 0;
       const uint32_t stage_bytes = sh.stage_units * kUnitBytes;
       // A stage of what lies at `from`, or its second unit `apart` further on.
@@ -401,13 +403,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         mbar_expect(ring.bar, stage_bytes + (cols ? kColBytes : 0));
         bulk_load(ring.at, from, apart ? kUnitBytes : stage_bytes, ring.bar);
         if (apart) bulk_load(ring.at + kUnitBytes, from + apart, kUnitBytes, ring.bar);
-        if (cols) bulk_load(col_base + col * 1024, cols, kColBytes, ring.bar);
+        if (cols) bulk_load(col_base + col * kColBytes, cols, kColBytes, ring.bar);
         ring.next();
         ++loads;
       };
       auto scores_units = [&](int64_t tile, const char* from_a) {
         const char* from = a.B + tile * tile_bytes;
-        const char* cols = PASS == Pass::kCols ? reinterpret_cast<const char*>(a.col) + tile * kColBytes : nullptr;
+        const char* cols = items_first(PASS) ? reinterpret_cast<const char*>(a.col) + tile * kColBytes : nullptr;
         if (sh.stage_units == sh.nk * PARTS) {
           load(from, cols);
         } else if (sh.stage_units == 2) {  // two units of a row's, or the halves of one
@@ -421,7 +423,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
               load(from + (p * sh.nk + kc) * (int64_t)kUnitBytes, kc == 0 && p == 0 ? cols : nullptr);
           }
         }
-        if (++col == sh.stages) col = 0;
+        if (++col == col_slots) col = 0;
       };
       auto sums_units = [&](int64_t tile) {
         const char* from = a.B + tile * tile_bytes;
@@ -489,7 +491,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const u64 scale2 = pack2(scale, scale);
     const bool negative = PASS == Pass::kCols && a.words->negative != 0u;
     uint32_t phase = 0, o_phase = 0;  // parities of s_full's next turn, a bit per buffer
-    int col0 = 0;  // stage of the run's first column data
+    int col0 = 0;  // slot of the run's first column data
+    float up = 0.f;  // kCols: item_up
     float m = 0.f, l = 0.f, at = 0.f;  // kStats, kMax: maximum (without the scale), sum, and m scale; kRows: sum
     while (walk.next(g)) {
       const int nt = tiles_of(g);
@@ -500,13 +503,17 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         const int64_t r = g.group * 128 + row;
         offset = r < rows_a ? a.up - a.row_max[r] : -1e30f;
       }
+      if (PASS == Pass::kCols && !BF16 && g.begins) {
+        const int64_t item = g.group * 128 + row;
+        up = item < rows_a ? item_up<BF16, PARTS>(*a.words, a.item_top, item) : 0.f;
+      }
       // Jobs go to the pairs by turns, and to the buffers by turns: with three buffers
       // both pairs come by each, so a pair counts the other's turns too.
       int col = col0, buf = 0;
       for (int32_t n = 0; n < jobs; ++n) {
         const int at_buf = buf, at_col = col;
         if (++buf == sh.buffers) buf = 0;
-        if (++col == sh.stages) col = 0;
+        if (nt == 1 || (n & 1)) col = col + 1 == col_slots ? 0 : col + 1;
         const uint32_t parity = (phase >> at_buf) & 1;
         phase ^= 1u << at_buf;
         if ((n & 1) != pair) continue;
@@ -520,12 +527,31 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         uint32_t r[kBoth ? 2 : 1][32];
         if constexpr (kBoth) tmem_load(r[0], s_at, r[1], s_at + 32);
         else tmem_load(r[0], s_at);
-        if constexpr (STATS) {
+        if constexpr (STATS && PASS != Pass::kMaxCols) {
           fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);
         }
-        if constexpr (STATS) {
+        if constexpr (PASS == Pass::kMaxCols) {
+          // (Columns after the last: the column data says -infinity.)
+          const ulonglong2* cols = reinterpret_cast<const ulonglong2*>(col_data + at_col * kColBytes + kColBytes / 2 * half);
+          float top[4] = {m, m, m, m};
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              const ulonglong2 q = cols[8 * c + i / 4];
+              float x, y;
+              unpack2(fma2(pack2(__uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1])), scale2, q.x), x, y);
+              top[(i >> 1) & 3] = max3(top[(i >> 1) & 3], x, y);
+              unpack2(fma2(pack2(__uint_as_float(r[c][i + 2]), __uint_as_float(r[c][i + 3])), scale2, q.y), x, y);
+              top[(i >> 1 & 3) + 1] = max3(top[(i >> 1 & 3) + 1], x, y);
+            }
+          m = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);
+        } else if constexpr (STATS) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             mask_scores(r[c], left - 32 * c);
@@ -554,8 +580,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
             m = m2, at = at2;
           }
         } else {
-          const ulonglong2* cols = reinterpret_cast<const ulonglong2*>(col_data + at_col * 1024 + kColBytes / 2 * half);
+          const ulonglong2* cols = reinterpret_cast<const ulonglong2*>(col_data + at_col * kColBytes + kColBytes / 2 * half);
           const u64 offset2 = pack2(offset, offset);
+          const float times_up = PARTS == 2 ? exp2f(up) : 0.f;
+          const u64 up2 = PARTS == 2 ? pack2(times_up, times_up) : pack2(up, up);
           u64 sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
@@ -576,11 +604,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
                 } else if (PARTS == 2) {
                   const ulonglong2 q = cols[16 * c + i / 2];
                   unpack2(fma2(s2, scale2, q.x), p[0], p[1]);
-                  unpack2(mul2(pack2(exp2_fast(p[0]), exp2_fast(p[1])), q.y), p[0], p[1]);
+                  unpack2(mul2(pack2(exp2_fast(p[0]), exp2_fast(p[1])), mul2(q.y, up2)), p[0], p[1]);
                 } else {
                   const ulonglong2 q = cols[8 * c + i / 4];
                   const u64 k = i & 2 ? q.y : q.x;
-                  unpack2(fma2(s2, scale2, k), p[0], p[1]);
+                  unpack2(fma2(s2, scale2, BF16 ? k : add2(k, up2)), p[0], p[1]);
                   p[0] = exp2_fast(p[0]), p[1] = exp2_fast(p[1]);
                   if (negative) {  // a factor's sign is the lowest bit of its logarithm
                     p[0] = __uint_as_float(__float_as_uint(p[0]) ^ ((uint32_t)k << 31));
@@ -602,7 +630,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         }
       }
       if (PASS == Pass::kRows && a.sums && g.ends && blockIdx.y == 0) a.sums[(g.slot * 4 + 2 * pair + half) * 128 + row] = l;
-      if (PASS == Pass::kCols) col0 = (col0 + g.len) % sh.stages;
+      if (items_first(PASS)) col0 = (col0 + g.len) % col_slots;
+      if (PASS == Pass::kMaxCols) {
+        const int64_t item = (g.group * sh.tiles + (nt == 2 ? pair : 0)) * 128 + row;
+        if (item < rows_a && m != -INFINITY) atomicMax(a.item_top + item, top_key(m));
+        continue;
+      }
       if (STATS) {
         a.stat[(g.slot * 4 + 2 * pair + half) * 128 + row] = make_float2(m == -INFINITY ? m : at, l);
         continue;
@@ -667,6 +700,7 @@ cudaError_t launch_type(bool bf16, int parts, const MmaArgs& a, int blocks, int 
 cudaError_t launch_mma(Pass pass, bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st) {
   if (pass == Pass::kStats) return launch_type<Pass::kStats>(bf16, parts, a, blocks, 1, st);
   if (pass == Pass::kMax) return launch_type<Pass::kMax>(bf16, parts, a, blocks, 1, st);
+  if (pass == Pass::kMaxCols) return launch_type<Pass::kMaxCols>(bf16, parts, a, blocks, 1, st);
   if (pass == Pass::kRows) return launch_type<Pass::kRows>(bf16, parts, a, blocks, out_chunks, st);
   return launch_type<Pass::kCols>(bf16, parts, a, blocks, out_chunks, st);
 }

@@ -10,13 +10,22 @@ namespace esspt {
 // What a pass makes of the scores S = A B^T b / ln 2:
 //   kStats  per row of A the maximum and the sum of 2^(S - maximum)
 //   kMax    per row of A the maximum
+//   kMaxCols  A = W, B = H: the maximum of S + col over B's rows, an item's over all blocks
 //   kRows   A = H, B = W: sum over B's rows of 2^(S - row_max) B, and of 2^(S - row_max)
 //   kCols   A = W, B = H: sum over B's rows t of 2^(S - maximum_t) factor_t B
-enum class Pass { kStats, kMax, kRows, kCols };
-__host__ __device__ constexpr bool only_scores(Pass pass) { return pass == Pass::kStats || pass == Pass::kMax; }
+enum class Pass { kStats, kMax, kMaxCols, kRows, kCols };
+__host__ __device__ constexpr bool only_scores(Pass pass) {
+  return pass == Pass::kStats || pass == Pass::kMax || pass == Pass::kMaxCols;
+}
+__host__ __device__ constexpr bool items_first(Pass pass) { return pass == Pass::kMaxCols || pass == Pass::kCols; }
 
 constexpr int kUnits = 13;             // units of shared memory
-constexpr float kHalfShift = 14.f;     // fp16 probabilities are kept 2^14 times as large
+constexpr float kHalfShift = 14.f;     // fp16 probabilities: the largest is kept as 2^14
+// Column data of a tile in shared memory lies in slots of its own, by turns.  Where the
+// scores alone are wanted (kMaxCols), a tile's stage is free before its columns were
+// read: by then at most five more tiles' scores are done, each block of eight warps
+// having two of the buffers and taking part in every second tile of a group.
+constexpr int kTopSlots = 8;           // slots beyond the stages, for that
 constexpr int kMmaThreads = 640;       // a warp that loads, one that multiplies, two spare, two groups of eight
 
 // How a pass uses shared and tensor memory: A's units stay (res) or come with every
@@ -62,7 +71,10 @@ struct MmaArgs {
   const float* row_max;  // kRows
   // kCols, fp32 rows: two columns to a float4, (-maximum, -maximum, factor, factor); of
   // 16-bit rows a float to a column, log2 |factor| - maximum with the sign as its lowest bit.
+  // kMaxCols: the latter for fp32 rows too.
   const float* col;
+  uint32_t* item_top;    // kMaxCols out, kCols: ManyScratch
+  int if_apart;          // only where weights_apart
   float2* stat;          // kStats, kMax out: [slot][4][128], by group and half of the columns
   float* sums;           // kRows out: sums of the probabilities, likewise, or null
   float up;              // kRows: probabilities are taken 2^up times as large
@@ -96,9 +108,29 @@ __device__ __forceinline__ float times_pow2(float x, int e) {
   const int e1 = e / 2;
   return x * __int_as_float((e1 + 127) << 23) * __int_as_float((e - e1 + 127) << 23);
 }
-// Weights are divided by the power of two that is at least the largest, where p is kept in fp16.
-__device__ __forceinline__ int weight_shift_of(uint32_t max_bits) {
-  return max_bits == 0u ? 0 : (int)(max_bits >> 23) - 127 + 1;
+// Whether the rows' weights differ by more than 2^8.
+__device__ __forceinline__ bool weights_apart(const ManyWords& w) {
+  return w.max_weight != 0u && (int)(w.max_weight >> 23) - (int)((0x7f800000u - w.min_weight) >> 23) > 8;
+}
+// Floats in their order as whole numbers; 0 is below all.
+__device__ __forceinline__ uint32_t top_key(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+// The power of two that an item's terms weight p are multiplied by in the sum over rows.
+// fp32 rows, whose result has fp32's range: by the item's own largest term, for what is
+// left of an item that is nobody's target may be 2^-40 and less of what a target gets.
+// fp16 rows: the result has no such values, so one power for all, by the largest weight,
+// does, unless the weights differ much: then a row of ordinary weight needs its own too.
+template <bool BF16, int PARTS>
+__device__ __forceinline__ float item_up(const ManyWords& w, const uint32_t* top, int64_t item) {
+  if (BF16) return 0.f;
+  if (PARTS == 1 && !weights_apart(w))
+    return w.max_weight == 0u ? kHalfShift : kHalfShift - 1.f - (float)((int)(w.max_weight >> 23) - 127);
+  const uint32_t key = top[item];
+  if (key == 0u) return 0.f;
+  const float m = __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+  return fminf(fmaxf(kHalfShift - ceilf(m), -100.f), 100.f);
 }
 
 cudaError_t launch_mma(Pass pass, bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st);

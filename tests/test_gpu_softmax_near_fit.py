@@ -66,3 +66,65 @@ def test_tail_of_a_large_catalogue(dtype, T, V, D, kind):
         if dtype != "f32":
             bound = bound + torch.finfo(TYPES[dtype]).eps / 2 * want.norm(dim=1) + 2.0**-25 * math.sqrt(D)
         assert bool((err <= bound).all()), float((err / bound).max())
+
+
+EPS = 2.0**-24
+
+
+def _dw(h, w, ids, weight, items):
+    """Rows `items` of dw in fp64, their terms' absolute sums, and the largest sum of a score's."""
+    h64, w64, at = h.double(), w.double(), ids.long()
+    s = h64 @ w64.T
+    p = torch.exp(s - torch.logsumexp(s, 1, keepdim=True))[:, items]
+    q = (at[:, None] == items[None]).double()
+    g = weight.double()[:, None] * (p - q)
+    mass = (weight.double().abs()[:, None] * (p + q)).T @ h64.abs()
+    return g.T @ h64, mass, float((h64.abs() @ w64.abs().T).max())
+
+
+def _check_items(r, h, w, ids, weight, items, dtype, D):
+    """Every value relative to its own terms: p is off by what its score is (2 ds: 8 eps a
+    product, 2 eps an addition), by exponentials and by halves of 11 bits (1e-5; 16-bit
+    rows: the type's half-unit), sums by 1e-4, the result by its rounding."""
+    want, mass, prod = _dw(h, w, ids, weight, items)
+    half = 2.0**-24 if dtype == "f32" else torch.finfo(TYPES[dtype]).eps / 2
+    ep = 4 * (D + 8) * EPS * prod + 1e-5 + half + 1e-4
+    err = (r.grad_w[items].double() - want).abs()
+    bound = ep * mass + half * want.abs() + (0 if dtype == "f32" else 2.0**-25)
+    assert bool((err <= bound).all()), float((err / bound).max())
+
+
+@pytest.mark.parametrize("T,V,D,gap", [(64, 1_000_003, 64, 28.0), (300, 100_003, 150, 40.0)])
+def test_items_that_are_nobodys_target(T, V, D, gap):
+    """Their gradients are sums of probabilities of 2^-40 and less: as good, relative to
+    themselves, as any other's."""
+    h, w, y = _fitted(T, V, D, "f32", gap, 6)
+    head = _head(T, V, D)
+    weight = torch.ones(T, device="cuda")
+    r = head.loss(h, w, y, weight=weight)
+    head.poll()
+    items = torch.arange(0, V, max(1, V // 2000), device="cuda")
+    items = items[~torch.isin(items, y.long())]
+    _check_items(r, h, w, y, weight, items, "f32", D)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,V,D", [(200, 3000, 64), (700, 9000, 150), (6, 3000, 64)])
+def test_one_weight_far_above_the_others(T, V, D, dtype, sign):
+    """A row with a weight of 1e8 that is fitted (p of its target near one): items that have
+    nothing of it keep the gradients of the other rows."""
+    g = torch.Generator("cuda").manual_seed(T)
+    w = torch.randn((V, D), generator=g, device="cuda") * 0.5
+    u = torch.nn.functional.normalize(torch.randn(D, generator=g, device="cuda"), dim=0)
+    h = torch.randn((T, D), generator=g, device="cuda") * 0.3
+    y = torch.randint(1, V, (T,), generator=g, device="cuda").int()
+    w[0], h[3], y[3] = 8.0 * u, 11.0 * u, 0  # 88 above the others' mean, their deviation is 5.5
+    h, w = h.to(TYPES[dtype]), w.to(TYPES[dtype])
+    weight = torch.rand(T, generator=g, device="cuda") + 0.5
+    weight[3] = 1e8 * sign
+    weight[4] *= -1
+    head = _head(T, V, D, dtype=TYPES[dtype])
+    r = head.loss(h, w, y, weight=weight)
+    head.poll()
+    _check_items(r, h, w, y, weight, torch.arange(1, V, device="cuda"), dtype, D)
