@@ -63,13 +63,14 @@ struct ManyWords {  // (device) what a call's kernels tell each other
   int32_t rows;                       // rows that are not ignored
   uint32_t negative;                  // whether one of their weights is
   uint32_t redo;                      // a row's reference was too low: the exact passes run
+  uint32_t huge;                      // a row's reference is past kHuge
 };
 struct ManyScratch {
   ManyWords* words;
   int32_t *act, *pos;      // [n] the kept rows in order; a row's place among them, or -1
   char *units_h, *units_w;
   float *row_max, *row_sum;  // [n] statistics of the kept rows, in order
-  float *col, *col_top;      // [2 (n up to 128)], [n up to 128] the kept rows as columns of dw: see MmaArgs
+  float *col, *col_top, *col_m, *col_f;  // [2 (n up to 128)], [n up to 128] the kept rows as columns of dw: see MmaArgs
   uint32_t* item_top;        // [V] an item's largest log2 of weight p over the rows (top_key); fp32 and fp16
   float* score;              // [n * top] scores of the targets
   float2* stat;              // partial statistics and

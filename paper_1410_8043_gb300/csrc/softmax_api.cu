@@ -11,7 +11,7 @@ namespace {
 
 struct Carve {
   size_t status, q, self, scores, part, stat, dh;
-  size_t words, act, pos, units_h, units_w, row_max, row_sum, score, col, col_top, item_top, slot_stat, out, key[2], val[2], tile_first, run_sum[2], sort;
+  size_t words, act, pos, units_h, units_w, row_max, row_sum, score, col, col_top, col_m, col_f, item_top, slot_stat, out, key[2], val[2], tile_first, run_sum[2], sort;
   size_t sort_bytes, total;
 };
 
@@ -101,7 +101,7 @@ Carve carve(const esspt_softmax_config& c) {
     k.row_sum = take(back * n * sizeof(float));
     k.score = take(entries);
     k.col = take(back * (n + 128) * sizeof(float2));
-    k.col_top = take(back * (n + 128) * sizeof(float));
+    for (size_t* p : {&k.col_top, &k.col_m, &k.col_f}) *p = take(back * (n + 128) * sizeof(float));
     k.item_top = take(back * V * sizeof(uint32_t));
     k.out = take(z.out);
     for (int i = 0; i < 2; ++i) k.key[i] = take(entries), k.val[i] = take(entries);
@@ -158,6 +158,7 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   s.row_max = static_cast<float*>(at(k.row_max)), s.row_sum = static_cast<float*>(at(k.row_sum));
   s.score = static_cast<float*>(at(k.score));
   s.col = static_cast<float*>(at(k.col)), s.col_top = static_cast<float*>(at(k.col_top));
+  s.col_m = static_cast<float*>(at(k.col_m)), s.col_f = static_cast<float*>(at(k.col_f));
   s.item_top = static_cast<uint32_t*>(at(k.item_top)), s.stat = static_cast<float2*>(at(k.slot_stat));
   s.out = static_cast<float*>(at(k.out));
   for (int i = 0; i < 2; ++i)

@@ -161,6 +161,7 @@ __global__ void __launch_bounds__(256) units_kernel(Many f, bool is_h) {
 // Column data of dw (MmaArgs); what the kernel makes of a score by it.
 template <int PARTS>
 __device__ __forceinline__ void set_col(const Many& f, int64_t pos, float m, float factor) {
+  f.s.col_m[pos] = -m, f.s.col_f[pos] = factor;
   if (PARTS == 2) {
     float* c = f.s.col + pos / 2 * 4 + (pos & 1);
     c[0] = -m, c[2] = factor;
@@ -253,7 +254,9 @@ __device__ __forceinline__ void finish_row(const Many& f, int64_t t, int64_t pos
   f.s.row_max[pos] = m;
   f.s.row_sum[pos] = l;
   const float weight = a.weight ? a.weight[t] : 1.f;
-  set_col<PARTS>(f, pos, m, weight / l);
+  // (l = 0: no item was within fp32's range of the reference, as with scores of infinity.)
+  set_col<PARTS>(f, pos, m, l == 0.f ? 0.f : weight / l);
+  if (fabsf(m) > kHuge) f.s.words->huge = 1u;
 }
 
 // A warp per row: its statistics, the scores of its targets, its loss.
@@ -298,10 +301,13 @@ __global__ void __launch_bounds__(256) reference_kernel(Many f) {
   float m, l;
   merge_slots(f, pos, f.sample, m, l);
   target_scores<T, VEC>(a, t, [&](int k, float q, float s) {
-    m = fmaxf(m, s);
+    if (f.sample < a.V) m = fmaxf(m, s);
     f.s.score[t * a.target.top + k] = s;
   });
   m = warp_max(m);
+  // (fp32 rows: in sixteenths, so that 14 - m and -m are exact and dh and dw have the same
+  // p.  16-bit rows: as it is, so that near a fit the target itself has p = 1, not rounded.)
+  if (sizeof(T) == 4 && fabsf(m) <= kHuge) m = rintf(m * 16.f) * 0.0625f;
   if ((threadIdx.x & 31) == 0) f.s.row_max[pos] = m == -INFINITY ? 0.f : m;
 }
 
@@ -325,7 +331,8 @@ __device__ __forceinline__ void add_slots(const Many& f, int64_t rows_a, int64_t
 // What rounding p to 16 bits took from the sum of a target's product.  Near a fit p - q
 // is small beside p, and that rounding would be most of it (p = 0.99, q = 1: 0.004 of
 // 0.01); other items' p are off by their own half-unit only.  (The score here and the
-// tensor core's differ in their last bits, so now and then p rounds the other way there.)
+// tensor core's differ in their last bits, so now and then p rounds the other way there;
+// past kHuge they have nothing in common, but there p is zero or one.)
 template <typename T>
 __device__ __forceinline__ float rounded_off(float p) {
   return sizeof(T) == 4 ? 0.f : p - to_float(from_float<T>(p));
@@ -363,7 +370,7 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
     loss2 = warp_sum(loss2);
     if (lane == 0 && blockIdx.y == 0) {
       finish_row<kParts>(f, t, pos, f.s.row_max[pos], l, loss2);
-      if (kMayRedo && !(l < 3e38f)) f.s.words->redo = 1u;
+      if (kMayRedo && !(l < 3e38f && l > 1e-30f)) f.s.words->redo = 1u;
     }
   } else if (pos >= 0) {
     row_sum = f.s.row_sum[pos];
@@ -393,7 +400,7 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
       const int64_t entry = t * a.target.top + k0 + lane;
       const int32_t lane_id = lane < count ? a.target.ids[entry] : -1;
       float c = lane >= count ? 0.f : a.target.logits ? -a.target.q[entry] : -1.f;
-      if (sizeof(T) == 2 && c != 0.f) c += ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - m + up)) * inv, -shift);
+      if (sizeof(T) == 2 && c != 0.f && fabsf(m) <= kHuge) c += ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - m + up)) * inv, -shift);
       const unsigned share = __ballot_sync(0xffffffffu, c != 0.f);
 #pragma unroll 4
       for (int i = 0; i < count; ++i) {
@@ -455,7 +462,7 @@ __global__ void factors_kernel(Many f, const uint32_t* key, const uint32_t* val,
   const int32_t t = (int32_t)(entry / (uint32_t)a.target.top);
   const float q = a.target.logits ? a.target.q[entry] : 1.f;
   float g = a.weight ? q * a.weight[t] : q;
-  if (sizeof(T) == 2) {
+  if (sizeof(T) == 2 && fabsf(f.s.row_max[f.s.pos[t]]) <= kHuge) {
     const int shift = item_shift<T>(f, key[i]);
     g -= ldexpf(rounded_off<T>(col_probability(f, f.s.pos[t], f.s.score[entry], (float)-shift)), shift);
   }
@@ -686,7 +693,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
 
   MmaArgs m{};
   m.A = s.units_h, m.B = s.units_w, m.words = s.words, m.V = a.V, m.b = a.b;
-  m.row_max = s.row_max, m.col = s.col, m.stat = s.stat, m.out = s.out, m.ld = f.ld;
+  m.row_max = s.row_max, m.col = s.col, m.col_m = s.col_m, m.col_f = s.col_f, m.stat = s.stat, m.out = s.out, m.ld = f.ld;
   m.status = a.target.status;
   // Tiles between additions in fp32.  4096 x 18k, K = 100, lists of 32: dh is 1.0e-6 off
   // with 32 tiles, 5.8e-7 with 16, 3.4e-7 with 8 (7.5e-7 by fp32 products of whole

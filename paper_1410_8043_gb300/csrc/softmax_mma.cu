@@ -154,13 +154,15 @@ struct Issue {
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) mma_ss(d, a + 2 * k, b + 2 * k, kIdesc, k > 0 ? 1u : add, leader);
   }
-  // All products of a pair of units: of halves in the order of their size, (lo, hi),
-  // (hi, lo), (hi, hi); lo lies a_lo and b_lo further.
+  // All products of a pair of units: of halves in the order of their size, W's lo first
+  // whichever operand it is, so that a score is the same number in every pass; lo lies
+  // a_lo and b_lo further.
   template <int STEPS>
   __device__ __forceinline__ void pair(uint32_t d, uint32_t a, uint32_t b, uint32_t a_lo, uint32_t b_lo, uint32_t add) {
     if constexpr (PARTS == 2) {
-      steps<STEPS>(d, a + a_lo, b, add);
-      steps<STEPS>(d, a, b + b_lo, 1);
+      constexpr bool kItems = items_first(PASS);
+      steps<STEPS>(d, kItems ? a + a_lo : a, kItems ? b : b + b_lo, add);
+      steps<STEPS>(d, kItems ? a : a + a_lo, kItems ? b + b_lo : b, 1);
       steps<STEPS>(d, a, b, 1);
     } else {
       steps<STEPS>(d, a, b, add);
@@ -331,6 +333,10 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
   return r;
 }
 
+// x y + z rounded after each operation.  (The intrinsics are never contracted; the packed
+// instructions are.)
+__device__ __forceinline__ float mul_then_add(float x, float y, float z) { return __fadd_rn(__fmul_rn(x, y), z); }
+
 // Scores of columns from `left` on become -infinity.  Only a tile at the end of B has
 // any: a branch of its own (as selects these were most of the instructions).
 __device__ __forceinline__ void mask_scores(uint32_t (&r)[32], int left) {
@@ -490,6 +496,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const float scale = fminf(fmaxf(ldexpf(a.b * kLog2e, -(shift_h + shift_w)), 1.1754944e-38f), 3.4028235e38f);
     const u64 scale2 = pack2(scale, scale);
     const bool negative = PASS == Pass::kCols && a.words->negative != 0u;
+    // Tiles of what is rare (rows past kHuge) go a way of their own, by vote: the control
+    // flow of a warp stays one.
+    const bool slow_cols = items_first(PASS) && __any_sync(0xffffffffu, a.words->huge != 0u);
     uint32_t phase = 0, o_phase = 0;  // parities of s_full's next turn, a bit per buffer
     int col0 = 0;  // slot of the run's first column data
     float up = 0.f;  // kCols: item_up
@@ -498,11 +507,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       const int nt = tiles_of(g);
       const int32_t jobs = nt * g.len;
       if (g.begins) m = -INFINITY, l = 0.f, at = 0.f;
-      float offset = 0.f;
+      float minus_m = 0.f;
+      bool slow = slow_cols;
       if (PASS == Pass::kRows) {
         const int64_t r = g.group * 128 + row;
-        offset = r < rows_a ? a.up - a.row_max[r] : -1e30f;
+        minus_m = r < rows_a ? -a.row_max[r] : -1e30f;
+        slow = __any_sync(0xffffffffu, r < rows_a && fabsf(minus_m) > kHuge);
       }
+      const float offset = minus_m + a.up;
       if (PASS == Pass::kCols && !BF16 && g.begins) {
         const int64_t item = g.group * 128 + row;
         up = item < rows_a ? item_up<BF16, PARTS>(*a.words, a.item_top, item) : 0.f;
@@ -522,6 +534,49 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         fence_after();
         const int left = (int)min((int64_t)64, rows_b - (g.first + j) * 128 - 64 * half);  // of this half's columns
         const uint32_t s_at = lanes + 128 * at_buf + 64 * half;
+        if (!only_scores(PASS) || PASS == Pass::kMaxCols) {
+          if (slow) {
+            // 16 columns at a time, scores rounded before maxima come off, column data by
+            // ordinary loads.
+            const int64_t from = (g.first + j) * 128 + 64 * half;
+            const float times_up = exp2f(up);
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              uint32_t x[16], hi[8];
+              tmem_load(x, s_at + 16 * c);
+              float p[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int64_t col = from + 16 * c + i;
+                const float s = __uint_as_float(x[i]);
+                if (PASS == Pass::kRows) {
+                  p[i] = 16 * c + i < left ? exp2_fast(mul_then_add(s, scale, minus_m) + a.up) : 0.f;
+                  l += p[i];
+                } else {
+                  p[i] = mul_then_add(s, scale, a.col_m[col]);
+                  if (PASS == Pass::kMaxCols) m = fmaxf(m, p[i] + log2f(fabsf(a.col_f[col])));
+                  else p[i] = exp2_fast(p[i]) * (a.col_f[col] * times_up);
+                }
+              }
+              if (PASS == Pass::kMaxCols) continue;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) hi[i] = pack16<BF16>(p[2 * i], p[2 * i + 1]);
+              if constexpr (PARTS == 2) {
+                uint32_t out[16];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out[i] = hi[i], out[8 + i] = pack16_rest(hi[i], p[2 * i], p[2 * i + 1]);
+                tmem_store16(s_at + 16 * c, out);
+              } else {
+                tmem_store8(s_at + 32 * (c >> 1) + 8 * (c & 1), hi);
+              }
+            }
+            if (PASS != Pass::kMaxCols) tmem_wait_store();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);
+            continue;
+          }
+        }
         // (fp32 rows: 32 columns at a time, for the registers.)
         constexpr bool kBoth = STATS || PARTS == 1;
         uint32_t r[kBoth ? 2 : 1][32];
@@ -567,11 +622,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
             const float at2 = m2 == -INFINITY ? 0.f : m2 * scale;
             const u64 minus = pack2(-at2, -at2);
             u64 sum[2] = {0ull, 0ull};
+            if (__any_sync(0xffffffffu, fabsf(at2) > kHuge)) {
+              float e = 0.f;
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              float x, y;
-              unpack2(fma2(pack2(__uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1])), scale2, minus), x, y);
-              sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(exp2_fast(x), exp2_fast(y)));
+              for (int i = 0; i < 32; ++i) e += exp2_fast(mul_then_add(__uint_as_float(r[c][i]), scale, -at2));
+              sum[0] = pack2(e, 0.f);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                float x, y;
+                unpack2(fma2(pack2(__uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1])), scale2, minus), x, y);
+                sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(exp2_fast(x), exp2_fast(y)));
+              }
             }
             // (The same maximum again has to leave l as it is: a factor off by its rounding
             // drifted by 7e-6 over 800 tiles.)

@@ -21,6 +21,13 @@ __host__ __device__ constexpr bool items_first(Pass pass) { return pass == Pass:
 
 constexpr int kUnits = 13;             // units of shared memory
 constexpr float kHalfShift = 14.f;     // fp16 probabilities: the largest is kept as 2^14
+// Scores this far from zero (in units of log 2) are rounded before the row's maximum is
+// taken off.  Below, one fused operation does both, and what is off is the rounding of
+// the maximum, 2^-14 at most.  Above, S b less a rounded maximum would be off by half a
+// unit of it: by 512 at 10^10, where all of a row's probabilities became zero or infinite.
+// Rounded first, the best item's difference is zero, as all passes form the same sums in
+// the same order.
+constexpr float kHuge = 1024.f;
 // Column data of a tile in shared memory lies in slots of its own, by turns.  Where the
 // scores alone are wanted (kMaxCols), a tile's stage is free before its columns were
 // read: by then at most five more tiles' scores are done, each block of eight warps
@@ -73,6 +80,7 @@ struct MmaArgs {
   // 16-bit rows a float to a column, log2 |factor| - maximum with the sign as its lowest bit.
   // kMaxCols: the latter for fp32 rows too.
   const float* col;
+  const float *col_m, *col_f;  // kMaxCols, kCols: -maximum and factor by themselves
   uint32_t* item_top;    // kMaxCols out, kCols: ManyScratch
   int if_apart;          // only where weights_apart
   float2* stat;          // kStats, kMax out: [slot][4][128], by group and half of the columns
