@@ -55,8 +55,10 @@ struct FewScratch {
 int few_blocks(int sms);
 
 // Many rows: operands in 16 KB units of 128 rows by 64 16-bit values (tensor.cuh);
-// fp32 values in two halves of 11 bits (x = hi + lo, both fp16, all of H and all of W
-// scaled by a power of two each), so that three products of halves give fp32's.
+// fp32 values in two halves of 11 bits (x = hi + lo, both fp16), so that three products of
+// halves give fp32's.  H and W are scaled by a power of two each, and a row that is more
+// than 2^8 below its matrix's largest value by a second one of its own (RowScale): a value
+// is held to 2^-40 of its row's largest, or to 2^-32, whatever the other rows are.
 struct ManyWords {  // (device) what a call's kernels tell each other
   uint32_t max_h, max_w, max_weight;  // largest finite magnitude, as fp32 bits
   uint32_t min_weight;                // smallest but zero, as its distance below infinity
@@ -64,11 +66,16 @@ struct ManyWords {  // (device) what a call's kernels tell each other
   uint32_t negative;                  // whether one of their weights is
   uint32_t redo;                      // a row's reference was too low: the exact passes run
   uint32_t huge;                      // a row's reference is past kHuge
+  uint32_t spread_h, spread_w;        // whether any row has a power of its own
+};
+struct RowScale {  // units hold the row 1 / c times as large as the matrix's power alone says
+  float c, log2_c;
 };
 struct ManyScratch {
   ManyWords* words;
   int32_t *act, *pos;      // [n] the kept rows in order; a row's place among them, or -1
   char *units_h, *units_w;
+  RowScale *scale_h, *scale_w;  // (fp32) of the kept rows and of W, up to whole tiles
   float *row_max, *row_sum;  // [n] statistics of the kept rows, in order
   float *col, *col_top, *col_m, *col_f;  // [2 (n up to 128)], [n up to 128] the kept rows as columns of dw: see MmaArgs
   uint32_t* item_top;        // [V] an item's largest log2 of weight p over the rows (top_key); fp32 and fp16

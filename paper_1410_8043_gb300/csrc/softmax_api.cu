@@ -11,7 +11,7 @@ namespace {
 
 struct Carve {
   size_t status, q, self, scores, part, stat, dh;
-  size_t words, act, pos, units_h, units_w, row_max, row_sum, score, col, col_top, col_m, col_f, item_top, slot_stat, out, key[2], val[2], tile_first, run_sum[2], sort;
+  size_t words, act, pos, units_h, units_w, scale_h, scale_w, row_max, row_sum, score, col, col_top, col_m, col_f, item_top, slot_stat, out, key[2], val[2], tile_first, run_sum[2], sort;
   size_t sort_bytes, total;
 };
 
@@ -96,6 +96,8 @@ Carve carve(const esspt_softmax_config& c) {
     k.pos = take(n * sizeof(int32_t));
     k.units_h = take(z.units_h);
     k.units_w = take(z.units_w);
+    k.scale_h = take(c.dtype == ESSPT_F32 ? (n + 128) * sizeof(RowScale) : 0);
+    k.scale_w = take(c.dtype == ESSPT_F32 ? (V + 128) * sizeof(RowScale) : 0);
     k.slot_stat = take(z.stat);
     k.row_max = take(back * n * sizeof(float));
     k.row_sum = take(back * n * sizeof(float));
@@ -155,6 +157,7 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   s.words = static_cast<ManyWords*>(at(k.words));
   s.act = static_cast<int32_t*>(at(k.act)), s.pos = static_cast<int32_t*>(at(k.pos));
   s.units_h = static_cast<char*>(at(k.units_h)), s.units_w = static_cast<char*>(at(k.units_w));
+  s.scale_h = static_cast<RowScale*>(at(k.scale_h)), s.scale_w = static_cast<RowScale*>(at(k.scale_w));
   s.row_max = static_cast<float*>(at(k.row_max)), s.row_sum = static_cast<float*>(at(k.row_sum));
   s.score = static_cast<float*>(at(k.score));
   s.col = static_cast<float*>(at(k.col)), s.col_top = static_cast<float*>(at(k.col_top));

@@ -2,7 +2,7 @@
 // passes over tiles of scores, and what joins their partial results.
 //
 //   compact    the kept rows in order (ignored ones cost nothing from here on)
-//   max, units H (kept rows) and W in 16 KB units, fp32 in two halves
+//   max, units H (kept rows) and W in 16 KB units, fp32 in two halves by powers of two
 //   stats      maximum and sum of every row, then its loss; or, with gradients, references
 //              for the rows: their maxima, of large problems of bf16 rows over a part of W
 //   rows       sum p w (and sum p), then dh and the loss
@@ -108,9 +108,95 @@ __global__ void __launch_bounds__(256) max_kernel(Many f) {
   block_max(top, is_h ? &f.s.words->max_h : &f.s.words->max_w);
 }
 
-// Rows to units: a thread makes 16 bytes (8 values) of a row.  The rows after the
-// last, up to the end of its tile, and the values after a row's last are zero.
-template <typename T, int PARTS, int VEC>
+// Where a row's piece of 8 values lies in its unit (tensor.cuh).
+__device__ __forceinline__ char* piece_of(char* units, int64_t r, int parts, int32_t nk, int32_t kc, int piece) {
+  const int row = (int)(r & 127);
+  return units + (((r >> 7) * parts * nk + kc) * (int64_t)kUnitBytes) + row * 128 + ((piece ^ (row & 7)) << 4);
+}
+// Values d .. d + 7 of a row, zero from D on.
+template <typename T, int VEC>
+__device__ __forceinline__ void load_piece(const T* row, int32_t d, int32_t D, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; e += VEC)
+    if (d + e < D) {  // (VEC divides D)
+      float k[VEC];
+      load_vec<T, VEC>(row + d + e, k);
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) v[e + q] = k[q];
+    }
+}
+
+// fp32 rows to units of halves, eight lanes to a row: its largest value first, which
+// decides whether the row takes a power of two of its own (in registers up to two units,
+// else read again).  The rows after the last, up to the end of its tile, and the values
+// after a row's last are zero.
+template <int VEC>
+__global__ void __launch_bounds__(256) units_f32_kernel(Many f, bool is_h) {
+  constexpr int kKept = 2, kApart = 8, kMost = 80;  // (2^80: sums of p stay in range)
+  const SoftmaxArgs& a = f.a;
+  const float* x = static_cast<const float*>(is_h ? a.h : a.w);
+  const int64_t rows = is_h ? f.s.words->rows : a.V, stride = is_h ? a.h_stride : a.w_stride;
+  char* units = is_h ? f.s.units_h : f.s.units_w;
+  RowScale* scales = is_h ? f.s.scale_h : f.s.scale_w;
+  const int32_t nk = f.shape.nk, lane8 = threadIdx.x & 7;
+  const uint32_t max_bits = is_h ? f.s.words->max_h : f.s.words->max_w;
+  const int shift = half_shift_of(max_bits);
+  const int64_t padded = (rows + 127) / 128 * 128;
+  bool any = false;
+  for (int64_t r = (int64_t)blockIdx.x * 32 + threadIdx.x / 8; r < padded; r += (int64_t)gridDim.x * 32) {
+    const float* row = x + (r >= rows ? 0 : is_h ? (int64_t)f.s.act[r] : r) * stride;
+    const int32_t D = r < rows ? a.D : 0;
+    float kept[kKept][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int kc = 0; kc < kKept; ++kc) {
+      load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, kept[kc]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, finite_bits(kept[kc][e]));
+    }
+    for (int32_t kc = kKept; kc < nk; ++kc) {
+      float v[8];
+      load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, finite_bits(v[e]));
+    }
+#pragma unroll
+    for (int off = 4; off > 0; off >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+    int own = top == 0u ? 0 : (int)(max_bits >> 23) - (int)(top >> 23);
+    own = own <= kApart ? 0 : min(own, kMost);
+    any |= own != 0;
+    if (lane8 == 0) {
+      scales[r] = RowScale{__int_as_float((127 - own) << 23), -(float)own};
+      if (!is_h && r < rows && f.s.col) f.s.item_top[r] = 0u;
+    }
+    auto put = [&](int32_t kc, const float (&v)[8]) {
+      alignas(16) __half hi[8], lo[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float s = times_pow2(v[e], shift + own);
+        hi[e] = __float2half_rn(s);
+        lo[e] = __float2half_rn(s - __half2float(hi[e]));
+      }
+      char* to = piece_of(units, r, 2, nk, kc, lane8);
+      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
+      *reinterpret_cast<uint4*>(to + nk * (int64_t)kUnitBytes) = *reinterpret_cast<const uint4*>(lo);
+    };
+#pragma unroll
+    for (int32_t kc = 0; kc < kKept; ++kc)
+      if (kc < nk) put(kc, kept[kc]);
+    for (int32_t kc = kKept; kc < nk; ++kc) {
+      float v[8];
+      load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, v);
+      put(kc, v);
+    }
+  }
+  if (__any_sync(0xffffffffu, any) && (threadIdx.x & 31) == 0) (is_h ? f.s.words->spread_h : f.s.words->spread_w) = 1u;
+}
+
+// 16-bit rows to units: a thread makes 16 bytes (8 values) of a row.  Zeros as above.
+template <typename T, int VEC>
 __global__ void __launch_bounds__(256) units_kernel(Many f, bool is_h) {
   const SoftmaxArgs& a = f.a;
   const T* x = static_cast<const T*>(is_h ? a.h : a.w);
@@ -118,43 +204,16 @@ __global__ void __launch_bounds__(256) units_kernel(Many f, bool is_h) {
   char* units = is_h ? f.s.units_h : f.s.units_w;
   const int32_t nk = f.shape.nk, pieces = nk * 8;
   const int64_t total = (rows + 127) / 128 * 128 * pieces;
-  const int shift = PARTS == 2 ? half_shift_of(is_h ? f.s.words->max_h : f.s.words->max_w) : 0;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / pieces;
     const int32_t c = (int32_t)(i - r * pieces);
     if (!is_h && c == 0 && r < rows && f.s.col) f.s.item_top[r] = 0u;
     float v[8];
+    load_piece<T, VEC>(x + (r >= rows ? 0 : is_h ? (int64_t)f.s.act[r] : r) * stride, c * 8, r < rows ? a.D : 0, v);
+    alignas(16) T out[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    if (r < rows) {
-      const T* from = x + (is_h ? f.s.act[r] : r) * stride + c * 8;
-#pragma unroll
-      for (int e = 0; e < 8; e += VEC)
-        if (c * 8 + e < a.D) {  // (VEC divides D)
-          float k[VEC];
-          load_vec<T, VEC>(from + e, k);
-#pragma unroll
-          for (int q = 0; q < VEC; ++q) v[e + q] = k[q];
-        }
-    }
-    const int row = (int)(r & 127), piece = c & 7;
-    char* to = units + (((r >> 7) * PARTS * nk + (c >> 3)) * (int64_t)kUnitBytes) + row * 128 + ((piece ^ (row & 7)) << 4);
-    if constexpr (PARTS == 2) {
-      alignas(16) __half hi[8], lo[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float s = times_pow2(v[e], shift);
-        hi[e] = __float2half_rn(s);
-        lo[e] = __float2half_rn(s - __half2float(hi[e]));
-      }
-      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
-      *reinterpret_cast<uint4*>(to + nk * (int64_t)kUnitBytes) = *reinterpret_cast<const uint4*>(lo);
-    } else {
-      alignas(16) T out[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) out[e] = from_float<T>(v[e]);
-      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(out);
-    }
+    for (int e = 0; e < 8; ++e) out[e] = from_float<T>(v[e]);
+    *reinterpret_cast<uint4*>(piece_of(units, r, 1, nk, c >> 3, c & 7)) = *reinterpret_cast<const uint4*>(out);
   }
 }
 
@@ -255,7 +314,7 @@ __device__ __forceinline__ void finish_row(const Many& f, int64_t t, int64_t pos
   f.s.row_sum[pos] = l;
   const float weight = a.weight ? a.weight[t] : 1.f;
   // (l = 0: no item was within fp32's range of the reference, as with scores of infinity.)
-  set_col<PARTS>(f, pos, m, l == 0.f ? 0.f : weight / l);
+  set_col<PARTS>(f, pos, m, l == 0.f ? 0.f : PARTS == 2 ? weight / l * f.s.scale_h[pos].c : weight / l);
   if (fabsf(m) > kHuge) f.s.words->huge = 1u;
 }
 
@@ -290,7 +349,8 @@ __global__ void __launch_bounds__(256) loss_kernel(Many f) {
 // of 2^-30 of the largest is still there; that leaves no room above one, and the sample
 // is all of W.  bf16 has fp32's range: there a sample does, probabilities may be larger
 // than one, and where they leave that range, which shows in the sums, the exact passes
-// run (grad_h_kernel).
+// run (grad_h_kernel).  (Of fp32 rows it is the maximum of what the
+// products hold: RowScale.)
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) reference_kernel(Many f) {
   const SoftmaxArgs& a = f.a;
@@ -633,11 +693,12 @@ bool rows_by(int vec, const SoftmaxArgs& a, bool grads) {
   return a.D % vec == 0 && ok(a.h, a.h_stride) && ok(a.w, a.w_stride) && (!grads || (ok(a.grad_h, a.D) && ok(a.grad_w, a.D)));
 }
 
-template <typename T, int PARTS, int VEC>
+template <typename T, int VEC>
 void launch_units(const Many& f, bool is_h) {
-  const int64_t rows = is_h ? f.a.n : f.a.V, pieces = (rows + 127) / 128 * 128 * f.shape.nk * 8;
+  const int64_t padded = ((is_h ? f.a.n : f.a.V) + 127) / 128 * 128, pieces = padded * (sizeof(T) == 4 ? 8 : f.shape.nk * 8);
   const int grid = (int)std::min<int64_t>((pieces + 255) / 256, 32ll * f.a.sms);
-  units_kernel<T, PARTS, VEC><<<grid, 256, 0, f.a.st>>>(f, is_h);
+  if constexpr (sizeof(T) == 4) units_f32_kernel<VEC><<<grid, 256, 0, f.a.st>>>(f, is_h);
+  else units_kernel<T, VEC><<<grid, 256, 0, f.a.st>>>(f, is_h);
 }
 
 int bits_of(uint32_t most) {
@@ -688,11 +749,11 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
     const int64_t work = std::max((int64_t)a.V, a.n) * a.D / VEC;
     max_kernel<VEC><<<dim3((unsigned)std::min<int64_t>((work + 255) / 256, 8ll * a.sms), 2), 256, 0, a.st>>>(f);
   }
-  launch_units<T, kParts, VEC>(f, true);
-  launch_units<T, kParts, VEC>(f, false);
+  launch_units<T, VEC>(f, true);
+  launch_units<T, VEC>(f, false);
 
   MmaArgs m{};
-  m.A = s.units_h, m.B = s.units_w, m.words = s.words, m.V = a.V, m.b = a.b;
+  m.A = s.units_h, m.B = s.units_w, m.scale_a = s.scale_h, m.scale_b = s.scale_w, m.words = s.words, m.V = a.V, m.b = a.b;
   m.row_max = s.row_max, m.col = s.col, m.col_m = s.col_m, m.col_f = s.col_f, m.stat = s.stat, m.out = s.out, m.ld = f.ld;
   m.status = a.target.status;
   // Tiles between additions in fp32.  4096 x 18k, K = 100, lists of 32: dh is 1.0e-6 off
@@ -742,7 +803,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   m.if_redo = f.if_redo = 0;
 
   if ((e = cudaStreamWaitEvent(a.st, s.join, 0)) != cudaSuccess) return e;
-  m.A = s.units_w, m.B = s.units_h, m.item_top = s.item_top;
+  m.A = s.units_w, m.B = s.units_h, m.scale_a = s.scale_w, m.scale_b = s.scale_h, m.item_top = s.item_top;
   if (!kBf16) {
     m.s = stats_shape, m.run = INT32_MAX, m.if_apart = kParts == 1, m.col = kParts == 2 ? s.col_top : s.col;
     if ((e = launch_mma(Pass::kMaxCols, false, kParts, m, a.sms, 1, a.st)) != cudaSuccess) return e;

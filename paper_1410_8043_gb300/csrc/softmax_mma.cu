@@ -491,14 +491,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const int row = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     const int shift_h = PARTS == 2 ? half_shift_of(a.words->max_h) : 0, shift_w = PARTS == 2 ? half_shift_of(a.words->max_w) : 0;
-    // (Kept off 0 and infinity: scores that far are 0 or overflow in any case, and
-    // masked ones stay -infinity.)
-    const float scale = fminf(fmaxf(ldexpf(a.b * kLog2e, -(shift_h + shift_w)), 1.1754944e-38f), 3.4028235e38f);
-    const u64 scale2 = pack2(scale, scale);
+    const float scale_all = ldexpf(a.b * kLog2e, -(shift_h + shift_w));
+    float scale = 0.f;  // of this thread's row
     const bool negative = PASS == Pass::kCols && a.words->negative != 0u;
-    // Tiles of what is rare (rows past kHuge) go a way of their own, by vote: the control
-    // flow of a warp stays one.
-    const bool slow_cols = items_first(PASS) && __any_sync(0xffffffffu, a.words->huge != 0u);
+    // Tiles of what is rare (rows past kHuge, rows of B with powers of their own) go a way of
+    // their own, by vote: the control flow of a warp stays one.
+    const bool slow_cols = __any_sync(0xffffffffu, (items_first(PASS) && a.words->huge != 0u) ||
+                                                       (PARTS == 2 && (items_first(PASS) ? a.words->spread_h : a.words->spread_w) != 0u));
     uint32_t phase = 0, o_phase = 0;  // parities of s_full's next turn, a bit per buffer
     int col0 = 0;  // slot of the run's first column data
     float up = 0.f;  // kCols: item_up
@@ -506,13 +505,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     while (walk.next(g)) {
       const int nt = tiles_of(g);
       const int32_t jobs = nt * g.len;
-      if (g.begins) m = -INFINITY, l = 0.f, at = 0.f;
+      if (g.begins) {
+        m = -INFINITY, l = 0.f, at = 0.f;
+        // (Kept off 0 and infinity: scores that far are 0 or overflow in any case, and
+        // masked ones stay -infinity.)
+        const int64_t r = (g.group * sh.tiles + (nt == 2 ? pair : 0)) * 128 + row;
+        scale = fminf(fmaxf(PARTS == 2 ? scale_all * a.scale_a[r].c : scale_all, 1.1754944e-38f), 3.4028235e38f);
+      }
+      const u64 scale2 = pack2(scale, scale);
       float minus_m = 0.f;
       bool slow = slow_cols;
       if (PASS == Pass::kRows) {
         const int64_t r = g.group * 128 + row;
         minus_m = r < rows_a ? -a.row_max[r] : -1e30f;
-        slow = __any_sync(0xffffffffu, r < rows_a && fabsf(minus_m) > kHuge);
+        slow |= __any_sync(0xffffffffu, r < rows_a && fabsf(minus_m) > kHuge);
       }
       const float offset = minus_m + a.up;
       if (PASS == Pass::kCols && !BF16 && g.begins) {
@@ -534,7 +540,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
         fence_after();
         const int left = (int)min((int64_t)64, rows_b - (g.first + j) * 128 - 64 * half);  // of this half's columns
         const uint32_t s_at = lanes + 128 * at_buf + 64 * half;
-        if (!only_scores(PASS) || PASS == Pass::kMaxCols) {
+        if (PARTS == 2 || !only_scores(PASS) || PASS == Pass::kMaxCols) {
           if (slow) {
             // 16 columns at a time, scores rounded before maxima come off, column data by
             // ordinary loads.
@@ -545,20 +551,41 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
               uint32_t x[16], hi[8];
               tmem_load(x, s_at + 16 * c);
               float p[16];
+              float m2 = m;
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
                 const int64_t col = from + 16 * c + i;
-                const float s = __uint_as_float(x[i]);
-                if (PASS == Pass::kRows) {
-                  p[i] = 16 * c + i < left ? exp2_fast(mul_then_add(s, scale, minus_m) + a.up) : 0.f;
-                  l += p[i];
+                const bool on = 16 * c + i < left;
+                const RowScale k = PARTS == 2 ? a.scale_b[col] : RowScale{1.f, 0.f};
+                const float s = __uint_as_float(x[i]) * k.c;
+                if (PASS == Pass::kStats) {
+                  p[i] = on ? s : -INFINITY;
+                  m2 = fmaxf(m2, p[i]);
+                } else if (PASS == Pass::kMax) {
+                  m2 = on ? fmaxf(m2, mul_then_add(s, scale, k.log2_c)) : m2;
+                } else if (PASS == Pass::kRows) {
+                  const float q = on ? exp2_fast(mul_then_add(s, scale, minus_m) + a.up) : 0.f;
+                  l += q;
+                  p[i] = q * k.c;
                 } else {
-                  p[i] = mul_then_add(s, scale, a.col_m[col]);
-                  if (PASS == Pass::kMaxCols) m = fmaxf(m, p[i] + log2f(fabsf(a.col_f[col])));
-                  else p[i] = exp2_fast(p[i]) * (a.col_f[col] * times_up);
+                  const float q = mul_then_add(s, scale, a.col_m[col]);
+                  if (PASS == Pass::kMaxCols) m2 = fmaxf(m2, q + log2f(fabsf(a.col_f[col])));
+                  else p[i] = exp2_fast(q) * (a.col_f[col] * times_up);
                 }
               }
-              if (PASS == Pass::kMaxCols) continue;
+              if (PASS == Pass::kStats) {
+                const float at2 = m2 == -INFINITY ? 0.f : m2 * scale;
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum += exp2_fast(mul_then_add(p[i], scale, -at2));
+                l = fmaf(l, m2 == m ? 1.f : m == -INFINITY ? 0.f : exp2_fast(at - at2), sum);
+                at = at2;
+              }
+              if (PASS == Pass::kMax) at = m2;
+              if (STATS) {
+                m = m2;
+                continue;
+              }
 #pragma unroll
               for (int i = 0; i < 8; ++i) hi[i] = pack16<BF16>(p[2 * i], p[2 * i + 1]);
               if constexpr (PARTS == 2) {
@@ -570,7 +597,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
                 tmem_store8(s_at + 32 * (c >> 1) + 8 * (c & 1), hi);
               }
             }
-            if (PASS != Pass::kMaxCols) tmem_wait_store();
+            if (!STATS) tmem_wait_store();
             fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.s_done + 8 * at_buf);

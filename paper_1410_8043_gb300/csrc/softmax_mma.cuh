@@ -9,9 +9,10 @@ namespace esspt {
 
 // What a pass makes of the scores S = A B^T b / ln 2:
 //   kStats  per row of A the maximum and the sum of 2^(S - maximum)
-//   kMax    per row of A the maximum
+//   kMax    per row of A the maximum (of S c of the columns' RowScale: what the products hold)
 //   kMaxCols  A = W, B = H: the maximum of S + col over B's rows, an item's over all blocks
-//   kRows   A = H, B = W: sum over B's rows of 2^(S - row_max) B, and of 2^(S - row_max)
+//   kRows   A = H, B = W: sum over B's rows of 2^(S - row_max) B, and of 2^(S - row_max);
+//           with RowScale, 2^(S - row_max) c meets the tensor cores, at most one as row_max is kMax's
 //   kCols   A = W, B = H: sum over B's rows t of 2^(S - maximum_t) factor_t B
 enum class Pass { kStats, kMax, kMaxCols, kRows, kCols };
 __host__ __device__ constexpr bool only_scores(Pass pass) {
@@ -71,6 +72,7 @@ __host__ __device__ constexpr MmaShape mma_shape(Pass pass, int32_t D, int parts
 
 struct MmaArgs {
   const char *A, *B;
+  const RowScale *scale_a, *scale_b;  // fp32 rows
   MmaShape s;
   const ManyWords* words;
   int32_t V;
@@ -108,7 +110,8 @@ struct Ranges {
   __host__ __device__ int64_t block_of(int64_t unit) const { return ((unit + 1) * blocks - 1) / units; }
 };
 
-// Scaling of fp32 operands: x 2^shift has its largest value in [2^14, 2^15).
+// Scaling of fp32 operands: x 2^shift has its largest value in [2^14, 2^15), and so has
+// a row of its own scale.
 __device__ __forceinline__ int half_shift_of(uint32_t max_bits) {
   return max_bits == 0u ? 0 : 14 - ((int)(max_bits >> 23) - 127);
 }
