@@ -26,7 +26,13 @@ struct TargetArgs {
   float* q;              // [n, top] out (lists only): the entries' shares, 0 where absent
   float* self;           // [n] out (lists only): sum q log q, or kIgnored
   uint32_t* status;
+  uint8_t* again;        // [n, top] out, or null: whether the row named the entry's item before
 };
+// Lists up to this long have their repeats found by the row's warp, entries 32 by 32 with
+// those before them, which grows with the square of the length; longer ones by the sorted
+// entries, which dh then waits for.  (4001 rows, lists of 64 over 200k items, bf16: calls of
+// 575 and 600 us, for the sort runs in the gaps between the passes.)
+constexpr int kAgainByWarp = 256;
 constexpr float kIgnored = 3.0e38f;  // (sum q log q is never positive)
 
 struct SoftmaxArgs {
@@ -83,6 +89,7 @@ struct ManyScratch {
   float2* stat;              // partial statistics and
   float* out;                // partial gradients by slot (Ranges, softmax_mma.cuh)
   uint32_t *key[2], *val[2]; // [n * top] entries by item
+  uint8_t* again;            // [n * top] TargetArgs (lists of 16-bit rows)
   int32_t* tile_first;       // [tiles of W + 1] first entry of a tile's items
   float* run_sum[2];         // [n * top / kRun (^2) + 1][D] sums over whole runs of one item
   void* sort_tmp;

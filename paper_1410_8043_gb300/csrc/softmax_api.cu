@@ -11,7 +11,7 @@ namespace {
 
 struct Carve {
   size_t status, q, self, scores, part, stat, dh;
-  size_t words, act, pos, units_h, units_w, scale_h, scale_w, row_max, row_sum, score, col, col_top, col_m, col_f, item_top, slot_stat, out, key[2], val[2], tile_first, run_sum[2], sort;
+  size_t words, act, pos, units_h, units_w, scale_h, scale_w, row_max, row_sum, score, col, col_top, col_m, col_f, item_top, slot_stat, out, key[2], val[2], again, tile_first, run_sum[2], sort;
   size_t sort_bytes, total;
 };
 
@@ -107,6 +107,7 @@ Carve carve(const esspt_softmax_config& c) {
     k.item_top = take(back * V * sizeof(uint32_t));
     k.out = take(z.out);
     for (int i = 0; i < 2; ++i) k.key[i] = take(entries), k.val[i] = take(entries);
+    k.again = take(c.dtype != ESSPT_F32 && c.max_top > 1 ? back * n * c.max_top : 0);
     k.tile_first = take(back * ((V + 127) / 128 + 1) * sizeof(int32_t));
     for (int i = 0; i < 2; ++i) k.run_sum[i] = take(z.run_sum[i]);
     k.sort = take(z.sort);
@@ -141,7 +142,9 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   a.h = h, a.w = w, a.h_stride = h_stride, a.w_stride = w_stride, a.n = n;
   a.V = (int32_t)c.n_items, a.D = c.width, a.dtype = c.dtype;
   a.target = TargetArgs{ids, logits, top, n, a.V, b, reinterpret_cast<float*>(sm->base + k.q),
-                        reinterpret_cast<float*>(sm->base + k.self), reinterpret_cast<uint32_t*>(sm->base + k.status)};
+                        reinterpret_cast<float*>(sm->base + k.self), reinterpret_cast<uint32_t*>(sm->base + k.status), nullptr};
+  if (c.dtype != ESSPT_F32 && grad_w && logits && top <= kAgainByWarp && n > kFewRows)
+    a.target.again = reinterpret_cast<uint8_t*>(sm->base + k.again);
   a.weight = weight, a.b = b, a.loss = loss, a.lse = lse, a.grad_h = grad_h, a.grad_w = grad_w;
   a.st = sm->st, a.sms = sm->sms;
   if (logits) SOFTMAX_CUDA(sm, launch_targets(a.target, a.st));
@@ -166,6 +169,7 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   s.out = static_cast<float*>(at(k.out));
   for (int i = 0; i < 2; ++i)
     s.key[i] = static_cast<uint32_t*>(at(k.key[i])), s.val[i] = static_cast<uint32_t*>(at(k.val[i]));
+  s.again = static_cast<uint8_t*>(at(k.again));
   s.tile_first = static_cast<int32_t*>(at(k.tile_first));
   for (int i = 0; i < 2; ++i) s.run_sum[i] = static_cast<float*>(at(k.run_sum[i]));
   s.sort_tmp = at(k.sort), s.sort_bytes = k.sort_bytes;

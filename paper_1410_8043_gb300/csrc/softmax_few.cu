@@ -52,14 +52,24 @@ __global__ void targets_kernel(TargetArgs a) {
   l = warp_sum(l);
   const float log2_l = log2f(l);
   float self = 0.f;
-  for (int k = lane; k < a.top; k += 32) {
+  float* shares = a.q + t * a.top;
+  for (int k0 = 0; k0 < a.top; k0 += 32) {
+    const int k = k0 + lane;
     float q = 0.f;
-    if (present && (uint32_t)ids[k] < (uint32_t)a.V) {
+    if (k < a.top && present && (uint32_t)ids[k] < (uint32_t)a.V) {
       const float d = (z[k] - m) * scale;
       q = exp2f(d) / l;
       if (q != 0.f) self += q * (d - log2_l);  // (NaN takes part)
     }
-    a.q[t * a.top + k] = q;
+    if (k < a.top) shares[k] = q;
+    if (!a.again) continue;
+    const int32_t id = q != 0.f ? ids[k] : -1;
+    bool again = (__match_any_sync(0xffffffffu, id) & ((1u << lane) - 1u)) != 0u;
+    for (int j0 = 0; j0 < k0; j0 += 32) {
+      const int32_t before = shares[j0 + lane] != 0.f ? ids[j0 + lane] : -1;
+      for (int j = 0; j < 32; ++j) again |= __shfl_sync(0xffffffffu, before, j) == id;
+    }
+    if (k < a.top) a.again[t * a.top + k] = again && id >= 0;
   }
   self = warp_sum(self);
   if (lane == 0) a.self[t] = present ? self * kLn2 : kIgnored;

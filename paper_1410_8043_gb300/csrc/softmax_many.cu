@@ -392,7 +392,8 @@ __device__ __forceinline__ void add_slots(const Many& f, int64_t rows_a, int64_t
 // is small beside p, and that rounding would be most of it (p = 0.99, q = 1: 0.004 of
 // 0.01); other items' p are off by their own half-unit only.  (The score here and the
 // tensor core's differ in their last bits, so now and then p rounds the other way there;
-// past kHuge they have nothing in common, but there p is zero or one.)
+// past kHuge they have nothing in common, but there p is zero or one.)  Of a list that
+// names an item more than once the first entry has it: p was rounded once.
 template <typename T>
 __device__ __forceinline__ float rounded_off(float p) {
   return sizeof(T) == 4 ? 0.f : p - to_float(from_float<T>(p));
@@ -460,7 +461,7 @@ __global__ void __launch_bounds__(256) grad_h_kernel(Many f) {
       const int64_t entry = t * a.target.top + k0 + lane;
       const int32_t lane_id = lane < count ? a.target.ids[entry] : -1;
       float c = lane >= count ? 0.f : a.target.logits ? -a.target.q[entry] : -1.f;
-      if (sizeof(T) == 2 && c != 0.f && fabsf(m) <= kHuge) c += ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - m + up)) * inv, -shift);
+      if (sizeof(T) == 2 && c != 0.f && fabsf(m) <= kHuge && !(a.target.top > 1 && f.s.again[entry])) c += ldexpf(rounded_off<T>(exp2_fast(f.s.score[entry] - m + up)) * inv, -shift);
       const unsigned share = __ballot_sync(0xffffffffu, c != 0.f);
 #pragma unroll 4
       for (int i = 0; i < count; ++i) {
@@ -488,6 +489,18 @@ __global__ void entries_kernel(Many f) {
   const bool share = id < (uint32_t)a.V && (!a.logits || a.q[i] != 0.f);
   f.s.key[0][i] = share ? id : (uint32_t)a.V;
   f.s.val[0][i] = (uint32_t)i;
+}
+
+// Whether the row of a sorted entry has named its item before.  The sort keeps the entries'
+// order, so that a row's entries of one item lie side by side.
+__device__ __forceinline__ bool named_again(const uint32_t* key, const uint32_t* val, int64_t i, uint32_t top) {
+  return i > 0 && key[i - 1] == key[i] && val[i - 1] / top == val[i] / top;
+}
+__global__ void again_kernel(Many f, const uint32_t* key, const uint32_t* val) {
+  const uint32_t top = (uint32_t)f.a.target.top;
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= f.a.n * top) return;
+  f.s.again[val[i]] = named_again(key, val, i, top);
 }
 
 // First entry of every tile of 128 items.
@@ -522,7 +535,7 @@ __global__ void factors_kernel(Many f, const uint32_t* key, const uint32_t* val,
   const int32_t t = (int32_t)(entry / (uint32_t)a.target.top);
   const float q = a.target.logits ? a.target.q[entry] : 1.f;
   float g = a.weight ? q * a.weight[t] : q;
-  if (sizeof(T) == 2 && fabsf(f.s.row_max[f.s.pos[t]]) <= kHuge) {
+  if (sizeof(T) == 2 && fabsf(f.s.row_max[f.s.pos[t]]) <= kHuge && !named_again(key, val, i, (uint32_t)a.target.top)) {
     const int shift = item_shift<T>(f, key[i]);
     g -= ldexpf(rounded_off<T>(col_probability(f, f.s.pos[t], f.s.score[entry], (float)-shift)), shift);
   }
@@ -718,6 +731,8 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   cudaError_t e = cudaMemsetAsync(s.words, 0, sizeof(ManyWords), a.st);
   if (e != cudaSuccess) return e;
   // The targets by item, on the handle's second stream beside what follows.
+  const bool join_early = sizeof(T) == 2 && a.target.top > 1 && !a.target.again;  // (dh asks for repeats)
+  auto join = [&] { return cudaStreamWaitEvent(a.st, s.join, 0); };
   const int64_t entries = a.n * a.target.top, tiles = ((int64_t)a.V + 127) / 128;
   cub::DoubleBuffer<uint32_t> key(s.key[0], s.key[1]), val(s.val[0], s.val[1]);
   // (The sort leaves one of its buffers of each pair free.)
@@ -742,6 +757,8 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
       return e;
     tile_first_kernel<<<(unsigned)(tiles / 256 + 1), 256, 0, s.side>>>(f, key.Current());
     if (sizeof(T) == 4) launch_runs(s.side);
+    else if (join_early)
+      again_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, s.side>>>(f, key.Current(), val.Current());
     if ((e = cudaEventRecord(s.join, s.side)) != cudaSuccess) return e;
   }
   compact_kernel<<<(unsigned)((a.n + 1023) / 1024), 1024, 0, a.st>>>(f);
@@ -780,7 +797,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
     if (err != cudaSuccess) return err;
     loss_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
     if (!grads) return cudaGetLastError();
-    if ((err = rows(false, if_redo)) != cudaSuccess) return err;
+    if ((err = rows(false, if_redo)) != cudaSuccess || (join_early && (err = join()) != cudaSuccess)) return err;
     grad_h_kernel<T, VEC, false><<<dim3(by_row, col_chunks), 256, 0, a.st>>>(f);
     return cudaGetLastError();
   };
@@ -793,7 +810,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
     f.sample = sampled ? (int32_t)(128 * (n_w / 16)) : a.V;
     if ((e = stats(Pass::kMax, f.sample, 0)) != cudaSuccess) return e;
     reference_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
-    if ((e = rows(true, 0)) != cudaSuccess) return e;
+    if ((e = rows(true, 0)) != cudaSuccess || (join_early && (e = join()) != cudaSuccess)) return e;
     grad_h_kernel<T, VEC, true><<<dim3(by_row, col_chunks), 256, 0, a.st>>>(f);
     if (sampled && (e = exact(1)) != cudaSuccess) return e;
   } else if ((e = exact(0)) != cudaSuccess) {
@@ -802,7 +819,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   if (!grads) return cudaSuccess;
   m.if_redo = f.if_redo = 0;
 
-  if ((e = cudaStreamWaitEvent(a.st, s.join, 0)) != cudaSuccess) return e;
+  if (!join_early && (e = join()) != cudaSuccess) return e;
   m.A = s.units_w, m.B = s.units_h, m.scale_a = s.scale_w, m.scale_b = s.scale_h, m.item_top = s.item_top;
   if (!kBf16) {
     m.s = stats_shape, m.run = INT32_MAX, m.if_apart = kParts == 1, m.col = kParts == 2 ? s.col_top : s.col;
