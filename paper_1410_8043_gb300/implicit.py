@@ -18,6 +18,7 @@ The output is one JSON object per reported clock, one line each.
 from __future__ import annotations
 
 import argparse
+import contextlib
 import json
 import sys
 
@@ -28,20 +29,50 @@ from . import esspt
 
 
 class Trainer:
-    """One model on a table: `n_users` + `n_items` rows of width K."""
+    """One model on a table: `n_users` + `n_items` rows of width K.
+
+    Everything runs on the table's stream (`stream`, default: the current one at
+    construction).  A call from another current stream comes after the work queued
+    there, and that stream's later work after the call.
+    """
 
     def __init__(self, n_users: int, n_items: int, K: int, P: int, s: int, batch: int, model: str = "ssp", seed: int = 1,
                  max_top: int = 1, init: float = 0.1, stream=None):
-        self.table = esspt.Table(n_users + n_items, K, P, s, model=model, stream=stream)
-        self.head = esspt.SoftmaxHead(batch, n_items, K, max_top=max_top, stream=stream)
-        rng = np.random.default_rng(seed)
-        self.table.table_init(rng.standard_normal((n_users + n_items, K), dtype=np.float32) * np.float32(init))
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
         self.n_users, self.P = n_users, P
-        self.items = torch.arange(n_users, n_users + n_items, dtype=torch.int32, device=self.table.device)
+        rng = np.random.default_rng(seed)
+        with self._in_order():
+            self.table = esspt.Table(n_users + n_items, K, P, s, model=model)
+            self.head = esspt.SoftmaxHead(batch, n_items, K, max_top=max_top)
+            self.table.table_init(rng.standard_normal((n_users + n_items, K), dtype=np.float32) * np.float32(init))
+            self.items = torch.arange(n_users, n_users + n_items, dtype=torch.int32, device=self.table.device)
+
+    @contextlib.contextmanager
+    def _in_order(self):
+        """On the table's stream, between what the current one has queued and what comes next."""
+        current = torch.cuda.current_stream(self.stream.device)
+        if current == self.stream:
+            yield lambda x: x
+            return
+        self.stream.wait_stream(current)
+
+        def hand_over(x):  # memory of one stream's, used by another
+            x.record_stream(current)
+            return x
+
+        try:
+            with torch.cuda.stream(self.stream):
+                yield hand_over
+        finally:
+            current.wait_stream(self.stream)
+
+    def _rows(self, worker: int, users):
+        return self.table.get(worker, users)[0], self.table.get(worker, self.items)[0]
 
     def rows(self, worker: int, users):
         """The rows of `users` and of all items, at the worker's read version."""
-        return self.table.get(worker, users)[0], self.table.get(worker, self.items)[0]
+        with self._in_order() as hand_over:
+            return tuple(hand_over(x) for x in self._rows(worker, users))
 
     def _push(self, worker: int, users, r, eta: float):
         self.table.inc(worker, users, r.grad_h.mul_(-eta))
@@ -50,13 +81,15 @@ class Trainer:
 
     def learn(self, worker: int, users, picks, eta: float):
         """One worker's part of a clock: steps of size eta down the sum of its batch's losses."""
-        h, w = self.rows(worker, users)
-        return self._push(worker, users, self.head.loss(h, w, picks), eta)
+        with self._in_order() as hand_over:
+            h, w = self._rows(worker, users)
+            return hand_over(self._push(worker, users, self.head.loss(h, w, picks), eta))
 
     def learn_from(self, worker: int, users, ids, logits, eta: float, inv_temperature: float = 1.0):
         """The same towards a teacher's top logits of the batch's users."""
-        h, w = self.rows(worker, users)
-        return self._push(worker, users, self.head.distill(h, w, ids, logits, inv_temperature=inv_temperature), eta)
+        with self._in_order() as hand_over:
+            h, w = self._rows(worker, users)
+            return hand_over(self._push(worker, users, self.head.distill(h, w, ids, logits, inv_temperature=inv_temperature), eta))
 
     def close(self):
         self.head.poll()
