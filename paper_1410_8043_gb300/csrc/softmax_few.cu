@@ -25,10 +25,6 @@ __global__ void targets_kernel(TargetArgs a) {
   const int lane = threadIdx.x & 31;
   if (t >= a.n) return;
   const int32_t* ids = a.ids + t * a.top;
-  if (!a.logits) {
-    if (lane == 0 && ids[0] >= a.V) atomicOr(a.status, kErrTarget);
-    return;
-  }
   const float* z = a.logits + t * a.top;
   const float scale = a.b * kLog2e;
   float m = -INFINITY, l = 0.f;
