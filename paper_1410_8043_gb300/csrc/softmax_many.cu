@@ -33,6 +33,7 @@ struct Many {
   int32_t sample;  // rows of W that the rows' references are taken over, 0: all (exact maxima)
   float up;        // probabilities of the rows pass are taken 2^up times as large
   int if_redo;     // only where words->redo is set
+  int high_tiles;  // tiles of the pass over high halves where that may have run, else 0
 };
 
 __device__ __forceinline__ uint32_t finite_bits(float x) {
@@ -145,25 +146,37 @@ __global__ void __launch_bounds__(256) units_f32_kernel(Many f, bool is_h) {
   const int shift = half_shift_of(max_bits);
   const int64_t padded = (rows + 127) / 128 * 128;
   bool any = false;
+  float norm = 0.f;
   for (int64_t r = (int64_t)blockIdx.x * 32 + threadIdx.x / 8; r < padded; r += (int64_t)gridDim.x * 32) {
     const float* row = x + (r >= rows ? 0 : is_h ? (int64_t)f.s.act[r] : r) * stride;
     const int32_t D = r < rows ? a.D : 0;
     float kept[kKept][8];
     uint32_t top = 0;
+    float squares = 0.f;
+    auto look = [&](const float (&v)[8]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        top = max(top, finite_bits(v[e]));
+        const float s = times_pow2(v[e], shift);
+        squares = fmaf(s, s, squares);
+      }
+    };
 #pragma unroll
     for (int kc = 0; kc < kKept; ++kc) {
       load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, kept[kc]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, finite_bits(kept[kc][e]));
+      look(kept[kc]);
     }
     for (int32_t kc = kKept; kc < nk; ++kc) {
       float v[8];
       load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, finite_bits(v[e]));
+      look(v);
     }
 #pragma unroll
-    for (int off = 4; off > 0; off >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+    for (int off = 4; off > 0; off >>= 1) {
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+      squares += __shfl_xor_sync(0xffffffffu, squares, off);
+    }
+    norm = fmaxf(norm, squares);  // (a row with NaN has no share in it, one with an infinity makes it infinite)
     int own = top == 0u ? 0 : (int)(max_bits >> 23) - (int)(top >> 23);
     own = own <= kApart ? 0 : min(own, kMost);
     any |= own != 0;
@@ -192,6 +205,10 @@ __global__ void __launch_bounds__(256) units_f32_kernel(Many f, bool is_h) {
       put(kc, v);
     }
   }
+  // (Only a larger one goes to the word that all blocks share.)
+  const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(norm));
+  uint32_t* to = is_h ? &f.s.words->norm_h : &f.s.words->norm_w;
+  if ((threadIdx.x & 31) == 0 && most > *(volatile uint32_t*)to) atomicMax(to, most);
   if (__any_sync(0xffffffffu, any) && (threadIdx.x & 31) == 0) (is_h ? f.s.words->spread_h : f.s.words->spread_w) = 1u;
 }
 
@@ -235,12 +252,12 @@ __device__ __forceinline__ float col_probability(const Many& f, int64_t pos, flo
 }
 
 // A warp's row: the maximum and sum of its partial statistics over W's first `items` rows.
-__device__ __forceinline__ void merge_slots(const Many& f, int64_t pos, int64_t items, float& m, float& l) {
+__device__ __forceinline__ void merge_slots(const Many& f, int64_t pos, int64_t items, int tiles, float& m, float& l) {
   const int64_t rows = f.s.words->rows;
-  const Ranges r(rows, items, f.shape.tiles, f.blocks);
-  const int64_t g = pos / (128 * f.shape.tiles);
-  const int tile = (int)(pos / 128 - g * f.shape.tiles), row = (int)(pos & 127);
-  const bool two = f.shape.tiles == 2 && (g * 2 + 1) * 128 < rows;  // half of the slot per tile, else all per row
+  const Ranges r(rows, items, tiles, f.blocks);
+  const int64_t g = pos / (128 * tiles);
+  const int tile = (int)(pos / 128 - g * tiles), row = (int)(pos & 127);
+  const bool two = tiles == 2 && (g * 2 + 1) * 128 < rows;  // half of the slot per tile, else all per row
   const int64_t i0 = r.block_of(g * r.n_b), i1 = r.block_of((g + 1) * r.n_b - 1);
   m = -INFINITY, l = 0.f;
   for (int64_t i = 4 * i0 + (threadIdx.x & 31); i < 4 * i1 + 4; i += 32) {
@@ -333,7 +350,7 @@ __global__ void __launch_bounds__(256) loss_kernel(Many f) {
     return;
   }
   float m, l, loss2 = 0.f;
-  merge_slots(f, pos, a.V, m, l);
+  merge_slots(f, pos, a.V, f.shape.tiles, m, l);
   const float lse2 = m + log2f(l);
   target_scores<T, VEC>(a, t, [&](int k, float q, float s) {
     loss2 += q * (lse2 - s);
@@ -359,7 +376,7 @@ __global__ void __launch_bounds__(256) reference_kernel(Many f) {
   const int64_t pos = f.s.pos[t];
   if (pos < 0) return;
   float m, l;
-  merge_slots(f, pos, f.sample, m, l);
+  merge_slots(f, pos, f.sample, f.high_tiles != 0 && high_halves_do(*f.s.words, a.b) ? f.high_tiles : f.shape.tiles, m, l);
   target_scores<T, VEC>(a, t, [&](int k, float q, float s) {
     if (f.sample < a.V) m = fmaxf(m, s);
     f.s.score[t * a.target.top + k] = s;
@@ -726,7 +743,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   const bool grads = a.grad_h != nullptr;
   const unsigned by_row = (unsigned)((a.n + 7) / 8), col_chunks = (unsigned)((a.D + 32 * VEC - 1) / (32 * VEC));
-  Many f{a, s, mma_shape(Pass::kStats, a.D, kParts), a.sms, (a.D + 15) / 16 * 16, kParts, 0, 0.f, 0};
+  Many f{a, s, mma_shape(Pass::kStats, a.D, kParts), a.sms, (a.D + 15) / 16 * 16, kParts, 0, 0.f, 0, 0};
   if (!grads) f.s.col = nullptr;
   cudaError_t e = cudaMemsetAsync(s.words, 0, sizeof(ManyWords), a.st);
   if (e != cudaSuccess) return e;
@@ -772,17 +789,33 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   MmaArgs m{};
   m.A = s.units_h, m.B = s.units_w, m.scale_a = s.scale_h, m.scale_b = s.scale_w, m.words = s.words, m.V = a.V, m.b = a.b;
   m.row_max = s.row_max, m.col = s.col, m.col_m = s.col_m, m.col_f = s.col_f, m.stat = s.stat, m.out = s.out, m.ld = f.ld;
-  m.status = a.target.status;
+  m.status = a.target.status, m.stored = kParts;
   // Tiles between additions in fp32.  4096 x 18k, K = 100, lists of 32: dh is 1.0e-6 off
   // with 32 tiles, 5.8e-7 with 16, 3.4e-7 with 8 (7.5e-7 by fp32 products of whole
   // matrices); the call takes as long with any of the three, to 1%.  Where the small
   // products of halves have no sums of their own, half as many tiles.
   const MmaShape stats_shape = mma_shape(Pass::kStats, a.D, kParts), rows_shape = mma_shape(Pass::kRows, a.D, kParts);
   const int out_chunks = (a.D + 255) / 256, run_tiles = kParts == 1 ? 128 : rows_shape.cross ? 16 : 8;
+  // Maxima, of large problems of fp32 rows by high halves where that does.
+  const int64_t n_w = ((int64_t)a.V + 127) / 128;
+  const bool large = n_w >= 32 && (a.n + 127) / 128 * n_w >= 24ll * a.sms;
+  const MmaShape high_shape = mma_shape(Pass::kMax, a.D, 1);
+  auto maxima = [&](Pass pass) {
+    m.run = INT32_MAX;
+    if (kParts == 2 && large) {
+      m.s = high_shape, m.if_high = 1;
+      const cudaError_t err = launch_mma(pass, false, 1, m, a.sms, 1, a.st);
+      if (err != cudaSuccess) return err;
+      m.if_high = -1;
+    }
+    m.s = stats_shape;
+    return launch_mma(pass, kBf16, kParts, m, a.sms, 1, a.st);
+  };
+  if (kParts == 2 && large) f.high_tiles = high_shape.tiles;
   // Maxima (and sums) over W's first `items` rows, and what is made of them.
   auto stats = [&](Pass pass, int32_t items, int if_redo) {
     f.shape = m.s = stats_shape, f.if_redo = m.if_redo = if_redo, m.V = items, m.run = INT32_MAX;
-    const cudaError_t err = launch_mma(pass, kBf16, kParts, m, a.sms, 1, a.st);
+    const cudaError_t err = pass == Pass::kMax ? maxima(pass) : launch_mma(pass, kBf16, kParts, m, a.sms, 1, a.st);
     m.V = a.V;
     return err;
   };
@@ -804,8 +837,7 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   // A pass over all scores of bf16 rows for their maxima alone is a fifth of the work.
   // Where it is more than that of the launches that stand by (about 10 us), references
   // from a sixteenth of W do, and the exact passes run only if one of them was too low.
-  const int64_t n_w = ((int64_t)a.V + 127) / 128;
-  const bool sampled = kBf16 && n_w >= 32 && (a.n + 127) / 128 * n_w >= 24ll * a.sms;
+  const bool sampled = kBf16 && large;
   if (grads && (sampled || !kBf16)) {
     f.sample = sampled ? (int32_t)(128 * (n_w / 16)) : a.V;
     if ((e = stats(Pass::kMax, f.sample, 0)) != cudaSuccess) return e;
@@ -822,8 +854,8 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   if (!join_early && (e = join()) != cudaSuccess) return e;
   m.A = s.units_w, m.B = s.units_h, m.scale_a = s.scale_w, m.scale_b = s.scale_h, m.item_top = s.item_top;
   if (!kBf16) {
-    m.s = stats_shape, m.run = INT32_MAX, m.if_apart = kParts == 1, m.col = kParts == 2 ? s.col_top : s.col;
-    if ((e = launch_mma(Pass::kMaxCols, false, kParts, m, a.sms, 1, a.st)) != cudaSuccess) return e;
+    m.if_apart = kParts == 1, m.col = kParts == 2 ? s.col_top : s.col;
+    if ((e = maxima(Pass::kMaxCols)) != cudaSuccess) return e;
     m.s = rows_shape, m.run = run_tiles, m.col = s.col;
   }
   if (sizeof(T) == 2) launch_runs(a.st);  // (wants the rows' sums and the items' references)

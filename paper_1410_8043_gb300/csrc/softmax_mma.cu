@@ -361,6 +361,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   const Ranges ranges(rows_a, rows_b, sh.tiles, gridDim.x);
   if (blockIdx.x >= ranges.blocks || (a.if_redo && a.words->redo == 0u)) return;
   if (PASS == Pass::kMaxCols && a.if_apart && !weights_apart(*a.words)) return;
+  if ((PASS == Pass::kMax || PASS == Pass::kMaxCols) && a.if_high != 0 && high_halves_do(*a.words, a.b) != (a.if_high > 0)) return;
 
   const uint32_t base = (smem_addr(smem) + 1023u) & ~1023u;
   const uint32_t a_base = base, b_base = base + (sh.res ? sh.tiles * sh.nk * PARTS : 0) * kUnitBytes;
@@ -393,7 +394,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   Run g;
   // A group's last tile may lie outside: then the groups of warps share the first.
   auto tiles_of = [&](const Run& s) { return sh.tiles == 2 && (s.group * 2 + 1) * 128 < rows_a ? 2 : 1; };
-  const int64_t tile_bytes = (int64_t)sh.nk * PARTS * kUnitBytes;
+  const int64_t tile_bytes = (int64_t)sh.nk * a.stored * kUnitBytes;  // from a tile to the next
 
   if (warp == 0) {
     // ---- loads ----
@@ -444,8 +445,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
           a_phase ^= 1;
           if (*dead) break;
           ++segs;
-          mbar_expect(bar.a_full, (uint32_t)(nt * tile_bytes));
-          bulk_load(a_base, from_a, (uint32_t)(nt * tile_bytes), bar.a_full);
+          const uint32_t kept = sh.nk * PARTS * kUnitBytes;
+          mbar_expect(bar.a_full, nt * kept);
+          for (int i = 0; i < nt; ++i) bulk_load(a_base + i * kept, from_a + i * tile_bytes, kept, bar.a_full);
         }
         for (int32_t j = 0; j < g.len; ++j) {
           scores_units(g.first + j, from_a);
@@ -490,7 +492,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
     const int pair = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3;
     const int row = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-    const int shift_h = PARTS == 2 ? half_shift_of(a.words->max_h) : 0, shift_w = PARTS == 2 ? half_shift_of(a.words->max_w) : 0;
+    const int shift_h = half_shift_of(a.words->max_h), shift_w = half_shift_of(a.words->max_w);  // (16-bit rows: 0)
     const float scale_all = ldexpf(a.b * kLog2e, -(shift_h + shift_w));
     float scale = 0.f;  // of this thread's row
     const bool negative = PASS == Pass::kCols && a.words->negative != 0u;

@@ -85,6 +85,8 @@ struct MmaArgs {
   const float *col_m, *col_f;  // kMaxCols, kCols: -maximum and factor by themselves
   uint32_t* item_top;    // kMaxCols out, kCols: ManyScratch
   int if_apart;          // only where weights_apart
+  int stored;            // parts of A and B in memory, of which the kernel's come first
+  int if_high;           // 1: only where high_halves_do, -1: only where not
   float2* stat;          // kStats, kMax out: [slot][4][128], by group and half of the columns
   float* sums;           // kRows out: sums of the probabilities, likewise, or null
   float up;              // kRows: probabilities are taken 2^up times as large
@@ -118,6 +120,15 @@ __device__ __forceinline__ int half_shift_of(uint32_t max_bits) {
 __device__ __forceinline__ float times_pow2(float x, int e) {
   const int e1 = e / 2;
   return x * __int_as_float((e1 + 127) << 23) * __int_as_float((e - e1 + 127) << 23);
+}
+// Maxima only decide powers of two that probabilities are taken times, with room for a
+// factor of two.  The high halves give them where what they leave out of a score, 2^-10 of
+// |h| |w| at most, is below one in units of log 2; a third of the products then.  (2048 x
+// 1M, K = 64: a call of 3.66 ms with exact maxima.)
+__device__ __forceinline__ bool high_halves_do(const ManyWords& w, float b) {
+  const float most = sqrtf(__uint_as_float(w.norm_h)) * sqrtf(__uint_as_float(w.norm_w));
+  return w.spread_h == 0u && w.spread_w == 0u &&
+         ldexpf(most * (b * kLog2e), -(half_shift_of(w.max_h) + half_shift_of(w.max_w)) - 10) < 1.f;
 }
 // Whether the rows' weights differ by more than 2^8.
 __device__ __forceinline__ bool weights_apart(const ManyWords& w) {
