@@ -74,6 +74,7 @@ struct ManyWords {  // (device) what a call's kernels tell each other
   uint32_t huge;                      // a row's reference is past kHuge
   uint32_t spread_h, spread_w;        // whether any row has a power of its own
   uint32_t norm_h, norm_w;            // (fp32) largest sum of a row's squares, by the matrix's power
+  uint32_t low;                       // (fp32) an item's weight p are all below kLow of the largest weight, or may be
 };
 struct RowScale {  // units hold the row 1 / c times as large as the matrix's power alone says
   float c, log2_c;

@@ -8,7 +8,7 @@
 //   rows       sum p w (and sum p), then dh and the loss
 //   entries    targets sorted by item on a second stream, sums over long runs of one item
 //   cols       fp32 rows (and fp16 rows of weights far apart): the largest weight p of every
-//              item; sum weight p h, then dw
+//              item, in large problems where a tile of rows says so; sum weight p h, then dw
 //
 // The kernels here are bound by bytes or by latency: 2048 x 1M, K = 64, fp32, GB300:
 // max 43 us (256 MB, 6.0 TB/s), units 72 (512 MB, 7.1 TB/s), dw 118 (512 MB, 4.3 TB/s,
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(1024) compact_kernel(Many f) {
     f.s.pos[t] = kept ? base : -1;
     if (kept) f.s.act[base] = (int32_t)t;
     if (!a.target.logits && a.target.ids[t] >= a.V) atomicOr(a.target.status, kErrTarget);
-    if (t == a.n - 1) f.s.words->rows = base + kept;
+    if (t == a.n - 1) f.s.words->rows = base + kept, f.s.words->low = f.high_tiles == 0;
   }
   if (a.weight && __any_sync(0xffffffffu, kept && a.weight[t] < 0.f) && lane == 0) f.s.words->negative = 1u;
   if (a.weight) {
@@ -130,12 +130,15 @@ __device__ __forceinline__ void load_piece(const T* row, int32_t d, int32_t D, f
 }
 
 // fp32 rows to units of halves, eight lanes to a row: its largest value first, which
-// decides whether the row takes a power of two of its own (in registers up to two units,
-// else read again).  The rows after the last, up to the end of its tile, and the values
+// decides whether the row takes a power of two of its own.  Rows of one or two units (NK)
+// are kept in registers, several at once, others (0) read again.  (1M x 64: 71 us.  The rows after the last, up to the end of its tile, and the values
 // after a row's last are zero.
-template <int VEC>
-__global__ void __launch_bounds__(256) units_f32_kernel(Many f, bool is_h) {
-  constexpr int kKept = 2, kApart = 8, kMost = 80;  // (2^80: sums of p stay in range)
+template <int VEC, int NK>
+__global__ void __launch_bounds__(256) units_f32_kernel(Many f, unsigned w_blocks) {
+  const bool is_h = blockIdx.x >= w_blocks;
+  const int64_t block = blockIdx.x - (is_h ? w_blocks : 0u), blocks = is_h ? gridDim.x - w_blocks : w_blocks;
+  constexpr int kKept = NK == 0 ? 1 : NK, U = NK == 0 ? 1 : 4 / NK;
+  constexpr int kApart = 8, kMost = 80;  // (2^80: sums of p stay in range)
   const SoftmaxArgs& a = f.a;
   const float* x = static_cast<const float*>(is_h ? a.h : a.w);
   const int64_t rows = is_h ? f.s.words->rows : a.V, stride = is_h ? a.h_stride : a.w_stride;
@@ -147,62 +150,73 @@ __global__ void __launch_bounds__(256) units_f32_kernel(Many f, bool is_h) {
   const int64_t padded = (rows + 127) / 128 * 128;
   bool any = false;
   float norm = 0.f;
-  for (int64_t r = (int64_t)blockIdx.x * 32 + threadIdx.x / 8; r < padded; r += (int64_t)gridDim.x * 32) {
-    const float* row = x + (r >= rows ? 0 : is_h ? (int64_t)f.s.act[r] : r) * stride;
-    const int32_t D = r < rows ? a.D : 0;
-    float kept[kKept][8];
-    uint32_t top = 0;
-    float squares = 0.f;
-    auto look = [&](const float (&v)[8]) {
+  const int64_t step = blocks * 32;
+  for (int64_t r0 = block * 32 + threadIdx.x / 8; r0 < padded; r0 += U * step) {
+    float all[U][kKept][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        top = max(top, finite_bits(v[e]));
-        const float s = times_pow2(v[e], shift);
-        squares = fmaf(s, s, squares);
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = r0 + u * step;
+      const float* row = x + (r >= rows ? 0 : is_h ? (int64_t)f.s.act[r] : r) * stride;
+#pragma unroll
+      for (int kc = 0; kc < kKept; ++kc) load_piece<float, VEC>(row, kc * 64 + lane8 * 8, r < rows ? a.D : 0, all[u][kc]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = r0 + u * step;
+      if (r >= padded) break;  // (whole warps: their four rows are of one tile)
+      const float* row = x + (r >= rows ? 0 : is_h ? (int64_t)f.s.act[r] : r) * stride;
+      const int32_t D = r < rows ? a.D : 0;
+      float(&kept)[kKept][8] = all[u];
+      uint32_t top = 0;
+      float squares = 0.f;
+      auto look = [&](const float (&v)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          top = max(top, finite_bits(v[e]));
+          const float s = times_pow2(v[e], shift);
+          squares = fmaf(s, s, squares);
+        }
+      };
+#pragma unroll
+      for (int kc = 0; kc < kKept; ++kc) look(kept[kc]);
+      for (int32_t kc = kKept; kc < nk; ++kc) {
+        float v[8];
+        load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, v);
+        look(v);
       }
-    };
 #pragma unroll
-    for (int kc = 0; kc < kKept; ++kc) {
-      load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, kept[kc]);
-      look(kept[kc]);
-    }
-    for (int32_t kc = kKept; kc < nk; ++kc) {
-      float v[8];
-      load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, v);
-      look(v);
-    }
-#pragma unroll
-    for (int off = 4; off > 0; off >>= 1) {
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
-      squares += __shfl_xor_sync(0xffffffffu, squares, off);
-    }
-    norm = fmaxf(norm, squares);  // (a row with NaN has no share in it, one with an infinity makes it infinite)
-    int own = top == 0u ? 0 : (int)(max_bits >> 23) - (int)(top >> 23);
-    own = own <= kApart ? 0 : min(own, kMost);
-    any |= own != 0;
-    if (lane8 == 0) {
-      scales[r] = RowScale{__int_as_float((127 - own) << 23), -(float)own};
-      if (!is_h && r < rows && f.s.col) f.s.item_top[r] = 0u;
-    }
-    auto put = [&](int32_t kc, const float (&v)[8]) {
-      alignas(16) __half hi[8], lo[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float s = times_pow2(v[e], shift + own);
-        hi[e] = __float2half_rn(s);
-        lo[e] = __float2half_rn(s - __half2float(hi[e]));
+      for (int off = 4; off > 0; off >>= 1) {
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+        squares += __shfl_xor_sync(0xffffffffu, squares, off);
       }
-      char* to = piece_of(units, r, 2, nk, kc, lane8);
-      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
-      *reinterpret_cast<uint4*>(to + nk * (int64_t)kUnitBytes) = *reinterpret_cast<const uint4*>(lo);
-    };
+      norm = fmaxf(norm, squares);  // (a row with NaN has no share in it, one with an infinity makes it infinite)
+      int own = top == 0u ? 0 : (int)(max_bits >> 23) - (int)(top >> 23);
+      own = own <= kApart ? 0 : min(own, kMost);
+      any |= own != 0;
+      if (lane8 == 0) {
+        scales[r] = RowScale{__int_as_float((127 - own) << 23), -(float)own};
+        if (!is_h && r < rows && f.s.col) f.s.item_top[r] = 0u;
+      }
+      auto put = [&](int32_t kc, const float (&v)[8]) {
+        alignas(16) __half hi[8], lo[8];
 #pragma unroll
-    for (int32_t kc = 0; kc < kKept; ++kc)
-      if (kc < nk) put(kc, kept[kc]);
-    for (int32_t kc = kKept; kc < nk; ++kc) {
-      float v[8];
-      load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, v);
-      put(kc, v);
+        for (int e = 0; e < 8; ++e) {
+          const float s = times_pow2(v[e], shift + own);
+          hi[e] = __float2half_rn(s);
+          lo[e] = __float2half_rn(s - __half2float(hi[e]));
+        }
+        char* to = piece_of(units, r, 2, nk, kc, lane8);
+        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
+        *reinterpret_cast<uint4*>(to + nk * (int64_t)kUnitBytes) = *reinterpret_cast<const uint4*>(lo);
+      };
+#pragma unroll
+      for (int32_t kc = 0; kc < kKept; ++kc)
+        put(kc, kept[kc]);
+      for (int32_t kc = kKept; kc < nk; ++kc) {
+        float v[8];
+        load_piece<float, VEC>(row, kc * 64 + lane8 * 8, D, v);
+        put(kc, v);
+      }
     }
   }
   // (Only a larger one goes to the word that all blocks share.)
@@ -214,14 +228,16 @@ __global__ void __launch_bounds__(256) units_f32_kernel(Many f, bool is_h) {
 
 // 16-bit rows to units: a thread makes 16 bytes (8 values) of a row.  Zeros as above.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(256) units_kernel(Many f, bool is_h) {
+__global__ void __launch_bounds__(256) units_kernel(Many f, unsigned w_blocks) {
+  const bool is_h = blockIdx.x >= w_blocks;
+  const int64_t block = blockIdx.x - (is_h ? w_blocks : 0u), blocks = is_h ? gridDim.x - w_blocks : w_blocks;
   const SoftmaxArgs& a = f.a;
   const T* x = static_cast<const T*>(is_h ? a.h : a.w);
   const int64_t rows = is_h ? f.s.words->rows : a.V, stride = is_h ? a.h_stride : a.w_stride;
   char* units = is_h ? f.s.units_h : f.s.units_w;
   const int32_t nk = f.shape.nk, pieces = nk * 8;
   const int64_t total = (rows + 127) / 128 * 128 * pieces;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+  for (int64_t i = block * 256 + threadIdx.x; i < total; i += blocks * 256) {
     const int64_t r = i / pieces;
     const int32_t c = (int32_t)(i - r * pieces);
     if (!is_h && c == 0 && r < rows && f.s.col) f.s.item_top[r] = 0u;
@@ -724,11 +740,25 @@ bool rows_by(int vec, const SoftmaxArgs& a, bool grads) {
 }
 
 template <typename T, int VEC>
-void launch_units(const Many& f, bool is_h) {
-  const int64_t padded = ((is_h ? f.a.n : f.a.V) + 127) / 128 * 128, pieces = padded * (sizeof(T) == 4 ? 8 : f.shape.nk * 8);
-  const int grid = (int)std::min<int64_t>((pieces + 255) / 256, 32ll * f.a.sms);
-  if constexpr (sizeof(T) == 4) units_f32_kernel<VEC><<<grid, 256, 0, f.a.st>>>(f, is_h);
-  else units_kernel<T, VEC><<<grid, 256, 0, f.a.st>>>(f, is_h);
+void launch_units(const Many& f) {  // W's and H's
+  auto padded = [](int64_t rows) { return (rows + 127) / 128 * 128; };
+  if constexpr (sizeof(T) == 4) {
+    // As many blocks as give each row of a thread its turn, or four to an SM.
+    const int each = f.shape.nk == 1 ? 4 : f.shape.nk == 2 ? 2 : 1;
+    auto blocks = [&](int64_t rows) {
+      return (unsigned)std::max(padded(rows) / 32 / each, std::min<int64_t>(padded(rows) / 32, 4ll * f.a.sms));
+    };
+    const unsigned w = blocks(f.a.V), both = w + blocks(f.a.n);
+    if (each == 4) units_f32_kernel<VEC, 1><<<both, 256, 0, f.a.st>>>(f, w);
+    else if (each == 2) units_f32_kernel<VEC, 2><<<both, 256, 0, f.a.st>>>(f, w);
+    else units_f32_kernel<VEC, 0><<<both, 256, 0, f.a.st>>>(f, w);
+  } else {
+    auto blocks = [&](int64_t rows) {
+      return (unsigned)std::min<int64_t>((padded(rows) * f.shape.nk * 8 + 255) / 256, 32ll * f.a.sms);
+    };
+    const unsigned w = blocks(f.a.V);
+    units_kernel<T, VEC><<<w + blocks(f.a.n), 256, 0, f.a.st>>>(f, w);
+  }
 }
 
 int bits_of(uint32_t most) {
@@ -778,18 +808,21 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
       again_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, s.side>>>(f, key.Current(), val.Current());
     if ((e = cudaEventRecord(s.join, s.side)) != cudaSuccess) return e;
   }
+  const int64_t n_w = ((int64_t)a.V + 127) / 128;
+  const bool large = n_w >= 32 && (a.n + 127) / 128 * n_w >= 24ll * a.sms;
+  const MmaShape high_shape = mma_shape(Pass::kMax, a.D, 1);
+  if (kParts == 2 && large) f.high_tiles = high_shape.tiles;
   compact_kernel<<<(unsigned)((a.n + 1023) / 1024), 1024, 0, a.st>>>(f);
   if constexpr (kParts == 2) {
     const int64_t work = std::max((int64_t)a.V, a.n) * a.D / VEC;
     max_kernel<VEC><<<dim3((unsigned)std::min<int64_t>((work + 255) / 256, 8ll * a.sms), 2), 256, 0, a.st>>>(f);
   }
-  launch_units<T, VEC>(f, true);
-  launch_units<T, VEC>(f, false);
+  launch_units<T, VEC>(f);
 
   MmaArgs m{};
   m.A = s.units_h, m.B = s.units_w, m.scale_a = s.scale_h, m.scale_b = s.scale_w, m.words = s.words, m.V = a.V, m.b = a.b;
   m.row_max = s.row_max, m.col = s.col, m.col_m = s.col_m, m.col_f = s.col_f, m.stat = s.stat, m.out = s.out, m.ld = f.ld;
-  m.status = a.target.status, m.stored = kParts;
+  m.status = a.target.status;
   // Tiles between additions in fp32.  4096 x 18k, K = 100, lists of 32: dh is 1.0e-6 off
   // with 32 tiles, 5.8e-7 with 16, 3.4e-7 with 8 (7.5e-7 by fp32 products of whole
   // matrices); the call takes as long with any of the three, to 1%.  Where the small
@@ -797,21 +830,10 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   const MmaShape stats_shape = mma_shape(Pass::kStats, a.D, kParts), rows_shape = mma_shape(Pass::kRows, a.D, kParts);
   const int out_chunks = (a.D + 255) / 256, run_tiles = kParts == 1 ? 128 : rows_shape.cross ? 16 : 8;
   // Maxima, of large problems of fp32 rows by high halves where that does.
-  const int64_t n_w = ((int64_t)a.V + 127) / 128;
-  const bool large = n_w >= 32 && (a.n + 127) / 128 * n_w >= 24ll * a.sms;
-  const MmaShape high_shape = mma_shape(Pass::kMax, a.D, 1);
   auto maxima = [&](Pass pass) {
-    m.run = INT32_MAX;
-    if (kParts == 2 && large) {
-      m.s = high_shape, m.if_high = 1;
-      const cudaError_t err = launch_mma(pass, false, 1, m, a.sms, 1, a.st);
-      if (err != cudaSuccess) return err;
-      m.if_high = -1;
-    }
-    m.s = stats_shape;
+    m.s = stats_shape, m.high = high_shape, m.try_high = kParts == 2 && large, m.run = INT32_MAX;
     return launch_mma(pass, kBf16, kParts, m, a.sms, 1, a.st);
   };
-  if (kParts == 2 && large) f.high_tiles = high_shape.tiles;
   // Maxima (and sums) over W's first `items` rows, and what is made of them.
   auto stats = [&](Pass pass, int32_t items, int if_redo) {
     f.shape = m.s = stats_shape, f.if_redo = m.if_redo = if_redo, m.V = items, m.run = INT32_MAX;
@@ -855,6 +877,11 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
   m.A = s.units_w, m.B = s.units_h, m.scale_a = s.scale_w, m.scale_b = s.scale_h, m.item_top = s.item_top;
   if (!kBf16) {
     m.if_apart = kParts == 1, m.col = kParts == 2 ? s.col_top : s.col;
+    if (kParts == 2 && large) {
+      m.low = &s.words->low;
+      if ((e = maxima(Pass::kMaxCols)) != cudaSuccess) return e;
+      m.low = nullptr, m.if_low = 1;
+    }
     if ((e = maxima(Pass::kMaxCols)) != cudaSuccess) return e;
     m.s = rows_shape, m.run = run_tiles, m.col = s.col;
   }

@@ -347,21 +347,21 @@ __device__ __forceinline__ void mask_scores(uint32_t (&r)[32], int left) {
     if (i >= left) r[i] = 0xff800000u;
 }
 
-template <Pass PASS, bool BF16, int PARTS>
-__global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ MmaArgs a) {
+// PARTS of the STORED parts of the operands, which come first in memory.
+template <Pass PASS, bool BF16, int PARTS, int STORED>
+__device__ __forceinline__ void mma_pass(const MmaArgs& a, const MmaShape& sh) {
   extern __shared__ __align__(1024) char smem[];
   __shared__ uint32_t tmem_at;
   __shared__ uint32_t dead_flag;
   constexpr bool STATS = only_scores(PASS);
   constexpr int kColBytes = PARTS == 2 && PASS == Pass::kCols ? 1024 : 512;  // of a tile's columns
-  const MmaShape sh = a.s;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int64_t rows_h = a.words->rows;
-  const int64_t rows_a = items_first(PASS) ? a.V : rows_h, rows_b = items_first(PASS) ? rows_h : a.V;
+  const bool looking = PASS == Pass::kMaxCols && a.low != nullptr;
+  const int64_t rows_a = items_first(PASS) ? a.V : rows_h, rows_b = !items_first(PASS) ? a.V : looking ? min(rows_h, (int64_t)128) : rows_h;
   const Ranges ranges(rows_a, rows_b, sh.tiles, gridDim.x);
   if (blockIdx.x >= ranges.blocks || (a.if_redo && a.words->redo == 0u)) return;
-  if (PASS == Pass::kMaxCols && a.if_apart && !weights_apart(*a.words)) return;
-  if ((PASS == Pass::kMax || PASS == Pass::kMaxCols) && a.if_high != 0 && high_halves_do(*a.words, a.b) != (a.if_high > 0)) return;
+  if (PASS == Pass::kMaxCols && ((a.if_apart && !weights_apart(*a.words)) || (a.if_low && a.words->low == 0u))) return;
 
   const uint32_t base = (smem_addr(smem) + 1023u) & ~1023u;
   const uint32_t a_base = base, b_base = base + (sh.res ? sh.tiles * sh.nk * PARTS : 0) * kUnitBytes;
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   Run g;
   // A group's last tile may lie outside: then the groups of warps share the first.
   auto tiles_of = [&](const Run& s) { return sh.tiles == 2 && (s.group * 2 + 1) * 128 < rows_a ? 2 : 1; };
-  const int64_t tile_bytes = (int64_t)sh.nk * a.stored * kUnitBytes;  // from a tile to the next
+  const int64_t tile_bytes = (int64_t)sh.nk * STORED * kUnitBytes;  // from a tile to the next
 
   if (warp == 0) {
     // ---- loads ----
@@ -724,7 +724,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
       if (items_first(PASS)) col0 = (col0 + g.len) % col_slots;
       if (PASS == Pass::kMaxCols) {
         const int64_t item = (g.group * sh.tiles + (nt == 2 ? pair : 0)) * 128 + row;
-        if (item < rows_a && m != -INFINITY) atomicMax(a.item_top + item, top_key(m));
+        if (looking) {  // (each half of a tile for itself; a single tile is one pair's alone)
+          if (item < rows_a && jobs > pair && !(m - log2f(__uint_as_float(a.words->max_weight)) >= kLow)) *a.low = 1u;
+        } else if (item < rows_a && m != -INFINITY) {
+          atomicMax(a.item_top + item, top_key(m));
+        }
         continue;
       }
       if (STATS) {
@@ -767,6 +771,17 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_consta
   __syncthreads();
   if (threadIdx.x == 0 && dead_flag) atomicOr(a.status, kErrStuck);
   if (warp == 1) tmem_free(tmem, 512);
+}
+
+template <Pass PASS, bool BF16, int PARTS>
+__global__ void __launch_bounds__(kMmaThreads, 1) mma_kernel(const __grid_constant__ MmaArgs a) {
+  if constexpr (PARTS == 2 && (PASS == Pass::kMax || PASS == Pass::kMaxCols)) {
+    if (a.try_high && high_halves_do(*a.words, a.b)) {
+      mma_pass<PASS, BF16, 1, 2>(a, a.high);
+      return;
+    }
+  }
+  mma_pass<PASS, BF16, PARTS, PARTS>(a, a.s);
 }
 
 template <Pass PASS, bool BF16, int PARTS>

@@ -85,8 +85,10 @@ struct MmaArgs {
   const float *col_m, *col_f;  // kMaxCols, kCols: -maximum and factor by themselves
   uint32_t* item_top;    // kMaxCols out, kCols: ManyScratch
   int if_apart;          // only where weights_apart
-  int stored;            // parts of A and B in memory, of which the kernel's come first
-  int if_high;           // 1: only where high_halves_do, -1: only where not
+  MmaShape high;         // kMax, kMaxCols of fp32 rows: for the high halves alone, where `try_high`
+  int try_high;          // and high_halves_do
+  uint32_t* low;         // kMaxCols: over B's first tile alone, to find what words->low says
+  int if_low;            // only where words->low is set
   float2* stat;          // kStats, kMax out: [slot][4][128], by group and half of the columns
   float* sums;           // kRows out: sums of the probabilities, likewise, or null
   float up;              // kRows: probabilities are taken 2^up times as large
@@ -130,6 +132,9 @@ __device__ __forceinline__ bool high_halves_do(const ManyWords& w, float b) {
   return w.spread_h == 0u && w.spread_w == 0u &&
          ldexpf(most * (b * kLog2e), -(half_shift_of(w.max_h) + half_shift_of(w.max_w)) - 10) < 1.f;
 }
+// Log2 of the weight p, relative to the largest weight, that one power of two for all items
+// still serves: halves of p in steps of 2^-39 then are 2^-15 of it.
+constexpr float kLow = -24.f;
 // Whether the rows' weights differ by more than 2^8.
 __device__ __forceinline__ bool weights_apart(const ManyWords& w) {
   return w.max_weight != 0u && (int)(w.max_weight >> 23) - (int)((0x7f800000u - w.min_weight) >> 23) > 8;
@@ -142,12 +147,14 @@ __device__ __forceinline__ uint32_t top_key(float x) {
 // The power of two that an item's terms weight p are multiplied by in the sum over rows.
 // fp32 rows, whose result has fp32's range: by the item's own largest term, for what is
 // left of an item that is nobody's target may be 2^-40 and less of what a target gets.
-// fp16 rows: the result has no such values, so one power for all, by the largest weight,
-// does, unless the weights differ much: then a row of ordinary weight needs its own too.
+// In large problems a tile of rows tells whether any item needs that (`low`; small ones
+// set it), else one power for all does, by the largest weight (2048 x 1M, K = 64: the maxima
+// of all take 320 us of 3190).  fp16 rows: the result has no such values, and that one
+// power does unless the weights differ much, so that ordinary rows' share is small.
 template <bool BF16, int PARTS>
 __device__ __forceinline__ float item_up(const ManyWords& w, const uint32_t* top, int64_t item) {
   if (BF16) return 0.f;
-  if (PARTS == 1 && !weights_apart(w))
+  if (PARTS == 2 ? w.low == 0u : !weights_apart(w))
     return w.max_weight == 0u ? kHalfShift : kHalfShift - 1.f - (float)((int)(w.max_weight >> 23) - 127);
   const uint32_t key = top[item];
   if (key == 0u) return 0.f;
