@@ -110,8 +110,8 @@ cudaError_t launch_many_rows(const SoftmaxArgs& a, const ManyScratch& s);
 
 cudaError_t launch_targets(const TargetArgs& a, cudaStream_t st);
 // Whether a call of n rows goes by scores kept (launch_few_rows).
-bool few_rows(int64_t n, int64_t V, int32_t D, bool grads);
-int few_groups(int64_t max_rows, int64_t V, int32_t D, bool backward);  // most groups of such a call
+bool few_rows(int64_t n, int64_t V, int32_t D, int32_t dtype, bool grads);
+int few_groups(int64_t max_rows, int64_t V, int32_t D, int32_t dtype, bool backward);  // most groups of such a call
 cudaError_t launch_few_rows(const SoftmaxArgs& a, const FewScratch& s);
 
 }  // namespace esspt

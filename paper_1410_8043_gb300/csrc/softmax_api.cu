@@ -82,7 +82,7 @@ Carve carve(const esspt_softmax_config& c) {
   k.status = take(kStatusBytes);
   k.q = take(n * c.max_top * sizeof(float));
   k.self = take(n * sizeof(float));
-  const size_t groups = (size_t)few_groups(c.max_rows, c.n_items, c.width, c.backward != 0);
+  const size_t groups = (size_t)few_groups(c.max_rows, c.n_items, c.width, c.dtype, c.backward != 0);
   const size_t few = groups > (size_t)few_blocks(kMaxSms) ? groups : (size_t)few_blocks(kMaxSms);
   k.scores = take(groups * V * kFewRows * sizeof(float));
   k.part = take(few * kFewRows * sizeof(float2));
@@ -149,7 +149,7 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   a.st = sm->st, a.sms = sm->sms;
   if (logits) SOFTMAX_CUDA(sm, launch_targets(a.target, a.st));
   auto at = [&](size_t offset) { return static_cast<void*>(sm->base + offset); };
-  if (few_rows(n, c.n_items, c.width, grad_w != nullptr)) {
+  if (few_rows(n, c.n_items, c.width, c.dtype, grad_w != nullptr)) {
     const FewScratch s{static_cast<float*>(at(k.scores)), static_cast<float2*>(at(k.part)),
                        static_cast<float*>(at(k.stat)), static_cast<float*>(at(k.dh)),
                        static_cast<uint32_t*>(at(k.status + kDoneAt))};

@@ -550,20 +550,22 @@ cudaError_t run(const SoftmaxArgs& a, const FewScratch& s) {
 int few_blocks(int sms) { return 4 * sms; }
 
 // By what both ways take, in us, fitted to 12 to 128 rows on 1000 to 800k items of 4 to
-// 500 values (fp32 and bf16, with gradients and without), and 2^24 scores kept at most.
-// With gradients, here and by tensor cores: 20k items, K = 64, 128 rows 90 and 108; 200k,
-// K = 64, 24 rows 164 and 213, 48 rows 286 and 215; 9k, K = 256, 128 rows 132 and 120.
-// Forward: 200k, K = 64, 24 rows 41 and 68, 48 rows 71 and 68; 9k, K = 256, 128 rows 37 and 44.
-bool few_rows(int64_t n, int64_t V, int32_t D, bool grads) {
+// 500 values (fp32 and bf16, with gradients and without), the tensor cores' by type, and
+// 2^24 scores kept at most.  Where they part, here and by tensor cores, with gradients:
+// 200k items, K = 64, fp32 42 rows 281 and 252, bf16 25 rows 177 and 171; K = 256, fp32 35
+// rows 662 and 650, bf16 23 rows 430 and 358.  Forward: 200k, K = 64, fp32 48 rows 70 and
+// 70, bf16 32 rows 43 and 43.
+bool few_rows(int64_t n, int64_t V, int32_t D, int32_t dtype, bool grads) {
   if (n <= kFewRows || n > kSmallRows) return n <= kFewRows;
   if (n * V > (1 << 24)) return false;
   const double items = (double)V, scores = n * items;
   const double few = grads ? 34 + items * (1.8e-4 + 3.5e-7 * D) + scores * (6.8e-6 + 2.4e-7 * D) : 10 + scores * (1e-6 + 8e-8 * D);
-  return few <= (grads ? 88 + items * (2e-4 + 6.3e-6 * D) : 36 + items * (5e-5 + 1e-6 * D));
+  const double type = dtype == ESSPT_F32 ? grads ? 1.26 : 1.18 : grads ? 0.9 : 0.85;
+  return few <= type * (grads ? 88 + items * (2e-4 + 6.3e-6 * D) : 36 + items * (5e-5 + 1e-6 * D));
 }
-int few_groups(int64_t max_rows, int64_t V, int32_t D, bool backward) {
+int few_groups(int64_t max_rows, int64_t V, int32_t D, int32_t dtype, bool backward) {
   int64_t n = std::min<int64_t>(max_rows, kSmallRows);
-  while (!few_rows(n, V, D, false) && !(backward && few_rows(n, V, D, true))) --n;
+  while (!few_rows(n, V, D, dtype, false) && !(backward && few_rows(n, V, D, dtype, true))) --n;
   return (int)((n + kFewRows - 1) / kFewRows);
 }
 
