@@ -98,6 +98,19 @@ class Trainer:
         self.table.close()
 
 
+def top_scores(h, r, top: int, piece: int = 65536):
+    """The `top` largest scores h r^T of every row and their items (int32), by pieces of `r`,
+    so that the scores of a large catalogue are never there as a whole."""
+    values = h.new_empty((h.shape[0], 0))
+    items = torch.empty((h.shape[0], 0), dtype=torch.int32, device=h.device)
+    for begin in range(0, r.shape[0], piece):
+        s = h @ r[begin:begin + piece].T
+        best = torch.topk(s, min(top, s.shape[1]), dim=1)
+        values, at = torch.topk(torch.cat([values, best.values], 1), min(top, values.shape[1] + best.values.shape[1]), dim=1)
+        items = torch.cat([items, best.indices.int() + begin], 1).gather(1, at)
+    return items, values
+
+
 def batches(i, j, worker, P: int, batch: int, clocks: int, seed: int):
     """Per clock and worker a batch of the events of the worker's users (device int32)."""
     rng = np.random.default_rng(seed)
@@ -126,8 +139,7 @@ def run(w, clocks: int, batch: int, eta: float, narrow: int, narrow_eta: float, 
             losses = []
             for p, u, _ in parts:
                 h, r = wide.rows(p, u)
-                best = torch.topk(h @ r.T, min(top, M), dim=1)  # (what a service stores of the wide model)
-                losses.append(small.learn_from(p, u, best.indices.int(), best.values, narrow_eta))
+                losses.append(small.learn_from(p, u, *top_scores(h, r, top), narrow_eta))  # (what a service stores of the wide model)
             small.table.clock()
             if c % every == 0 or c in (1, clocks):
                 emit({"model": f"K={narrow} from K={w.K}", "clock": c, "divergence": float(torch.cat(losses).mean())})
