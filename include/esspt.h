@@ -315,11 +315,22 @@ esspt_status esspt_mf_worker_objective_noalloc(esspt_ctx* ctx, int32_t version, 
  *     dw_v = b sum_t weight_t (p_tv - q_tv) h_t
  * The n x V scores are not kept: they are formed piece by piece, as often as they
  * are needed.  (Calls of up to ESSPT_SOFTMAX_FEW_ROWS rows, and of up to 128 where
- * that is faster, keep theirs in the workspace, whose size counts them.)
+ * that is faster, keep theirs in the workspace, whose size counts them: 32 V bytes
+ * for 8 rows, 2^24 scores at most for more.)
  *
- * Values are fp32, bf16 or fp16, H, W and both gradients alike.  Products are
- * exact to fp32 rounding for fp32 rows; sums, statistics, losses and weights are
- * fp32; of 16-bit rows the p_tv that meet a tensor core are rounded to 16 bits.
+ * Values are fp32, bf16 or fp16, H, W and both gradients alike; sums, statistics,
+ * losses and weights are fp32.  Where tensor cores take the products:
+ *   - an fp32 value is held to 2^-32 of its own row's largest, whatever the sizes of
+ *     the other rows, so that scores are exact to fp32 rounding beside the row's size
+ *     (a row more than 2^80 below its matrix's largest value: beside 2^-80 of that);
+ *   - a p_tv has 22 bits (fp32 rows) or its type's (16-bit rows).  Of fp32 and fp16 rows
+ *     they are steps of 2^-38 at least, of the row's largest in dh, and in dw of the
+ *     item's largest weight_t p_tv, or of the largest weight where no item is 2^24 below
+ *     it (fp16: unless weights differ by more than 2^8).  bf16 has no such floor;
+ *   - their sums truncate, by about 10^-6 of sum |terms|.  So a gradient is exact
+ *     relative to its terms, sum (p + q) |w| and |h|; near a fit, where p - q is small
+ *     beside p, what is left has that error, and in 16 bits a single target's p may
+ *     round to the unit beside its own.
  * Results do not depend on the order in which the GPU runs its blocks. */
 typedef enum { ESSPT_F32 = 0, ESSPT_BF16 = 1, ESSPT_F16 = 2 } esspt_dtype;
 

@@ -2,10 +2,10 @@
 // problems, where launches and latency count: the scores of groups of kFewRows rows
 // are kept, W is read once for them and once for dh.  All in fp32.
 //
-// 1M items, K = 64, fp32, eight rows, GB300: scores 58 us (256 MB, 4.4 TB/s: loads in
-// flight), dw 100 (320 MB), dh 82 (288 MB, 3.5 TB/s), against 38 us for 256 MB.  A
-// single row's scores without gradients: a call of 50 us in fp32 and 34 in bf16, where
-// the kernel for eight rows takes 64 and 55.
+// 1M items, K = 64, fp32, eight rows, GB300: scores that are kept 63 us (288 MB, 4.5 TB/s:
+// loads in flight), dw 98 (320 MB, 3.3 TB/s), dh 94 (288 MB, 3.1 TB/s), where 256 MB are 38
+// us.  A single row's scores without gradients: a call of 49 us in fp32 and 33 in bf16,
+// where the kernel for eight rows takes 64 and 55.
 #include <algorithm>
 
 #include "ptx.cuh"

@@ -11,8 +11,8 @@
 //              item, in large problems where a tile of rows says so; sum weight p h, then dw
 //
 // The kernels here are bound by bytes or by latency: 2048 x 1M, K = 64, fp32, GB300:
-// max 43 us (256 MB, 6.0 TB/s), units 72 (512 MB, 7.1 TB/s), dw 118 (512 MB, 4.3 TB/s,
-// with its scattered targets) of the call's 2550.
+// max 52 us (256 MB, 4.9 TB/s), units 84 (512 MB, 6.1 TB/s), dw 133 (512 MB, 3.9 TB/s,
+// with its scattered targets) of the call's 2890.
 #include <cub/device/device_radix_sort.cuh>
 
 #include <algorithm>
@@ -131,7 +131,8 @@ __device__ __forceinline__ void load_piece(const T* row, int32_t d, int32_t D, f
 
 // fp32 rows to units of halves, eight lanes to a row: its largest value first, which
 // decides whether the row takes a power of two of its own.  Rows of one or two units (NK)
-// are kept in registers, several at once, others (0) read again.  (1M x 64: 71 us.  The rows after the last, up to the end of its tile, and the values
+// are kept in registers, several at once, others (0) read again (100k x 64: 12 us, by one
+// row at a time 16).  The rows after the last, up to the end of its tile, and the values
 // after a row's last are zero.
 template <int VEC, int NK>
 __global__ void __launch_bounds__(256) units_f32_kernel(Many f, unsigned w_blocks) {
@@ -628,9 +629,9 @@ __global__ void __launch_bounds__(256) runs_kernel(Many f, const uint32_t* key, 
 
 // dw: b (sum weight p h - sum weight q h), some items to a block.  Most items are
 // nobody's target: those rows go through all threads side by side, the others a warp
-// each (2048 x 1M, K = 64: a warp for every item took 470 us, this 118).
+// each (2048 x 1M, K = 64: a warp for every item took 470 us, this 133).
 // Items of a block: 16 where 64 would leave SMs idle, 64 up to 32 blocks of them per SM,
-// else 128 (that case: 118 us, by 64 129).
+// else 128 (that case: a tenth less than by 64).
 constexpr int kItems = 128;
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) grad_w_kernel(Many f, int per_block, const uint32_t* key, const int32_t* row,

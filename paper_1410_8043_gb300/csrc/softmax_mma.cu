@@ -13,10 +13,11 @@
 // proportion to its length; sums run over at most `run` tiles and are then added in fp32.
 //
 // Rows and cols pass, 2048 x 120k, GB300 (tensor pipe active / instruction issue /
-// exponentials, of their peaks): bf16, K = 64: 64 and 75 us (45/60/45%, 37/50/38%):
-// issue, tensor cores and exponentials share the limit; K = 256: 190 and 199 us
-// (59/23/15%, 55/22/14%) and fp32, K = 100: 247 and 222 us (60/24/11%, 68/28/13%): the
-// products, and their waits for loads (a tile of B is 64 KB at both).
+// exponentials, of their peaks): bf16, K = 64: 67 and 81 us (40/54/44%, 32/43/36%): no one
+// of them is full; K = 256: 193 and 208 us (54/21/15%, 50/20/14%) and fp32, K = 100: 258 and
+// 224 us (56/23/11%, 65/30/13%): the products, and their waits for loads (a tile of B is 64
+// KB at both).  Maxima by high halves, fp32, K = 64: 40 us (33/46/0%): the chain from a
+// tile's products to its maxima and back to the buffer.
 #include <type_traits>
 
 #include "ptx.cuh"

@@ -386,8 +386,10 @@ class SoftmaxHead:
 
     `loss` is cross entropy against one item per row, `distill` the divergence
     from a teacher's top logits; both give the gradients of the weighted sum of
-    the rows' losses.  The n x n_items scores are never kept.  The workspace is
-    allocated here once.  Work runs on `stream` (default: the current one at
+    the rows' losses as tensors: there is no autograd graph, a program hands them on
+    itself (`h.backward(r.grad_h)`).  The n x n_items scores are not kept (but for calls
+    of up to 8 rows, and of up to 128 where that is faster: at most 8 n_items or 2^24 of
+    them, in the workspace).  The workspace is allocated here once.  Work runs on `stream` (default: the current one at
     construction); a call from another current stream is ordered after the work
     queued there, and that stream's later work after the call.  Calls may be captured
     in a CUDA graph, where `stream` is the captured one.
