@@ -143,7 +143,7 @@ esspt_status run(esspt_softmax* sm, const void* h, int64_t h_stride, const void*
   a.V = (int32_t)c.n_items, a.D = c.width, a.dtype = c.dtype;
   a.target = TargetArgs{ids, logits, top, n, a.V, b, reinterpret_cast<float*>(sm->base + k.q),
                         reinterpret_cast<float*>(sm->base + k.self), reinterpret_cast<uint32_t*>(sm->base + k.status), nullptr};
-  if (c.dtype != ESSPT_F32 && grad_w && logits && top <= kAgainByWarp && n > kFewRows)
+  if (c.dtype != ESSPT_F32 && grad_w && logits && top > 1 && top <= kAgainByWarp && n > kFewRows)  // (k.again holds lists)
     a.target.again = reinterpret_cast<uint8_t*>(sm->base + k.again);
   a.weight = weight, a.b = b, a.loss = loss, a.lse = lse, a.grad_h = grad_h, a.grad_w = grad_w;
   a.st = sm->st, a.sms = sm->sms;
