@@ -852,9 +852,12 @@ cudaError_t run(const SoftmaxArgs& a, const ManyScratch& s) {
     cudaError_t err = stats(Pass::kStats, a.V, if_redo);
     if (err != cudaSuccess) return err;
     loss_kernel<T, VEC><<<by_row, 256, 0, a.st>>>(f);
-    if (!grads) return cudaGetLastError();
-    if ((err = rows(false, if_redo)) != cudaSuccess || (join_early && (err = join()) != cudaSuccess)) return err;
-    grad_h_kernel<T, VEC, false><<<dim3(by_row, col_chunks), 256, 0, a.st>>>(f);
+    if constexpr (kBf16) {
+      if (grads) {
+        if ((err = rows(false, if_redo)) != cudaSuccess || (join_early && (err = join()) != cudaSuccess)) return err;
+        grad_h_kernel<T, VEC, false><<<dim3(by_row, col_chunks), 256, 0, a.st>>>(f);
+      }
+    }
     return cudaGetLastError();
   };
   // A pass over all scores of bf16 rows for their maxima alone is a fifth of the work.

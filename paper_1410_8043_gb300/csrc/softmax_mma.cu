@@ -807,7 +807,8 @@ cudaError_t launch_type(bool bf16, int parts, const MmaArgs& a, int blocks, int 
 cudaError_t launch_mma(Pass pass, bool bf16, int parts, const MmaArgs& a, int blocks, int out_chunks, cudaStream_t st) {
   if (pass == Pass::kStats) return launch_type<Pass::kStats>(bf16, parts, a, blocks, 1, st);
   if (pass == Pass::kMax) return launch_type<Pass::kMax>(bf16, parts, a, blocks, 1, st);
-  if (pass == Pass::kMaxCols) return launch_type<Pass::kMaxCols>(bf16, parts, a, blocks, 1, st);
+  if (pass == Pass::kMaxCols)  // (bf16 rows have none)
+    return parts == 2 ? launch<Pass::kMaxCols, false, 2>(a, blocks, 1, st) : launch<Pass::kMaxCols, false, 1>(a, blocks, 1, st);
   if (pass == Pass::kRows) return launch_type<Pass::kRows>(bf16, parts, a, blocks, out_chunks, st);
   return launch_type<Pass::kCols>(bf16, parts, a, blocks, out_chunks, st);
 }
