@@ -409,6 +409,209 @@ esspt_status esspt_softmax_poll(esspt_softmax* sm);
  * on it.  NULL gives the last esspt_softmax_create() error. */
 const char* esspt_softmax_last_error(const esspt_softmax* sm);
 
+/* ---- Embedding lookup and its gradient ------------------------------------ */
+
+/* Rows of a table W [V, D] by id, scaled, and the gradient that goes back to W: what
+ * comes before the softmax (or any network) and after it.
+ *     out_t = scale W[id_t]
+ *     dW_v  = scale sum_{t: id_t = v} dout_t
+ * Values are fp32, bf16 or fp16, W, out and the gradients alike; products and sums are
+ * fp32, rounded once.  An id < 0 is padding: its out row is zeros and its dout row is
+ * not read.  An id >= V is treated as padding and reported as ESSPT_EINVAL by
+ * esspt_embed_poll().  The sums go over the tokens sorted by id, then by place, in an
+ * order that sizes alone decide: results do not depend on the order in which the GPU runs
+ * its blocks. */
+typedef struct {
+  int64_t max_tokens; /* most ids per call, 1..2^30 */
+  int64_t n_rows;     /* V: rows of W, 1..2^30 */
+  int32_t width;      /* D: values per row, 1..8192 */
+  int32_t dtype;      /* esspt_dtype of W, out and the gradients */
+  int32_t backward;   /* 1 = calls may ask for gradients */
+  void* stream;       /* cudaStream_t; NULL = legacy default stream */
+} esspt_embed_config;
+
+typedef struct esspt_embed esspt_embed;
+
+/* Bytes of device workspace a handle needs.  0 on invalid config. */
+size_t esspt_embed_workspace_bytes(const esspt_embed_config* cfg);
+
+/* Create a handle over caller-allocated device workspace (256-byte aligned, kept until
+ * esspt_embed_destroy(), not written by others).  A handle's calls share the workspace: they
+ * run in its stream's order, and graphs that captured calls of one handle may not run at
+ * the same time.  ESSPT_EINVAL on a bad config, ESSPT_ENOSPC on a short workspace. */
+esspt_status esspt_embed_create(const esspt_embed_config* cfg, void* d_workspace, size_t bytes, esspt_embed** out);
+
+/* Release the host-side handle (not the workspace).  Synchronises the stream
+ * first.  NULL is accepted. */
+esspt_status esspt_embed_destroy(esspt_embed* em);
+
+/* The rows of d_ids (device int32[n], 0 <= n <= max_tokens) out of d_w (rows w_stride >= D
+ * values apart), scaled by any finite `scale`, to d_out (rows D apart).  Any alignment of the
+ * type itself; rows of 16 bytes' multiples are the fast ones.  d_out may not overlap d_w.
+ * Asynchronous on the handle's stream. */
+esspt_status esspt_embed_lookup(esspt_embed* em, const void* d_w, int64_t w_stride, const int32_t* d_ids, int64_t n,
+                                float scale, void* d_out);
+
+/* The gradient to W of sum(out * dout): d_grad holds dout (rows grad_stride >= D values
+ * apart), d_grad_w [V, D] the result (rows D apart).  accumulate = 0: every row is written,
+ * with zeros where no token asks for it.  accumulate = 1: the sums are added to what
+ * d_grad_w holds (a softmax's gradient to the same rows), and rows that no token asks for
+ * are neither read nor written.  d_grad_w may not overlap d_grad or d_ids.  Asynchronous on
+ * the handle's stream.  ESSPT_EINVAL if the handle was made without backward. */
+esspt_status esspt_embed_gradient(esspt_embed* em, const int32_t* d_ids, const void* d_grad, int64_t grad_stride,
+                                  int64_t n, float scale, int32_t accumulate, void* d_grad_w);
+
+/* Synchronise the stream and report, then clear, any error latched on the device
+ * (ESSPT_EINVAL: an id >= V; ESSPT_ECUDA: a wait inside a kernel ran out, which is not
+ * expected, and the results since the last poll are void). */
+esspt_status esspt_embed_poll(esspt_embed* em);
+
+/* Text of the last error on this handle ("" if none), valid until the next call
+ * on it.  NULL gives the last esspt_embed_create() error. */
+const char* esspt_embed_last_error(const esspt_embed* em);
+
+/* ---- Layer norm ------------------------------------------------------------ */
+
+/* Rows x [n, D] (looked up, or hidden states) normed to mean 0 and variance 1:
+ *     mean_t = sum_d x_td / D,   rstd_t = 1 / sqrt(sum_d (x_td - mean_t)^2 / D + eps),
+ *     x^_td = (x_td - mean_t) rstd_t,   y_td = x^_td w_d + b_d
+ * and back from dy, with g_td = dy_td w_d:
+ *     dx_td = rstd_t (g_td - mean_d g_t - x^_td mean_d(g_t x^_t))
+ *     dw_d = sum_t dy_td x^_td,   db_d = sum_t dy_td
+ * Rows are fp32, bf16 or fp16 (x, y, dy, dx alike); w, b and their gradients are fp32 or
+ * of the rows' type; statistics and sums are fp32, the variance from differences to the
+ * mean.  A row of equal values gives y = b.  NaN or infinity in a row makes that row NaN,
+ * and in the backward pass the weights' gradients too.  Results do not depend on the order in
+ * which the GPU runs its blocks. */
+typedef struct {
+  int64_t max_rows;     /* most rows per call, 1..2^31-1 */
+  int32_t width;        /* D: values per row, 1..8192 */
+  int32_t dtype;        /* esspt_dtype of the rows */
+  int32_t weight_dtype; /* esspt_dtype of w, b, dw, db: ESSPT_F32 or dtype */
+  int32_t backward;     /* 1 = calls may ask for gradients */
+  float eps;            /* > 0 and finite */
+  void* stream;         /* cudaStream_t; NULL = legacy default stream */
+} esspt_norm_config;
+
+typedef struct esspt_norm esspt_norm;
+
+/* Bytes of device workspace a handle needs.  0 on invalid config. */
+size_t esspt_norm_workspace_bytes(const esspt_norm_config* cfg);
+
+/* Create a handle over caller-allocated device workspace, as esspt_embed_create(). */
+esspt_status esspt_norm_create(const esspt_norm_config* cfg, void* d_workspace, size_t bytes, esspt_norm** out);
+
+/* Release the host-side handle (not the workspace).  Synchronises the stream
+ * first.  NULL is accepted. */
+esspt_status esspt_norm_destroy(esspt_norm* nm);
+
+/* The forward pass over n rows (0 <= n <= max_rows) of d_x, x_stride >= D values apart.
+ * d_weight, d_bias: D values each, or NULL for 1 and 0.  d_y: rows D apart.  d_mean, d_rstd:
+ * fp32[n] for the backward pass, or both NULL.  Outputs may not overlap inputs.
+ * Asynchronous on the handle's stream. */
+esspt_status esspt_norm_forward(esspt_norm* nm, const void* d_x, int64_t x_stride, int64_t n, const void* d_weight,
+                                const void* d_bias, void* d_y, float* d_mean, float* d_rstd);
+
+/* The backward pass, from the same x, weights and the statistics that the forward pass
+ * gave.  d_dx (rows D apart), d_dweight and d_dbias (D values each) overwrite; any of them may
+ * be NULL.  n = 0 writes zeros to d_dweight and d_dbias.  Outputs may not overlap inputs.
+ * Asynchronous on the handle's stream.  ESSPT_EINVAL if the handle was made without backward. */
+esspt_status esspt_norm_backward(esspt_norm* nm, const void* d_dy, int64_t dy_stride, const void* d_x,
+                                 int64_t x_stride, int64_t n, const void* d_weight, const float* d_mean,
+                                 const float* d_rstd, void* d_dx, void* d_dweight, void* d_dbias);
+
+/* Text of the last error on this handle ("" if none), valid until the next call
+ * on it.  NULL gives the last esspt_norm_create() error. */
+const char* esspt_norm_last_error(const esspt_norm* nm);
+
+/* ---- AdamW over many tensors ------------------------------------------------ */
+
+/* One step over a list of fp32 tensors, t the number of the step:
+ *     g = grad_scale grad,   m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2
+ *     p = p (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+ * in fp32, m and v by products and sums rounded one by one in the order written.  A tensor may
+ * have a 16-bit copy that a network runs on: it is rewritten from p, and the tensor's gradients are of
+ * its type; without a copy gradients are fp32.
+ *
+ * The moments are kept in the workspace, in 32 bits, or in 8: m and u = sqrt(v) in blocks
+ * of 128 values with an exponent E each,
+ *     |m| = (1 + j/8) 2^(E - 15 + e),   u = (1 + j/16) 2^(E - 15 + e),   e = 0..15,
+ * code 8 e + j (and the sign) or 16 e + j, code 0 being zero; E is the least, from -111 on, that the block's
+ * largest value needs.  The step itself takes the moments before they are held so.  A value x
+ * between two that lie d apart is held as d floor(x / d + rho), rho = r / 2^16, so that
+ * moving averages move by less than a step of the format in the mean (rounded to the nearest, an
+ * average of 0.999 would stand still: its changes are a tenth of a percent, half a step 3 to 6).  Below the
+ * least code, m is held as it or as 0 by the same rule, and u, which divides, as it.  r is the high (m) or low (u)
+ * half of h(i, t), a hash of the value's place i in the flat order, the step and the seed, with
+ *     mix(x): x ^= x >> 16, x *= 0x5851F42D, x ^= x >> 15, x *= 0x2545F491, x ^= x >> 16
+ *     h(i, t) = mix((lo(i) 0x9E3779B1 + hi(i) 0x85EBCA77) ^ mix(lo(seed) ^ mix(hi(seed) ^ mix(t))))
+ * over 32-bit words (lo, hi: a number's low and high word; of t the low one).  So a run can be
+ * repeated bit for bit.
+ *
+ * Flat order: the tensors one behind the other, each beginning at a multiple of 128 values. */
+typedef struct {
+  float* d_param;     /* device, `count` fp32 values */
+  void* d_copy;       /* device, `count` values of copy_dtype, or NULL */
+  int64_t count;      /* >= 0 */
+  float weight_decay; /* >= 0 and finite */
+} esspt_adamw_tensor;
+
+typedef struct {
+  int32_t n_tensors;  /* 1..2^20 */
+  int32_t state_bits; /* 32 or 8 */
+  int32_t copy_dtype; /* ESSPT_BF16 or ESSPT_F16: of the copies and their tensors' gradients */
+  int32_t reserved;   /* 0 */
+  double beta1, beta2; /* in [0, 1) */
+  double eps;         /* > 0 and finite in fp32 */
+  uint64_t seed;      /* of the rounding of 8-bit moments */
+  void* stream;       /* cudaStream_t; NULL = legacy default stream */
+} esspt_adamw_config;
+
+typedef struct esspt_adamw esspt_adamw;
+
+/* Length of the flat order of moments.  0 on an invalid config or list. */
+int64_t esspt_adamw_moment_values(const esspt_adamw_config* cfg, const esspt_adamw_tensor* tensors);
+
+/* Bytes of device workspace a handle needs.  0 on an invalid config or list. */
+size_t esspt_adamw_workspace_bytes(const esspt_adamw_config* cfg, const esspt_adamw_tensor* tensors);
+
+/* Create a handle with zero moments, before step 1.  `tensors` (host) is copied; the
+ * tensors may not overlap.  The workspace is as of esspt_embed_create(); with 32 bits it begins with
+ * m and then v, fp32 each, in flat order.  Synchronises the stream. */
+esspt_status esspt_adamw_create(const esspt_adamw_config* cfg, const esspt_adamw_tensor* tensors, void* d_workspace,
+                                size_t bytes, esspt_adamw** out);
+
+/* Release the host-side handle (not the workspace).  Synchronises the stream
+ * first.  NULL is accepted. */
+esspt_status esspt_adamw_destroy(esspt_adamw* aw);
+
+/* One step.  h_grads: host array of n_tensors device pointers, read before the call returns;
+ * a NULL leaves its tensor, copy and moments as they are.  lr: the step size, finite;
+ * d_lr, if not NULL, a device fp32 that is read instead when the step runs.  d_grad_scale: a
+ * device fp32 that multiplies gradients (a clipping factor, a loss scale's inverse), or NULL for 1.  The number
+ * of the step is counted on the device, so that a step captured in a CUDA graph counts at every replay.
+ * NaN or infinity in a gradient makes NaN of what the formula does, and with 8 bits of its
+ * block's moments (as a moment past 1.875 2^127 does).  Asynchronous on the handle's stream. */
+esspt_status esspt_adamw_step(esspt_adamw* aw, const void* const* h_grads, float lr, const float* d_lr,
+                              const float* d_grad_scale);
+
+/* The moments in flat order: m, and v (32 bits, fp32 each) or sqrt(v) (8 bits, bf16 each,
+ * which holds all of a code's bits), both 16-byte aligned.  Zeros between tensors.  Asynchronous on the handle's
+ * stream. */
+esspt_status esspt_adamw_moments(esspt_adamw* aw, void* d_m, void* d_second);
+
+/* Take moments as esspt_adamw_moments() gives them (8 bits: any bf16, rounded to the nearest code, what it gave
+ * exactly), and the number of steps taken, >= 0.  A negative value of `second` is taken as 0; what lies between tensors
+ * is not read.  Asynchronous on the handle's stream. */
+esspt_status esspt_adamw_load(esspt_adamw* aw, const void* d_m, const void* d_second, int64_t steps);
+
+/* Synchronise the stream and give the number of steps taken. */
+esspt_status esspt_adamw_steps(esspt_adamw* aw, int64_t* steps);
+
+/* Text of the last error on this handle ("" if none), valid until the next call
+ * on it.  NULL gives the last esspt_adamw_create() error. */
+const char* esspt_adamw_last_error(const esspt_adamw* aw);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,6 +32,12 @@ EXPORTS = (
     "esspt_mf_sequential_work_bytes", "esspt_mf_sgd_clock_sequential",
     "esspt_softmax_workspace_bytes", "esspt_softmax_create", "esspt_softmax_destroy", "esspt_softmax_loss",
     "esspt_softmax_distill", "esspt_softmax_poll", "esspt_softmax_last_error",
+    "esspt_embed_workspace_bytes", "esspt_embed_create", "esspt_embed_destroy", "esspt_embed_lookup",
+    "esspt_embed_gradient", "esspt_embed_poll", "esspt_embed_last_error",
+    "esspt_norm_workspace_bytes", "esspt_norm_create", "esspt_norm_destroy", "esspt_norm_forward",
+    "esspt_norm_backward", "esspt_norm_last_error",
+    "esspt_adamw_moment_values", "esspt_adamw_workspace_bytes", "esspt_adamw_create", "esspt_adamw_destroy",
+    "esspt_adamw_step", "esspt_adamw_moments", "esspt_adamw_load", "esspt_adamw_steps", "esspt_adamw_last_error",
 )
 
 
@@ -68,6 +74,52 @@ class SoftmaxConfig(ctypes.Structure):
         ("dtype", ctypes.c_int32),
         ("max_top", ctypes.c_int32),
         ("backward", ctypes.c_int32),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class EmbedConfig(ctypes.Structure):
+    _fields_ = [
+        ("max_tokens", ctypes.c_int64),
+        ("n_rows", ctypes.c_int64),
+        ("width", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("backward", ctypes.c_int32),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class NormConfig(ctypes.Structure):
+    _fields_ = [
+        ("max_rows", ctypes.c_int64),
+        ("width", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+        ("backward", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [
+        ("d_param", ctypes.c_void_p),
+        ("d_copy", ctypes.c_void_p),
+        ("count", ctypes.c_int64),
+        ("weight_decay", ctypes.c_float),
+    ]
+
+
+class AdamWConfig(ctypes.Structure):
+    _fields_ = [
+        ("n_tensors", ctypes.c_int32),
+        ("state_bits", ctypes.c_int32),
+        ("copy_dtype", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("seed", ctypes.c_uint64),
         ("stream", ctypes.c_void_p),
     ]
 
@@ -117,6 +169,28 @@ def lib() -> ctypes.CDLL:
         "esspt_softmax_distill": (ctypes.c_int, [P, P, I64, P, I64, P, P, I32, I64, P, ctypes.c_float, P, P, P, P]),
         "esspt_softmax_poll": (ctypes.c_int, [P]),
         "esspt_softmax_last_error": (ctypes.c_char_p, [P]),
+        "esspt_embed_workspace_bytes": (SZ, [P]),
+        "esspt_embed_create": (ctypes.c_int, [P, P, SZ, P]),
+        "esspt_embed_destroy": (ctypes.c_int, [P]),
+        "esspt_embed_lookup": (ctypes.c_int, [P, P, I64, P, I64, ctypes.c_float, P]),
+        "esspt_embed_gradient": (ctypes.c_int, [P, P, P, I64, I64, ctypes.c_float, I32, P]),
+        "esspt_embed_poll": (ctypes.c_int, [P]),
+        "esspt_embed_last_error": (ctypes.c_char_p, [P]),
+        "esspt_norm_workspace_bytes": (SZ, [P]),
+        "esspt_norm_create": (ctypes.c_int, [P, P, SZ, P]),
+        "esspt_norm_destroy": (ctypes.c_int, [P]),
+        "esspt_norm_forward": (ctypes.c_int, [P, P, I64, I64, P, P, P, P, P]),
+        "esspt_norm_backward": (ctypes.c_int, [P, P, I64, P, I64, I64, P, P, P, P, P, P]),
+        "esspt_norm_last_error": (ctypes.c_char_p, [P]),
+        "esspt_adamw_moment_values": (I64, [P, P]),
+        "esspt_adamw_workspace_bytes": (SZ, [P, P]),
+        "esspt_adamw_create": (ctypes.c_int, [P, P, P, SZ, P]),
+        "esspt_adamw_destroy": (ctypes.c_int, [P]),
+        "esspt_adamw_step": (ctypes.c_int, [P, P, ctypes.c_float, P, P]),
+        "esspt_adamw_moments": (ctypes.c_int, [P, P, P]),
+        "esspt_adamw_load": (ctypes.c_int, [P, P, P, I64]),
+        "esspt_adamw_steps": (ctypes.c_int, [P, P]),
+        "esspt_adamw_last_error": (ctypes.c_char_p, [P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -531,3 +605,344 @@ class SoftmaxHead:
     def poll(self) -> None:
         """esspt_softmax_poll: synchronise and raise on a target or id outside the catalogue."""
         self._check(self._lib.esspt_softmax_poll(self._h))
+
+
+class _Operator:
+    """What the handles of the operators on rows share: where they run, errors, the end.
+
+    Work runs on `stream` (default: the current one at construction).  A call from
+    another current stream is ordered after the work queued there, and that stream's later
+    work after the call.  Calls may be captured in a CUDA graph, where `stream` is the
+    captured one.
+    """
+
+    _name = ""
+
+    def _open(self, dtype, device, stream):
+        self._h = None
+        if not torch.cuda.is_available():
+            raise RuntimeError("esspt needs a CUDA device")
+        self._lib = lib()
+        if dtype not in DTYPES:
+            raise EssptError(EINVAL, f"dtype must be one of {', '.join(str(d) for d in DTYPES)}")
+        device = torch.device(device if device is not None else "cuda")
+        self.device = device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self.dtype = dtype
+        self._stream_ptr = self.stream.cuda_stream
+
+    def _create(self, *config) -> None:
+        """The workspace and the handle of a configuration (and what else its calls take)."""
+        nbytes = getattr(self._lib, f"esspt_{self._name}_workspace_bytes")(*config)
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+            st = getattr(self._lib, f"esspt_{self._name}_create")(*config, self.workspace.data_ptr(), nbytes, ctypes.byref(h))
+        if st != OK:
+            raise EssptError(st, getattr(self._lib, f"esspt_{self._name}_last_error")(None).decode())
+        self._h = h
+
+    def _check(self, st: int) -> None:
+        if st != OK:
+            raise EssptError(st, getattr(self._lib, f"esspt_{self._name}_last_error")(self._h).decode())
+
+    def _call(self, call, *args) -> None:
+        """One of the library's calls, in order with the current stream."""
+        current = torch.cuda.current_stream(self.device)
+        elsewhere = current.cuda_stream != self._stream_ptr
+        if elsewhere:
+            self.stream.wait_stream(current)
+        if torch.cuda.current_device() == self.device.index:
+            st = call(self._h, *args)
+        else:
+            with torch.cuda.device(self.device):
+                st = call(self._h, *args)
+        if elsewhere:
+            current.wait_stream(self.stream)
+        if st != OK:
+            self._check(st)
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            getattr(self._lib, f"esspt_{self._name}_destroy")(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _rows(self, x, n, width, dtype, name) -> torch.Tensor:
+        """`x` as rows that the library reads in place; another layout is copied."""
+        if not isinstance(x, torch.Tensor) or x.dtype is not dtype or x.device != self.device:
+            raise EssptError(EINVAL, f"{name} must be a {dtype} tensor on {self.device}")
+        shape = x.shape
+        if len(shape) != 2 or shape[1] != width or (n is not None and shape[0] != n):
+            raise EssptError(EINVAL, f"{name} has shape {tuple(shape)}, not ({n if n is not None else 'n'}, {width})")
+        if (x.stride(1) != 1 and width > 1) or (shape[0] > 1 and x.stride(0) < width):
+            x = x.contiguous()
+        return x
+
+    def _values(self, x, shape, dtype, name) -> torch.Tensor:
+        """`x`, read as contiguous values."""
+        if not isinstance(x, torch.Tensor) or x.dtype is not dtype or x.device != self.device or x.shape != shape:
+            raise EssptError(EINVAL, f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {self.device}")
+        return x if x.is_contiguous() else x.contiguous()
+
+    def _out(self, x, shape, dtype, name) -> torch.Tensor:
+        if x is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        if not isinstance(x, torch.Tensor) or x.dtype is not dtype or x.device != self.device or x.shape != shape or not x.is_contiguous():
+            raise EssptError(EINVAL, f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
+        return x
+
+
+def _stride(x) -> int:
+    """Values from one row to the next."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+class Embedding(_Operator):
+    """Rows of a table of `n_rows` by id, and the gradient back to it (one `esspt_embed` handle).
+
+    `lookup` gives scale * w[ids], zeros where an id is negative (padding); `gradient`
+    sums scale * grad over the tokens of each row, in a fixed order: the same inputs
+    give the same bits.  There is no autograd graph.  The workspace is allocated here once.
+    """
+
+    __doc__ += _Operator.__doc__.split("\n", 1)[1]
+    _name = "embed"
+
+    def __init__(self, max_tokens: int, n_rows: int, width: int, dtype=torch.float32, backward: bool = True, device=None,
+                 stream=None):
+        self._open(dtype, device, stream)
+        self.max_tokens, self.n_rows, self.width, self.backward = max_tokens, n_rows, width, backward
+        self._create(ctypes.byref(EmbedConfig(max_tokens, n_rows, width, DTYPES[dtype], int(backward),
+                                              ctypes.c_void_p(self._stream_ptr))))
+
+    def _ids(self, ids) -> torch.Tensor:
+        if not isinstance(ids, torch.Tensor) or ids.device != self.device or ids.dim() != 1:
+            raise EssptError(EINVAL, f"ids must be a tensor of shape (n,) on {self.device}")
+        if ids.shape[0] > self.max_tokens:
+            raise EssptError(EINVAL, f"{ids.shape[0]} ids, more than max_tokens = {self.max_tokens}")
+        if ids.dtype is not torch.int32:
+            if ids.dtype is not torch.int64:
+                raise EssptError(EINVAL, "ids must hold torch.int32 values")
+            ids = ids.clamp(-1, 2**31 - 1).to(torch.int32)  # (past 32 bits is outside the table all the same)
+        return ids if ids.is_contiguous() else ids.contiguous()
+
+    def lookup(self, w, ids, scale: float = 1.0, out=None) -> torch.Tensor:
+        """esspt_embed_lookup: rows of w (n_rows, width), which may be strided, by ids
+        int32 (n,)."""
+        ids = self._ids(ids)
+        w = self._rows(w, self.n_rows, self.width, self.dtype, "w")
+        n = ids.shape[0]
+        out = self._out(out, (n, self.width), self.dtype, "out")
+        self._call(self._lib.esspt_embed_lookup, w.data_ptr(), _stride(w), ids.data_ptr(), n, scale, out.data_ptr())
+        return out
+
+    def gradient(self, ids, grad, scale: float = 1.0, grad_w=None, accumulate: bool = False) -> torch.Tensor:
+        """esspt_embed_gradient: from grad (n, width), which may be strided, that of a
+        whole table; with `accumulate` added to grad_w, whose other rows stay as they are."""
+        ids = self._ids(ids)
+        n = ids.shape[0]
+        grad = self._rows(grad, n, self.width, self.dtype, "grad")
+        if accumulate and grad_w is None:
+            raise EssptError(EINVAL, "accumulate needs a grad_w")
+        grad_w = self._out(grad_w, (self.n_rows, self.width), self.dtype, "grad_w")
+        self._call(self._lib.esspt_embed_gradient, ids.data_ptr(), grad.data_ptr(), _stride(grad), n, scale,
+                   int(bool(accumulate)), grad_w.data_ptr())
+        return grad_w
+
+    def poll(self) -> None:
+        """esspt_embed_poll: synchronise and raise on an id outside the table."""
+        self._check(self._lib.esspt_embed_poll(self._h))
+
+
+class NormResult(NamedTuple):
+    """y, and fp32[n] of a row's mean and 1 / standard deviation for the backward pass."""
+
+    y: torch.Tensor
+    mean: torch.Tensor
+    rstd: torch.Tensor
+
+
+class NormGradients(NamedTuple):
+    grad_x: torch.Tensor | None
+    grad_weight: torch.Tensor | None
+    grad_bias: torch.Tensor | None
+
+
+class LayerNorm(_Operator):
+    """Layer norm of rows, forward and backward (one `esspt_norm` handle).
+
+    Weights and their gradients are `weight_dtype` (default: the rows').  There is no
+    autograd graph: a program keeps mean and rstd of `forward` for `backward`.
+    """
+
+    __doc__ += _Operator.__doc__.split("\n", 1)[1]
+    _name = "norm"
+
+    def __init__(self, max_rows: int, width: int, dtype=torch.float32, weight_dtype=None, eps: float = 1e-5,
+                 backward: bool = True, device=None, stream=None):
+        self._open(dtype, device, stream)
+        weight_dtype = weight_dtype if weight_dtype is not None else dtype
+        if weight_dtype not in DTYPES:
+            raise EssptError(EINVAL, f"weight_dtype must be {dtype} or torch.float32")
+        self.max_rows, self.width, self.weight_dtype, self.eps, self.backwards = max_rows, width, weight_dtype, eps, backward
+        self._create(ctypes.byref(NormConfig(max_rows, width, DTYPES[dtype], DTYPES[weight_dtype], int(backward), eps,
+                                             ctypes.c_void_p(self._stream_ptr))))
+
+    def _n(self, x) -> int:
+        if x.shape[0] > self.max_rows:
+            raise EssptError(EINVAL, f"{x.shape[0]} rows, more than max_rows = {self.max_rows}")
+        return x.shape[0]
+
+    def _weights(self, x, name):
+        return None if x is None else self._values(x, (self.width,), self.weight_dtype, name)
+
+    def forward(self, x, weight=None, bias=None, y=None) -> NormResult:
+        """esspt_norm_forward: rows x (n, width), which may be strided; weight and bias
+        (width,), or None for 1 and 0."""
+        x = self._rows(x, None, self.width, self.dtype, "x")
+        n = self._n(x)
+        weight, bias = self._weights(weight, "weight"), self._weights(bias, "bias")
+        y = self._out(y, (n, self.width), self.dtype, "y")
+        stats = torch.empty((2, n), dtype=torch.float32, device=self.device)
+        mean, rstd = stats.unbind()
+        self._call(self._lib.esspt_norm_forward, x.data_ptr(), _stride(x), n, _ptr(weight), _ptr(bias), y.data_ptr(),
+                   mean.data_ptr(), rstd.data_ptr())
+        return NormResult(y, mean, rstd)
+
+    def backward(self, dy, x, mean, rstd, weight=None, grad_x=None, need_x: bool = True, need_weights: bool = True) -> NormGradients:
+        """esspt_norm_backward: from dy and the x, mean, rstd and weight of a forward pass;
+        need_x and need_weights say which gradients are wanted."""
+        x = self._rows(x, None, self.width, self.dtype, "x")
+        n = self._n(x)
+        dy = self._rows(dy, n, self.width, self.dtype, "dy")
+        mean, rstd = self._values(mean, (n,), torch.float32, "mean"), self._values(rstd, (n,), torch.float32, "rstd")
+        weight = self._weights(weight, "weight")
+        grad_x = self._out(grad_x, (n, self.width), self.dtype, "grad_x") if need_x else None
+        dw = db = None
+        if need_weights:
+            dw, db = torch.empty((2, self.width), dtype=self.weight_dtype, device=self.device).unbind()
+        self._call(self._lib.esspt_norm_backward, dy.data_ptr(), _stride(dy), x.data_ptr(), _stride(x), n, _ptr(weight),
+                   mean.data_ptr(), rstd.data_ptr(), _ptr(grad_x), _ptr(dw), _ptr(db))
+        return NormGradients(grad_x, dw, db)
+
+
+class Moments(NamedTuple):
+    """Of all tensors in flat order (`AdamW.places`): m, and v (32 bits) or sqrt(v) (8 bits, bf16)."""
+
+    m: torch.Tensor
+    second: torch.Tensor
+
+
+class AdamW(_Operator):
+    """AdamW steps over many fp32 tensors at once (one `esspt_adamw` handle).
+
+    `params` are updated in place; where `copies` has a 16-bit tensor, it is rewritten
+    from its parameter and the parameter's gradients are of its type.  `weight_decay`:
+    one for all, or one each.  With `state_bits` 8 moments are held in 8 bits, rounded up or down by a hash of
+    `seed`, the step and the value's place.  The handle keeps references to the tensors.
+    """
+
+    __doc__ += _Operator.__doc__.split("\n", 1)[1]
+    _name = "adamw"
+
+    def __init__(self, params, copies=None, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, state_bits: int = 32,
+                 seed: int = 0, device=None, stream=None):
+        params = list(params)
+        copies = [None] * len(params) if copies is None else list(copies)
+        if device is None and params and isinstance(params[0], torch.Tensor) and params[0].is_cuda:
+            device = params[0].device
+        self._open(torch.float32, device, stream)
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(params)
+        if len(copies) != len(params) or len(decay) != len(params):
+            raise EssptError(EINVAL, f"{len(params)} params, {len(copies)} copies, {len(decay)} weight decays")
+        kinds = {c.dtype for c in copies if isinstance(c, torch.Tensor)}
+        if len(kinds) > 1 or not kinds <= {torch.bfloat16, torch.float16}:
+            raise EssptError(EINVAL, "copies must all be bf16, or all fp16")
+        copy_dtype = kinds.pop() if kinds else torch.bfloat16
+        self.places, self._like, end = [], [], 0
+        recs = (AdamWTensor * max(1, len(params)))()
+        for k, (p, c) in enumerate(zip(params, copies)):
+            self._in_place(p, None, torch.float32, f"params[{k}]")
+            if c is not None:
+                self._in_place(c, p.shape, copy_dtype, f"copies[{k}]")
+            recs[k] = AdamWTensor(_ptr(p), _ptr(c), p.numel(), decay[k])
+            self.places.append(end)
+            self._like.append((p.shape, torch.float32 if c is None else copy_dtype))
+            end += -(-p.numel() // 128) * 128
+        self.params, self.copies, self.state_bits, self.values = params, copies, state_bits, end
+        self._grads = (ctypes.c_void_p * max(1, len(params)))()
+        self._create(ctypes.byref(AdamWConfig(len(params), state_bits, DTYPES[copy_dtype], 0, betas[0], betas[1], eps,
+                                              seed & 0xFFFFFFFFFFFFFFFF, ctypes.c_void_p(self._stream_ptr))), recs)
+
+    def _in_place(self, x, shape, dtype, name) -> None:
+        if not isinstance(x, torch.Tensor) or x.dtype is not dtype or x.device != self.device or not x.is_contiguous() or (
+                shape is not None and x.shape != shape):
+            raise EssptError(EINVAL, f"{name} must be a contiguous {dtype} tensor on {self.device}"
+                             + (f" of shape {tuple(shape)}" if shape is not None else ""))
+
+    def _scalar(self, x, name):
+        if x is None:
+            return None
+        if not isinstance(x, torch.Tensor) or x.dtype is not torch.float32 or x.device != self.device or x.numel() != 1:
+            raise EssptError(EINVAL, f"{name} must be one fp32 value on {self.device}")
+        return x
+
+    def step(self, grads, lr, grad_scale=None) -> None:
+        """esspt_adamw_step: one step along `grads`, one for each parameter, None to leave it as it is.
+        `lr` is a number or one fp32 value on the device, `grad_scale` such a value or None."""
+        if len(grads) != len(self._like):
+            raise EssptError(EINVAL, f"{len(grads)} gradients for {len(self._like)} params")
+        kept, at, on = [], self._grads, self.device
+        for k, (g, (shape, dtype)) in enumerate(zip(grads, self._like)):
+            if g is None:
+                at[k] = None
+                continue
+            if not isinstance(g, torch.Tensor) or g.dtype is not dtype or g.device != on or g.shape != shape:
+                raise EssptError(EINVAL, f"grads[{k}] must be a {dtype} tensor of shape {tuple(shape)} on {on}")
+            if not g.is_contiguous():
+                g = g.contiguous()
+                kept.append(g)
+            at[k] = g.data_ptr()
+        scale = self._scalar(grad_scale, "grad_scale")
+        d_lr = self._scalar(lr, "lr") if isinstance(lr, torch.Tensor) else None
+        self._call(self._lib.esspt_adamw_step, at, 0.0 if d_lr is not None else lr, _ptr(d_lr), _ptr(scale))
+
+    def moments(self) -> Moments:
+        """The moments in flat order: with 32 bits the state itself, with 8 what its codes stand for
+        (esspt_adamw_moments)."""
+        n = self.values
+        if self.state_bits == 32:
+            torch.cuda.current_stream(self.device).wait_stream(self.stream)
+            both = self.workspace[:8 * n].view(torch.float32)
+            return Moments(both[:n], both[n:])
+        m, second = torch.empty((2, n), dtype=torch.bfloat16, device=self.device).unbind()
+        self._call(self._lib.esspt_adamw_moments, m.data_ptr(), second.data_ptr())
+        return Moments(m, second)
+
+    def load(self, m, second, step: int) -> None:
+        """esspt_adamw_load: moments as `moments` gives them (any floating type), and the number of steps taken."""
+        dtype = torch.float32 if self.state_bits == 32 else torch.bfloat16
+        for x in (m, second):
+            if not isinstance(x, torch.Tensor) or x.device != self.device or x.shape != (self.values,) or not x.is_floating_point():
+                raise EssptError(EINVAL, f"moments must be floating-point tensors of shape ({self.values},) on {self.device}")
+        m, second = m.to(dtype).contiguous(), second.to(dtype).contiguous()
+        self._call(self._lib.esspt_adamw_load, m.data_ptr(), second.data_ptr(), step)
+
+    @property
+    def steps(self) -> int:
+        """esspt_adamw_steps: steps taken so far (synchronises)."""
+        n = ctypes.c_int64()
+        self._check(self._lib.esspt_adamw_steps(self._h, ctypes.byref(n)))
+        return n.value

@@ -1,0 +1,237 @@
+"""Layer norm on the GPU, forward and backward, against the definition in fp64.
+
+Tolerances, eps = 2^-24.  A sum over a row goes through at most 64 additions in a thread, 5 in a warp and 32 across
+warps: 101, taken as 128 eps of the sum of magnitudes.  So
+  mean: 128 eps mean|x|;  x - mean: that and eps of itself;  rstd: half of the variance's 2 eps + 128 eps, a square
+  root, a quotient: 70 eps, and half the square of the mean's error in standard deviations;
+  y: |w| (the error of x - mean) rstd + 72 eps |x^ w| + 2 eps (|x^ w| + |b|) + the rounding of the result;
+  dx, from the statistics that the call is given: x^ is off by 3 eps, sums by 128 + 8 eps of their terms' magnitudes:
+  140 eps rstd (|g| + mean|g| + |x^| mean|g x^|) + the rounding;
+  dw, db: a thread's rows (600 at most here), up to 256 groups of a block, 128 blocks of a warp, 8 warps: fewer
+  than n of them are not empty: min(n, 992) + 8 eps of the sum of magnitudes + the rounding.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0**-24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {name: torch.finfo(t).eps / 2 for name, t in TYPES.items()}
+TINY = {"f32": 2.0**-140, "bf16": 2.0**-133, "f16": 2.0**-24}
+
+
+def _esspt():
+    from paper_1410_8043_gb300 import esspt
+
+    return esspt
+
+
+def _inputs(n, D, dtype, wtype, seed, stride=0, offset=1.0):
+    g = torch.Generator("cuda").manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    x = (r(n, D + stride) + offset * r(n, 1)).to(TYPES[dtype])[:, :D]
+    dy = r(n, D + stride).to(TYPES[dtype])[:, :D]
+    return x, dy, (1 + 0.3 * r(D)).to(TYPES[wtype]), (0.3 * r(D)).to(TYPES[wtype])
+
+
+def _check_forward(r, x, w, b, dtype, eps=1e-5):
+    x, w, b = x.double(), (w.double() if w is not None else 1.0), (b.double() if b is not None else 0.0)
+    mean = x.mean(1)
+    d = x - mean[:, None]
+    rstd = 1 / (d.square().mean(1) + eps).sqrt()
+    mean_err = 128 * EPS * x.abs().mean(1)
+    assert bool(((r.mean.double() - mean).abs() <= mean_err + TINY["f32"]).all())
+    assert bool(((r.rstd.double() / rstd - 1).abs() <= 70 * EPS + (mean_err * rstd).square() / 2).all())
+    xh = d * rstd[:, None]
+    off = (mean_err[:, None] + EPS * d.abs()) * rstd[:, None] + (72 * EPS + (mean_err * rstd).square()[:, None]) * xh.abs()
+    want = xh * w + b
+    bw = w.abs() if torch.is_tensor(w) else 1.0
+    bb = b.abs() if torch.is_tensor(b) else 0.0
+    tol = off * bw + 2 * EPS * (xh.abs() * bw + bb) + HALF[dtype] * (1 + 1e-3) * want.abs() + TINY[dtype]
+    err = (r.y.double() - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+def _check_backward(g, dy, x, mean, rstd, w, dtype, wtype):
+    n, D = x.shape
+    dy, x, mean, rstd = dy.double(), x.double(), mean.double()[:, None], rstd.double()[:, None]
+    xh = (x - mean) * rstd
+    gr = dy * (w.double() if w is not None else 1.0)
+    want = rstd * (gr - gr.mean(1, keepdim=True) - xh * (gr * xh).mean(1, keepdim=True))
+    tol = 140 * EPS * rstd * (gr.abs() + gr.abs().mean(1, keepdim=True) + xh.abs() * (gr * xh).abs().mean(1, keepdim=True))
+    tol = tol + HALF[dtype] * (1 + 1e-3) * want.abs() + TINY[dtype]
+    if g.grad_x is not None:
+        err = (g.grad_x.double() - want).abs()
+        assert bool((err <= tol).all()), float((err / tol).max())
+    if g.grad_weight is not None:
+        for got, terms in ((g.grad_weight, dy * xh), (g.grad_bias, dy)):
+            want = terms.sum(0)
+            tol = (min(n, 992) + 8) * EPS * terms.abs().sum(0) + HALF[wtype] * (1 + 1e-3) * want.abs() + TINY[wtype]
+            err = (got.double() - want).abs()
+            assert bool((err <= tol).all()), float((err / tol).max())
+
+
+# Rows of one value to 8192, at and around vectors, warps and blocks; one row to many.
+SHAPES = [(1, 1), (1, 100), (5, 2), (3, 3), (100, 4), (257, 7), (33, 8), (1000, 16), (4096, 100), (77, 127), (513, 128), (64, 255), (1, 256),
+          (300, 257), (999, 512), (65, 513), (130, 1000), (129, 1024), (1, 2048), (700, 2048), (64, 2049), (50, 4095), (40, 4096), (33, 5001),
+          (7, 8191), (330, 8192), (20_001, 33), (60_001, 10)]
+
+
+@pytest.mark.parametrize("dtype, wtype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "f16")])
+@pytest.mark.parametrize("n, D", SHAPES)
+def test_against_fp64(n, D, dtype, wtype):
+    x, dy, w, b = _inputs(n, D, dtype, wtype, n + D, stride=(0, 3, 8)[(n + D) % 3])
+    ln = _esspt().LayerNorm(n, D, dtype=TYPES[dtype], weight_dtype=TYPES[wtype])
+    r = ln.forward(x, w, b)
+    _check_forward(r, x, w, b, dtype)
+    g = ln.backward(dy, x, r.mean, r.rstd, w)
+    _check_backward(g, dy, x, r.mean, r.rstd, w, dtype, wtype)
+    again = ln.backward(dy, x, r.mean, r.rstd, w, grad_x=torch.full_like(g.grad_x, math.nan))
+    assert all(torch.equal(a, c) for a, c in zip(g, again))  # the same bits
+    ln.close()
+
+
+@pytest.mark.parametrize("D", [24, 100, 1000, 4104])
+def test_without_weights_and_parts(D):
+    """No weight or bias; one gradient without the other; fewer rows than the most."""
+    x, dy, w, b = _inputs(50, D, "f32", "f32", D)
+    ln = _esspt().LayerNorm(70, D)
+    for ww, bb in ((None, None), (w, None), (None, b)):
+        r = ln.forward(x, ww, bb)
+        _check_forward(r, x, ww, bb, "f32")
+        _check_backward(ln.backward(dy, x, r.mean, r.rstd, ww), dy, x, r.mean, r.rstd, ww, "f32", "f32")
+    whole = ln.backward(dy, x, r.mean, r.rstd, w)
+    only_x = ln.backward(dy, x, r.mean, r.rstd, w, need_weights=False)
+    only_w = ln.backward(dy, x, r.mean, r.rstd, w, need_x=False)
+    assert only_x.grad_weight is None and torch.equal(only_x.grad_x, whole.grad_x)
+    assert only_w.grad_x is None and torch.equal(only_w.grad_weight, whole.grad_weight) and torch.equal(only_w.grad_bias, whole.grad_bias)
+    none = ln.forward(x[:0], w, b)
+    assert none.y.shape == (0, D)
+    g = ln.backward(dy[:0], x[:0], none.mean, none.rstd, w)
+    assert bool((g.grad_weight == 0).all()) and bool((g.grad_bias == 0).all())
+    ln.close()
+
+
+@pytest.mark.parametrize("D", [12, 200, 3000])
+def test_gradients_against_differences(D):
+    """d/dh of sum(y dy) along a direction: the formula in fp64 by central differences, the kernels' by products.  The
+    differences' own error is of h^2 = 1e-8; the kernels' of 140 eps of magnitudes."""
+    x, dy, w, b = _inputs(30, D, "f32", "f32", 5)
+    ln = _esspt().LayerNorm(30, D)
+    r = ln.forward(x, w, b)
+    g = ln.backward(dy, x, r.mean, r.rstd, w)
+    ln.close()
+    dirs = [torch.randn_like(t).double() for t in (x, w, b)]
+
+    def f(h):
+        X, W, B = (t.double() + h * d for t, d in zip((x, w, b), dirs))
+        d = X - X.mean(1, keepdim=True)
+        return ((d / (d.square().mean(1, keepdim=True) + 1e-5).sqrt() * W + B) * dy.double()).sum()
+
+    h = 1e-4
+    want = (f(h) - f(-h)) / (2 * h)
+    terms = [t.double() * d for t, d in zip(g, dirs)]
+    got, mass = sum(t.sum() for t in terms), sum(t.abs().sum() for t in terms)
+    assert abs(float(got - want)) <= 2e-5 * float(mass)
+
+
+@pytest.mark.parametrize("D", [100, 1000, 4096])
+def test_hard_rows(D):
+    """Equal values give the bias; a far mean; huge and tiny rows; NaN and infinity spoil their own row, and the weights'
+    gradients; rows of zeros."""
+    g = torch.Generator("cuda").manual_seed(2)
+    x = torch.randn((9, D), generator=g, device="cuda")
+    x[0], x[1], x[5] = 0.1, 0.0, -1e30
+    x[2] += 1e4
+    x[3] *= 1e15
+    x[4] *= 1e-18
+    w, b = torch.randn(D, generator=g, device="cuda"), torch.randn(D, generator=g, device="cuda")
+    ln = _esspt().LayerNorm(9, D)
+    r = ln.forward(x, w, b)
+    _check_forward(type(r)(r.y[[0, 1, 2, 3, 4, 6, 7, 8]], r.mean[[0, 1, 2, 3, 4, 6, 7, 8]], r.rstd[[0, 1, 2, 3, 4, 6, 7, 8]]),
+                   x[[0, 1, 2, 3, 4, 6, 7, 8]], w, b, "f32")
+    assert float((r.y[0] - b).abs().max()) <= 1e-4 and torch.equal(r.y[1], b)
+    x[6, D // 2], x[7, 0] = math.nan, math.inf
+    bad = ln.forward(x, w, b)
+    assert bool(torch.isnan(bad.y[[6, 7]]).all()) and torch.equal(bad.y[[0, 1, 2, 3, 4, 8]], r.y[[0, 1, 2, 3, 4, 8]])
+    dy = torch.randn((9, D), generator=g, device="cuda")
+    clean = ln.backward(dy, torch.where(torch.isfinite(x), x, 0.0), r.mean, r.rstd, w)
+    back = ln.backward(dy, x, bad.mean, bad.rstd, w)
+    assert bool(torch.isnan(back.grad_x[[6, 7]]).all()) and torch.equal(back.grad_x[[0, 1, 2, 4, 8]], clean.grad_x[[0, 1, 2, 4, 8]])
+    assert bool(torch.isnan(back.grad_weight).all()) and bool(torch.isfinite(back.grad_bias).all())
+    ln.close()
+
+
+def test_offsets_past_32_bits():
+    n, D = 1_100_000, 2048
+    x = torch.zeros((n, D), dtype=torch.bfloat16, device="cuda")
+    x[-3:] = torch.randn((3, D), device="cuda").to(torch.bfloat16)
+    ln = _esspt().LayerNorm(n, D, dtype=torch.bfloat16)
+    r = ln.forward(x)
+    _check_forward(type(r)(r.y[-4:], r.mean[-4:], r.rstd[-4:]), x[-4:], None, None, "bf16")
+    g = ln.backward(x, x, r.mean, r.rstd, need_weights=False)
+    _check_backward(type(g)(g.grad_x[-4:], None, None), x[-4:], x[-4:], r.mean[-4:], r.rstd[-4:], None, "bf16", "bf16")
+    ln.close()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("D, shift", [(64, 1), (64, 4), (2048, 1), (101, 1)])
+def test_addresses_off_the_vectors(D, shift, dtype):
+    """Rows and weights that begin anywhere in memory."""
+    n = 40
+    buf = torch.randn(3 * n * D + 64, device="cuda").to(TYPES[dtype])
+    x, dy = buf[shift:shift + n * D].view(n, D), buf[n * D + shift:2 * n * D + shift].view(n, D)
+    w, b = buf[-D - 3:-3], buf[-D - 1:-1]
+    ln = _esspt().LayerNorm(n, D, dtype=TYPES[dtype])
+    y = torch.zeros(n * D + 8, dtype=TYPES[dtype], device="cuda")
+    r = ln.forward(x, w, b, y=y[shift:shift + n * D].view(n, D))
+    _check_forward(r, x, w, b, dtype)
+    assert bool((y[:shift] == 0).all()) and bool((y[shift + n * D:] == 0).all())
+    _check_backward(ln.backward(dy, x, r.mean, r.rstd, w), dy, x, r.mean, r.rstd, w, dtype, dtype)
+    ln.close()
+
+
+def test_another_stream_and_a_graph():
+    side = torch.cuda.Stream()
+    n, D = 300, 96
+    ln = _esspt().LayerNorm(n, D, stream=side)
+    x, dy, w, b = _inputs(n, D, "f32", "f32", 3)
+    _check_forward(ln.forward(x, w, b), x, w, b, "f32")
+    u, v = x.clone(), dy.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        r = ln.forward(u, w, b)
+        g = ln.backward(v, u, r.mean, r.rstd, w)
+    for X, Y in ((x, dy), (dy.contiguous(), x), (x, dy)):
+        u.copy_(X), v.copy_(Y)
+        graph.replay()
+        _check_forward(r, u, w, b, "f32")
+        _check_backward(g, v, u, r.mean, r.rstd, w, "f32", "f32")
+    torch.cuda.synchronize()
+    ln.close()
+
+
+def test_refusals():
+    e = _esspt()
+    ln = e.LayerNorm(8, 4, backward=False)
+    x, w = torch.zeros((8, 4), device="cuda"), torch.zeros(4, device="cuda")
+    s = torch.zeros(8, device="cuda")
+    for call in (
+        lambda: e.LayerNorm(0, 4), lambda: e.LayerNorm(8, 9000), lambda: e.LayerNorm(8, 4, eps=0.0),
+        lambda: e.LayerNorm(8, 4, weight_dtype=torch.float16), lambda: e.LayerNorm(8, 4, dtype=torch.float64),
+        lambda: ln.backward(x, x, s, s, w), lambda: ln.forward(x.half(), w, w), lambda: ln.forward(x[:, :3], w, w),
+        lambda: ln.forward(x, w[:3], w), lambda: ln.forward(x, w, w.half()), lambda: ln.forward(x.cpu(), w, w),
+        lambda: ln.forward(torch.zeros((9, 4), device="cuda"), w, w), lambda: ln.forward(x, w, w, y=x[:7]),
+    ):
+        with pytest.raises(e.EssptError):
+            call()
+    ln.close()
+    ln = e.LayerNorm(8, 4)
+    for call in (lambda: ln.backward(x[:7], x, s, s, w), lambda: ln.backward(x, x, s[:7], s, w), lambda: ln.backward(x, x, s, s.half(), w)):
+        with pytest.raises(e.EssptError):
+            call()
+    ln.close()
