@@ -1,7 +1,7 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens: kernels and C-ABI.
-#include <cub/device/device_radix_sort.cuh>
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "operator.h"
 #include "rows.cuh"
@@ -65,64 +65,515 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(Lookup a) {
   }
 }
 
-// Padding sorts behind all rows.
-__global__ void keys_kernel(const int32_t* ids, int64_t n, int32_t V, uint32_t* key, uint32_t* val, uint32_t* status) {
-  const int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (t >= n) return;
-  const int32_t id = ids[t];
-  if (id >= V) atomicOr(status, kErrId);
-  key[t] = (uint32_t)id < (uint32_t)V ? id : V;
-  val[t] = (uint32_t)t;
-}
-
+// ---- the gradient of few tokens: one kernel --------------------------------------------------------------------
+//
+// A block owns a range of the table's rows, of a tile of columns.  It reads all ids, keeps the tokens of its
+// rows, sorts them by row and place in shared memory, and sums them: a row's tokens by one group of lanes, or
+// by all groups in turn where there are more than kLong.
 struct Gradient {
+  const int32_t* ids;
   const void* grad;
   int64_t grad_stride;
-  const uint32_t *key, *val;  // sorted
   int64_t n;
-  int32_t V, D, per_row;
+  int32_t V, D, per_row;  // per_row: vectors of a row
+  int32_t lanes;          // of a group: a power of two
   float scale;
   int accumulate;
   void* out;
+  uint32_t* status;
+  uint2* pairs;           // (row, place) of the tokens, sorted
+  float* part;            // [blocks][2][D]
+  int32_t rows, place_bits;  // (few tokens) rows of a block; bits of a place
 };
 
-__device__ __forceinline__ int64_t lower_bound(const uint32_t* key, int64_t n, uint32_t v) {
-  int64_t lo = 0;
-  while (n > 0) {
-    const int64_t half = n / 2;
-    if (key[lo + half] < v) {
-      lo += half + 1;
-      n -= half + 1;
-    } else {
-      n = half;
-    }
-  }
-  return lo;
-}
+constexpr int kFew = 16384;      // tokens that go this way at most
+constexpr int kFewThreads = 512;
+constexpr int kFewBlocks = 304;  // two for each of 152 SMs
+constexpr int kLong = 32;
 
-// A warp per row of the result.
-template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) gradient_kernel(Gradient a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t v = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-  if (v >= a.V) return;
-  const int64_t begin = lower_bound(a.key, a.n, (uint32_t)v);
-  int64_t end = begin;
-  while (end < a.n && a.key[end] == v) ++end;
-  if (begin == end && a.accumulate) return;
-  const T* grad = static_cast<const T*>(a.grad);
-  T* out = static_cast<T*>(a.out) + v * a.D;
-  for (int c = lane; c < a.per_row; c += 32) {
-    float sum[VEC] = {}, x[VEC];
-    for (int64_t i = begin; i < end; ++i) {
-      load_vec<T, VEC>(grad + a.val[i] * a.grad_stride + c * VEC, x);
+// Writes the sums of a row's columns lane + k * lanes of a tile (in vectors).
+template <typename T, int VEC, int K>
+__device__ __forceinline__ void emit(const Gradient& a, int64_t row, int c0, const float (&sum)[K][VEC]) {
+  T* out = static_cast<T*>(a.out) + row * a.D;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[j] += x[j];
-    }
+  for (int k = 0; k < K; ++k) {
+    const int c = c0 + k * a.lanes;
+    if (c >= a.per_row) break;
+    float x[VEC] = {};
     if (a.accumulate) load_vec<T, VEC>(out + c * VEC, x);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) sum[j] = a.accumulate ? fmaf(sum[j], a.scale, x[j]) : sum[j] * a.scale;
-    store_vec<T, VEC>(out + c * VEC, sum);
+    for (int j = 0; j < VEC; ++j) x[j] = a.accumulate ? fmaf(sum[k][j], a.scale, x[j]) : sum[k][j] * a.scale;
+    store_vec<T, VEC>(out + c * VEC, x);
+  }
+}
+
+// Adds U tokens' rows to `sum`, one behind the other, all loads first; place[u] < 0: none.
+template <typename T, int VEC, int K, int U>
+__device__ __forceinline__ void add_rows(const Gradient& a, const int64_t (&place)[U], int c0, float (&sum)[K][VEC]) {
+  const T* grad = static_cast<const T*>(a.grad);
+  float x[U][K][VEC];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[u][k][j] = 0.f;
+      const int c = c0 + k * a.lanes;
+      if (place[u] >= 0 && c < a.per_row) load_vec<T, VEC>(grad + place[u] * a.grad_stride + c * VEC, x[u][k]);
+    }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum[k][j] += x[u][k][j];
+}
+
+template <typename T, int VEC, int K>
+__global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
+  extern __shared__ uint32_t list[];  // (row in the range, place) of the block's tokens
+  __shared__ uint32_t count, n_long, longs[kFew / kLong];
+  __shared__ float red[kFewThreads * K * VEC];
+  constexpr int U = 8 / K;
+  const int tid = threadIdx.x, lane = tid & (a.lanes - 1), group = tid / a.lanes, groups = kFewThreads / a.lanes;
+  const int c0 = blockIdx.y * a.lanes * K + lane;
+  const int64_t lo = (int64_t)blockIdx.x * a.rows, hi = lo + a.rows < a.V ? lo + a.rows : a.V;
+  if (tid == 0) count = n_long = 0;
+  __syncthreads();
+  for (int64_t i0 = tid; i0 < a.n; i0 += kFewThreads * 8) {
+    int32_t id[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) id[k] = i0 + k * kFewThreads < a.n ? a.ids[i0 + k * kFewThreads] : -1;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (id[k] >= a.V && blockIdx.x == 0) atomicOr(a.status, kErrId);
+      if (id[k] >= lo && id[k] < hi)
+        list[atomicAdd(&count, 1u)] = (uint32_t)(id[k] - lo) << a.place_bits | (uint32_t)(i0 + k * kFewThreads);
+    }
+  }
+  if (!a.accumulate) {  // rows without tokens; the others are written again below
+    const float zero[K][VEC] = {};
+    for (int64_t v = lo + group; v < hi; v += groups) emit<T, VEC, K>(a, v, c0, zero);
+  }
+  __syncthreads();
+  const uint32_t m = count;
+  if (m == 0) return;
+  uint32_t size = 2;
+  while (size < m) size *= 2;
+  for (uint32_t i = m + tid; i < size; i += kFewThreads) list[i] = 0xffffffffu;
+  for (uint32_t run = 2; run <= size; run *= 2)
+    for (uint32_t dist = run / 2; dist > 0; dist /= 2) {
+      __syncthreads();
+      for (uint32_t t = tid; t < size / 2; t += kFewThreads) {
+        const uint32_t i = 2 * t - (t & (dist - 1)), j = i + dist;
+        const uint32_t x = list[i], y = list[j];
+        if ((x > y) == ((i & run) == 0)) list[i] = y, list[j] = x;
+      }
+    }
+  __syncthreads();
+  const uint32_t place_mask = (1u << a.place_bits) - 1;
+  for (uint32_t i = group; i < m; i += groups) {
+    const uint32_t row = list[i] >> a.place_bits;
+    if (i > 0 && list[i - 1] >> a.place_bits == row) continue;
+    uint32_t end = i + 1;
+    while (end < m && end - i <= kLong && list[end] >> a.place_bits == row) ++end;
+    if (end - i > kLong) {
+      if (lane == 0) longs[atomicAdd(&n_long, 1u)] = i;
+      continue;
+    }
+    float sum[K][VEC] = {};
+    for (uint32_t at = i; at < end; at += U) {
+      int64_t place[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) place[u] = at + u < end ? (int64_t)(list[at + u] & place_mask) : -1;
+      add_rows<T, VEC, K, U>(a, place, c0, sum);
+    }
+    emit<T, VEC, K>(a, lo + row, c0, sum);
+  }
+  __syncthreads();
+  for (uint32_t k = 0; k < n_long; ++k) {
+    const uint32_t begin = longs[k], row = list[begin] >> a.place_bits;
+    uint32_t end = begin, left = m - begin;
+    while (left > 0) {
+      const uint32_t half = left / 2;
+      if (list[end + half] >> a.place_bits <= row)
+        end += half + 1, left -= half + 1;
+      else
+        left = half;
+    }
+    float sum[K][VEC] = {};
+    for (uint32_t at = begin + group; at < end; at += U * groups) {
+      int64_t place[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) place[u] = at + u * groups < end ? (int64_t)(list[at + u * groups] & place_mask) : -1;
+      add_rows<T, VEC, K, U>(a, place, c0, sum);
+    }
+#pragma unroll
+    for (int q = 0; q < K * VEC; ++q) red[q * kFewThreads + tid] = sum[q / VEC][q % VEC];
+    for (int s = groups / 2; s > 0; s /= 2) {
+      __syncthreads();
+      if (group < s)
+#pragma unroll
+        for (int q = 0; q < K * VEC; ++q) red[q * kFewThreads + tid] += red[q * kFewThreads + tid + s * a.lanes];
+    }
+    if (group == 0) {
+#pragma unroll
+      for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] = red[q * kFewThreads + tid];
+      emit<T, VEC, K>(a, lo + row, c0, sum);
+    }
+    __syncthreads();
+  }
+}
+
+// ---- many tokens: sorted by row and place, digit by digit -----------------------------------------------------------
+//
+// A pass over a digit of the rows: `count_kernel` counts a tile's tokens by digit, `scan_kernel` turns the
+// counts of a digit into places among its tokens, `move_kernel` moves the tokens there; equal digits keep
+// their order.  Padding has the key V, behind all rows.  While the sort's kernels wait for memory, further blocks of
+// them write the gradient's zeros.
+constexpr int kMostBits = 11, kMostBins = 1 << kMostBits;
+constexpr int kRound = 2048;     // tokens that a block moves at once, 256 a warp
+constexpr int kMostTiles = 1216;
+
+struct Sort {
+  const int32_t* ids;  // first pass; null: `from`
+  const uint2* from;
+  uint2* to;
+  int64_t n;
+  int32_t V;
+  int shift, bins, tiles;
+  int64_t tile;        // tokens of a tile: a multiple of kRound
+  uint32_t* counts;    // [bins][tiles]
+  uint32_t* totals;    // [bins]
+  uint32_t* status;
+  char* zero;          // a share of the gradient, to be set to zero
+  int64_t zero_bytes;
+  int zero_blocks;
+};
+
+__device__ __forceinline__ uint32_t key_of(const Sort& a, int64_t i) {
+  if (!a.ids) return a.from[i].x;
+  const int32_t id = a.ids[i];
+  return (uint32_t)id < (uint32_t)a.V ? (uint32_t)id : (uint32_t)a.V;
+}
+
+// Blocks behind a kernel's own write zeros.
+__device__ void write_zeros(const Sort& a, int block) {
+  const int64_t head = ((16 - (reinterpret_cast<uintptr_t>(a.zero) & 15)) & 15) < a.zero_bytes
+                           ? (16 - (reinterpret_cast<uintptr_t>(a.zero) & 15)) & 15
+                           : a.zero_bytes;
+  const int64_t body = (a.zero_bytes - head) / 16;
+  uint4* to = reinterpret_cast<uint4*>(a.zero + head);
+  const int64_t step = (int64_t)a.zero_blocks * kThreads;
+  int64_t i = (int64_t)block * kThreads + threadIdx.x;
+  for (; i + 3 * step < body; i += 4 * step) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to[i + k * step] = make_uint4(0, 0, 0, 0);
+  }
+  for (; i < body; i += step) to[i] = make_uint4(0, 0, 0, 0);
+  if (block == 0) {
+    for (int64_t k = threadIdx.x * 2; k < head; k += 2 * kThreads) *reinterpret_cast<uint16_t*>(a.zero + k) = 0;
+    for (int64_t k = head + body * 16 + threadIdx.x * 2; k < a.zero_bytes; k += 2 * kThreads)
+      *reinterpret_cast<uint16_t*>(a.zero + k) = 0;
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) count_kernel(Sort a) {
+  __shared__ uint32_t bins[kMostBins];
+  if ((int)blockIdx.x >= a.tiles) return write_zeros(a, blockIdx.x - a.tiles);
+  for (int d = threadIdx.x; d < a.bins; d += kThreads) bins[d] = 0;
+  __syncthreads();
+  const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
+  for (int64_t i = first + threadIdx.x; i < end; i += kThreads) {
+    const uint32_t key = key_of(a, i);
+    if (a.ids && a.ids[i] >= a.V) atomicOr(a.status, kErrId);
+    atomicAdd(&bins[(key >> a.shift) & (a.bins - 1)], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < a.bins; d += kThreads) a.counts[(int64_t)d * a.tiles + blockIdx.x] = bins[d];
+}
+
+// A warp per digit.
+__global__ void __launch_bounds__(kThreads) scan_kernel(Sort a) {
+  const int own = (a.bins + kThreads / 32 - 1) / (kThreads / 32), lane = threadIdx.x & 31;
+  if ((int)blockIdx.x >= own) return write_zeros(a, blockIdx.x - own);
+  const int d = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  if (d >= a.bins) return;
+  uint32_t* row = a.counts + (int64_t)d * a.tiles;
+  uint32_t sum = 0;
+  for (int t0 = 0; t0 < a.tiles; t0 += 32) {
+    const uint32_t c = t0 + lane < a.tiles ? row[t0 + lane] : 0;
+    uint32_t up = c;
+#pragma unroll
+    for (int off = 1; off < 32; off *= 2) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, up, off);
+      if (lane >= off) up += x;
+    }
+    if (t0 + lane < a.tiles) row[t0 + lane] = sum + up - c;
+    sum += __shfl_sync(0xffffffffu, up, 31);
+  }
+  if (lane == 0) a.totals[d] = sum;
+}
+
+__global__ void __launch_bounds__(kThreads) move_kernel(Sort a) {
+  constexpr int kWarps = kThreads / 32, kEach = kRound / kThreads;
+  __shared__ uint32_t place[kMostBins], warp_sum[kWarps];
+  __shared__ uint16_t ahead[kWarps][kMostBins];  // a digit's tokens in a round before a warp's next ones
+  if ((int)blockIdx.x >= a.tiles) return write_zeros(a, blockIdx.x - a.tiles);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  {  // where the digits begin: each thread's run of digits, warps, all
+    const int each = (a.bins + kThreads - 1) / kThreads, d0 = threadIdx.x * each;
+    uint32_t sum = 0;
+    for (int d = d0; d < d0 + each && d < a.bins; ++d) sum += a.totals[d];
+    uint32_t up = sum;
+#pragma unroll
+    for (int off = 1; off < 32; off *= 2) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, up, off);
+      if (lane >= off) up += x;
+    }
+    if (lane == 31) warp_sum[warp] = up;
+    __syncthreads();
+    uint32_t before = up - sum;
+    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    for (int d = d0; d < d0 + each && d < a.bins; ++d) {
+      place[d] = before + a.counts[(int64_t)d * a.tiles + blockIdx.x];
+      before += a.totals[d];
+    }
+  }
+  const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
+  for (int64_t r = first; r < end; r += kRound) {
+    for (int d = lane; d < a.bins; d += 32) ahead[warp][d] = 0;
+    __syncwarp();
+    uint32_t key[kEach], val[kEach], rank[kEach];
+    const int64_t mine = r + warp * (32 * kEach) + lane;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int64_t i = mine + k * 32;
+      key[k] = val[k] = 0;
+      if (i >= end) continue;
+      if (a.ids)
+        key[k] = key_of(a, i), val[k] = (uint32_t)i;
+      else
+        key[k] = a.from[i].x, val[k] = a.from[i].y;
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const bool live = mine + k * 32 < end;
+      const uint32_t d = (key[k] >> a.shift) & (a.bins - 1);
+      const uint32_t same = __match_any_sync(0xffffffffu, live ? d : 0xffffffffu);
+      rank[k] = live ? ahead[warp][d] + __popc(same & ((1u << lane) - 1)) : 0;
+      __syncwarp();
+      if (live && lane == __ffs(same) - 1) ahead[warp][d] += (uint16_t)__popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    uint32_t total[kMostBins / kThreads];
+#pragma unroll
+    for (int j = 0; j < kMostBins / kThreads; ++j) {
+      const int d = threadIdx.x + j * kThreads;
+      if (d >= a.bins) break;
+      uint32_t sum = 0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const uint32_t c = ahead[w][d];
+        ahead[w][d] = (uint16_t)sum;
+        sum += c;
+      }
+      total[j] = sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (mine + k * 32 >= end) continue;
+      const uint32_t d = (key[k] >> a.shift) & (a.bins - 1);
+      a.to[place[d] + ahead[warp][d] + rank[k]] = make_uint2(key[k], val[k]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kMostBins / kThreads; ++j)
+      if (threadIdx.x + j * kThreads < a.bins) place[threadIdx.x + j * kThreads] += total[j];
+  }
+}
+
+// ---- many tokens: the sums ------------------------------------------------------------------------------------
+//
+// A group of lanes adds kChunk sorted tokens.  Rows that begin and end among them are written; the sums of those
+// that do not are joined over the groups of a block, and what crosses blocks goes to `part`: [block][0] the sum of the
+// row that the block's first token shares with the block before, [block][1] of the row that goes on behind the block.
+constexpr int kChunk = 32;
+
+template <typename T, int VEC, int K>
+__global__ void __launch_bounds__(kThreads) sums_kernel(Gradient a) {
+  constexpr int U = 8 / K;
+  __shared__ float head[K * VEC][kThreads], tail[K * VEC][kThreads];
+  __shared__ uint8_t flags[kThreads];  // of a group: 1 a head, 2 a tail, 4 the head is the whole chunk and goes on
+  __shared__ uint32_t tail_key[kThreads];
+  const int tid = threadIdx.x, lane = tid & (a.lanes - 1), group = tid / a.lanes, groups = kThreads / a.lanes;
+  const int c0 = blockIdx.y * a.lanes * K + lane;
+  const int64_t begin = ((int64_t)blockIdx.x * groups + group) * kChunk, end = begin + kChunk < a.n ? begin + kChunk : a.n;
+  float sum[K][VEC] = {};
+  uint32_t f = 0;
+  if (begin < end) {
+    uint32_t row = a.pairs[begin].x;
+    bool shared_row = begin > 0 && a.pairs[begin - 1].x == row;
+    const bool goes_on = end < a.n && a.pairs[end].x == a.pairs[end - 1].x;
+    auto finish = [&]() {
+      if (row >= (uint32_t)a.V) return;
+      if (shared_row) {
+        f |= 1;
+#pragma unroll
+        for (int q = 0; q < K * VEC; ++q) head[q][tid] = sum[q / VEC][q % VEC];
+      } else {
+        emit<T, VEC, K>(a, row, c0, sum);
+      }
+    };
+    for (int64_t i = begin; i < end; i += U) {
+      uint2 p[U];
+      float x[U][K][VEC];
+#pragma unroll
+      for (int u = 0; u < U; ++u) p[u] = i + u < end ? a.pairs[i + u] : make_uint2(0xffffffffu, 0);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) x[u][k][j] = 0.f;
+          const int c = c0 + k * a.lanes;
+          if (p[u].x < (uint32_t)a.V && c < a.per_row)
+            load_vec<T, VEC>(static_cast<const T*>(a.grad) + p[u].y * a.grad_stride + c * VEC, x[u][k]);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i + u >= end) break;
+        if (p[u].x != row) {
+          finish();
+          row = p[u].x;
+          shared_row = false;
+#pragma unroll
+          for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] = 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] += x[u][q / VEC][q % VEC];
+      }
+    }
+    if (!goes_on || row >= (uint32_t)a.V) {
+      finish();
+    } else if (shared_row) {
+      finish();
+      f |= 4;
+    } else {
+      f |= 2;
+#pragma unroll
+      for (int q = 0; q < K * VEC; ++q) tail[q][tid] = sum[q / VEC][q % VEC];
+      if (lane == 0) tail_key[group] = row;
+    }
+  }
+  if (lane == 0) flags[group] = (uint8_t)f;
+  __syncthreads();
+  // Rows shared by the block's groups: from a tail on, and from the block's first token on.
+  for (int from_head = 0; from_head < 2; ++from_head) {
+    if (from_head ? group != 0 || !(flags[0] & 1) : !(flags[group] & 2)) continue;
+    int g = group;
+    bool open = true;
+    if (from_head) {
+#pragma unroll
+      for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] = head[q][tid];
+      open = flags[0] & 4;
+    } else {
+#pragma unroll
+      for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] = tail[q][tid];
+    }
+    while (open && ++g < groups) {
+#pragma unroll
+      for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] += head[q][g * a.lanes + lane];
+      open = flags[g] & 4;
+    }
+    if (!from_head && !open) {
+      emit<T, VEC, K>(a, tail_key[group], c0, sum);
+      continue;
+    }
+    float* to = a.part + (2 * (int64_t)blockIdx.x + (from_head ? 0 : 1)) * a.D;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = c0 + k * a.lanes;
+      if (c >= a.per_row) break;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) to[c * VEC + j] = sum[k][j];
+    }
+  }
+}
+
+// Rows that cross blocks of the sums: a warp for each block in which one begins, all warps in turn for rows of more than
+// kFewParts of them.
+constexpr int kFewParts = 16, kJoinColumns = 128;
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) join_kernel(Gradient a, int64_t block_tokens) {
+  constexpr int kWarps = kThreads / 32, K = kJoinColumns / 32;
+  __shared__ float red[kWarps][kJoinColumns];
+  __shared__ int64_t parts[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, c0 = blockIdx.y * kJoinColumns + lane;
+  const int64_t first = (int64_t)blockIdx.x * kWarps, b = first + warp, end = (b + 1) * block_tokens;
+  int64_t more = 0;  // parts behind the first
+  if (end < a.n) {
+    const uint32_t row = a.pairs[end - 1].x;
+    const bool begins = b == 0 || a.pairs[end - block_tokens - 1].x != row;
+    if (row < (uint32_t)a.V && begins && a.pairs[end].x == row)
+      for (bool on = true; on;) {
+        const int64_t at = end + (more + lane) * block_tokens;  // whether the row goes on into that block
+        const uint32_t yes = __ballot_sync(0xffffffffu, at < a.n && a.pairs[at < a.n ? at : end].x == row);
+        on = yes == 0xffffffffu;
+        more += on ? 32 : __ffs(~yes) - 1;
+      }
+  }
+  if (lane == 0) parts[warp] = more;
+  auto sum_parts = [&](int64_t from, int64_t many, int64_t k0, int step, float (&sum)[K]) {
+    for (int64_t k = k0; k < many; k += 4 * step) {
+      float x[4][K];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int q = 0; q < K; ++q) {
+          const bool live = k + u * step < many && c0 + q * 32 < a.D;
+          x[u][q] = live ? a.part[2 * (from + 1 + k + u * step) * a.D + c0 + q * 32] : 0.f;
+        }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int q = 0; q < K; ++q) sum[q] += x[u][q];
+    }
+  };
+  auto write = [&](int64_t from, const float (&sum)[K]) {
+    T* out = static_cast<T*>(a.out) + (int64_t)a.pairs[(from + 1) * block_tokens - 1].x * a.D;
+#pragma unroll
+    for (int q = 0; q < K; ++q) {
+      const int c = c0 + q * 32;
+      if (c >= a.D) break;
+      const float all = a.part[(2 * from + 1) * a.D + c] + sum[q];
+      out[c] = from_float<T>(a.accumulate ? fmaf(all, a.scale, to_float(out[c])) : all * a.scale);
+    }
+  };
+  if (more > 0 && more <= kFewParts) {
+    float sum[K] = {};
+    sum_parts(b, more, 0, 1, sum);
+    write(b, sum);
+  }
+  __syncthreads();
+  for (int w = 0; w < kWarps; ++w) {
+    if (parts[w] <= kFewParts) continue;
+    float sum[K] = {};
+    sum_parts(first + w, parts[w], warp, kWarps, sum);
+#pragma unroll
+    for (int q = 0; q < K; ++q) red[warp][q * 32 + lane] = sum[q];
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+      for (int q = 0; q < K; ++q)
+#pragma unroll
+        for (int k = 1; k < kWarps; ++k) sum[q] += red[k][q * 32 + lane];
+      write(first + w, sum);
+    }
+    __syncthreads();
   }
 }
 
@@ -141,8 +592,37 @@ int bits_of(uint32_t most) {
   return b;
 }
 
+// Passes of the sort over keys 0..V and bits of a pass's digit.
+struct Digits {
+  int passes, bits;
+};
+Digits digits(int64_t V) {
+  const int all = bits_of((uint32_t)V), passes = (all + kMostBits - 1) / kMostBits;
+  return {passes, (all + passes - 1) / passes};
+}
+
+int64_t tile_tokens(int64_t n) {  // at most kMostTiles tiles
+  const int64_t rounds = (n + (int64_t)kRound * kMostTiles - 1) / ((int64_t)kRound * kMostTiles);
+  return kRound * (rounds > 0 ? rounds : 1);
+}
+
+// Lanes of a group: the power of two that holds a row's `vectors`, up to a warp.
+int lanes_of(int vectors) {
+  int lanes = 1;
+  while (lanes < 32 && lanes < vectors) lanes *= 2;
+  return lanes;
+}
+
+// Whether a call of n tokens goes by one kernel: few of them, and a block's rows and a place fit 32 bits.
+bool does_few(int64_t n, int64_t V, int32_t D) {
+  if (n > kFew) return false;
+  const int columns = (D + 31) / 32;  // at most so many tiles of columns
+  const int64_t blocks = columns < kFewBlocks ? kFewBlocks / columns : 1;
+  return (uint64_t)((V + blocks - 1) / blocks) << bits_of((uint32_t)n - 1) <= 0xffffffffull;
+}
+
 struct Carve {
-  size_t status, key[2], val[2], sort, sort_bytes, total;
+  size_t status, pairs[2], counts, totals, part, total;
 };
 
 Carve carve(const esspt_embed_config& c) {
@@ -154,31 +634,98 @@ Carve carve(const esspt_embed_config& c) {
     return at;
   };
   k.status = take(sizeof(uint32_t));
-  if (c.backward) {
-    for (int i = 0; i < 2; ++i) k.key[i] = take(c.max_tokens * 4), k.val[i] = take(c.max_tokens * 4);
-    cub::DoubleBuffer<uint32_t> none(nullptr, nullptr);
-    cub::DeviceRadixSort::SortPairs(nullptr, k.sort_bytes, none, none, (int)c.max_tokens, 0, bits_of((uint32_t)c.n_rows));
-    k.sort = take(k.sort_bytes);
+  if (c.backward && !does_few(c.max_tokens, c.n_rows, c.width)) {
+    const int64_t n = c.max_tokens, tile = tile_tokens(n);
+    const Digits d = digits(c.n_rows);
+    for (int i = 0; i < 2; ++i) k.pairs[i] = take(n * sizeof(uint2));
+    k.counts = take(((size_t)((n + tile - 1) / tile) << d.bits) * sizeof(uint32_t));
+    k.totals = take(((size_t)1 << d.bits) * sizeof(uint32_t));
+    // a block of the sums has kThreads / lanes groups; most blocks where rows take 32 lanes
+    const int64_t fewest = kThreads / lanes_of(c.width) * kChunk;
+    k.part = take((size_t)((n + fewest - 1) / fewest) * 2 * c.width * sizeof(float));
   }
   k.total = o;
   return k;
 }
 
-// `f` as a kernel of this type and vector width, with the arguments that call() takes.
+// f(type, vector, K) for a type and the bytes that its rows can be read in: 16, or single values, where a lane
+// takes four that lie a group apart.
 template <typename F>
 cudaError_t by_type(int dtype, int bytes, F f) {
-  if (dtype == ESSPT_F32) {
-    if (bytes >= 16) return f((float*)nullptr, std::integral_constant<int, 4>{});
-    return f((float*)nullptr, std::integral_constant<int, 1>{});
+  auto go = [&](auto* type) {
+    using T = std::remove_pointer_t<decltype(type)>;
+    if (bytes >= 16) return f(type, std::integral_constant<int, 16 / sizeof(T)>{}, std::integral_constant<int, 1>{});
+    return f(type, std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+  };
+  if (dtype == ESSPT_F32) return go((float*)nullptr);
+  if (dtype == ESSPT_BF16) return go((__nv_bfloat16*)nullptr);
+  return go((__half*)nullptr);
+}
+
+template <typename T, int VEC, int K>
+cudaError_t launch_few(Gradient a, cudaStream_t st) {
+  a.per_row = a.D / VEC;
+  a.lanes = lanes_of((a.per_row + K - 1) / K);
+  const int columns = (a.per_row + a.lanes * K - 1) / (a.lanes * K);
+  int64_t blocks = kFewBlocks / columns;
+  blocks = blocks < 1 ? 1 : blocks > a.V ? a.V : blocks;
+  a.rows = (int32_t)((a.V + blocks - 1) / blocks);
+  blocks = (a.V + a.rows - 1) / a.rows;
+  a.place_bits = bits_of((uint32_t)a.n - 1);
+  if (((uint64_t)a.rows << a.place_bits) > 0xffffffffull) return cudaErrorInvalidValue;  // (does_few says no)
+  uint32_t size = 2;
+  while (size < a.n) size *= 2;
+  auto* kernel = few_kernel<T, VEC, K>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFew * sizeof(uint32_t));
+  if (e != cudaSuccess) return e;
+  kernel<<<dim3((unsigned)blocks, (unsigned)columns), kFewThreads, size * sizeof(uint32_t), st>>>(a);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_sort(const esspt_embed& em, const Carve& k, Gradient& a) {
+  const Digits d = digits(a.V);
+  auto words = [&](size_t o) { return reinterpret_cast<uint32_t*>(em.base + o); };
+  Sort s{};
+  s.ids = a.ids, s.n = a.n, s.V = a.V, s.bins = 1 << d.bits;
+  s.tile = tile_tokens(a.n), s.tiles = (int)((a.n + s.tile - 1) / s.tile);
+  s.counts = words(k.counts), s.totals = words(k.totals), s.status = a.status;
+  const int64_t bytes = a.accumulate ? 0 : (int64_t)a.V * a.D * (int64_t)size_of(em.cfg.dtype);
+  const int64_t share = (bytes / (3 * d.passes) + 15) & ~(int64_t)15;
+  int64_t zeroed = 0;
+  auto zeros = [&] {  // the next kernel's share
+    s.zero = static_cast<char*>(a.out) + zeroed;
+    s.zero_bytes = bytes - zeroed < share ? bytes - zeroed : share;
+    zeroed += s.zero_bytes;
+    const int64_t blocks = (s.zero_bytes + kThreads * 64 - 1) / (kThreads * 64), most = 4 * em.sms;
+    s.zero_blocks = (int)(blocks < most ? blocks : most);
+    return (unsigned)s.zero_blocks;
+  };
+  for (int pass = 0; pass < d.passes; ++pass) {
+    s.shift = pass * d.bits;
+    s.to = reinterpret_cast<uint2*>(em.base + k.pairs[pass & 1]);
+    unsigned more = zeros();
+    count_kernel<<<s.tiles + more, kThreads, 0, em.st>>>(s);
+    more = zeros();
+    scan_kernel<<<(s.bins + kThreads / 32 - 1) / (kThreads / 32) + more, kThreads, 0, em.st>>>(s);
+    more = zeros();
+    move_kernel<<<s.tiles + more, kThreads, 0, em.st>>>(s);
+    s.ids = nullptr, s.from = s.to;
   }
-  if (dtype == ESSPT_BF16) {
-    if (bytes >= 16) return f((__nv_bfloat16*)nullptr, std::integral_constant<int, 8>{});
-    if (bytes >= 4) return f((__nv_bfloat16*)nullptr, std::integral_constant<int, 2>{});
-    return f((__nv_bfloat16*)nullptr, std::integral_constant<int, 1>{});
-  }
-  if (bytes >= 16) return f((__half*)nullptr, std::integral_constant<int, 8>{});
-  if (bytes >= 4) return f((__half*)nullptr, std::integral_constant<int, 2>{});
-  return f((__half*)nullptr, std::integral_constant<int, 1>{});
+  a.pairs = s.to;
+  return cudaGetLastError();
+}
+
+template <typename T, int VEC, int K>
+cudaError_t launch_sums(Gradient a, cudaStream_t st) {
+  a.per_row = a.D / VEC;
+  a.lanes = lanes_of((a.per_row + K - 1) / K);
+  const int columns = (a.per_row + a.lanes * K - 1) / (a.lanes * K);
+  const int64_t tokens = kThreads / a.lanes * kChunk, blocks = (a.n + tokens - 1) / tokens;
+  sums_kernel<T, VEC, K><<<dim3((unsigned)blocks, (unsigned)columns), kThreads, 0, st>>>(a);
+  constexpr int kWarps = kThreads / 32;
+  join_kernel<T><<<dim3((unsigned)((blocks + kWarps - 1) / kWarps), (unsigned)((a.D + kJoinColumns - 1) / kJoinColumns)), kThreads, 0,
+                   st>>>(a, tokens);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -228,7 +775,7 @@ esspt_status esspt_embed_lookup(esspt_embed* em, const void* d_w, int64_t w_stri
     return em->err.fail(ESSPT_EINVAL, "a pointer is not aligned to its type");
   Lookup a{d_w, w_stride, d_ids, n, (int32_t)c.n_rows, c.width, 0, scale, d_out, reinterpret_cast<uint32_t*>(em->base)};
   const int bytes = vector_bytes(c.width, size, (uintptr_t)d_w | (uintptr_t)d_out | (uintptr_t)w_stride * size);
-  const cudaError_t launched = by_type(c.dtype, bytes, [&](auto* type, auto vec) {
+  const cudaError_t launched = by_type(c.dtype, bytes, [&](auto* type, auto vec, auto) {
     using T = std::remove_pointer_t<decltype(type)>;
     a.per_row = c.width / vec;
     const int64_t blocks = (n * a.per_row + kThreads * kDeep - 1) / (kThreads * kDeep);
@@ -256,22 +803,19 @@ esspt_status esspt_embed_gradient(esspt_embed* em, const int32_t* d_ids, const v
     if (!accumulate) ESSPT_CUDA(em->err, cudaMemsetAsync(d_grad_w, 0, (size_t)c.n_rows * c.width * size, em->st));
     return ESSPT_OK;
   }
-  const Carve k = carve(c);
-  auto at = [&](size_t o) { return reinterpret_cast<uint32_t*>(em->base + o); };
-  cub::DoubleBuffer<uint32_t> key(at(k.key[0]), at(k.key[1])), val(at(k.val[0]), at(k.val[1]));
-  keys_kernel<<<(unsigned)((n + kThreads - 1) / kThreads), kThreads, 0, em->st>>>(d_ids, n, (int32_t)c.n_rows, key.Current(),
-                                                                                  val.Current(), at(k.status));
-  ESSPT_CUDA(em->err, cudaGetLastError());
-  size_t bytes = k.sort_bytes;
-  ESSPT_CUDA(em->err, cub::DeviceRadixSort::SortPairs(em->base + k.sort, bytes, key, val, (int)n, 0,
-                                                      bits_of((uint32_t)c.n_rows), em->st));
-  Gradient a{d_grad, grad_stride, key.Current(), val.Current(), n, (int32_t)c.n_rows, c.width, 0, scale, accumulate, d_grad_w};
-  const int vb = vector_bytes(c.width, size, (uintptr_t)d_grad | (uintptr_t)d_grad_w | (uintptr_t)grad_stride * size);
-  const cudaError_t launched = by_type(c.dtype, vb, [&](auto* type, auto vec) {
+  Gradient a{};
+  a.ids = d_ids, a.grad = d_grad, a.grad_stride = grad_stride, a.n = n, a.V = (int32_t)c.n_rows, a.D = c.width;
+  a.scale = scale, a.accumulate = accumulate != 0, a.out = d_grad_w, a.status = reinterpret_cast<uint32_t*>(em->base);
+  const int bytes = vector_bytes(c.width, size, (uintptr_t)d_grad | (uintptr_t)d_grad_w | (uintptr_t)grad_stride * size);
+  const bool few = does_few(n, c.n_rows, c.width);
+  if (!few) {
+    const Carve k = carve(c);
+    a.part = reinterpret_cast<float*>(em->base + k.part);
+    ESSPT_CUDA(em->err, launch_sort(*em, k, a));
+  }
+  const cudaError_t launched = by_type(c.dtype, bytes, [&](auto* type, auto vec, auto k) {
     using T = std::remove_pointer_t<decltype(type)>;
-    a.per_row = c.width / vec;
-    gradient_kernel<T, vec><<<(unsigned)((c.n_rows + 7) / 8), kThreads, 0, em->st>>>(a);
-    return cudaGetLastError();
+    return few ? launch_few<T, vec, k>(a, em->st) : launch_sums<T, vec, k>(a, em->st);
   });
   ESSPT_CUDA(em->err, launched);
   return ESSPT_OK;
