@@ -1,8 +1,8 @@
 // Layer norm, forward and backward: kernels and C-ABI.
 //
-// A group of `threads` lanes holds a row in registers (a part of a warp, a warp, or a whole
-// block for wide rows), N vectors of VEC values a thread, so that a row is read once: the mean first,
-// then the variance from differences to it.  All arithmetic in fp32.
+// A group of lanes (a part of a warp, a warp, or for wide rows a block) holds a row in registers, N vectors of
+// VEC values a lane, so that a row is read once.  Groups stay and go through rows: their weights stay in registers, and the
+// next row's loads are under way while this one is summed.  All arithmetic is fp32.
 #include <cmath>
 #include <new>
 #include <type_traits>
@@ -24,8 +24,13 @@ namespace {
 
 thread_local Errors g_create;
 
-constexpr int kMaxSms = 256;   // what the workspace is sized for
-constexpr int kBlocksPerSm = 4;  // of the backward pass, whose blocks keep partial sums
+constexpr int kMaxSms = 256;  // what the workspace is sized for
+// Threads of a wide row's block, at most: 256 with up to eight values each, 512 with more.
+constexpr int most_wide(int values) { return values <= 8 ? 256 : 512; }
+constexpr int kMostWarps = 16;
+
+// Threads that an SM holds: with eight values each 64 registers do forward, 80 backward; with more 128.
+constexpr int resident(bool back, int values) { return values > 8 ? 512 : back ? 768 : 1024; }
 
 struct Norm {
   const void *x, *dy;
@@ -40,38 +45,34 @@ struct Norm {
   int want_w;     // whether they are asked for
 };
 
-// The sum over a row's group of threads; `shared` has a float2 for each warp.
-template <bool WIDE>
-__device__ __forceinline__ float2 group_sum(float2 v, int lanes, float2* shared) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    if (!WIDE && off >= lanes) continue;
-    v.x += __shfl_xor_sync(0xffffffffu, v.x, off);
-    v.y += __shfl_xor_sync(0xffffffffu, v.y, off);
-  }
-  if (WIDE) {
-    const int warp = threadIdx.x / 32, warps = blockDim.x / 32;
-    if ((threadIdx.x & 31) == 0) shared[warp] = v;
-    __syncthreads();
-    v = make_float2(0.f, 0.f);
-    for (int i = 0; i < warps; ++i) v.x += shared[i].x, v.y += shared[i].y;
-    __syncthreads();
-  }
-  return v;
-}
-
 template <typename T, int VEC, int N>
-__device__ __forceinline__ void load_row(const T* row, int D, int lane, int lanes, bool live, float (&x)[N][VEC]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int c = (lane + i * lanes) * VEC;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) x[i][j] = 0.f;
-    if (live && c < D) load_vec<T, VEC>(row + c, x[i]);
-  }
-}
+struct Row {
+  struct alignas(VEC * sizeof(T)) Pack {
+    T v[VEC];
+  };
+  Pack p[N];
 
-// Weights by single values: they may stand anywhere, and come from the caches.
+  __device__ __forceinline__ void load(const T* row, int D, int lane, int lanes, bool live) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (lane + i * lanes) * VEC;
+      if (live && c < D) {
+        p[i] = *reinterpret_cast<const Pack*>(row + c);
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) p[i].v[j] = from_float<T>(0.f);
+      }
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[N][VEC]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[i][j] = to_float(p[i].v[j]);
+  }
+};
+
+// Weights by single values: they may stand anywhere, and are read once.
 template <typename W, int VEC, int N>
 __device__ __forceinline__ void load_weights(const void* from, float otherwise, int D, int lane, int lanes, float (&x)[N][VEC]) {
   const W* w = static_cast<const W*>(from);
@@ -84,60 +85,109 @@ __device__ __forceinline__ void load_weights(const void* from, float otherwise, 
     }
 }
 
-template <typename T, typename W, int VEC, int N, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_forward_kernel(Norm a) {
-  __shared__ float2 shared[32];
-  const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
-  const int64_t t = WIDE ? blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / lanes) + threadIdx.x / lanes;
-  const bool live = t < a.n;
-  float x[N][VEC], w[N][VEC], b[N][VEC];
-  load_row<T, VEC, N>(static_cast<const T*>(a.x) + t * a.x_stride, a.D, lane, lanes, live, x);
-  load_weights<W, VEC, N>(a.weight, 1.f, a.D, lane, lanes, w);
-  load_weights<W, VEC, N>(a.bias, 0.f, a.D, lane, lanes, b);
-  float2 s = make_float2(0.f, 0.f);
+// The sum over the lanes of a warp that hold one row.
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) s.x += x[i][j];
-  const float mean = group_sum<WIDE>(s, lanes, shared).x * a.inv_D;
-  s.x = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      x[i][j] -= mean;
-      if ((lane + i * lanes) * VEC + j < a.D) s.x += x[i][j] * x[i][j];
-    }
-  const float rstd = 1.f / sqrtf(group_sum<WIDE>(s, lanes, shared).x * a.inv_D + a.eps);
-  if (!live) return;
-  T* y = static_cast<T*>(a.y) + t * a.D;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int c = (lane + i * lanes) * VEC;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) x[i][j] = x[i][j] * rstd * w[i][j] + b[i][j];
-    if (c < a.D) store_vec<T, VEC>(y + c, x[i]);
+  for (int off = 16; off > 0; off >>= 1) {
+    const float other = __shfl_xor_sync(0xffffffffu, v, off);
+    if (off < lanes) v += other;
   }
-  if (lane == 0 && a.mean) a.mean[t] = mean, a.rstd[t] = rstd;
+  return v;
 }
 
-// Blocks stay and go through rows; a thread's columns are the same in all of them, and it keeps their sums for dw
-// and db.  At the end the groups of a block add theirs, one behind the other.
+
 template <typename T, typename W, int VEC, int N, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_backward_kernel(Norm a) {
-  extern __shared__ float sums[];  // [2][D]
-  __shared__ float2 shared[32];
+__global__ void __launch_bounds__(WIDE ? most_wide(VEC * N) : 256, resident(false, VEC * N) / (WIDE ? most_wide(VEC * N) : 256)) norm_forward_kernel(Norm a) {
+  __shared__ float2 shared[2][kMostWarps];
   const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
-  const int groups = blockDim.x / lanes, group = threadIdx.x / lanes;
+  const int groups = blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
+  const T* rows = static_cast<const T*>(a.x);
+  Row<T, VEC, N> next;
+  int64_t t = (int64_t)blockIdx.x * groups + group;
+  const int64_t step = (int64_t)gridDim.x * groups;
+  next.load(rows + t * a.x_stride, a.D, lane, lanes, t < a.n);
+  float w[N][VEC], b[N][VEC];
+  load_weights<W, VEC, N>(a.weight, 1.f, a.D, lane, lanes, w);
+  load_weights<W, VEC, N>(a.bias, 0.f, a.D, lane, lanes, b);
+  auto count = [&](int warp) {  // values of a warp
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int left = a.D - (warp * 32 + i * lanes) * VEC;
+      c += left < 0 ? 0 : left < 32 * VEC ? left : 32 * VEC;
+    }
+    return (float)c;
+  };
+  const int warp = threadIdx.x / 32, other = threadIdx.x & 31;
+  const float inv_own = WIDE ? 1.f / fmaxf(count(warp), 1.f) : a.inv_D, count_other = WIDE && other < blockDim.x / 32 ? count(other) : 0.f;
+  for (int64_t t0 = (int64_t)blockIdx.x * groups, turn = 0; t0 < a.n; t0 += step, t += step, turn ^= 1) {
+    float x[N][VEC];
+    next.get(x);
+    next.load(rows + (t + step) * a.x_stride, a.D, lane, lanes, t + step < a.n);
+    // Mean and squares of differences to it, of the lanes of a warp.
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) s += x[i][j];
+    s = lanes_sum(s, WIDE ? 32 : lanes);
+    float mean = s * inv_own, m2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float d = x[i][j] - mean;
+        if ((lane + i * lanes) * VEC + j < a.D) m2 += d * d;
+      }
+    m2 = lanes_sum(m2, WIDE ? 32 : lanes);
+    if (WIDE) {
+      // Of the warps: squares about the row's mean are those about a warp's and their distance's.
+      if (other == 0) shared[turn][warp] = make_float2(mean, m2);
+      __syncthreads();  // (the next row's go to the other half)
+      const float2 v = count_other > 0.f ? shared[turn][other] : make_float2(0.f, 0.f);
+      mean = lanes_sum(count_other * v.x, 32) * a.inv_D;
+      m2 = lanes_sum(v.y + count_other * (v.x - mean) * (v.x - mean), 32);
+    }
+    const float rstd = 1.f / sqrtf(m2 * a.inv_D + a.eps);
+    if (t >= a.n) continue;
+    T* y = static_cast<T*>(a.y) + t * a.D;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (lane + i * lanes) * VEC;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[i][j] = (x[i][j] - mean) * rstd * w[i][j] + b[i][j];
+      if (c < a.D) store_vec<T, VEC>(y + c, x[i]);
+    }
+    if (lane == 0 && a.mean) a.mean[t] = mean, a.rstd[t] = rstd;
+  }
+}
+
+// A thread's columns are the same in all rows, and it keeps their sums for dw and db; at the end those of a
+// block are added, the groups of a warp by shuffles, then warp behind warp.
+template <typename T, typename W, int VEC, int N, bool WIDE>
+__global__ void __launch_bounds__(WIDE ? most_wide(VEC * N) : 256, resident(true, VEC * N) / (WIDE ? most_wide(VEC * N) : 256)) norm_backward_kernel(Norm a) {
+  extern __shared__ float sums[];  // [2][D]
+  __shared__ float2 shared[2][kMostWarps];
+  const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
+  const int groups = blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
+  Row<T, VEC, N> next_x, next_dy;
+  int64_t t = (int64_t)blockIdx.x * groups + group;
+  const int64_t step = (int64_t)gridDim.x * groups;
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto load = [&](int64_t at) {
+    const bool live = at < a.n;
+    next_x.load(static_cast<const T*>(a.x) + at * a.x_stride, a.D, lane, lanes, live);
+    next_dy.load(static_cast<const T*>(a.dy) + at * a.dy_stride, a.D, lane, lanes, live);
+    next_mean = live ? a.mean[at] : 0.f, next_rstd = live ? a.rstd[at] : 0.f;
+  };
+  load(t);
   float w[N][VEC], dw[N][VEC] = {}, db[N][VEC] = {};
   load_weights<W, VEC, N>(a.weight, 1.f, a.D, lane, lanes, w);
-  for (int64_t t0 = (int64_t)blockIdx.x * groups; t0 < a.n; t0 += (int64_t)gridDim.x * groups) {
-    const int64_t t = t0 + group;
-    const bool live = t < a.n;
+  for (int64_t t0 = (int64_t)blockIdx.x * groups, turn = 0; t0 < a.n; t0 += step, t += step, turn ^= 1) {
     float x[N][VEC], dy[N][VEC];
-    load_row<T, VEC, N>(static_cast<const T*>(a.x) + t * a.x_stride, a.D, lane, lanes, live, x);
-    load_row<T, VEC, N>(static_cast<const T*>(a.dy) + t * a.dy_stride, a.D, lane, lanes, live, dy);
-    const float mean = live ? a.mean[t] : 0.f, rstd = live ? a.rstd[t] : 0.f;
+    next_x.get(x), next_dy.get(dy);
+    const float mean = next_mean, rstd = next_rstd;
+    load(t + step);
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -149,9 +199,16 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_backward_kernel(Norm a
         dy[i][j] *= w[i][j];
         if ((lane + i * lanes) * VEC + j < a.D) s.x += dy[i][j], s.y += dy[i][j] * x[i][j];
       }
-    s = group_sum<WIDE>(s, lanes, shared);
+    if (!a.y) continue;
+    s = make_float2(lanes_sum(s.x, WIDE ? 32 : lanes), lanes_sum(s.y, WIDE ? 32 : lanes));
+    if (WIDE) {
+      if ((threadIdx.x & 31) == 0) shared[turn][threadIdx.x / 32] = s;
+      __syncthreads();  // (the next row's go to the other half)
+      s = make_float2(0.f, 0.f);
+      for (int k = 0; k < (int)blockDim.x / 32; ++k) s.x += shared[turn][k].x, s.y += shared[turn][k].y;
+    }
     s.x *= a.inv_D, s.y *= a.inv_D;
-    if (!live || !a.y) continue;
+    if (t >= a.n) continue;
     T* dx = static_cast<T*>(a.y) + t * a.D;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -162,38 +219,57 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_backward_kernel(Norm a
     }
   }
   if (!a.want_w) return;
-  for (int k = 0; k < groups; ++k) {
-    if (group == k) {
+  if (!WIDE) {
+    for (int off = 16; off >= lanes; off >>= 1)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          dw[i][j] += __shfl_xor_sync(0xffffffffu, dw[i][j], off);
+          db[i][j] += __shfl_xor_sync(0xffffffffu, db[i][j], off);
+        }
+  }
+  float* part = a.part + (int64_t)blockIdx.x * 2 * a.D;
+  const int warp = WIDE ? 0 : threadIdx.x / 32, warps = WIDE ? 1 : blockDim.x / 32;
+  for (int k = 0; k < warps; ++k) {
+    if (warp == k && (WIDE || (threadIdx.x & 31) < lanes)) {
+      float* to = k == warps - 1 ? part : sums;
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
           const int c = (lane + i * lanes) * VEC + j;
           if (c < a.D) {
-            sums[c] = (k ? sums[c] : 0.f) + dw[i][j];
-            sums[a.D + c] = (k ? sums[a.D + c] : 0.f) + db[i][j];
+            to[c] = (k ? sums[c] : 0.f) + dw[i][j];
+            to[a.D + c] = (k ? sums[a.D + c] : 0.f) + db[i][j];
           }
         }
     }
-    __syncthreads();
+    if (k < warps - 1) __syncthreads();
   }
-  for (int c = threadIdx.x; c < 2 * a.D; c += blockDim.x) a.part[(int64_t)blockIdx.x * 2 * a.D + c] = sums[c];
 }
 
-// dw and db from the blocks' sums: 32 columns to a block, a warp for every eighth block's.
+// dw and db from the blocks' sums: 32 columns to a block, whose warps take every 16th block's.
+constexpr int kWeightWarps = 16;
 template <typename W>
-__global__ void __launch_bounds__(256) norm_weights_kernel(const float* part, int blocks, int D, W* dw, W* db) {
-  __shared__ float sums[8][33];
+__global__ void __launch_bounds__(32 * kWeightWarps) norm_weights_kernel(const float* part, int blocks, int D, W* dw, W* db) {
+  __shared__ float sums[kWeightWarps][33];
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x / 32;
   float s = 0.f;
   if (c < 2 * D)
-    for (int k = warp; k < blocks; k += 8) s += part[(int64_t)k * 2 * D + c];
+    for (int k0 = warp; k0 < blocks; k0 += 8 * kWeightWarps) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = k0 + u * kWeightWarps < blocks ? part[(int64_t)(k0 + u * kWeightWarps) * 2 * D + c] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += x[u];
+    }
   sums[warp][threadIdx.x & 31] = s;
   __syncthreads();
   if (warp || c >= 2 * D) return;
   s = 0.f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) s += sums[k][threadIdx.x];
+  for (int k = 0; k < kWeightWarps; ++k) s += sums[k][threadIdx.x];
   W* to = c < D ? dw : db;
   if (to) to[c < D ? c : c - D] = from_float<W>(s);
 }
@@ -208,60 +284,63 @@ const char* config_fault(const esspt_norm_config* c) {
   return nullptr;
 }
 
-size_t workspace(const esspt_norm_config& c) {
-  return 256 + (c.backward ? up256((size_t)kMaxSms * kBlocksPerSm * 2 * c.width * sizeof(float)) : 0);
-}
-
-// How a row is spread over threads: the threads of a block and of a row, and N.
+// How rows of D values are spread over threads: those of a block and of a row, vectors of a thread (N), and
+// blocks of an SM.
 struct Spread {
-  int threads, lanes, n;
+  int threads, lanes, n, resident;
   bool wide;
 };
-Spread spread(int vectors, int most) {
-  Spread s{256, 32, 1, false};
+Spread spread(int D, int vec, bool back) {
+  const int vectors = (D + vec - 1) / vec;
+  Spread s{256, 32, 1, 0, false};
   if (vectors <= 32) {
     while (s.lanes / 2 >= vectors && s.lanes > 1) s.lanes /= 2;
-  } else if (vectors <= 64 && most >= 2) {
+  } else if (vectors <= 64) {
     s.n = 2;
   } else {
     s.wide = true;
-    s.n = most;
-    while (s.n > 1 && (vectors + s.n / 2 - 1) / (s.n / 2) <= 256) s.n /= 2;
+    while ((vectors + s.n - 1) / s.n > most_wide(s.n * vec)) s.n *= 2;
     s.threads = s.lanes = ((vectors + s.n - 1) / s.n + 31) / 32 * 32;
   }
+  s.resident = resident(back, s.n * vec) / s.threads;
   return s;
 }
 
-template <bool BACK, typename T, typename W, int VEC, int N>
+size_t workspace(const esspt_norm_config& c) {
+  if (!c.backward) return 256;
+  const Spread a = spread(c.width, 16 / (int)size_of(c.dtype), true), b = spread(c.width, 1, true);
+  const size_t blocks = (size_t)kMaxSms * (a.resident > b.resident ? a.resident : b.resident);
+  return 256 + up256(blocks * 2 * c.width * sizeof(float));
+}
+
+template <bool BACK, typename T, typename W, int VEC, int N, bool WIDE>
 cudaError_t launch(const Spread& s, const Norm& a, unsigned blocks, cudaStream_t st) {
-  const size_t shared = BACK ? 2 * a.D * sizeof(float) : 0;
-  if (s.wide) {
-    auto* kernel = BACK ? norm_backward_kernel<T, W, VEC, N, true> : norm_forward_kernel<T, W, VEC, N, true>;
-    if (BACK) {
-      cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * 8192 * 4);
-      if (e != cudaSuccess) return e;
-    }
-    kernel<<<blocks, s.threads, shared, st>>>(a);
-  } else {
-    auto* kernel = BACK ? norm_backward_kernel<T, W, VEC, N, false> : norm_forward_kernel<T, W, VEC, N, false>;
-    kernel<<<blocks, s.threads, shared, st>>>(a);
+  if (!BACK) {
+    norm_forward_kernel<T, W, VEC, N, WIDE><<<blocks, s.threads, 0, st>>>(a);
+    return cudaGetLastError();
   }
+  auto* kernel = norm_backward_kernel<T, W, VEC, N, WIDE>;
+  kernel<<<blocks, s.threads, WIDE ? 0 : 2 * a.D * sizeof(float), st>>>(a);  // (rows of one warp: at most 4 KB)
   return cudaGetLastError();
 }
 
 template <bool BACK, typename T, typename W, int VEC>
 cudaError_t launch_by_size(Norm& a, int sms, unsigned* blocks, cudaStream_t st) {
-  const Spread s = spread((a.D + VEC - 1) / VEC, VEC == 1 ? 8 : VEC == 4 ? 4 : 2);
+  const Spread s = spread(a.D, VEC, BACK);
   a.lanes = s.lanes;
   const int64_t groups = (a.n + s.threads / s.lanes - 1) / (s.threads / s.lanes);
-  *blocks = (unsigned)(BACK && groups > sms * kBlocksPerSm ? sms * kBlocksPerSm : groups);
+  *blocks = (unsigned)(groups > sms * s.resident ? sms * s.resident : groups);
+  if (!s.wide)
+    return s.n == 1 ? launch<BACK, T, W, VEC, 1, false>(s, a, *blocks, st) : launch<BACK, T, W, VEC, 2, false>(s, a, *blocks, st);
   switch (s.n) {
-    case 1: return launch<BACK, T, W, VEC, 1>(s, a, *blocks, st);
-    case 2: return launch<BACK, T, W, VEC, 2>(s, a, *blocks, st);
+    case 1: return launch<BACK, T, W, VEC, 1, true>(s, a, *blocks, st);
+    case 2: return launch<BACK, T, W, VEC, 2, true>(s, a, *blocks, st);
     case 4:
-      if constexpr (VEC <= 4) return launch<BACK, T, W, VEC, 4>(s, a, *blocks, st);
-    default:
-      if constexpr (VEC == 1) return launch<BACK, T, W, VEC, 8>(s, a, *blocks, st);
+      if constexpr (VEC <= 4) return launch<BACK, T, W, VEC, 4, true>(s, a, *blocks, st);
+    case 8:
+      if constexpr (VEC == 1) return launch<BACK, T, W, VEC, 8, true>(s, a, *blocks, st);
+    case 16:
+      if constexpr (VEC == 1) return launch<BACK, T, W, VEC, 16, true>(s, a, *blocks, st);
   }
   return cudaErrorInvalidConfiguration;
 }
@@ -370,12 +449,12 @@ esspt_status esspt_norm_backward(esspt_norm* nm, const void* d_dy, int64_t dy_st
   if (!a.want_w) return ESSPT_OK;
   const unsigned columns = (2 * c.width + 31) / 32;
   if (c.weight_dtype == ESSPT_F32)
-    norm_weights_kernel<<<columns, 256, 0, nm->st>>>(a.part, (int)blocks, c.width, (float*)d_dweight, (float*)d_dbias);
+    norm_weights_kernel<<<columns, 32 * kWeightWarps, 0, nm->st>>>(a.part, (int)blocks, c.width, (float*)d_dweight, (float*)d_dbias);
   else if (c.weight_dtype == ESSPT_BF16)
-    norm_weights_kernel<<<columns, 256, 0, nm->st>>>(a.part, (int)blocks, c.width, (__nv_bfloat16*)d_dweight,
+    norm_weights_kernel<<<columns, 32 * kWeightWarps, 0, nm->st>>>(a.part, (int)blocks, c.width, (__nv_bfloat16*)d_dweight,
                                                      (__nv_bfloat16*)d_dbias);
   else
-    norm_weights_kernel<<<columns, 256, 0, nm->st>>>(a.part, (int)blocks, c.width, (__half*)d_dweight, (__half*)d_dbias);
+    norm_weights_kernel<<<columns, 32 * kWeightWarps, 0, nm->st>>>(a.part, (int)blocks, c.width, (__half*)d_dweight, (__half*)d_dbias);
   ESSPT_CUDA(nm->err, cudaGetLastError());
   return ESSPT_OK;
 }

@@ -648,17 +648,18 @@ class _Operator:
 
     def _call(self, call, *args) -> None:
         """One of the library's calls, in order with the current stream."""
-        current = torch.cuda.current_stream(self.device)
-        elsewhere = current.cuda_stream != self._stream_ptr
-        if elsewhere:
-            self.stream.wait_stream(current)
-        if torch.cuda.current_device() == self.device.index:
-            st = call(self._h, *args)
+        index = self.device.index
+        if torch._C._cuda_getCurrentRawStream(index) == self._stream_ptr and torch._C._cuda_getDevice() == index:
+            st = call(self._h, *args)  # the usual call
         else:
+            current = torch.cuda.current_stream(self.device)
+            elsewhere = current.cuda_stream != self._stream_ptr
+            if elsewhere:
+                self.stream.wait_stream(current)
             with torch.cuda.device(self.device):
                 st = call(self._h, *args)
-        if elsewhere:
-            current.wait_stream(self.stream)
+            if elsewhere:
+                current.wait_stream(self.stream)
         if st != OK:
             self._check(st)
 
@@ -815,8 +816,8 @@ class LayerNorm(_Operator):
         n = self._n(x)
         weight, bias = self._weights(weight, "weight"), self._weights(bias, "bias")
         y = self._out(y, (n, self.width), self.dtype, "y")
-        stats = torch.empty((2, n), dtype=torch.float32, device=self.device)
-        mean, rstd = stats.unbind()
+        mean = torch.empty(n, dtype=torch.float32, device=self.device)
+        rstd = torch.empty_like(mean)
         self._call(self._lib.esspt_norm_forward, x.data_ptr(), _stride(x), n, _ptr(weight), _ptr(bias), y.data_ptr(),
                    mean.data_ptr(), rstd.data_ptr())
         return NormResult(y, mean, rstd)
@@ -832,7 +833,8 @@ class LayerNorm(_Operator):
         grad_x = self._out(grad_x, (n, self.width), self.dtype, "grad_x") if need_x else None
         dw = db = None
         if need_weights:
-            dw, db = torch.empty((2, self.width), dtype=self.weight_dtype, device=self.device).unbind()
+            dw = torch.empty(self.width, dtype=self.weight_dtype, device=self.device)
+            db = torch.empty_like(dw)
         self._call(self._lib.esspt_norm_backward, dy.data_ptr(), _stride(dy), x.data_ptr(), _stride(x), n, _ptr(weight),
                    mean.data_ptr(), rstd.data_ptr(), _ptr(grad_x), _ptr(dw), _ptr(db))
         return NormGradients(grad_x, dw, db)
