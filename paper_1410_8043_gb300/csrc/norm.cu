@@ -1,13 +1,15 @@
 // Layer norm, forward and backward: kernels and C-ABI.
 //
 // A group of lanes (a part of a warp, a warp, or for wide rows a block) holds a row in registers, N vectors of
-// VEC values a lane, so that a row is read once.  Groups stay and go through rows: their weights stay in registers, and the
-// next row's loads are under way while this one is summed.  All arithmetic is fp32.
+// VEC values a lane, so that a row is read once.  Groups stay and go through rows: their weights stay in registers, and
+// each thread's parts of the next rows are copied to its own places in shared memory meanwhile.  All arithmetic is fp32,
+// two values an instruction.
 #include <cmath>
 #include <new>
 #include <type_traits>
 
 #include "operator.h"
+#include "ptx.cuh"
 #include "rows.cuh"
 
 using namespace esspt;
@@ -25,12 +27,9 @@ namespace {
 thread_local Errors g_create;
 
 constexpr int kMaxSms = 256;  // what the workspace is sized for
-// Threads of a wide row's block, at most: 256 with up to eight values each, 512 with more.
-constexpr int most_wide(int values) { return values <= 8 ? 256 : 512; }
-constexpr int kMostWarps = 16;
-
-// Threads that an SM holds: with eight values each 64 registers do forward, 80 backward; with more 128.
-constexpr int resident(bool back, int values) { return values > 8 ? 512 : back ? 768 : 1024; }
+constexpr int kThreads = 256;  // of a block whose rows take a warp or less
+constexpr int kMostWide = 512, kMostWarps = kMostWide / 32;  // of a wide row's block
+constexpr int kMostValues = 16;  // of a thread
 
 struct Norm {
   const void *x, *dy;
@@ -39,53 +38,92 @@ struct Norm {
   int32_t lanes;  // threads of a row: a power of two up to 32, or the block
   float inv_D, eps;
   const void *weight, *bias;
+  int weight_f32;  // their type, where it is not the rows'
   void* y;        // dx in the backward pass
   float *mean, *rstd;
   float* part;    // [blocks][2][D] sums for dw and db
   int want_w;     // whether they are asked for
 };
 
-template <typename T, int VEC, int N>
-struct Row {
-  struct alignas(VEC * sizeof(T)) Pack {
-    T v[VEC];
-  };
-  Pack p[N];
+// A thread's N vectors of a row as pairs of fp32 values (one value alone has a zero beside it).
+template <int VEC, int N>
+constexpr int kPairs = (VEC * N + 1) / 2;
 
-  __device__ __forceinline__ void load(const T* row, int D, int lane, int lanes, bool live) {
+template <typename T, int VEC, int N>
+struct alignas(VEC * sizeof(T)) Pack {
+  T v[VEC];
+};
+
+template <typename T, int VEC, int N>
+__device__ __forceinline__ void to_pairs(const Pack<T, VEC, N> (&p)[N], u64 (&x)[kPairs<VEC, N>]) {
+#pragma unroll
+  for (int q = 0; q < kPairs<VEC, N>; ++q) {
+    const int e = 2 * q, f = e + 1;
+    x[q] = pack2(to_float(p[e / VEC].v[e % VEC]), f < VEC * N ? to_float(p[f % (VEC * N) / VEC].v[f % VEC]) : 0.f);
+  }
+}
+
+// Rows on their way to a thread.  Parts of 4 bytes or more go to shared memory, kDepth - 1 rows ahead; smaller ones
+// stay in registers, a row ahead.  What lies outside a row or the rows reads as zero.
+template <typename T, int VEC, int N>
+struct Incoming {
+  using P = Pack<T, VEC, N>;
+  static constexpr bool kAsync = sizeof(P) >= 4;
+  // (64 bytes a row for 512 threads, two such rows backward: 200 KB of three stages)
+  static constexpr int kDepth = sizeof(P) < 16 ? 2 : N * sizeof(P) < 64 ? 4 : 3;
+  char* slots;
+  P next[kAsync ? 1 : N];
+
+  __device__ __forceinline__ static int bytes(int threads) { return kAsync ? kDepth * N * threads * (int)sizeof(P) : 0; }
+  __device__ __forceinline__ P* slot(int stage, int i) {
+    return reinterpret_cast<P*>(slots) + (stage * N + i) * blockDim.x + threadIdx.x;
+  }
+  __device__ __forceinline__ void fetch(int stage, const T* row, int D, int lane, int lanes, bool live) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = (lane + i * lanes) * VEC;
-      if (live && c < D) {
-        p[i] = *reinterpret_cast<const Pack*>(row + c);
+      if constexpr (sizeof(P) >= 16) {
+        cp_async16_if(slot(stage, i), row + c, live && c < D);
+      } else if constexpr (kAsync) {
+        cp_async4_if(slot(stage, i), row + c, live && c < D);
       } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) p[i].v[j] = from_float<T>(0.f);
+        next[i].v[0] = live && c < D ? row[c] : from_float<T>(0.f);
       }
     }
   }
-  __device__ __forceinline__ void get(float (&x)[N][VEC]) const {
+  __device__ __forceinline__ void take(int stage, int D, int lane, int lanes, bool live, u64 (&x)[kPairs<VEC, N>]) {
+    P p[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) {
+      if constexpr (kAsync) {
+        p[i] = *slot(stage, i);
+        if (!live || (lane + i * lanes) * VEC >= D) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) x[i][j] = to_float(p[i].v[j]);
+          for (int j = 0; j < VEC; ++j) p[i].v[j] = from_float<T>(0.f);
+        }
+      } else {
+        p[i] = next[i];
+      }
+    }
+    to_pairs<T, VEC, N>(p, x);
   }
 };
 
 // Weights by single values: they may stand anywhere, and are read once.
-template <typename W, int VEC, int N>
-__device__ __forceinline__ void load_weights(const void* from, float otherwise, int D, int lane, int lanes, float (&x)[N][VEC]) {
-  const W* w = static_cast<const W*>(from);
+template <typename T, int VEC, int N>
+__device__ __forceinline__ void load_weights(const Norm& a, const void* from, float otherwise, int lane, u64 (&x)[kPairs<VEC, N>]) {
+  float w[2 * kPairs<VEC, N>];
 #pragma unroll
-  for (int i = 0; i < N; ++i)
+  for (int e = 0; e < 2 * kPairs<VEC, N>; ++e) {
+    const int c = (lane + e / VEC * a.lanes) * VEC + e % VEC;
+    w[e] = otherwise;
+    if (from && e < VEC * N && c < a.D) w[e] = a.weight_f32 ? static_cast<const float*>(from)[c] : to_float(static_cast<const T*>(from)[c]);
+  }
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      const int c = (lane + i * lanes) * VEC + j;
-      x[i][j] = w && c < D ? to_float(w[c]) : otherwise;
-    }
+  for (int q = 0; q < kPairs<VEC, N>; ++q) x[q] = pack2(w[2 * q], w[2 * q + 1]);
 }
 
-// The sum over the lanes of a warp that hold one row.
+// The sum over the lanes of a warp that hold one row; of up to kMostWarps of them.
 __device__ __forceinline__ float lanes_sum(float v, int lanes) {
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) {
@@ -94,21 +132,48 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
   }
   return v;
 }
+__device__ __forceinline__ float warps_sum(float v) {
+#pragma unroll
+  for (int off = kMostWarps / 2; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+  return v;
+}
 
+template <typename T, int VEC, int N>
+__device__ __forceinline__ void store_pairs(T* row, int D, int lane, int lanes, const u64 (&x)[kPairs<VEC, N>]) {
+  float v[2 * kPairs<VEC, N>];
+#pragma unroll
+  for (int q = 0; q < kPairs<VEC, N>; ++q) unpack2(x[q], v[2 * q], v[2 * q + 1]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (lane + i * lanes) * VEC;
+    float out[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) out[j] = v[i * VEC + j];
+    if (c < D) store_vec<T, VEC>(row + c, out);
+  }
+}
 
-template <typename T, typename W, int VEC, int N, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? most_wide(VEC * N) : 256, resident(false, VEC * N) / (WIDE ? most_wide(VEC * N) : 256)) norm_forward_kernel(Norm a) {
+template <typename T, int VEC, int N, bool WIDE>
+__global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_forward_kernel(Norm a) {
+  extern __shared__ __align__(16) char dynamic[];
   __shared__ float2 shared[2][kMostWarps];
+  constexpr int Q = kPairs<VEC, N>;
+  using In = Incoming<T, VEC, N>;
   const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
-  const int groups = blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
+  const int groups = WIDE ? 1 : blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
   const T* rows = static_cast<const T*>(a.x);
-  Row<T, VEC, N> next;
+  In in;
+  in.slots = dynamic;
   int64_t t = (int64_t)blockIdx.x * groups + group;
   const int64_t step = (int64_t)gridDim.x * groups;
-  next.load(rows + t * a.x_stride, a.D, lane, lanes, t < a.n);
-  float w[N][VEC], b[N][VEC];
-  load_weights<W, VEC, N>(a.weight, 1.f, a.D, lane, lanes, w);
-  load_weights<W, VEC, N>(a.bias, 0.f, a.D, lane, lanes, b);
+#pragma unroll
+  for (int k = 0; k < In::kDepth - 1; ++k) {
+    in.fetch(k, rows + (t + k * step) * a.x_stride, a.D, lane, lanes, t + k * step < a.n);
+    cp_async_commit();
+  }
+  u64 w[Q], b[Q];
+  load_weights<T, VEC, N>(a, a.weight, 1.f, lane, w);
+  load_weights<T, VEC, N>(a, a.bias, 0.f, lane, b);
   auto count = [&](int warp) {  // values of a warp
     int c = 0;
 #pragma unroll
@@ -118,132 +183,167 @@ __global__ void __launch_bounds__(WIDE ? most_wide(VEC * N) : 256, resident(fals
     }
     return (float)c;
   };
-  const int warp = threadIdx.x / 32, other = threadIdx.x & 31;
-  const float inv_own = WIDE ? 1.f / fmaxf(count(warp), 1.f) : a.inv_D, count_other = WIDE && other < blockDim.x / 32 ? count(other) : 0.f;
-  for (int64_t t0 = (int64_t)blockIdx.x * groups, turn = 0; t0 < a.n; t0 += step, t += step, turn ^= 1) {
-    float x[N][VEC];
-    next.get(x);
-    next.load(rows + (t + step) * a.x_stride, a.D, lane, lanes, t + step < a.n);
+  const int warp = threadIdx.x / 32, other = threadIdx.x & (kMostWarps - 1);
+  const float inv_own = WIDE ? 1.f / fmaxf(count(warp), 1.f) : a.inv_D;
+  const float count_other = WIDE && other < blockDim.x / 32 ? count(other) : 0.f;
+  int stage = 0, turn = 0;
+  for (int64_t t0 = (int64_t)blockIdx.x * groups; t0 < a.n; t0 += step, t += step, turn ^= 1) {
+    u64 x[Q];
+    if (In::kAsync) {
+      in.fetch((stage + In::kDepth - 1) % In::kDepth, rows + (t + (In::kDepth - 1) * step) * a.x_stride, a.D, lane, lanes,
+               t + (In::kDepth - 1) * step < a.n);
+      cp_async_commit();
+      cp_async_wait<In::kDepth - 1>();
+    }
+    in.take(stage, a.D, lane, lanes, t < a.n, x);
+    if (!In::kAsync) in.fetch(0, rows + (t + step) * a.x_stride, a.D, lane, lanes, t + step < a.n);
+    stage = (stage + 1) % In::kDepth;
     // Mean and squares of differences to it, of the lanes of a warp.
-    float s = 0.f;
+    u64 sum = x[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int q = 1; q < Q; ++q) sum = add2(sum, x[q]);
+    float mean = lanes_sum(sum2(sum), WIDE ? 32 : lanes) * inv_own;
+    const u64 minus = pack2(-mean, -mean);
+    u64 squares = 0;
+    float single = 0.f;  // (of vectors of one value each its own)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) s += x[i][j];
-    s = lanes_sum(s, WIDE ? 32 : lanes);
-    float mean = s * inv_own, m2 = 0.f;
+    for (int i = 0; i < N; ++i) {
+      if ((lane + i * lanes) * VEC >= a.D) continue;
+      if constexpr (VEC == 1) {
+        float lo, hi;
+        unpack2(x[i / 2], lo, hi);
+        const float d = (i % 2 ? hi : lo) - mean;
+        single = fmaf(d, d, single);
+      } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float d = x[i][j] - mean;
-        if ((lane + i * lanes) * VEC + j < a.D) m2 += d * d;
+        for (int q = i * VEC / 2; q < (i + 1) * VEC / 2; ++q) {
+          const u64 d = add2(x[q], minus);
+          squares = fma2(d, d, squares);
+        }
       }
-    m2 = lanes_sum(m2, WIDE ? 32 : lanes);
+    }
+    float m2 = lanes_sum(sum2(squares) + single, WIDE ? 32 : lanes);
     if (WIDE) {
       // Of the warps: squares about the row's mean are those about a warp's and their distance's.
-      if (other == 0) shared[turn][warp] = make_float2(mean, m2);
+      if ((threadIdx.x & 31) == 0) shared[turn][warp] = make_float2(mean, m2);
       __syncthreads();  // (the next row's go to the other half)
       const float2 v = count_other > 0.f ? shared[turn][other] : make_float2(0.f, 0.f);
-      mean = lanes_sum(count_other * v.x, 32) * a.inv_D;
-      m2 = lanes_sum(v.y + count_other * (v.x - mean) * (v.x - mean), 32);
+      mean = warps_sum(count_other * v.x) * a.inv_D;
+      m2 = warps_sum(v.y + count_other * (v.x - mean) * (v.x - mean));
     }
     const float rstd = 1.f / sqrtf(m2 * a.inv_D + a.eps);
     if (t >= a.n) continue;
-    T* y = static_cast<T*>(a.y) + t * a.D;
+    const u64 m = pack2(-mean, -mean), r = pack2(rstd, rstd);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = (lane + i * lanes) * VEC;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) x[i][j] = (x[i][j] - mean) * rstd * w[i][j] + b[i][j];
-      if (c < a.D) store_vec<T, VEC>(y + c, x[i]);
-    }
+    for (int q = 0; q < Q; ++q) x[q] = fma2(mul2(add2(x[q], m), r), w[q], b[q]);
+    store_pairs<T, VEC, N>(static_cast<T*>(a.y) + t * a.D, a.D, lane, lanes, x);
     if (lane == 0 && a.mean) a.mean[t] = mean, a.rstd[t] = rstd;
   }
 }
 
 // A thread's columns are the same in all rows, and it keeps their sums for dw and db; at the end those of a
 // block are added, the groups of a warp by shuffles, then warp behind warp.
-template <typename T, typename W, int VEC, int N, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? most_wide(VEC * N) : 256, resident(true, VEC * N) / (WIDE ? most_wide(VEC * N) : 256)) norm_backward_kernel(Norm a) {
-  extern __shared__ float sums[];  // [2][D]
+template <typename T, int VEC, int N, bool WIDE>
+__global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_backward_kernel(Norm a) {
+  extern __shared__ __align__(16) char dynamic[];
   __shared__ float2 shared[2][kMostWarps];
+  constexpr int Q = kPairs<VEC, N>;
+  using In = Incoming<T, VEC, N>;
   const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
-  const int groups = blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
-  Row<T, VEC, N> next_x, next_dy;
+  const int groups = WIDE ? 1 : blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
+  In in_x, in_dy;
+  in_x.slots = dynamic;
+  in_dy.slots = dynamic + In::bytes(blockDim.x);
+  float2* stats = reinterpret_cast<float2*>(dynamic + 2 * In::bytes(blockDim.x)) + threadIdx.x;  // [kDepth][threads]
   int64_t t = (int64_t)blockIdx.x * groups + group;
   const int64_t step = (int64_t)gridDim.x * groups;
-  float next_mean = 0.f, next_rstd = 0.f;
-  auto load = [&](int64_t at) {
+  float2 next_stats = make_float2(0.f, 0.f);
+  auto fetch = [&](int stage, int64_t at) {
     const bool live = at < a.n;
-    next_x.load(static_cast<const T*>(a.x) + at * a.x_stride, a.D, lane, lanes, live);
-    next_dy.load(static_cast<const T*>(a.dy) + at * a.dy_stride, a.D, lane, lanes, live);
-    next_mean = live ? a.mean[at] : 0.f, next_rstd = live ? a.rstd[at] : 0.f;
+    in_x.fetch(stage, static_cast<const T*>(a.x) + at * a.x_stride, a.D, lane, lanes, live);
+    in_dy.fetch(stage, static_cast<const T*>(a.dy) + at * a.dy_stride, a.D, lane, lanes, live);
+    if (In::kAsync) {
+      cp_async4_if(&stats[stage * blockDim.x].x, a.mean + at, live);
+      cp_async4_if(&stats[stage * blockDim.x].y, a.rstd + at, live);
+      cp_async_commit();
+    } else {
+      next_stats = live ? make_float2(a.mean[at], a.rstd[at]) : make_float2(0.f, 0.f);
+    }
   };
-  load(t);
-  float w[N][VEC], dw[N][VEC] = {}, db[N][VEC] = {};
-  load_weights<W, VEC, N>(a.weight, 1.f, a.D, lane, lanes, w);
-  for (int64_t t0 = (int64_t)blockIdx.x * groups, turn = 0; t0 < a.n; t0 += step, t += step, turn ^= 1) {
-    float x[N][VEC], dy[N][VEC];
-    next_x.get(x), next_dy.get(dy);
-    const float mean = next_mean, rstd = next_rstd;
-    load(t + step);
-    float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+  for (int k = 0; k < In::kDepth - 1; ++k) fetch(k, t + k * step);
+  u64 w[Q], dw[Q], db[Q];
+  load_weights<T, VEC, N>(a, a.weight, 1.f, lane, w);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        x[i][j] = (x[i][j] - mean) * rstd;
-        dw[i][j] += dy[i][j] * x[i][j];
-        db[i][j] += dy[i][j];
-        dy[i][j] *= w[i][j];
-        if ((lane + i * lanes) * VEC + j < a.D) s.x += dy[i][j], s.y += dy[i][j] * x[i][j];
-      }
+  for (int q = 0; q < Q; ++q) dw[q] = db[q] = 0;
+  int stage = 0, turn = 0;
+  for (int64_t t0 = (int64_t)blockIdx.x * groups; t0 < a.n; t0 += step, t += step, turn ^= 1) {
+    u64 x[Q], dy[Q];
+    if (In::kAsync) {
+      fetch((stage + In::kDepth - 1) % In::kDepth, t + (In::kDepth - 1) * step);
+      cp_async_wait<In::kDepth - 1>();
+    }
+    in_x.take(stage, a.D, lane, lanes, t < a.n, x);
+    in_dy.take(stage, a.D, lane, lanes, t < a.n, dy);
+    float2 s = In::kAsync ? stats[stage * blockDim.x] : next_stats;
+    if (t >= a.n) s = make_float2(0.f, 0.f);
+    if (!In::kAsync) fetch(0, t + step);
+    stage = (stage + 1) % In::kDepth;
+    const float rstd = s.y;
+    const u64 m = pack2(-s.x, -s.x), r = pack2(rstd, rstd);
+    u64 sum_g = 0, sum_gx = 0;  // (outside a row dy is zero)
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      x[q] = mul2(add2(x[q], m), r);
+      dw[q] = fma2(dy[q], x[q], dw[q]);
+      db[q] = add2(dy[q], db[q]);
+      dy[q] = mul2(dy[q], w[q]);
+      sum_g = add2(sum_g, dy[q]);
+      sum_gx = fma2(dy[q], x[q], sum_gx);
+    }
     if (!a.y) continue;
-    s = make_float2(lanes_sum(s.x, WIDE ? 32 : lanes), lanes_sum(s.y, WIDE ? 32 : lanes));
+    s = make_float2(lanes_sum(sum2(sum_g), WIDE ? 32 : lanes), lanes_sum(sum2(sum_gx), WIDE ? 32 : lanes));
     if (WIDE) {
+      const int other = threadIdx.x & (kMostWarps - 1);
       if ((threadIdx.x & 31) == 0) shared[turn][threadIdx.x / 32] = s;
       __syncthreads();  // (the next row's go to the other half)
-      s = make_float2(0.f, 0.f);
-      for (int k = 0; k < (int)blockDim.x / 32; ++k) s.x += shared[turn][k].x, s.y += shared[turn][k].y;
+      s = other < blockDim.x / 32 ? shared[turn][other] : make_float2(0.f, 0.f);
+      s = make_float2(warps_sum(s.x), warps_sum(s.y));
     }
-    s.x *= a.inv_D, s.y *= a.inv_D;
     if (t >= a.n) continue;
-    T* dx = static_cast<T*>(a.y) + t * a.D;
+    const u64 g = pack2(-s.x * a.inv_D, -s.x * a.inv_D), gx = pack2(-s.y * a.inv_D, -s.y * a.inv_D);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = (lane + i * lanes) * VEC;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) x[i][j] = rstd * (dy[i][j] - s.x - x[i][j] * s.y);
-      if (c < a.D) store_vec<T, VEC>(dx + c, x[i]);
-    }
+    for (int q = 0; q < Q; ++q) x[q] = mul2(add2(fma2(x[q], gx, dy[q]), g), r);
+    store_pairs<T, VEC, N>(static_cast<T*>(a.y) + t * a.D, a.D, lane, lanes, x);
   }
   if (!a.want_w) return;
+  float* sums = reinterpret_cast<float*>(dynamic);  // [2][D] (rows of a warp: the copies' places, which are done with)
   if (!WIDE) {
     for (int off = 16; off >= lanes; off >>= 1)
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          dw[i][j] += __shfl_xor_sync(0xffffffffu, dw[i][j], off);
-          db[i][j] += __shfl_xor_sync(0xffffffffu, db[i][j], off);
-        }
+      for (int q = 0; q < Q; ++q) {
+        dw[q] = add2(dw[q], __shfl_xor_sync(0xffffffffu, dw[q], off));
+        db[q] = add2(db[q], __shfl_xor_sync(0xffffffffu, db[q], off));
+      }
+    cp_async_wait_all();
+    __syncthreads();
   }
   float* part = a.part + (int64_t)blockIdx.x * 2 * a.D;
   const int warp = WIDE ? 0 : threadIdx.x / 32, warps = WIDE ? 1 : blockDim.x / 32;
   for (int k = 0; k < warps; ++k) {
     if (warp == k && (WIDE || (threadIdx.x & 31) < lanes)) {
       float* to = k == warps - 1 ? part : sums;
+      float v[2 * Q], u[2 * Q];
 #pragma unroll
-      for (int i = 0; i < N; ++i)
+      for (int q = 0; q < Q; ++q) unpack2(dw[q], v[2 * q], v[2 * q + 1]), unpack2(db[q], u[2 * q], u[2 * q + 1]);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const int c = (lane + i * lanes) * VEC + j;
-          if (c < a.D) {
-            to[c] = (k ? sums[c] : 0.f) + dw[i][j];
-            to[a.D + c] = (k ? sums[a.D + c] : 0.f) + db[i][j];
-          }
+      for (int e = 0; e < VEC * N; ++e) {
+        const int c = (lane + e / VEC * lanes) * VEC + e % VEC;
+        if (c < a.D) {
+          to[c] = (k ? sums[c] : 0.f) + v[e];
+          to[a.D + c] = (k ? sums[a.D + c] : 0.f) + u[e];
         }
+      }
     }
     if (k < warps - 1) __syncthreads();
   }
@@ -291,18 +391,24 @@ struct Spread {
   bool wide;
 };
 Spread spread(int D, int vec, bool back) {
-  const int vectors = (D + vec - 1) / vec;
-  Spread s{256, 32, 1, 0, false};
-  if (vectors <= 32) {
+  const int vectors = (D + vec - 1) / vec, most = kMostValues / vec;
+  Spread s{kThreads, 32, 1, 0, false};
+  auto next = [vec](int n) { return vec == 1 ? n * 4 : n * 2; };  // 1, 4, 16 single values; 1, 2, 4 vectors
+  if (vectors <= 32 * most) {
+    while (s.n * 32 < vectors) s.n = next(s.n);
     while (s.lanes / 2 >= vectors && s.lanes > 1) s.lanes /= 2;
-  } else if (vectors <= 64) {
-    s.n = 2;
   } else {
+    // the fewest idle lanes, where a thread's work for a row is about its values' and eight values' more
+    int best = 1 << 30;
+    for (int n = 1; n <= most; n = next(n)) {
+      const int threads = ((vectors + n - 1) / n + 31) / 32 * 32, cost = threads * (n * vec + 8);
+      if (threads <= kMostWide && cost <= best) best = cost, s.n = n, s.threads = threads;
+    }
     s.wide = true;
-    while ((vectors + s.n - 1) / s.n > most_wide(s.n * vec)) s.n *= 2;
-    s.threads = s.lanes = ((vectors + s.n - 1) / s.n + 31) / 32 * 32;
+    s.lanes = s.threads;
   }
-  s.resident = resident(back, s.n * vec) / s.threads;
+  // by registers: up to 64 with eight values; with 16 up to 80 forward, 120 backward (single values: 128)
+  s.resident = (s.n * vec <= 8 ? 1024 : vec > 1 && !back ? 768 : 512) / s.threads;
   return s;
 }
 
@@ -313,53 +419,53 @@ size_t workspace(const esspt_norm_config& c) {
   return 256 + up256(blocks * 2 * c.width * sizeof(float));
 }
 
-template <bool BACK, typename T, typename W, int VEC, int N, bool WIDE>
+template <bool BACK, typename T, int VEC, int N, bool WIDE>
 cudaError_t launch(const Spread& s, const Norm& a, unsigned blocks, cudaStream_t st) {
-  if (!BACK) {
-    norm_forward_kernel<T, W, VEC, N, WIDE><<<blocks, s.threads, 0, st>>>(a);
-    return cudaGetLastError();
+  using In = Incoming<T, VEC, N>;
+  const size_t row = In::kAsync ? (size_t)In::kDepth * N * s.threads * VEC * sizeof(T) : 0;
+  auto* kernel = BACK ? norm_backward_kernel<T, VEC, N, WIDE> : norm_forward_kernel<T, VEC, N, WIDE>;
+  size_t shared = BACK ? 2 * row + (In::kAsync ? In::kDepth * s.threads * sizeof(float2) : 0) : row;
+  if (BACK && !WIDE && shared < 2 * a.D * sizeof(float)) shared = 2 * a.D * sizeof(float);
+  if (shared > 47 * 1024) {  // (static shared memory counts too)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    if (e != cudaSuccess) return e;
   }
-  auto* kernel = norm_backward_kernel<T, W, VEC, N, WIDE>;
-  kernel<<<blocks, s.threads, WIDE ? 0 : 2 * a.D * sizeof(float), st>>>(a);  // (rows of one warp: at most 4 KB)
+  kernel<<<blocks, s.threads, shared, st>>>(a);
   return cudaGetLastError();
 }
 
-template <bool BACK, typename T, typename W, int VEC>
+template <bool BACK, typename T, int VEC>
 cudaError_t launch_by_size(Norm& a, int sms, unsigned* blocks, cudaStream_t st) {
   const Spread s = spread(a.D, VEC, BACK);
   a.lanes = s.lanes;
   const int64_t groups = (a.n + s.threads / s.lanes - 1) / (s.threads / s.lanes);
   *blocks = (unsigned)(groups > sms * s.resident ? sms * s.resident : groups);
-  if (!s.wide)
-    return s.n == 1 ? launch<BACK, T, W, VEC, 1, false>(s, a, *blocks, st) : launch<BACK, T, W, VEC, 2, false>(s, a, *blocks, st);
-  switch (s.n) {
-    case 1: return launch<BACK, T, W, VEC, 1, true>(s, a, *blocks, st);
-    case 2: return launch<BACK, T, W, VEC, 2, true>(s, a, *blocks, st);
-    case 4:
-      if constexpr (VEC <= 4) return launch<BACK, T, W, VEC, 4, true>(s, a, *blocks, st);
-    case 8:
-      if constexpr (VEC == 1) return launch<BACK, T, W, VEC, 8, true>(s, a, *blocks, st);
-    case 16:
-      if constexpr (VEC == 1) return launch<BACK, T, W, VEC, 16, true>(s, a, *blocks, st);
+  auto go = [&](auto n) {
+    return s.wide ? launch<BACK, T, VEC, n, true>(s, a, *blocks, st) : launch<BACK, T, VEC, n, false>(s, a, *blocks, st);
+  };
+  if (s.n == 1) return go(std::integral_constant<int, 1>{});
+  if constexpr (VEC > 1) {
+    if (s.n == 2) return go(std::integral_constant<int, 2>{});
+  }
+  if constexpr (VEC <= 4) {
+    if (s.n == 4) return go(std::integral_constant<int, 4>{});
+  }
+  if constexpr (VEC == 1) {
+    if (s.n == 16) return go(std::integral_constant<int, 16>{});
   }
   return cudaErrorInvalidConfiguration;
 }
 
-template <bool BACK, typename T, typename W>
-cudaError_t launch_by_width(Norm& a, int bytes, int sms, unsigned* blocks, cudaStream_t st) {
-  if (bytes >= 16) return launch_by_size<BACK, T, W, 16 / sizeof(T)>(a, sms, blocks, st);
-  return launch_by_size<BACK, T, W, 1>(a, sms, blocks, st);
-}
-
 template <bool BACK>
 cudaError_t launch_norm(const esspt_norm_config& c, Norm& a, int bytes, int sms, unsigned* blocks, cudaStream_t st) {
-  const bool f32 = c.weight_dtype == ESSPT_F32;
-  if (c.dtype == ESSPT_F32) return launch_by_width<BACK, float, float>(a, bytes, sms, blocks, st);
-  if (c.dtype == ESSPT_BF16)
-    return f32 ? launch_by_width<BACK, __nv_bfloat16, float>(a, bytes, sms, blocks, st)
-               : launch_by_width<BACK, __nv_bfloat16, __nv_bfloat16>(a, bytes, sms, blocks, st);
-  return f32 ? launch_by_width<BACK, __half, float>(a, bytes, sms, blocks, st)
-             : launch_by_width<BACK, __half, __half>(a, bytes, sms, blocks, st);
+  a.weight_f32 = c.weight_dtype == ESSPT_F32;
+  auto go = [&](auto* type) {
+    using T = std::remove_pointer_t<decltype(type)>;
+    return bytes >= 16 ? launch_by_size<BACK, T, 16 / sizeof(T)>(a, sms, blocks, st) : launch_by_size<BACK, T, 1>(a, sms, blocks, st);
+  };
+  if (c.dtype == ESSPT_F32) return go((float*)nullptr);
+  if (c.dtype == ESSPT_BF16) return go((__nv_bfloat16*)nullptr);
+  return go((__half*)nullptr);
 }
 
 }  // namespace
