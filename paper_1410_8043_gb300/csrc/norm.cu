@@ -64,47 +64,66 @@ __device__ __forceinline__ void to_pairs(const Pack<T, VEC, N> (&p)[N], u64 (&x)
 }
 
 // Rows on their way to a thread.  Parts of 4 bytes or more go to shared memory, kDepth - 1 rows ahead; smaller ones
-// stay in registers, a row ahead.  What lies outside a row or the rows reads as zero.
+// stay in registers, a row ahead.  What lies outside a row or the rows is zero.
 template <typename T, int VEC, int N>
 struct Incoming {
   using P = Pack<T, VEC, N>;
   static constexpr bool kAsync = sizeof(P) >= 4;
   // (64 bytes a row for 512 threads, two such rows backward: 200 KB of three stages)
   static constexpr int kDepth = sizeof(P) < 16 ? 2 : N * sizeof(P) < 64 ? 4 : 3;
-  char* slots;
+  P *first, *read, *write;  // the thread's slot of the first stage, of the one to take from, of the one to fetch to
+  int pitch;                // slots from one vector to the next
+  int stage_read, stage_write;
+  const T* at;              // its first vector of the next row to fetch
+  int64_t step;             // values to that of the one after
   P next[kAsync ? 1 : N];
 
   __device__ __forceinline__ static int bytes(int threads) { return kAsync ? kDepth * N * threads * (int)sizeof(P) : 0; }
-  __device__ __forceinline__ P* slot(int stage, int i) {
-    return reinterpret_cast<P*>(slots) + (stage * N + i) * blockDim.x + threadIdx.x;
-  }
-  __device__ __forceinline__ void fetch(int stage, const T* row, int D, int lane, int lanes, bool live) {
+  __device__ __forceinline__ Incoming(char* slots, const T* from, int64_t step_, int D, int lane, int lanes)
+      : first(reinterpret_cast<P*>(slots) + threadIdx.x), read(first), write(first), pitch(blockDim.x), stage_read(0),
+        stage_write(0), at(from + lane * VEC), step(step_) {
+    if constexpr (kAsync) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = (lane + i * lanes) * VEC;
-      if constexpr (sizeof(P) >= 16) {
-        cp_async16_if(slot(stage, i), row + c, live && c < D);
-      } else if constexpr (kAsync) {
-        cp_async4_if(slot(stage, i), row + c, live && c < D);
-      } else {
-        next[i].v[0] = live && c < D ? row[c] : from_float<T>(0.f);
-      }
+      for (int k = 0; k < kDepth * N; ++k)
+        if ((lane + k % N * lanes) * VEC >= D) first[k * pitch] = zero();
     }
   }
-  __device__ __forceinline__ void take(int stage, int D, int lane, int lanes, bool live, u64 (&x)[kPairs<VEC, N>]) {
-    P p[N];
+  __device__ __forceinline__ static P zero() {
+    P p;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) p.v[j] = from_float<T>(0.f);
+    return p;
+  }
+  __device__ __forceinline__ void advance(P*& slot, int& stage) {
+    const bool wrap = stage == kDepth - 1;
+    slot = wrap ? first : slot + N * pitch;
+    stage = wrap ? 0 : stage + 1;
+  }
+  __device__ __forceinline__ void fetch(int D, int lane, int lanes, bool live) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      const bool inside = (lane + i * lanes) * VEC < D;
       if constexpr (kAsync) {
-        p[i] = *slot(stage, i);
-        if (!live || (lane + i * lanes) * VEC >= D) {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) p[i].v[j] = from_float<T>(0.f);
+        if (inside && live) {
+          if constexpr (sizeof(P) >= 16)
+            cp_async16(write + i * pitch, at + i * lanes * VEC);
+          else
+            cp_async4(write + i * pitch, at + i * lanes * VEC);
+        } else if (inside) {
+          write[i * pitch] = zero();
         }
       } else {
-        p[i] = next[i];
+        next[i].v[0] = inside && live ? at[i * lanes] : from_float<T>(0.f);
       }
     }
+    if constexpr (kAsync) advance(write, stage_write);
+    at += step;
+  }
+  __device__ __forceinline__ void take(u64 (&x)[kPairs<VEC, N>]) {
+    P p[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = kAsync ? read[i * pitch] : next[kAsync ? 0 : i];
+    if constexpr (kAsync) advance(read, stage_read);
     to_pairs<T, VEC, N>(p, x);
   }
 };
@@ -123,7 +142,7 @@ __device__ __forceinline__ void load_weights(const Norm& a, const void* from, fl
   for (int q = 0; q < kPairs<VEC, N>; ++q) x[q] = pack2(w[2 * q], w[2 * q + 1]);
 }
 
-// The sum over the lanes of a warp that hold one row; of up to kMostWarps of them.
+// The sum over the lanes of a warp that hold one row; over those that hold the warps' sums.
 __device__ __forceinline__ float lanes_sum(float v, int lanes) {
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) {
@@ -132,9 +151,16 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
   }
   return v;
 }
-__device__ __forceinline__ float warps_sum(float v) {
+__device__ __forceinline__ float warps_sum(float v, int warps) {  // (a power of two)
+  for (int off = warps / 2; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+  return v;
+}
+// Two sums over a warp: x's in the lower half of the lanes, y's in the upper.
+__device__ __forceinline__ float warp_sums(float x, float y) {
+  const bool upper = threadIdx.x & 16;
+  float v = (upper ? y : x) + __shfl_xor_sync(0xffffffffu, upper ? x : y, 16);
 #pragma unroll
-  for (int off = kMostWarps / 2; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+  for (int off = 8; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
   return v;
 }
 
@@ -161,16 +187,16 @@ __global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_forward_kern
   using In = Incoming<T, VEC, N>;
   const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
   const int groups = WIDE ? 1 : blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
-  const T* rows = static_cast<const T*>(a.x);
-  In in;
-  in.slots = dynamic;
-  int64_t t = (int64_t)blockIdx.x * groups + group;
+  int64_t t = (int64_t)blockIdx.x * groups + group, ahead = t;  // the row at hand, the next one to fetch
   const int64_t step = (int64_t)gridDim.x * groups;
+  In in(dynamic, static_cast<const T*>(a.x) + t * a.x_stride, step * a.x_stride, a.D, lane, lanes);
+  auto fetch = [&]() {
+    in.fetch(a.D, lane, lanes, ahead < a.n);
+    if (In::kAsync) cp_async_commit();
+    ahead += step;
+  };
 #pragma unroll
-  for (int k = 0; k < In::kDepth - 1; ++k) {
-    in.fetch(k, rows + (t + k * step) * a.x_stride, a.D, lane, lanes, t + k * step < a.n);
-    cp_async_commit();
-  }
+  for (int k = 0; k < In::kDepth - 1; ++k) fetch();
   u64 w[Q], b[Q];
   load_weights<T, VEC, N>(a, a.weight, 1.f, lane, w);
   load_weights<T, VEC, N>(a, a.bias, 0.f, lane, b);
@@ -183,21 +209,20 @@ __global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_forward_kern
     }
     return (float)c;
   };
-  const int warp = threadIdx.x / 32, other = threadIdx.x & (kMostWarps - 1);
+  int warps = 1;
+  while (WIDE && warps * 32 < blockDim.x) warps *= 2;
+  const int warp = threadIdx.x / 32, other = threadIdx.x & (warps - 1);
   const float inv_own = WIDE ? 1.f / fmaxf(count(warp), 1.f) : a.inv_D;
   const float count_other = WIDE && other < blockDim.x / 32 ? count(other) : 0.f;
-  int stage = 0, turn = 0;
+  int turn = 0;
   for (int64_t t0 = (int64_t)blockIdx.x * groups; t0 < a.n; t0 += step, t += step, turn ^= 1) {
     u64 x[Q];
     if (In::kAsync) {
-      in.fetch((stage + In::kDepth - 1) % In::kDepth, rows + (t + (In::kDepth - 1) * step) * a.x_stride, a.D, lane, lanes,
-               t + (In::kDepth - 1) * step < a.n);
-      cp_async_commit();
+      fetch();
       cp_async_wait<In::kDepth - 1>();
     }
-    in.take(stage, a.D, lane, lanes, t < a.n, x);
-    if (!In::kAsync) in.fetch(0, rows + (t + step) * a.x_stride, a.D, lane, lanes, t + step < a.n);
-    stage = (stage + 1) % In::kDepth;
+    in.take(x);
+    if (!In::kAsync) fetch();
     // Mean and squares of differences to it, of the lanes of a warp.
     u64 sum = x[0];
 #pragma unroll
@@ -228,10 +253,10 @@ __global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_forward_kern
       if ((threadIdx.x & 31) == 0) shared[turn][warp] = make_float2(mean, m2);
       __syncthreads();  // (the next row's go to the other half)
       const float2 v = count_other > 0.f ? shared[turn][other] : make_float2(0.f, 0.f);
-      mean = warps_sum(count_other * v.x) * a.inv_D;
-      m2 = warps_sum(v.y + count_other * (v.x - mean) * (v.x - mean));
+      mean = warps_sum(count_other * v.x, warps) * a.inv_D;
+      m2 = warps_sum(v.y + count_other * (v.x - mean) * (v.x - mean), warps);
     }
-    const float rstd = 1.f / sqrtf(m2 * a.inv_D + a.eps);
+    const float rstd = rsqrtf(m2 * a.inv_D + a.eps);
     if (t >= a.n) continue;
     const u64 m = pack2(-mean, -mean), r = pack2(rstd, rstd);
 #pragma unroll
@@ -251,44 +276,47 @@ __global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_backward_ker
   using In = Incoming<T, VEC, N>;
   const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
   const int groups = WIDE ? 1 : blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
-  In in_x, in_dy;
-  in_x.slots = dynamic;
-  in_dy.slots = dynamic + In::bytes(blockDim.x);
-  float2* stats = reinterpret_cast<float2*>(dynamic + 2 * In::bytes(blockDim.x)) + threadIdx.x;  // [kDepth][threads]
-  int64_t t = (int64_t)blockIdx.x * groups + group;
+  int64_t t = (int64_t)blockIdx.x * groups + group, ahead = t;  // the row at hand, the next one to fetch
   const int64_t step = (int64_t)gridDim.x * groups;
-  float2 next_stats = make_float2(0.f, 0.f);
-  auto fetch = [&](int stage, int64_t at) {
-    const bool live = at < a.n;
-    in_x.fetch(stage, static_cast<const T*>(a.x) + at * a.x_stride, a.D, lane, lanes, live);
-    in_dy.fetch(stage, static_cast<const T*>(a.dy) + at * a.dy_stride, a.D, lane, lanes, live);
-    if (In::kAsync) {
-      cp_async4_if(&stats[stage * blockDim.x].x, a.mean + at, live);
-      cp_async4_if(&stats[stage * blockDim.x].y, a.rstd + at, live);
-      cp_async_commit();
-    } else {
-      next_stats = live ? make_float2(a.mean[at], a.rstd[at]) : make_float2(0.f, 0.f);
-    }
+  In in_x(dynamic, static_cast<const T*>(a.x) + t * a.x_stride, step * a.x_stride, a.D, lane, lanes);
+  In in_dy(dynamic + In::bytes(blockDim.x), static_cast<const T*>(a.dy) + t * a.dy_stride, step * a.dy_stride, a.D, lane, lanes);
+  auto fetch = [&]() {
+    in_x.fetch(a.D, lane, lanes, ahead < a.n);
+    in_dy.fetch(a.D, lane, lanes, ahead < a.n);
+    if (In::kAsync) cp_async_commit();
+    ahead += step;
   };
+  auto stats = [&](int64_t at) { return at < a.n ? make_float2(a.mean[at], a.rstd[at]) : make_float2(0.f, 0.f); };
 #pragma unroll
-  for (int k = 0; k < In::kDepth - 1; ++k) fetch(k, t + k * step);
+  for (int k = 0; k < In::kDepth - 1; ++k) fetch();
+  // Statistics of as many rows as a warp's part of a row has lanes, a lane each, and the next so many under way.
+  const int own_lanes = WIDE ? 32 : lanes, own_lane = threadIdx.x & (own_lanes - 1), lane0 = (threadIdx.x & 31) - own_lane;
+  float2 now = stats(t + own_lane * step), later = stats(t + (own_lanes + own_lane) * step);
+  int turns_left = own_lanes;
   u64 w[Q], dw[Q], db[Q];
   load_weights<T, VEC, N>(a, a.weight, 1.f, lane, w);
 #pragma unroll
   for (int q = 0; q < Q; ++q) dw[q] = db[q] = 0;
-  int stage = 0, turn = 0;
+  int warps = 1;
+  while (WIDE && warps * 32 < blockDim.x) warps *= 2;
+  int turn = 0;
   for (int64_t t0 = (int64_t)blockIdx.x * groups; t0 < a.n; t0 += step, t += step, turn ^= 1) {
     u64 x[Q], dy[Q];
     if (In::kAsync) {
-      fetch((stage + In::kDepth - 1) % In::kDepth, t + (In::kDepth - 1) * step);
+      fetch();
       cp_async_wait<In::kDepth - 1>();
     }
-    in_x.take(stage, a.D, lane, lanes, t < a.n, x);
-    in_dy.take(stage, a.D, lane, lanes, t < a.n, dy);
-    float2 s = In::kAsync ? stats[stage * blockDim.x] : next_stats;
-    if (t >= a.n) s = make_float2(0.f, 0.f);
-    if (!In::kAsync) fetch(0, t + step);
-    stage = (stage + 1) % In::kDepth;
+    in_x.take(x);
+    in_dy.take(dy);
+    if (turns_left == 0) {
+      now = later, later = stats(t + (own_lanes + own_lane) * step);
+      turns_left = own_lanes;
+    }
+    float2 s;
+    s.x = __shfl_sync(0xffffffffu, now.x, lane0 + own_lanes - turns_left);
+    s.y = __shfl_sync(0xffffffffu, now.y, lane0 + own_lanes - turns_left);
+    --turns_left;
+    if (!In::kAsync) fetch();
     const float rstd = s.y;
     const u64 m = pack2(-s.x, -s.x), r = pack2(rstd, rstd);
     u64 sum_g = 0, sum_gx = 0;  // (outside a row dy is zero)
@@ -302,13 +330,15 @@ __global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_backward_ker
       sum_gx = fma2(dy[q], x[q], sum_gx);
     }
     if (!a.y) continue;
-    s = make_float2(lanes_sum(sum2(sum_g), WIDE ? 32 : lanes), lanes_sum(sum2(sum_gx), WIDE ? 32 : lanes));
     if (WIDE) {
-      const int other = threadIdx.x & (kMostWarps - 1);
-      if ((threadIdx.x & 31) == 0) shared[turn][threadIdx.x / 32] = s;
+      const float v = warp_sums(sum2(sum_g), sum2(sum_gx));
+      if ((threadIdx.x & 15) == 0) (threadIdx.x & 16 ? shared[turn][threadIdx.x / 32].y : shared[turn][threadIdx.x / 32].x) = v;
       __syncthreads();  // (the next row's go to the other half)
+      const int other = threadIdx.x & (warps - 1);
       s = other < blockDim.x / 32 ? shared[turn][other] : make_float2(0.f, 0.f);
-      s = make_float2(warps_sum(s.x), warps_sum(s.y));
+      s = make_float2(warps_sum(s.x, warps), warps_sum(s.y, warps));
+    } else {
+      s = make_float2(lanes_sum(sum2(sum_g), lanes), lanes_sum(sum2(sum_gx), lanes));
     }
     if (t >= a.n) continue;
     const u64 g = pack2(-s.x * a.inv_D, -s.x * a.inv_D), gx = pack2(-s.y * a.inv_D, -s.y * a.inv_D);
@@ -329,10 +359,10 @@ __global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_backward_ker
     __syncthreads();
   }
   float* part = a.part + (int64_t)blockIdx.x * 2 * a.D;
-  const int warp = WIDE ? 0 : threadIdx.x / 32, warps = WIDE ? 1 : blockDim.x / 32;
-  for (int k = 0; k < warps; ++k) {
-    if (warp == k && (WIDE || (threadIdx.x & 31) < lanes)) {
-      float* to = k == warps - 1 ? part : sums;
+  const int turns = WIDE ? 1 : blockDim.x / 32;
+  for (int k = 0; k < turns; ++k) {
+    if (WIDE || (threadIdx.x / 32 == k && (threadIdx.x & 31) < lanes)) {
+      float* to = k == turns - 1 ? part : sums;
       float v[2 * Q], u[2 * Q];
 #pragma unroll
       for (int q = 0; q < Q; ++q) unpack2(dw[q], v[2 * q], v[2 * q + 1]), unpack2(db[q], u[2 * q], u[2 * q + 1]);
@@ -345,12 +375,12 @@ __global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_backward_ker
         }
       }
     }
-    if (k < warps - 1) __syncthreads();
+    if (k < turns - 1) __syncthreads();
   }
 }
 
-// dw and db from the blocks' sums: 32 columns to a block, whose warps take every 16th block's.
-constexpr int kWeightWarps = 16;
+// dw and db from the blocks' sums: 32 columns to a block, whose warps take every 32nd block's.
+constexpr int kWeightWarps = 32;
 template <typename W>
 __global__ void __launch_bounds__(32 * kWeightWarps) norm_weights_kernel(const float* part, int blocks, int D, W* dw, W* db) {
   __shared__ float sums[kWeightWarps][33];
@@ -424,7 +454,7 @@ cudaError_t launch(const Spread& s, const Norm& a, unsigned blocks, cudaStream_t
   using In = Incoming<T, VEC, N>;
   const size_t row = In::kAsync ? (size_t)In::kDepth * N * s.threads * VEC * sizeof(T) : 0;
   auto* kernel = BACK ? norm_backward_kernel<T, VEC, N, WIDE> : norm_forward_kernel<T, VEC, N, WIDE>;
-  size_t shared = BACK ? 2 * row + (In::kAsync ? In::kDepth * s.threads * sizeof(float2) : 0) : row;
+  size_t shared = BACK ? 2 * row : row;
   if (BACK && !WIDE && shared < 2 * a.D * sizeof(float)) shared = 2 * a.D * sizeof(float);
   if (shared > 47 * 1024) {  // (static shared memory counts too)
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);

@@ -30,13 +30,26 @@ __device__ __forceinline__ void load_vec(const T* p, float (&x)[VEC]) {
 #pragma unroll
   for (int i = 0; i < VEC; ++i) x[i] = to_float(k.v[i]);
 }
+// Two values rounded to a type, one behind the other.
+__device__ __forceinline__ void round_pair(float x, float y, float* to) { to[0] = x, to[1] = y; }
+__device__ __forceinline__ void round_pair(float x, float y, __nv_bfloat16* to) {
+  *reinterpret_cast<__nv_bfloat162*>(to) = __floats2bfloat162_rn(x, y);
+}
+__device__ __forceinline__ void round_pair(float x, float y, __half* to) {
+  *reinterpret_cast<__half2*>(to) = __floats2half2_rn(x, y);
+}
 template <typename T, int VEC>
 __device__ __forceinline__ void store_vec(T* p, const float (&x)[VEC]) {
   struct alignas(VEC * sizeof(T)) Pack {
     T v[VEC];
   } k;
+  if constexpr (VEC % 2 == 0) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) k.v[i] = from_float<T>(x[i]);
+    for (int i = 0; i < VEC; i += 2) round_pair(x[i], x[i + 1], k.v + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) k.v[i] = from_float<T>(x[i]);
+  }
   *reinterpret_cast<Pack*>(p) = k;
 }
 
