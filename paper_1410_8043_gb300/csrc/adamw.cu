@@ -1,11 +1,11 @@
 // AdamW over many tensors at once, moments in 32 or in 8 bits: kernels and C-ABI.
 //
-// The tensors are cut into tiles of 4096 values, a block takes a tile, a warp a block of 128 values of it at a time,
-// four values a thread.
+// The tensors are cut into tiles of 4096 values.  Blocks stay and go through tiles, the next one's record under way;
+// a warp takes 512 values of a tile, four blocks of 128, four values a thread of each, all loads first.
 #include <cmath>
 #include <cstring>
-#include <limits>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "operator.h"
@@ -18,20 +18,22 @@ namespace {
 constexpr int kBlock = 128;     // values with an exponent of their own (8 bits)
 constexpr int kTile = 4096;     // values a block takes
 constexpr int kThreads = 256;
+constexpr int kBatch = 4;       // blocks of 128 whose loads a warp has under way together
+// Blocks of an SM: 128 registers for the loads of 32-bit moments, 80 for the arithmetic of 8-bit ones.  (31 million
+// values in 32 bits with 16-bit copies: 137 us, three blocks 145, batches of two 145; 192 million in 8 bits: 867, two blocks 914.)
+constexpr int resident(int bits) { return bits == 32 ? 2 : 3; }
 constexpr int kGroup = 440;     // tensors of a launch: their gradients' addresses are among its parameters
 constexpr uint32_t kNoNumber = 255;  // exponent of a block that is NaN
 
-struct Tensor {
-  float* p;
+// A tile: up to kTile values of a tensor, from `first` on.
+struct alignas(16) Tile {
+  float* p;           // the tile's first value
   void* copy;
-  int64_t count, at;  // at: its place in the flat order
+  int64_t first, at;  // at: its place in the flat order
+  uint32_t tensor;
+  int32_t count;
   float decay;
   uint32_t vector;    // whether p and copy are aligned to four values
-};
-
-// A tile: values [index * kTile, ...) of a tensor.
-struct Tile {
-  uint32_t tensor, index;
 };
 
 // Steps taken, and b1, b2 to that power.
@@ -47,7 +49,6 @@ struct Moments {
 };
 
 struct Step {
-  const Tensor* tensors;
   const Tile* tiles;
   State* state;
   Moments held;
@@ -65,8 +66,10 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x = (x ^ (x >> 15)) * 0x2545F491u;
   return x ^ (x >> 16);
 }
-__device__ __forceinline__ uint32_t place_hash(int64_t i, uint32_t key) {
-  return mix(((uint32_t)i * 0x9E3779B1u + (uint32_t)(i >> 32) * 0x85EBCA77u) ^ key);
+__device__ __forceinline__ float sqrt_fast(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 // 8-bit magnitudes are fp32's bits without the low 23 - FRACTION ones, above an exponent: a floor of x is a
@@ -81,9 +84,15 @@ template <int FRACTION, bool KEEP>  // KEEP: what is below the least code is hel
 __device__ __forceinline__ uint32_t hold(float x, uint32_t e, uint32_t r) {
   constexpr int kDrop = 23 - FRACTION;
   const uint32_t zero = (e - 15) << 23, least = zero + (1u << kDrop), b = __float_as_uint(x);
-  if (b >= least) return (b - zero + (r << (kDrop - 16))) >> kDrop & (16u << FRACTION) - 1;  // (the mask: of NaN alone)
-  if (KEEP) return x > 0.f;
-  return x >= (float)(65536u - r) * (__uint_as_float(least) * (1.f / 65536.f));
+  const uint32_t code = (b - zero + (r << (kDrop - 16))) >> kDrop & (16u << FRACTION) - 1;  // (the mask: of NaN alone)
+  uint32_t low;
+  if (KEEP) {
+    low = x > 0.f;
+  } else {
+    const float rest = __uint_as_float(0x4B000000u | (65536u - r)) - 8388608.f;  // 65536 - r, a whole number below 2^23
+    low = x >= rest * (__uint_as_float(least) * (1.f / 65536.f));
+  }
+  return b >= least ? code : low;
 }
 template <int FRACTION>
 __device__ __forceinline__ float held(uint32_t code, uint32_t e) {
@@ -133,73 +142,110 @@ __device__ __forceinline__ float largest(const float (&x)[4]) {  // of magnitude
   return __uint_as_float(top);
 }
 
-template <int BITS, typename H>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(__grid_constant__ const Step a) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const State s = *a.state;
-  const float lr = a.d_lr ? *a.d_lr : a.lr, scale = a.grad_scale ? *a.grad_scale : 1.f;
-  const float rate = lr / (float)(1.0 - s.b1t * a.b1d), root = sqrtf((float)(1.0 - s.b2t * a.b2d));
-  const uint32_t key = mix(a.seed_lo ^ mix(a.seed_hi ^ mix((uint32_t)(s.steps + 1))));
-  for (uint32_t k = blockIdx.x; k < a.n_tiles; k += gridDim.x) {
-    const Tile tile = a.tiles[k];
-    const Tensor t = a.tensors[tile.tensor];
-    const void* grad = a.grads[tile.tensor - a.first_tensor];
-    if (!grad) continue;
-    const float keep = 1.f - lr * t.decay;
-    const bool aligned = t.vector && (uintptr_t)grad % (t.copy ? 8 : 16) == 0;
-    for (int b = warp; b < kTile / kBlock; b += kThreads / 32) {
-      const int64_t i = (int64_t)tile.index * kTile + b * kBlock, left = t.count - i;
-      if (left <= 0) break;
-      const int64_t at = t.at + i;
-      const bool vector = aligned && left >= kBlock;
-      float p[4], g[4], m[4], v[4];
-      get4(t.p + i, vector, lane, left, p);
-      if (t.copy)
-        get4(static_cast<const H*>(grad) + i, vector, lane, left, g);
-      else
-        get4(static_cast<const float*>(grad) + i, vector, lane, left, g);
-      if (BITS == 32) {
-        get4(a.held.m + at, vector, lane, left, m);
-        get4(a.held.v + at, vector, lane, left, v);
-      } else {
-        uint32_t mc[4], uc[4];
-        get_codes(a.held.mc + at, vector, lane, mc);
-        get_codes(a.held.uc + at, vector, lane, uc);
-        const uint32_t me = a.held.me[at / kBlock], ue = a.held.ue[at / kBlock];
+// What a step's blocks have in common.
+struct Rates {
+  float lr, rate, inv_root, scale;
+  uint32_t key;
+};
+
+// B blocks of 128 values, one behind the other, by a warp.  Sums and products of moments are single operations (not
+// contracted): 8-bit moments are the same wherever they are computed.
+template <int BITS, typename G, typename H, bool COPY, int B, bool VECTOR>
+__device__ __forceinline__ void update(const Step& a, const Tile& t, const G* grad, const Rates& c, int lane, int i, int left) {
+  float p[B][4], g[B][4], m[B][4], v[B][4];
+  uint32_t mc[B][4], uc[B][4], me[B], ue[B];
+  const int64_t at = t.at + i;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float u = held<4>(uc[j], ue);
-          m[j] = held_m(mc[j], me), v[j] = __fmul_rn(u, u);
-        }
+  for (int k = 0; k < B; ++k) {
+    get4(t.p + i + k * kBlock, VECTOR, lane, left, p[k]);
+    get4(grad + i + k * kBlock, VECTOR, lane, left, g[k]);
+    if (BITS == 32) {
+      get4(a.held.m + at + k * kBlock, VECTOR, lane, left, m[k]);
+      get4(a.held.v + at + k * kBlock, VECTOR, lane, left, v[k]);
+    } else {
+      get_codes(a.held.mc + at + k * kBlock, VECTOR, lane, mc[k]);
+      get_codes(a.held.uc + at + k * kBlock, VECTOR, lane, uc[k]);
+      me[k] = a.held.me[at / kBlock + k], ue[k] = a.held.ue[at / kBlock + k];
+    }
+  }
+  const float keep = 1.f - c.lr * t.decay;
+#pragma unroll
+  for (int k = 0; k < B; ++k) {
+    float u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (BITS == 8) {
+        const float old = held<4>(uc[k][j], ue[k]);
+        m[k][j] = held_m(mc[k][j], me[k]), v[k][j] = __fmul_rn(old, old);
       }
-      float u[4];
+      if (!VECTOR && lane + 32 * j >= left) m[k][j] = v[k][j] = 0.f;  // between tensors
+      const float gs = __fmul_rn(g[k][j], c.scale);
+      m[k][j] = __fadd_rn(__fmul_rn(m[k][j], a.b1), __fmul_rn(gs, a.one_b1));
+      v[k][j] = __fadd_rn(__fmul_rn(v[k][j], a.b2), __fmul_rn(__fmul_rn(gs, gs), a.one_b2));
+      u[j] = BITS == 8 ? __fsqrt_rn(v[k][j]) : sqrt_fast(v[k][j]);
+      // (the quotient is off by 2 units; its divisor stays below 2^126, for 1 - beta2^t is 2^-53 at least)
+      p[k][j] = fmaf(p[k][j], keep, -__fdividef(c.rate * m[k][j], fmaf(u[j], c.inv_root, a.eps)));
+    }
+    put4(t.p + i + k * kBlock, VECTOR, lane, left, p[k]);
+    if (COPY) put4(static_cast<H*>(t.copy) + i + k * kBlock, VECTOR, lane, left, p[k]);
+    if (BITS == 32) {
+      put4(a.held.m + at + k * kBlock, VECTOR, lane, left, m[k]);
+      put4(a.held.v + at + k * kBlock, VECTOR, lane, left, v[k]);
+    } else {
+      me[k] = block_exponent<3>(largest(m[k])), ue[k] = block_exponent<4>(largest(u));
+      const int64_t place = at + k * kBlock + (VECTOR ? lane * 4 : lane);
+      // (a block does not cross a multiple of 2^32)
+      const uint32_t from = (uint32_t)(place >> 32) * 0x85EBCA77u + (uint32_t)place * 0x9E3779B1u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (!vector && lane + 32 * j >= left) m[j] = v[j] = 0.f;  // between tensors
-        const float gs = __fmul_rn(g[j], scale);
-        m[j] = __fadd_rn(__fmul_rn(m[j], a.b1), __fmul_rn(gs, a.one_b1));
-        v[j] = __fadd_rn(__fmul_rn(v[j], a.b2), __fmul_rn(__fmul_rn(gs, gs), a.one_b2));
-        u[j] = __fsqrt_rn(v[j]);
-        p[j] = p[j] * keep - rate * m[j] / (u[j] / root + a.eps);
+        const uint32_t h = mix((from + (VECTOR ? j : 32 * j) * 0x9E3779B1u) ^ c.key);
+        mc[k][j] = hold_m(m[k][j], me[k], h >> 16), uc[k][j] = hold<4, true>(u[j], ue[k], h & 0xffffu);
       }
-      put4(t.p + i, vector, lane, left, p);
-      if (t.copy) put4(static_cast<H*>(t.copy) + i, vector, lane, left, p);
-      if (BITS == 32) {
-        put4(a.held.m + at, vector, lane, left, m);
-        put4(a.held.v + at, vector, lane, left, v);
-      } else {
-        const uint32_t me = block_exponent<3>(largest(m)), ue = block_exponent<4>(largest(u));
-        uint32_t mc[4], uc[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t h = place_hash(at + (vector ? lane * 4 + j : lane + 32 * j), key);
-          mc[j] = hold_m(m[j], me, h >> 16), uc[j] = hold<4, true>(u[j], ue, h & 0xffffu);
-        }
-        put_codes(a.held.mc + at, vector, lane, mc);
-        put_codes(a.held.uc + at, vector, lane, uc);
-        if (lane == 0) a.held.me[at / kBlock] = (uint8_t)me, a.held.ue[at / kBlock] = (uint8_t)ue;
-      }
+      put_codes(a.held.mc + at + k * kBlock, VECTOR, lane, mc[k]);
+      put_codes(a.held.uc + at + k * kBlock, VECTOR, lane, uc[k]);
+      if (lane == 0) a.held.me[at / kBlock + k] = (uint8_t)me[k], a.held.ue[at / kBlock + k] = (uint8_t)ue[k];
     }
+  }
+}
+
+template <int BITS, typename H, bool COPY>
+__device__ __forceinline__ void update_tile(const Step& a, const Tile& t, const void* grads, const Rates& c, int lane, int warp) {
+  using G = std::conditional_t<COPY, H, float>;
+  const G* grad = static_cast<const G*>(grads) + t.first;
+  const bool aligned = t.vector && (uintptr_t)grad % (4 * sizeof(G)) == 0;
+  constexpr int kMine = kTile / (kThreads / 32), kAtOnce = kBatch * kBlock;
+  const int begin = warp * kMine;
+  if (aligned && t.count >= begin + kMine) {
+    for (int i = begin; i < begin + kMine; i += kAtOnce) update<BITS, G, H, COPY, kBatch, true>(a, t, grad, c, lane, i, kAtOnce);
+    return;
+  }
+  for (int i = begin; i < begin + kMine && i < t.count; i += kBlock) {
+    if (aligned && t.count >= i + kBlock)
+      update<BITS, G, H, COPY, 1, true>(a, t, grad, c, lane, i, kBlock);
+    else
+      update<BITS, G, H, COPY, 1, false>(a, t, grad, c, lane, i, t.count - i);
+  }
+}
+
+template <int BITS, typename H>
+__global__ void __launch_bounds__(kThreads, resident(BITS)) adamw_kernel(__grid_constant__ const Step a) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  Tile next{};
+  if (blockIdx.x < a.n_tiles) next = a.tiles[blockIdx.x];
+  const State s = *a.state;
+  Rates c;
+  c.lr = a.d_lr ? *a.d_lr : a.lr, c.scale = a.grad_scale ? *a.grad_scale : 1.f;
+  c.rate = c.lr / (float)(1.0 - s.b1t * a.b1d), c.inv_root = 1.f / sqrtf((float)(1.0 - s.b2t * a.b2d));
+  c.key = mix(a.seed_lo ^ mix(a.seed_hi ^ mix((uint32_t)(s.steps + 1))));
+  for (uint32_t k = blockIdx.x; k < a.n_tiles; k += gridDim.x) {
+    const Tile t = next;
+    if (k + gridDim.x < a.n_tiles) next = a.tiles[k + gridDim.x];
+    const void* grads = a.grads[t.tensor - a.first_tensor];
+    if (!grads) continue;
+    if (t.copy)
+      update_tile<BITS, H, true>(a, t, grads, c, lane, warp);
+    else
+      update_tile<BITS, H, false>(a, t, grads, c, lane, warp);
   }
   if (!a.tick) return;
   // Every block has read the state before it counts itself here; the last one counts the step.
@@ -210,31 +256,42 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(__grid_constant__ const
     *a.state = State{s.steps + 1, s.b1t * a.b1d, s.b2t * a.b2d, 0u};
 }
 
-// Eight-bit moments as bf16, which holds all of a code's bits; and moments taken from outside (8 bits: to the
-// nearest code).
-__global__ void __launch_bounds__(kThreads) moments_kernel(Moments held_at, int64_t blocks, __nv_bfloat16* m, __nv_bfloat16* u) {
-  const int lane = threadIdx.x & 31;
-  const int64_t b = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-  if (b >= blocks) return;
-  const int64_t at = b * kBlock;
-  uint32_t mc[4], uc[4];
-  float x[4], y[4];
-  get_codes(held_at.mc + at, true, lane, mc);
-  get_codes(held_at.uc + at, true, lane, uc);
-  const uint32_t me = held_at.me[b], ue = held_at.ue[b];
+// Eight-bit moments as bf16, which holds all of a code's bits: a thread takes eight values of a block, four times.
+constexpr int kEach = 4;
+__global__ void __launch_bounds__(kThreads) moments_kernel(Moments from, int64_t values, __nv_bfloat16* m, __nv_bfloat16* u) {
+  const int64_t first = ((int64_t)blockIdx.x * kThreads * kEach + threadIdx.x) * 8;
+  uint2 mc[kEach], uc[kEach];
+  uint32_t me[kEach], ue[kEach];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = held_m(mc[j], me), y[j] = held<4>(uc[j], ue);
-  put4(m + at, true, lane, kBlock, x);
-  put4(u + at, true, lane, kBlock, y);
+  for (int k = 0; k < kEach; ++k) {
+    const int64_t i = first + (int64_t)k * kThreads * 8;
+    mc[k] = uc[k] = make_uint2(0, 0), me[k] = ue[k] = 16;
+    if (i >= values) continue;
+    mc[k] = *reinterpret_cast<const uint2*>(from.mc + i), uc[k] = *reinterpret_cast<const uint2*>(from.uc + i);
+    me[k] = from.me[i / kBlock], ue[k] = from.ue[i / kBlock];
+  }
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int64_t i = first + (int64_t)k * kThreads * 8;
+    if (i >= values) break;
+    float x[8], y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = held_m((j < 4 ? mc[k].x : mc[k].y) >> 8 * (j % 4) & 255u, me[k]);
+      y[j] = held<4>((j < 4 ? uc[k].x : uc[k].y) >> 8 * (j % 4) & 255u, ue[k]);
+    }
+    store_vec<__nv_bfloat16, 8>(m + i, x);
+    store_vec<__nv_bfloat16, 8>(u + i, y);
+  }
 }
+
+// Moments taken from outside (8 bits: to the nearest code).
 template <int BITS>
-__global__ void __launch_bounds__(kThreads) load_kernel(const Tensor* tensors, const Tile* tiles, Moments to, const void* m, const void* second) {
+__global__ void __launch_bounds__(kThreads) load_kernel(const Tile* tiles, Moments to, const void* m, const void* second) {
   const int lane = threadIdx.x & 31;
-  const Tile tile = tiles[blockIdx.x];
-  const Tensor t = tensors[tile.tensor];
-  for (int b = threadIdx.x / 32; b < kTile / kBlock; b += kThreads / 32) {
-    const int64_t i = (int64_t)tile.index * kTile + b * kBlock, left = t.count - i, at = t.at + i;
-    if (left <= 0) break;
+  const Tile t = tiles[blockIdx.x];
+  for (int i = threadIdx.x / 32 * kBlock; i < t.count; i += kThreads / 32 * kBlock) {
+    const int64_t at = t.at + i, left = t.count - i;
     float x[4], y[4];
     if (BITS == 32) {
       get4(static_cast<const float*>(m) + at, false, lane, left, x);
@@ -294,7 +351,7 @@ Sizes measure(const esspt_adamw_config* c, const esspt_adamw_tensor* t) {
 }
 
 struct Carve {
-  size_t first, second, exp_first, exp_second, state, tensors, tiles, total;
+  size_t first, second, exp_first, exp_second, state, tiles, total;
 };
 
 Carve carve(const esspt_adamw_config& c, const Sizes& z) {
@@ -310,7 +367,6 @@ Carve carve(const esspt_adamw_config& c, const Sizes& z) {
   k.second = take(z.values * size);
   if (c.state_bits == 8) k.exp_first = take(z.values / kBlock), k.exp_second = take(z.values / kBlock);
   k.state = take(sizeof(State));
-  k.tensors = take(c.n_tensors * sizeof(Tensor));
   k.tiles = take(z.tiles * sizeof(Tile));
   k.total = o;
   return k;
@@ -342,21 +398,22 @@ namespace {
 
 esspt_status fill(esspt_adamw* aw, const esspt_adamw_tensor* tensors) {
   const esspt_adamw_config& c = aw->cfg;
-  std::vector<Tensor> recs;
   std::vector<Tile> tiles;
   int64_t at = 0;
   for (int k = 0; k < c.n_tensors; ++k) {
     const esspt_adamw_tensor& t = tensors[k];
     const bool vector = !misaligned(t.d_param, 16) && !misaligned(t.d_copy, 8);
-    recs.push_back(Tensor{t.d_param, t.d_copy, t.count, at, t.weight_decay, vector});
     aw->sizes.push_back(t.count == 0 ? 0 : t.d_copy ? 2 : 4);
     if (k % kGroup == 0) aw->first_tile.push_back((uint32_t)tiles.size());
-    for (int64_t i = 0; i * kTile < t.count; ++i) tiles.push_back(Tile{(uint32_t)k, (uint32_t)i});
+    for (int64_t i = 0; i < t.count; i += kTile) {
+      const int64_t left = t.count - i;
+      tiles.push_back(Tile{t.d_param + i, t.d_copy ? static_cast<uint16_t*>(t.d_copy) + i : nullptr, i, at + i, (uint32_t)k,
+                           (int32_t)(left < kTile ? left : kTile), t.weight_decay, vector});
+    }
     at += (t.count + kBlock - 1) / kBlock * kBlock;
   }
   aw->first_tile.push_back((uint32_t)tiles.size());
   ESSPT_CUDA(g_create, cudaMemsetAsync(aw->base, 0, aw->k.state, aw->st));
-  ESSPT_CUDA(g_create, cudaMemcpyAsync(aw->base + aw->k.tensors, recs.data(), recs.size() * sizeof(Tensor), cudaMemcpyHostToDevice, aw->st));
   ESSPT_CUDA(g_create, cudaMemcpyAsync(aw->base + aw->k.tiles, tiles.data(), tiles.size() * sizeof(Tile), cudaMemcpyHostToDevice, aw->st));
   state_kernel<<<1, 1, 0, aw->st>>>(reinterpret_cast<State*>(aw->base + aw->k.state), State{0, 1.0, 1.0, 0u});
   ESSPT_CUDA(g_create, cudaGetLastError());
@@ -371,8 +428,6 @@ void launch(const esspt_adamw_config& c, unsigned blocks, cudaStream_t st, const
   else
     adamw_kernel<BITS, __half><<<blocks, kThreads, 0, st>>>(a);
 }
-
-unsigned warps_for(int64_t blocks) { return (unsigned)((blocks + kThreads / 32 - 1) / (kThreads / 32)); }
 
 }  // namespace
 
@@ -444,7 +499,6 @@ esspt_status esspt_adamw_step(esspt_adamw* aw, const void* const* h_grads, float
     if (aw->sizes[k] && misaligned(h_grads[k], aw->sizes[k]))
       return aw->err.fail(ESSPT_EINVAL, "a pointer is not aligned to its type");
   Step a{};
-  a.tensors = reinterpret_cast<const Tensor*>(aw->base + aw->k.tensors);
   a.state = reinterpret_cast<State*>(aw->base + aw->k.state);
   a.held = aw->moments();
   a.lr = lr, a.b1 = (float)c.beta1, a.b2 = (float)c.beta2;
@@ -460,7 +514,7 @@ esspt_status esspt_adamw_step(esspt_adamw* aw, const void* const* h_grads, float
     a.tick = k + here == c.n_tensors;
     memcpy(a.grads, h_grads + k, here * sizeof(void*));
     if (a.n_tiles == 0 && !a.tick) continue;
-    const unsigned blocks = a.n_tiles ? a.n_tiles : 1;
+    const unsigned most = (unsigned)(resident(c.state_bits) * aw->sms), blocks = a.n_tiles == 0 ? 1 : a.n_tiles < most ? a.n_tiles : most;
     if (c.state_bits == 32)
       launch<32>(c, blocks, aw->st, a);
     else
@@ -482,9 +536,9 @@ esspt_status esspt_adamw_moments(esspt_adamw* aw, void* d_m, void* d_second) {
     ESSPT_CUDA(aw->err, cudaMemcpyAsync(d_second, aw->base + aw->k.second, bytes, cudaMemcpyDeviceToDevice, aw->st));
     return ESSPT_OK;
   }
-  const int64_t blocks = aw->values / kBlock;
-  moments_kernel<<<warps_for(blocks), kThreads, 0, aw->st>>>(aw->moments(), blocks, static_cast<__nv_bfloat16*>(d_m),
-                                                             static_cast<__nv_bfloat16*>(d_second));
+  const int64_t each = kThreads * kEach * 8, blocks = (aw->values + each - 1) / each;
+  moments_kernel<<<(unsigned)blocks, kThreads, 0, aw->st>>>(aw->moments(), aw->values, static_cast<__nv_bfloat16*>(d_m),
+                                                            static_cast<__nv_bfloat16*>(d_second));
   ESSPT_CUDA(aw->err, cudaGetLastError());
   return ESSPT_OK;
 }
@@ -498,12 +552,11 @@ esspt_status esspt_adamw_load(esspt_adamw* aw, const void* d_m, const void* d_se
   const size_t size = c.state_bits == 32 ? 4 : 2;
   if (misaligned(d_m, size) || misaligned(d_second, size)) return aw->err.fail(ESSPT_EINVAL, "a pointer is not aligned to its type");
   if (const uint32_t tiles = aw->first_tile.back()) {
-    const Tensor* rec = reinterpret_cast<const Tensor*>(aw->base + aw->k.tensors);
     const Tile* tile = reinterpret_cast<const Tile*>(aw->base + aw->k.tiles);
     if (c.state_bits == 32)
-      load_kernel<32><<<tiles, kThreads, 0, aw->st>>>(rec, tile, aw->moments(), d_m, d_second);
+      load_kernel<32><<<tiles, kThreads, 0, aw->st>>>(tile, aw->moments(), d_m, d_second);
     else
-      load_kernel<8><<<tiles, kThreads, 0, aw->st>>>(rec, tile, aw->moments(), d_m, d_second);
+      load_kernel<8><<<tiles, kThreads, 0, aw->st>>>(tile, aw->moments(), d_m, d_second);
   }
   ESSPT_CUDA(aw->err, cudaGetLastError());
   state_kernel<<<1, 1, 0, aw->st>>>(reinterpret_cast<State*>(aw->base + aw->k.state),
