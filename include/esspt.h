@@ -536,7 +536,7 @@ const char* esspt_norm_last_error(const esspt_norm* nm);
  * The moments are kept in the workspace, in 32 bits, or in 8: m and u = sqrt(v) in blocks
  * of 128 values with an exponent E each,
  *     |m| = (1 + j/8) 2^(E - 15 + e),   u = (1 + j/16) 2^(E - 15 + e),   e = 0..15,
- * code 8 e + j (and the sign) or 16 e + j, code 0 being zero; E is the least, from -111 on, that the block's
+ * code 8 e + j (and the sign, 128) or 16 e + j, codes 0 and 128 of m being zero; E is the least, from -111 on, that the block's
  * largest value needs.  The step itself takes the moments before they are held so.  A value x
  * between two that lie d apart is held as d floor(x / d + rho), rho = r / 2^16, so that
  * moving averages move by less than a step of the format in the mean (rounded to the nearest, an
@@ -562,7 +562,7 @@ typedef struct {
   int32_t copy_dtype; /* ESSPT_BF16 or ESSPT_F16: of the copies and their tensors' gradients */
   int32_t reserved;   /* 0 */
   double beta1, beta2; /* in [0, 1) */
-  double eps;         /* > 0 and finite in fp32 */
+  double eps;         /* finite in fp32, 2^-126 at least */
   uint64_t seed;      /* of the rounding of 8-bit moments */
   void* stream;       /* cudaStream_t; NULL = legacy default stream */
 } esspt_adamw_config;

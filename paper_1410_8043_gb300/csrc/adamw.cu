@@ -2,6 +2,7 @@
 //
 // The tensors are cut into tiles of 4096 values.  Blocks stay and go through tiles, the next one's record under way;
 // a warp takes 512 values of a tile, four blocks of 128, four values a thread of each, all loads first.
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -66,6 +67,12 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x = (x ^ (x >> 15)) * 0x2545F491u;
   return x ^ (x >> 16);
 }
+// (both to a unit or two; of normal numbers, for which ftz does nothing)
+__device__ __forceinline__ float reciprocal_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ float sqrt_fast(float x) {
   float r;
   asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -73,40 +80,51 @@ __device__ __forceinline__ float sqrt_fast(float x) {
 }
 
 // 8-bit magnitudes are fp32's bits without the low 23 - FRACTION ones, above an exponent: a floor of x is a
-// shift of its bits, and so is floor(x / d + rho) with rho's bits added below.
+// shift of its bits, and so is floor(x / d + rho) with rho's bits added below.  Of m the highest bit is the sign (code 128
+// is zero too).
 template <int FRACTION>
 __device__ __forceinline__ uint32_t block_exponent(float largest_of_four) {
   const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(largest_of_four) & 0x7fffffffu);
   const uint32_t e = (top + ((1u << (23 - FRACTION)) - 1)) >> 23;
   return e < 16 ? 16 : e > kNoNumber ? kNoNumber : e;
 }
+// Codes in the low byte; bits above it are to be dropped.  All lanes of a warp come here together: values below the
+// least code are rare, but for blocks of zeros, and have a way of their own.
 template <int FRACTION, bool KEEP>  // KEEP: what is below the least code is held as it, not as it or zero
-__device__ __forceinline__ uint32_t hold(float x, uint32_t e, uint32_t r) {
+__device__ __forceinline__ void hold(const float (&x)[4], uint32_t e, const uint32_t (&r)[4], uint32_t (&code)[4]) {
   constexpr int kDrop = 23 - FRACTION;
-  const uint32_t zero = (e - 15) << 23, least = zero + (1u << kDrop), b = __float_as_uint(x);
-  const uint32_t code = (b - zero + (r << (kDrop - 16))) >> kDrop & (16u << FRACTION) - 1;  // (the mask: of NaN alone)
-  uint32_t low;
-  if (KEEP) {
-    low = x > 0.f;
-  } else {
-    const float rest = __uint_as_float(0x4B000000u | (65536u - r)) - 8388608.f;  // 65536 - r, a whole number below 2^23
-    low = x >= rest * (__uint_as_float(least) * (1.f / 65536.f));
+  const uint32_t zero = (e - 15) << 23, least = zero + (1u << kDrop);
+  uint32_t smallest = 0x7fffffffu;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t b = __float_as_uint(x[j]) & 0x7fffffffu;
+    smallest = min(smallest, b);
+    code[j] = (b - zero + (r[j] << (kDrop - 16))) >> kDrop;
   }
-  return b >= least ? code : low;
+  if (__any_sync(0xffffffffu, smallest < least)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float a = fabsf(x[j]);
+      // a / least + rho >= 1, rho = r / 2^16: as a >= (2^16 - r) (least / 2^16), which has no rounding
+      const uint32_t low = KEEP ? a > 0.f : a >= (float)(65536u - r[j]) * (__uint_as_float(least) * (1.f / 65536.f));
+      if (__float_as_uint(a) < least) code[j] = low;
+    }
+  }
 }
+__device__ __forceinline__ void hold_m(const float (&x)[4], uint32_t e, const uint32_t (&r)[4], uint32_t (&code)[4]) {
+  hold<3, false>(x, e, r, code);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) code[j] = (code[j] & 127u) | (__float_as_uint(x[j]) >> 24 & 128u);
+}
+// What a code stands for in a block that is not NaN.
 template <int FRACTION>
 __device__ __forceinline__ float held(uint32_t code, uint32_t e) {
-  if (e == kNoNumber) return __uint_as_float(0x7fffffffu);
   return code ? __uint_as_float((code << (23 - FRACTION)) + ((e - 15) << 23)) : 0.f;
 }
 __device__ __forceinline__ float held_m(uint32_t code, uint32_t e) {
-  const float x = held<3>(code & 127u, e);
-  return code & 128u ? -x : x;
+  return __uint_as_float(__float_as_uint(held<3>(code & 127u, e)) | (code & 128u) << 24);
 }
-__device__ __forceinline__ uint32_t hold_m(float x, uint32_t e, uint32_t r) {
-  const uint32_t code = hold<3, false>(fabsf(x), e, r);
-  return code && x < 0.f ? code | 128u : code;
-}
+__device__ __forceinline__ float unless_nan(float x, uint32_t e) { return e == kNoNumber ? __uint_as_float(0x7fffffffu) : x; }
 
 // Four values of a block: one behind the other, or 32 apart where they are not aligned.
 template <typename T>
@@ -129,7 +147,7 @@ __device__ __forceinline__ void get_codes(const uint8_t* from, bool vector, int 
 }
 __device__ __forceinline__ void put_codes(uint8_t* to, bool vector, int lane, const uint32_t (&c)[4]) {
   if (vector) {
-    reinterpret_cast<uint32_t*>(to)[lane] = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+    reinterpret_cast<uint32_t*>(to)[lane] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
     return;
   }
 #pragma unroll
@@ -172,6 +190,8 @@ __device__ __forceinline__ void update(const Step& a, const Tile& t, const G* gr
 #pragma unroll
   for (int k = 0; k < B; ++k) {
     float u[4];
+    // (a NaN block's codes count for nothing)
+    const float b1 = BITS == 8 ? unless_nan(a.b1, me[k]) : a.b1, b2 = BITS == 8 ? unless_nan(a.b2, ue[k]) : a.b2;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (BITS == 8) {
@@ -180,11 +200,10 @@ __device__ __forceinline__ void update(const Step& a, const Tile& t, const G* gr
       }
       if (!VECTOR && lane + 32 * j >= left) m[k][j] = v[k][j] = 0.f;  // between tensors
       const float gs = __fmul_rn(g[k][j], c.scale);
-      m[k][j] = __fadd_rn(__fmul_rn(m[k][j], a.b1), __fmul_rn(gs, a.one_b1));
-      v[k][j] = __fadd_rn(__fmul_rn(v[k][j], a.b2), __fmul_rn(__fmul_rn(gs, gs), a.one_b2));
+      m[k][j] = __fadd_rn(__fmul_rn(m[k][j], b1), __fmul_rn(gs, a.one_b1));
+      v[k][j] = __fadd_rn(__fmul_rn(v[k][j], b2), __fmul_rn(__fmul_rn(gs, gs), a.one_b2));
       u[j] = BITS == 8 ? __fsqrt_rn(v[k][j]) : sqrt_fast(v[k][j]);
-      // (the quotient is off by 2 units; its divisor stays below 2^126, for 1 - beta2^t is 2^-53 at least)
-      p[k][j] = fmaf(p[k][j], keep, -__fdividef(c.rate * m[k][j], fmaf(u[j], c.inv_root, a.eps)));
+      p[k][j] = fmaf(p[k][j], keep, -(c.rate * m[k][j]) * reciprocal_fast(fmaf(u[j], c.inv_root, a.eps)));
     }
     put4(t.p + i + k * kBlock, VECTOR, lane, left, p[k]);
     if (COPY) put4(static_cast<H*>(t.copy) + i + k * kBlock, VECTOR, lane, left, p[k]);
@@ -196,11 +215,14 @@ __device__ __forceinline__ void update(const Step& a, const Tile& t, const G* gr
       const int64_t place = at + k * kBlock + (VECTOR ? lane * 4 : lane);
       // (a block does not cross a multiple of 2^32)
       const uint32_t from = (uint32_t)(place >> 32) * 0x85EBCA77u + (uint32_t)place * 0x9E3779B1u;
+      uint32_t high[4], low[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t h = mix((from + (VECTOR ? j : 32 * j) * 0x9E3779B1u) ^ c.key);
-        mc[k][j] = hold_m(m[k][j], me[k], h >> 16), uc[k][j] = hold<4, true>(u[j], ue[k], h & 0xffffu);
+        high[j] = h >> 16, low[j] = h & 0xffffu;
       }
+      hold_m(m[k], me[k], high, mc[k]);
+      hold<4, true>(u, ue[k], low, uc[k]);
       put_codes(a.held.mc + at + k * kBlock, VECTOR, lane, mc[k]);
       put_codes(a.held.uc + at + k * kBlock, VECTOR, lane, uc[k]);
       if (lane == 0) a.held.me[at / kBlock + k] = (uint8_t)me[k], a.held.ue[at / kBlock + k] = (uint8_t)ue[k];
@@ -277,8 +299,8 @@ __global__ void __launch_bounds__(kThreads) moments_kernel(Moments from, int64_t
     float x[8], y[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      x[j] = held_m((j < 4 ? mc[k].x : mc[k].y) >> 8 * (j % 4) & 255u, me[k]);
-      y[j] = held<4>((j < 4 ? uc[k].x : uc[k].y) >> 8 * (j % 4) & 255u, ue[k]);
+      x[j] = unless_nan(held_m((j < 4 ? mc[k].x : mc[k].y) >> 8 * (j % 4) & 255u, me[k]), me[k]);
+      y[j] = unless_nan(held<4>((j < 4 ? uc[k].x : uc[k].y) >> 8 * (j % 4) & 255u, ue[k]), ue[k]);
     }
     store_vec<__nv_bfloat16, 8>(m + i, x);
     store_vec<__nv_bfloat16, 8>(u + i, y);
@@ -309,8 +331,9 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const Tile* tiles, Momen
     }
     const uint32_t me = block_exponent<3>(largest(x)), ue = block_exponent<4>(largest(y));
     uint32_t mc[4], uc[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) mc[j] = hold_m(x[j], me, 0x8000u), uc[j] = hold<4, true>(y[j], ue, 0x8000u);
+    const uint32_t half[4] = {0x8000u, 0x8000u, 0x8000u, 0x8000u};
+    hold_m(x, me, half, mc);
+    hold<4, true>(y, ue, half, uc);
     put_codes(to.mc + at, false, lane, mc);
     put_codes(to.uc + at, false, lane, uc);
     if (lane == 0) to.me[at / kBlock] = (uint8_t)me, to.ue[at / kBlock] = (uint8_t)ue;
@@ -338,7 +361,7 @@ Sizes measure(const esspt_adamw_config* c, const esspt_adamw_tensor* t) {
   if (c->copy_dtype != ESSPT_BF16 && c->copy_dtype != ESSPT_F16) return no("copy_dtype must be bf16 or fp16");
   if (c->reserved != 0) return no("reserved must be 0");
   if (!(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0)) return no("betas must be in [0, 1)");
-  if (!((float)c->eps > 0.f) || !std::isfinite((float)c->eps)) return no("eps must be positive and finite in fp32");
+  if (!((float)c->eps >= FLT_MIN) || !std::isfinite((float)c->eps)) return no("eps must be finite and 2^-126 at least");
   for (int k = 0; k < c->n_tensors; ++k) {
     if (t[k].count < 0 || t[k].count > (int64_t)1 << 40) return no("a count must be in [0, 2^40]");
     if (!(t[k].weight_decay >= 0.f) || !std::isfinite(t[k].weight_decay))
