@@ -84,6 +84,7 @@ struct Gradient {
   uint2* pairs;           // (row, place) of the tokens, sorted
   float* part;            // [blocks][2][D]
   int32_t rows, place_bits;  // (few tokens) rows of a block; bits of a place
+  int32_t gap_blocks;        // (many tokens) blocks that set gaps to zero
 };
 
 constexpr int kFew = 16384;      // tokens that go this way at most
@@ -91,18 +92,47 @@ constexpr int kFewThreads = 512;
 constexpr int kFewBlocks = 304;  // two for each of 152 SMs
 constexpr int kLong = 32;
 
-// Writes the sums of a row's columns lane + k * lanes of a tile (in vectors).
+// A vector as it stands in memory: half the registers of fp32 values for 16-bit types.
+template <typename T, int VEC>
+struct alignas(VEC * sizeof(T)) Raw {
+  T v[VEC];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) v[j] = from_float<T>(0.f);
+  }
+};
+
+// A row's columns lane + k * lanes of a tile (in vectors): what the result holds before (zeros if it is overwritten), and
+// the result from that and the sums.
 template <typename T, int VEC, int K>
-__device__ __forceinline__ void emit(const Gradient& a, int64_t row, int c0, const float (&sum)[K][VEC]) {
+__device__ __forceinline__ void read_old(const Gradient& a, int64_t row, int c0, Raw<T, VEC> (&old)[K]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c = c0 + k * a.lanes;
+    if (a.accumulate && c < a.per_row)
+      old[k] = *reinterpret_cast<const Raw<T, VEC>*>(static_cast<const T*>(a.out) + row * a.D + c * VEC);
+    else
+      old[k].clear();
+  }
+}
+template <typename T, int VEC, int K>
+__device__ __forceinline__ void write_zeros(const Gradient& a, int64_t row, int c0) {
+  Raw<T, VEC> zero;
+  zero.clear();
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (c0 + k * a.lanes < a.per_row) *reinterpret_cast<Raw<T, VEC>*>(static_cast<T*>(a.out) + row * a.D + (c0 + k * a.lanes) * VEC) = zero;
+}
+template <typename T, int VEC, int K>
+__device__ __forceinline__ void emit(const Gradient& a, int64_t row, int c0, const float (&sum)[K][VEC], const Raw<T, VEC> (&old)[K]) {
   T* out = static_cast<T*>(a.out) + row * a.D;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int c = c0 + k * a.lanes;
     if (c >= a.per_row) break;
-    float x[VEC] = {};
-    if (a.accumulate) load_vec<T, VEC>(out + c * VEC, x);
+    float x[VEC];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) x[j] = a.accumulate ? fmaf(sum[k][j], a.scale, x[j]) : sum[k][j] * a.scale;
+    for (int j = 0; j < VEC; ++j) x[j] = a.accumulate ? fmaf(sum[k][j], a.scale, to_float(old[k].v[j])) : sum[k][j] * a.scale;
     store_vec<T, VEC>(out + c * VEC, x);
   }
 }
@@ -111,22 +141,23 @@ __device__ __forceinline__ void emit(const Gradient& a, int64_t row, int c0, con
 template <typename T, int VEC, int K, int U>
 __device__ __forceinline__ void add_rows(const Gradient& a, const int64_t (&place)[U], int c0, float (&sum)[K][VEC]) {
   const T* grad = static_cast<const T*>(a.grad);
-  float x[U][K][VEC];
+  Raw<T, VEC> x[U][K];
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) x[u][k][j] = 0.f;
       const int c = c0 + k * a.lanes;
-      if (place[u] >= 0 && c < a.per_row) load_vec<T, VEC>(grad + place[u] * a.grad_stride + c * VEC, x[u][k]);
+      if (place[u] >= 0 && c < a.per_row)
+        x[u][k] = *reinterpret_cast<const Raw<T, VEC>*>(grad + place[u] * a.grad_stride + c * VEC);
+      else
+        x[u][k].clear();
     }
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[k][j] += x[u][k][j];
+      for (int j = 0; j < VEC; ++j) sum[k][j] += to_float(x[u][k].v[j]);
 }
 
 template <typename T, int VEC, int K>
@@ -151,19 +182,22 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
         list[atomicAdd(&count, 1u)] = (uint32_t)(id[k] - lo) << a.place_bits | (uint32_t)(i0 + k * kFewThreads);
     }
   }
-  if (!a.accumulate) {  // rows without tokens; the others are written again below
-    const float zero[K][VEC] = {};
-    for (int64_t v = lo + group; v < hi; v += groups) emit<T, VEC, K>(a, v, c0, zero);
-  }
+  if (!a.accumulate)  // rows without tokens; the others are written again below
+    for (int64_t v = lo + group; v < hi; v += groups) write_zeros<T, VEC, K>(a, v, c0);
   __syncthreads();
   const uint32_t m = count;
   if (m == 0) return;
   uint32_t size = 2;
   while (size < m) size *= 2;
   for (uint32_t i = m + tid; i < size; i += kFewThreads) list[i] = 0xffffffffu;
+  bool apart = true;  // whether the last exchanges went past a warp's own 64 entries
   for (uint32_t run = 2; run <= size; run *= 2)
     for (uint32_t dist = run / 2; dist > 0; dist /= 2) {
-      __syncthreads();
+      if (apart || dist > 32)
+        __syncthreads();
+      else
+        __syncwarp();
+      apart = dist > 32;
       for (uint32_t t = tid; t < size / 2; t += kFewThreads) {
         const uint32_t i = 2 * t - (t & (dist - 1)), j = i + dist;
         const uint32_t x = list[i], y = list[j];
@@ -182,13 +216,15 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
       continue;
     }
     float sum[K][VEC] = {};
+    Raw<T, VEC> old[K];
+    read_old<T, VEC, K>(a, lo + row, c0, old);
     for (uint32_t at = i; at < end; at += U) {
       int64_t place[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) place[u] = at + u < end ? (int64_t)(list[at + u] & place_mask) : -1;
       add_rows<T, VEC, K, U>(a, place, c0, sum);
     }
-    emit<T, VEC, K>(a, lo + row, c0, sum);
+    emit<T, VEC, K>(a, lo + row, c0, sum, old);
   }
   __syncthreads();
   for (uint32_t k = 0; k < n_long; ++k) {
@@ -202,6 +238,8 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
         left = half;
     }
     float sum[K][VEC] = {};
+    Raw<T, VEC> old[K];
+    if (group == 0) read_old<T, VEC, K>(a, lo + row, c0, old);
     for (uint32_t at = begin + group; at < end; at += U * groups) {
       int64_t place[U];
 #pragma unroll
@@ -219,7 +257,7 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
     if (group == 0) {
 #pragma unroll
       for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] = red[q * kFewThreads + tid];
-      emit<T, VEC, K>(a, lo + row, c0, sum);
+      emit<T, VEC, K>(a, lo + row, c0, sum, old);
     }
     __syncthreads();
   }
@@ -246,9 +284,6 @@ struct Sort {
   uint32_t* counts;    // [bins][tiles]
   uint32_t* totals;    // [bins]
   uint32_t* status;
-  char* zero;          // a share of the gradient, to be set to zero
-  int64_t zero_bytes;
-  int zero_blocks;
 };
 
 __device__ __forceinline__ uint32_t key_of(const Sort& a, int64_t i) {
@@ -257,30 +292,8 @@ __device__ __forceinline__ uint32_t key_of(const Sort& a, int64_t i) {
   return (uint32_t)id < (uint32_t)a.V ? (uint32_t)id : (uint32_t)a.V;
 }
 
-// Blocks behind a kernel's own write zeros.
-__device__ void write_zeros(const Sort& a, int block) {
-  const int64_t head = ((16 - (reinterpret_cast<uintptr_t>(a.zero) & 15)) & 15) < a.zero_bytes
-                           ? (16 - (reinterpret_cast<uintptr_t>(a.zero) & 15)) & 15
-                           : a.zero_bytes;
-  const int64_t body = (a.zero_bytes - head) / 16;
-  uint4* to = reinterpret_cast<uint4*>(a.zero + head);
-  const int64_t step = (int64_t)a.zero_blocks * kThreads;
-  int64_t i = (int64_t)block * kThreads + threadIdx.x;
-  for (; i + 3 * step < body; i += 4 * step) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) to[i + k * step] = make_uint4(0, 0, 0, 0);
-  }
-  for (; i < body; i += step) to[i] = make_uint4(0, 0, 0, 0);
-  if (block == 0) {
-    for (int64_t k = threadIdx.x * 2; k < head; k += 2 * kThreads) *reinterpret_cast<uint16_t*>(a.zero + k) = 0;
-    for (int64_t k = head + body * 16 + threadIdx.x * 2; k < a.zero_bytes; k += 2 * kThreads)
-      *reinterpret_cast<uint16_t*>(a.zero + k) = 0;
-  }
-}
-
 __global__ void __launch_bounds__(kThreads) count_kernel(Sort a) {
   __shared__ uint32_t bins[kMostBins];
-  if ((int)blockIdx.x >= a.tiles) return write_zeros(a, blockIdx.x - a.tiles);
   for (int d = threadIdx.x; d < a.bins; d += kThreads) bins[d] = 0;
   __syncthreads();
   const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
@@ -295,9 +308,7 @@ __global__ void __launch_bounds__(kThreads) count_kernel(Sort a) {
 
 // A warp per digit.
 __global__ void __launch_bounds__(kThreads) scan_kernel(Sort a) {
-  const int own = (a.bins + kThreads / 32 - 1) / (kThreads / 32), lane = threadIdx.x & 31;
-  if ((int)blockIdx.x >= own) return write_zeros(a, blockIdx.x - own);
-  const int d = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  const int lane = threadIdx.x & 31, d = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
   if (d >= a.bins) return;
   uint32_t* row = a.counts + (int64_t)d * a.tiles;
   uint32_t sum = 0;
@@ -319,7 +330,6 @@ __global__ void __launch_bounds__(kThreads) move_kernel(Sort a) {
   constexpr int kWarps = kThreads / 32, kEach = kRound / kThreads;
   __shared__ uint32_t place[kMostBins], warp_sum[kWarps];
   __shared__ uint16_t ahead[kWarps][kMostBins];  // a digit's tokens in a round before a warp's next ones
-  if ((int)blockIdx.x >= a.tiles) return write_zeros(a, blockIdx.x - a.tiles);
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   {  // where the digits begin: each thread's run of digits, warps, all
     const int each = (a.bins + kThreads - 1) / kThreads, d0 = threadIdx.x * each;
@@ -397,75 +407,146 @@ __global__ void __launch_bounds__(kThreads) move_kernel(Sort a) {
 
 // ---- many tokens: the sums ------------------------------------------------------------------------------------
 //
-// A group of lanes adds kChunk sorted tokens.  Rows that begin and end among them are written; the sums of those
+// A group of lanes adds a chunk of sorted tokens.  Rows that begin and end among them are written; the sums of those
 // that do not are joined over the groups of a block, and what crosses blocks goes to `part`: [block][0] the sum of the
 // row that the block's first token shares with the block before, [block][1] of the row that goes on behind the block.
-constexpr int kChunk = 32;
+// Rows without tokens are set to zero by the group that ends the row before them, or, more than kGap in a row, by blocks of
+// their own.
+constexpr int kGap = 64;
+constexpr int kMostChunk = 32, kMostTokens = 2048;  // of a group, of a block
+__host__ __device__ constexpr int chunk_of(int lanes) { return 8 * lanes < kMostChunk ? 8 * lanes : kMostChunk; }
 
-template <typename T, int VEC, int K>
-__global__ void __launch_bounds__(kThreads) sums_kernel(Gradient a) {
-  constexpr int U = 8 / K;
+__device__ __forceinline__ void zero_bytes(char* to, int64_t bytes, int lane) {  // by a warp; 2 bytes' multiples
+  const int64_t first = (16 - (reinterpret_cast<uintptr_t>(to) & 15)) & 15, head = first < bytes ? first : bytes;
+  for (int64_t k = 2 * lane; k < head; k += 64) *reinterpret_cast<uint16_t*>(to + k) = 0;
+  const int64_t body = (bytes - head) / 16;
+  for (int64_t k = lane; k < body; k += 32) reinterpret_cast<uint4*>(to + head)[k] = make_uint4(0, 0, 0, 0);
+  for (int64_t k = head + body * 16 + 2 * lane; k < bytes; k += 64) *reinterpret_cast<uint16_t*>(to + k) = 0;
+}
+
+// A warp's 31 ranges of kGap rows: what lies in gaps of more than that many rows.
+constexpr int kGapRows = 31 * kGap;
+template <typename T>
+__device__ void zero_gaps(const Gradient& a, int64_t warp) {
+  const int lane = threadIdx.x & 31;
+  const int64_t v = warp * kGapRows + lane * kGap;  // a lane's range begins here
+  int64_t at = 0, left = v < a.V ? a.n : 0;         // the first token of row v or behind it
+  while (left > 0) {
+    const int64_t half = left / 2;
+    if (a.pairs[at + half].x < (uint32_t)v)
+      at += half + 1, left -= half + 1;
+    else
+      left = half;
+  }
+  int64_t before = -1, behind = a.V;  // the rows with tokens next to v
+  if (v < a.V) {
+    if (at > 0) before = a.pairs[at - 1].x;
+    if (at < a.n && a.pairs[at].x < (uint32_t)a.V) behind = a.pairs[at].x;
+  } else {  // (nothing is there; the last rows' gap ends at V)
+    int64_t lo = 0, many = a.n;
+    while (many > 0) {
+      const int64_t half = many / 2;
+      if (a.pairs[lo + half].x < (uint32_t)a.V)
+        lo += half + 1, many -= half + 1;
+      else
+        many = half;
+    }
+    if (lo > 0) before = a.pairs[lo - 1].x;
+  }
+  const int64_t next_before = __shfl_down_sync(0xffffffffu, before, 1), next_behind = __shfl_down_sync(0xffffffffu, behind, 1);
+  const int64_t end = v + kGap < a.V ? v + kGap : a.V;
+  const bool inside = lane < 31 && v < a.V;
+  // the gap around the range's first row, and another one around its last
+  int64_t from[2] = {v, next_before + 1}, to[2] = {behind < end ? behind : end, end};
+  if (!inside || behind - before - 1 <= kGap) to[0] = from[0];
+  if (!inside || next_before < v || next_behind - next_before - 1 <= kGap) to[1] = from[1];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    for (uint32_t some = __ballot_sync(0xffffffffu, to[k] > from[k]); some; some &= some - 1) {
+      const int64_t f = __shfl_sync(0xffffffffu, from[k], __ffs(some) - 1), t = __shfl_sync(0xffffffffu, to[k], __ffs(some) - 1);
+      zero_bytes(static_cast<char*>(a.out) + f * a.D * sizeof(T), (t - f) * a.D * sizeof(T), lane);
+    }
+}
+
+template <typename T, int VEC, int K, bool ADD>
+__global__ void __launch_bounds__(kThreads, 3) sums_kernel(Gradient a) {
+  constexpr int U = (ADD ? 4 : 8) / K;
   __shared__ float head[K * VEC][kThreads], tail[K * VEC][kThreads];
   __shared__ uint8_t flags[kThreads];  // of a group: 1 a head, 2 a tail, 4 the head is the whole chunk and goes on
-  __shared__ uint32_t tail_key[kThreads];
-  const int tid = threadIdx.x, lane = tid & (a.lanes - 1), group = tid / a.lanes, groups = kThreads / a.lanes;
+  __shared__ uint2 pairs[kMostTokens];
+  __shared__ uint32_t key_before, key_behind;
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x < a.gap_blocks) {
+    if (blockIdx.y == 0) zero_gaps<T>(a, (int64_t)blockIdx.x * (kThreads / 32) + tid / 32);
+    return;
+  }
+  const int lane = tid & (a.lanes - 1), group = tid / a.lanes, groups = kThreads / a.lanes, chunk = chunk_of(a.lanes);
   const int c0 = blockIdx.y * a.lanes * K + lane;
-  const int64_t begin = ((int64_t)blockIdx.x * groups + group) * kChunk, end = begin + kChunk < a.n ? begin + kChunk : a.n;
+  const int64_t block = blockIdx.x - a.gap_blocks, first = block * groups * chunk;
+  const int many = a.n - first < groups * chunk ? (int)(a.n - first) : groups * chunk;  // the block's tokens
+  for (int i = tid; i < many; i += kThreads) pairs[i] = a.pairs[first + i];
+  if (tid == 0) {
+    key_before = first > 0 ? a.pairs[first - 1].x : 0xffffffffu;
+    key_behind = first + many < a.n ? a.pairs[first + many].x : 0xffffffffu;
+  }
+  __syncthreads();
+  const uint32_t V = (uint32_t)a.V;
+  auto key = [&](int i) { return i < many ? pairs[i].x : key_behind; };
+  const int begin = group * chunk, end = begin + chunk < many ? begin + chunk : many;
   float sum[K][VEC] = {};
   uint32_t f = 0;
   if (begin < end) {
-    uint32_t row = a.pairs[begin].x;
-    bool shared_row = begin > 0 && a.pairs[begin - 1].x == row;
-    const bool goes_on = end < a.n && a.pairs[end].x == a.pairs[end - 1].x;
-    auto finish = [&]() {
-      if (row >= (uint32_t)a.V) return;
-      if (shared_row) {
-        f |= 1;
-#pragma unroll
-        for (int q = 0; q < K * VEC; ++q) head[q][tid] = sum[q / VEC][q % VEC];
-      } else {
-        emit<T, VEC, K>(a, row, c0, sum);
-      }
-    };
-    for (int64_t i = begin; i < end; i += U) {
+    const uint32_t before = begin > 0 ? pairs[begin - 1].x : key_before;
+    bool shared_row = before == pairs[begin].x;
+    if (!ADD && first + begin == 0 && pairs[0].x <= kGap)  // rows before the first token's
+      for (uint32_t v = 0; v < pairs[0].x && v < V; ++v) write_zeros<T, VEC, K>(a, v, c0);
+    for (int i = begin; i < end; i += U) {
       uint2 p[U];
-      float x[U][K][VEC];
-#pragma unroll
-      for (int u = 0; u < U; ++u) p[u] = i + u < end ? a.pairs[i + u] : make_uint2(0xffffffffu, 0);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) x[u][k][j] = 0.f;
-          const int c = c0 + k * a.lanes;
-          if (p[u].x < (uint32_t)a.V && c < a.per_row)
-            load_vec<T, VEC>(static_cast<const T*>(a.grad) + p[u].y * a.grad_stride + c * VEC, x[u][k]);
-        }
+      uint32_t after[U];
+      Raw<T, VEC> x[U][K], old[ADD ? U : 1][K];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (i + u >= end) break;
-        if (p[u].x != row) {
-          finish();
-          row = p[u].x;
-          shared_row = false;
+        p[u] = i + u < end ? pairs[i + u] : make_uint2(0xffffffffu, 0);
+        after[u] = key(i + u + 1);
+      }
 #pragma unroll
-          for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] = 0.f;
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          const int c = c0 + k * a.lanes;
+          if (p[u].x < V && c < a.per_row)
+            x[u][k] = *reinterpret_cast<const Raw<T, VEC>*>(static_cast<const T*>(a.grad) + p[u].y * a.grad_stride + c * VEC);
+          else
+            x[u][k].clear();
         }
+        if (ADD && p[u].x < V && after[u] != p[u].x) read_old<T, VEC, K>(a, p[u].x, c0, old[u]);
+      }
 #pragma unroll
-        for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] += x[u][q / VEC][q % VEC];
+      for (int u = 0; u < U; ++u) {
+        if (p[u].x >= V) break;
+#pragma unroll
+        for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] += to_float(x[u][q / VEC].v[q % VEC]);
+        if (after[u] == p[u].x) continue;
+        if (shared_row) {
+          f |= 1;
+#pragma unroll
+          for (int q = 0; q < K * VEC; ++q) head[q][tid] = sum[q / VEC][q % VEC];
+        } else {
+          emit<T, VEC, K>(a, p[u].x, c0, sum, old[ADD ? u : 0]);
+        }
+        shared_row = false;
+#pragma unroll
+        for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] = 0.f;
+        const uint32_t next = after[u] < V ? after[u] : V;
+        if (!ADD && next - p[u].x - 1 <= kGap)
+          for (uint32_t v = p[u].x + 1; v < next; ++v) write_zeros<T, VEC, K>(a, v, c0);
       }
     }
-    if (!goes_on || row >= (uint32_t)a.V) {
-      finish();
-    } else if (shared_row) {
-      finish();
-      f |= 4;
-    } else {
-      f |= 2;
+    const uint32_t last = pairs[end - 1].x;
+    if (last < V && key(end) == last) {  // the row goes on behind the chunk
+      f |= shared_row ? 5 : 2;
 #pragma unroll
-      for (int q = 0; q < K * VEC; ++q) tail[q][tid] = sum[q / VEC][q % VEC];
-      if (lane == 0) tail_key[group] = row;
+      for (int q = 0; q < K * VEC; ++q) (shared_row ? head : tail)[q][tid] = sum[q / VEC][q % VEC];
     }
   }
   if (lane == 0) flags[group] = (uint8_t)f;
@@ -489,10 +570,13 @@ __global__ void __launch_bounds__(kThreads) sums_kernel(Gradient a) {
       open = flags[g] & 4;
     }
     if (!from_head && !open) {
-      emit<T, VEC, K>(a, tail_key[group], c0, sum);
+      Raw<T, VEC> old[K];
+      const uint32_t row = pairs[end - 1].x;
+      read_old<T, VEC, K>(a, row, c0, old);
+      emit<T, VEC, K>(a, row, c0, sum, old);
       continue;
     }
-    float* to = a.part + (2 * (int64_t)blockIdx.x + (from_head ? 0 : 1)) * a.D;
+    float* to = a.part + (2 * block + (from_head ? 0 : 1)) * a.D;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = c0 + k * a.lanes;
@@ -640,8 +724,9 @@ Carve carve(const esspt_embed_config& c) {
     for (int i = 0; i < 2; ++i) k.pairs[i] = take(n * sizeof(uint2));
     k.counts = take(((size_t)((n + tile - 1) / tile) << d.bits) * sizeof(uint32_t));
     k.totals = take(((size_t)1 << d.bits) * sizeof(uint32_t));
-    // a block of the sums has kThreads / lanes groups; most blocks where rows take 32 lanes
-    const int64_t fewest = kThreads / lanes_of(c.width) * kChunk;
+    // blocks of the sums: most where rows take 32 lanes, fewer tokens a block
+    const int lanes = lanes_of(c.width);
+    const int64_t fewest = kThreads / lanes * chunk_of(lanes);
     k.part = take((size_t)((n + fewest - 1) / fewest) * 2 * c.width * sizeof(float));
   }
   k.total = o;
@@ -689,26 +774,12 @@ cudaError_t launch_sort(const esspt_embed& em, const Carve& k, Gradient& a) {
   s.ids = a.ids, s.n = a.n, s.V = a.V, s.bins = 1 << d.bits;
   s.tile = tile_tokens(a.n), s.tiles = (int)((a.n + s.tile - 1) / s.tile);
   s.counts = words(k.counts), s.totals = words(k.totals), s.status = a.status;
-  const int64_t bytes = a.accumulate ? 0 : (int64_t)a.V * a.D * (int64_t)size_of(em.cfg.dtype);
-  const int64_t share = (bytes / (3 * d.passes) + 15) & ~(int64_t)15;
-  int64_t zeroed = 0;
-  auto zeros = [&] {  // the next kernel's share
-    s.zero = static_cast<char*>(a.out) + zeroed;
-    s.zero_bytes = bytes - zeroed < share ? bytes - zeroed : share;
-    zeroed += s.zero_bytes;
-    const int64_t blocks = (s.zero_bytes + kThreads * 64 - 1) / (kThreads * 64), most = 4 * em.sms;
-    s.zero_blocks = (int)(blocks < most ? blocks : most);
-    return (unsigned)s.zero_blocks;
-  };
   for (int pass = 0; pass < d.passes; ++pass) {
     s.shift = pass * d.bits;
     s.to = reinterpret_cast<uint2*>(em.base + k.pairs[pass & 1]);
-    unsigned more = zeros();
-    count_kernel<<<s.tiles + more, kThreads, 0, em.st>>>(s);
-    more = zeros();
-    scan_kernel<<<(s.bins + kThreads / 32 - 1) / (kThreads / 32) + more, kThreads, 0, em.st>>>(s);
-    more = zeros();
-    move_kernel<<<s.tiles + more, kThreads, 0, em.st>>>(s);
+    count_kernel<<<s.tiles, kThreads, 0, em.st>>>(s);
+    scan_kernel<<<(s.bins + kThreads / 32 - 1) / (kThreads / 32), kThreads, 0, em.st>>>(s);
+    move_kernel<<<s.tiles, kThreads, 0, em.st>>>(s);
     s.ids = nullptr, s.from = s.to;
   }
   a.pairs = s.to;
@@ -720,8 +791,14 @@ cudaError_t launch_sums(Gradient a, cudaStream_t st) {
   a.per_row = a.D / VEC;
   a.lanes = lanes_of((a.per_row + K - 1) / K);
   const int columns = (a.per_row + a.lanes * K - 1) / (a.lanes * K);
-  const int64_t tokens = kThreads / a.lanes * kChunk, blocks = (a.n + tokens - 1) / tokens;
-  sums_kernel<T, VEC, K><<<dim3((unsigned)blocks, (unsigned)columns), kThreads, 0, st>>>(a);
+  const int64_t tokens = kThreads / a.lanes * chunk_of(a.lanes), blocks = (a.n + tokens - 1) / tokens;
+  const int64_t rows = (int64_t)kThreads / 32 * kGapRows;
+  a.gap_blocks = a.accumulate ? 0 : (int32_t)((a.V + rows - 1) / rows);
+  const dim3 grid((unsigned)(a.gap_blocks + blocks), (unsigned)columns);
+  if (a.accumulate)
+    sums_kernel<T, VEC, K, true><<<grid, kThreads, 0, st>>>(a);
+  else
+    sums_kernel<T, VEC, K, false><<<grid, kThreads, 0, st>>>(a);
   constexpr int kWarps = kThreads / 32;
   join_kernel<T><<<dim3((unsigned)((blocks + kWarps - 1) / kWarps), (unsigned)((a.D + kJoinColumns - 1) / kJoinColumns)), kThreads, 0,
                    st>>>(a, tokens);
