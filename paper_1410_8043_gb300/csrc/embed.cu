@@ -84,7 +84,7 @@ struct Gradient {
   uint2* pairs;           // (row, place) of the tokens, sorted
   float* part;            // [blocks][2][D]
   int32_t rows, place_bits;  // (few tokens) rows of a block; bits of a place
-  int32_t gap_blocks;        // (many tokens) blocks that set gaps to zero
+  int32_t chunk, gap_blocks; // (many tokens) tokens of a group; blocks that set gaps to zero
 };
 
 constexpr int kFew = 16384;      // tokens that go this way at most
@@ -281,7 +281,8 @@ struct Sort {
   int32_t V;
   int shift, bins, tiles;
   int64_t tile;        // tokens of a tile: a multiple of kRound
-  uint32_t* counts;    // [bins][tiles]
+  uint32_t* counts;    // [bins][pitch], pitch: tiles up to a multiple of 4
+  int pitch;
   uint32_t* totals;    // [bins]
   uint32_t* status;
 };
@@ -294,47 +295,68 @@ __device__ __forceinline__ uint32_t key_of(const Sort& a, int64_t i) {
 
 __global__ void __launch_bounds__(kThreads) count_kernel(Sort a) {
   __shared__ uint32_t bins[kMostBins];
+  const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
   for (int d = threadIdx.x; d < a.bins; d += kThreads) bins[d] = 0;
   __syncthreads();
-  const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
-  for (int64_t i = first + threadIdx.x; i < end; i += kThreads) {
-    const uint32_t key = key_of(a, i);
-    if (a.ids && a.ids[i] >= a.V) atomicOr(a.status, kErrId);
-    atomicAdd(&bins[(key >> a.shift) & (a.bins - 1)], 1u);
+  for (int64_t r = first + threadIdx.x; r < end; r += kRound) {
+    uint32_t key[kRound / kThreads];
+#pragma unroll
+    for (int k = 0; k < kRound / kThreads; ++k) {
+      const int64_t i = r + k * kThreads;
+      key[k] = i >= end ? 0 : a.ids ? (uint32_t)a.ids[i] : a.from[i].x;
+    }
+#pragma unroll
+    for (int k = 0; k < kRound / kThreads; ++k) {
+      if (r + k * kThreads >= end) break;
+      if (a.ids && key[k] - (uint32_t)a.V < 0x80000000u - (uint32_t)a.V) atomicOr(a.status, kErrId);
+      atomicAdd(&bins[(min(key[k], (uint32_t)a.V) >> a.shift) & (a.bins - 1)], 1u);
+    }
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < a.bins; d += kThreads) a.counts[(int64_t)d * a.tiles + blockIdx.x] = bins[d];
+  for (int d = threadIdx.x; d < a.bins; d += kThreads) a.counts[(int64_t)d * a.pitch + blockIdx.x] = bins[d];
 }
 
-// A warp per digit.
+// A warp per digit, four tiles a lane at a time.
 __global__ void __launch_bounds__(kThreads) scan_kernel(Sort a) {
   const int lane = threadIdx.x & 31, d = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
   if (d >= a.bins) return;
-  uint32_t* row = a.counts + (int64_t)d * a.tiles;
+  uint32_t* row = a.counts + (int64_t)d * a.pitch;
   uint32_t sum = 0;
-  for (int t0 = 0; t0 < a.tiles; t0 += 32) {
-    const uint32_t c = t0 + lane < a.tiles ? row[t0 + lane] : 0;
-    uint32_t up = c;
+#pragma unroll 4
+  for (int t = lane * 4; t - lane * 4 < a.tiles; t += 128) {
+    uint4 c = t < a.tiles ? *reinterpret_cast<const uint4*>(row + t) : make_uint4(0, 0, 0, 0);
+    if (t + 1 >= a.tiles) c.y = 0;
+    if (t + 2 >= a.tiles) c.z = 0;
+    if (t + 3 >= a.tiles) c.w = 0;
+    const uint32_t own = c.x + c.y + c.z + c.w;
+    uint32_t up = own;
 #pragma unroll
     for (int off = 1; off < 32; off *= 2) {
       const uint32_t x = __shfl_up_sync(0xffffffffu, up, off);
       if (lane >= off) up += x;
     }
-    if (t0 + lane < a.tiles) row[t0 + lane] = sum + up - c;
+    const uint32_t at = sum + up - own;
+    if (t < a.tiles) *reinterpret_cast<uint4*>(row + t) = make_uint4(at, at + c.x, at + c.x + c.y, at + c.x + c.y + c.z);
     sum += __shfl_sync(0xffffffffu, up, 31);
   }
   if (lane == 0) a.totals[d] = sum;
 }
 
-__global__ void __launch_bounds__(kThreads) move_kernel(Sort a) {
-  constexpr int kWarps = kThreads / 32, kEach = kRound / kThreads;
+__global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
+  constexpr int kWarps = kThreads / 32, kEach = kRound / kThreads, kDigits = kMostBins / kThreads;
   __shared__ uint32_t place[kMostBins], warp_sum[kWarps];
   __shared__ uint16_t ahead[kWarps][kMostBins];  // a digit's tokens in a round before a warp's next ones
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   {  // where the digits begin: each thread's run of digits, warps, all
     const int each = (a.bins + kThreads - 1) / kThreads, d0 = threadIdx.x * each;
-    uint32_t sum = 0;
-    for (int d = d0; d < d0 + each && d < a.bins; ++d) sum += a.totals[d];
+    uint32_t total[kDigits], count[kDigits], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kDigits; ++j) {
+      const bool live = j < each && d0 + j < a.bins;
+      total[j] = live ? a.totals[d0 + j] : 0;
+      count[j] = live ? a.counts[(int64_t)(d0 + j) * a.pitch + blockIdx.x] : 0;
+      sum += total[j];
+    }
     uint32_t up = sum;
 #pragma unroll
     for (int off = 1; off < 32; off *= 2) {
@@ -345,9 +367,10 @@ __global__ void __launch_bounds__(kThreads) move_kernel(Sort a) {
     __syncthreads();
     uint32_t before = up - sum;
     for (int w = 0; w < warp; ++w) before += warp_sum[w];
-    for (int d = d0; d < d0 + each && d < a.bins; ++d) {
-      place[d] = before + a.counts[(int64_t)d * a.tiles + blockIdx.x];
-      before += a.totals[d];
+#pragma unroll
+    for (int j = 0; j < kDigits; ++j) {
+      if (j < each && d0 + j < a.bins) place[d0 + j] = before + count[j];
+      before += total[j];
     }
   }
   const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
@@ -413,8 +436,7 @@ __global__ void __launch_bounds__(kThreads) move_kernel(Sort a) {
 // Rows without tokens are set to zero by the group that ends the row before them, or, more than kGap in a row, by blocks of
 // their own.
 constexpr int kGap = 64;
-constexpr int kMostChunk = 32, kMostTokens = 2048;  // of a group, of a block
-__host__ __device__ constexpr int chunk_of(int lanes) { return 8 * lanes < kMostChunk ? 8 * lanes : kMostChunk; }
+constexpr int kMostTokens = 2048;  // of a block
 
 __device__ __forceinline__ void zero_bytes(char* to, int64_t bytes, int lane) {  // by a warp; 2 bytes' multiples
   const int64_t first = (16 - (reinterpret_cast<uintptr_t>(to) & 15)) & 15, head = first < bytes ? first : bytes;
@@ -480,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 3) sums_kernel(Gradient a) {
     if (blockIdx.y == 0) zero_gaps<T>(a, (int64_t)blockIdx.x * (kThreads / 32) + tid / 32);
     return;
   }
-  const int lane = tid & (a.lanes - 1), group = tid / a.lanes, groups = kThreads / a.lanes, chunk = chunk_of(a.lanes);
+  const int lane = tid & (a.lanes - 1), group = tid / a.lanes, groups = kThreads / a.lanes, chunk = a.chunk;
   const int c0 = blockIdx.y * a.lanes * K + lane;
   const int64_t block = blockIdx.x - a.gap_blocks, first = block * groups * chunk;
   const int many = a.n - first < groups * chunk ? (int)(a.n - first) : groups * chunk;  // the block's tokens
@@ -705,6 +727,21 @@ bool does_few(int64_t n, int64_t V, int32_t D) {
   return (uint64_t)((V + blocks - 1) / blocks) << bits_of((uint32_t)n - 1) <= 0xffffffffull;
 }
 
+// Tokens of a group of the sums: 32 (8 of a lane, where that is less), fewer where there would not be kSumWarps warps.
+constexpr int64_t kSumWarps = 24 * 152;
+int chunk_of(int64_t n, int lanes) {
+  const int most = 8 * lanes < 32 ? 8 * lanes : 32;
+  int chunk = most;
+  while (chunk > 8 && n * lanes < kSumWarps * 32 * chunk) chunk /= 2;
+  return chunk;
+}
+// Blocks of the sums of up to n tokens, in which a block has eight warps: those of shorter chunks are fewer than twice kSumWarps.
+int64_t most_blocks(int64_t n, int lanes) {
+  const int64_t tokens = kThreads / lanes * (8 * lanes < 32 ? 8 * lanes : 32), blocks = (n + tokens - 1) / tokens;
+  const int64_t few = kSumWarps * 2 / (kThreads / 32) + 1;
+  return blocks > few ? blocks : few;
+}
+
 struct Carve {
   size_t status, pairs[2], counts, totals, part, total;
 };
@@ -719,15 +756,14 @@ Carve carve(const esspt_embed_config& c) {
   };
   k.status = take(sizeof(uint32_t));
   if (c.backward && !does_few(c.max_tokens, c.n_rows, c.width)) {
-    const int64_t n = c.max_tokens, tile = tile_tokens(n);
+    const int64_t n = c.max_tokens;
     const Digits d = digits(c.n_rows);
     for (int i = 0; i < 2; ++i) k.pairs[i] = take(n * sizeof(uint2));
-    k.counts = take(((size_t)((n + tile - 1) / tile) << d.bits) * sizeof(uint32_t));
+    const int64_t tiles = (n + kRound - 1) / kRound;  // (longer tiles are fewer)
+    k.counts = take(((size_t)((tiles < kMostTiles ? tiles : kMostTiles) + 3) << d.bits) * sizeof(uint32_t));
     k.totals = take(((size_t)1 << d.bits) * sizeof(uint32_t));
-    // blocks of the sums: most where rows take 32 lanes, fewer tokens a block
-    const int lanes = lanes_of(c.width);
-    const int64_t fewest = kThreads / lanes * chunk_of(lanes);
-    k.part = take((size_t)((n + fewest - 1) / fewest) * 2 * c.width * sizeof(float));
+    // (most blocks where rows take most lanes)
+    k.part = take((size_t)most_blocks(n, lanes_of(c.width)) * 2 * c.width * sizeof(float));
   }
   k.total = o;
   return k;
@@ -773,6 +809,7 @@ cudaError_t launch_sort(const esspt_embed& em, const Carve& k, Gradient& a) {
   Sort s{};
   s.ids = a.ids, s.n = a.n, s.V = a.V, s.bins = 1 << d.bits;
   s.tile = tile_tokens(a.n), s.tiles = (int)((a.n + s.tile - 1) / s.tile);
+  s.pitch = (s.tiles + 3) & ~3;
   s.counts = words(k.counts), s.totals = words(k.totals), s.status = a.status;
   for (int pass = 0; pass < d.passes; ++pass) {
     s.shift = pass * d.bits;
@@ -791,7 +828,8 @@ cudaError_t launch_sums(Gradient a, cudaStream_t st) {
   a.per_row = a.D / VEC;
   a.lanes = lanes_of((a.per_row + K - 1) / K);
   const int columns = (a.per_row + a.lanes * K - 1) / (a.lanes * K);
-  const int64_t tokens = kThreads / a.lanes * chunk_of(a.lanes), blocks = (a.n + tokens - 1) / tokens;
+  a.chunk = chunk_of(a.n, a.lanes);
+  const int64_t tokens = kThreads / a.lanes * a.chunk, blocks = (a.n + tokens - 1) / tokens;
   const int64_t rows = (int64_t)kThreads / 32 * kGapRows;
   a.gap_blocks = a.accumulate ? 0 : (int32_t)((a.V + rows - 1) / rows);
   const dim3 grid((unsigned)(a.gap_blocks + blocks), (unsigned)columns);

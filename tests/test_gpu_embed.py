@@ -137,6 +137,20 @@ def test_ids_outside_the_table(T):
     em.close()
 
 
+def test_sorts_of_every_length_fit_the_workspace():
+    """Fewer tokens may take more tiles of the sort than the most do: 2.49M of 10M."""
+    T, V, D = 10_000_000, 3000, 1
+    em = _esspt().Embedding(T, V, D)
+    guard = torch.full((1 << 20,), 7, dtype=torch.uint8, device="cuda")
+    for n in (2_490_368, 2_490_369, T, 20_000):
+        ids = torch.randint(-1, V, (n,), dtype=torch.int32, device="cuda")
+        got = em.gradient(ids, torch.ones((n, 1), device="cuda"))
+        assert torch.equal(got[:, 0].long(), torch.bincount(ids.long() + 1, minlength=V + 1)[1:])
+    assert bool((guard == 7).all())
+    em.poll()
+    em.close()
+
+
 def test_special_values():
     """Infinity and NaN go to their own row alone; fp16 sums past its range are infinite."""
     em = _esspt().Embedding(6, 9, 8, dtype=torch.float16)
