@@ -10,13 +10,13 @@
 namespace esspt {
 
 template <typename... Params, typename... Args>
-cudaError_t launch_chained(void (*kernel)(Params...), int blocks, int threads, cudaStream_t st, bool chained,
+cudaError_t launch_chained(void (*kernel)(Params...), dim3 blocks, int threads, cudaStream_t st, bool chained,
                            const Args&... args) {
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = chained ? 1 : 0;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.gridDim = blocks;
   cfg.blockDim = dim3((unsigned)threads);
   cfg.stream = st;
   cfg.attrs = &at;

@@ -3,7 +3,9 @@
 #include <new>
 #include <type_traits>
 
+#include "chained.cuh"
 #include "operator.h"
+#include "ptx.cuh"
 #include "rows.cuh"
 
 using namespace esspt;
@@ -297,6 +299,7 @@ __global__ void __launch_bounds__(kThreads) count_kernel(Sort a) {
   __shared__ uint32_t bins[kMostBins];
   const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
   for (int d = threadIdx.x; d < a.bins; d += kThreads) bins[d] = 0;
+  await_previous_kernel();
   __syncthreads();
   for (int64_t r = first + threadIdx.x; r < end; r += kRound) {
     uint32_t key[kRound / kThreads];
@@ -319,6 +322,7 @@ __global__ void __launch_bounds__(kThreads) count_kernel(Sort a) {
 // A warp per digit, four tiles a lane at a time.
 __global__ void __launch_bounds__(kThreads) scan_kernel(Sort a) {
   const int lane = threadIdx.x & 31, d = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  await_previous_kernel();
   if (d >= a.bins) return;
   uint32_t* row = a.counts + (int64_t)d * a.pitch;
   uint32_t sum = 0;
@@ -347,6 +351,7 @@ __global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
   __shared__ uint32_t place[kMostBins], warp_sum[kWarps];
   __shared__ uint16_t ahead[kWarps][kMostBins];  // a digit's tokens in a round before a warp's next ones
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  await_previous_kernel();
   {  // where the digits begin: each thread's run of digits, warps, all
     const int each = (a.bins + kThreads - 1) / kThreads, d0 = threadIdx.x * each;
     uint32_t total[kDigits], count[kDigits], sum = 0;
@@ -491,13 +496,14 @@ __device__ void zero_gaps(const Gradient& a, int64_t warp) {
 }
 
 template <typename T, int VEC, int K, bool ADD>
-__global__ void __launch_bounds__(kThreads, 3) sums_kernel(Gradient a) {
+__global__ void __launch_bounds__(kThreads, 4) sums_kernel(Gradient a) {
   constexpr int U = (ADD ? 4 : 8) / K;
   __shared__ float head[K * VEC][kThreads], tail[K * VEC][kThreads];
   __shared__ uint8_t flags[kThreads];  // of a group: 1 a head, 2 a tail, 4 the head is the whole chunk and goes on
   __shared__ uint2 pairs[kMostTokens];
   __shared__ uint32_t key_before, key_behind;
   const int tid = threadIdx.x;
+  await_previous_kernel();
   if ((int)blockIdx.x < a.gap_blocks) {
     if (blockIdx.y == 0) zero_gaps<T>(a, (int64_t)blockIdx.x * (kThreads / 32) + tid / 32);
     return;
@@ -621,6 +627,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(Gradient a, int64_t bloc
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, c0 = blockIdx.y * kJoinColumns + lane;
   const int64_t first = (int64_t)blockIdx.x * kWarps, b = first + warp, end = (b + 1) * block_tokens;
   int64_t more = 0;  // parts behind the first
+  await_previous_kernel();
   if (end < a.n) {
     const uint32_t row = a.pairs[end - 1].x;
     const bool begins = b == 0 || a.pairs[end - block_tokens - 1].x != row;
@@ -814,13 +821,14 @@ cudaError_t launch_sort(const esspt_embed& em, const Carve& k, Gradient& a) {
   for (int pass = 0; pass < d.passes; ++pass) {
     s.shift = pass * d.bits;
     s.to = reinterpret_cast<uint2*>(em.base + k.pairs[pass & 1]);
-    count_kernel<<<s.tiles, kThreads, 0, em.st>>>(s);
-    scan_kernel<<<(s.bins + kThreads / 32 - 1) / (kThreads / 32), kThreads, 0, em.st>>>(s);
-    move_kernel<<<s.tiles, kThreads, 0, em.st>>>(s);
+    cudaError_t e = launch_chained(count_kernel, s.tiles, kThreads, em.st, pass > 0, s);
+    if (e == cudaSuccess) e = launch_chained(scan_kernel, (s.bins + kThreads / 32 - 1) / (kThreads / 32), kThreads, em.st, true, s);
+    if (e == cudaSuccess) e = launch_chained(move_kernel, s.tiles, kThreads, em.st, true, s);
+    if (e != cudaSuccess) return e;
     s.ids = nullptr, s.from = s.to;
   }
   a.pairs = s.to;
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 template <typename T, int VEC, int K>
@@ -833,14 +841,12 @@ cudaError_t launch_sums(Gradient a, cudaStream_t st) {
   const int64_t rows = (int64_t)kThreads / 32 * kGapRows;
   a.gap_blocks = a.accumulate ? 0 : (int32_t)((a.V + rows - 1) / rows);
   const dim3 grid((unsigned)(a.gap_blocks + blocks), (unsigned)columns);
-  if (a.accumulate)
-    sums_kernel<T, VEC, K, true><<<grid, kThreads, 0, st>>>(a);
-  else
-    sums_kernel<T, VEC, K, false><<<grid, kThreads, 0, st>>>(a);
+  cudaError_t e = a.accumulate ? launch_chained(sums_kernel<T, VEC, K, true>, grid, kThreads, st, true, a)
+                               : launch_chained(sums_kernel<T, VEC, K, false>, grid, kThreads, st, true, a);
+  if (e != cudaSuccess) return e;
   constexpr int kWarps = kThreads / 32;
-  join_kernel<T><<<dim3((unsigned)((blocks + kWarps - 1) / kWarps), (unsigned)((a.D + kJoinColumns - 1) / kJoinColumns)), kThreads, 0,
-                   st>>>(a, tokens);
-  return cudaGetLastError();
+  const dim3 joins((unsigned)((blocks + kWarps - 1) / kWarps), (unsigned)((a.D + kJoinColumns - 1) / kJoinColumns));
+  return launch_chained(join_kernel<T>, joins, kThreads, st, true, a, tokens);
 }
 
 }  // namespace

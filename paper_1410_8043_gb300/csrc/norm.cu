@@ -8,6 +8,7 @@
 #include <new>
 #include <type_traits>
 
+#include "chained.cuh"
 #include "operator.h"
 #include "ptx.cuh"
 #include "rows.cuh"
@@ -386,6 +387,7 @@ __global__ void __launch_bounds__(32 * kWeightWarps) norm_weights_kernel(const f
   __shared__ float sums[kWeightWarps][33];
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x / 32;
   float s = 0.f;
+  await_previous_kernel();
   if (c < 2 * D)
     for (int k0 = warp; k0 < blocks; k0 += 8 * kWeightWarps) {
       float x[8];
@@ -584,14 +586,15 @@ esspt_status esspt_norm_backward(esspt_norm* nm, const void* d_dy, int64_t dy_st
   ESSPT_CUDA(nm->err, launch_norm<true>(c, a, bytes, nm->sms, &blocks, nm->st));
   if (!a.want_w) return ESSPT_OK;
   const unsigned columns = (2 * c.width + 31) / 32;
-  if (c.weight_dtype == ESSPT_F32)
-    norm_weights_kernel<<<columns, 32 * kWeightWarps, 0, nm->st>>>(a.part, (int)blocks, c.width, (float*)d_dweight, (float*)d_dbias);
-  else if (c.weight_dtype == ESSPT_BF16)
-    norm_weights_kernel<<<columns, 32 * kWeightWarps, 0, nm->st>>>(a.part, (int)blocks, c.width, (__nv_bfloat16*)d_dweight,
-                                                     (__nv_bfloat16*)d_dbias);
-  else
-    norm_weights_kernel<<<columns, 32 * kWeightWarps, 0, nm->st>>>(a.part, (int)blocks, c.width, (__half*)d_dweight, (__half*)d_dbias);
-  ESSPT_CUDA(nm->err, cudaGetLastError());
+  auto weights = [&](auto* type) {
+    using W = std::remove_pointer_t<decltype(type)>;
+    return launch_chained(norm_weights_kernel<W>, columns, 32 * kWeightWarps, nm->st, true, (const float*)a.part, (int)blocks, c.width,
+                          (W*)d_dweight, (W*)d_dbias);
+  };
+  const cudaError_t e = c.weight_dtype == ESSPT_F32    ? weights((float*)nullptr)
+                        : c.weight_dtype == ESSPT_BF16 ? weights((__nv_bfloat16*)nullptr)
+                                                       : weights((__half*)nullptr);
+  ESSPT_CUDA(nm->err, e);
   return ESSPT_OK;
 }
 
