@@ -14,7 +14,8 @@ struct esspt_embed {
   esspt_embed_config cfg{};
   cudaStream_t st = nullptr;
   char* base = nullptr;
-  int sms = 0;
+  cudaStream_t side = nullptr;  // gradients are set to zero there, beside the sort
+  cudaEvent_t fork = nullptr, join = nullptr;
   Errors err;
 };
 
@@ -86,7 +87,7 @@ struct Gradient {
   uint2* pairs;           // (row, place) of the tokens, sorted
   float* part;            // [blocks][2][D]
   int32_t rows, place_bits;  // (few tokens) rows of a block; bits of a place
-  int32_t chunk, gap_blocks; // (many tokens) tokens of a group; blocks that set gaps to zero
+  int32_t chunk;             // (many tokens) tokens of a group
 };
 
 constexpr int kFew = 16384;      // tokens that go this way at most
@@ -94,15 +95,47 @@ constexpr int kFewThreads = 512;
 constexpr int kFewBlocks = 304;  // two for each of 152 SMs
 constexpr int kLong = 32;
 
-// A vector as it stands in memory: half the registers of fp32 values for 16-bit types.
+// A vector as it stands in memory (half the registers of fp32 values for 16-bit types): 16 bytes, or one value.
 template <typename T, int VEC>
-struct alignas(VEC * sizeof(T)) Raw {
-  T v[VEC];
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) v[j] = from_float<T>(0.f);
+using Raw = std::conditional_t<VEC == 1, T, uint4>;
+template <typename T, int VEC>
+__device__ __forceinline__ Raw<T, VEC> load_raw(const T* p, bool there) {  // zeros where it is not
+  if constexpr (VEC == 1) {
+    T r = from_float<T>(0.f);
+    if (there) r = *p;
+    return r;
+  } else {
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (there) r = *reinterpret_cast<const uint4*>(p);
+    return r;
   }
-};
+}
+__device__ __forceinline__ float2 halves(uint32_t w, const __nv_bfloat16*) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ float2 halves(uint32_t w, const __half*) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+template <typename T, int VEC>
+__device__ __forceinline__ void to_floats(const Raw<T, VEC>& r, float (&x)[VEC]) {
+  if constexpr (VEC == 1) {
+    x[0] = to_float(r);
+  } else if constexpr (VEC == 4) {
+    x[0] = __uint_as_float(r.x), x[1] = __uint_as_float(r.y), x[2] = __uint_as_float(r.z), x[3] = __uint_as_float(r.w);
+  } else {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 v = halves(w[j], (const T*)nullptr);
+      x[2 * j] = v.x, x[2 * j + 1] = v.y;
+    }
+  }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void add_raw(const Raw<T, VEC>& r, float (&sum)[VEC]) {
+  float x[VEC];
+  to_floats<T, VEC>(r, x);
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] += x[j];
+}
 
 // A row's columns lane + k * lanes of a tile (in vectors): what the result holds before (zeros if it is overwritten), and
 // the result from that and the sums.
@@ -111,19 +144,21 @@ __device__ __forceinline__ void read_old(const Gradient& a, int64_t row, int c0,
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int c = c0 + k * a.lanes;
-    if (a.accumulate && c < a.per_row)
-      old[k] = *reinterpret_cast<const Raw<T, VEC>*>(static_cast<const T*>(a.out) + row * a.D + c * VEC);
-    else
-      old[k].clear();
+    old[k] = load_raw<T, VEC>(static_cast<const T*>(a.out) + row * a.D + c * VEC, a.accumulate && c < a.per_row);
   }
 }
 template <typename T, int VEC, int K>
-__device__ __forceinline__ void write_zeros(const Gradient& a, int64_t row, int c0) {
-  Raw<T, VEC> zero;
-  zero.clear();
+__device__ __forceinline__ void write_zeros(const Gradient& a, int64_t row, uint32_t rows, int c0, int step) {
+  T* to = static_cast<T*>(a.out) + row * a.D + c0 * VEC;
+  for (uint32_t v = 0; v < rows; v += step, to += step * a.D)
 #pragma unroll
-  for (int k = 0; k < K; ++k)
-    if (c0 + k * a.lanes < a.per_row) *reinterpret_cast<Raw<T, VEC>*>(static_cast<T*>(a.out) + row * a.D + (c0 + k * a.lanes) * VEC) = zero;
+    for (int k = 0; k < K; ++k)
+      if (c0 + k * a.lanes < a.per_row) {
+        if constexpr (VEC * sizeof(T) == 16)
+          *reinterpret_cast<uint4*>(to + k * a.lanes * VEC) = make_uint4(0, 0, 0, 0);
+        else
+          to[k * a.lanes] = from_float<T>(0.f);
+      }
 }
 template <typename T, int VEC, int K>
 __device__ __forceinline__ void emit(const Gradient& a, int64_t row, int c0, const float (&sum)[K][VEC], const Raw<T, VEC> (&old)[K]) {
@@ -133,8 +168,9 @@ __device__ __forceinline__ void emit(const Gradient& a, int64_t row, int c0, con
     const int c = c0 + k * a.lanes;
     if (c >= a.per_row) break;
     float x[VEC];
+    if (a.accumulate) to_floats<T, VEC>(old[k], x);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) x[j] = a.accumulate ? fmaf(sum[k][j], a.scale, to_float(old[k].v[j])) : sum[k][j] * a.scale;
+    for (int j = 0; j < VEC; ++j) x[j] = a.accumulate ? fmaf(sum[k][j], a.scale, x[j]) : sum[k][j] * a.scale;
     store_vec<T, VEC>(out + c * VEC, x);
   }
 }
@@ -149,17 +185,12 @@ __device__ __forceinline__ void add_rows(const Gradient& a, const int64_t (&plac
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = c0 + k * a.lanes;
-      if (place[u] >= 0 && c < a.per_row)
-        x[u][k] = *reinterpret_cast<const Raw<T, VEC>*>(grad + place[u] * a.grad_stride + c * VEC);
-      else
-        x[u][k].clear();
+      x[u][k] = load_raw<T, VEC>(grad + place[u] * a.grad_stride + c * VEC, place[u] >= 0 && c < a.per_row);
     }
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[k][j] += to_float(x[u][k].v[j]);
+    for (int k = 0; k < K; ++k) add_raw<T, VEC>(x[u][k], sum[k]);
 }
 
 template <typename T, int VEC, int K>
@@ -185,7 +216,7 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
     }
   }
   if (!a.accumulate)  // rows without tokens; the others are written again below
-    for (int64_t v = lo + group; v < hi; v += groups) write_zeros<T, VEC, K>(a, v, c0);
+    if (lo + group < hi) write_zeros<T, VEC, K>(a, lo + group, (uint32_t)(hi - lo - group), c0, groups);
   __syncthreads();
   const uint32_t m = count;
   if (m == 0) return;
@@ -438,62 +469,8 @@ __global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
 // A group of lanes adds a chunk of sorted tokens.  Rows that begin and end among them are written; the sums of those
 // that do not are joined over the groups of a block, and what crosses blocks goes to `part`: [block][0] the sum of the
 // row that the block's first token shares with the block before, [block][1] of the row that goes on behind the block.
-// Rows without tokens are set to zero by the group that ends the row before them, or, more than kGap in a row, by blocks of
-// their own.
-constexpr int kGap = 64;
+// Rows without tokens have been set to zero beside the sort.
 constexpr int kMostTokens = 2048;  // of a block
-
-__device__ __forceinline__ void zero_bytes(char* to, int64_t bytes, int lane) {  // by a warp; 2 bytes' multiples
-  const int64_t first = (16 - (reinterpret_cast<uintptr_t>(to) & 15)) & 15, head = first < bytes ? first : bytes;
-  for (int64_t k = 2 * lane; k < head; k += 64) *reinterpret_cast<uint16_t*>(to + k) = 0;
-  const int64_t body = (bytes - head) / 16;
-  for (int64_t k = lane; k < body; k += 32) reinterpret_cast<uint4*>(to + head)[k] = make_uint4(0, 0, 0, 0);
-  for (int64_t k = head + body * 16 + 2 * lane; k < bytes; k += 64) *reinterpret_cast<uint16_t*>(to + k) = 0;
-}
-
-// A warp's 31 ranges of kGap rows: what lies in gaps of more than that many rows.
-constexpr int kGapRows = 31 * kGap;
-template <typename T>
-__device__ void zero_gaps(const Gradient& a, int64_t warp) {
-  const int lane = threadIdx.x & 31;
-  const int64_t v = warp * kGapRows + lane * kGap;  // a lane's range begins here
-  int64_t at = 0, left = v < a.V ? a.n : 0;         // the first token of row v or behind it
-  while (left > 0) {
-    const int64_t half = left / 2;
-    if (a.pairs[at + half].x < (uint32_t)v)
-      at += half + 1, left -= half + 1;
-    else
-      left = half;
-  }
-  int64_t before = -1, behind = a.V;  // the rows with tokens next to v
-  if (v < a.V) {
-    if (at > 0) before = a.pairs[at - 1].x;
-    if (at < a.n && a.pairs[at].x < (uint32_t)a.V) behind = a.pairs[at].x;
-  } else {  // (nothing is there; the last rows' gap ends at V)
-    int64_t lo = 0, many = a.n;
-    while (many > 0) {
-      const int64_t half = many / 2;
-      if (a.pairs[lo + half].x < (uint32_t)a.V)
-        lo += half + 1, many -= half + 1;
-      else
-        many = half;
-    }
-    if (lo > 0) before = a.pairs[lo - 1].x;
-  }
-  const int64_t next_before = __shfl_down_sync(0xffffffffu, before, 1), next_behind = __shfl_down_sync(0xffffffffu, behind, 1);
-  const int64_t end = v + kGap < a.V ? v + kGap : a.V;
-  const bool inside = lane < 31 && v < a.V;
-  // the gap around the range's first row, and another one around its last
-  int64_t from[2] = {v, next_before + 1}, to[2] = {behind < end ? behind : end, end};
-  if (!inside || behind - before - 1 <= kGap) to[0] = from[0];
-  if (!inside || next_before < v || next_behind - next_before - 1 <= kGap) to[1] = from[1];
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    for (uint32_t some = __ballot_sync(0xffffffffu, to[k] > from[k]); some; some &= some - 1) {
-      const int64_t f = __shfl_sync(0xffffffffu, from[k], __ffs(some) - 1), t = __shfl_sync(0xffffffffu, to[k], __ffs(some) - 1);
-      zero_bytes(static_cast<char*>(a.out) + f * a.D * sizeof(T), (t - f) * a.D * sizeof(T), lane);
-    }
-}
 
 template <typename T, int VEC, int K, bool ADD>
 __global__ void __launch_bounds__(kThreads, 4) sums_kernel(Gradient a) {
@@ -504,13 +481,9 @@ __global__ void __launch_bounds__(kThreads, 4) sums_kernel(Gradient a) {
   __shared__ uint32_t key_before, key_behind;
   const int tid = threadIdx.x;
   await_previous_kernel();
-  if ((int)blockIdx.x < a.gap_blocks) {
-    if (blockIdx.y == 0) zero_gaps<T>(a, (int64_t)blockIdx.x * (kThreads / 32) + tid / 32);
-    return;
-  }
   const int lane = tid & (a.lanes - 1), group = tid / a.lanes, groups = kThreads / a.lanes, chunk = a.chunk;
   const int c0 = blockIdx.y * a.lanes * K + lane;
-  const int64_t block = blockIdx.x - a.gap_blocks, first = block * groups * chunk;
+  const int64_t block = blockIdx.x, first = block * groups * chunk;
   const int many = a.n - first < groups * chunk ? (int)(a.n - first) : groups * chunk;  // the block's tokens
   for (int i = tid; i < many; i += kThreads) pairs[i] = a.pairs[first + i];
   if (tid == 0) {
@@ -526,8 +499,6 @@ __global__ void __launch_bounds__(kThreads, 4) sums_kernel(Gradient a) {
   if (begin < end) {
     const uint32_t before = begin > 0 ? pairs[begin - 1].x : key_before;
     bool shared_row = before == pairs[begin].x;
-    if (!ADD && first + begin == 0 && pairs[0].x <= kGap)  // rows before the first token's
-      for (uint32_t v = 0; v < pairs[0].x && v < V; ++v) write_zeros<T, VEC, K>(a, v, c0);
     for (int i = begin; i < end; i += U) {
       uint2 p[U];
       uint32_t after[U];
@@ -542,10 +513,7 @@ __global__ void __launch_bounds__(kThreads, 4) sums_kernel(Gradient a) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
           const int c = c0 + k * a.lanes;
-          if (p[u].x < V && c < a.per_row)
-            x[u][k] = *reinterpret_cast<const Raw<T, VEC>*>(static_cast<const T*>(a.grad) + p[u].y * a.grad_stride + c * VEC);
-          else
-            x[u][k].clear();
+          x[u][k] = load_raw<T, VEC>(static_cast<const T*>(a.grad) + p[u].y * a.grad_stride + c * VEC, p[u].x < V && c < a.per_row);
         }
         if (ADD && p[u].x < V && after[u] != p[u].x) read_old<T, VEC, K>(a, p[u].x, c0, old[u]);
       }
@@ -553,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 4) sums_kernel(Gradient a) {
       for (int u = 0; u < U; ++u) {
         if (p[u].x >= V) break;
 #pragma unroll
-        for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] += to_float(x[u][q / VEC].v[q % VEC]);
+        for (int k = 0; k < K; ++k) add_raw<T, VEC>(x[u][k], sum[k]);
         if (after[u] == p[u].x) continue;
         if (shared_row) {
           f |= 1;
@@ -565,9 +533,6 @@ __global__ void __launch_bounds__(kThreads, 4) sums_kernel(Gradient a) {
         shared_row = false;
 #pragma unroll
         for (int q = 0; q < K * VEC; ++q) sum[q / VEC][q % VEC] = 0.f;
-        const uint32_t next = after[u] < V ? after[u] : V;
-        if (!ADD && next - p[u].x - 1 <= kGap)
-          for (uint32_t v = p[u].x + 1; v < next; ++v) write_zeros<T, VEC, K>(a, v, c0);
       }
     }
     const uint32_t last = pairs[end - 1].x;
@@ -810,6 +775,21 @@ cudaError_t launch_few(Gradient a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+cudaError_t set_to_zero(const esspt_embed& em, const Gradient& a) {
+  cudaError_t e = cudaEventRecord(em.fork, em.st);
+  if (e == cudaSuccess) e = cudaStreamWaitEvent(em.side, em.fork, 0);
+  if (e == cudaSuccess) e = cudaMemsetAsync(a.out, 0, (size_t)a.V * a.D * size_of(em.cfg.dtype), em.side);
+  if (e == cudaSuccess) e = cudaEventRecord(em.join, em.side);
+  return e;
+}
+
+void release(esspt_embed* em) {
+  if (em->fork) cudaEventDestroy(em->fork);
+  if (em->join) cudaEventDestroy(em->join);
+  if (em->side) cudaStreamDestroy(em->side);
+  delete em;
+}
+
 cudaError_t launch_sort(const esspt_embed& em, const Carve& k, Gradient& a) {
   const Digits d = digits(a.V);
   auto words = [&](size_t o) { return reinterpret_cast<uint32_t*>(em.base + o); };
@@ -838,11 +818,9 @@ cudaError_t launch_sums(Gradient a, cudaStream_t st) {
   const int columns = (a.per_row + a.lanes * K - 1) / (a.lanes * K);
   a.chunk = chunk_of(a.n, a.lanes);
   const int64_t tokens = kThreads / a.lanes * a.chunk, blocks = (a.n + tokens - 1) / tokens;
-  const int64_t rows = (int64_t)kThreads / 32 * kGapRows;
-  a.gap_blocks = a.accumulate ? 0 : (int32_t)((a.V + rows - 1) / rows);
-  const dim3 grid((unsigned)(a.gap_blocks + blocks), (unsigned)columns);
+  const dim3 grid((unsigned)blocks, (unsigned)columns);
   cudaError_t e = a.accumulate ? launch_chained(sums_kernel<T, VEC, K, true>, grid, kThreads, st, true, a)
-                               : launch_chained(sums_kernel<T, VEC, K, false>, grid, kThreads, st, true, a);
+                               : launch_chained(sums_kernel<T, VEC, K, false>, grid, kThreads, st, false, a);  // (it waits for the zeros too)
   if (e != cudaSuccess) return e;
   constexpr int kWarps = kThreads / 32;
   const dim3 joins((unsigned)((blocks + kWarps - 1) / kWarps), (unsigned)((a.D + kJoinColumns - 1) / kJoinColumns));
@@ -860,24 +838,30 @@ esspt_status esspt_embed_create(const esspt_embed_config* cfg, void* d_workspace
   if (const char* why = config_fault(cfg)) return g_create.fail(ESSPT_EINVAL, why);
   if (!out || !d_workspace || misaligned(d_workspace, 256)) return g_create.fail(ESSPT_EINVAL, "null or misaligned pointer");
   if (bytes < carve(*cfg).total) return g_create.fail(ESSPT_ENOSPC, "workspace too small");
-  int dev = 0, sms = 0;
-  ESSPT_CUDA(g_create, cudaGetDevice(&dev));
-  ESSPT_CUDA(g_create, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   ESSPT_CUDA(g_create, cudaMemsetAsync(d_workspace, 0, 256, static_cast<cudaStream_t>(cfg->stream)));
   esspt_embed* em = new (std::nothrow) esspt_embed;
   if (!em) return g_create.fail(ESSPT_ENOSPC, "out of host memory");
   em->cfg = *cfg;
   em->st = static_cast<cudaStream_t>(cfg->stream);
   em->base = static_cast<char*>(d_workspace);
-  em->sms = sms;
+  if (cfg->backward && !does_few(cfg->max_tokens, cfg->n_rows, cfg->width)) {
+    cudaError_t e = cudaStreamCreateWithFlags(&em->side, cudaStreamNonBlocking);
+    if (e == cudaSuccess) e = cudaEventCreateWithFlags(&em->fork, cudaEventDisableTiming);
+    if (e == cudaSuccess) e = cudaEventCreateWithFlags(&em->join, cudaEventDisableTiming);
+    if (e != cudaSuccess) {
+      release(em);
+      return g_create.cuda(e, "esspt_embed_create");
+    }
+  }
   *out = em;
   return ESSPT_OK;
 }
 
 esspt_status esspt_embed_destroy(esspt_embed* em) {
   if (!em) return ESSPT_OK;
-  const cudaError_t e = cudaStreamSynchronize(em->st);
-  delete em;
+  cudaError_t e = cudaStreamSynchronize(em->st);
+  if (e == cudaSuccess && em->side) e = cudaStreamSynchronize(em->side);  // (after a call that failed half-way)
+  release(em);
   return e == cudaSuccess ? ESSPT_OK : g_create.cuda(e, "esspt_embed_destroy");
 }
 
@@ -932,7 +916,9 @@ esspt_status esspt_embed_gradient(esspt_embed* em, const int32_t* d_ids, const v
   if (!few) {
     const Carve k = carve(c);
     a.part = reinterpret_cast<float*>(em->base + k.part);
+    if (!accumulate) ESSPT_CUDA(em->err, set_to_zero(*em, a));
     ESSPT_CUDA(em->err, launch_sort(*em, k, a));
+    if (!accumulate) ESSPT_CUDA(em->err, cudaStreamWaitEvent(em->st, em->join, 0));
   }
   const cudaError_t launched = by_type(c.dtype, bytes, [&](auto* type, auto vec, auto k) {
     using T = std::remove_pointer_t<decltype(type)>;
