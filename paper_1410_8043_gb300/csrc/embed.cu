@@ -314,8 +314,7 @@ struct Sort {
   int32_t V;
   int shift, bins, tiles;
   int64_t tile;        // tokens of a tile: a multiple of kRound
-  uint32_t* counts;    // [bins][pitch], pitch: tiles up to a multiple of 4
-  int pitch;
+  uint32_t* counts;    // [tiles][bins]
   uint32_t* totals;    // [bins]
   uint32_t* status;
 };
@@ -347,50 +346,70 @@ __global__ void __launch_bounds__(kThreads) count_kernel(Sort a) {
     }
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < a.bins; d += kThreads) a.counts[(int64_t)d * a.pitch + blockIdx.x] = bins[d];
+  for (int d = threadIdx.x; d < a.bins; d += kThreads) a.counts[(int64_t)blockIdx.x * a.bins + d] = bins[d];
 }
 
-// A warp per digit, four tiles a lane at a time.
-__global__ void __launch_bounds__(kThreads) scan_kernel(Sort a) {
-  const int lane = threadIdx.x & 31, d = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+// 32 digits a block, one a lane; each warp has a run of tiles.
+constexpr int kScanWarps = 32, kScanTiles = (kMostTiles + kScanWarps - 1) / kScanWarps;
+__global__ void __launch_bounds__(32 * kScanWarps) scan_kernel(Sort a) {
+  __shared__ uint32_t sums[kScanWarps][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, d = blockIdx.x * 32 + lane;
+  const int each = (a.tiles + kScanWarps - 1) / kScanWarps, begin = warp * each, end = min(begin + each, a.tiles);
   await_previous_kernel();
-  if (d >= a.bins) return;
-  uint32_t* row = a.counts + (int64_t)d * a.pitch;
-  uint32_t sum = 0;
-#pragma unroll 4
-  for (int t = lane * 4; t - lane * 4 < a.tiles; t += 128) {
-    uint4 c = t < a.tiles ? *reinterpret_cast<const uint4*>(row + t) : make_uint4(0, 0, 0, 0);
-    if (t + 1 >= a.tiles) c.y = 0;
-    if (t + 2 >= a.tiles) c.z = 0;
-    if (t + 3 >= a.tiles) c.w = 0;
-    const uint32_t own = c.x + c.y + c.z + c.w;
-    uint32_t up = own;
+  const bool live = d < a.bins;
+  uint32_t* column = a.counts + d;
+  uint32_t own[kScanTiles], sum = 0;
 #pragma unroll
-    for (int off = 1; off < 32; off *= 2) {
-      const uint32_t x = __shfl_up_sync(0xffffffffu, up, off);
-      if (lane >= off) up += x;
-    }
-    const uint32_t at = sum + up - own;
-    if (t < a.tiles) *reinterpret_cast<uint4*>(row + t) = make_uint4(at, at + c.x, at + c.x + c.y, at + c.x + c.y + c.z);
-    sum += __shfl_sync(0xffffffffu, up, 31);
+  for (int k = 0; k < kScanTiles; ++k) own[k] = live && begin + k < end ? column[(int64_t)(begin + k) * a.bins] : 0;
+#pragma unroll
+  for (int k = 0; k < kScanTiles; ++k) sum += own[k];
+  sums[warp][lane] = sum;
+  __syncthreads();
+  uint32_t before = 0;
+  for (int w = 0; w < warp; ++w) before += sums[w][lane];
+  if (!live) return;
+  if (warp == kScanWarps - 1) a.totals[d] = before + sum;
+#pragma unroll
+  for (int k = 0; k < kScanTiles; ++k) {
+    if (begin + k >= end) break;
+    column[(int64_t)(begin + k) * a.bins] = before;
+    before += own[k];
   }
-  if (lane == 0) a.totals[d] = sum;
 }
 
 __global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
-  constexpr int kWarps = kThreads / 32, kEach = kRound / kThreads, kDigits = kMostBins / kThreads;
+  constexpr int kWarps = kThreads / 32, kEach = kRound / kThreads, kRuns = kMostBins / kThreads / 4;
   __shared__ uint32_t place[kMostBins], warp_sum[kWarps];
-  __shared__ uint16_t ahead[kWarps][kMostBins];  // a digit's tokens in a round before a warp's next ones
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  await_previous_kernel();
-  {  // where the digits begin: each thread's run of digits, warps, all
-    const int each = (a.bins + kThreads - 1) / kThreads, d0 = threadIdx.x * each;
-    uint32_t total[kDigits], count[kDigits], sum = 0;
+  __shared__ __align__(16) uint16_t ahead[kWarps][kMostBins];  // a digit's tokens in a round before a warp's next ones
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, tid = threadIdx.x;
+  const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
+  const int each = (a.bins + kThreads - 1) / kThreads;
+  uint32_t key[kEach], val[kEach];
+  auto load = [&](int64_t r) {
+    const int64_t mine = r + warp * (32 * kEach) + lane;
 #pragma unroll
-    for (int j = 0; j < kDigits; ++j) {
-      const bool live = j < each && d0 + j < a.bins;
-      total[j] = live ? a.totals[d0 + j] : 0;
-      count[j] = live ? a.counts[(int64_t)(d0 + j) * a.pitch + blockIdx.x] : 0;
+    for (int k = 0; k < kEach; ++k) {
+      const int64_t i = mine + k * 32;
+      key[k] = val[k] = 0;
+      if (i >= end) continue;
+      if (a.ids) {
+        key[k] = key_of(a, i), val[k] = (uint32_t)i;
+      } else {
+        const uint2 p = a.from[i];
+        key[k] = p.x, val[k] = p.y;
+      }
+    }
+  };
+  await_previous_kernel();
+  load(first);
+  {  // where the digits begin: each thread's run of digits, warps, all
+    uint32_t total[4 * kRuns], count[4 * kRuns], sum = 0;
+#pragma unroll
+    for (int j = 0; j < 4 * kRuns; ++j) {
+      const int d = tid * each + j;
+      const bool live = j < each && d < a.bins;
+      total[j] = live ? a.totals[d] : 0;
+      count[j] = live ? a.counts[(int64_t)blockIdx.x * a.bins + d] : 0;
       sum += total[j];
     }
     uint32_t up = sum;
@@ -404,27 +423,17 @@ __global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
     uint32_t before = up - sum;
     for (int w = 0; w < warp; ++w) before += warp_sum[w];
 #pragma unroll
-    for (int j = 0; j < kDigits; ++j) {
-      if (j < each && d0 + j < a.bins) place[d0 + j] = before + count[j];
+    for (int j = 0; j < 4 * kRuns; ++j) {
+      if (j < each && tid * each + j < a.bins) place[tid * each + j] = before + count[j];
       before += total[j];
     }
   }
-  const int64_t first = blockIdx.x * a.tile, end = first + a.tile < a.n ? first + a.tile : a.n;
   for (int64_t r = first; r < end; r += kRound) {
-    for (int d = lane; d < a.bins; d += 32) ahead[warp][d] = 0;
+    if (r > first) load(r);
+    for (int d = lane * 8; d < a.bins; d += 256) *reinterpret_cast<uint4*>(&ahead[warp][d]) = make_uint4(0, 0, 0, 0);
     __syncwarp();
-    uint32_t key[kEach], val[kEach], rank[kEach];
     const int64_t mine = r + warp * (32 * kEach) + lane;
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int64_t i = mine + k * 32;
-      key[k] = val[k] = 0;
-      if (i >= end) continue;
-      if (a.ids)
-        key[k] = key_of(a, i), val[k] = (uint32_t)i;
-      else
-        key[k] = a.from[i].x, val[k] = a.from[i].y;
-    }
+    uint32_t rank[kEach];
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       const bool live = mine + k * 32 < end;
@@ -436,19 +445,21 @@ __global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
       __syncwarp();
     }
     __syncthreads();
-    uint32_t total[kMostBins / kThreads];
+    // Four digits at once in two words (a round's counts of a digit stay below 2^16).
+    uint2 all[kRuns];
 #pragma unroll
-    for (int j = 0; j < kMostBins / kThreads; ++j) {
-      const int d = threadIdx.x + j * kThreads;
+    for (int j = 0; j < kRuns; ++j) {
+      const int d = (tid + j * kThreads) * 4;
       if (d >= a.bins) break;
-      uint32_t sum = 0;
+      uint2 sum = make_uint2(0, 0);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const uint32_t c = ahead[w][d];
-        ahead[w][d] = (uint16_t)sum;
-        sum += c;
+        uint2* at = reinterpret_cast<uint2*>(&ahead[w][d]);
+        const uint2 c = *at;
+        *at = sum;
+        sum.x += c.x, sum.y += c.y;
       }
-      total[j] = sum;
+      all[j] = sum;
     }
     __syncthreads();
 #pragma unroll
@@ -459,9 +470,24 @@ __global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kMostBins / kThreads; ++j)
-      if (threadIdx.x + j * kThreads < a.bins) place[threadIdx.x + j * kThreads] += total[j];
+    for (int j = 0; j < kRuns; ++j) {
+      const int d = (tid + j * kThreads) * 4;
+      if (d >= a.bins) break;
+      place[d] += all[j].x & 0xffffu, place[d + 1] += all[j].x >> 16;
+      place[d + 2] += all[j].y & 0xffffu, place[d + 3] += all[j].y >> 16;
+    }
   }
+}
+
+// Zeros beside the sort, past the caches' older lines.
+__global__ void __launch_bounds__(kThreads) zero_kernel(char* to, int64_t bytes) {
+  const int64_t first = (16 - (reinterpret_cast<uintptr_t>(to) & 15)) & 15, head = first < bytes ? first : bytes;
+  const int64_t body = (bytes - head) / 16, step = (int64_t)gridDim.x * kThreads;
+  uint4* words = reinterpret_cast<uint4*>(to + head);
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < body; i += step) __stcs(words + i, make_uint4(0, 0, 0, 0));
+  if (blockIdx.x != 0) return;
+  for (int64_t k = 2 * threadIdx.x; k < head; k += 2 * kThreads) *reinterpret_cast<uint16_t*>(to + k) = 0;
+  for (int64_t k = head + body * 16 + 2 * threadIdx.x; k < bytes; k += 2 * kThreads) *reinterpret_cast<uint16_t*>(to + k) = 0;
 }
 
 // ---- many tokens: the sums ------------------------------------------------------------------------------------
@@ -473,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
 constexpr int kMostTokens = 2048;  // of a block
 
 template <typename T, int VEC, int K, bool ADD>
-__global__ void __launch_bounds__(kThreads, 4) sums_kernel(Gradient a) {
+__global__ void __launch_bounds__(kThreads, ADD ? 4 : 3) sums_kernel(Gradient a) {
   constexpr int U = (ADD ? 4 : 8) / K;
   __shared__ float head[K * VEC][kThreads], tail[K * VEC][kThreads];
   __shared__ uint8_t flags[kThreads];  // of a group: 1 a head, 2 a tail, 4 the head is the whole chunk and goes on
@@ -676,7 +702,8 @@ struct Digits {
 };
 Digits digits(int64_t V) {
   const int all = bits_of((uint32_t)V), passes = (all + kMostBits - 1) / kMostBits;
-  return {passes, (all + passes - 1) / passes};
+  const int bits = (all + passes - 1) / passes;
+  return {passes, bits < 3 ? 3 : bits};  // (digits are taken by eights)
 }
 
 int64_t tile_tokens(int64_t n) {  // at most kMostTiles tiles
@@ -732,7 +759,7 @@ Carve carve(const esspt_embed_config& c) {
     const Digits d = digits(c.n_rows);
     for (int i = 0; i < 2; ++i) k.pairs[i] = take(n * sizeof(uint2));
     const int64_t tiles = (n + kRound - 1) / kRound;  // (longer tiles are fewer)
-    k.counts = take(((size_t)((tiles < kMostTiles ? tiles : kMostTiles) + 3) << d.bits) * sizeof(uint32_t));
+    k.counts = take(((size_t)(tiles < kMostTiles ? tiles : kMostTiles) << d.bits) * sizeof(uint32_t));
     k.totals = take(((size_t)1 << d.bits) * sizeof(uint32_t));
     // (most blocks where rows take most lanes)
     k.part = take((size_t)most_blocks(n, lanes_of(c.width)) * 2 * c.width * sizeof(float));
@@ -775,10 +802,14 @@ cudaError_t launch_few(Gradient a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+constexpr int64_t kZeroBlocks = 304;
 cudaError_t set_to_zero(const esspt_embed& em, const Gradient& a) {
   cudaError_t e = cudaEventRecord(em.fork, em.st);
   if (e == cudaSuccess) e = cudaStreamWaitEvent(em.side, em.fork, 0);
-  if (e == cudaSuccess) e = cudaMemsetAsync(a.out, 0, (size_t)a.V * a.D * size_of(em.cfg.dtype), em.side);
+  if (e != cudaSuccess) return e;
+  const int64_t bytes = (int64_t)a.V * a.D * size_of(em.cfg.dtype), blocks = (bytes + kThreads * 64 - 1) / (kThreads * 64);
+  zero_kernel<<<(unsigned)(blocks < kZeroBlocks ? blocks : kZeroBlocks), kThreads, 0, em.side>>>(static_cast<char*>(a.out), bytes);
+  e = cudaGetLastError();
   if (e == cudaSuccess) e = cudaEventRecord(em.join, em.side);
   return e;
 }
@@ -796,13 +827,12 @@ cudaError_t launch_sort(const esspt_embed& em, const Carve& k, Gradient& a) {
   Sort s{};
   s.ids = a.ids, s.n = a.n, s.V = a.V, s.bins = 1 << d.bits;
   s.tile = tile_tokens(a.n), s.tiles = (int)((a.n + s.tile - 1) / s.tile);
-  s.pitch = (s.tiles + 3) & ~3;
   s.counts = words(k.counts), s.totals = words(k.totals), s.status = a.status;
   for (int pass = 0; pass < d.passes; ++pass) {
     s.shift = pass * d.bits;
     s.to = reinterpret_cast<uint2*>(em.base + k.pairs[pass & 1]);
     cudaError_t e = launch_chained(count_kernel, s.tiles, kThreads, em.st, pass > 0, s);
-    if (e == cudaSuccess) e = launch_chained(scan_kernel, (s.bins + kThreads / 32 - 1) / (kThreads / 32), kThreads, em.st, true, s);
+    if (e == cudaSuccess) e = launch_chained(scan_kernel, (s.bins + 31) / 32, 32 * kScanWarps, em.st, true, s);
     if (e == cudaSuccess) e = launch_chained(move_kernel, s.tiles, kThreads, em.st, true, s);
     if (e != cudaSuccess) return e;
     s.ids = nullptr, s.from = s.to;

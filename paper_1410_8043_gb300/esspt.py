@@ -887,6 +887,9 @@ class AdamW(_Operator):
         self._grads = (ctypes.c_void_p * max(1, len(params)))()
         self._create(ctypes.byref(AdamWConfig(len(params), state_bits, DTYPES[copy_dtype], 0, betas[0], betas[1], eps,
                                               seed & 0xFFFFFFFFFFFFFFFF, ctypes.c_void_p(self._stream_ptr))), recs)
+        if state_bits == 32:
+            both = self.workspace[:8 * end].view(torch.float32)
+            self._moments = Moments(both[:end], both[end:])
 
     def _in_place(self, x, shape, dtype, name) -> None:
         if not isinstance(x, torch.Tensor) or x.dtype is not dtype or x.device != self.device or not x.is_contiguous() or (
@@ -906,29 +909,30 @@ class AdamW(_Operator):
         `lr` is a number or one fp32 value on the device, `grad_scale` such a value or None."""
         if len(grads) != len(self._like):
             raise EssptError(EINVAL, f"{len(grads)} gradients for {len(self._like)} params")
-        kept, at, on = [], self._grads, self.device
-        for k, (g, (shape, dtype)) in enumerate(zip(grads, self._like)):
+        kept, at, on = [], [], self.device
+        for g, (shape, dtype) in zip(grads, self._like):
             if g is None:
-                at[k] = None
+                at.append(None)
                 continue
-            if not isinstance(g, torch.Tensor) or g.dtype is not dtype or g.device != on or g.shape != shape:
-                raise EssptError(EINVAL, f"grads[{k}] must be a {dtype} tensor of shape {tuple(shape)} on {on}")
+            if not isinstance(g, torch.Tensor) or g.dtype is not dtype or g.shape != shape or g.device != on:
+                raise EssptError(EINVAL, f"grads[{len(at)}] must be a {dtype} tensor of shape {tuple(shape)} on {on}")
             if not g.is_contiguous():
                 g = g.contiguous()
                 kept.append(g)
-            at[k] = g.data_ptr()
+            at.append(g.data_ptr())
+        self._grads[:] = at
         scale = self._scalar(grad_scale, "grad_scale")
         d_lr = self._scalar(lr, "lr") if isinstance(lr, torch.Tensor) else None
-        self._call(self._lib.esspt_adamw_step, at, 0.0 if d_lr is not None else lr, _ptr(d_lr), _ptr(scale))
+        self._call(self._lib.esspt_adamw_step, self._grads, 0.0 if d_lr is not None else lr, _ptr(d_lr), _ptr(scale))
 
     def moments(self) -> Moments:
         """The moments in flat order: with 32 bits the state itself, with 8 what its codes stand for
         (esspt_adamw_moments)."""
         n = self.values
         if self.state_bits == 32:
-            torch.cuda.current_stream(self.device).wait_stream(self.stream)
-            both = self.workspace[:8 * n].view(torch.float32)
-            return Moments(both[:n], both[n:])
+            if torch._C._cuda_getCurrentRawStream(self.device.index) != self._stream_ptr:
+                torch.cuda.current_stream(self.device).wait_stream(self.stream)
+            return self._moments
         m, second = torch.empty((2, n), dtype=torch.bfloat16, device=self.device).unbind()
         self._call(self._lib.esspt_adamw_moments, m.data_ptr(), second.data_ptr())
         return Moments(m, second)
