@@ -305,6 +305,7 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
 constexpr int kMostBits = 11, kMostBins = 1 << kMostBits;
 constexpr int kRound = 2048;     // tokens that a block moves at once, 256 a warp
 constexpr int kMostTiles = 1216;
+constexpr int kFewTiles = 64;    // (33 tiles: the call took 42 us with a scan)
 
 struct Sort {
   const int32_t* ids;  // first pass; null: `from`
@@ -315,6 +316,7 @@ struct Sort {
   int shift, bins, tiles;
   int64_t tile;        // tokens of a tile: a multiple of kRound
   uint32_t* counts;    // [tiles][bins]
+  int direct;          // few tiles: each block adds the counts of those before it, and nothing is scanned
   uint32_t* totals;    // [bins]
   uint32_t* status;
 };
@@ -408,10 +410,24 @@ __global__ void __launch_bounds__(kThreads, 4) move_kernel(Sort a) {
     for (int j = 0; j < 4 * kRuns; ++j) {
       const int d = tid * each + j;
       const bool live = j < each && d < a.bins;
-      total[j] = live ? a.totals[d] : 0;
-      count[j] = live ? a.counts[(int64_t)blockIdx.x * a.bins + d] : 0;
-      sum += total[j];
+      total[j] = live && !a.direct ? a.totals[d] : 0;
+      count[j] = live && !a.direct ? a.counts[(int64_t)blockIdx.x * a.bins + d] : 0;
     }
+    if (a.direct)
+      for (int t = 0; t < a.tiles; t += 8) {
+#pragma unroll
+        for (int j = 0; j < 4 * kRuns; ++j) {
+          const int d = tid * each + j;
+          if (j >= each || d >= a.bins) break;
+          uint32_t c[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) c[k] = t + k < a.tiles ? a.counts[(t + k) * a.bins + d] : 0;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) total[j] += c[k], count[j] += t + k < (int)blockIdx.x ? c[k] : 0;
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < 4 * kRuns; ++j) sum += total[j];
     uint32_t up = sum;
 #pragma unroll
     for (int off = 1; off < 32; off *= 2) {
@@ -803,14 +819,17 @@ cudaError_t launch_few(Gradient a, cudaStream_t st) {
 }
 
 constexpr int64_t kZeroBlocks = 304;
-cudaError_t set_to_zero(const esspt_embed& em, const Gradient& a) {
-  cudaError_t e = cudaEventRecord(em.fork, em.st);
-  if (e == cudaSuccess) e = cudaStreamWaitEvent(em.side, em.fork, 0);
+constexpr int64_t kZeroInLine = 48 << 20;  // zeros of up to so many bytes, 8 us, come before the sort: two streams' events cost as much
+// `beside`: on the side stream, which the sums then wait for.
+cudaError_t set_to_zero(const esspt_embed& em, const Gradient& a, int64_t bytes, bool beside) {
+  cudaError_t e = beside ? cudaEventRecord(em.fork, em.st) : cudaSuccess;
+  if (e == cudaSuccess && beside) e = cudaStreamWaitEvent(em.side, em.fork, 0);
   if (e != cudaSuccess) return e;
-  const int64_t bytes = (int64_t)a.V * a.D * size_of(em.cfg.dtype), blocks = (bytes + kThreads * 64 - 1) / (kThreads * 64);
-  zero_kernel<<<(unsigned)(blocks < kZeroBlocks ? blocks : kZeroBlocks), kThreads, 0, em.side>>>(static_cast<char*>(a.out), bytes);
+  const int64_t blocks = (bytes + kThreads * 64 - 1) / (kThreads * 64);
+  zero_kernel<<<(unsigned)(blocks < kZeroBlocks ? blocks : kZeroBlocks), kThreads, 0, beside ? em.side : em.st>>>(
+      static_cast<char*>(a.out), bytes);
   e = cudaGetLastError();
-  if (e == cudaSuccess) e = cudaEventRecord(em.join, em.side);
+  if (e == cudaSuccess && beside) e = cudaEventRecord(em.join, em.side);
   return e;
 }
 
@@ -827,12 +846,13 @@ cudaError_t launch_sort(const esspt_embed& em, const Carve& k, Gradient& a) {
   Sort s{};
   s.ids = a.ids, s.n = a.n, s.V = a.V, s.bins = 1 << d.bits;
   s.tile = tile_tokens(a.n), s.tiles = (int)((a.n + s.tile - 1) / s.tile);
+  s.direct = s.tiles <= kFewTiles;
   s.counts = words(k.counts), s.totals = words(k.totals), s.status = a.status;
   for (int pass = 0; pass < d.passes; ++pass) {
     s.shift = pass * d.bits;
     s.to = reinterpret_cast<uint2*>(em.base + k.pairs[pass & 1]);
     cudaError_t e = launch_chained(count_kernel, s.tiles, kThreads, em.st, pass > 0, s);
-    if (e == cudaSuccess) e = launch_chained(scan_kernel, (s.bins + 31) / 32, 32 * kScanWarps, em.st, true, s);
+    if (e == cudaSuccess && !s.direct) e = launch_chained(scan_kernel, (s.bins + 31) / 32, 32 * kScanWarps, em.st, true, s);
     if (e == cudaSuccess) e = launch_chained(move_kernel, s.tiles, kThreads, em.st, true, s);
     if (e != cudaSuccess) return e;
     s.ids = nullptr, s.from = s.to;
@@ -946,9 +966,11 @@ esspt_status esspt_embed_gradient(esspt_embed* em, const int32_t* d_ids, const v
   if (!few) {
     const Carve k = carve(c);
     a.part = reinterpret_cast<float*>(em->base + k.part);
-    if (!accumulate) ESSPT_CUDA(em->err, set_to_zero(*em, a));
+    const int64_t bytes = accumulate ? 0 : c.n_rows * c.width * (int64_t)size;
+    const bool beside = bytes > kZeroInLine;
+    if (bytes > 0) ESSPT_CUDA(em->err, set_to_zero(*em, a, bytes, beside));
     ESSPT_CUDA(em->err, launch_sort(*em, k, a));
-    if (!accumulate) ESSPT_CUDA(em->err, cudaStreamWaitEvent(em->st, em->join, 0));
+    if (beside) ESSPT_CUDA(em->err, cudaStreamWaitEvent(em->st, em->join, 0));
   }
   const cudaError_t launched = by_type(c.dtype, bytes, [&](auto* type, auto vec, auto k) {
     using T = std::remove_pointer_t<decltype(type)>;
