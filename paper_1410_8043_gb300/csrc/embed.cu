@@ -734,9 +734,13 @@ int lanes_of(int vectors) {
   return lanes;
 }
 
-// Whether a call of n tokens goes by one kernel: few of them, and a block's rows and a place fit 32 bits.
-bool does_few(int64_t n, int64_t V, int32_t D) {
-  if (n > kFew) return false;
+// Whether a call of n tokens goes by one kernel: up to kAlwaysFew of them, or 3.5 MB of rows (a popular row's are added by one
+// SM), and a block's rows and a place fit 32 bits.  Measured in a graph, one kernel and by the sort, us: 4000 tokens, 5000
+// rows of 100 fp32 values 14.5 and 20.5, of 1000 21 and 25; 8000 of 100 values 20.6 and 20.6, of 257 25.6 and 23.3, of 1000
+// 33 and 29; 16000 of 16 values 25 and 22, of 100 37 and 22.  The sort's six or seven launches cost the host 20 us too.
+constexpr int kAlwaysFew = 4096;
+bool does_few(int64_t n, int64_t V, int32_t D, size_t size) {
+  if (n > kFew || (n > kAlwaysFew && n * D * (int64_t)size > 3'500'000)) return false;
   const int columns = (D + 31) / 32;  // at most so many tiles of columns
   const int64_t blocks = columns < kFewBlocks ? kFewBlocks / columns : 1;
   return (uint64_t)((V + blocks - 1) / blocks) << bits_of((uint32_t)n - 1) <= 0xffffffffull;
@@ -770,7 +774,7 @@ Carve carve(const esspt_embed_config& c) {
     return at;
   };
   k.status = take(sizeof(uint32_t));
-  if (c.backward && !does_few(c.max_tokens, c.n_rows, c.width)) {
+  if (c.backward && !does_few(c.max_tokens, c.n_rows, c.width, size_of(c.dtype))) {
     const int64_t n = c.max_tokens;
     const Digits d = digits(c.n_rows);
     for (int i = 0; i < 2; ++i) k.pairs[i] = take(n * sizeof(uint2));
@@ -894,7 +898,7 @@ esspt_status esspt_embed_create(const esspt_embed_config* cfg, void* d_workspace
   em->cfg = *cfg;
   em->st = static_cast<cudaStream_t>(cfg->stream);
   em->base = static_cast<char*>(d_workspace);
-  if (cfg->backward && !does_few(cfg->max_tokens, cfg->n_rows, cfg->width)) {
+  if (cfg->backward && !does_few(cfg->max_tokens, cfg->n_rows, cfg->width, size_of(cfg->dtype))) {
     cudaError_t e = cudaStreamCreateWithFlags(&em->side, cudaStreamNonBlocking);
     if (e == cudaSuccess) e = cudaEventCreateWithFlags(&em->fork, cudaEventDisableTiming);
     if (e == cudaSuccess) e = cudaEventCreateWithFlags(&em->join, cudaEventDisableTiming);
@@ -962,7 +966,7 @@ esspt_status esspt_embed_gradient(esspt_embed* em, const int32_t* d_ids, const v
   a.ids = d_ids, a.grad = d_grad, a.grad_stride = grad_stride, a.n = n, a.V = (int32_t)c.n_rows, a.D = c.width;
   a.scale = scale, a.accumulate = accumulate != 0, a.out = d_grad_w, a.status = reinterpret_cast<uint32_t*>(em->base);
   const int bytes = vector_bytes(c.width, size, (uintptr_t)d_grad | (uintptr_t)d_grad_w | (uintptr_t)grad_stride * size);
-  const bool few = does_few(n, c.n_rows, c.width);
+  const bool few = does_few(n, c.n_rows, c.width, size);
   if (!few) {
     const Carve k = carve(c);
     a.part = reinterpret_cast<float*>(em->base + k.part);
