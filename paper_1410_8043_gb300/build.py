@@ -18,7 +18,8 @@ LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libesspt.so")
 SOURCES = ["table_kernels.cu", "mf_kernels.cu", "seq_kernels.cu", "layout.cu", "stream_layout.cu", "objective.cu",
            "esspt_api.cu", "noalloc.cu", "softmax_api.cu", "softmax_few.cu",
-           "softmax_many.cu", "softmax_mma.cu", "embed.cu", "norm.cu", "adamw.cu"]
+           "softmax_many.cu", "softmax_mma.cu", "embed.cu", "norm.cu", "norm_f32.cu",
+           "norm_bf16.cu", "norm_f16.cu", "adamw.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -22,7 +22,7 @@ struct esspt_embed {
 namespace {
 
 constexpr uint32_t kErrId = 1u;
-constexpr int kThreads = 256, kDeep = 4;
+constexpr int kThreads = 256;
 
 thread_local Errors g_create;
 
@@ -37,19 +37,28 @@ struct Lookup {
   uint32_t* status;
 };
 
-// A block takes kThreads * kDeep vectors of the result, one behind the other; a thread
-// has kDeep loads under way.
+// Loads that a thread has under way: 64 bytes, or 16 of them.
+template <typename T, int VEC>
+constexpr int kDeep = VEC * sizeof(T) >= 16 ? 4 : VEC * sizeof(T) >= 4 ? 8 : 16;
+
+// A block takes kThreads * kDeep vectors of the result, one behind the other.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kThreads) lookup_kernel(Lookup a) {
-  const int64_t first = (int64_t)blockIdx.x * (kThreads * kDeep), all = a.n * a.per_row;
+  constexpr int kMany = kDeep<T, VEC>;
+  const int64_t first = (int64_t)blockIdx.x * (kThreads * kMany), all = a.n * a.per_row;
   const int64_t row0 = first / a.per_row;
   const uint32_t rest = (uint32_t)(first - row0 * a.per_row);
   const T* w = static_cast<const T*>(a.w);
   T* out = static_cast<T*>(a.out);
-  float x[kDeep][VEC];
+  const float inv = 1.f / (float)a.per_row;
+  float x[kMany][VEC];
 #pragma unroll
-  for (int k = 0; k < kDeep; ++k) {
-    const uint32_t at = rest + k * kThreads + threadIdx.x, row = at / (uint32_t)a.per_row, col = at - row * a.per_row;
+  for (int k = 0; k < kMany; ++k) {
+    const uint32_t at = rest + k * kThreads + threadIdx.x;
+    uint32_t row = (uint32_t)((float)at * inv);  // (of numbers below 2^14: off by one at most)
+    int32_t col = (int32_t)(at - row * a.per_row);
+    if (col < 0) --row, col += a.per_row;
+    if (col >= a.per_row) ++row, col -= a.per_row;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) x[k][i] = 0.f;
     if (first + k * kThreads + threadIdx.x < all) {
@@ -59,7 +68,7 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(Lookup a) {
     }
   }
 #pragma unroll
-  for (int k = 0; k < kDeep; ++k) {
+  for (int k = 0; k < kMany; ++k) {
     const int64_t at = first + k * kThreads + threadIdx.x;
     if (at >= all) break;
 #pragma unroll
@@ -934,13 +943,23 @@ esspt_status esspt_embed_lookup(esspt_embed* em, const void* d_w, int64_t w_stri
     return em->err.fail(ESSPT_EINVAL, "a pointer is not aligned to its type");
   Lookup a{d_w, w_stride, d_ids, n, (int32_t)c.n_rows, c.width, 0, scale, d_out, reinterpret_cast<uint32_t*>(em->base)};
   const int bytes = vector_bytes(c.width, size, (uintptr_t)d_w | (uintptr_t)d_out | (uintptr_t)w_stride * size);
-  const cudaError_t launched = by_type(c.dtype, bytes, [&](auto* type, auto vec, auto) {
+  auto go = [&](auto* type, auto vec) {
     using T = std::remove_pointer_t<decltype(type)>;
     a.per_row = c.width / vec;
-    const int64_t blocks = (n * a.per_row + kThreads * kDeep - 1) / (kThreads * kDeep);
+    const int64_t each = kThreads * kDeep<T, vec>, blocks = (n * a.per_row + each - 1) / each;
     lookup_kernel<T, vec><<<(unsigned)blocks, kThreads, 0, em->st>>>(a);
     return cudaGetLastError();
-  });
+  };
+  auto by_vector = [&](auto* type) {
+    constexpr int kSize = sizeof(*type);
+    if (bytes >= 16) return go(type, std::integral_constant<int, 16 / kSize>{});
+    if (bytes >= 8) return go(type, std::integral_constant<int, 8 / kSize>{});
+    if (bytes >= 4) return go(type, std::integral_constant<int, 4 / kSize>{});
+    return go(type, std::integral_constant<int, 1>{});
+  };
+  const cudaError_t launched = c.dtype == ESSPT_F32    ? by_vector((float*)nullptr)
+                               : c.dtype == ESSPT_BF16 ? by_vector((__nv_bfloat16*)nullptr)
+                                                       : by_vector((__half*)nullptr);
   ESSPT_CUDA(em->err, launched);
   return ESSPT_OK;
 }

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "chained.cuh"
+#include "norm.h"
 #include "operator.h"
 #include "ptx.cuh"
 #include "rows.cuh"
@@ -28,357 +29,6 @@ namespace {
 thread_local Errors g_create;
 
 constexpr int kMaxSms = 256;  // what the workspace is sized for
-constexpr int kThreads = 256;  // of a block whose rows take a warp or less
-constexpr int kMostWide = 512, kMostWarps = kMostWide / 32;  // of a wide row's block
-constexpr int kMostValues = 16;  // of a thread
-
-struct Norm {
-  const void *x, *dy;
-  int64_t x_stride, dy_stride, n;
-  int32_t D;
-  int32_t lanes;  // threads of a row: a power of two up to 32, or the block
-  float inv_D, eps;
-  const void *weight, *bias;
-  int weight_f32;  // their type, where it is not the rows'
-  void* y;        // dx in the backward pass
-  float *mean, *rstd;
-  float* part;    // [blocks][2][D] sums for dw and db
-  int want_w;     // whether they are asked for
-};
-
-// A thread's N vectors of a row as pairs of fp32 values (one value alone has a zero beside it).
-template <int VEC, int N>
-constexpr int kPairs = (VEC * N + 1) / 2;
-
-template <typename T, int VEC, int N>
-struct alignas(VEC * sizeof(T)) Pack {
-  T v[VEC];
-};
-
-template <typename T, int VEC, int N>
-__device__ __forceinline__ void to_pairs(const Pack<T, VEC, N> (&p)[N], u64 (&x)[kPairs<VEC, N>]) {
-#pragma unroll
-  for (int q = 0; q < kPairs<VEC, N>; ++q) {
-    const int e = 2 * q, f = e + 1;
-    x[q] = pack2(to_float(p[e / VEC].v[e % VEC]), f < VEC * N ? to_float(p[f % (VEC * N) / VEC].v[f % VEC]) : 0.f);
-  }
-}
-
-// Rows on their way to a thread.  Parts of 4 bytes or more go to shared memory, kDepth - 1 rows ahead; smaller ones
-// stay in registers, a row ahead.  What lies outside a row or the rows is zero.
-template <typename T, int VEC, int N>
-struct Incoming {
-  using P = Pack<T, VEC, N>;
-  static constexpr bool kAsync = sizeof(P) >= 4;
-  // (64 bytes a row for 512 threads, two such rows backward: 200 KB of three stages)
-  static constexpr int kDepth = sizeof(P) < 16 ? 2 : N * sizeof(P) < 64 ? 4 : 3;
-  P *first, *read, *write;  // the thread's slot of the first stage, of the one to take from, of the one to fetch to
-  int pitch;                // slots from one vector to the next
-  int stage_read, stage_write;
-  const T* at;              // its first vector of the next row to fetch
-  int64_t step;             // values to that of the one after
-  P next[kAsync ? 1 : N];
-
-  __device__ __forceinline__ static int bytes(int threads) { return kAsync ? kDepth * N * threads * (int)sizeof(P) : 0; }
-  __device__ __forceinline__ Incoming(char* slots, const T* from, int64_t step_, int D, int lane, int lanes)
-      : first(reinterpret_cast<P*>(slots) + threadIdx.x), read(first), write(first), pitch(blockDim.x), stage_read(0),
-        stage_write(0), at(from + lane * VEC), step(step_) {
-    if constexpr (kAsync) {
-#pragma unroll
-      for (int k = 0; k < kDepth * N; ++k)
-        if ((lane + k % N * lanes) * VEC >= D) first[k * pitch] = zero();
-    }
-  }
-  __device__ __forceinline__ static P zero() {
-    P p;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) p.v[j] = from_float<T>(0.f);
-    return p;
-  }
-  __device__ __forceinline__ void advance(P*& slot, int& stage) {
-    const bool wrap = stage == kDepth - 1;
-    slot = wrap ? first : slot + N * pitch;
-    stage = wrap ? 0 : stage + 1;
-  }
-  __device__ __forceinline__ void fetch(int D, int lane, int lanes, bool live) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const bool inside = (lane + i * lanes) * VEC < D;
-      if constexpr (kAsync) {
-        if (inside && live) {
-          if constexpr (sizeof(P) >= 16)
-            cp_async16(write + i * pitch, at + i * lanes * VEC);
-          else
-            cp_async4(write + i * pitch, at + i * lanes * VEC);
-        } else if (inside) {
-          write[i * pitch] = zero();
-        }
-      } else {
-        next[i].v[0] = inside && live ? at[i * lanes] : from_float<T>(0.f);
-      }
-    }
-    if constexpr (kAsync) advance(write, stage_write);
-    at += step;
-  }
-  __device__ __forceinline__ void take(u64 (&x)[kPairs<VEC, N>]) {
-    P p[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) p[i] = kAsync ? read[i * pitch] : next[kAsync ? 0 : i];
-    if constexpr (kAsync) advance(read, stage_read);
-    to_pairs<T, VEC, N>(p, x);
-  }
-};
-
-// Weights by single values: they may stand anywhere, and are read once.
-template <typename T, int VEC, int N>
-__device__ __forceinline__ void load_weights(const Norm& a, const void* from, float otherwise, int lane, u64 (&x)[kPairs<VEC, N>]) {
-  float w[2 * kPairs<VEC, N>];
-#pragma unroll
-  for (int e = 0; e < 2 * kPairs<VEC, N>; ++e) {
-    const int c = (lane + e / VEC * a.lanes) * VEC + e % VEC;
-    w[e] = otherwise;
-    if (from && e < VEC * N && c < a.D) w[e] = a.weight_f32 ? static_cast<const float*>(from)[c] : to_float(static_cast<const T*>(from)[c]);
-  }
-#pragma unroll
-  for (int q = 0; q < kPairs<VEC, N>; ++q) x[q] = pack2(w[2 * q], w[2 * q + 1]);
-}
-
-// The sum over the lanes of a warp that hold one row; over those that hold the warps' sums.
-__device__ __forceinline__ float lanes_sum(float v, int lanes) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    const float other = __shfl_xor_sync(0xffffffffu, v, off);
-    if (off < lanes) v += other;
-  }
-  return v;
-}
-__device__ __forceinline__ float warps_sum(float v, int warps) {  // (a power of two)
-  for (int off = warps / 2; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-  return v;
-}
-// Two sums over a warp: x's in the lower half of the lanes, y's in the upper.
-__device__ __forceinline__ float warp_sums(float x, float y) {
-  const bool upper = threadIdx.x & 16;
-  float v = (upper ? y : x) + __shfl_xor_sync(0xffffffffu, upper ? x : y, 16);
-#pragma unroll
-  for (int off = 8; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-  return v;
-}
-
-template <typename T, int VEC, int N>
-__device__ __forceinline__ void store_pairs(T* row, int D, int lane, int lanes, const u64 (&x)[kPairs<VEC, N>]) {
-  float v[2 * kPairs<VEC, N>];
-#pragma unroll
-  for (int q = 0; q < kPairs<VEC, N>; ++q) unpack2(x[q], v[2 * q], v[2 * q + 1]);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int c = (lane + i * lanes) * VEC;
-    float out[VEC];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) out[j] = v[i * VEC + j];
-    if (c < D) store_vec<T, VEC>(row + c, out);
-  }
-}
-
-template <typename T, int VEC, int N, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_forward_kernel(Norm a) {
-  extern __shared__ __align__(16) char dynamic[];
-  __shared__ float2 shared[2][kMostWarps];
-  constexpr int Q = kPairs<VEC, N>;
-  using In = Incoming<T, VEC, N>;
-  const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
-  const int groups = WIDE ? 1 : blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
-  int64_t t = (int64_t)blockIdx.x * groups + group, ahead = t;  // the row at hand, the next one to fetch
-  const int64_t step = (int64_t)gridDim.x * groups;
-  In in(dynamic, static_cast<const T*>(a.x) + t * a.x_stride, step * a.x_stride, a.D, lane, lanes);
-  auto fetch = [&]() {
-    in.fetch(a.D, lane, lanes, ahead < a.n);
-    if (In::kAsync) cp_async_commit();
-    ahead += step;
-  };
-#pragma unroll
-  for (int k = 0; k < In::kDepth - 1; ++k) fetch();
-  u64 w[Q], b[Q];
-  load_weights<T, VEC, N>(a, a.weight, 1.f, lane, w);
-  load_weights<T, VEC, N>(a, a.bias, 0.f, lane, b);
-  auto count = [&](int warp) {  // values of a warp
-    int c = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int left = a.D - (warp * 32 + i * lanes) * VEC;
-      c += left < 0 ? 0 : left < 32 * VEC ? left : 32 * VEC;
-    }
-    return (float)c;
-  };
-  int warps = 1;
-  while (WIDE && warps * 32 < blockDim.x) warps *= 2;
-  const int warp = threadIdx.x / 32, other = threadIdx.x & (warps - 1);
-  const float inv_own = WIDE ? 1.f / fmaxf(count(warp), 1.f) : a.inv_D;
-  const float count_other = WIDE && other < blockDim.x / 32 ? count(other) : 0.f;
-  int turn = 0;
-  for (int64_t t0 = (int64_t)blockIdx.x * groups; t0 < a.n; t0 += step, t += step, turn ^= 1) {
-    u64 x[Q];
-    if (In::kAsync) {
-      fetch();
-      cp_async_wait<In::kDepth - 1>();
-    }
-    in.take(x);
-    if (!In::kAsync) fetch();
-    // Mean and squares of differences to it, of the lanes of a warp.
-    u64 sum = x[0];
-#pragma unroll
-    for (int q = 1; q < Q; ++q) sum = add2(sum, x[q]);
-    float mean = lanes_sum(sum2(sum), WIDE ? 32 : lanes) * inv_own;
-    const u64 minus = pack2(-mean, -mean);
-    u64 squares = 0;
-    float single = 0.f;  // (of vectors of one value each its own)
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if ((lane + i * lanes) * VEC >= a.D) continue;
-      if constexpr (VEC == 1) {
-        float lo, hi;
-        unpack2(x[i / 2], lo, hi);
-        const float d = (i % 2 ? hi : lo) - mean;
-        single = fmaf(d, d, single);
-      } else {
-#pragma unroll
-        for (int q = i * VEC / 2; q < (i + 1) * VEC / 2; ++q) {
-          const u64 d = add2(x[q], minus);
-          squares = fma2(d, d, squares);
-        }
-      }
-    }
-    float m2 = lanes_sum(sum2(squares) + single, WIDE ? 32 : lanes);
-    if (WIDE) {
-      // Of the warps: squares about the row's mean are those about a warp's and their distance's.
-      if ((threadIdx.x & 31) == 0) shared[turn][warp] = make_float2(mean, m2);
-      __syncthreads();  // (the next row's go to the other half)
-      const float2 v = count_other > 0.f ? shared[turn][other] : make_float2(0.f, 0.f);
-      mean = warps_sum(count_other * v.x, warps) * a.inv_D;
-      m2 = warps_sum(v.y + count_other * (v.x - mean) * (v.x - mean), warps);
-    }
-    const float rstd = rsqrtf(m2 * a.inv_D + a.eps);
-    if (t >= a.n) continue;
-    const u64 m = pack2(-mean, -mean), r = pack2(rstd, rstd);
-#pragma unroll
-    for (int q = 0; q < Q; ++q) x[q] = fma2(mul2(add2(x[q], m), r), w[q], b[q]);
-    store_pairs<T, VEC, N>(static_cast<T*>(a.y) + t * a.D, a.D, lane, lanes, x);
-    if (lane == 0 && a.mean) a.mean[t] = mean, a.rstd[t] = rstd;
-  }
-}
-
-// A thread's columns are the same in all rows, and it keeps their sums for dw and db; at the end those of a
-// block are added, the groups of a warp by shuffles, then warp behind warp.
-template <typename T, int VEC, int N, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_backward_kernel(Norm a) {
-  extern __shared__ __align__(16) char dynamic[];
-  __shared__ float2 shared[2][kMostWarps];
-  constexpr int Q = kPairs<VEC, N>;
-  using In = Incoming<T, VEC, N>;
-  const int lanes = WIDE ? blockDim.x : a.lanes, lane = threadIdx.x & (WIDE ? ~0 : lanes - 1);
-  const int groups = WIDE ? 1 : blockDim.x / lanes, group = WIDE ? 0 : threadIdx.x / lanes;
-  int64_t t = (int64_t)blockIdx.x * groups + group, ahead = t;  // the row at hand, the next one to fetch
-  const int64_t step = (int64_t)gridDim.x * groups;
-  In in_x(dynamic, static_cast<const T*>(a.x) + t * a.x_stride, step * a.x_stride, a.D, lane, lanes);
-  In in_dy(dynamic + In::bytes(blockDim.x), static_cast<const T*>(a.dy) + t * a.dy_stride, step * a.dy_stride, a.D, lane, lanes);
-  auto fetch = [&]() {
-    in_x.fetch(a.D, lane, lanes, ahead < a.n);
-    in_dy.fetch(a.D, lane, lanes, ahead < a.n);
-    if (In::kAsync) cp_async_commit();
-    ahead += step;
-  };
-  auto stats = [&](int64_t at) { return at < a.n ? make_float2(a.mean[at], a.rstd[at]) : make_float2(0.f, 0.f); };
-#pragma unroll
-  for (int k = 0; k < In::kDepth - 1; ++k) fetch();
-  // Statistics of as many rows as a warp's part of a row has lanes, a lane each, and the next so many under way.
-  const int own_lanes = WIDE ? 32 : lanes, own_lane = threadIdx.x & (own_lanes - 1), lane0 = (threadIdx.x & 31) - own_lane;
-  float2 now = stats(t + own_lane * step), later = stats(t + (own_lanes + own_lane) * step);
-  int turns_left = own_lanes;
-  u64 w[Q], dw[Q], db[Q];
-  load_weights<T, VEC, N>(a, a.weight, 1.f, lane, w);
-#pragma unroll
-  for (int q = 0; q < Q; ++q) dw[q] = db[q] = 0;
-  int warps = 1;
-  while (WIDE && warps * 32 < blockDim.x) warps *= 2;
-  int turn = 0;
-  for (int64_t t0 = (int64_t)blockIdx.x * groups; t0 < a.n; t0 += step, t += step, turn ^= 1) {
-    u64 x[Q], dy[Q];
-    if (In::kAsync) {
-      fetch();
-      cp_async_wait<In::kDepth - 1>();
-    }
-    in_x.take(x);
-    in_dy.take(dy);
-    if (turns_left == 0) {
-      now = later, later = stats(t + (own_lanes + own_lane) * step);
-      turns_left = own_lanes;
-    }
-    float2 s;
-    s.x = __shfl_sync(0xffffffffu, now.x, lane0 + own_lanes - turns_left);
-    s.y = __shfl_sync(0xffffffffu, now.y, lane0 + own_lanes - turns_left);
-    --turns_left;
-    if (!In::kAsync) fetch();
-    const float rstd = s.y;
-    const u64 m = pack2(-s.x, -s.x), r = pack2(rstd, rstd);
-    u64 sum_g = 0, sum_gx = 0;  // (outside a row dy is zero)
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      x[q] = mul2(add2(x[q], m), r);
-      dw[q] = fma2(dy[q], x[q], dw[q]);
-      db[q] = add2(dy[q], db[q]);
-      dy[q] = mul2(dy[q], w[q]);
-      sum_g = add2(sum_g, dy[q]);
-      sum_gx = fma2(dy[q], x[q], sum_gx);
-    }
-    if (!a.y) continue;
-    if (WIDE) {
-      const float v = warp_sums(sum2(sum_g), sum2(sum_gx));
-      if ((threadIdx.x & 15) == 0) (threadIdx.x & 16 ? shared[turn][threadIdx.x / 32].y : shared[turn][threadIdx.x / 32].x) = v;
-      __syncthreads();  // (the next row's go to the other half)
-      const int other = threadIdx.x & (warps - 1);
-      s = other < blockDim.x / 32 ? shared[turn][other] : make_float2(0.f, 0.f);
-      s = make_float2(warps_sum(s.x, warps), warps_sum(s.y, warps));
-    } else {
-      s = make_float2(lanes_sum(sum2(sum_g), lanes), lanes_sum(sum2(sum_gx), lanes));
-    }
-    if (t >= a.n) continue;
-    const u64 g = pack2(-s.x * a.inv_D, -s.x * a.inv_D), gx = pack2(-s.y * a.inv_D, -s.y * a.inv_D);
-#pragma unroll
-    for (int q = 0; q < Q; ++q) x[q] = mul2(add2(fma2(x[q], gx, dy[q]), g), r);
-    store_pairs<T, VEC, N>(static_cast<T*>(a.y) + t * a.D, a.D, lane, lanes, x);
-  }
-  if (!a.want_w) return;
-  float* sums = reinterpret_cast<float*>(dynamic);  // [2][D] (rows of a warp: the copies' places, which are done with)
-  if (!WIDE) {
-    for (int off = 16; off >= lanes; off >>= 1)
-#pragma unroll
-      for (int q = 0; q < Q; ++q) {
-        dw[q] = add2(dw[q], __shfl_xor_sync(0xffffffffu, dw[q], off));
-        db[q] = add2(db[q], __shfl_xor_sync(0xffffffffu, db[q], off));
-      }
-    cp_async_wait_all();
-    __syncthreads();
-  }
-  float* part = a.part + (int64_t)blockIdx.x * 2 * a.D;
-  const int turns = WIDE ? 1 : blockDim.x / 32;
-  for (int k = 0; k < turns; ++k) {
-    if (WIDE || (threadIdx.x / 32 == k && (threadIdx.x & 31) < lanes)) {
-      float* to = k == turns - 1 ? part : sums;
-      float v[2 * Q], u[2 * Q];
-#pragma unroll
-      for (int q = 0; q < Q; ++q) unpack2(dw[q], v[2 * q], v[2 * q + 1]), unpack2(db[q], u[2 * q], u[2 * q + 1]);
-#pragma unroll
-      for (int e = 0; e < VEC * N; ++e) {
-        const int c = (lane + e / VEC * lanes) * VEC + e % VEC;
-        if (c < a.D) {
-          to[c] = (k ? sums[c] : 0.f) + v[e];
-          to[a.D + c] = (k ? sums[a.D + c] : 0.f) + u[e];
-        }
-      }
-    }
-    if (k < turns - 1) __syncthreads();
-  }
-}
 
 // dw and db from the blocks' sums: 32 columns to a block, whose warps take every 32nd block's.
 constexpr int kWeightWarps = 32;
@@ -409,39 +59,12 @@ __global__ void __launch_bounds__(32 * kWeightWarps) norm_weights_kernel(const f
 const char* config_fault(const esspt_norm_config* c) {
   if (!c) return "null config";
   if (c->max_rows < 1 || c->max_rows >= ((int64_t)1 << 31)) return "max_rows must be in [1, 2^31 - 1]";
-  if (c->width < 1 || c->width > 8192) return "width must be in [1, 8192]";
+  static_assert(kNormWidth == 8192, "the text below");
+  if (c->width < 1 || c->width > kNormWidth) return "width must be in [1, 8192]";
   if (c->dtype < ESSPT_F32 || c->dtype > ESSPT_F16) return "unknown dtype";
   if (c->weight_dtype != ESSPT_F32 && c->weight_dtype != c->dtype) return "weight_dtype must be fp32 or the rows'";
   if (!(c->eps > 0.f) || !std::isfinite(c->eps)) return "eps must be positive and finite";
   return nullptr;
-}
-
-// How rows of D values are spread over threads: those of a block and of a row, vectors of a thread (N), and
-// blocks of an SM.
-struct Spread {
-  int threads, lanes, n, resident;
-  bool wide;
-};
-Spread spread(int D, int vec, bool back) {
-  const int vectors = (D + vec - 1) / vec, most = kMostValues / vec;
-  Spread s{kThreads, 32, 1, 0, false};
-  auto next = [vec](int n) { return vec == 1 ? n * 4 : n * 2; };  // 1, 4, 16 single values; 1, 2, 4 vectors
-  if (vectors <= 32 * most) {
-    while (s.n * 32 < vectors) s.n = next(s.n);
-    while (s.lanes / 2 >= vectors && s.lanes > 1) s.lanes /= 2;
-  } else {
-    // the fewest idle lanes, where a thread's work for a row is about its values' and eight values' more
-    int best = 1 << 30;
-    for (int n = 1; n <= most; n = next(n)) {
-      const int threads = ((vectors + n - 1) / n + 31) / 32 * 32, cost = threads * (n * vec + 8);
-      if (threads <= kMostWide && cost <= best) best = cost, s.n = n, s.threads = threads;
-    }
-    s.wide = true;
-    s.lanes = s.threads;
-  }
-  // by registers: up to 64 with eight values; with 16 up to 80 forward, 120 backward (single values: 128)
-  s.resident = (s.n * vec <= 8 ? 1024 : vec > 1 && !back ? 768 : 512) / s.threads;
-  return s;
 }
 
 size_t workspace(const esspt_norm_config& c) {
@@ -451,53 +74,11 @@ size_t workspace(const esspt_norm_config& c) {
   return 256 + up256(blocks * 2 * c.width * sizeof(float));
 }
 
-template <bool BACK, typename T, int VEC, int N, bool WIDE>
-cudaError_t launch(const Spread& s, const Norm& a, unsigned blocks, cudaStream_t st) {
-  using In = Incoming<T, VEC, N>;
-  const size_t row = In::kAsync ? (size_t)In::kDepth * N * s.threads * VEC * sizeof(T) : 0;
-  auto* kernel = BACK ? norm_backward_kernel<T, VEC, N, WIDE> : norm_forward_kernel<T, VEC, N, WIDE>;
-  size_t shared = BACK ? 2 * row : row;
-  if (BACK && !WIDE && shared < 2 * a.D * sizeof(float)) shared = 2 * a.D * sizeof(float);
-  if (shared > 47 * 1024) {  // (static shared memory counts too)
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
-    if (e != cudaSuccess) return e;
-  }
-  kernel<<<blocks, s.threads, shared, st>>>(a);
-  return cudaGetLastError();
-}
-
-template <bool BACK, typename T, int VEC>
-cudaError_t launch_by_size(Norm& a, int sms, unsigned* blocks, cudaStream_t st) {
-  const Spread s = spread(a.D, VEC, BACK);
-  a.lanes = s.lanes;
-  const int64_t groups = (a.n + s.threads / s.lanes - 1) / (s.threads / s.lanes);
-  *blocks = (unsigned)(groups > sms * s.resident ? sms * s.resident : groups);
-  auto go = [&](auto n) {
-    return s.wide ? launch<BACK, T, VEC, n, true>(s, a, *blocks, st) : launch<BACK, T, VEC, n, false>(s, a, *blocks, st);
-  };
-  if (s.n == 1) return go(std::integral_constant<int, 1>{});
-  if constexpr (VEC > 1) {
-    if (s.n == 2) return go(std::integral_constant<int, 2>{});
-  }
-  if constexpr (VEC <= 4) {
-    if (s.n == 4) return go(std::integral_constant<int, 4>{});
-  }
-  if constexpr (VEC == 1) {
-    if (s.n == 16) return go(std::integral_constant<int, 16>{});
-  }
-  return cudaErrorInvalidConfiguration;
-}
-
-template <bool BACK>
-cudaError_t launch_norm(const esspt_norm_config& c, Norm& a, int bytes, int sms, unsigned* blocks, cudaStream_t st) {
+cudaError_t launch(const esspt_norm_config& c, Norm& a, bool back, int bytes, int sms, unsigned* blocks, cudaStream_t st) {
   a.weight_f32 = c.weight_dtype == ESSPT_F32;
-  auto go = [&](auto* type) {
-    using T = std::remove_pointer_t<decltype(type)>;
-    return bytes >= 16 ? launch_by_size<BACK, T, 16 / sizeof(T)>(a, sms, blocks, st) : launch_by_size<BACK, T, 1>(a, sms, blocks, st);
-  };
-  if (c.dtype == ESSPT_F32) return go((float*)nullptr);
-  if (c.dtype == ESSPT_BF16) return go((__nv_bfloat16*)nullptr);
-  return go((__half*)nullptr);
+  if (c.dtype == ESSPT_F32) return launch_norm<float>(a, back, bytes, sms, blocks, st);
+  if (c.dtype == ESSPT_BF16) return launch_norm<__nv_bfloat16>(a, back, bytes, sms, blocks, st);
+  return launch_norm<__half>(a, back, bytes, sms, blocks, st);
 }
 
 }  // namespace
@@ -550,7 +131,7 @@ esspt_status esspt_norm_forward(esspt_norm* nm, const void* d_x, int64_t x_strid
   a.weight = d_weight, a.bias = d_bias, a.y = d_y, a.mean = d_mean, a.rstd = d_rstd;
   unsigned blocks = 0;
   const int bytes = vector_bytes(c.width, size, (uintptr_t)d_x | (uintptr_t)d_y | (uintptr_t)x_stride * size);
-  ESSPT_CUDA(nm->err, launch_norm<false>(c, a, bytes, nm->sms, &blocks, nm->st));
+  ESSPT_CUDA(nm->err, launch(c, a, false, bytes, nm->sms, &blocks, nm->st));
   return ESSPT_OK;
 }
 
@@ -583,7 +164,7 @@ esspt_status esspt_norm_backward(esspt_norm* nm, const void* d_dy, int64_t dy_st
   unsigned blocks = 0;
   const int bytes = vector_bytes(c.width, size, (uintptr_t)d_x | (uintptr_t)d_dy | (uintptr_t)d_dx |
                                                     (uintptr_t)x_stride * size | (uintptr_t)dy_stride * size);
-  ESSPT_CUDA(nm->err, launch_norm<true>(c, a, bytes, nm->sms, &blocks, nm->st));
+  ESSPT_CUDA(nm->err, launch(c, a, true, bytes, nm->sms, &blocks, nm->st));
   if (!a.want_w) return ESSPT_OK;
   const unsigned columns = (2 * c.width + 31) / 32;
   auto weights = [&](auto* type) {
