@@ -37,31 +37,44 @@ struct Lookup {
   uint32_t* status;
 };
 
-// Loads that a thread has under way: 64 bytes, or 16 of them.
+// Loads that a thread has under way: 64 bytes, or eight of them.
 template <typename T, int VEC>
-constexpr int kDeep = VEC * sizeof(T) >= 16 ? 4 : VEC * sizeof(T) >= 4 ? 8 : 16;
+constexpr int kDeep = VEC * sizeof(T) >= 16 ? 4 : 8;
 
-// A block takes kThreads * kDeep vectors of the result, one behind the other.
-template <typename T, int VEC>
+// A block takes kThreads * kDeep vectors of the result, one behind the other, whatever rows they are of.  PAIRS: rows of an
+// odd number of 16-bit values, of which two of the result, from one row or two, make a word to write.  (60000 rows of 1001
+// bf16 values: 146 us value by value.)
+template <typename T, int VEC, bool PAIRS>
 __global__ void __launch_bounds__(kThreads) lookup_kernel(Lookup a) {
-  constexpr int kMany = kDeep<T, VEC>;
-  const int64_t first = (int64_t)blockIdx.x * (kThreads * kMany), all = a.n * a.per_row;
-  const int64_t row0 = first / a.per_row;
-  const uint32_t rest = (uint32_t)(first - row0 * a.per_row);
+  constexpr int kMany = kDeep<T, VEC>, kEach = PAIRS ? 2 : VEC;
+  const int64_t first = (int64_t)blockIdx.x * (kThreads * kMany), all = PAIRS ? (a.n * a.D + 1) / 2 : a.n * a.per_row;
+  const int64_t row0 = (PAIRS ? 2 * first : first) / a.per_row;
+  const uint32_t rest = (uint32_t)((PAIRS ? 2 * first : first) - row0 * a.per_row);
   const T* w = static_cast<const T*>(a.w);
   T* out = static_cast<T*>(a.out);
   const float inv = 1.f / (float)a.per_row;
-  float x[kMany][VEC];
+  auto row_of = [&](uint32_t row) -> const T* {  // null: padding, or behind the last
+    const int32_t id = row0 + row < a.n ? a.ids[row0 + row] : -1;
+    if (id >= a.V) atomicOr(a.status, kErrId);
+    return (uint32_t)id < (uint32_t)a.V ? w + id * a.w_stride : nullptr;
+  };
+  float x[kMany][kEach];
 #pragma unroll
   for (int k = 0; k < kMany; ++k) {
-    const uint32_t at = rest + k * kThreads + threadIdx.x;
+    const uint32_t at = rest + (k * kThreads + threadIdx.x) * (PAIRS ? 2 : 1);
     uint32_t row = (uint32_t)((float)at * inv);  // (of numbers below 2^14: off by one at most)
     int32_t col = (int32_t)(at - row * a.per_row);
     if (col < 0) --row, col += a.per_row;
     if (col >= a.per_row) ++row, col -= a.per_row;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) x[k][i] = 0.f;
-    if (first + k * kThreads + threadIdx.x < all) {
+    for (int i = 0; i < kEach; ++i) x[k][i] = 0.f;
+    if (first + k * kThreads + threadIdx.x >= all) continue;
+    if constexpr (PAIRS) {
+      const T* from = row_of(row);
+      if (from) x[k][0] = to_float(from[col]);
+      if (++col == a.per_row) from = row_of(row + 1), col = 0;
+      if (from) x[k][1] = to_float(from[col]);
+    } else {
       const int32_t id = a.ids[row0 + row];
       if (id >= a.V) atomicOr(a.status, kErrId);
       if ((uint32_t)id < (uint32_t)a.V) load_vec<T, VEC>(w + id * a.w_stride + col * VEC, x[k]);
@@ -72,8 +85,11 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(Lookup a) {
     const int64_t at = first + k * kThreads + threadIdx.x;
     if (at >= all) break;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) x[k][i] *= a.scale;
-    store_vec<T, VEC>(out + at * VEC, x[k]);
+    for (int i = 0; i < kEach; ++i) x[k][i] *= a.scale;
+    if (PAIRS && 2 * at + 1 == a.n * a.D)
+      out[2 * at] = from_float<T>(x[k][0]);
+    else
+      store_vec<T, kEach>(out + at * kEach, x[k]);
   }
 }
 
@@ -943,19 +959,22 @@ esspt_status esspt_embed_lookup(esspt_embed* em, const void* d_w, int64_t w_stri
     return em->err.fail(ESSPT_EINVAL, "a pointer is not aligned to its type");
   Lookup a{d_w, w_stride, d_ids, n, (int32_t)c.n_rows, c.width, 0, scale, d_out, reinterpret_cast<uint32_t*>(em->base)};
   const int bytes = vector_bytes(c.width, size, (uintptr_t)d_w | (uintptr_t)d_out | (uintptr_t)w_stride * size);
-  auto go = [&](auto* type, auto vec) {
+  auto go = [&](auto* type, auto vec, auto pairs) {
     using T = std::remove_pointer_t<decltype(type)>;
     a.per_row = c.width / vec;
-    const int64_t each = kThreads * kDeep<T, vec>, blocks = (n * a.per_row + each - 1) / each;
-    lookup_kernel<T, vec><<<(unsigned)blocks, kThreads, 0, em->st>>>(a);
+    const int64_t each = kThreads * kDeep<T, vec>, all = pairs ? (n * c.width + 1) / 2 : n * a.per_row;
+    lookup_kernel<T, vec, pairs><<<(unsigned)((all + each - 1) / each), kThreads, 0, em->st>>>(a);
     return cudaGetLastError();
   };
   auto by_vector = [&](auto* type) {
     constexpr int kSize = sizeof(*type);
-    if (bytes >= 16) return go(type, std::integral_constant<int, 16 / kSize>{});
-    if (bytes >= 8) return go(type, std::integral_constant<int, 8 / kSize>{});
-    if (bytes >= 4) return go(type, std::integral_constant<int, 4 / kSize>{});
-    return go(type, std::integral_constant<int, 1>{});
+    if (bytes >= 16) return go(type, std::integral_constant<int, 16 / kSize>{}, std::false_type{});
+    if (bytes >= 8) return go(type, std::integral_constant<int, 8 / kSize>{}, std::false_type{});
+    if (bytes >= 4) return go(type, std::integral_constant<int, 4 / kSize>{}, std::false_type{});
+    if constexpr (kSize == 2) {
+      if (!misaligned(d_out, 4)) return go(type, std::integral_constant<int, 1>{}, std::true_type{});
+    }
+    return go(type, std::integral_constant<int, 1>{}, std::false_type{});
   };
   const cudaError_t launched = c.dtype == ESSPT_F32    ? by_vector((float*)nullptr)
                                : c.dtype == ESSPT_BF16 ? by_vector((__nv_bfloat16*)nullptr)
