@@ -13,7 +13,13 @@ would have stored them.
 
     python -m paper_1410_8043_gb300.implicit --workload tiny --clocks 40 --narrow 8
 
-The output is one JSON object per reported clock, one line each.
+With `--dense` the same model is also trained by itself, without a table of versions:
+rows are looked up (`Embedding`), normed (`LayerNorm`), scored against all items (`SoftmaxHead`), and the
+gradients go back the same way to one `AdamW` step over all parameters (`DenseTrainer`).
+
+    python -m paper_1410_8043_gb300.implicit --workload tiny --clocks 0 --narrow 0 --dense 40 --bits 8
+
+The output is one JSON object per reported clock or step, one line each.
 """
 from __future__ import annotations
 
@@ -98,6 +104,57 @@ class Trainer:
         self.table.close()
 
 
+class DenseTrainer:
+    """One model by itself: scores of all items from normed rows of a table of inputs.
+
+    `n_inputs` rows (users, say) are the inputs, or, if it is None, the items themselves (what was picked
+    before predicts what is picked next), whose rows then get both gradients.  Parameters are fp32; with a
+    16-bit `dtype` the tables have copies of that type, on which everything but the norm's weights runs.  All handles run on
+    the current stream at construction; a step with `lr` on the device may be captured in a CUDA graph.
+    """
+
+    def __init__(self, n_inputs: int | None, n_items: int, K: int, batch: int, dtype=torch.float32, state_bits: int = 32,
+                 scale: float = 1.0, seed: int = 1, init: float = 0.1, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0):
+        self.tied, self.scale = n_inputs is None, scale
+        g = torch.Generator("cuda").manual_seed(seed)
+        rows = [n_items] if self.tied else [n_items, n_inputs]
+        tables = [torch.randn((n, K), generator=g, device="cuda") * init for n in rows]
+        self.weight, self.bias = torch.ones(K, device="cuda"), torch.zeros(K, device="cuda")
+        self.params = tables + [self.weight, self.bias]
+        run_on = tables if dtype is torch.float32 else [t.to(dtype) for t in tables]
+        self.items, self.inputs = run_on[0], run_on[-1]
+        copies = [None] * 4 if dtype is torch.float32 else run_on + [None, None]
+        self.embedding = esspt.Embedding(batch, rows[-1], K, dtype=dtype)
+        self.norm = esspt.LayerNorm(batch, K, dtype=dtype, weight_dtype=torch.float32)
+        self.head = esspt.SoftmaxHead(batch, n_items, K, dtype=dtype)
+        self.adamw = esspt.AdamW(self.params, copies=copies[:len(self.params)], betas=betas, eps=eps,
+                                 weight_decay=[weight_decay] * len(tables) + [0.0, 0.0], state_bits=state_bits, seed=seed)
+
+    def gradients(self, inputs, picks, weight=None):
+        """Of the sum of a batch's (weighted) losses: the losses, and a gradient for each of `params`."""
+        x = self.embedding.lookup(self.inputs, inputs, scale=self.scale)
+        n = self.norm.forward(x, self.weight, self.bias)
+        r = self.head.loss(n.y, self.items, picks, weight=weight)
+        b = self.norm.backward(r.grad_h, x, n.mean, n.rstd, self.weight)
+        if self.tied:
+            tables = [self.embedding.gradient(inputs, b.grad_x, scale=self.scale, grad_w=r.grad_w, accumulate=True)]
+        else:
+            tables = [r.grad_w, self.embedding.gradient(inputs, b.grad_x, scale=self.scale)]
+        return r.loss, tables + [b.grad_weight, b.grad_bias]
+
+    def learn(self, inputs, picks, lr, weight=None):
+        """One step on a batch of inputs (ids, negative ones padding) and the items picked after them."""
+        loss, grads = self.gradients(inputs, picks, weight)
+        self.adamw.step(grads, lr)
+        return loss
+
+    def close(self):
+        self.embedding.poll()
+        self.head.poll()
+        for handle in (self.embedding, self.norm, self.head, self.adamw):
+            handle.close()
+
+
 def top_scores(h, r, top: int, piece: int = 65536):
     """The `top` largest scores h r^T of every row and their items (int32), by pieces of `r`,
     so that the scores of a large catalogue are never there as a whole."""
@@ -147,6 +204,19 @@ def run(w, clocks: int, batch: int, eta: float, narrow: int, narrow_eta: float, 
     wide.close()
 
 
+def run_dense(w, steps: int, batch: int, lr: float, bits: int, dtype, every: int, emit) -> None:
+    """The model by itself on the same events, all workers' batches together."""
+    d = w.make_data()
+    worker, _ = w.partition()
+    liked = np.flatnonzero(d.D >= np.quantile(d.D, 0.75))
+    model = DenseTrainer(w.n_users, w.n_items, w.K, batch * w.P, dtype=dtype, state_bits=bits)
+    for c, parts in enumerate(batches(d.i[liked], d.j[liked], worker, w.P, batch, steps, 3), 1):
+        loss = model.learn(torch.cat([u for _, u, _ in parts]), torch.cat([k for _, _, k in parts]), lr)
+        if c % every == 0 or c in (1, steps):
+            emit({"model": f"dense K={w.K}", "step": c, "loss": float(loss.mean())})
+    model.close()
+
+
 def main(argv=None) -> int:
     from gen import workload
 
@@ -160,9 +230,19 @@ def main(argv=None) -> int:
                     help="its step size per event (a popular item is on most lists: its row's steps add up)")
     ap.add_argument("--top", type=int, default=20, help="length of the teacher's lists")
     ap.add_argument("--every", type=int, default=10, help="clocks between reports")
+    ap.add_argument("--dense", type=int, default=0, help="steps of the model by itself, by AdamW (0: none)")
+    ap.add_argument("--lr", type=float, default=0.01, help="its step size")
+    ap.add_argument("--bits", type=int, default=32, choices=(32, 8), help="bits of its moments")
+    ap.add_argument("--dtype", default="float32", choices=("float32", "bfloat16", "float16"), help="what it runs in")
     args = ap.parse_args(argv)
-    run(workload(args.workload), args.clocks, args.batch, args.eta, args.narrow, args.narrow_eta, args.top, args.every,
-        lambda row: print(json.dumps(row), file=sys.stdout, flush=True))
+
+    def emit(row):
+        print(json.dumps(row), file=sys.stdout, flush=True)
+
+    if args.clocks:
+        run(workload(args.workload), args.clocks, args.batch, args.eta, args.narrow, args.narrow_eta, args.top, args.every, emit)
+    if args.dense:
+        run_dense(workload(args.workload), args.dense, args.batch, args.lr, args.bits, getattr(torch, args.dtype), args.every, emit)
     return 0
 
 
