@@ -1,7 +1,10 @@
 // AdamW over many tensors at once, moments in 32 or in 8 bits: kernels and C-ABI.
 //
 // The tensors are cut into tiles of 4096 values.  Blocks stay and go through tiles, the next one's record under way;
-// a warp takes 512 values of a tile, four blocks of 128, four values a thread of each, all loads first.
+// a warp takes 512 values of a tile, four blocks of 128, four values a thread of each.  With 32-bit moments all loads of a
+// tile come first, and memory is the bound: 31 million values with 16-bit copies move 28 bytes each at 6.4 TB/s.  With 8 bits
+// the next tile is copied to shared memory meanwhile, and arithmetic is the bound, some 95 instructions a value: 192 million
+// values take 617 us at 16 bytes each, 5 TB/s.
 #include <cfloat>
 #include <cmath>
 #include <cstring>
@@ -10,6 +13,7 @@
 #include <vector>
 
 #include "operator.h"
+#include "ptx.cuh"
 #include "rows.cuh"
 
 using namespace esspt;
@@ -19,10 +23,10 @@ namespace {
 constexpr int kBlock = 128;     // values with an exponent of their own (8 bits)
 constexpr int kTile = 4096;     // values a block takes
 constexpr int kThreads = 256;
-constexpr int kBatch = 4;       // blocks of 128 whose loads a warp has under way together
-// Blocks of an SM: 128 registers for the loads of 32-bit moments, 80 for the arithmetic of 8-bit ones.  (31 million
-// values in 32 bits with 16-bit copies: 137 us, three blocks 145, batches of two 145; 192 million in 8 bits: 867, two blocks 914.)
-constexpr int resident(int bits) { return bits == 32 ? 2 : 3; }
+constexpr int kMine = kTile / (kThreads / 32), kBatch = kMine / kBlock;  // values and blocks of a warp
+// Blocks of an SM: 128 registers for the loads of 32-bit moments (31 million values with 16-bit copies: 137 us, three blocks
+// 145); for 8-bit ones 180 KB of stages.
+constexpr int kResident = 2;
 constexpr int kGroup = 440;     // tensors of a launch: their gradients' addresses are among its parameters
 constexpr uint32_t kNoNumber = 255;  // exponent of a block that is NaN
 
@@ -46,7 +50,8 @@ struct State {
 
 struct Moments {
   float *m, *v;             // 32 bits
-  uint8_t *mc, *uc, *me, *ue;  // 8 bits: codes and exponents
+  uint8_t *mc, *uc;         // 8 bits: codes, and
+  uint32_t* e;              // exponents of a block, m's + 256 u's
 };
 
 struct Step {
@@ -166,91 +171,151 @@ struct Rates {
   uint32_t key;
 };
 
-// B blocks of 128 values, one behind the other, by a warp.  Sums and products of moments are single operations (not
-// contracted): 8-bit moments are the same wherever they are computed.
-template <int BITS, typename G, typename H, bool COPY, int B, bool VECTOR>
-__device__ __forceinline__ void update(const Step& a, const Tile& t, const G* grad, const Rates& c, int lane, int i, int left) {
-  float p[B][4], g[B][4], m[B][4], v[B][4];
-  uint32_t mc[B][4], uc[B][4], me[B], ue[B];
+// What a thread has of a block of 128 values.
+template <int BITS>
+struct Values {
+  float p[4], g[4], m[4], v[4];  // (moments of 32 bits)
+  uint32_t mc[4], uc[4], e;      // (of 8)
+};
+
+template <int BITS, typename G, bool VECTOR>
+__device__ __forceinline__ void read(const Step& a, const Tile& t, const G* grad, int lane, int i, int left, Values<BITS>& x) {
   const int64_t at = t.at + i;
-#pragma unroll
-  for (int k = 0; k < B; ++k) {
-    get4(t.p + i + k * kBlock, VECTOR, lane, left, p[k]);
-    get4(grad + i + k * kBlock, VECTOR, lane, left, g[k]);
-    if (BITS == 32) {
-      get4(a.held.m + at + k * kBlock, VECTOR, lane, left, m[k]);
-      get4(a.held.v + at + k * kBlock, VECTOR, lane, left, v[k]);
-    } else {
-      get_codes(a.held.mc + at + k * kBlock, VECTOR, lane, mc[k]);
-      get_codes(a.held.uc + at + k * kBlock, VECTOR, lane, uc[k]);
-      me[k] = a.held.me[at / kBlock + k], ue[k] = a.held.ue[at / kBlock + k];
-    }
+  get4(t.p + i, VECTOR, lane, left, x.p);
+  get4(grad + i, VECTOR, lane, left, x.g);
+  if (BITS == 32) {
+    get4(a.held.m + at, VECTOR, lane, left, x.m);
+    get4(a.held.v + at, VECTOR, lane, left, x.v);
+  } else {
+    get_codes(a.held.mc + at, VECTOR, lane, x.mc);
+    get_codes(a.held.uc + at, VECTOR, lane, x.uc);
+    x.e = a.held.e[at / kBlock];
   }
+}
+
+// The step of a block.  Sums and products of moments are single operations (not contracted): 8-bit moments are the same
+// wherever they are computed.
+template <int BITS, typename H, bool COPY, bool VECTOR>
+__device__ __forceinline__ void update(const Step& a, const Tile& t, const Rates& c, int lane, int i, int left, Values<BITS>& x) {
+  const int64_t at = t.at + i;
+  const uint32_t me = x.e & 255u, ue = x.e >> 8;
   const float keep = 1.f - c.lr * t.decay;
+  // (a NaN block's codes count for nothing)
+  const float b1 = BITS == 8 ? unless_nan(a.b1, me) : a.b1, b2 = BITS == 8 ? unless_nan(a.b2, ue) : a.b2;
+  float u[4];
 #pragma unroll
-  for (int k = 0; k < B; ++k) {
-    float u[4];
-    // (a NaN block's codes count for nothing)
-    const float b1 = BITS == 8 ? unless_nan(a.b1, me[k]) : a.b1, b2 = BITS == 8 ? unless_nan(a.b2, ue[k]) : a.b2;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (BITS == 8) {
-        const float old = held<4>(uc[k][j], ue[k]);
-        m[k][j] = held_m(mc[k][j], me[k]), v[k][j] = __fmul_rn(old, old);
-      }
-      if (!VECTOR && lane + 32 * j >= left) m[k][j] = v[k][j] = 0.f;  // between tensors
-      const float gs = __fmul_rn(g[k][j], c.scale);
-      m[k][j] = __fadd_rn(__fmul_rn(m[k][j], b1), __fmul_rn(gs, a.one_b1));
-      v[k][j] = __fadd_rn(__fmul_rn(v[k][j], b2), __fmul_rn(__fmul_rn(gs, gs), a.one_b2));
-      u[j] = BITS == 8 ? __fsqrt_rn(v[k][j]) : sqrt_fast(v[k][j]);
-      p[k][j] = fmaf(p[k][j], keep, -(c.rate * m[k][j]) * reciprocal_fast(fmaf(u[j], c.inv_root, a.eps)));
+  for (int j = 0; j < 4; ++j) {
+    if (BITS == 8) {
+      const float old = held<4>(x.uc[j], ue);
+      x.m[j] = held_m(x.mc[j], me), x.v[j] = __fmul_rn(old, old);
     }
-    put4(t.p + i + k * kBlock, VECTOR, lane, left, p[k]);
-    if (COPY) put4(static_cast<H*>(t.copy) + i + k * kBlock, VECTOR, lane, left, p[k]);
-    if (BITS == 32) {
-      put4(a.held.m + at + k * kBlock, VECTOR, lane, left, m[k]);
-      put4(a.held.v + at + k * kBlock, VECTOR, lane, left, v[k]);
-    } else {
-      me[k] = block_exponent<3>(largest(m[k])), ue[k] = block_exponent<4>(largest(u));
-      const int64_t place = at + k * kBlock + (VECTOR ? lane * 4 : lane);
-      // (a block does not cross a multiple of 2^32)
-      const uint32_t from = (uint32_t)(place >> 32) * 0x85EBCA77u + (uint32_t)place * 0x9E3779B1u;
-      uint32_t high[4], low[4];
+    if (!VECTOR && lane + 32 * j >= left) x.m[j] = x.v[j] = 0.f;  // between tensors
+    const float gs = __fmul_rn(x.g[j], c.scale);
+    x.m[j] = __fadd_rn(__fmul_rn(x.m[j], b1), __fmul_rn(gs, a.one_b1));
+    x.v[j] = __fadd_rn(__fmul_rn(x.v[j], b2), __fmul_rn(__fmul_rn(gs, gs), a.one_b2));
+    u[j] = BITS == 8 ? __fsqrt_rn(x.v[j]) : sqrt_fast(x.v[j]);
+    x.p[j] = fmaf(x.p[j], keep, -(c.rate * x.m[j]) * reciprocal_fast(fmaf(u[j], c.inv_root, a.eps)));
+  }
+  put4(t.p + i, VECTOR, lane, left, x.p);
+  if (COPY) put4(static_cast<H*>(t.copy) + i, VECTOR, lane, left, x.p);
+  if (BITS == 32) {
+    put4(a.held.m + at, VECTOR, lane, left, x.m);
+    put4(a.held.v + at, VECTOR, lane, left, x.v);
+    return;
+  }
+  const uint32_t new_me = block_exponent<3>(largest(x.m)), new_ue = block_exponent<4>(largest(u));
+  const int64_t place = at + (VECTOR ? lane * 4 : lane);
+  // (a block does not cross a multiple of 2^32)
+  const uint32_t from = (uint32_t)(place >> 32) * 0x85EBCA77u + (uint32_t)place * 0x9E3779B1u;
+  uint32_t high[4], low[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t h = mix((from + (VECTOR ? j : 32 * j) * 0x9E3779B1u) ^ c.key);
-        high[j] = h >> 16, low[j] = h & 0xffffu;
-      }
-      hold_m(m[k], me[k], high, mc[k]);
-      hold<4, true>(u, ue[k], low, uc[k]);
-      put_codes(a.held.mc + at + k * kBlock, VECTOR, lane, mc[k]);
-      put_codes(a.held.uc + at + k * kBlock, VECTOR, lane, uc[k]);
-      if (lane == 0) a.held.me[at / kBlock + k] = (uint8_t)me[k], a.held.ue[at / kBlock + k] = (uint8_t)ue[k];
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t h = mix((from + (VECTOR ? j : 32 * j) * 0x9E3779B1u) ^ c.key);
+    high[j] = h >> 16, low[j] = h & 0xffffu;
+  }
+  hold_m(x.m, new_me, high, x.mc);
+  hold<4, true>(u, new_ue, low, x.uc);
+  put_codes(a.held.mc + at, VECTOR, lane, x.mc);
+  put_codes(a.held.uc + at, VECTOR, lane, x.uc);
+  if (lane == 0) a.held.e[at / kBlock] = new_me | new_ue << 8;
+}
+
+// A warp's part of a tile whose values it cannot have four at a time, or not all of them.
+template <int BITS, typename G, typename H, bool COPY>
+__device__ __forceinline__ void update_singly(const Step& a, const Tile& t, const G* grad, bool aligned, const Rates& c, int lane, int begin) {
+  for (int i = begin; i < begin + kMine && i < t.count; i += kBlock) {
+    Values<BITS> x;
+    if (aligned && t.count >= i + kBlock) {
+      read<BITS, G, true>(a, t, grad, lane, i, kBlock, x);
+      update<BITS, H, COPY, true>(a, t, c, lane, i, kBlock, x);
+    } else {
+      read<BITS, G, false>(a, t, grad, lane, i, t.count - i, x);
+      update<BITS, H, COPY, false>(a, t, c, lane, i, t.count - i, x);
     }
   }
 }
 
+// Tiles of a block on their way to it (8 bits): a thread's part of a warp's four blocks of 128 values, in shared memory of
+// its own.
+struct Stage {
+  float4 p[kBatch][kThreads];
+  float4 g[kBatch][kThreads];  // (16-bit gradients: the first half of it)
+  uint32_t mc[kBatch][kThreads], uc[kBatch][kThreads], e[kBatch][kThreads];
+};
+
+// A tile by the block, or (`stage` given) what of it has come to shared memory.
 template <int BITS, typename H, bool COPY>
-__device__ __forceinline__ void update_tile(const Step& a, const Tile& t, const void* grads, const Rates& c, int lane, int warp) {
+__device__ __forceinline__ void update_tile(const Step& a, const Tile& t, const void* grads, const Rates& c, int lane, int warp,
+                                            const Stage* stage) {
   using G = std::conditional_t<COPY, H, float>;
   const G* grad = static_cast<const G*>(grads) + t.first;
   const bool aligned = t.vector && (uintptr_t)grad % (4 * sizeof(G)) == 0;
-  constexpr int kMine = kTile / (kThreads / 32), kAtOnce = kBatch * kBlock;
   const int begin = warp * kMine;
-  if (aligned && t.count >= begin + kMine) {
-    for (int i = begin; i < begin + kMine; i += kAtOnce) update<BITS, G, H, COPY, kBatch, true>(a, t, grad, c, lane, i, kAtOnce);
-    return;
+  if (!aligned || t.count < begin + kMine) return update_singly<BITS, G, H, COPY>(a, t, grad, aligned, c, lane, begin);
+  if constexpr (BITS == 32) {
+    Values<BITS> x[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) read<BITS, G, true>(a, t, grad, lane, begin + k * kBlock, kBlock, x[k]);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) update<BITS, H, COPY, true>(a, t, c, lane, begin + k * kBlock, kBlock, x[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      Values<BITS> x;
+      const int tid = threadIdx.x;
+      load_vec<float, 4>(reinterpret_cast<const float*>(&stage->p[k][tid]), x.p);
+      load_vec<G, 4>(reinterpret_cast<const G*>(&stage->g[k][tid]), x.g);
+      const uint32_t mc = stage->mc[k][tid], uc = stage->uc[k][tid];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x.mc[j] = mc >> 8 * j & 255u, x.uc[j] = uc >> 8 * j & 255u;
+      x.e = stage->e[k][tid];
+      update<BITS, H, COPY, true>(a, t, c, lane, begin + k * kBlock, kBlock, x);
+    }
   }
-  for (int i = begin; i < begin + kMine && i < t.count; i += kBlock) {
-    if (aligned && t.count >= i + kBlock)
-      update<BITS, G, H, COPY, 1, true>(a, t, grad, c, lane, i, kBlock);
+}
+
+// Sends for what update_tile() takes from a stage.
+__device__ __forceinline__ void fetch_tile(const Step& a, const Tile& t, int lane, int warp, Stage* stage) {
+  const void* grads = a.grads[t.tensor - a.first_tensor];
+  const int size = t.copy ? 2 : 4, begin = warp * kMine, tid = threadIdx.x;
+  const char* grad = static_cast<const char*>(grads) + t.first * size;
+  if (!grads || !t.vector || (uintptr_t)grad % (4 * size) != 0 || t.count < begin + kMine) return;
+#pragma unroll
+  for (int k = 0; k < kBatch; ++k) {
+    const int i = begin + k * kBlock + lane * 4;
+    cp_async16(&stage->p[k][tid], t.p + i);
+    if (t.copy)
+      cp_async8(&stage->g[k][tid], grad + i * 2);
     else
-      update<BITS, G, H, COPY, 1, false>(a, t, grad, c, lane, i, t.count - i);
+      cp_async16(&stage->g[k][tid], grad + i * 4);
+    cp_async4(&stage->mc[k][tid], a.held.mc + t.at + i);
+    cp_async4(&stage->uc[k][tid], a.held.uc + t.at + i);
+    cp_async4(&stage->e[k][tid], a.held.e + (t.at + i) / kBlock);
   }
 }
 
 template <int BITS, typename H>
-__global__ void __launch_bounds__(kThreads, resident(BITS)) adamw_kernel(__grid_constant__ const Step a) {
+__global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(__grid_constant__ const Step a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   Tile next{};
   if (blockIdx.x < a.n_tiles) next = a.tiles[blockIdx.x];
@@ -259,15 +324,37 @@ __global__ void __launch_bounds__(kThreads, resident(BITS)) adamw_kernel(__grid_
   c.lr = a.d_lr ? *a.d_lr : a.lr, c.scale = a.grad_scale ? *a.grad_scale : 1.f;
   c.rate = c.lr / (float)(1.0 - s.b1t * a.b1d), c.inv_root = 1.f / sqrtf((float)(1.0 - s.b2t * a.b2d));
   c.key = mix(a.seed_lo ^ mix(a.seed_hi ^ mix((uint32_t)(s.steps + 1))));
+  extern __shared__ __align__(16) char dynamic[];
+  Stage *now = reinterpret_cast<Stage*>(dynamic), *later = now + 1;
+  Tile t{};
+  if (BITS == 8) {
+    t = next;
+    if (blockIdx.x < a.n_tiles) fetch_tile(a, t, lane, warp, now);
+    cp_async_commit();
+    if (blockIdx.x + gridDim.x < a.n_tiles) next = a.tiles[blockIdx.x + gridDim.x];
+  }
   for (uint32_t k = blockIdx.x; k < a.n_tiles; k += gridDim.x) {
-    const Tile t = next;
-    if (k + gridDim.x < a.n_tiles) next = a.tiles[k + gridDim.x];
-    const void* grads = a.grads[t.tensor - a.first_tensor];
-    if (!grads) continue;
-    if (t.copy)
-      update_tile<BITS, H, true>(a, t, grads, c, lane, warp);
-    else
-      update_tile<BITS, H, false>(a, t, grads, c, lane, warp);
+    Tile after{};
+    if (BITS == 8) {
+      if (k + gridDim.x < a.n_tiles) fetch_tile(a, next, lane, warp, later);
+      cp_async_commit();
+      if (k + 2 * (uint64_t)gridDim.x < a.n_tiles) after = a.tiles[k + 2 * gridDim.x];
+      cp_async_wait<1>();
+    } else {
+      t = next;
+      if (k + gridDim.x < a.n_tiles) next = a.tiles[k + gridDim.x];
+    }
+    if (const void* grads = a.grads[t.tensor - a.first_tensor]) {
+      if (t.copy)
+        update_tile<BITS, H, true>(a, t, grads, c, lane, warp, now);
+      else
+        update_tile<BITS, H, false>(a, t, grads, c, lane, warp, now);
+    }
+    if (BITS == 8) {
+      Stage* free = now;
+      now = later, later = free;
+      t = next, next = after;
+    }
   }
   if (!a.tick) return;
   // Every block has read the state before it counts itself here; the last one counts the step.
@@ -290,7 +377,7 @@ __global__ void __launch_bounds__(kThreads) moments_kernel(Moments from, int64_t
     mc[k] = uc[k] = make_uint2(0, 0), me[k] = ue[k] = 16;
     if (i >= values) continue;
     mc[k] = *reinterpret_cast<const uint2*>(from.mc + i), uc[k] = *reinterpret_cast<const uint2*>(from.uc + i);
-    me[k] = from.me[i / kBlock], ue[k] = from.ue[i / kBlock];
+    me[k] = from.e[i / kBlock] & 255u, ue[k] = from.e[i / kBlock] >> 8;
   }
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
@@ -336,7 +423,7 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const Tile* tiles, Momen
     hold<4, true>(y, ue, half, uc);
     put_codes(to.mc + at, false, lane, mc);
     put_codes(to.uc + at, false, lane, uc);
-    if (lane == 0) to.me[at / kBlock] = (uint8_t)me, to.ue[at / kBlock] = (uint8_t)ue;
+    if (lane == 0) to.e[at / kBlock] = me | ue << 8;
   }
 }
 __global__ void state_kernel(State* to, State s) { *to = s; }
@@ -374,7 +461,7 @@ Sizes measure(const esspt_adamw_config* c, const esspt_adamw_tensor* t) {
 }
 
 struct Carve {
-  size_t first, second, exp_first, exp_second, state, tiles, total;
+  size_t first, second, exponents, state, tiles, total;
 };
 
 Carve carve(const esspt_adamw_config& c, const Sizes& z) {
@@ -388,7 +475,7 @@ Carve carve(const esspt_adamw_config& c, const Sizes& z) {
   const size_t size = c.state_bits / 8;
   k.first = take(z.values * size, false);  // (v directly behind m)
   k.second = take(z.values * size);
-  if (c.state_bits == 8) k.exp_first = take(z.values / kBlock), k.exp_second = take(z.values / kBlock);
+  if (c.state_bits == 8) k.exponents = take(z.values / kBlock * sizeof(uint32_t));
   k.state = take(sizeof(State));
   k.tiles = take(z.tiles * sizeof(Tile));
   k.total = o;
@@ -409,11 +496,14 @@ struct esspt_adamw {
   Errors err;
 
   Moments moments() const {
-    if (cfg.state_bits == 32)
-      return Moments{reinterpret_cast<float*>(base + k.first), reinterpret_cast<float*>(base + k.second), nullptr, nullptr, nullptr,
-                     nullptr};
-    auto at = [this](size_t o) { return reinterpret_cast<uint8_t*>(base + o); };
-    return Moments{nullptr, nullptr, at(k.first), at(k.second), at(k.exp_first), at(k.exp_second)};
+    Moments h{};
+    if (cfg.state_bits == 32) {
+      h.m = reinterpret_cast<float*>(base + k.first), h.v = reinterpret_cast<float*>(base + k.second);
+    } else {
+      h.mc = reinterpret_cast<uint8_t*>(base + k.first), h.uc = reinterpret_cast<uint8_t*>(base + k.second);
+      h.e = reinterpret_cast<uint32_t*>(base + k.exponents);
+    }
+    return h;
   }
 };
 
@@ -445,11 +535,15 @@ esspt_status fill(esspt_adamw* aw, const esspt_adamw_tensor* tensors) {
 }
 
 template <int BITS>
-void launch(const esspt_adamw_config& c, unsigned blocks, cudaStream_t st, const Step& a) {
-  if (c.copy_dtype == ESSPT_BF16)
-    adamw_kernel<BITS, __nv_bfloat16><<<blocks, kThreads, 0, st>>>(a);
-  else
-    adamw_kernel<BITS, __half><<<blocks, kThreads, 0, st>>>(a);
+cudaError_t launch(const esspt_adamw_config& c, unsigned blocks, cudaStream_t st, const Step& a) {
+  auto* kernel = c.copy_dtype == ESSPT_BF16 ? adamw_kernel<BITS, __nv_bfloat16> : adamw_kernel<BITS, __half>;
+  const int shared = BITS == 8 ? 2 * sizeof(Stage) : 0;
+  if (shared > 0) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<blocks, kThreads, shared, st>>>(a);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -537,12 +631,8 @@ esspt_status esspt_adamw_step(esspt_adamw* aw, const void* const* h_grads, float
     a.tick = k + here == c.n_tensors;
     memcpy(a.grads, h_grads + k, here * sizeof(void*));
     if (a.n_tiles == 0 && !a.tick) continue;
-    const unsigned most = (unsigned)(resident(c.state_bits) * aw->sms), blocks = a.n_tiles == 0 ? 1 : a.n_tiles < most ? a.n_tiles : most;
-    if (c.state_bits == 32)
-      launch<32>(c, blocks, aw->st, a);
-    else
-      launch<8>(c, blocks, aw->st, a);
-    ESSPT_CUDA(aw->err, cudaGetLastError());
+    const unsigned most = (unsigned)(kResident * aw->sms), blocks = a.n_tiles == 0 ? 1 : a.n_tiles < most ? a.n_tiles : most;
+    ESSPT_CUDA(aw->err, c.state_bits == 32 ? launch<32>(c, blocks, aw->st, a) : launch<8>(c, blocks, aw->st, a));
   }
   return ESSPT_OK;
 }
