@@ -42,8 +42,8 @@ template <typename T, int VEC, int N>
 struct Incoming {
   using P = Pack<T, VEC, N>;
   static constexpr bool kAsync = sizeof(P) >= 4;
-  // (64 bytes a row for 512 threads, two such rows backward: 200 KB of three stages)
-  static constexpr int kDepth = sizeof(P) < 16 ? 2 : N * sizeof(P) < 64 ? 4 : 3;
+  // (64 bytes a row for 512 threads, two such rows backward: 200 KB of three stages; four are not faster)
+  static constexpr int kDepth = sizeof(P) < 16 ? 2 : 3;
   P *first, *read, *write;  // the thread's slot of the first stage, of the one to take from, of the one to fetch to
   int pitch;                // slots from one vector to the next
   int stage_read, stage_write;
