@@ -607,6 +607,9 @@ class SoftmaxHead:
         self._check(self._lib.esspt_softmax_poll(self._h))
 
 
+_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 class _Operator:
     """What the handles of the operators on rows share: where they run, errors, the end.
 
@@ -629,7 +632,7 @@ class _Operator:
         self.device = device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         self.dtype = dtype
-        self._stream_ptr = self.stream.cuda_stream
+        self._stream_ptr, self._index = self.stream.cuda_stream, self.device.index
 
     def _create(self, *config) -> None:
         """The workspace and the handle of a configuration (and what else its calls take)."""
@@ -648,8 +651,7 @@ class _Operator:
 
     def _call(self, call, *args) -> None:
         """One of the library's calls, in order with the current stream."""
-        index = self.device.index
-        if torch._C._cuda_getCurrentRawStream(index) == self._stream_ptr and torch._C._cuda_getDevice() == index:
+        if _current_stream(self._index) == self._stream_ptr and _current_device() == self._index:
             st = call(self._h, *args)  # the usual call
         else:
             current = torch.cuda.current_stream(self.device)
@@ -687,7 +689,7 @@ class _Operator:
         shape = x.shape
         if len(shape) != 2 or shape[1] != width or (n is not None and shape[0] != n):
             raise EssptError(EINVAL, f"{name} has shape {tuple(shape)}, not ({n if n is not None else 'n'}, {width})")
-        if (x.stride(1) != 1 and width > 1) or (shape[0] > 1 and x.stride(0) < width):
+        if not x.is_contiguous() and ((x.stride(1) != 1 and width > 1) or (shape[0] > 1 and x.stride(0) < width)):
             x = x.contiguous()
         return x
 
@@ -707,7 +709,7 @@ class _Operator:
 
 def _stride(x) -> int:
     """Values from one row to the next."""
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return x.stride(0) if x.shape[0] != 1 else x.shape[1]
 
 
 class Embedding(_Operator):
@@ -745,7 +747,10 @@ class Embedding(_Operator):
         ids = self._ids(ids)
         w = self._rows(w, self.n_rows, self.width, self.dtype, "w")
         n = ids.shape[0]
-        out = self._out(out, (n, self.width), self.dtype, "out")
+        if out is None:
+            out = torch.empty((n, self.width), dtype=self.dtype, device=self.device)
+        else:
+            out = self._out(out, (n, self.width), self.dtype, "out")
         self._call(self._lib.esspt_embed_lookup, w.data_ptr(), _stride(w), ids.data_ptr(), n, scale, out.data_ptr())
         return out
 
@@ -798,6 +803,7 @@ class LayerNorm(_Operator):
         if weight_dtype not in DTYPES:
             raise EssptError(EINVAL, f"weight_dtype must be {dtype} or torch.float32")
         self.max_rows, self.width, self.weight_dtype, self.eps, self.backwards = max_rows, width, weight_dtype, eps, backward
+        self._shape = (width,)
         self._create(ctypes.byref(NormConfig(max_rows, width, DTYPES[dtype], DTYPES[weight_dtype], int(backward), eps,
                                              ctypes.c_void_p(self._stream_ptr))))
 
@@ -806,16 +812,19 @@ class LayerNorm(_Operator):
             raise EssptError(EINVAL, f"{x.shape[0]} rows, more than max_rows = {self.max_rows}")
         return x.shape[0]
 
-    def _weights(self, x, name):
-        return None if x is None else self._values(x, (self.width,), self.weight_dtype, name)
-
     def forward(self, x, weight=None, bias=None, y=None) -> NormResult:
         """esspt_norm_forward: rows x (n, width), which may be strided; weight and bias
         (width,), or None for 1 and 0."""
         x = self._rows(x, None, self.width, self.dtype, "x")
         n = self._n(x)
-        weight, bias = self._weights(weight, "weight"), self._weights(bias, "bias")
-        y = self._out(y, (n, self.width), self.dtype, "y")
+        if weight is not None:
+            weight = self._values(weight, self._shape, self.weight_dtype, "weight")
+        if bias is not None:
+            bias = self._values(bias, self._shape, self.weight_dtype, "bias")
+        if y is None:
+            y = torch.empty((n, self.width), dtype=self.dtype, device=self.device)
+        else:
+            y = self._out(y, (n, self.width), self.dtype, "y")
         mean = torch.empty(n, dtype=torch.float32, device=self.device)
         rstd = torch.empty_like(mean)
         self._call(self._lib.esspt_norm_forward, x.data_ptr(), _stride(x), n, _ptr(weight), _ptr(bias), y.data_ptr(),
@@ -829,7 +838,8 @@ class LayerNorm(_Operator):
         n = self._n(x)
         dy = self._rows(dy, n, self.width, self.dtype, "dy")
         mean, rstd = self._values(mean, (n,), torch.float32, "mean"), self._values(rstd, (n,), torch.float32, "rstd")
-        weight = self._weights(weight, "weight")
+        if weight is not None:
+            weight = self._values(weight, self._shape, self.weight_dtype, "weight")
         grad_x = self._out(grad_x, (n, self.width), self.dtype, "grad_x") if need_x else None
         dw = db = None
         if need_weights:
@@ -930,7 +940,7 @@ class AdamW(_Operator):
         (esspt_adamw_moments)."""
         n = self.values
         if self.state_bits == 32:
-            if torch._C._cuda_getCurrentRawStream(self.device.index) != self._stream_ptr:
+            if _current_stream(self._index) != self._stream_ptr:
                 torch.cuda.current_stream(self.device).wait_stream(self.stream)
             return self._moments
         m, second = torch.empty((2, n), dtype=torch.bfloat16, device=self.device).unbind()
