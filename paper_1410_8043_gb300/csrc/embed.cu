@@ -41,7 +41,8 @@ struct Lookup {
 template <typename T, int VEC>
 constexpr int kDeep = VEC * sizeof(T) >= 16 ? 4 : 8;
 
-// A block takes kThreads * kDeep vectors of the result, one behind the other, whatever rows they are of.  PAIRS: rows of an
+// A block takes kThreads * kDeep vectors of the result, one behind the other, whatever rows they are of: memory is the bound
+// (262147 rows of 64 fp32 values out of a million: 16 us for 88 MB; 60000 of 1000: 69 us, 7 TB/s).  PAIRS: rows of an
 // odd number of 16-bit values, of which two of the result, from one row or two, make a word to write.  (60000 rows of 1001
 // bf16 values: 146 us value by value.)
 template <typename T, int VEC, bool PAIRS>
@@ -97,7 +98,8 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(Lookup a) {
 //
 // A block owns a range of the table's rows, of a tile of columns.  It reads all ids, keeps the tokens of its
 // rows, sorts them by row and place in shared memory, and sums them: a row's tokens by one group of lanes, or
-// by all groups in turn where there are more than kLong.
+// by all groups in turn where there are more than kLong.  One launch, no scratch memory; the block of the most popular row
+// bounds it (8195 tokens of 100 fp32 values, 740 of them one row's: 20 us; 97 tokens of 16: 4 us).
 struct Gradient {
   const int32_t* ids;
   const void* grad;
@@ -325,8 +327,8 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
 //
 // A pass over a digit of the rows: `count_kernel` counts a tile's tokens by digit, `scan_kernel` turns the
 // counts of a digit into places among its tokens, `move_kernel` moves the tokens there; equal digits keep
-// their order.  Padding has the key V, behind all rows.  While the sort's kernels wait for memory, further blocks of
-// them write the gradient's zeros.
+// their order.  Padding has the key V, behind all rows.  What bounds it are the kernels' own chains of loads and
+// exchanges in shared memory (a million tokens of 2^20 rows, two digits of ten bits: 4 + 6 + 14 us and 5 + 6 + 13).
 constexpr int kMostBits = 11, kMostBins = 1 << kMostBits;
 constexpr int kRound = 2048;     // tokens that a block moves at once, 256 a warp
 constexpr int kMostTiles = 1216;
@@ -558,7 +560,8 @@ __global__ void __launch_bounds__(kThreads) zero_kernel(char* to, int64_t bytes)
 // A group of lanes adds a chunk of sorted tokens.  Rows that begin and end among them are written; the sums of those
 // that do not are joined over the groups of a block, and what crosses blocks goes to `part`: [block][0] the sum of the
 // row that the block's first token shares with the block before, [block][1] of the row that goes on behind the block.
-// Rows without tokens have been set to zero beside the sort.
+// Rows without tokens have been set to zero beside the sort.  Every group has the same number of tokens, however popular
+// a row is; eight loads are under way (a million tokens of 64 fp32 values: 52 us, 230 MB read and 50 written).
 constexpr int kMostTokens = 2048;  // of a block
 
 template <typename T, int VEC, int K, bool ADD>

@@ -51,16 +51,6 @@ __device__ __forceinline__ void cp_async16_if(void* smem, const void* gmem, bool
                "l"(gmem), "r"((int)pred)
                : "memory");
 }
-// The same without a condition, 16 bytes past L1, 8 and 4 through it.
-__device__ __forceinline__ void cp_async16(void* smem, const void* gmem) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
-}
-__device__ __forceinline__ void cp_async8(void* smem, const void* gmem) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((unsigned)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
-}
-__device__ __forceinline__ void cp_async4(void* smem, const void* gmem) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((unsigned)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
-}
 // Streaming 32-bit load (read once per clock): skip L1, evict-first in L2.
 __device__ __forceinline__ int32_t ld_stream_i32(const int32_t* p, uint64_t pol) {
   int32_t r;
