@@ -419,7 +419,7 @@ const char* esspt_softmax_last_error(const esspt_softmax* sm);
  * fp32, rounded once.  An id < 0 is padding: its out row is zeros and its dout row is
  * not read.  An id >= V is treated as padding and reported as ESSPT_EINVAL by
  * esspt_embed_poll().  The sums go over the tokens sorted by id, then by place, in an
- * order that sizes alone decide: results do not depend on the order in which the GPU runs
+ * order that the ids alone decide: results do not depend on the order in which the GPU runs
  * its blocks. */
 typedef struct {
   int64_t max_tokens; /* most ids per call, 1..2^30 */
@@ -438,7 +438,8 @@ size_t esspt_embed_workspace_bytes(const esspt_embed_config* cfg);
 /* Create a handle over caller-allocated device workspace (256-byte aligned, kept until
  * esspt_embed_destroy(), not written by others).  A handle's calls share the workspace: they
  * run in its stream's order, and graphs that captured calls of one handle may not run at
- * the same time.  ESSPT_EINVAL on a bad config, ESSPT_ENOSPC on a short workspace. */
+ * the same time.  Large gradients are set to zero on a second stream of the handle, so that a call may be captured if
+ * the handle's stream is not the legacy default one.  ESSPT_EINVAL on a bad config, ESSPT_ENOSPC on a short workspace. */
 esspt_status esspt_embed_create(const esspt_embed_config* cfg, void* d_workspace, size_t bytes, esspt_embed** out);
 
 /* Release the host-side handle (not the workspace).  Synchronises the stream
@@ -462,8 +463,7 @@ esspt_status esspt_embed_gradient(esspt_embed* em, const int32_t* d_ids, const v
                                   int64_t n, float scale, int32_t accumulate, void* d_grad_w);
 
 /* Synchronise the stream and report, then clear, any error latched on the device
- * (ESSPT_EINVAL: an id >= V; ESSPT_ECUDA: a wait inside a kernel ran out, which is not
- * expected, and the results since the last poll are void). */
+ * (ESSPT_EINVAL: an id >= V). */
 esspt_status esspt_embed_poll(esspt_embed* em);
 
 /* Text of the last error on this handle ("" if none), valid until the next call

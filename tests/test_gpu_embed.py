@@ -210,6 +210,53 @@ def test_another_stream_and_a_graph(T):
     em.close()
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T, V, D", [(40, 30, 33), (40, 30, 64), (3001, 500, 7), (30_000, 700, 101), (30_000, 700, 16)])
+@pytest.mark.parametrize("shift", [1, 2, 4])
+def test_addresses_off_the_vectors(T, V, D, shift, dtype):
+    """Tables, gradients and results that begin anywhere in memory, and nothing written beside them."""
+    w, ids, grad = _inputs(T, V, D, dtype, 2 * (T + D))
+    em = _esspt().Embedding(T, V, D, dtype=TYPES[dtype])
+
+    def placed(x, rows, cols):
+        buf = torch.full((rows * cols + 16,), 7.0, dtype=TYPES[dtype], device="cuda")
+        view = buf[shift:shift + rows * cols].view(rows, cols)
+        if x is not None:
+            view.copy_(x)
+        return buf, view
+
+    _, w2 = placed(w, V, D)
+    _, grad2 = placed(grad, T, D)
+    rows, out = placed(None, T, D)
+    _check_lookup(em.lookup(w2, ids, scale=3.0, out=out), w, ids, 3.0, dtype)
+    table, total = placed(None, V, D)
+    _check_gradient(em.gradient(ids, grad2, grad_w=total), ids, grad, 1.0, dtype, V)
+    for buf, n in ((rows, T * D), (table, V * D)):
+        assert bool((buf[:shift] == 7).all()) and bool((buf[shift + n:] == 7).all())
+    em.close()
+
+
+def test_zeros_beside_the_sort_in_a_graph():
+    """A gradient large enough for the handle's second stream, captured, onto a table of NaN."""
+    T, V, D = 20_000, 300_000, 64
+    side = torch.cuda.Stream()
+    em = _esspt().Embedding(T, V, D, stream=side)
+    _, ids, grad = _inputs(T, V, D, "f32", 8)
+    out = torch.full((V, D), math.nan, device="cuda")
+    a, b = ids.clone(), grad.clone()
+    _check_gradient(em.gradient(ids, grad, grad_w=out), ids, grad, 1.0, "f32", V)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        em.gradient(a, b, grad_w=out)
+    for x, y in ((ids, grad), (ids.flip(0), grad.flip(0)), (ids, grad)):
+        a.copy_(x), b.copy_(y), out.fill_(math.nan)
+        graph.replay()
+        _check_gradient(out, x, y, 1.0, "f32", V)
+    torch.cuda.synchronize()
+    em.close()
+
+
 def test_refusals():
     e = _esspt()
     em = e.Embedding(8, 10, 4, backward=False)
