@@ -480,7 +480,8 @@ const char* esspt_embed_last_error(const esspt_embed* em);
  *     dw_d = sum_t dy_td x^_td,   db_d = sum_t dy_td
  * Rows are fp32, bf16 or fp16 (x, y, dy, dx alike); w, b and their gradients are fp32 or
  * of the rows' type; statistics and sums are fp32, the variance from differences to the
- * mean.  A row of equal values gives y = b.  NaN or infinity in a row makes that row NaN,
+ * mean (whose squares overflow past 2^63: x^ is 0 there).  A row of equal values gives y = b, to rounding.  NaN or
+ * infinity in a row makes that row NaN,
  * and in the backward pass the weights' gradients too.  Results do not depend on the order in
  * which the GPU runs its blocks. */
 typedef struct {
