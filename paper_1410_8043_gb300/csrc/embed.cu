@@ -121,6 +121,7 @@ constexpr int kFew = 16384;      // tokens that go this way at most
 constexpr int kFewThreads = 512;
 constexpr int kFewBlocks = 304;  // two for each of 152 SMs
 constexpr int kLong = 32;
+constexpr int kStarts = 2048;
 
 // A vector as it stands in memory (half the registers of fp32 values for 16-bit types): 16 bytes, or one value.
 template <typename T, int VEC>
@@ -220,10 +221,60 @@ __device__ __forceinline__ void add_rows(const Gradient& a, const int64_t (&plac
     for (int k = 0; k < K; ++k) add_raw<T, VEC>(x[u][k], sum[k]);
 }
 
+// Sorts up to two entries a thread, in a list with room for 4 * kFewThreads: by exchanges that get ever longer and back (bitonic), within
+// a warp by shuffles, between warps through two halves of the list in turn.  (519 entries: exchanges in the list alone took
+// 7 of the call's 20 us.)
+__device__ __forceinline__ void sort_in_registers(uint32_t* list, uint32_t m, uint32_t size) {
+  const uint32_t tid = threadIdx.x;
+  const bool two = size > kFewThreads, live = (tid & ~31u) < size;  // (other warps have nothing but sentinels)
+  uint32_t x = tid < m ? list[tid] : 0xffffffffu, y = kFewThreads + tid < m ? list[kFewThreads + tid] : 0xffffffffu;
+  uint32_t half = 2 * kFewThreads;  // (the entries were in the other one)
+  for (uint32_t run = 2; run <= size; run *= 2) {
+    const bool up_x = (tid & run) == 0, up_y = ((kFewThreads + tid) & run) == 0;
+    uint32_t dist = run / 2;
+    if (dist == kFewThreads) {  // (the last run's first)
+      const uint32_t low = min(x, y);
+      y = max(x, y), x = low;
+      dist /= 2;
+    }
+    for (; dist >= 32; dist /= 2) {
+      if (live) list[half + tid] = x;
+      if (two) list[half + kFewThreads + tid] = y;
+      __syncthreads();
+      const bool lower = (tid & dist) == 0;
+      if (live) {
+        const uint32_t other = list[half + (tid ^ dist)];
+        x = lower == up_x ? min(x, other) : max(x, other);
+      }
+      if (two) {
+        const uint32_t other = list[half + kFewThreads + (tid ^ dist)];
+        y = lower == up_y ? min(y, other) : max(y, other);
+      }
+      half ^= 2 * kFewThreads;
+    }
+    if (!live) continue;
+#pragma unroll
+    for (uint32_t d = 16; d > 0; d /= 2) {
+      if (d >= run) continue;
+      const bool lower = (tid & d) == 0;
+      const uint32_t ox = __shfl_xor_sync(0xffffffffu, x, d);
+      x = lower == up_x ? min(x, ox) : max(x, ox);
+      if (two) {
+        const uint32_t oy = __shfl_xor_sync(0xffffffffu, y, d);
+        y = lower == up_y ? min(y, oy) : max(y, oy);
+      }
+    }
+  }
+  __syncthreads();
+  if (tid < m) list[tid] = x;
+  if (kFewThreads + tid < m) list[kFewThreads + tid] = y;
+}
+
 template <typename T, int VEC, int K>
 __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
   extern __shared__ uint32_t list[];  // (row in the range, place) of the block's tokens
-  __shared__ uint32_t count, n_long, longs[kFew / kLong];
+  __shared__ uint32_t count, n_long, longs[kFew / kLong], warp_starts[kFewThreads / 32];
+  __shared__ uint16_t starts[kStarts];
   __shared__ float red[kFewThreads * K * VEC];
   constexpr int U = 8 / K;
   const int tid = threadIdx.x, lane = tid & (a.lanes - 1), group = tid / a.lanes, groups = kFewThreads / a.lanes;
@@ -231,16 +282,31 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
   const int64_t lo = (int64_t)blockIdx.x * a.rows, hi = lo + a.rows < a.V ? lo + a.rows : a.V;
   if (tid == 0) count = n_long = 0;
   __syncthreads();
-  for (int64_t i0 = tid; i0 < a.n; i0 += kFewThreads * 8) {
+  for (int base = 0; base < (int)a.n; base += kFewThreads * 8) {
+    const int i0 = base + tid;
     int32_t id[8];
+    uint32_t mine = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) id[k] = i0 + k * kFewThreads < a.n ? a.ids[i0 + k * kFewThreads] : -1;
+    for (int k = 0; k < 8; ++k) id[k] = i0 + k * kFewThreads < (int)a.n ? a.ids[i0 + k * kFewThreads] : -1;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       if (id[k] >= a.V && blockIdx.x == 0) atomicOr(a.status, kErrId);
-      if (id[k] >= lo && id[k] < hi)
-        list[atomicAdd(&count, 1u)] = (uint32_t)(id[k] - lo) << a.place_bits | (uint32_t)(i0 + k * kFewThreads);
+      mine += id[k] >= lo && id[k] < hi;
     }
+    if (!__any_sync(0xffffffffu, mine)) continue;
+    // One addition for a warp (a popular row's tokens would queue for the counter).
+    uint32_t at = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off *= 2) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, at, off);
+      if ((tid & 31) >= off) at += x;
+    }
+    uint32_t first = 0;
+    if ((tid & 31) == 31) first = atomicAdd(&count, at);
+    at += __shfl_sync(0xffffffffu, first, 31) - mine;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (id[k] >= lo && id[k] < hi) list[at++] = (uint32_t)(id[k] - lo) << a.place_bits | (uint32_t)(i0 + k * kFewThreads);
   }
   if (!a.accumulate)  // rows without tokens; the others are written again below
     if (lo + group < hi) write_zeros<T, VEC, K>(a, lo + group, (uint32_t)(hi - lo - group), c0, groups);
@@ -249,54 +315,79 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
   if (m == 0) return;
   uint32_t size = 2;
   while (size < m) size *= 2;
-  for (uint32_t i = m + tid; i < size; i += kFewThreads) list[i] = 0xffffffffu;
-  bool apart = true;  // whether the last exchanges went past a warp's own 64 entries
-  for (uint32_t run = 2; run <= size; run *= 2)
-    for (uint32_t dist = run / 2; dist > 0; dist /= 2) {
-      if (apart || dist > 32)
+  if (size <= 2 * kFewThreads) {
+    sort_in_registers(list, m, size);
+  } else {
+    for (uint32_t i = m + tid; i < size; i += kFewThreads) list[i] = 0xffffffffu;
+    for (uint32_t run = 2; run <= size; run *= 2)
+      for (uint32_t dist = run / 2; dist > 0; dist /= 2) {
         __syncthreads();
-      else
-        __syncwarp();
-      apart = dist > 32;
-      for (uint32_t t = tid; t < size / 2; t += kFewThreads) {
-        const uint32_t i = 2 * t - (t & (dist - 1)), j = i + dist;
-        const uint32_t x = list[i], y = list[j];
-        if ((x > y) == ((i & run) == 0)) list[i] = y, list[j] = x;
+        for (uint32_t t = tid; t < size / 2; t += kFewThreads) {
+          const uint32_t i = 2 * t - (t & (dist - 1)), j = i + dist;
+          const uint32_t x = list[i], y = list[j];
+          if ((x > y) == ((i & run) == 0)) list[i] = y, list[j] = x;
+        }
       }
-    }
+  }
   __syncthreads();
   const uint32_t place_mask = (1u << a.place_bits) - 1;
-  for (uint32_t i = group; i < m; i += groups) {
-    const uint32_t row = list[i] >> a.place_bits;
-    if (i > 0 && list[i - 1] >> a.place_bits == row) continue;
-    uint32_t end = i + 1;
-    while (end < m && end - i <= kLong && list[end] >> a.place_bits == row) ++end;
-    if (end - i > kLong) {
-      if (lane == 0) longs[atomicAdd(&n_long, 1u)] = i;
-      continue;
+  auto row_at = [&](uint32_t i) { return list[i] >> a.place_bits; };
+  auto segment = [&](uint32_t begin, uint32_t end) {  // a row's tokens
+    if (end - begin > kLong) {
+      if (lane == 0) longs[atomicAdd(&n_long, 1u)] = begin | end << 16;
+      return;
     }
+    const int64_t row = lo + row_at(begin);
     float sum[K][VEC] = {};
     Raw<T, VEC> old[K];
-    read_old<T, VEC, K>(a, lo + row, c0, old);
-    for (uint32_t at = i; at < end; at += U) {
+    read_old<T, VEC, K>(a, row, c0, old);
+    for (uint32_t at = begin; at < end; at += U) {
       int64_t place[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) place[u] = at + u < end ? (int64_t)(list[at + u] & place_mask) : -1;
       add_rows<T, VEC, K, U>(a, place, c0, sum);
     }
-    emit<T, VEC, K>(a, lo + row, c0, sum, old);
+    emit<T, VEC, K>(a, row, c0, sum, old);
+  };
+  // Where rows begin, in order, for the groups to take in turn; past kStarts entries they look for themselves.
+  if (m <= kStarts) {
+    uint32_t many = 0;
+    for (uint32_t base = 0; base < m; base += kFewThreads) {
+      const uint32_t t = base + tid;
+      const bool begins = t < m && (t == 0 || row_at(t) != row_at(t - 1));
+      const uint32_t some = __ballot_sync(0xffffffffu, begins);
+      if ((tid & 31) == 0) warp_starts[tid / 32] = __popc(some);
+      __syncthreads();
+      uint32_t before = many, all = 0;
+#pragma unroll
+      for (int w = 0; w < kFewThreads / 32; ++w) {
+        const uint32_t c = warp_starts[w];
+        before += w < tid / 32 ? c : 0;
+        all += c;
+      }
+      if (begins) starts[before + __popc(some & ((1u << (tid & 31)) - 1))] = (uint16_t)t;
+      many += all;
+      __syncthreads();
+    }
+    for (uint32_t k = group; k < many; k += groups) segment(starts[k], k + 1 < many ? starts[k + 1] : m);
+  } else {
+    for (uint32_t i = group; i < m; i += groups) {
+      const uint32_t row = row_at(i);
+      if (i > 0 && row_at(i - 1) == row) continue;
+      uint32_t end = i, left = m - i;
+      while (left > 0) {
+        const uint32_t half = left / 2;
+        if (row_at(end + half) <= row)
+          end += half + 1, left -= half + 1;
+        else
+          left = half;
+      }
+      segment(i, end);
+    }
   }
   __syncthreads();
   for (uint32_t k = 0; k < n_long; ++k) {
-    const uint32_t begin = longs[k], row = list[begin] >> a.place_bits;
-    uint32_t end = begin, left = m - begin;
-    while (left > 0) {
-      const uint32_t half = left / 2;
-      if (list[end + half] >> a.place_bits <= row)
-        end += half + 1, left -= half + 1;
-      else
-        left = half;
-    }
+    const uint32_t begin = longs[k] & 0xffffu, end = longs[k] >> 16, row = row_at(begin);
     float sum[K][VEC] = {};
     Raw<T, VEC> old[K];
     if (group == 0) read_old<T, VEC, K>(a, lo + row, c0, old);
@@ -863,7 +954,7 @@ cudaError_t launch_few(Gradient a, cudaStream_t st) {
   blocks = (a.V + a.rows - 1) / a.rows;
   a.place_bits = bits_of((uint32_t)a.n - 1);
   if (((uint64_t)a.rows << a.place_bits) > 0xffffffffull) return cudaErrorInvalidValue;  // (does_few says no)
-  uint32_t size = 2;
+  uint32_t size = 4 * kFewThreads;
   while (size < a.n) size *= 2;
   auto* kernel = few_kernel<T, VEC, K>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFew * sizeof(uint32_t));
