@@ -253,9 +253,8 @@ __device__ __forceinline__ void sort_in_registers(uint32_t* list, uint32_t m, ui
       half ^= 2 * kFewThreads;
     }
     if (!live) continue;
-#pragma unroll
-    for (uint32_t d = 16; d > 0; d /= 2) {
-      if (d >= run) continue;
+#pragma unroll 1
+    for (uint32_t d = run < 32 ? run / 2 : 16; d > 0; d /= 2) {  // (a loop: unrolled, its instructions take longer to come)
       const bool lower = (tid & d) == 0;
       const uint32_t ox = __shfl_xor_sync(0xffffffffu, x, d);
       x = lower == up_x ? min(x, ox) : max(x, ox);
