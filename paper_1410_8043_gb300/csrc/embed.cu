@@ -99,7 +99,8 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(Lookup a) {
 // A block owns a range of the table's rows, of a tile of columns.  It reads all ids, keeps the tokens of its
 // rows, sorts them by row and place in shared memory, and sums them: a row's tokens by one group of lanes, or
 // by all groups in turn where there are more than kLong.  One launch, no scratch memory; the block of the most popular row
-// bounds it (8195 tokens of 100 fp32 values, 740 of them one row's: 20 us; 97 tokens of 16: 4 us).
+// bounds it (8195 tokens of 100 fp32 values, some 500 of them one row's: 19 us, of which a quarter each are the ids, the sort and
+// that row's sum; 97 tokens of 16: 4 us).
 struct Gradient {
   const int32_t* ids;
   const void* grad;
@@ -222,8 +223,8 @@ __device__ __forceinline__ void add_rows(const Gradient& a, const int64_t (&plac
 }
 
 // Sorts up to two entries a thread, in a list with room for 4 * kFewThreads: by exchanges that get ever longer and back (bitonic), within
-// a warp by shuffles, between warps through two halves of the list in turn.  (519 entries: exchanges in the list alone took
-// 7 of the call's 20 us.)
+// a warp by shuffles, between warps through two halves of the list in turn.  (Exchanges in the list alone, with every warp at work for
+// every size: 23 us for 19 of a call of 8195 tokens.)
 __device__ __forceinline__ void sort_in_registers(uint32_t* list, uint32_t m, uint32_t size) {
   const uint32_t tid = threadIdx.x;
   const bool two = size > kFewThreads, live = (tid & ~31u) < size;  // (other warps have nothing but sentinels)
@@ -876,8 +877,9 @@ int lanes_of(int vectors) {
 
 // Whether a call of n tokens goes by one kernel: up to kAlwaysFew of them, or 3.5 MB of rows (a popular row's are added by one
 // SM), and a block's rows and a place fit 32 bits.  Measured in a graph, one kernel and by the sort, us: 4000 tokens, 5000
-// rows of 100 fp32 values 14.5 and 20.5, of 1000 21 and 25; 8000 of 100 values 20.6 and 20.6, of 257 25.6 and 23.3, of 1000
-// 33 and 29; 16000 of 16 values 25 and 22, of 100 37 and 22.  The sort's six or seven launches cost the host 20 us too.
+// rows of 100 fp32 values 11 and 20, of 1000 19 and 25; 8000 of 100 values 16 and 21, of 257 20 and 23, of 1000
+// 27 and 29 (500 rows: 16 and 16, 23 and 18, 27 and 21); 16000 of 16 values 25 and 22, of 100 30 and 22.  The sort's six or
+// seven launches cost the host 20 us too.
 constexpr int kAlwaysFew = 4096;
 bool does_few(int64_t n, int64_t V, int32_t D, size_t size) {
   if (n > kFew || (n > kAlwaysFew && n * D * (int64_t)size > 3'500'000)) return false;
