@@ -530,7 +530,8 @@ const char* esspt_norm_last_error(const esspt_norm* nm);
 /* One step over a list of fp32 tensors, t the number of the step:
  *     g = grad_scale grad,   m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2
  *     p = p (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
- * in fp32, m and v by products and sums rounded one by one in the order written.  A tensor may
+ * in fp32, m and v by products and sums rounded one by one in the order written; p less the sum of its decay and the
+ * step, so that an lr decay too small to change 1 counts too (an infinite p stays that).  A tensor may
  * have a 16-bit copy that a network runs on: it is rewritten from p, and the tensor's gradients are of
  * its type; without a copy gradients are fp32.
  *

@@ -199,7 +199,9 @@ template <int BITS, typename H, bool COPY, bool VECTOR>
 __device__ __forceinline__ void update(const Step& a, const Tile& t, const Rates& c, int lane, int i, int left, Values<BITS>& x) {
   const int64_t at = t.at + i;
   const uint32_t me = x.e & 255u, ue = x.e >> 8;
-  const float keep = 1.f - c.lr * t.decay;
+  // The decay's part is added to the step and taken off p with it: 1 - lr decay, rounded, would be the same for all values
+  // and steps, and have two bits of an lr decay of 2^-23 and none of one below 2^-25.
+  const float decay = c.lr * t.decay;
   // (a NaN block's codes count for nothing)
   const float b1 = BITS == 8 ? unless_nan(a.b1, me) : a.b1, b2 = BITS == 8 ? unless_nan(a.b2, ue) : a.b2;
   float u[4];
@@ -214,7 +216,9 @@ __device__ __forceinline__ void update(const Step& a, const Tile& t, const Rates
     x.m[j] = __fadd_rn(__fmul_rn(x.m[j], b1), __fmul_rn(gs, a.one_b1));
     x.v[j] = __fadd_rn(__fmul_rn(x.v[j], b2), __fmul_rn(__fmul_rn(gs, gs), a.one_b2));
     u[j] = BITS == 8 ? __fsqrt_rn(x.v[j]) : sqrt_fast(x.v[j]);
-    x.p[j] = fmaf(x.p[j], keep, -(c.rate * x.m[j]) * reciprocal_fast(fmaf(u[j], c.inv_root, a.eps)));
+    float step = c.rate * x.m[j] * reciprocal_fast(fmaf(u[j], c.inv_root, a.eps));
+    if (decay != 0.f && fabsf(x.p[j]) <= FLT_MAX) step = fmaf(decay, x.p[j], step);  // (an infinite p stays that)
+    x.p[j] -= step;
   }
   put4(t.p + i, VECTOR, lane, left, x.p);
   if (COPY) put4(static_cast<H*>(t.copy) + i, VECTOR, lane, left, x.p);

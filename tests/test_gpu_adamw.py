@@ -347,3 +347,44 @@ def test_refusals():
             call()
     assert opt.steps == 0 and bool((p == 0).all())
     opt.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr, decay", [(1e-5, 0.01), (2e-6, 0.01), (1e-3, 0.1)])
+def test_small_decay_adds_up(lr, decay, bits):
+    """lr decay near 2^-23 (1e-7) and below 2^-25 (2e-8), where 1 - lr decay has one bit of it, or none.
+
+    Two handles on the same gradients, with decay and without: their moments, and so their steps, have the same bits, and
+    the mean difference of the parameters grows each step by lr decay times the mean of those that decay.  Values in (1, 2)
+    lie 2^-23 apart; steps of many sizes (after the first, which is lr for all) round them either way, off by a sd of
+    2^-23 / sqrt(12) each, and in the first step all by half of 2^-23 at most.  So over T steps of N values the mean is off by
+    8 sd sqrt(2 T / N) + 2^-23; lr decay has two roundings, a step's sum one (2 + 1 eps of itself, taken as 8)."""
+    N, T = 1 << 20, 64
+    g = torch.Generator("cuda").manual_seed(7)
+    p = torch.rand(N, generator=g, device="cuda") * 0.5 + 1.25
+    q = p.clone()
+    with_, without = _esspt().AdamW([p], state_bits=bits, weight_decay=decay, seed=5), _esspt().AdamW([q], state_bits=bits, weight_decay=0.0, seed=5)
+    want = 0.0
+    for _ in range(T):
+        grad = torch.randn(N, generator=g, device="cuda") * 0.1
+        want += lr * decay * float(p.double().mean())
+        with_.step([grad], lr), without.step([grad], lr)
+    assert torch.equal(with_.moments().m, without.moments().m)
+    got = float((q.double() - p.double()).mean())
+    tol = 8 * 2.0**-23 / math.sqrt(12) * math.sqrt(2 * T / N) + 2.0**-23 + 8 * EPS * want
+    assert abs(got - want) <= tol, (got, want, tol)
+    with_.close(), without.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("decay", [0.0, 0.1])
+def test_parameters_that_are_no_numbers(bits, decay):
+    """An infinite parameter stays that (p (1 - lr decay) less a step), NaN stays NaN, and neither touches another."""
+    p = _tensors([(600,)], 3)[0]
+    p[5], p[200], p[599] = math.inf, -math.inf, math.nan
+    opt = _esspt().AdamW([p], state_bits=bits, weight_decay=decay)
+    for t in range(3):
+        opt.step(_tensors([(600,)], t), LR)
+    assert float(p[5]) == math.inf and float(p[200]) == -math.inf and math.isnan(float(p[599]))
+    assert int(torch.isfinite(p).sum()) == 597
+    opt.close()
