@@ -235,3 +235,110 @@ def test_refusals():
         with pytest.raises(e.EssptError):
             call()
     ln.close()
+
+
+# Sums over a row: up to 16 additions of a thread, 5 of a warp and 4 of warps, and a product: 26, taken as 32 eps.
+SUM = 32 * EPS
+
+
+def _check_far_rows(r, x, w, b, dtype, eps=1e-5):
+    """As _check_forward, where the mean may be far from zero.  The first mean is off by up to e1 = SUM mean|x|; differences d to
+    it are at most e1 + |x - mean|, off by eps of that.  Beyond 4 standard deviations the mean is corrected by theirs, which
+    is off by SUM of their greatest, so that x - mean is off by (SUM + 3 eps) times that in all (e), whatever the mean is; below, by e1
+    more, and the variance by e1^2.  The sum of squares about the first mean, less D times the correction's square, is off by 3 SUM + 6 eps of D
+    times the greatest d's square; 1 / sqrt by half of that, and 4 eps.  The mean that is given is one rounding more."""
+    x, w, b = x.double(), w.double(), b.double()
+    mean = x.mean(1, keepdim=True)
+    d = x - mean
+    var = d.square().mean(1, keepdim=True) + eps
+    rstd = 1 / var.sqrt()
+    e1 = SUM * x.abs().mean(1, keepdim=True)
+    top = d.abs().amax(1, keepdim=True) + e1
+    near = torch.where(mean.abs() * rstd < 4.01, e1, 0.0)
+    e = (SUM + 3 * EPS) * top + near
+    rel = (1.5 * SUM + 3 * EPS) * top.square() / var + (near * rstd).square() + 4 * EPS
+    assert bool(((r.mean.double()[:, None] - mean).abs() <= EPS * mean.abs() + e + TINY["f32"]).all())
+    assert bool(((r.rstd.double()[:, None] / rstd - 1).abs() <= rel).all())
+    xh = d * rstd
+    want = xh * w + b
+    tol = (e * rstd + (rel + 3 * EPS) * xh.abs()) * w.abs() * (1 + rel) + 2 * EPS * ((xh * w).abs() + b.abs())
+    tol = tol + HALF[dtype] * (1 + 1e-3) * want.abs() + TINY[dtype]
+    err = (r.y.double() - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+FAR = [1000.1, 4097.3, 20000.7, 65000.3, -1e5, 1e-5, 3e9]
+
+
+def _far(dtype):
+    x = torch.tensor(FAR, device="cuda")
+    return (x.clamp(-40_000, 40_000) if dtype == "f16" else x).to(TYPES[dtype])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("D", [1, 7, 33, 100, 500, 513, 1000, 1002, 2049, 8192])
+def test_equal_values_give_the_bias(D, dtype):
+    """Whatever the value is: the sum's and the mean's roundings are taken off again, where they count."""
+    x = _far(dtype)[:, None].expand(-1, D).contiguous()
+    _, _, w, b = _inputs(1, D, dtype, "f32", D)
+    ln = _esspt().LayerNorm(len(FAR), D, dtype=TYPES[dtype], weight_dtype=torch.float32)
+    r = ln.forward(x, w, b)
+    ln.close()
+    _check_far_rows(r, x, w, b, dtype)
+    # rstd is 1 / sqrt(eps) = 317 at most; |x^| SUM^2 |x| rstd, or SUM |x| rstd where that is below 4 SUM
+    size = x[:, :1].double().abs()
+    assert torch.equal(r.mean[size[:, 0] > 0.013], x[:, 0].float()[size[:, 0] > 0.013])
+    tol = torch.where(size < 0.013, SUM, SUM * SUM) * size * 317 * w.double().abs() + HALF[dtype] * 1.001 * b.double().abs() + TINY[dtype]
+    assert bool(((r.y.double() - b.double()).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("D", [2, 33, 100, 500, 513, 1000, 2049, 8192])
+def test_rows_near_one_value(D, dtype):
+    """Rows that vary by a few of their type's last places about a far mean; a part of a wide row far from the rest."""
+    g = torch.Generator("cuda").manual_seed(D)
+    far = _far(dtype)[:5].float()
+    place = torch.exp2(torch.floor(torch.log2(far.abs()))) * 2 * HALF[dtype]
+    x = far[:, None] + torch.randint(-2, 3, (5, D), generator=g, device="cuda") * place[:, None]
+    x = torch.cat([x, x, x])
+    x[5:10, :D // 3] *= -0.5
+    x[10:] += torch.randn((5, D), generator=g, device="cuda") * 0.01 * x[10:].abs()
+    x = x.to(TYPES[dtype])
+    _, _, w, b = _inputs(1, D, dtype, "f32", D)
+    ln = _esspt().LayerNorm(15, D, dtype=TYPES[dtype], weight_dtype=torch.float32)
+    r = ln.forward(x, w, b)
+    ln.close()
+    _check_far_rows(r, x, w, b, dtype)
+
+
+@pytest.mark.parametrize("D", [100, 500, 1000, 8192])
+def test_rows_whose_squares_overflow(D):
+    """x^ is 0 there and y the bias, with the mean corrected or not; infinity and NaN make the row NaN all the same."""
+    g = torch.Generator("cuda").manual_seed(D)
+    x = torch.randn((6, D), generator=g, device="cuda") * torch.tensor([1e20, 1e25, 1e30, 1e33, 1.0, 1.0], device="cuda")[:, None]
+    x[4], x[5] = -1e30, 1e30
+    x[4, 0] = -1.5e30
+    b = torch.randn(D, generator=g, device="cuda")
+    ln = _esspt().LayerNorm(6, D)
+    r = ln.forward(x, None, b)
+    assert torch.equal(r.y[:5], b.expand(5, D)) and bool((r.rstd[:5] == 0).all()) and bool(torch.isfinite(r.mean).all())
+    assert torch.equal(r.y[5], b)  # (equal values)
+    x[0, D - 1], x[1, 0], x[2, D // 2] = math.nan, math.inf, -math.inf
+    y = ln.forward(x, None, b).y
+    assert bool(torch.isnan(y[:3]).all()) and torch.equal(y[3:], r.y[3:])
+    ln.close()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("D", [3, 16, 33, 100, 500, 1001, 2048])
+def test_a_row_does_not_depend_on_its_neighbours(D, dtype):
+    """Rows far from zero beside others, in any order: the same bits."""
+    n = 200
+    x, _, w, b = _inputs(n, D, dtype, "f32", D)
+    x = (x.float() + 300.0 * (torch.rand((n, 1), device="cuda") < 0.3)).to(TYPES[dtype])
+    ln = _esspt().LayerNorm(n, D, dtype=TYPES[dtype], weight_dtype=torch.float32)
+    r = ln.forward(x, w, b)
+    order = torch.randperm(n, device="cuda")
+    s = ln.forward(x[order], w, b)
+    ln.close()
+    assert all(torch.equal(p[order], q) for p, q in zip(r, s))
