@@ -433,12 +433,16 @@ __global__ void __launch_bounds__(WIDE ? kMostWide : kThreads) norm_backward_ker
 template <bool BACK, typename T, int VEC, int N, bool WIDE>
 cudaError_t launch(const Spread& s, const Norm& a, unsigned blocks, cudaStream_t st) {
   using In = Incoming<T, VEC, N>;
-  const size_t row = In::kAsync ? (size_t)In::kDepth * N * s.threads * VEC * sizeof(T) : 0;
+  auto bytes = [](int threads, int D) {
+    const size_t rows = (size_t)(BACK ? 2 : 1) * (In::kAsync ? In::kDepth * N * threads * VEC * (int)sizeof(T) : 0), sums = 2 * D * sizeof(float);
+    return BACK && !WIDE && rows < sums ? sums : rows;
+  };
+  const size_t shared = bytes(s.threads, a.D);
   auto* kernel = BACK ? norm_backward_kernel<T, VEC, N, WIDE> : norm_forward_kernel<T, VEC, N, WIDE>;
-  size_t shared = BACK ? 2 * row : row;
-  if (BACK && !WIDE && shared < 2 * a.D * sizeof(float)) shared = 2 * a.D * sizeof(float);
   if (shared > 47 * 1024) {  // (static shared memory counts too)
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    // The limit is the kernel's, not this call's: always what its widest rows take, as another thread may be about to launch it.
+    const size_t most = bytes(WIDE ? kMostWide : kThreads, 32 * N * VEC);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
     if (e != cudaSuccess) return e;
   }
   kernel<<<blocks, s.threads, shared, st>>>(a);

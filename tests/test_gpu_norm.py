@@ -342,3 +342,38 @@ def test_a_row_does_not_depend_on_its_neighbours(D, dtype):
     s = ln.forward(x[order], w, b)
     ln.close()
     assert all(torch.equal(p[order], q) for p, q in zip(r, s))
+
+
+def test_two_widths_from_two_threads():
+    """Handles of one kind and several widths, whose rows take different amounts of shared memory, called at the same time.
+    The library's own calls, which other threads' run beside: with a limit of shared memory set for each call, one in thirty failed."""
+    import threading
+
+    e = _esspt()
+    call, failed, done = e.lib().esspt_norm_forward, [], []
+
+    def work(D):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                ln = e.LayerNorm(2, D, stream=stream)
+                x = torch.randn((2, D), device="cuda")
+                want = ln.forward(x).y
+                y = torch.zeros_like(x)
+                args = (ln._h, x.data_ptr(), D, 2, None, None, y.data_ptr(), None, None)
+                for _ in range(300):
+                    failed.extend(D for _ in range(50) if call(*args) != e.OK)
+                    stream.synchronize()
+                assert torch.equal(y, want)
+                ln.close()
+            done.append(D)
+        except Exception as err:  # noqa: BLE001
+            failed.append((D, err))
+
+    widths = (8192, 5000, 4800, 7000, 8192, 5000)
+    threads = [threading.Thread(target=work, args=(D,)) for D in widths]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed and len(done) == len(widths), failed[:10]
