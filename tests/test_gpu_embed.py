@@ -280,3 +280,81 @@ def test_refusals():
             call()
     assert torch.equal(em.lookup(w.T.contiguous().T + 1, ids), grad + 1)  # another layout is copied
     em.close()
+
+
+# -- sums that no order rounds ----------------------------------------------------
+
+
+def _whole(T, V, D, dtype, at, seed, stride=0):
+    """Gradients and a table of whole numbers up to 8, NaN at padding; what is to come out of them in fp64, half of the sums."""
+    g = torch.Generator("cuda").manual_seed(seed)
+    grad = torch.randint(-8, 9, (T, D + stride), generator=g, device="cuda").to(TYPES[dtype])[:, :D]
+    grad[at < 0] = math.nan
+    before = torch.randint(-8, 9, (V, D), generator=g, device="cuda").to(TYPES[dtype])
+    kept = at >= 0
+    sums = torch.zeros((V, D), dtype=torch.float64, device="cuda").index_add_(0, at[kept].long(), grad[kept].double())
+    return grad, before, 0.5 * sums
+
+
+def _check_whole(em, at, grad, before, want, dtype):
+    """Sums stay below 2^24 and are whole: fp32 holds them in any order, and the result is rounded once, to its type."""
+    assert float(want.abs().max()) < 2**22
+    t = TYPES[dtype]
+    assert torch.equal(em.gradient(at, grad, scale=0.5, grad_w=torch.full_like(before, math.nan)), want.float().to(t))
+    got = em.gradient(at, grad, scale=0.5, grad_w=before.clone(), accumulate=True)
+    assert torch.equal(got, (before.double() + want).float().to(t))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T, V, D", SHAPES + [(120_000, 1000, 9), (200_003, 40, 100), (250_000, 3, 64), (500_000, 300_000, 40)])
+def test_no_token_is_lost(T, V, D, dtype):
+    """Every shape with one popular row (up to half of the tokens), equal to the last bit: what bounds the kernels'
+    rounding grows with a row's tokens and would hide one that is left out or added twice."""
+    _, at, _ = _inputs(T, V, 1, dtype, T + V + D)
+    grad, before, want = _whole(T, V, D, dtype, at, T, stride=(0, 3, 8)[(T + D) % 3])
+    em = _esspt().Embedding(T, V, D, dtype=TYPES[dtype])
+    _check_whole(em, at, grad, before, want, dtype)
+    em.poll()
+    em.close()
+
+
+@pytest.mark.parametrize("ids", ["same", "two", "padding", "distinct", "sorted", "blocks", "last"])
+@pytest.mark.parametrize("T, V, D", [(3000, 4000, 20), (16_384, 16_384, 7), (30_000, 30_000, 64), (50_000, 60_000, 8), (130_000, 130_000, 33)])
+def test_no_token_is_lost_in_any_order(T, V, D, ids):
+    """Rows of all tokens (as many parts as there are blocks), runs that end at and beside the blocks' ends."""
+    g = torch.Generator().manual_seed(T)
+    at = {"same": torch.full((T,), 3), "two": torch.arange(T) % 2 * (V - 1), "padding": torch.full((T,), -1), "distinct": torch.randperm(V, generator=g)[:T],
+          "sorted": torch.arange(T) // 7, "blocks": (torch.arange(T) + 1) // 256 // 2,
+          "last": torch.where(torch.rand(T, generator=g) < 0.3, -1, V - 1)}[ids].to(torch.int32).cuda()
+    grad, before, want = _whole(T, V, D, "f32", at, T + 1)
+    em = _esspt().Embedding(T, V, D)
+    _check_whole(em, at, grad, before, want, "f32")
+    em.close()
+
+
+@pytest.mark.parametrize("T, V, D", [(40_000, 700, 64), (300_000, 2**20, 4), (1_000_003, 5000, 1), (2_500_000, 3000, 2), (17_000, 2**22 + 1, 16), (16_400, 9, 8192)])
+def test_nothing_behind_the_workspace_is_written(T, V, D):
+    """The library's handle on a part of a buffer, the bytes right behind the workspace kept in view, for as many tokens as
+    the handle takes and fewer."""
+    import ctypes
+
+    e = _esspt()
+    L = e.lib()
+    cfg = e.EmbedConfig(T, V, D, 0, 1, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    size = L.esspt_embed_workspace_bytes(ctypes.byref(cfg))
+    tail = 8 << 20
+    buf = torch.full((size + tail + 256,), 7, dtype=torch.uint8, device="cuda")
+    skip = -buf.data_ptr() % 256
+    h = ctypes.c_void_p()
+    assert L.esspt_embed_create(ctypes.byref(cfg), buf.data_ptr() + skip, size, ctypes.byref(h)) == e.OK
+    total = torch.empty((V, D), device="cuda")
+    for n in sorted({T, T - 1, T // 2, T * 3 // 4, T // 3 + 1, 16_385, 2049}):
+        at = torch.randint(-1, V, (n,), dtype=torch.int32, device="cuda")
+        grad = torch.ones((n, D), device="cuda")
+        for accumulate in (0, 1):
+            st = L.esspt_embed_gradient(h, at.data_ptr(), grad.data_ptr(), D, n, 1.0, accumulate, total.data_ptr())
+            assert st == e.OK, L.esspt_embed_last_error(h)
+        count = torch.bincount(at.long() + 1, minlength=V + 1)[1:]
+        assert torch.equal(total, (2 * count).float()[:, None].expand(V, D))
+        assert bool((buf[:skip] == 7).all()) and bool((buf[skip + size:] == 7).all())
+    assert L.esspt_embed_poll(h) == e.OK and L.esspt_embed_destroy(h) == e.OK

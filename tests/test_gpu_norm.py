@@ -377,3 +377,17 @@ def test_two_widths_from_two_threads():
     for t in threads:
         t.join()
     assert not failed and len(done) == len(widths), failed[:10]
+
+
+@pytest.mark.parametrize("n, D", [(60_001, 10), (20_001, 33), (4096, 100), (3001, 1000), (700, 2048), (330, 8192)])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_no_row_is_lost_from_the_sums(n, D, dtype):
+    """db of whole numbers: sums below 2^24, which no order rounds."""
+    g = torch.Generator("cuda").manual_seed(n)
+    x = torch.randn((n, D), generator=g, device="cuda").to(TYPES[dtype])
+    dy = torch.randint(-8, 9, (n, D), generator=g, device="cuda").to(TYPES[dtype])
+    ln = _esspt().LayerNorm(n, D, dtype=TYPES[dtype], weight_dtype=torch.float32)
+    r = ln.forward(x)
+    got = ln.backward(dy, x, r.mean, r.rstd).grad_bias
+    ln.close()
+    assert torch.equal(got.double(), dy.double().sum(0))
