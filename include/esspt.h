@@ -581,7 +581,7 @@ int64_t esspt_adamw_moment_values(const esspt_adamw_config* cfg, const esspt_ada
 size_t esspt_adamw_workspace_bytes(const esspt_adamw_config* cfg, const esspt_adamw_tensor* tensors);
 
 /* Create a handle with zero moments, before step 1.  `tensors` (host) is copied; the
- * tensors may not overlap.  The workspace is as of esspt_embed_create(); with 32 bits it begins with
+ * tensors and copies may not overlap (ESSPT_EINVAL).  The workspace is as of esspt_embed_create(); with 32 bits it begins with
  * m and then v, fp32 each, in flat order.  Synchronises the stream. */
 esspt_status esspt_adamw_create(const esspt_adamw_config* cfg, const esspt_adamw_tensor* tensors, void* d_workspace,
                                 size_t bytes, esspt_adamw** out);

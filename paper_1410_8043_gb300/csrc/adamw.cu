@@ -5,11 +5,13 @@
 // tile come first, and memory is the bound: 31 million values with 16-bit copies move 28 bytes each at 6.4 TB/s.  With 8 bits
 // the next tile is copied to shared memory meanwhile, and arithmetic is the bound, some 95 instructions a value: 192 million
 // values take 617 us at 16 bytes each, 5 TB/s.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
 #include <type_traits>
+#include <utility>
 #include <vector>
 
 #include "operator.h"
@@ -513,6 +515,22 @@ struct esspt_adamw {
 
 namespace {
 
+// Whether two tensors or copies share memory: their tiles would be written by two blocks at once.
+bool overlap(const esspt_adamw_config& c, const esspt_adamw_tensor* tensors) {
+  std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+  for (int k = 0; k < c.n_tensors; ++k) {
+    const esspt_adamw_tensor& t = tensors[k];
+    if (t.count == 0) continue;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(t.d_param), copy = reinterpret_cast<uintptr_t>(t.d_copy);
+    spans.push_back({p, p + t.count * sizeof(float)});
+    if (copy) spans.push_back({copy, copy + t.count * 2});
+  }
+  std::sort(spans.begin(), spans.end());
+  for (size_t k = 1; k < spans.size(); ++k)
+    if (spans[k].first < spans[k - 1].second) return true;
+  return false;
+}
+
 esspt_status fill(esspt_adamw* aw, const esspt_adamw_tensor* tensors) {
   const esspt_adamw_config& c = aw->cfg;
   std::vector<Tile> tiles;
@@ -573,6 +591,11 @@ esspt_status esspt_adamw_create(const esspt_adamw_config* cfg, const esspt_adamw
     if (tensors[k].count > 0 && !tensors[k].d_param) return g_create.fail(ESSPT_EINVAL, "null pointer");
     if (misaligned(tensors[k].d_param, 4) || misaligned(tensors[k].d_copy, 2))
       return g_create.fail(ESSPT_EINVAL, "a pointer is not aligned to its type");
+  }
+  try {
+    if (overlap(*cfg, tensors)) return g_create.fail(ESSPT_EINVAL, "two tensors overlap");
+  } catch (const std::bad_alloc&) {
+    return g_create.fail(ESSPT_ENOSPC, "out of host memory");
   }
   if (!out || !d_workspace || misaligned(d_workspace, 256)) return g_create.fail(ESSPT_EINVAL, "null or misaligned pointer");
   if (bytes < carve(*cfg, z).total) return g_create.fail(ESSPT_ENOSPC, "workspace too small");

@@ -388,3 +388,17 @@ def test_parameters_that_are_no_numbers(bits, decay):
     assert float(p[5]) == math.inf and float(p[200]) == -math.inf and math.isnan(float(p[599]))
     assert int(torch.isfinite(p).sum()) == 597
     opt.close()
+
+
+def test_the_same_tensor_twice():
+    """Refused; neighbours in one buffer are not."""
+    e = _esspt()
+    buf = torch.zeros(1000, device="cuda")
+    for params in ([buf, buf], [buf[:300], buf[299:]], [buf, buf[500:501]]):
+        with pytest.raises(e.EssptError) as err:
+            e.AdamW(params)
+        assert err.value.status == e.EINVAL
+    opt = e.AdamW([buf[300:], buf[:300], buf[:0]], weight_decay=0.0)
+    opt.step([torch.ones(700, device="cuda"), torch.ones(300, device="cuda"), buf[:0]], LR)
+    assert float((buf + LR).abs().max()) <= 1e-7
+    opt.close()

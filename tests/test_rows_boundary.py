@@ -128,3 +128,20 @@ def test_no_gpu_means_no_handles():
         esspt.LayerNorm(4, 8)
     with pytest.raises(RuntimeError):
         esspt.AdamW([torch.zeros(4)])
+
+
+@pytest.mark.parametrize("tensors, wrong", [
+    ([(4096, 0, 100), (4096, 0, 100)], True), ([(4096, 0, 100), (4492, 0, 10)], True), ([(4492, 0, 10), (4096, 0, 100)], True),
+    ([(4096, 4400, 100)], True), ([(4096, 8192, 100), (8392, 0, 5), (8388, 0, 0)], False), ([(4096, 8192, 100), (8388, 0, 5)], True),
+    ([(4096, 8192, 100), (16384, 8390, 3)], True), ([(4096, 0, 100), (4496, 0, 10)], False), ([(0, 0, 0), (0, 0, 0), (4096, 0, 1)], False),
+    ([(4096, 0, 0), (4096, 0, 7)], False)])
+def test_adamw_refuses_tensors_that_overlap(L, tensors, wrong):
+    """The same parameter twice, or parts of it: blocks would write it at the same time.  Empty ones are nowhere."""
+    from paper_1410_8043_gb300 import esspt
+
+    recs = (esspt.AdamWTensor * len(tensors))(*[esspt.AdamWTensor(p or None, c or None, n, 0.0) for p, c, n in tensors])
+    cfg = esspt.AdamWConfig(len(tensors), 32, 1, 0, 0.9, 0.999, 1e-8, 0, None)
+    need, h = L.esspt_adamw_workspace_bytes(ctypes.byref(cfg), recs), ctypes.c_void_p()
+    # (one byte too few where nothing overlaps: refused for that, and nothing is made of these addresses)
+    st = L.esspt_adamw_create(ctypes.byref(cfg), recs, ctypes.c_void_p(1 << 30), ctypes.c_size_t(need if wrong else need - 1), ctypes.byref(h))
+    assert (st == esspt.EINVAL and b"overlap" in L.esspt_adamw_last_error(None)) if wrong else st == esspt.ENOSPC
