@@ -665,9 +665,15 @@ class _Operator:
         if st != OK:
             self._check(st)
 
+    def _wait(self, call, *args) -> None:
+        """One of the library's calls that wait for the stream: of the default stream, the handle's device's."""
+        with torch.cuda.device(self.device):
+            self._check(call(self._h, *args))
+
     def close(self) -> None:
         if getattr(self, "_h", None):
-            getattr(self._lib, f"esspt_{self._name}_destroy")(self._h)
+            with torch.cuda.device(self.device):
+                getattr(self._lib, f"esspt_{self._name}_destroy")(self._h)
             self._h = None
 
     def __del__(self):
@@ -769,7 +775,7 @@ class Embedding(_Operator):
 
     def poll(self) -> None:
         """esspt_embed_poll: synchronise and raise on an id outside the table."""
-        self._check(self._lib.esspt_embed_poll(self._h))
+        self._wait(self._lib.esspt_embed_poll)
 
 
 class NormResult(NamedTuple):
@@ -960,5 +966,5 @@ class AdamW(_Operator):
     def steps(self) -> int:
         """esspt_adamw_steps: steps taken so far (synchronises)."""
         n = ctypes.c_int64()
-        self._check(self._lib.esspt_adamw_steps(self._h, ctypes.byref(n)))
+        self._wait(self._lib.esspt_adamw_steps, ctypes.byref(n))
         return n.value

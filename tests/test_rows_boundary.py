@@ -145,3 +145,33 @@ def test_adamw_refuses_tensors_that_overlap(L, tensors, wrong):
     # (one byte too few where nothing overlaps: refused for that, and nothing is made of these addresses)
     st = L.esspt_adamw_create(ctypes.byref(cfg), recs, ctypes.c_void_p(1 << 30), ctypes.c_size_t(need if wrong else need - 1), ctypes.byref(h))
     assert (st == esspt.EINVAL and b"overlap" in L.esspt_adamw_last_error(None)) if wrong else st == esspt.ENOSPC
+
+
+def test_waits_are_for_the_handles_device(monkeypatch):
+    """Polls, step counts and the end are called with the handle's device current: its default stream is that device's."""
+    from paper_1410_8043_gb300 import esspt
+
+    current, seen = ["cuda:0"], []
+
+    class Device:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            current.append(self.device)
+
+        def __exit__(self, *exc):
+            current.pop()
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: seen.append((name, current[-1])) or 0
+
+    monkeypatch.setattr(esspt.torch.cuda, "device", Device)
+    em, aw = esspt.Embedding.__new__(esspt.Embedding), esspt.AdamW.__new__(esspt.AdamW)
+    for handle in (em, aw):
+        handle._lib, handle._h, handle.device = Library(), 1, "cuda:1"
+    em.poll()
+    assert aw.steps == 0
+    em.close(), aw.close(), aw.close()
+    assert seen == [(f"esspt_{name}", "cuda:1") for name in ("embed_poll", "adamw_steps", "embed_destroy", "adamw_destroy")]
