@@ -480,7 +480,7 @@ const char* esspt_embed_last_error(const esspt_embed* em);
  *     dw_d = sum_t dy_td x^_td,   db_d = sum_t dy_td
  * Rows are fp32, bf16 or fp16 (x, y, dy, dx alike); w, b and their gradients are fp32 or
  * of the rows' type; statistics and sums are fp32, the variance from differences to the
- * mean (whose squares overflow past 2^63: x^ is 0 there).  Where the mean is more than 4 standard deviations (of
+ * mean (whose squares overflow past 2^63: x^ is 0 there).  Where the mean is more than 8 standard deviations (of
  * variance + eps) from zero it is corrected by the mean of those differences, so that rows of
  * nearly equal values keep theirs, and a row of equal values gives y = b, to rounding.  The mean that is given is
  * rounded to fp32, and the backward pass takes it as it is: its x^ is off by up to 2^-24 |mean| rstd.  NaN or

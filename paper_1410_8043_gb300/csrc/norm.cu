@@ -1,9 +1,5 @@
-// Layer norm, forward and backward: kernels and C-ABI.
-//
-// A group of lanes (a part of a warp, a warp, or for wide rows a block) holds a row in registers, N vectors of
-// VEC values a lane, so that a row is read once.  Groups stay and go through rows: their weights stay in registers, and
-// each thread's parts of the next rows are copied to its own places in shared memory meanwhile.  All arithmetic is fp32,
-// two values an instruction.
+// Layer norm, forward and backward: the C-ABI, and the kernel that adds the blocks' sums for the weights.  The others are in
+// norm.cuh.
 #include <cmath>
 #include <new>
 #include <type_traits>

@@ -6,9 +6,9 @@
 // two values an instruction.
 //
 // Memory is the bound for rows of 16-byte vectors, with issue close behind for 16-bit ones (32771 rows of 2048 bf16 values:
-// forward 50 us, 5.4 TB/s, issue 67% of the time; backward 65 us, 6.2 TB/s, and 14 us for the weights' sums; fp32: 94 and
-// 129 us, 5.7 and 6.2 TB/s).  Sixteen values a thread halve what eight pay in sums over a row.  Rows of an odd number of 16-bit values
-// go by single ones: 77 and 143 us for 2047 values.
+// forward 47 us, 5.7 TB/s, issue 67% of the time; backward 65 us, 6.2 TB/s, and 14 us for the weights' sums; fp32: 93 and
+// 129 us, 5.8 and 6.2 TB/s).  Sixteen values a thread halve what eight pay in sums over a row.  Rows of an odd number of 16-bit values
+// go by single ones: 82 and 143 us for 2047 values.
 #pragma once
 
 #include <cfloat>
@@ -28,13 +28,13 @@ constexpr int kThreads = kNormThreads, kMostWide = kNormWide, kMostWarps = kMost
 template <int VEC, int N>
 constexpr int kPairs = (VEC * N + 1) / 2;
 
-template <typename T, int VEC, int N>
+template <typename T, int VEC>
 struct alignas(VEC * sizeof(T)) Pack {
   T v[VEC];
 };
 
 template <typename T, int VEC, int N>
-__device__ __forceinline__ void to_pairs(const Pack<T, VEC, N> (&p)[N], u64 (&x)[kPairs<VEC, N>]) {
+__device__ __forceinline__ void to_pairs(const Pack<T, VEC> (&p)[N], u64 (&x)[kPairs<VEC, N>]) {
 #pragma unroll
   for (int q = 0; q < kPairs<VEC, N>; ++q) {
     const int e = 2 * q, f = e + 1;
@@ -46,7 +46,7 @@ __device__ __forceinline__ void to_pairs(const Pack<T, VEC, N> (&p)[N], u64 (&x)
 // stay in registers, a row ahead.  What lies outside a row or the rows is zero.
 template <typename T, int VEC, int N>
 struct Incoming {
-  using P = Pack<T, VEC, N>;
+  using P = Pack<T, VEC>;
   static constexpr bool kAsync = sizeof(P) >= 4;
   // (64 bytes a row for 512 threads, two such rows backward: 200 KB of three stages; four are not faster)
   static constexpr int kDepth = sizeof(P) < 16 ? 2 : 3;
@@ -172,18 +172,17 @@ __device__ __forceinline__ void store_pairs(T* row, int D, int lane, int lanes, 
 // The mean is a rounded sum times a rounded 1 / D, off by some 10 units of its last place.  In rows that vary by little more than
 // that, all differences to it are off, and the variance by that error's square.  Rows whose mean is more than kFar standard
 // deviations (of variance + eps) from zero are corrected: the differences have no such error, and their own mean says how far
-// the first one was off.  It is done once a row is written, from its copy in shared memory, so that it costs other rows nothing
-// (where all rows had it in line, 32771 of 2048 bf16 values took 65 us for 54, 20000 of 8192 181 for 144; now, if all are far,
-// 95 and 267).  In others the error is at most some 10 kFar units of x^.
-constexpr float kFar = 4.f;
+// the first one was off.  In others x^ is off by some 10 kFar units at most.  It is done once a row is written, from its copy in
+// shared memory, for other rows' registers and speed: in line for all of them it took 10 to 25% more of the pass; now 32771 rows of
+// 2048 bf16 values take 47 us, and 87 if all are far, 20000 of 8192 136 and 257.  Asking takes 3 to 7% of rows of up to 256 values.
+constexpr float kFar = 8.f;
 
 // What such rows take, in loops, for few registers.  `from`: a thread's first vector of the row, in shared memory where it was
 // copied, `step` values to its next one.
 template <typename T, int VEC>
 __device__ __forceinline__ float2 far_sums(const T* from, int step, int c, int lanes, int D, float mean) {
   float2 sums = make_float2(0.f, 0.f);  // of differences to `mean`, and their squares
-  constexpr int kUnroll = VEC == 1 ? 4 : 1;
-#pragma unroll kUnroll
+#pragma unroll 1
   for (; c < D; c += lanes * VEC, from += step) {
     float v[VEC];
     load_vec<T, VEC>(from, v);
@@ -276,8 +275,8 @@ __global__ void __launch_bounds__(WIDE ? (VEC >= 4 ? 768 : kMostWide) : kThreads
       mean = warps_sum(__fmul_rn(count_other, v.x), warps) * a.inv_D;
       m2 = warps_sum(v.y + count_other * (v.x - mean) * (v.x - mean), warps);
     }
-    const float var = m2 * a.inv_D + a.eps, rstd = rsqrtf(var);
-    const bool far = mean * mean > kFar * kFar * var;  // (not where squares overflow or are NaN)
+    const float rstd = rsqrtf(m2 * a.inv_D + a.eps);
+    const bool far = fabsf(mean) * rstd > kFar;  // (not where squares overflow or are NaN)
     if ((WIDE || t < a.n) && (In::kAsync || !far)) {
       const u64 m = pack2(-mean, -mean), r = pack2(rstd, rstd);
 #pragma unroll
@@ -309,7 +308,7 @@ __global__ void __launch_bounds__(WIDE ? (VEC >= 4 ? 768 : kMostWide) : kThreads
       for (int q = 0; q < Q; ++q) x[q] = fma2(mul2(add2(add2(x[q], m), m_far), r), w[q], b[q]);
       store_pairs<T, VEC, N>(row, a.D, lane, lanes, x);
     } else {
-#pragma unroll 4
+#pragma unroll 1
       for (int c = lane; c < a.D; c += lanes, from += pitch)
         row[c] = from_float<T>(fmaf((to_float(*from) - mean - rest) * rstd_far, weight_at<T>(a, a.weight, 1.f, c), weight_at<T>(a, a.bias, 0.f, c)));
     }

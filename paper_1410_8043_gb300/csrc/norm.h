@@ -42,8 +42,8 @@ inline Spread spread(int D, int vec, bool back) {
     s.threads = s.lanes = ((vectors + most - 1) / most + 31) / 32 * 32;
     s.wide = true;
   }
-  // by registers: up to 64 with eight values; with 16 up to 80 (vectors of four or eight, forward), 128.  (60000 rows of 500
-  // bf16 values, in pairs, forward: 36 us, with 768 threads 41.)
+  // by registers: up to 64 with eight values; with 16 up to 80 (vectors of four or eight, forward), 128.  (60000 rows of 1002
+  // bf16 values, in pairs, forward: 57 us, with 768 threads 68.)
   s.resident = (s.n * vec <= 8 ? 1024 : vec >= 4 && !back ? 768 : 512) / s.threads;
   return s;
 }
