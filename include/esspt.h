@@ -419,8 +419,8 @@ const char* esspt_softmax_last_error(const esspt_softmax* sm);
  * fp32, rounded once.  An id < 0 is padding: its out row is zeros and its dout row is
  * not read.  An id >= V is treated as padding and reported as ESSPT_EINVAL by
  * esspt_embed_poll().  The sums go over the tokens sorted by id, then by place, in an
- * order that the ids alone decide: results do not depend on the order in which the GPU runs
- * its blocks. */
+ * order that the call decides (its ids and sizes, and the alignment of its addresses and strides): the
+ * same call gives the same bits, and results do not depend on the order in which the GPU runs its blocks. */
 typedef struct {
   int64_t max_tokens; /* most ids per call, 1..2^30 */
   int64_t n_rows;     /* V: rows of W, 1..2^30 */
@@ -544,8 +544,10 @@ const char* esspt_norm_last_error(const esspt_norm* nm);
  * code 8 e + j (and the sign, 128) or 16 e + j, codes 0 and 128 of m being zero; E is the least, from -111 on, that the block's
  * largest value needs.  The step itself takes the moments before they are held so.  A value x
  * between two that lie d apart is held as d floor(x / d + rho), rho = r / 2^16, so that
- * moving averages move by less than a step of the format in the mean (rounded to the nearest, an
- * average of 0.999 would stand still: its changes are a tenth of a percent, half a step 3 to 6).  Below the
+ * m and u move by less than a step of the format in the mean (rounded to the nearest, an
+ * average of 0.999 would stand still: its changes are a tenth of a percent, half a step 3 to 6).  v = u^2 then lies above its
+ * mean by the rounding's variance at every step: with b2 = 0.999 and random gradients it settles 2 to 3% above the one
+ * in 32 bits, and steps come out some 1% shorter.  Below the
  * least code, m is held as it or as 0 by the same rule, and u, which divides, as it.  r is the high (m) or low (u)
  * half of h(i, t), a hash of the value's place i in the flat order, the step and the seed, with
  *     mix(x): x ^= x >> 16, x *= 0x5851F42D, x ^= x >> 15, x *= 0x2545F491, x ^= x >> 16
@@ -591,7 +593,8 @@ esspt_status esspt_adamw_create(const esspt_adamw_config* cfg, const esspt_adamw
 esspt_status esspt_adamw_destroy(esspt_adamw* aw);
 
 /* One step.  h_grads: host array of n_tensors device pointers, read before the call returns;
- * a NULL leaves its tensor, copy and moments as they are.  lr: the step size, finite;
+ * a NULL leaves its tensor, copy and moments as they are, but the step counts for all: the tensor's next one is corrected
+ * (1 - b^t) as if it had had a gradient in every step.  lr: the step size, finite;
  * d_lr, if not NULL, a device fp32 that is read instead when the step runs.  d_grad_scale: a
  * device fp32 that multiplies gradients (a clipping factor, a loss scale's inverse), or NULL for 1.  The number
  * of the step is counted on the device, so that a step captured in a CUDA graph counts at every replay.

@@ -3,8 +3,8 @@
 // The tensors are cut into tiles of 4096 values.  Blocks stay and go through tiles, the next one's record under way;
 // a warp takes 512 values of a tile, four blocks of 128, four values a thread of each.  With 32-bit moments all loads of a
 // tile come first, and memory is the bound: 31 million values with 16-bit copies move 28 bytes each at 6.4 TB/s.  With 8 bits
-// the next tile is copied to shared memory meanwhile, and arithmetic is the bound, some 95 instructions a value: 192 million
-// values take 617 us at 16 bytes each, 5 TB/s.
+// the next tile is copied to shared memory meanwhile, and arithmetic is the bound, some 99 instructions a value: 192 million
+// values take 621 us at 16 bytes each, 4.9 TB/s.
 #include <algorithm>
 #include <cfloat>
 #include <cmath>

@@ -41,10 +41,11 @@ struct Lookup {
 template <typename T, int VEC>
 constexpr int kDeep = VEC * sizeof(T) >= 16 ? 4 : 8;
 
-// A block takes kThreads * kDeep vectors of the result, one behind the other, whatever rows they are of: memory is the bound
-// (262147 rows of 64 fp32 values out of a million: 16 us for 88 MB; 60000 of 1000: 69 us, 7 TB/s).  PAIRS: rows of an
-// odd number of 16-bit values, of which two of the result, from one row or two, make a word to write.  (60000 rows of 1001
-// bf16 values: 146 us value by value.)
+// A block takes kThreads * kDeep vectors of the result, one behind the other, whatever rows they are of.  Memory is the bound of
+// wide rows (60000 of 1000 fp32 values: 69 us, 7 TB/s), latency and issue of short ones: 262147 rows of 64 out of a million take
+// 16 us for 88 MB, with DRAM at 22% and issue at 57%, and a thread asks for an id only when the one before it is there.  PAIRS: rows
+// of an odd number of 16-bit values, of which two of the result, from one row or two, make a word to write.  (60000 rows of
+// 1001 bf16 values: 146 us value by value.)
 template <typename T, int VEC, bool PAIRS>
 __global__ void __launch_bounds__(kThreads) lookup_kernel(Lookup a) {
   constexpr int kMany = kDeep<T, VEC>, kEach = PAIRS ? 2 : VEC;
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(Gradient a) {
 // A pass over a digit of the rows: `count_kernel` counts a tile's tokens by digit, `scan_kernel` turns the
 // counts of a digit into places among its tokens, `move_kernel` moves the tokens there; equal digits keep
 // their order.  Padding has the key V, behind all rows.  What bounds it are the kernels' own chains of loads and
-// exchanges in shared memory (a million tokens of 2^20 rows, two digits of ten bits: 4 + 6 + 14 us and 5 + 6 + 13).
+// exchanges in shared memory (a million tokens of a million rows, two digits of ten bits: 4 + 6 + 14 us and 5 + 6 + 13).
 constexpr int kMostBits = 11, kMostBins = 1 << kMostBits;
 constexpr int kRound = 2048;     // tokens that a block moves at once, 256 a warp
 constexpr int kMostTiles = 1216;
@@ -878,8 +879,9 @@ int lanes_of(int vectors) {
 // Whether a call of n tokens goes by one kernel: up to kAlwaysFew of them, or 3.5 MB of rows (a popular row's are added by one
 // SM), and a block's rows and a place fit 32 bits.  Measured in a graph, one kernel and by the sort, us: 4000 tokens, 5000
 // rows of 100 fp32 values 11 and 20, of 1000 19 and 25; 8000 of 100 values 16 and 21, of 257 20 and 23, of 1000
-// 27 and 29 (500 rows: 16 and 16, 23 and 18, 27 and 21); 16000 of 16 values 25 and 22, of 100 30 and 22.  The sort's six or
-// seven launches cost the host 20 us too.
+// 27 and 29 (500 rows: 16 and 16, 23 and 18, 27 and 21); 16000 of 16 values 25 and 22, of 100 30 and 22.  So the table's
+// rows count too, and the rule, which leaves them out, is up to 3 us off in a graph; the sort's six or seven launches cost
+// the host of an eager call 20 us.
 constexpr int kAlwaysFew = 4096;
 bool does_few(int64_t n, int64_t V, int32_t D, size_t size) {
   if (n > kFew || (n > kAlwaysFew && n * D * (int64_t)size > 3'500'000)) return false;

@@ -71,7 +71,10 @@ __device__ __forceinline__ void red_add_v4(float4* p, float4 v) { atomicAdd(p, v
 
 // One float4 slice as two packed fp32 pairs, the operands of the packed fp32
 // instructions (sm_100 and later): two IEEE fp32 operations per instruction,
-// each rounded as its scalar form.
+// rounded as their scalar forms, but that the assembler fuses a product and the
+// sum it goes to, rounded once, in spite of the .rn (a million random a b + c:
+// all as fma, a fifth unlike two roundings).  Where both roundings are meant,
+// the scalar intrinsics keep them.
 typedef unsigned long long u64;
 struct f2x2 {
   u64 lo, hi;
