@@ -866,7 +866,7 @@ class Moments(NamedTuple):
 class AdamW(_Operator):
     """AdamW steps over many fp32 tensors at once (one `esspt_adamw` handle).
 
-    `params` are updated in place; where `copies` has a 16-bit tensor, it is rewritten
+    `params` are updated in place and may not share memory; where `copies` has a 16-bit tensor, it is rewritten
     from its parameter and the parameter's gradients are of its type.  `weight_decay`:
     one for all, or one each.  With `state_bits` 8 moments are held in 8 bits, rounded up or down by a hash of
     `seed`, the step and the value's place.  The handle keeps references to the tensors.
